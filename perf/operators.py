@@ -206,9 +206,8 @@ def _plain(st):
     g, u = _values(*_quantize(g, mode)), _values(*_quantize(u, mode))  # as the checkpoints keep them
     dh = _values(*_quantize(st["dy"], mode)) @ wd
     a, da = _act(g, case["act"])
-    d = torch.stack([dh * u * da, dh * a])
-    dv = _values(*_quantize(d, mode))
-    db = d.to(torch.bfloat16).float()  # the gradients of g and u are handed on in bf16
+    db = torch.stack([dh * u * da, dh * a]).to(torch.bfloat16).float()  # the gradients of g and u are bf16 tensors
+    dv = _values(*_quantize(db, mode))
     return {"y": y, "dx": (dv[0] @ w[0] + dv[1] @ w[1]).to(out), "dwgu": (db.transpose(1, 2) @ xv).to(out),
             "dwd": (st["dy"].float().T @ h).to(out)}
 
@@ -297,7 +296,7 @@ def exact(case, seed):
     g, u = fp8(g)[2], fp8(u)[2]
     dh = fp8(st["dy"])[2] @ wd
     a, slope = value_and_slope(g)
-    dg, du = dh * u * slope, dh * a
+    dg, du = [d.to(torch.float32).to(torch.bfloat16) for d in (dh * u * slope, dh * a)]  # bf16 tensors by definition
     dx = fp8(dg)[2] @ wg + fp8(du)[2] @ wu
-    as_kept = [d.to(torch.float32).to(torch.bfloat16).to(D) for d in (dg, du)]
-    return {"y": y, "dx": dx, "dwgu": torch.stack([d.T @ xv for d in as_kept]), "dwd": st["dy"].to(D).T @ h}
+    dwgu = torch.stack([dg.to(D).T @ xv, du.to(D).T @ xv])
+    return {"y": y, "dx": dx, "dwgu": dwgu, "dwd": st["dy"].to(D).T @ h}
