@@ -329,6 +329,101 @@ int zq_w4a8_linear_noalloc(const uint8_t* q, const float* sx, int64_t M, int64_t
                            zq_out_dtype ydt, int64_t ldy, void* stream);
 int zq_w4a8_linear_noalloc_status(int* detail, void* stream);
 
+/*
+ * ---- FP8 with block scales -------------------------------------------------------------------------
+ * (Not operators of the paper.  Models are also published, and fine-tuned, with E4M3 codes on both sides and one FP32
+ * scale per block of 128; these entry points serve them next to the token-wise scheme above.)
+ *
+ * A quantized tensor is its E4M3 codes, dense and row-major, and the FP32 scales of its blocks; the value is
+ * code * scale.  Activations: blocks of one row x 128 features, scale[kb, m] with the ROW INDEX INNERMOST
+ * ([ceil(K/128), M]).  Weights: blocks of 128 x 128, scale[nb, kb] ([ceil(N/128), ceil(K/128)]).  The last blocks
+ * may be ragged.  Scale of a block whose absolute maximum is a:
+ *   a == 0: 1 ; a not finite (an infinity or NaN in the block): NaN, and the block stands for NaN ; otherwise
+ *   ZQ_SCALE_NONE: s = max(fl32(a / 448), 2^-126)
+ *   ZQ_SCALE_M1  : that, rounded up to a power of two (as M1 does for weight groups)
+ *   code = RNE_E4M3(fl32(x * fl32(1 / s))), saturating at +-448.
+ * ZQ_SCALE_M2 is refused (ZQ_ERR_MODE).  K (features) is a multiple of 16 throughout; codes are 16-byte aligned.
+ */
+
+/*
+ * x : bf16 [M, ldx], 16-byte aligned, ldx >= K, ldx % 8 == 0;  q : out, E4M3 [M, K];  s : out, FP32 [ceil(K/128), M].
+ * This is also how an activation is kept as an 8-bit checkpoint (1.03 bytes per element instead of 2); with
+ * ZQ_SCALE_M1 every code * scale is a bf16 number, so that reading it back rounds nothing.  M == 0 is a no-op.
+ */
+int zq_quantize_fp8_block(const void* x_bf16, int64_t M, int64_t K, int64_t ldx, zq_scale_mode mode, uint8_t* q,
+                          float* s, void* stream);
+/* W : FP32 [N, K] dense, 16-byte aligned;  q : out, E4M3 [N, K];  s : out, FP32 [ceil(N/128), ceil(K/128)]. */
+int zq_quantize_weight_fp8_block(const float* W, int64_t N, int64_t K, zq_scale_mode mode, uint8_t* q, float* s,
+                                 void* stream);
+/* Codes [N, K] and scales of a weight -> codes [K, N] and scales of its transpose, what the gradient with respect to
+ * the layer's input multiplies by (laid out once per weight).  N % 16 == 0. */
+int zq_transpose_weight_fp8_block(const uint8_t* q, const float* s, int64_t N, int64_t K, uint8_t* qt, float* st,
+                                  void* stream);
+
+/* Workspace of the entry points below for M rows of K features (256-byte aligned, zeroed once with
+ * zq_workspace_init; a workspace for M rows serves fewer; its status words are read with zq_device_status).  Calls
+ * that are given codes, and zq_fp8_weight_grad, need zq_fp8_block_workspace_bytes(0, 16) only.  0: refused sizes. */
+size_t zq_fp8_block_workspace_bytes(int64_t M, int64_t K);
+
+/*
+ * Linear layer:  y[m, n] = sum_p sum_k x^[p, m, k] w^[p, n, k].
+ * parts : 1, or 2 for a sum over two pairs of operands (the input gradient of two projections of the same input)
+ * q, s  : activations [parts][M, K] and their scales [parts][ceil(K/128), M]; or x_bf16 [M, ldx] (parts == 1,
+ *         q = s = NULL), which the call quantizes with `mode`
+ * w, ws : weights [parts][N, K] and scales [parts][ceil(N/128), ceil(K/128)]
+ * y     : out [M, ldy], FP32 or bf16 (ydt), element-aligned, ldy >= N; any N
+ * The products of a block are summed by the tensor core, scaled and summed over the blocks in FP32; results do not
+ * vary from run to run.  M == 0 or N == 0 is a no-op.
+ */
+int zq_fp8_block_linear(const uint8_t* q, const float* s, const void* x_bf16, int64_t ldx, zq_scale_mode mode,
+                        int parts, int64_t M, int64_t N, int64_t K, const uint8_t* w, const float* ws, void* y,
+                        zq_out_dtype ydt, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Activations of the gated feed-forward block: v / (1 + exp(-v)); v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2;
+ * max(v, 0) */
+typedef enum { ZQ_ACT_SILU = 0, ZQ_ACT_GELU_TANH = 1, ZQ_ACT_RELU = 2 } zq_activation;
+
+/*
+ * Gated linear layer, the first half of the gated feed-forward block (gate and up projection, activation and
+ * product in one kernel):  g = x^ Wg^T, u = x^ Wu^T,  h = act(g) u.
+ * w, ws   : [2][F, K] codes (gate, up) and [2][ceil(F/128), ceil(K/128)] scales;  F % 16 == 0
+ * h_bf16  : out [M, ldh] or NULL;  hq, hs : out, h quantized with `mode` ([M, F], [ceil(F/128), M]) or NULL: what
+ *           the down projection takes as q, s.  h is not rounded before it is quantized.  At least one of the two.
+ * gu, gus : out or NULL: g and u quantized with `mode`, [2][M, F] and [2][ceil(F/128), M], kept for the backward pass
+ * Activations, mode, workspace as zq_fp8_block_linear.
+ */
+int zq_fp8_gated_linear(const uint8_t* q, const float* s, const void* x_bf16, int64_t ldx, zq_scale_mode mode,
+                        int64_t M, int64_t F, int64_t K, const uint8_t* w, const float* ws, zq_activation act,
+                        void* h_bf16, int64_t ldh, uint8_t* hq, float* hs, uint8_t* gu, float* gus, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/*
+ * Its backward pass, from the gradient dy of the block's output y = h^ Wd^T (quantizers are passed straight through):
+ *   dh = dy^ Wd ;  du = bf16(dh act(g^)) ;  dg = bf16(dh u^ act'(g^)) ;  and both quantized with `mode`.
+ * q, s    : dy quantized, [M, K] and [ceil(K/128), M]; or dy_bf16 [M, lddy]
+ * wt, wts : the down projection's weight transposed (zq_transpose_weight_fp8_block): [F, K]
+ * gu, gus : what zq_fp8_gated_linear kept
+ * dgu_bf16: out, bf16 [2][M, F] (dg, du);  dguq, dgus : out, the same quantized, [2][M, F] and [2][ceil(F/128), M]
+ * Then dx = zq_fp8_block_linear(parts = 2) of (dguq, dgus) with the transposed gate and up weights, and
+ * dW = zq_fp8_weight_grad of dgu_bf16 and the checkpoint of x.
+ */
+int zq_fp8_gated_linear_backward(const uint8_t* q, const float* s, const void* dy_bf16, int64_t lddy,
+                                 zq_scale_mode mode, int64_t M, int64_t F, int64_t K, const uint8_t* wt,
+                                 const float* wts, zq_activation act, const uint8_t* gu, const float* gus,
+                                 void* dgu_bf16, uint8_t* dguq, float* dgus, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
+/*
+ * Weight gradient from an 8-bit activation checkpoint:  dW[p][n, k] = sum_m G[p][m, n] bf16(code[m, k] s[k/128, m])
+ * (the rounding to bf16 is none with power-of-two scales), summed in FP32.
+ * G    : bf16, parts (1 .. 64) matrices [M, ldg], g_stride elements apart; ldg >= N; ldg and g_stride multiples of 8
+ * q, s : the checkpoint, [M, K] and [ceil(K/128), M]
+ * dw   : out, [parts][N, K] dense, FP32 or bf16, 16-byte aligned; any N.  M == 0 gives zeros.
+ */
+int zq_fp8_weight_grad(const void* g_bf16, int64_t ldg, int64_t g_stride, int parts, const uint8_t* q, const float* s,
+                       int64_t M, int64_t N, int64_t K, void* dw, zq_out_dtype dwdt, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
 /* Number of kernels of this library launched by the calling process so far (all entry points). */
 int64_t zq_launch_count(void);
 

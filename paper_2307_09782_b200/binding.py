@@ -28,7 +28,12 @@ EXPORTS = [
     "zq_w4a8_linear_host_workspace_bytes", "zq_w4a8_linear_host", "zq_device_status", "zq_launch_count",
     "zq_w4a8_linear_noalloc_max_scratch_bytes", "zq_w4a8_linear_noalloc", "zq_w4a8_linear_noalloc_status", "zq_w4a8_linear_plan", "zq_selftest_bounded_wait", "zq_lorc_workspace_bytes", "zq_lorc_factors",
     "zq_w4a8_linear_fused_out", "zq_quantize_act_fp8_scaled", "zq_set_exclusive_device",
+    "zq_quantize_fp8_block", "zq_quantize_weight_fp8_block", "zq_transpose_weight_fp8_block",
+    "zq_fp8_block_workspace_bytes", "zq_fp8_block_linear", "zq_fp8_gated_linear", "zq_fp8_gated_linear_backward",
+    "zq_fp8_weight_grad",
 ]
+ACT_SILU, ACT_GELU_TANH, ACT_RELU = 0, 1, 2
+ACTIVATIONS = {"silu": ACT_SILU, "gelu_tanh": ACT_GELU_TANH, "relu": ACT_RELU}
 PLAN_FIELDS = ("bm", "m_tiles", "n_tiles", "ctas", "stream", "persist", "splits", "kb_per_split", "base", "rem",
                "tail_pos0", "m_group", "partial_floats", "sms", "pair")
 
@@ -93,6 +98,24 @@ def lib() -> C.CDLL:
         L.zq_quantize_act_fp8_scaled.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, ci, vp, vp]
         L.zq_set_exclusive_device.restype = ci
         L.zq_set_exclusive_device.argtypes = [ci]
+        L.zq_quantize_fp8_block.restype = ci
+        L.zq_quantize_fp8_block.argtypes = [vp, i64, i64, i64, ci, vp, vp, vp]
+        L.zq_quantize_weight_fp8_block.restype = ci
+        L.zq_quantize_weight_fp8_block.argtypes = [vp, i64, i64, ci, vp, vp, vp]
+        L.zq_transpose_weight_fp8_block.restype = ci
+        L.zq_transpose_weight_fp8_block.argtypes = [vp, vp, i64, i64, vp, vp, vp]
+        L.zq_fp8_block_workspace_bytes.restype = sz
+        L.zq_fp8_block_workspace_bytes.argtypes = [i64, i64]
+        L.zq_fp8_block_linear.restype = ci
+        L.zq_fp8_block_linear.argtypes = [vp, vp, vp, i64, ci, ci, i64, i64, i64, vp, vp, vp, ci, i64, vp, sz, vp]
+        L.zq_fp8_gated_linear.restype = ci
+        L.zq_fp8_gated_linear.argtypes = [vp, vp, vp, i64, ci, i64, i64, i64, vp, vp, ci, vp, i64, vp, vp, vp, vp, vp, sz,
+                                          vp]
+        L.zq_fp8_gated_linear_backward.restype = ci
+        L.zq_fp8_gated_linear_backward.argtypes = [vp, vp, vp, i64, ci, i64, i64, i64, vp, vp, ci, vp, vp, vp, vp, vp, vp,
+                                                   sz, vp]
+        L.zq_fp8_weight_grad.restype = ci
+        L.zq_fp8_weight_grad.argtypes = [vp, i64, i64, ci, vp, vp, i64, i64, i64, vp, ci, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -312,3 +335,213 @@ def device_status(workspace: torch.Tensor):
     d = C.c_int(0)
     st = lib().zq_device_status(_ptr(workspace), C.byref(d), _stream())
     return int(st), int(d.value)
+
+
+# ---- FP8 with block scales --------------------------------------------------------------------------
+
+@dataclass
+class Fp8Block:
+    """Activations as E4M3 codes with one scale per row and 128 features (``zq_quantize_fp8_block``)."""
+    codes: torch.Tensor   # uint8 [M, K] (or [parts, M, K])
+    scale: torch.Tensor   # float32 [ceil(K / 128), M] (or [parts, ...]): the row index is innermost
+
+    def values(self) -> torch.Tensor:
+        """The FP32 values the codes stand for (a convenience for inspection, not a hot path)."""
+        K = self.codes.shape[-1]
+        s = self.scale.transpose(-1, -2).repeat_interleave(128, -1)[..., :K]
+        return self.codes.view(torch.float8_e4m3fn).float() * s
+
+
+@dataclass
+class Fp8Weight:
+    """Weights as E4M3 codes with one scale per 128 x 128 block (``zq_quantize_weight_fp8_block``); ``parts`` = 2 for the
+    stacked gate and up projections."""
+    codes: torch.Tensor   # uint8 [N, K] or [parts, N, K]
+    scale: torch.Tensor   # float32 [ceil(N / 128), ceil(K / 128)] or [parts, ...]
+    N: int
+    K: int
+    parts: int = 1
+
+    def __post_init__(self):
+        lead = (self.parts,) if self.parts > 1 else ()
+        nb, kb = (self.N + 127) // 128, (self.K + 127) // 128
+        if tuple(self.codes.shape) != (*lead, self.N, self.K) or tuple(self.scale.shape) != (*lead, nb, kb):
+            raise ValueError(f"codes {tuple(self.codes.shape)} / scales {tuple(self.scale.shape)} do not belong to "
+                             f"{self.parts} x [{self.N}, {self.K}]")
+        _expect(self.codes, torch.uint8, "codes")
+        _expect(self.scale, torch.float32, "scale")
+
+    def values(self) -> torch.Tensor:
+        s = self.scale.repeat_interleave(128, -1)[..., :self.K].repeat_interleave(128, -2)[..., :self.N, :]
+        return self.codes.view(torch.float8_e4m3fn).float() * s
+
+
+def _expect(t: torch.Tensor, dtype, name: str):
+    if t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor is needed, got {t.dtype}, strides {t.stride()}")
+
+
+def _rows(x: torch.Tensor, name: str) -> int:
+    """The row stride of a bf16 matrix whose rows are contiguous."""
+    if x.dtype != torch.bfloat16 or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError(f"{name}: a bf16 matrix with contiguous rows is needed, got {x.dtype} {tuple(x.shape)}, "
+                         f"strides {x.stride()}")
+    return x.stride(0) if x.shape[0] > 1 else max(x.shape[1], (x.shape[1] + 7) // 8 * 8)
+
+
+def fp8_block_linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    """Workspace for :func:`fp8_block_linear` and the gated layers on M rows of K features (N does not matter)."""
+    return int(lib().zq_fp8_block_workspace_bytes(M, K))
+
+
+def _blocks(n: int) -> int:
+    return (n + 127) // 128
+
+
+def quantize_fp8_block(x: torch.Tensor, mode="none") -> Fp8Block:
+    """x: bf16 [M, K] (row stride allowed); ``mode`` "none" (FP32 scales) or "M1" (powers of two)."""
+    ldx = _rows(x, "x")
+    M, K = x.shape
+    q = torch.empty((M, K), dtype=torch.uint8, device=x.device)
+    s = torch.empty((_blocks(K), M), dtype=torch.float32, device=x.device)
+    _check(lib().zq_quantize_fp8_block(_ptr(x), M, K, ldx, _mode(mode), _ptr(q), _ptr(s), _stream()),
+           "zq_quantize_fp8_block")
+    return Fp8Block(q, s)
+
+
+def quantize_weight_fp8_block(W: torch.Tensor, mode="none") -> Fp8Weight:
+    """W: float32 [N, K] or [parts, N, K], contiguous."""
+    _expect(W, torch.float32, "W")
+    parts = W.shape[0] if W.dim() == 3 else 1
+    N, K = W.shape[-2:]
+    lead = W.shape[:-2] if parts > 1 else ()
+    q = torch.empty((*lead, N, K), dtype=torch.uint8, device=W.device)
+    s = torch.empty((*lead, _blocks(N), _blocks(K)), dtype=torch.float32, device=W.device)
+    for i in range(parts):
+        Wi, qi, si = (W.view(parts, N, K)[i], q.view(parts, N, K)[i], s.view(parts, _blocks(N), _blocks(K))[i])
+        _check(lib().zq_quantize_weight_fp8_block(_ptr(Wi), N, K, _mode(mode), _ptr(qi), _ptr(si), _stream()),
+               "zq_quantize_weight_fp8_block")
+    return Fp8Weight(q, s, N, K, parts)
+
+
+def transpose_fp8_weight(w: Fp8Weight) -> Fp8Weight:
+    """The transposed weight (of each part): [N, K] -> [K, N]."""
+    lead = (w.parts,) if w.parts > 1 else ()
+    nb, kb = _blocks(w.N), _blocks(w.K)
+    q = torch.empty((*lead, w.K, w.N), dtype=torch.uint8, device=w.codes.device)
+    s = torch.empty((*lead, kb, nb), dtype=torch.float32, device=w.codes.device)
+    for i in range(w.parts):
+        _check(lib().zq_transpose_weight_fp8_block(
+            _ptr(w.codes.view(w.parts, w.N, w.K)[i]), _ptr(w.scale.view(w.parts, nb, kb)[i]), w.N, w.K,
+            _ptr(q.view(w.parts, w.K, w.N)[i]), _ptr(s.view(w.parts, kb, nb)[i]), _stream()),
+            "zq_transpose_weight_fp8_block")
+    return Fp8Weight(q, s, w.K, w.N, w.parts)
+
+
+def _activations(x, q, K: int, parts: int):
+    """(codes, scales, x, ldx, M) of an operand given raw (``x``) or quantized (``q``)."""
+    if (x is None) == (q is None):
+        raise ValueError("give the activations either raw (x) or quantized (q)")
+    if x is not None:
+        ldx = _rows(x, "x")
+        if x.shape[1] != K:
+            raise ValueError(f"x has {x.shape[1]} features, the weight {K}")
+        return None, None, x, ldx, x.shape[0]
+    _expect(q.codes, torch.uint8, "q.codes")
+    _expect(q.scale, torch.float32, "q.scale")
+    M = q.codes.shape[-2]
+    lead = (parts,) if parts > 1 else ()
+    if tuple(q.codes.shape) != (*lead, M, K) or tuple(q.scale.shape) != (*lead, _blocks(K), M):
+        raise ValueError(f"codes {tuple(q.codes.shape)} / scales {tuple(q.scale.shape)} do not fit {parts} x [M, {K}]")
+    return q.codes, q.scale, None, K, M
+
+
+def _fp8_workspace(workspace, M: int, K: int, device):
+    return make_workspace(lib().zq_fp8_block_workspace_bytes(M, K), device) if workspace is None else workspace
+
+
+def fp8_block_linear(w: Fp8Weight, *, x=None, q: Optional[Fp8Block] = None, mode="none", out_dtype=torch.float32, y=None,
+                     workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y [M, N] = the linear layer; activations raw (bf16 ``x``, quantized with ``mode``) or quantized (``q``).  With
+    ``w.parts`` = 2 the sum over two pairs of operands (``q`` then holds two as well)."""
+    codes, scale, x, ldx, M = _activations(x, q, w.K, w.parts)
+    if y is None:
+        y = torch.empty((M, w.N), dtype=out_dtype, device=w.codes.device)
+    elif y.shape != (M, w.N) or y.dtype not in (torch.float32, torch.bfloat16) or (w.N > 1 and y.stride(1) != 1):
+        raise ValueError(f"y: a float32 or bf16 [{M}, {w.N}] matrix with contiguous rows is needed")
+    ydt = OUT_F32 if y.dtype == torch.float32 else OUT_BF16
+    workspace = _fp8_workspace(workspace, M, w.K, w.codes.device)
+    _check(lib().zq_fp8_block_linear(_ptr(codes), _ptr(scale), _ptr(x), ldx, _mode(mode), w.parts, M, w.N, w.K,
+                                     _ptr(w.codes), _ptr(w.scale), _ptr(y), ydt, y.stride(0) if M > 1 else w.N,
+                                     _ptr(workspace), workspace.numel(), _stream()), "zq_fp8_block_linear")
+    return y
+
+
+def _act(act) -> int:
+    return ACTIVATIONS[act] if isinstance(act, str) else int(act)
+
+
+def fp8_gated_linear(w: Fp8Weight, *, x=None, q: Optional[Fp8Block] = None, act="silu", mode="none", bf16=True,
+                     quantized=False, checkpoint=False, workspace: Optional[torch.Tensor] = None):
+    """h = act(x Wg^T) * (x Wu^T) with ``w`` the stacked (gate, up) weights.  Returns (h bf16 [M, F] | None,
+    h quantized | None, g and u quantized ([2, M, F]) | None) as asked for by ``bf16``, ``quantized``, ``checkpoint``."""
+    if w.parts != 2:
+        raise ValueError("the gated layer takes the stacked (gate, up) weights: parts = 2")
+    codes, scale, x, ldx, M = _activations(x, q, w.K, 1)
+    F, dev, fb = w.N, w.codes.device, _blocks(w.N)
+    h = torch.empty((M, F), dtype=torch.bfloat16, device=dev) if bf16 else None
+    hq = gu = None
+    if quantized:
+        hq = Fp8Block(torch.empty((M, F), dtype=torch.uint8, device=dev),
+                      torch.empty((fb, M), dtype=torch.float32, device=dev))
+    if checkpoint:
+        gu = Fp8Block(torch.empty((2, M, F), dtype=torch.uint8, device=dev),
+                      torch.empty((2, fb, M), dtype=torch.float32, device=dev))
+    workspace = _fp8_workspace(workspace, M, w.K, dev)
+    _check(lib().zq_fp8_gated_linear(_ptr(codes), _ptr(scale), _ptr(x), ldx, _mode(mode), M, F, w.K, _ptr(w.codes),
+                                     _ptr(w.scale), _act(act), _ptr(h), F, _ptr(hq and hq.codes), _ptr(hq and hq.scale),
+                                     _ptr(gu and gu.codes), _ptr(gu and gu.scale), _ptr(workspace), workspace.numel(),
+                                     _stream()), "zq_fp8_gated_linear")
+    return h, hq, gu
+
+
+def fp8_gated_linear_backward(wt: Fp8Weight, gu: Fp8Block, *, dy=None, q: Optional[Fp8Block] = None, act="silu",
+                              mode="none", workspace: Optional[torch.Tensor] = None):
+    """Gradients of g and u from the gradient of the block's output (bf16 ``dy`` or quantized ``q``), the transposed down
+    projection ``wt`` and the checkpoint ``gu``.  Returns (bf16 [2, M, F], the same quantized)."""
+    codes, scale, dy, lddy, M = _activations(dy, q, wt.K, 1)
+    F, dev, fb = wt.N, wt.codes.device, _blocks(wt.N)
+    if tuple(gu.codes.shape) != (2, M, F) or tuple(gu.scale.shape) != (2, fb, M):
+        raise ValueError(f"the checkpoint {tuple(gu.codes.shape)} does not fit [2, {M}, {F}]")
+    _expect(gu.codes, torch.uint8, "gu.codes")
+    _expect(gu.scale, torch.float32, "gu.scale")
+    d = torch.empty((2, M, F), dtype=torch.bfloat16, device=dev)
+    dq = Fp8Block(torch.empty((2, M, F), dtype=torch.uint8, device=dev),
+                  torch.empty((2, fb, M), dtype=torch.float32, device=dev))
+    workspace = _fp8_workspace(workspace, M, wt.K, dev)
+    _check(lib().zq_fp8_gated_linear_backward(_ptr(codes), _ptr(scale), _ptr(dy), lddy, _mode(mode), M, F, wt.K,
+                                              _ptr(wt.codes), _ptr(wt.scale), _act(act), _ptr(gu.codes),
+                                              _ptr(gu.scale), _ptr(d), _ptr(dq.codes), _ptr(dq.scale),
+                                              _ptr(workspace), workspace.numel(), _stream()),
+           "zq_fp8_gated_linear_backward")
+    return d, dq
+
+
+def fp8_weight_grad(g: torch.Tensor, q: Fp8Block, *, out_dtype=torch.float32,
+                    workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dW = g^T x^ with the checkpoint ``q`` of x.  g: bf16 [M, N] (row stride allowed) -> [N, K]; or contiguous
+    [parts, M, N] -> [parts, N, K]."""
+    parts = g.shape[0] if g.dim() == 3 else 1
+    g0 = g[0] if g.dim() == 3 else g
+    ldg = _rows(g0, "g")
+    M, N = g0.shape
+    codes, scale, _, _, Mq = _activations(None, q, q.codes.shape[-1], 1)
+    if Mq != M:
+        raise ValueError(f"g has {M} rows, the checkpoint {Mq}")
+    K = codes.shape[-1]
+    dw = torch.empty((parts, N, K) if g.dim() == 3 else (N, K), dtype=out_dtype, device=g.device)
+    workspace = _fp8_workspace(workspace, 0, 16, g.device)
+    _check(lib().zq_fp8_weight_grad(_ptr(g), ldg, g.stride(0) if g.dim() == 3 else 0, parts, _ptr(codes), _ptr(scale),
+                                    M, N, K, _ptr(dw), OUT_F32 if out_dtype == torch.float32 else OUT_BF16,
+                                    _ptr(workspace), workspace.numel(), _stream()), "zq_fp8_weight_grad")
+    return dw

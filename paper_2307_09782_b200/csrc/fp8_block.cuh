@@ -1,0 +1,144 @@
+// Pieces shared by the FP8 operators with block scales: E4M3 codes whose scale belongs to a block of 128, one
+// row by 128 input features for activations, 128 x 128 for weights (FP32 scales, or rounded up to a power of two).
+// See include/zqfp.h for the operators' definitions.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <mutex>
+
+#include "act_cast.cuh"
+#include "w4a8_gemm_shared.cuh"
+
+namespace zq {
+namespace fp8b {
+
+constexpr int kBlk = 128;
+inline int64_t blocks_of(int64_t n) { return (n + kBlk - 1) / kBlk; }
+
+enum Kind {
+  kPlain = 0,     // y = a b^T
+  kGated = 1,     // b is (gate, up): h = act(a g^T) (a u^T), in bf16 and / or quantized; g and u kept in 8 bits on request
+  kGatedBwd = 2,  // y = a b^T is the gradient of h: the gradients of g and u, from the 8-bit g and u
+};
+
+struct GemmArgs8 {
+  const uint8_t* a;  // [parts][M][K] E4M3 (kGated: [M][K])
+  const float* sa;   // [parts][ceil(K / 128)][M]
+  const uint8_t* b;  // [parts][N][K] E4M3 (kGated: [2][N][K])
+  const float* sb;   // [parts][ceil(N / 128)][ceil(K / 128)]
+  int64_t M, N, K;
+  int parts;         // segments of the K sum (kPlain)
+  int kind, act, mode;
+  void* y;           // kPlain: [M][ldy] FP32 or bf16; kGated: h bf16 [M][ldy] or NULL; kGatedBwd: bf16 [2][M][N]
+  int ydt;
+  int64_t ldy;
+  uint8_t* q;        // kGated: codes of h [M][N] or NULL; kGatedBwd: codes of the gradients [2][M][N]
+  float* s;          // their scales, [ceil(N / 128)][M] each
+  uint8_t* ck;       // [2][M][N] codes of g and u (kGated: written when not NULL; kGatedBwd: read)
+  float* cks;        // [2][ceil(N / 128)][M]
+  int* status;
+};
+
+int launch_quantize_block(const void* x, int64_t M, int64_t K, int64_t ldx, int mode, uint8_t* q, float* s,
+                          cudaStream_t st);
+int launch_quantize_weight_block(const float* w, int64_t N, int64_t K, int mode, uint8_t* q, float* s, cudaStream_t st);
+int launch_transpose_weight_block(const uint8_t* q, const float* s, int64_t N, int64_t K, uint8_t* qt, float* st_,
+                                  cudaStream_t st);
+int launch_block_gemm(const GemmArgs8& a, cudaStream_t st);
+struct WgradArgs {
+  const void* g;     // bf16 [parts] x [M][ldg], g_stride elements apart
+  int64_t ldg, g_stride;
+  const uint8_t* q;  // [M][K]
+  const float* s;    // [ceil(K / 128)][M]
+  int parts;
+  int64_t M, N, K;
+  void* dw;          // [parts][N][K]
+  int dwdt;
+  int* status;
+};
+int launch_wgrad(const WgradArgs& a, cudaStream_t st);
+
+#ifdef __CUDACC__
+// A 3-D tensor of bytes [parts][rows][K] (dense), boxes of 128 bytes x `box_rows` rows, 128-byte swizzle: one
+// K-major operand tile of the tensor core.  Beyond the tensor the copy engine fills in zeros.
+inline bool make_code_map(CUtensorMap* m, const void* base, uint64_t K, uint64_t rows, uint64_t parts, uint32_t box_rows) {
+  gemm::EncodeTiledFn fn = gemm::encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {K, rows, parts};
+  const cuuint64_t strides[2] = {K, K * rows};
+  const cuuint32_t box[3] = {kBlk, box_rows, 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The scale of a block from the bits of its absolute maximum (as unsigned numbers they order like the values, and
+// NaN and infinity are above all finite ones, so a maximum over bits keeps them):
+//   0 -> 1 ; not finite -> NaN (the whole block then stands for NaN) ; else max(fl32(a / 448), 2^-126), which keeps
+//   1 / s finite, rounded up to a power of two on request (the carry of the mantissa moves the exponent).
+__device__ __forceinline__ float block_scale(uint32_t amax_bits, bool pow2) {
+  if (amax_bits == 0u) return 1.0f;
+  if (amax_bits >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
+  float s = fmaxf(__fdiv_rn(__uint_as_float(amax_bits), 448.0f), 1.17549435e-38f);
+  if (pow2) s = __uint_as_float((__float_as_uint(s) + 0x7FFFFFu) & 0x7F800000u);
+  return s;
+}
+__device__ __forceinline__ float block_inv(float s) { return __frcp_rn(s); }
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// Four FP32 values -> four E4M3 bytes of v * inv.
+__device__ __forceinline__ uint32_t cast4(float a, float b, float c, float d, float inv) {
+  return cvt_e4m3x2(__fmul_rn(a, inv), __fmul_rn(b, inv)) | (cvt_e4m3x2(__fmul_rn(c, inv), __fmul_rn(d, inv)) << 16);
+}
+// Two E4M3 bytes -> FP32 (exact: every E4M3 value is an FP16 value).
+__device__ __forceinline__ float2 decode2(uint16_t w) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(w));
+  __half2 h2;
+  *reinterpret_cast<uint32_t*>(&h2) = h;
+  return __half22float2(h2);
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// The activations.  SiLU and the tanh form of GELU are both v * sigmoid(w(v)), with w = v and
+// w = 2 sqrt(2 / pi) (v + 0.044715 v^3), since (1 + tanh z) / 2 = sigmoid(2 z).  1 / (1 + exp(-w)) with the fast
+// exponential and division is good to about 1e-6 relative: 2^-13 of a bf16 rounding step.
+template <int ACT>
+__device__ __forceinline__ float act_sigmoid(float v) {
+  const float w = ACT == ZQ_ACT_SILU ? v : 1.5957691216057308f * v * fmaf(0.044715f * v, v, 1.0f);
+  return __fdividef(1.0f, 1.0f + __expf(-w));
+}
+template <int ACT>
+__device__ __forceinline__ float act_value(float v) {
+  if (ACT == ZQ_ACT_RELU) return v < 0.0f ? 0.0f : v;  // keeps NaN
+  return v * act_sigmoid<ACT>(v);
+}
+// value and derivative: v p and p + v p (1 - p) w'
+template <int ACT>
+__device__ __forceinline__ void act_both(float v, float& value, float& slope) {
+  if (ACT == ZQ_ACT_RELU) {
+    value = v < 0.0f ? 0.0f : v;
+    slope = v > 0.0f ? 1.0f : 0.0f;
+    return;
+  }
+  const float p = act_sigmoid<ACT>(v);
+  const float dw = ACT == ZQ_ACT_SILU ? 1.0f : 1.5957691216057308f * fmaf(0.134145f * v, v, 1.0f);
+  value = v * p;
+  slope = fmaf(value * (1.0f - p), dw, p);
+}
+
+__device__ __forceinline__ void raise_error8(int* status, volatile int* abort_flag, int detail) {
+  *abort_flag = 1;
+  if (atomicCAS(status, 0, ZQ_ERR_DEVICE_TIMEOUT) == 0) status[1] = detail;
+}
+#endif  // __CUDACC__
+
+}  // namespace fp8b
+}  // namespace zq

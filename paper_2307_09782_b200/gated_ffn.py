@@ -1,0 +1,84 @@
+"""The gated feed-forward block on the FP8 operators with block scales: y = (act(x Wg^T) * (x Wu^T)) Wd^T, for serving and
+for training with 8-bit activation checkpoints.  It only strings the calls of :mod:`binding` together.
+"""
+from __future__ import annotations
+
+from dataclasses import dataclass
+from typing import Optional
+
+import torch
+
+from . import binding
+from .binding import Fp8Block, Fp8Weight
+
+
+@dataclass
+class SavedActivations:
+    """What a training pass keeps for its backward pass: x, (g, u) and h, all in 8 bits."""
+    x: Fp8Block
+    gu: Fp8Block
+    h: Fp8Block
+
+
+class GatedFfnFp8:
+    """``gate_up``: stacked gate and up weights (parts = 2, [F, K]); ``down``: [K_out, F].
+
+    ``mode``: how activations are scaled, "none" (FP32 scales) or "M1" (powers of two, which the 8-bit checkpoints
+    turn back into bf16 without rounding: the one to train with).  ``training`` lays the transposed weights out as well.
+    A block keeps one workspace per stream and device it is used on, grown on demand.
+    """
+
+    def __init__(self, gate_up: Fp8Weight, down: Fp8Weight, act: str = "silu", mode: str = "none", training: bool = False):
+        if gate_up.parts != 2 or down.parts != 1 or down.K != gate_up.N:
+            raise ValueError(f"gate_up is 2 x [F, K] and down [K_out, F]: got {gate_up.parts} x [{gate_up.N}, {gate_up.K}] "
+                             f"and [{down.N}, {down.K}]")
+        self.gate_up, self.down, self.act, self.mode = gate_up, down, act, mode
+        self.gate_up_t: Optional[Fp8Weight] = None
+        self.down_t: Optional[Fp8Weight] = None
+        self._workspaces = {}
+        if training:
+            self.gate_up_t = binding.transpose_fp8_weight(gate_up)
+            self.down_t = binding.transpose_fp8_weight(down)
+
+    @classmethod
+    def from_weights(cls, gate: torch.Tensor, up: torch.Tensor, down: torch.Tensor, **kw) -> "GatedFfnFp8":
+        """From float32 weights [F, K], [F, K], [K_out, F] (their blocks are scaled with the rule ``mode`` names)."""
+        mode = kw.get("mode", "none")
+        return cls(binding.quantize_weight_fp8_block(torch.stack([gate, up]), mode),
+                   binding.quantize_weight_fp8_block(down.contiguous(), mode), **kw)
+
+    def workspace(self, M: int) -> torch.Tensor:
+        dev = self.down.codes.device
+        key = (dev, torch.cuda.current_stream(dev).cuda_stream)
+        need = binding.fp8_block_linear_workspace_bytes(M, 0, max(self.gate_up.K, self.down.N))
+        ws = self._workspaces.get(key)
+        if ws is None or ws.numel() < need:
+            ws = self._workspaces[key] = binding.make_workspace(need, dev)
+        return ws
+
+    def forward(self, x: torch.Tensor, out_dtype=torch.bfloat16) -> torch.Tensor:
+        """x bf16 [M, K] -> y [M, K_out]; h goes from one kernel to the next in its quantized form."""
+        ws = self.workspace(x.shape[0])
+        _, h, _ = binding.fp8_gated_linear(self.gate_up, x=x, act=self.act, mode=self.mode, bf16=False, quantized=True,
+                                           workspace=ws)
+        return binding.fp8_block_linear(self.down, q=h, out_dtype=out_dtype, workspace=ws)
+
+    def forward_train(self, x: torch.Tensor, out_dtype=torch.bfloat16):
+        """(y, what :meth:`backward` needs)."""
+        ws = self.workspace(x.shape[0])
+        xq = binding.quantize_fp8_block(x, self.mode)
+        _, h, gu = binding.fp8_gated_linear(self.gate_up, q=xq, act=self.act, mode=self.mode, bf16=False, quantized=True,
+                                            checkpoint=True, workspace=ws)
+        return binding.fp8_block_linear(self.down, q=h, out_dtype=out_dtype, workspace=ws), SavedActivations(xq, gu, h)
+
+    def backward(self, dy: torch.Tensor, saved: SavedActivations, out_dtype=torch.bfloat16):
+        """dy bf16 [M, K_out] -> (dx [M, K], dW of (gate, up) [2, F, K], dW of down [K_out, F])."""
+        if self.down_t is None or self.gate_up_t is None:
+            raise ValueError("the backward pass needs the transposed weights: construct the block with training=True")
+        ws = self.workspace(dy.shape[0])
+        dgu, dguq = binding.fp8_gated_linear_backward(self.down_t, saved.gu, dy=dy, act=self.act, mode=self.mode,
+                                                      workspace=ws)
+        dx = binding.fp8_block_linear(self.gate_up_t, q=dguq, out_dtype=out_dtype, workspace=ws)
+        dwgu = binding.fp8_weight_grad(dgu, saved.x, out_dtype=out_dtype, workspace=ws)
+        dwd = binding.fp8_weight_grad(dy, saved.h, out_dtype=out_dtype, workspace=ws)
+        return dx, dwgu, dwd
