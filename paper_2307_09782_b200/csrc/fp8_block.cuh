@@ -134,6 +134,12 @@ __device__ __forceinline__ void act_both(float v, float& value, float& slope) {
   slope = fmaf(value * (1.0f - p), dw, p);
 }
 
+// Registers per thread from here on, for a whole warpgroup (each warp of it executes one of these).
+template <int N>
+__device__ __forceinline__ void regs_give() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_take() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+
 __device__ __forceinline__ void raise_error8(int* status, volatile int* abort_flag, int detail) {
   *abort_flag = 1;
   if (atomicCAS(status, 0, ZQ_ERR_DEVICE_TIMEOUT) == 0) status[1] = detail;

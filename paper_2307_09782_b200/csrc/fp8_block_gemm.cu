@@ -29,8 +29,8 @@ constexpr int kABytes = kTileM * kBlk, kBBytes = kTileN * kBlk;
 constexpr int kEpiWarps = 8, kEpiThreads = 256;
 constexpr int kProducerWarp = 8, kMmaWarp = 9;
 constexpr int kThreads = 384;  // three warpgroups; the two epilogue ones take registers over from the third
-// 384 threads start with 168 registers each: 2 x 128 x 216 + 128 x 72 is what the block was given
-constexpr int kEpiRegs = 216, kOtherRegs = 72;
+// 384 threads start with 168 registers each: 2 x 128 x 224 + 128 x 56 is what the block was given
+constexpr int kEpiRegs = 224, kOtherRegs = 56;
 static_assert(256 * kEpiRegs + 128 * kOtherRegs <= kThreads * 168, "register split");
 constexpr int kStageBuf = 32 * 128;  // staging of one epilogue warp: 32 rows of 128 bytes
 constexpr int kOffA = 0;
@@ -178,10 +178,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   if (threadIdx.x == 0) pdl_launch_dependents();
 
   if (warp >= kEpiWarps) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-  } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpiRegs));
-  }
+  regs_give<kOtherRegs>();
   if (warp == kProducerWarp) {
     if (ok_start) {
       const bool issuer = elect_one();
@@ -272,8 +269,10 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       }
       __syncwarp();
     }
-  } else if (warp < kEpiWarps) {
+  }
+  } else {
     // ---- epilogue warps
+    regs_take<kEpiRegs>();
     const int quarter = warp & 3, half = warp >> 2;
     const int row = quarter * 32 + lane;
     const uint32_t lane_base = static_cast<uint32_t>(quarter * 32) << 16;
