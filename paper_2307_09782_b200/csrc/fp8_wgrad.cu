@@ -1,65 +1,382 @@
-// Weight gradient from an 8-bit activation checkpoint: dW[n, k] = sum_m G[m, n] * (code[m, k] * s[k / 128, m]).
+// Weight gradient from an 8-bit activation checkpoint:
+//   dW[p][n, k] = sum_m G[p][m, n] * bf16(code[m, k] * s[k / 128, m])
 //
-// Plain tiled kernel on the CUDA cores: 64 x 64 outputs per CTA, 16 tokens at a time through shared memory,
-// 4 x 4 outputs per thread.
+// The sum runs over tokens, along which the checkpoint's scales change with every row: they cannot be taken out of
+// the sum, so the codes are turned back into bf16 on the way to the tensor core (exactly, with power-of-two scales)
+// and multiplied by the bf16 gradient.  Only the codes cross HBM and L2; the bf16 values exist in shared memory.
+//
+// Tile: 128 input features (the MMA's 128-row operand, converted once per 256 outputs) x 256 outputs, tokens by 64.
+// In memory both operands have the token index outermost, so both are MN-major for the tensor core: 64 elements
+// (128 bytes) of a token per row, 64 token rows = 8 KB per chunk of 64 columns, 128-byte swizzle.
+// Converters (4 warps, a token row and 64 features per thread) read a stage's 8 KB of codes, scale, round and write
+// 16 KB of bf16 into a ring of their own; the gradient's tiles go from the copy engine to the tensor core untouched.
+// Per 64 tokens the MMAs take 512 cycles, the conversion about 180 issue slots of each SM quarter.
+//
+// Two accumulators of 256 columns: the stores of one tile overlap the sums of the next.
+// Warp roles: 0..3 epilogue, 4..7 converters, 8 producer, 9 tensor memory and MMAs.
 #include "fp8_block.cuh"
 
 namespace zq {
 namespace fp8b {
 namespace {
 
-constexpr int kT = 64, kTok = 16;
+constexpr int kTok = 64;                         // tokens per stage
+constexpr int kTileK = 128, kTileN = 256;
+constexpr int kGBytes = kTok * kTileN * 2;       // four chunks of 64 outputs x 64 tokens
+constexpr int kXBytes = kTok * kTileK;           // codes
+constexpr int kCBytes = kTok * kTileK * 2;       // converted: two chunks of 64 features x 64 tokens
+constexpr int kChunk = kTok * 128;               // bytes of a chunk
+constexpr int kStages = 4, kConv = 3;
+constexpr int kOffG = 0;
+constexpr int kOffC = kOffG + kStages * kGBytes;
+constexpr int kOffX = kOffC + kConv * kCBytes;
+constexpr int kOffBars = kOffX + kStages * kXBytes;
+constexpr int kNumBars = 2 * kStages + 2 * kConv + 4 + 1;
+constexpr int kOffMisc = kOffBars + kNumBars * 8;
+constexpr int kSmemBytes = kOffMisc + 16;
+static_assert(kSmemBytes <= 227 * 1024, "shared memory");
+constexpr int kConvWarp0 = 4, kProducerWarp = 8, kMmaWarp = 9, kThreads = 320;
 
-__global__ void __launch_bounds__(256)
-wgrad_simple_kernel(const __nv_bfloat16* __restrict__ g, int64_t ldg, int64_t g_stride, const uint8_t* __restrict__ q,
-                    const float* __restrict__ s, int64_t M, int64_t N, int64_t K, void* __restrict__ dw, int dwdt) {
-  __shared__ float s_g[kTok][kT], s_x[kTok][kT];
-  const int64_t n0 = static_cast<int64_t>(blockIdx.y) * kT, k0 = static_cast<int64_t>(blockIdx.x) * kT;
-  g += blockIdx.z * g_stride;
-  const int tn = threadIdx.x >> 4, tk = threadIdx.x & 15;
-  float acc[4][4] = {};
-  for (int64_t m0 = 0; m0 < M; m0 += kTok) {
-    for (int i = threadIdx.x; i < kTok * kT; i += 256) {
-      const int r = i / kT, c = i % kT;
-      const int64_t m = m0 + r;
-      s_g[r][c] = m < M && n0 + c < N ? __bfloat162float(g[m * ldg + n0 + c]) : 0.0f;
-      float v = 0.0f;
-      if (m < M && k0 + c < K)
-        v = __bfloat162float(__float2bfloat16_rn(decode2(q[m * K + k0 + c]).x * s[((k0 + c) / kBlk) * M + m]));
-      s_x[r][c] = v;
+enum { kErrProducerW = 31, kErrMmaW = 32, kErrEpilogueW = 33, kErrAlignW = 34, kErrConvertW = 35 };
+
+struct PW {
+  int M, N, K;
+  int steps;  // stages per tile
+  int k_tiles, n_tiles, tiles, n_group;
+  const float* s;
+  void* dw;
+  int* status;
+};
+
+__device__ __forceinline__ void tile_of(const PW& p, int pos, int& part, int& nt, int& kt) {
+  const int per_part = p.n_tiles * p.k_tiles;
+  part = pos / per_part;
+  pos -= part * per_part;
+  const int per_group = p.n_group * p.k_tiles;
+  const int g = pos / per_group, within = pos - g * per_group;
+  const int gn = min(p.n_group, p.n_tiles - g * p.n_group);
+  nt = g * p.n_group + within % gn;
+  kt = within / gn;
+}
+
+// MN-major operand, 128-byte swizzle: 64 elements of the M / N extent per 128-byte row, 8 rows of K per atom.
+// Leading offset: the next 64 elements (a chunk further); stride offset: the next 8 rows of K.
+__device__ __forceinline__ uint64_t desc_mn128(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= uint64_t((smem_addr >> 4) & 0x3FFF);
+  d |= uint64_t(kChunk >> 4) << 16;
+  d |= uint64_t(1024 >> 4) << 32;
+  d |= uint64_t(1) << 46;
+  d |= uint64_t(2) << 61;
+  return d;
+}
+// bf16 x bf16 -> FP32, both operands MN-major, D is 128 x n
+__device__ __forceinline__ uint32_t idesc_bf16_mn(uint32_t n) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+__device__ __forceinline__ void umma_f16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// Two codes -> two bf16 values of code * s.
+__device__ __forceinline__ uint32_t widen2(uint16_t w, float s) {
+  const float2 f = decode2(w);
+  return pack_bf16(f.x * s, f.y * s);
+}
+
+template <bool F32>
+__global__ void __launch_bounds__(kThreads, 1)
+fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant__ CUtensorMap tm_x, const PW p) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBars);
+  uint64_t* full = bars;                    // [stages] gradient and codes landed                (converters, MMA wait)
+  uint64_t* empty = full + kStages;         // [stages] the MMAs that read the stage are done     (producer waits)
+  uint64_t* conv_full = empty + kStages;    // [conv] the converted tile is written               (MMA waits)
+  uint64_t* conv_empty = conv_full + kConv; // [conv] the MMAs that read it are done              (converters wait)
+  uint64_t* acc_full = conv_empty + kConv;  // [2] a tile's sums are complete                     (epilogue waits)
+  uint64_t* acc_empty = acc_full + 2;       // [2] the epilogue has read them                     (MMA waits)
+  uint64_t* drain_bar = acc_empty + 2;
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + kOffMisc);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(smem + kOffMisc + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
     }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < kTok; ++r)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(s_g[r][tn * 4 + i], s_x[r][tk * 4 + j], acc[i][j]);
-    __syncthreads();
+    for (int i = 0; i < kConv; ++i) {
+      mbar_init(&conv_full[i], 4);
+      mbar_init(&conv_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&acc_full[i], 1);
+      mbar_init(&acc_empty[i], 4);
+    }
+    mbar_init(drain_bar, 1);
+    *s_abort = 0;
+    fence_mbar_init();
+    if ((smem_u32(smem) & 1023u) != 0) raise_error8(p.status, s_abort, kErrAlignW);
   }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int64_t n = n0 + tn * 4 + i, k = k0 + tk * 4 + j;
-      if (n < N && k < K) {
-        const int64_t o = (blockIdx.z * N + n) * K + k;
-        if (dwdt == ZQ_OUT_F32)
-          static_cast<float*>(dw)[o] = acc[i][j];
-        else
-          static_cast<__nv_bfloat16*>(dw)[o] = __float2bfloat16_rn(acc[i][j]);
+  if (warp == kProducerWarp && lane == 0) {
+    prefetch_tensormap(&tm_g);
+    prefetch_tensormap(&tm_x);
+  }
+  if (warp == kMmaWarp) tmem_alloc(s_tmem, 512);
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *s_tmem;
+  const bool ok_start = *s_abort == 0;
+  if (threadIdx.x == 0) pdl_launch_dependents();
+
+  if (warp == kProducerWarp) {
+    if (ok_start) {
+      const bool issuer = elect_one();
+      pdl_wait();
+      int s = 0, issued = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int pos = blockIdx.x; ok && pos < p.tiles; pos += gridDim.x) {
+        int part, nt, kt;
+        tile_of(p, pos, part, nt, kt);
+        for (int i = 0; i < p.steps; ++i) {
+          if (issued >= kStages && !mbar_wait(&empty[s], ph ^ 1, s_abort)) {
+            if (issuer) raise_error8(p.status, s_abort, kErrProducerW);
+            ok = false;
+            break;
+          }
+          if (issuer) {
+            mbar_arrive_expect_tx(&full[s], kGBytes + kXBytes);
+            tma_load_3d(smem + kOffX + s * kXBytes, &tm_x, kt * kTileK, i * kTok, 0, &full[s]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              tma_load_3d(smem + kOffG + s * kGBytes + c * kChunk, &tm_g, nt * kTileN + c * 64, i * kTok, part, &full[s]);
+          }
+          __syncwarp();
+          ++issued;
+          if (++s == kStages) {
+            s = 0;
+            ph ^= 1;
+          }
+        }
+      }
+      // never leave with copies still in flight
+      for (int i = max(0, issued - kStages); i < issued; ++i) {
+        uint32_t spin = 0;
+        while (!mbar_try_wait(&full[i % kStages], (i / kStages) & 1) && ++spin < kSpinLimit) {
+        }
       }
     }
+  } else if (warp == kMmaWarp) {
+    if (ok_start) {
+      const bool issuer = elect_one();
+      const uint64_t adesc0 = desc_mn128(smem_u32(smem + kOffC));
+      const uint64_t bdesc0 = desc_mn128(smem_u32(smem + kOffG));
+      const uint32_t idesc = idesc_bf16_mn(kTileN);
+      int s = 0, c = 0, tile = 0;
+      uint32_t ph = 0, cph = 0;
+      bool failed = false;
+      for (int pos = blockIdx.x; !failed && pos < p.tiles; pos += gridDim.x, ++tile) {
+        const int buf = tile & 1;
+        if (tile >= 2 && !mbar_wait(&acc_empty[buf], ((tile >> 1) - 1) & 1, s_abort)) {
+          failed = true;
+          break;
+        }
+        for (int i = 0; i < p.steps; ++i) {
+          if (!mbar_wait(&full[s], ph, s_abort) || !mbar_wait(&conv_full[c], cph, s_abort)) {
+            failed = true;
+            break;
+          }
+          tc_fence_after_sync();
+          if (issuer) {
+            const uint64_t ad = adesc0 + static_cast<uint64_t>((c * kCBytes) >> 4);
+            const uint64_t bd = bdesc0 + static_cast<uint64_t>((s * kGBytes) >> 4);
+#pragma unroll
+            for (int k = 0; k < kTok / 16; ++k)  // 16 token rows of 128 bytes further
+              umma_f16(tmem_base + buf * kTileN, ad + k * (2048 >> 4), bd + k * (2048 >> 4), idesc, (i > 0 || k > 0) ? 1u : 0u);
+            umma_commit(&empty[s]);
+            umma_commit(&conv_empty[c]);
+            if (i + 1 == p.steps) umma_commit(&acc_full[buf]);
+          }
+          __syncwarp();
+          if (++s == kStages) {
+            s = 0;
+            ph ^= 1;
+          }
+          if (++c == kConv) {
+            c = 0;
+            cph ^= 1;
+          }
+        }
+      }
+      if (failed) {
+        if (issuer) {
+          raise_error8(p.status, s_abort, kErrMmaW);
+          umma_commit(drain_bar);
+        }
+        uint32_t spin = 0;
+        while (!mbar_try_wait(drain_bar, 0) && ++spin < kSpinLimit) {
+        }
+      }
+      __syncwarp();
+    }
+  } else if (warp >= kConvWarp0) {
+    // ---- converters: thread = token row (t % 64) and chunk of 64 features (t / 64)
+    const int t = threadIdx.x - kConvWarp0 * 32;
+    const int row = t & 63, chunk = t >> 6;
+    const int sw = row & 7;
+    bool failed = !ok_start;
+    int s = 0, c = 0, n = 0;
+    uint32_t ph = 0, cph = 0;
+    pdl_wait();
+    for (int pos = blockIdx.x; !failed && pos < p.tiles; pos += gridDim.x) {
+      int part, nt, kt;
+      tile_of(p, pos, part, nt, kt);
+      const float* sc = p.s + static_cast<int64_t>(kt) * p.M;
+      float s_next = row < p.M ? __ldg(sc + row) : 0.0f;
+      for (int i = 0; i < p.steps; ++i, ++n) {
+        const float scale = s_next;
+        const int m_next = (i + 1) * kTok + row;
+        if (i + 1 < p.steps) s_next = m_next < p.M ? __ldg(sc + m_next) : 0.0f;
+        if (!mbar_wait_warp(&full[s], ph, s_abort) || (n >= kConv && !mbar_wait_warp(&conv_empty[c], cph ^ 1, s_abort))) {
+          if (lane == 0) raise_error8(p.status, s_abort, kErrConvertW);
+          failed = true;
+          break;
+        }
+        const uint4* src = reinterpret_cast<const uint4*>(smem + kOffX + s * kXBytes + row * 128);
+        uint4* dst = reinterpret_cast<uint4*>(smem + kOffC + c * kCBytes + chunk * kChunk + row * 128);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint4 v = src[(chunk * 4 + j) ^ sw];
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+          uint32_t o[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            o[2 * e] = widen2(static_cast<uint16_t>(w[e]), scale);
+            o[2 * e + 1] = widen2(static_cast<uint16_t>(w[e] >> 16), scale);
+          }
+          dst[(2 * j) ^ sw] = make_uint4(o[0], o[1], o[2], o[3]);
+          dst[(2 * j + 1) ^ sw] = make_uint4(o[4], o[5], o[6], o[7]);
+        }
+        fence_proxy_async_smem();  // the tensor core reads what these stores wrote
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&conv_full[c]);
+        if (++s == kStages) {
+          s = 0;
+          ph ^= 1;
+        }
+        if (++c == kConv) {
+          c = 0;
+          cph ^= 1;
+        }
+      }
+    }
+  } else {
+    // ---- epilogue: thread = input feature; a column is one output channel, 32 neighbouring features per warp
+    bool failed = !ok_start;
+    const uint32_t lane_base = static_cast<uint32_t>(warp * 32) << 16;
+    int tile = 0;
+    pdl_wait();
+    for (int pos = blockIdx.x; !failed && pos < p.tiles; pos += gridDim.x, ++tile) {
+      int part, nt, kt;
+      tile_of(p, pos, part, nt, kt);
+      const int buf = tile & 1;
+      if (!mbar_wait_warp(&acc_full[buf], (tile >> 1) & 1, s_abort)) {
+        if (lane == 0) raise_error8(p.status, s_abort, kErrEpilogueW);
+        failed = true;
+        break;
+      }
+      tc_fence_after_sync();
+      const int k = kt * kTileK + warp * 32 + lane;
+      const int n0 = nt * kTileN;
+      const int cols = k < p.K ? p.N - n0 : 0;
+      const int64_t base = (static_cast<int64_t>(part) * p.N + n0) * p.K + k;
+      const uint32_t ta = tmem_base + buf * kTileN + lane_base;
+#pragma unroll 1
+      for (int c = 0; c < kTileN; c += 16) {
+        float v[16];
+        tmem_ld16(ta + c, v);
+        tmem_ld_wait_regs<16>(v);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (c + e < cols) {
+            const int64_t o = base + static_cast<int64_t>(c + e) * p.K;
+            if (F32)
+              static_cast<float*>(p.dw)[o] = v[e];
+            else
+              static_cast<__nv_bfloat16*>(p.dw)[o] = __float2bfloat16_rn(v[e]);
+          }
+      }
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&acc_empty[buf]);
+    }
+  }
+
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem_base, 512);
+  }
+}
+
+// G as a 3-D tensor [parts][M][N] of bf16, boxes of 64 elements x 64 tokens.
+bool make_grad_map(CUtensorMap* m, const WgradArgs& a) {
+  gemm::EncodeTiledFn fn = gemm::encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(a.N), static_cast<cuuint64_t>(a.M), static_cast<cuuint64_t>(a.parts)};
+  const int64_t part = a.parts > 1 ? a.g_stride : a.M * a.ldg;
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(a.ldg) * 2, static_cast<cuuint64_t>(part) * 2};
+  const cuuint32_t box[3] = {64, kTok, 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.g), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool F32>
+int launch_cfg(const CUtensorMap& tg, const CUtensorMap& tx, const PW& p, unsigned grid, cudaStream_t st) {
+  static std::once_flag once;
+  static cudaError_t attr = cudaSuccess;
+  std::call_once(once, [] {
+    attr = cudaFuncSetAttribute(fp8_wgrad_kernel<F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  });
+  if (attr != cudaSuccess) return ZQ_ERR_CUDA;
+  const cudaError_t e = launch_chained(fp8_wgrad_kernel<F32>, dim3(grid), dim3(kThreads), kSmemBytes, st, false, tg, tx, p);
+  count_launch();
+  return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
 }
 
 }  // namespace
 
 int launch_wgrad(const WgradArgs& a, cudaStream_t st) {
-  const dim3 grid(static_cast<unsigned>((a.K + kT - 1) / kT), static_cast<unsigned>((a.N + kT - 1) / kT),
-                  static_cast<unsigned>(a.parts));
-  if (grid.y > 65535) return ZQ_ERR_SHAPE;
-  wgrad_simple_kernel<<<grid, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(a.g), a.ldg, a.g_stride, a.q, a.s, a.M,
-                                            a.N, a.K, a.dw, a.dwdt);
-  count_launch();
-  return cudaGetLastError() == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
+  PW p{};
+  p.M = static_cast<int>(a.M);
+  p.N = static_cast<int>(a.N);
+  p.K = static_cast<int>(a.K);
+  p.steps = static_cast<int>((a.M + kTok - 1) / kTok);
+  p.k_tiles = static_cast<int>(blocks_of(a.K));
+  p.n_tiles = static_cast<int>((a.N + kTileN - 1) / kTileN);
+  p.n_group = 8;
+  const int64_t tiles = static_cast<int64_t>(p.k_tiles) * p.n_tiles * a.parts;
+  if (tiles > 0x3FFFFFFF) return ZQ_ERR_SHAPE;
+  p.tiles = static_cast<int>(tiles);
+  p.s = a.s;
+  p.dw = a.dw;
+  p.status = a.status;
+  CUtensorMap tg, tx;
+  if (!make_grad_map(&tg, a) ||
+      !make_code_map(&tx, a.q, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.M), 1, kTok))
+    return ZQ_ERR_CUDA;
+  const unsigned grid = static_cast<unsigned>(tiles < sm_count() ? tiles : sm_count());
+  return a.dwdt == ZQ_OUT_F32 ? launch_cfg<true>(tg, tx, p, grid, st) : launch_cfg<false>(tg, tx, p, grid, st);
 }
 
 }  // namespace fp8b
