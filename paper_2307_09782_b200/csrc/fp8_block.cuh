@@ -39,6 +39,9 @@ struct GemmArgs8 {
   uint8_t* ck;       // [2][M][N] codes of g and u (kGated: written when not NULL; kGatedBwd: read)
   float* cks;        // [2][ceil(N / 128)][M]
   int* status;
+  // launch_block_few only: raw activations, which the kernel quantizes itself (a and sa unused)
+  const void* x;     // bf16 [M][ldx]
+  int64_t ldx;
 };
 
 int launch_quantize_block(const void* x, int64_t M, int64_t K, int64_t ldx, int mode, uint8_t* q, float* s,
@@ -46,7 +49,11 @@ int launch_quantize_block(const void* x, int64_t M, int64_t K, int64_t ldx, int 
 int launch_quantize_weight_block(const float* w, int64_t N, int64_t K, int mode, uint8_t* q, float* s, cudaStream_t st);
 int launch_transpose_weight_block(const uint8_t* q, const float* s, int64_t N, int64_t K, uint8_t* qt, float* st_,
                                   cudaStream_t st);
-int launch_block_gemm(const GemmArgs8& a, cudaStream_t st);
+int launch_block_gemm(const GemmArgs8& a, cudaStream_t st);  // many tokens
+constexpr int64_t kFewTokens = 64;
+bool few_takes(const GemmArgs8& a);
+bool few_takes_raw(const GemmArgs8& a);
+int launch_block_few(const GemmArgs8& a, cudaStream_t st);   // few tokens
 struct WgradArgs {
   const void* g;     // bf16 [parts] x [M][ldg], g_stride elements apart
   int64_t ldg, g_stride;

@@ -27,9 +27,10 @@ Ws8 ws8(int64_t M, int64_t K) {
   return w;
 }
 
-// Activations given as codes or raw.  Raw ones are quantized into the workspace first.
-int take_activations(const uint8_t*& q, const float*& s, const void* x, int64_t ldx, int64_t M, int64_t K, int mode,
-                     void* workspace, size_t workspace_bytes, cudaStream_t st) {
+// Activations given as codes or raw.  Raw ones are quantized into the workspace first, or, with few tokens, by the
+// kernel that multiplies them.
+int quantize_raw(const uint8_t*& q, const float*& s, const void* x, int64_t ldx, int64_t M, int64_t K, int mode,
+                 void* workspace, size_t workspace_bytes, cudaStream_t st) {
   if (!x) return ZQ_OK;
   const Ws8 w = ws8(M, K);
   uint8_t* base = static_cast<uint8_t*>(workspace);
@@ -40,6 +41,22 @@ int take_activations(const uint8_t*& q, const float*& s, const void* x, int64_t 
   s = s_ws;
   return launch_quantize_block(x, M, K, ldx, mode, q_ws, s_ws, st);
 }
+
+int launch(GemmArgs8& a, const uint8_t* q, const float* s, const void* x, int64_t ldx, void* workspace,
+           size_t workspace_bytes, void* stream) {
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  a.status = static_cast<int*>(workspace);
+  if (x && few_takes_raw(a)) {
+    a.x = x;
+    a.ldx = ldx;
+    return launch_block_few(a, st);
+  }
+  if (int e = quantize_raw(q, s, x, ldx, a.M, a.K, a.mode, workspace, workspace_bytes, st)) return e;
+  a.a = q;
+  a.sa = s;
+  return few_takes(a) ? launch_block_few(a, st) : launch_block_gemm(a, st);
+}
+
 int check_activations(const uint8_t* q, const float* s, const void* x, int64_t ldx, int64_t M, int64_t K, void* workspace,
                       size_t workspace_bytes) {
   if (x ? (q || s) : (!q || !s)) return ZQ_ERR_NULL;
@@ -103,11 +120,7 @@ int zq_fp8_block_linear(const uint8_t* q, const float* s, const void* x_bf16, in
   if (!al16(w) || (reinterpret_cast<uintptr_t>(y) & (ydt == ZQ_OUT_F32 ? 3u : 1u))) return ZQ_ERR_ALIGN;
   if (int e = check_activations(q, s, x_bf16, ldx, M, K, workspace, workspace_bytes)) return e;
   if (int e = check_device_sm100()) return e;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (int e = take_activations(q, s, x_bf16, ldx, M, K, mode, workspace, workspace_bytes, st)) return e;
   GemmArgs8 a{};
-  a.a = q;
-  a.sa = s;
   a.b = w;
   a.sb = ws;
   a.M = M;
@@ -119,8 +132,7 @@ int zq_fp8_block_linear(const uint8_t* q, const float* s, const void* x_bf16, in
   a.y = y;
   a.ydt = ydt;
   a.ldy = ldy;
-  a.status = static_cast<int*>(workspace);
-  return launch_block_gemm(a, st);
+  return launch(a, q, s, x_bf16, ldx, workspace, workspace_bytes, stream);
 }
 
 int zq_fp8_gated_linear(const uint8_t* q, const float* s, const void* x_bf16, int64_t ldx, zq_scale_mode mode, int64_t M,
@@ -134,11 +146,7 @@ int zq_fp8_gated_linear(const uint8_t* q, const float* s, const void* x_bf16, in
   if (!al16(w) || !al16(hq) || !al16(gu) || (reinterpret_cast<uintptr_t>(h_bf16) & 1u)) return ZQ_ERR_ALIGN;
   if (int e = check_activations(q, s, x_bf16, ldx, M, K, workspace, workspace_bytes)) return e;
   if (int e = check_device_sm100()) return e;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (int e = take_activations(q, s, x_bf16, ldx, M, K, mode, workspace, workspace_bytes, st)) return e;
   GemmArgs8 a{};
-  a.a = q;
-  a.sa = s;
   a.b = w;
   a.sb = ws;
   a.M = M;
@@ -155,8 +163,7 @@ int zq_fp8_gated_linear(const uint8_t* q, const float* s, const void* x_bf16, in
   a.s = hs;
   a.ck = gu;
   a.cks = gus;
-  a.status = static_cast<int*>(workspace);
-  return launch_block_gemm(a, st);
+  return launch(a, q, s, x_bf16, ldx, workspace, workspace_bytes, stream);
 }
 
 int zq_fp8_gated_linear_backward(const uint8_t* q, const float* s, const void* dy_bf16, int64_t lddy, zq_scale_mode mode,
@@ -170,11 +177,7 @@ int zq_fp8_gated_linear_backward(const uint8_t* q, const float* s, const void* d
   if (!al16(wt) || !al16(gu) || !al16(dgu_bf16) || !al16(dguq)) return ZQ_ERR_ALIGN;
   if (int e = check_activations(q, s, dy_bf16, lddy, M, K, workspace, workspace_bytes)) return e;
   if (int e = check_device_sm100()) return e;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (int e = take_activations(q, s, dy_bf16, lddy, M, K, mode, workspace, workspace_bytes, st)) return e;
   GemmArgs8 a{};
-  a.a = q;
-  a.sa = s;
   a.b = wt;
   a.sb = wts;
   a.M = M;
@@ -191,8 +194,7 @@ int zq_fp8_gated_linear_backward(const uint8_t* q, const float* s, const void* d
   a.s = dgus;
   a.ck = const_cast<uint8_t*>(gu);
   a.cks = const_cast<float*>(gus);
-  a.status = static_cast<int*>(workspace);
-  return launch_block_gemm(a, st);
+  return launch(a, q, s, dy_bf16, lddy, workspace, workspace_bytes, stream);
 }
 
 int zq_fp8_weight_grad(const void* g_bf16, int64_t ldg, int64_t g_stride, int parts, const uint8_t* q, const float* s,

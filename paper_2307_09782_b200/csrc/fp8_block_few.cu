@@ -1,0 +1,554 @@
+// Matrix product of E4M3 operands with block scales, few tokens: the linear layer and the gated linear layer of
+// decoding.
+//
+// What bounds it is the weights' way from HBM.  Orientation: output channels are the lanes (the MMA's 128-row
+// operand), so that a weight tile is read once for all tokens of the call, and BM = 16, 32, 64 or 128 tokens are
+// its columns.  A tile of 128 channels (kGated: 128 of the gate and the same 128 of the up projection) is worked on by
+// a cluster of 1, 2, 4 or 8 CTAs that share its K blocks; several CTAs are resident on an SM, so that the device has
+// enough copies in flight.  The cluster's partial sums meet through distributed shared memory: rank r adds up the
+// tokens that are its share, in rank order (the same result every time), and finishes them: one launch, no
+// scratch in global memory.
+//
+// The tensor core adds up one block of 128; the epilogue warps multiply it by the block's scale (of the weight
+// tile, one number; of the tokens, one per column, read from shared memory) and add it to running sums in registers.
+//
+// RAW (up to 16 tokens): the kernel quantizes the activations itself, one launch per layer.  A block's scale belongs to
+// 128 features of one token, so a CTA needs nothing but its own K blocks of x for it: four warps read them (from L2:
+// every cluster reads the same), find the maximum, cast, and write the operand tile and its scales.  The codes are
+// those of zq_quantize_fp8_block.  With more tokens the cast of a K block in every CTA takes longer than its weights'
+// way from HBM (32 tokens, 7168 -> 28672: 134 us), and a separate quantizer costs less.
+//
+// Warp roles: 0..3 epilogue (kGated: 0..3 gate, 4..7 up), then 4 quantizer warps (without RAW the first of them
+// copies the tokens' scales), 1 producer, 1 tensor memory and MMAs.
+#include "fp8_block.cuh"
+
+namespace zq {
+namespace fp8b {
+namespace {
+
+using gemm::named_bar_sync;
+
+enum { kErrProducerF = 41, kErrMmaF = 42, kErrEpilogueF = 43, kErrAlignF = 44, kErrQuantF = 45 };
+
+struct PF {
+  int M, N, K;
+  int kblocks, segs, nblocks;
+  int n_tiles, cluster;
+  const float* sa;
+  const float* sb;
+  const __nv_bfloat16* x;  // RAW
+  int64_t ldx;
+  void* y;
+  int64_t ldy;
+  int y_f32;
+  uint8_t* q;
+  float* s;
+  uint8_t* ck;
+  float* cks;
+  int act, pow2;
+  int* status;
+};
+
+template <int BM, bool GATED>
+struct FewCfg {
+  static constexpr int kMats = GATED ? 2 : 1;
+  static constexpr int kEpiWarps = 4 * kMats;
+  static constexpr int kQuantWarp0 = kEpiWarps, kQuantWarps = 4;
+  static constexpr int kProducerWarp = kEpiWarps + 4, kMmaWarp = kEpiWarps + 5;
+  static constexpr int kThreads = 32 * (kEpiWarps + 6);
+  static constexpr int kWBytes = kMats * 128 * kBlk, kTokBytes = BM * kBlk;
+  static constexpr int kStageBytes = kWBytes + kTokBytes;
+  // CTAs per SM wanted, and with them the stages that fit
+  static constexpr int kCtas = GATED ? (BM <= 32 ? 2 : 1) : (BM <= 32 ? 3 : 2);
+  static constexpr int kSmemEach = 226 * 1024 / kCtas - 1024;
+  static constexpr int kMisc = 1024 + 4 * BM * 12;
+  static constexpr int kStagesFit = (kSmemEach - kMisc) / kStageBytes;
+  static constexpr int kStages = kStagesFit > 8 ? 8 : kStagesFit;
+  static constexpr int kRedBytes = kMats * BM * 128 * 4;  // partial sums, in the stages' memory once they are done
+  static constexpr int kNB = 2;                           // accumulators
+  static constexpr int kCols = kNB * kMats * BM;
+  static constexpr int kTmemCols = kCols <= 32 ? 32 : (kCols <= 64 ? 64 : (kCols <= 128 ? 128 : 256));
+  static constexpr int offTok = kStages * kWBytes;
+  static constexpr int offSc = offTok + kStages * kTokBytes;  // [stages][BM] token scales
+  static constexpr int offMax = offSc + kStages * BM * 4;     // [kMats][4] maxima of the final step
+  static constexpr int offBars = offMax + 64;
+  static constexpr int kNumBars = 3 * kStages + 2 * kNB + 1;
+  static constexpr int offMisc = offBars + kNumBars * 8;
+  static constexpr int kSmemBytes = offMisc + 16;
+  static_assert(kStages >= 3, "pipeline depth");
+  static_assert(kRedBytes <= offSc, "the partial sums must fit the stages");
+  static_assert(kSmemBytes <= kSmemEach, "shared memory");
+  static_assert(kTmemCols * kCtas <= 512 && kCols <= 256, "tensor memory");
+  static_assert((BM * 4) % 16 == 0 && kTokBytes % 1024 == 0, "alignment");
+};
+
+__device__ __forceinline__ float ld_cluster(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float act_any(int act, float v) {
+  if (act == ZQ_ACT_SILU) return act_value<ZQ_ACT_SILU>(v);
+  if (act == ZQ_ACT_GELU_TANH) return act_value<ZQ_ACT_GELU_TANH>(v);
+  return act_value<ZQ_ACT_RELU>(v);
+}
+
+template <int BM, bool GATED, bool RAW>
+__global__ void __launch_bounds__(FewCfg<BM, GATED>::kThreads, FewCfg<BM, GATED>::kCtas)
+fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_q, const PF p) {
+  using C = FewCfg<BM, GATED>;
+  constexpr int NS = C::kStages;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::offBars);
+  uint64_t* full = bars;                // [NS] the copies of the stage landed              (MMA waits)
+  uint64_t* tok_full = full + NS;       // [NS] token codes (RAW) and scales are written    (MMA, epilogue wait)
+  uint64_t* empty = tok_full + NS;      // [NS] MMAs done and scales read                   (producer, quantizer wait)
+  uint64_t* acc_full = empty + NS;      // [NB] a K block's products are complete           (epilogue waits)
+  uint64_t* acc_empty = acc_full + C::kNB;
+  uint64_t* drain_bar = acc_empty + C::kNB;
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + C::offMisc);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(smem + C::offMisc + 4);
+  float* s_sc = reinterpret_cast<float*>(smem + C::offSc);
+  uint32_t* s_max = reinterpret_cast<uint32_t*>(smem + C::offMax);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < NS; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&tok_full[i], 1);
+      mbar_init(&empty[i], 1 + C::kEpiWarps);
+    }
+    for (int i = 0; i < C::kNB; ++i) {
+      mbar_init(&acc_full[i], 1);
+      mbar_init(&acc_empty[i], C::kEpiWarps);
+    }
+    mbar_init(drain_bar, 1);
+    *s_abort = 0;
+    fence_mbar_init();
+    if ((smem_u32(smem) & 1023u) != 0) raise_error8(p.status, s_abort, kErrAlignF);
+  }
+  if (warp == C::kProducerWarp && lane == 0) {
+    prefetch_tensormap(&tm_w);
+    if (!RAW) prefetch_tensormap(&tm_q);
+  }
+  if (warp == C::kMmaWarp) tmem_alloc(s_tmem, C::kTmemCols);
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *s_tmem;
+  const bool ok_start = *s_abort == 0;
+  if (threadIdx.x == 0) pdl_launch_dependents();
+
+  // this CTA's share: K blocks [kb0, kb1) of tile nt, tokens [m0, m0 + BM)
+  const int rank = static_cast<int>(blockIdx.x) % p.cluster, nt = static_cast<int>(blockIdx.x) / p.cluster;
+  const int m0 = static_cast<int>(blockIdx.y) * BM;
+  const int kb_all = p.segs * p.kblocks;
+  const int kb0 = static_cast<int>(static_cast<int64_t>(kb_all) * rank / p.cluster);
+  const int kb1 = static_cast<int>(static_cast<int64_t>(kb_all) * (rank + 1) / p.cluster);
+  const int nkb = kb1 - kb0;
+  const int m_here = min(BM, p.M - m0);
+
+  float run[BM];  // epilogue warps
+#pragma unroll
+  for (int c = 0; c < BM; ++c) run[c] = 0.0f;
+
+  if (warp == C::kProducerWarp) {
+    if (ok_start) {
+      const bool issuer = elect_one();
+      auto issue_weights = [&](int s, int kb) {
+        if (!issuer) return;
+        const int seg = kb / p.kblocks, k = (kb - seg * p.kblocks) * kBlk;
+        uint8_t* d = smem + s * C::kWBytes;
+        mbar_arrive_expect_tx(&full[s], C::kWBytes + (RAW ? 0 : C::kTokBytes));
+        tma_load_3d(d, &tm_w, k, nt * kBlk, GATED ? 0 : seg, &full[s]);
+        if (GATED) tma_load_3d(d + C::kWBytes / 2, &tm_w, k, nt * kBlk, 1, &full[s]);
+      };
+      auto issue_tokens = [&](int s, int kb) {
+        if (RAW || !issuer) return;
+        const int seg = kb / p.kblocks, k = (kb - seg * p.kblocks) * kBlk;
+        tma_load_3d(smem + C::offTok + s * C::kTokBytes, &tm_q, k, m0, seg, &full[s]);
+      };
+      // weights are the layer's own read-only data: their first copies go out before the wait for the kernel ahead
+      // in the stream, whose output the tokens may be
+      const int first = min(NS, nkb);
+      for (int i = 0; i < first; ++i) issue_weights(i, kb0 + i);
+      __syncwarp();
+      pdl_wait();
+      for (int i = 0; i < first; ++i) issue_tokens(i, kb0 + i);
+      __syncwarp();
+      bool ok = true;
+      int s = first == NS ? 0 : first, issued = first;
+      uint32_t ph = 1;
+      for (int i = first; i < nkb; ++i) {
+        if (!mbar_wait(&empty[s], ph ^ 1, s_abort)) {
+          if (issuer) raise_error8(p.status, s_abort, kErrProducerF);
+          ok = false;
+          break;
+        }
+        issue_weights(s, kb0 + i);
+        issue_tokens(s, kb0 + i);
+        __syncwarp();
+        ++issued;
+        if (++s == NS) {
+          s = 0;
+          ph ^= 1;
+        }
+      }
+      (void)ok;
+      // never leave with copies still in flight
+      for (int i = max(0, issued - NS); i < issued; ++i) {
+        uint32_t spin = 0;
+        while (!mbar_try_wait(&full[i % NS], (i / NS) & 1) && ++spin < kSpinLimit) {
+        }
+      }
+    }
+  } else if (warp == C::kMmaWarp) {
+    if (ok_start) {
+      const bool issuer = elect_one();
+      const uint64_t adesc0 = umma_desc_k128(smem_u32(smem));
+      const uint64_t bdesc0 = umma_desc_k128(smem_u32(smem + C::offTok));
+      const uint32_t idesc = umma_idesc_e4m3(BM);
+      int s = 0;
+      uint32_t ph = 0;
+      bool failed = false;
+      for (int i = 0; i < nkb; ++i) {
+        const int buf = i % C::kNB;
+        if ((i >= C::kNB && !mbar_wait(&acc_empty[buf], ((i / C::kNB) - 1) & 1, s_abort)) ||
+            !mbar_wait(&full[s], ph, s_abort) || !mbar_wait(&tok_full[s], ph, s_abort)) {
+          failed = true;
+          break;
+        }
+        tc_fence_after_sync();
+        if (issuer) {
+          const uint64_t ad = adesc0 + static_cast<uint64_t>((s * C::kWBytes) >> 4);
+          const uint64_t bd = bdesc0 + static_cast<uint64_t>((s * C::kTokBytes) >> 4);
+#pragma unroll
+          for (int mat = 0; mat < C::kMats; ++mat)
+#pragma unroll
+            for (int k = 0; k < kBlk / 32; ++k)
+              umma_f8(tmem_base + (buf * C::kMats + mat) * BM, ad + ((mat * 128 * kBlk) >> 4) + 2 * k, bd + 2 * k, idesc,
+                      k > 0 ? 1u : 0u);
+          umma_commit(&empty[s]);
+          umma_commit(&acc_full[buf]);
+        }
+        __syncwarp();
+        if (++s == NS) {
+          s = 0;
+          ph ^= 1;
+        }
+      }
+      if (failed && issuer) raise_error8(p.status, s_abort, kErrMmaF);
+      // tensor memory is released only when every MMA has completed, also where another role has given up
+      if (issuer) umma_commit(drain_bar);
+      uint32_t spin = 0;
+      while (!mbar_try_wait(drain_bar, 0) && ++spin < kSpinLimit) {
+      }
+      __syncwarp();
+    }
+  } else if (warp >= C::kQuantWarp0) {
+    pdl_wait();
+    const int qw = warp - C::kQuantWarp0;
+    if (RAW) {
+      // A warp takes the K blocks of the stages that are its own (stage % 4 == qw): 16 lanes per token row, two rows at a
+      // time.  Its next block's x is on its way while this one is cast, so that up to four blocks are under way at a
+      // time.  A stage belongs to one warp because a parity wait tells only two neighbouring phases of a barrier apart:
+      // whoever waits for a stage has to see every use of it.
+      constexpr int kPairs = BM / 2;
+      const int hl = lane & 15, r0 = lane >> 4;
+      uint4 nxt[kPairs];
+      auto fetch = [&](int kb) {
+        const int k = kb * kBlk + hl * 8;
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+          const int r = r0 + 2 * j;
+          nxt[j] = make_uint4(0u, 0u, 0u, 0u);
+          if (r < m_here && k < p.K) nxt[j] = __ldg(reinterpret_cast<const uint4*>(p.x + static_cast<int64_t>(m0 + r) * p.ldx + k));
+        }
+      };
+      auto next_own = [&](int i) {
+        do ++i;
+        while ((i % NS) % C::kQuantWarps != qw);
+        return i;
+      };
+      int i_next = qw;
+      if (qw >= NS) i_next = nkb;  // fewer stages than warps: nothing to do
+      if (ok_start && i_next < nkb) fetch(kb0 + i_next);
+      while (ok_start && i_next < nkb) {
+        const int i = i_next;
+        const int s = i % NS;
+        uint4 v[kPairs];
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) v[j] = nxt[j];
+        i_next = next_own(i);
+        if (i_next < nkb) fetch(kb0 + i_next);
+        if (i >= NS && !mbar_wait_warp(&empty[s], ((i / NS) - 1) & 1, s_abort)) {
+          if (lane == 0) raise_error8(p.status, s_abort, kErrQuantF);
+          break;
+        }
+        uint8_t* tok = smem + C::offTok + s * C::kTokBytes;
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+          const int r = r0 + 2 * j;
+          if (2 * j < m_here) {  // uniform: one of the two rows is a token
+            const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+            uint32_t a = 0u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a = max(a, max((w[e] << 16) & 0x7FFF0000u, w[e] & 0x7FFF0000u));
+#pragma unroll
+            for (int o = 8; o; o >>= 1) a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
+            const float sc = block_scale(a, p.pow2 != 0), inv = block_inv(sc);
+            // the operand's 128-byte swizzle: 16-byte piece XOR row; columns past the last token stay what they
+            // were, their sums are never looked at
+            if (r < m_here) {
+              *reinterpret_cast<uint2*>(tok + r * kBlk + (((hl >> 1) ^ (r & 7)) << 4) + (hl & 1) * 8) = cast8(v[j], inv);
+              if (hl == 0) s_sc[s * BM + r] = sc;
+            }
+          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&tok_full[s]);
+      }
+    } else if (qw == 0) {
+      int s = 0;
+      uint32_t ph = 0;
+      for (int i = 0; ok_start && i < nkb; ++i) {
+        const float* src = p.sa + static_cast<int64_t>(kb0 + i) * p.M + m0;  // [segs][kblocks][M]
+        float v[BM / 32 + 1];
+#pragma unroll
+        for (int c = 0; c < BM; c += 32) v[c / 32] = c + lane < m_here ? __ldg(src + c + lane) : 0.0f;
+        if (i >= NS && !mbar_wait_warp(&empty[s], ph ^ 1, s_abort)) {
+          if (lane == 0) raise_error8(p.status, s_abort, kErrQuantF);
+          break;
+        }
+#pragma unroll
+        for (int c = 0; c < BM; c += 32)
+          if (c + lane < BM) s_sc[s * BM + c + lane] = v[c / 32];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&tok_full[s]);
+        if (++s == NS) {
+          s = 0;
+          ph ^= 1;
+        }
+      }
+    }
+  } else {
+    // ---- epilogue warps: running sums of one channel and all tokens
+    const int mat = warp >> 2;
+    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    bool failed = !ok_start;
+    int s = 0;
+    uint32_t ph = 0;
+    const float* sb0 = p.sb + static_cast<int64_t>(nt) * p.kblocks;
+    const int64_t sb_part = static_cast<int64_t>(p.nblocks) * p.kblocks;
+    auto weight_scale = [&](int kb) {
+      const int seg = kb / p.kblocks;
+      return __ldg(sb0 + (GATED ? mat : seg) * sb_part + (kb - seg * p.kblocks));
+    };
+    float sw_next = nkb > 0 ? weight_scale(kb0) : 0.0f;
+    pdl_wait();
+    for (int i = 0; i < nkb; ++i) {
+      const float sw = sw_next;
+      if (i + 1 < nkb) sw_next = weight_scale(kb0 + i + 1);
+      const int buf = i % C::kNB;
+      if (!failed && (!mbar_wait_warp(&tok_full[s], ph, s_abort) ||
+                      !mbar_wait_warp(&acc_full[buf], (i / C::kNB) & 1, s_abort))) {
+        if (lane == 0) raise_error8(p.status, s_abort, kErrEpilogueF);
+        failed = true;
+      }
+      tc_fence_after_sync();
+      if (!failed) {
+        const uint32_t t = tmem_base + (buf * C::kMats + mat) * BM + lane_base;
+        const float4* sc = reinterpret_cast<const float4*>(s_sc + s * BM);
+        float nxt[16];
+        tmem_ld16(t, nxt);
+#pragma unroll
+        for (int c = 0; c < BM; c += 16) {
+          float v[16];
+          tmem_ld_wait_regs<16>(nxt);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[e] = nxt[e];
+          if (c + 16 < BM) tmem_ld16(t + c + 16, nxt);
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const float4 f = sc[(c + e) / 4];
+            run[c + e] = fmaf(f.x * sw, v[e], run[c + e]);
+            run[c + e + 1] = fmaf(f.y * sw, v[e + 1], run[c + e + 1]);
+            run[c + e + 2] = fmaf(f.z * sw, v[e + 2], run[c + e + 2]);
+            run[c + e + 3] = fmaf(f.w * sw, v[e + 3], run[c + e + 3]);
+          }
+        }
+      }
+      tc_fence_before_sync();
+      __syncwarp();
+      // a warp that has given up counts itself in nowhere: nobody may take what it has not waited for as free
+      if (failed) break;
+      if (lane == 0) {
+        mbar_arrive(&acc_empty[buf]);
+        mbar_arrive(&empty[s]);
+      }
+      if (++s == NS) {
+        s = 0;
+        ph ^= 1;
+      }
+    }
+  }
+
+  // Every copy has landed and every MMA has completed once all roles are here: the stages' memory is free.
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  if (warp == C::kMmaWarp) tmem_dealloc(tmem_base, C::kTmemCols);
+  float* red = reinterpret_cast<float*>(smem);  // [kMats][BM][128]
+  if (warp < C::kEpiWarps) {
+#pragma unroll
+    for (int c = 0; c < BM; ++c) red[((warp >> 2) * BM + c) * 128 + (warp & 3) * 32 + lane] = run[c];
+  }
+  cluster_sync_all();
+  if (warp < C::kEpiWarps && *s_abort == 0) {
+    // group g of 128 threads finishes tokens rank * per + g, + groups, ...; thread = channel
+    const int grp = warp >> 2, ch = (warp & 3) * 32 + lane;
+    const int n = nt * kBlk + ch;
+    const bool n_ok = n < p.N;
+    const int per = BM / p.cluster;
+    const int c_end = min(m_here, (rank + 1) * per);
+    const uint32_t base = smem_u32(red) + ch * 4;
+    for (int c = rank * per + grp; c < c_end; c += C::kMats) {
+      const int64_t m = m0 + c;
+      float v[C::kMats];
+#pragma unroll
+      for (int mat = 0; mat < C::kMats; ++mat) {
+        v[mat] = 0.0f;
+        for (int r = 0; r < p.cluster; ++r) v[mat] += ld_cluster(map_to_rank(base + (mat * BM + c) * 512, r));
+      }
+      if (!GATED) {
+        if (n_ok) {
+          if (p.y_f32)
+            static_cast<float*>(p.y)[m * p.ldy + n] = v[0];
+          else
+            static_cast<__nv_bfloat16*>(p.y)[m * p.ldy + n] = __float2bfloat16_rn(v[0]);
+        }
+      } else {
+        const float g = v[0], u = v[C::kMats - 1];
+        // channels past N hold zeros (the copy engine filled their weights with zeros)
+        const float h = act_any(p.act, g) * u;
+        if (p.y && n_ok) static_cast<__nv_bfloat16*>(p.y)[m * p.ldy + n] = __float2bfloat16_rn(h);
+        if (p.q || p.ck) {
+          uint32_t a[3] = {abs_bits(h), abs_bits(g), abs_bits(u)};
+          uint32_t* mx = s_max + grp * 8;
+#pragma unroll
+          for (int j = 0; j < 3; ++j) {
+            if (j > 0 && !p.ck) break;
+            uint32_t b = a[j];
+#pragma unroll
+            for (int o = 16; o; o >>= 1) b = max(b, __shfl_xor_sync(0xFFFFFFFFu, b, o));
+            if (lane == 0) mx[warp & 3] = b;
+            named_bar_sync(1 + grp, 128);
+            b = max(max(mx[0], mx[1]), max(mx[2], mx[3]));
+            named_bar_sync(1 + grp, 128);
+            uint8_t* qd = j == 0 ? p.q : p.ck + (j - 1) * static_cast<int64_t>(p.M) * p.N;
+            float* sd = j == 0 ? p.s : p.cks + (j - 1) * static_cast<int64_t>(p.nblocks) * p.M;
+            if (j == 0 && !p.q) continue;
+            const float sc = block_scale(b, p.pow2 != 0), inv = block_inv(sc);
+            const float w = j == 0 ? h : (j == 1 ? g : u);
+            if (n_ok) qd[m * p.N + n] = static_cast<uint8_t>(cvt_e4m3x2(__fmul_rn(w, inv), 0.0f) & 0xFF);
+            if (ch == 0) sd[static_cast<int64_t>(nt) * p.M + m] = sc;
+          }
+        }
+      }
+    }
+  }
+  cluster_sync_all();  // nobody leaves while a peer reads its sums
+}
+
+template <int BM, bool GATED, bool RAW>
+int launch_cfg(const CUtensorMap& tw, const CUtensorMap& tq, const PF& p, int m_tiles, cudaStream_t st) {
+  using C = FewCfg<BM, GATED>;
+  static std::once_flag once;
+  static cudaError_t attr_err = cudaSuccess;
+  std::call_once(once, [] {
+    attr_err = cudaFuncSetAttribute(fp8_block_few_kernel<BM, GATED, RAW>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    C::kSmemBytes);
+  });
+  if (attr_err != cudaSuccess) return ZQ_ERR_CUDA;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(p.n_tiles * p.cluster), static_cast<unsigned>(m_tiles));
+  cfg.blockDim = dim3(C::kThreads);
+  cfg.dynamicSmemBytes = C::kSmemBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = static_cast<unsigned>(p.cluster);
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, fp8_block_few_kernel<BM, GATED, RAW>, tw, tq, p);
+  count_launch();
+  return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
+}
+
+template <int BM>
+constexpr int ctas_per_sm(bool gated) {
+  return gated ? FewCfg<BM, true>::kCtas : FewCfg<BM, false>::kCtas;
+}
+
+}  // namespace
+
+bool few_takes(const GemmArgs8& a) { return a.kind != kGatedBwd && a.M <= kFewTokens; }
+bool few_takes_raw(const GemmArgs8& a) { return few_takes(a) && a.M <= 16; }
+
+int launch_block_few(const GemmArgs8& a, cudaStream_t st) {
+  const bool gated = a.kind == kGated, raw = a.x != nullptr;
+  PF p{};
+  p.M = static_cast<int>(a.M);
+  p.N = static_cast<int>(a.N);
+  p.K = static_cast<int>(a.K);
+  p.kblocks = static_cast<int>(blocks_of(a.K));
+  p.segs = gated ? 1 : a.parts;
+  p.nblocks = p.n_tiles = static_cast<int>(blocks_of(a.N));
+  p.sa = a.sa;
+  p.sb = a.sb;
+  p.x = static_cast<const __nv_bfloat16*>(a.x);
+  p.ldx = a.ldx;
+  p.y = a.y;
+  p.ldy = a.ldy;
+  p.y_f32 = a.ydt == ZQ_OUT_F32;
+  p.q = a.q;
+  p.s = a.s;
+  p.ck = a.ck;
+  p.cks = a.cks;
+  p.act = a.act;
+  p.pow2 = a.mode == ZQ_SCALE_M1;
+  p.status = a.status;
+  const int bm = a.M <= 16 ? 16 : (a.M <= 32 ? 32 : 64);
+  const int slots = sm_count() * (bm == 16 ? ctas_per_sm<16>(gated) : (bm == 32 ? ctas_per_sm<32>(gated) : ctas_per_sm<64>(gated)));
+  // the widest cluster with which all CTAs are resident at once and none has fewer than two K blocks
+  p.cluster = 1;
+  while (p.cluster < 8 && p.n_tiles * p.cluster * 2 <= slots && p.segs * p.kblocks >= p.cluster * 4) p.cluster *= 2;
+  if (static_cast<int64_t>(p.n_tiles) * p.cluster > 0x7FFFFFFF) return ZQ_ERR_SHAPE;
+  CUtensorMap tw, tq;
+  if (!make_code_map(&tw, a.b, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.N),
+                     gated ? 2u : static_cast<uint64_t>(p.segs), kBlk))
+    return ZQ_ERR_CUDA;
+  if (raw)
+    tq = tw;  // not used
+  else if (!make_code_map(&tq, a.a, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.M), static_cast<uint64_t>(p.segs),
+                          static_cast<uint32_t>(bm)))
+    return ZQ_ERR_CUDA;
+  if (gated) {
+    if (raw) return launch_cfg<16, true, true>(tw, tq, p, 1, st);
+    if (bm == 16) return launch_cfg<16, true, false>(tw, tq, p, 1, st);
+    if (bm == 32) return launch_cfg<32, true, false>(tw, tq, p, 1, st);
+    return launch_cfg<64, true, false>(tw, tq, p, 1, st);
+  }
+  if (raw) return launch_cfg<16, false, true>(tw, tq, p, 1, st);
+  if (bm == 16) return launch_cfg<16, false, false>(tw, tq, p, 1, st);
+  if (bm == 32) return launch_cfg<32, false, false>(tw, tq, p, 1, st);
+  return launch_cfg<64, false, false>(tw, tq, p, 1, st);
+}
+
+}  // namespace fp8b
+}  // namespace zq

@@ -258,14 +258,11 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
           }
         }
       }
-      if (failed) {
-        if (issuer) {
-          raise_error8(p.status, s_abort, kErrMma8);
-          umma_commit(drain_bar);  // let the MMAs already issued finish before tensor memory is released
-        }
-        uint32_t spin = 0;
-        while (!mbar_try_wait(drain_bar, 0) && ++spin < kSpinLimit) {
-        }
+      if (failed && issuer) raise_error8(p.status, s_abort, kErrMma8);
+      // tensor memory is released only when every MMA has completed, also where another role has given up
+      if (issuer) umma_commit(drain_bar);
+      uint32_t spin = 0;
+      while (!mbar_try_wait(drain_bar, 0) && ++spin < kSpinLimit) {
       }
       __syncwarp();
     }
@@ -323,7 +320,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         }
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&acc_empty[b]);
+        if (lane == 0 && !failed) mbar_arrive(&acc_empty[b]);
       }
       const int wm0 = m0 + quarter * 32;
       const int rows = failed ? 0 : min(32, p.M - wm0);  // may be <= 0

@@ -215,14 +215,11 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
           }
         }
       }
-      if (failed) {
-        if (issuer) {
-          raise_error8(p.status, s_abort, kErrMmaW);
-          umma_commit(drain_bar);
-        }
-        uint32_t spin = 0;
-        while (!mbar_try_wait(drain_bar, 0) && ++spin < kSpinLimit) {
-        }
+      if (failed && issuer) raise_error8(p.status, s_abort, kErrMmaW);
+      // tensor memory is released only when every MMA has completed, also where another role has given up
+      if (issuer) umma_commit(drain_bar);
+      uint32_t spin = 0;
+      while (!mbar_try_wait(drain_bar, 0) && ++spin < kSpinLimit) {
       }
       __syncwarp();
     }

@@ -115,7 +115,8 @@ def test_quantize_weight_and_transpose(N, K, mode):
 # ---- linear ------------------------------------------------------------------------------------------------------------
 LINEAR = [(1, 16, 1), (1, 128, 128), (1, 4096, 300), (2, 528, 129), (7, 144, 1000), (16, 2048, 128), (17, 1040, 1001),
           (33, 272, 257), (64, 1536, 640), (65, 400, 2), (100, 1040, 1001), (129, 256, 384), (130, 2064, 513),
-          (257, 144, 255), (500, 640, 900)]
+          (257, 144, 255), (500, 640, 900),
+          (2, 8192, 130), (16, 8208, 128), (40, 8192, 130)]  # long rows: every ring of the kernels wraps around
 
 
 @pytest.mark.parametrize("M,K,N", LINEAR)
@@ -218,7 +219,7 @@ def quantized_values(b, i=None):
 
 
 GATED = [(1, 16, 16), (1, 512, 400), (3, 144, 128), (16, 1040, 272), (30, 256, 144), (64, 272, 640), (70, 528, 720),
-         (130, 400, 144), (300, 144, 272)]
+         (130, 400, 144), (300, 144, 272), (1, 8192, 144), (16, 8208, 128)]
 
 
 @pytest.mark.parametrize("M,K,F", GATED)
