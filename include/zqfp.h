@@ -424,6 +424,32 @@ int zq_fp8_weight_grad(const void* g_bf16, int64_t ldg, int64_t g_stride, int pa
                        int64_t M, int64_t N, int64_t K, void* dw, zq_out_dtype dwdt, void* workspace,
                        size_t workspace_bytes, void* stream);
 
+/*
+ * The gated feed-forward block in one call, for callers who want nothing of what is in between: the calls above strung
+ * together,  y = (act(x Wg^T) (x Wu^T)) Wd^T,  x quantized with `mode`, h handed on in its quantized form.
+ * gate_up : [2][F, K] codes, gate_ups their scales;  down : [N, F] codes, downs their scales
+ * y       : out [M, ldy], FP32 or bf16;  F % 16 == 0, any N
+ * saved   : out or NULL (serving): zq_fp8_gated_ffn_saved_bytes(M, K, F) bytes, 256-byte aligned: the 8-bit
+ *           checkpoints of x, g, u and h with their scales, for zq_fp8_gated_ffn_backward
+ * workspace : zq_fp8_gated_ffn_workspace_bytes(M, K, F, N, training) bytes, as above (training = 0 is enough for
+ *           this call); one for M rows serves fewer.
+ */
+size_t zq_fp8_gated_ffn_saved_bytes(int64_t M, int64_t K, int64_t F);
+size_t zq_fp8_gated_ffn_workspace_bytes(int64_t M, int64_t K, int64_t F, int64_t N, int training);
+int zq_fp8_gated_ffn(const void* x_bf16, int64_t ldx, zq_scale_mode mode, int64_t M, int64_t K, int64_t F, int64_t N,
+                     const uint8_t* gate_up, const float* gate_ups, const uint8_t* down, const float* downs,
+                     zq_activation act, void* y, zq_out_dtype ydt, int64_t ldy, void* saved, void* workspace,
+                     size_t workspace_bytes, void* stream);
+/*
+ * Its backward pass:  dx = dg^ Wg + du^ Wu [M, K],  dW of (gate, up) [2][F, K],  dW of down [N, F], all of type `dt`,
+ * dense.  gate_up_t : [2][K, F] and down_t : [F, N], the transposed weights (so K % 16 == 0 and N % 16 == 0);
+ * workspace with training = 1.
+ */
+int zq_fp8_gated_ffn_backward(const void* dy_bf16, int64_t lddy, zq_scale_mode mode, int64_t M, int64_t K, int64_t F,
+                              int64_t N, const void* saved, const uint8_t* gate_up_t, const float* gate_up_ts,
+                              const uint8_t* down_t, const float* down_ts, zq_activation act, void* dx, void* dw_gate_up,
+                              void* dw_down, zq_out_dtype dt, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Number of kernels of this library launched by the calling process so far (all entry points). */
 int64_t zq_launch_count(void);
 

@@ -30,7 +30,8 @@ EXPORTS = [
     "zq_w4a8_linear_fused_out", "zq_quantize_act_fp8_scaled", "zq_set_exclusive_device",
     "zq_quantize_fp8_block", "zq_quantize_weight_fp8_block", "zq_transpose_weight_fp8_block",
     "zq_fp8_block_workspace_bytes", "zq_fp8_block_linear", "zq_fp8_gated_linear", "zq_fp8_gated_linear_backward",
-    "zq_fp8_weight_grad",
+    "zq_fp8_weight_grad", "zq_fp8_gated_ffn_saved_bytes", "zq_fp8_gated_ffn_workspace_bytes", "zq_fp8_gated_ffn",
+    "zq_fp8_gated_ffn_backward",
 ]
 ACT_SILU, ACT_GELU_TANH, ACT_RELU = 0, 1, 2
 ACTIVATIONS = {"silu": ACT_SILU, "gelu_tanh": ACT_GELU_TANH, "relu": ACT_RELU}
@@ -114,6 +115,15 @@ def lib() -> C.CDLL:
         L.zq_fp8_gated_linear_backward.restype = ci
         L.zq_fp8_gated_linear_backward.argtypes = [vp, vp, vp, i64, ci, i64, i64, i64, vp, vp, ci, vp, vp, vp, vp, vp, vp,
                                                    sz, vp]
+        L.zq_fp8_gated_ffn_saved_bytes.restype = sz
+        L.zq_fp8_gated_ffn_saved_bytes.argtypes = [i64, i64, i64]
+        L.zq_fp8_gated_ffn_workspace_bytes.restype = sz
+        L.zq_fp8_gated_ffn_workspace_bytes.argtypes = [i64, i64, i64, i64, ci]
+        L.zq_fp8_gated_ffn.restype = ci
+        L.zq_fp8_gated_ffn.argtypes = [vp, i64, ci, i64, i64, i64, i64, vp, vp, vp, vp, ci, vp, ci, i64, vp, vp, sz, vp]
+        L.zq_fp8_gated_ffn_backward.restype = ci
+        L.zq_fp8_gated_ffn_backward.argtypes = [vp, i64, ci, i64, i64, i64, i64, vp, vp, vp, vp, vp, ci, vp, vp, vp, ci, vp,
+                                                sz, vp]
         L.zq_fp8_weight_grad.restype = ci
         L.zq_fp8_weight_grad.argtypes = [vp, i64, i64, ci, vp, vp, i64, i64, i64, vp, ci, vp, sz, vp]
         _lib = L
@@ -142,11 +152,12 @@ def _layout(layout) -> int:
 
 
 def _ptr(t: Optional[torch.Tensor]):
-    return None if t is None else C.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    """The current stream's handle (torch.cuda.current_stream().cuda_stream, without building a Stream object: 3 us)."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _check(status: int, where: str):
@@ -386,7 +397,8 @@ def _rows(x: torch.Tensor, name: str) -> int:
     if x.dtype != torch.bfloat16 or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
         raise ValueError(f"{name}: a bf16 matrix with contiguous rows is needed, got {x.dtype} {tuple(x.shape)}, "
                          f"strides {x.stride()}")
-    return x.stride(0) if x.shape[0] > 1 else max(x.shape[1], (x.shape[1] + 7) // 8 * 8)
+    M, K = x.shape
+    return x.stride(0) if M > 1 else (K + 7) // 8 * 8
 
 
 def fp8_block_linear_workspace_bytes(M: int, N: int, K: int) -> int:
@@ -456,8 +468,19 @@ def _activations(x, q, K: int, parts: int):
     return q.codes, q.scale, None, K, M
 
 
+_fp8_workspaces = {}
+
+
 def _fp8_workspace(workspace, M: int, K: int, device):
-    return make_workspace(lib().zq_fp8_block_workspace_bytes(M, K), device) if workspace is None else workspace
+    """The caller's workspace, or one that is kept per device and stream and grown on demand."""
+    if workspace is not None:
+        return workspace
+    key = (device, _stream())
+    need = lib().zq_fp8_block_workspace_bytes(M, K)
+    ws = _fp8_workspaces.get(key)
+    if ws is None or ws.numel() < need:
+        ws = _fp8_workspaces[key] = make_workspace(need, device)
+    return ws
 
 
 def fp8_block_linear(w: Fp8Weight, *, x=None, q: Optional[Fp8Block] = None, mode="none", out_dtype=torch.float32, y=None,
@@ -545,3 +568,56 @@ def fp8_weight_grad(g: torch.Tensor, q: Fp8Block, *, out_dtype=torch.float32,
                                     M, N, K, _ptr(dw), OUT_F32 if out_dtype == torch.float32 else OUT_BF16,
                                     _ptr(workspace), workspace.numel(), _stream()), "zq_fp8_weight_grad")
     return dw
+
+
+def fp8_gated_ffn_saved_bytes(M: int, K: int, F: int) -> int:
+    return int(lib().zq_fp8_gated_ffn_saved_bytes(M, K, F))
+
+
+def fp8_gated_ffn_workspace_bytes(M: int, K: int, F: int, N: int, training: bool = False) -> int:
+    return int(lib().zq_fp8_gated_ffn_workspace_bytes(M, K, F, N, 1 if training else 0))
+
+
+def fp8_gated_ffn(gate_up: Fp8Weight, down: Fp8Weight, x: torch.Tensor, *, act="silu", mode="none",
+                  out_dtype=torch.bfloat16, save=False, workspace: torch.Tensor):
+    """The gated feed-forward block in one call: y = (act(x Wg^T) * (x Wu^T)) Wd^T.  With ``save`` returns (y, the uint8
+    buffer that :func:`fp8_gated_ffn_backward` reads), else y."""
+    ldx = _rows(x, "x")
+    M, K = x.shape
+    F, N = gate_up.N, down.N
+    if gate_up.parts != 2 or down.parts != 1 or gate_up.K != K or down.K != F:
+        raise ValueError(f"x [{M}, {K}], gate_up {gate_up.parts} x [{F}, {gate_up.K}] and down [{N}, {down.K}] do not belong "
+                         "together")
+    y = torch.empty((M, N), dtype=out_dtype, device=x.device)
+    saved = torch.empty((fp8_gated_ffn_saved_bytes(M, K, F),), dtype=torch.uint8, device=x.device) if save else None
+    _check(lib().zq_fp8_gated_ffn(x.data_ptr(), ldx, _mode(mode), M, K, F, N, gate_up.codes.data_ptr(),
+                                  gate_up.scale.data_ptr(), down.codes.data_ptr(), down.scale.data_ptr(), _act(act),
+                                  y.data_ptr(), OUT_F32 if out_dtype == torch.float32 else OUT_BF16, N, _ptr(saved),
+                                  workspace.data_ptr(), workspace.numel(), _stream()), "zq_fp8_gated_ffn")
+    return (y, saved) if save else y
+
+
+def fp8_gated_ffn_backward(gate_up_t: Fp8Weight, down_t: Fp8Weight, dy: torch.Tensor, saved: torch.Tensor, *, act="silu",
+                           mode="none", out_dtype=torch.bfloat16, workspace: torch.Tensor):
+    """(dx [M, K], dW of (gate, up) [2, F, K], dW of down [N, F]) from dy bf16 [M, N], the transposed weights and what
+    :func:`fp8_gated_ffn` saved."""
+    lddy = _rows(dy, "dy")
+    M, N = dy.shape
+    F, K = down_t.N, gate_up_t.N
+    if gate_up_t.parts != 2 or down_t.parts != 1 or gate_up_t.K != F or down_t.K != N:
+        raise ValueError(f"dy [{M}, {N}], gate_up_t {gate_up_t.parts} x [{K}, {gate_up_t.K}] and down_t [{F}, {down_t.K}] do "
+                         "not belong together")
+    _expect(saved, torch.uint8, "saved")
+    if saved.numel() != fp8_gated_ffn_saved_bytes(M, K, F):
+        raise ValueError(f"what was saved ({saved.numel()} bytes) is not of {M} tokens")
+    dev = dy.device
+    dx = torch.empty((M, K), dtype=out_dtype, device=dev)
+    dwgu = torch.empty((2, F, K), dtype=out_dtype, device=dev)
+    dwd = torch.empty((N, F), dtype=out_dtype, device=dev)
+    _check(lib().zq_fp8_gated_ffn_backward(dy.data_ptr(), lddy, _mode(mode), M, K, F, N, saved.data_ptr(),
+                                           gate_up_t.codes.data_ptr(), gate_up_t.scale.data_ptr(),
+                                           down_t.codes.data_ptr(), down_t.scale.data_ptr(), _act(act), dx.data_ptr(),
+                                           dwgu.data_ptr(), dwd.data_ptr(),
+                                           OUT_F32 if out_dtype == torch.float32 else OUT_BF16, workspace.data_ptr(),
+                                           workspace.numel(), _stream()), "zq_fp8_gated_ffn_backward")
+    return dx, dwgu, dwd

@@ -229,4 +229,128 @@ int zq_fp8_weight_grad(const void* g_bf16, int64_t ldg, int64_t g_stride, int pa
   return launch_wgrad(a, st);
 }
 
+namespace {
+
+// What the block keeps for its backward pass.
+struct Saved {
+  size_t xq, xs, gu, gus, hq, hs, total;
+};
+Saved saved_layout(int64_t M, int64_t K, int64_t F) {
+  Saved v{};
+  const size_t m = static_cast<size_t>(M), kb = static_cast<size_t>(blocks_of(K)), fb = static_cast<size_t>(blocks_of(F));
+  v.xs = v.xq + up256(m * K);
+  v.gu = v.xs + up256(kb * m * 4);
+  v.gus = v.gu + up256(2 * m * F);
+  v.hq = v.gus + up256(2 * fb * m * 4);
+  v.hs = v.hq + up256(m * F);
+  v.total = v.hs + up256(fb * m * 4);
+  return v;
+}
+// Workspace of the whole block: the head, then the quantized input of the pass (x or dy), then either h or the
+// gradients of g and u in bf16 and quantized.
+struct WsFfn {
+  size_t hq, hs, d, dq, ds, total;
+};
+WsFfn ws_ffn(int64_t M, int64_t K, int64_t F, int64_t N, bool training) {
+  WsFfn v{};
+  const size_t m = static_cast<size_t>(M), fb = static_cast<size_t>(blocks_of(F));
+  const size_t in_x = ws8(M, K).total, in_dy = training ? ws8(M, N).total : 0;
+  v.hq = v.d = in_x > in_dy ? in_x : in_dy;
+  v.hs = v.hq + up256(m * F);
+  v.total = v.hs + up256(fb * m * 4);
+  v.dq = v.d + up256(4 * m * F);
+  v.ds = v.dq + up256(2 * m * F);
+  const size_t bwd = v.ds + up256(2 * fb * m * 4);
+  if (training && bwd > v.total) v.total = bwd;
+  return v;
+}
+bool ffn_sizes_ok(int64_t M, int64_t K, int64_t F, int64_t N) {
+  return rows_ok(M) && k_ok(K) && k_ok(F) && rows_ok(N);
+}
+
+}  // namespace
+
+size_t zq_fp8_gated_ffn_saved_bytes(int64_t M, int64_t K, int64_t F) {
+  return ffn_sizes_ok(M, K, F, 0) ? saved_layout(M, K, F).total : 0;
+}
+
+size_t zq_fp8_gated_ffn_workspace_bytes(int64_t M, int64_t K, int64_t F, int64_t N, int training) {
+  if (!ffn_sizes_ok(M, K, F, N) || (training && !k_ok(N))) return 0;
+  return ws_ffn(M, K, F, N, training != 0).total;
+}
+
+int zq_fp8_gated_ffn(const void* x, int64_t ldx, zq_scale_mode mode, int64_t M, int64_t K, int64_t F, int64_t N,
+                     const uint8_t* gate_up, const float* gate_ups, const uint8_t* down, const float* downs,
+                     zq_activation act, void* y, zq_out_dtype ydt, int64_t ldy, void* saved, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+  // everything the second call would refuse is refused before the first one launches
+  if (!scale_rule_ok(mode) || !act_ok(act) || (ydt != ZQ_OUT_F32 && ydt != ZQ_OUT_BF16)) return ZQ_ERR_MODE;
+  if (!ffn_sizes_ok(M, K, F, N) || ldx < K || ldy < N) return ZQ_ERR_SHAPE;
+  if (M == 0) return ZQ_OK;
+  if (!x || !gate_up || !gate_ups || (N > 0 && (!down || !downs || !y))) return ZQ_ERR_NULL;
+  if (!al16(x) || ldx % 8 || !al16(gate_up) || !al16(down) || (reinterpret_cast<uintptr_t>(saved) & 255u) ||
+      (reinterpret_cast<uintptr_t>(y) & (ydt == ZQ_OUT_F32 ? 3u : 1u)))
+    return ZQ_ERR_ALIGN;
+  if (!workspace) return ZQ_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return ZQ_ERR_ALIGN;
+  const WsFfn w = ws_ffn(M, K, F, N, false);
+  if (workspace_bytes < w.total) return ZQ_ERR_WORKSPACE;
+  uint8_t* base = static_cast<uint8_t*>(workspace);
+  if (!saved) {
+    uint8_t* hq = base + w.hq;
+    float* hs = reinterpret_cast<float*>(base + w.hs);
+    if (int e = zq_fp8_gated_linear(nullptr, nullptr, x, ldx, mode, M, F, K, gate_up, gate_ups, act, nullptr, 0, hq, hs,
+                                    nullptr, nullptr, workspace, workspace_bytes, stream))
+      return e;
+    return zq_fp8_block_linear(hq, hs, nullptr, 0, mode, 1, M, N, F, down, downs, y, ydt, ldy, workspace, workspace_bytes,
+                               stream);
+  }
+  const Saved v = saved_layout(M, K, F);
+  uint8_t* sv = static_cast<uint8_t*>(saved);
+  uint8_t* xq = sv + v.xq;
+  float* xs = reinterpret_cast<float*>(sv + v.xs);
+  uint8_t* hq = sv + v.hq;
+  float* hs = reinterpret_cast<float*>(sv + v.hs);
+  if (int e = zq_quantize_fp8_block(x, M, K, ldx, mode, xq, xs, stream)) return e;
+  if (int e = zq_fp8_gated_linear(xq, xs, nullptr, 0, mode, M, F, K, gate_up, gate_ups, act, nullptr, 0, hq, hs, sv + v.gu,
+                                  reinterpret_cast<float*>(sv + v.gus), workspace, workspace_bytes, stream))
+    return e;
+  return zq_fp8_block_linear(hq, hs, nullptr, 0, mode, 1, M, N, F, down, downs, y, ydt, ldy, workspace, workspace_bytes,
+                             stream);
+}
+
+int zq_fp8_gated_ffn_backward(const void* dy, int64_t lddy, zq_scale_mode mode, int64_t M, int64_t K, int64_t F, int64_t N,
+                              const void* saved, const uint8_t* gate_up_t, const float* gate_up_ts, const uint8_t* down_t,
+                              const float* down_ts, zq_activation act, void* dx, void* dw_gate_up, void* dw_down,
+                              zq_out_dtype dt, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!scale_rule_ok(mode) || !act_ok(act) || (dt != ZQ_OUT_F32 && dt != ZQ_OUT_BF16)) return ZQ_ERR_MODE;
+  if (!ffn_sizes_ok(M, K, F, N) || !k_ok(N) || lddy < N) return ZQ_ERR_SHAPE;
+  if (!dw_gate_up || !dw_down || (M > 0 && (!dy || !saved || !gate_up_t || !gate_up_ts || !down_t || !down_ts || !dx)))
+    return ZQ_ERR_NULL;
+  if (!al16(dy) || lddy % 8 || !al16(gate_up_t) || !al16(down_t) || !al16(dw_gate_up) || !al16(dw_down) ||
+      (reinterpret_cast<uintptr_t>(saved) & 255u) || (reinterpret_cast<uintptr_t>(dx) & (dt == ZQ_OUT_F32 ? 3u : 1u)))
+    return ZQ_ERR_ALIGN;
+  if (!workspace) return ZQ_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return ZQ_ERR_ALIGN;
+  const WsFfn w = ws_ffn(M, K, F, N, true);
+  if (workspace_bytes < w.total) return ZQ_ERR_WORKSPACE;
+  const Saved v = saved_layout(M, K, F);
+  const uint8_t* sv = static_cast<const uint8_t*>(saved);
+  uint8_t* base = static_cast<uint8_t*>(workspace);
+  uint8_t* dq = base + w.dq;
+  float* ds = reinterpret_cast<float*>(base + w.ds);
+  if (int e = zq_fp8_gated_linear_backward(nullptr, nullptr, dy, lddy, mode, M, F, N, down_t, down_ts, act, sv + v.gu,
+                                           reinterpret_cast<const float*>(sv + v.gus), base + w.d, dq, ds, workspace,
+                                           workspace_bytes, stream))
+    return e;
+  if (int e = zq_fp8_block_linear(dq, ds, nullptr, 0, mode, 2, M, K, F, gate_up_t, gate_up_ts, dx, dt, K, workspace,
+                                  workspace_bytes, stream))
+    return e;
+  if (int e = zq_fp8_weight_grad(base + w.d, F, M * F, 2, sv + v.xq, reinterpret_cast<const float*>(sv + v.xs), M, F, K,
+                                 dw_gate_up, dt, workspace, workspace_bytes, stream))
+    return e;
+  return zq_fp8_weight_grad(dy, lddy, 0, 1, sv + v.hq, reinterpret_cast<const float*>(sv + v.hs), M, N, F, dw_down, dt,
+                            workspace, workspace_bytes, stream);
+}
+
 }  // extern "C"

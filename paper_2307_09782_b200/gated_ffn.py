@@ -1,23 +1,15 @@
 """The gated feed-forward block on the FP8 operators with block scales: y = (act(x Wg^T) * (x Wu^T)) Wd^T, for serving and
-for training with 8-bit activation checkpoints.  It only strings the calls of :mod:`binding` together.
+for training with 8-bit activation checkpoints.  It keeps the weights and
+the workspaces; the work is done by the calls of :mod:`binding`.
 """
 from __future__ import annotations
 
-from dataclasses import dataclass
 from typing import Optional
 
 import torch
 
 from . import binding
-from .binding import Fp8Block, Fp8Weight
-
-
-@dataclass
-class SavedActivations:
-    """What a training pass keeps for its backward pass: x, (g, u) and h, all in 8 bits."""
-    x: Fp8Block
-    gu: Fp8Block
-    h: Fp8Block
+from .binding import Fp8Weight
 
 
 class GatedFfnFp8:
@@ -49,36 +41,27 @@ class GatedFfnFp8:
 
     def workspace(self, M: int) -> torch.Tensor:
         dev = self.down.codes.device
-        key = (dev, torch.cuda.current_stream(dev).cuda_stream)
-        need = binding.fp8_block_linear_workspace_bytes(M, 0, max(self.gate_up.K, self.down.N))
-        ws = self._workspaces.get(key)
-        if ws is None or ws.numel() < need:
-            ws = self._workspaces[key] = binding.make_workspace(need, dev)
+        key = (dev, binding._stream())
+        ws, rows = self._workspaces.get(key, (None, -1))
+        if rows < M:
+            ws = binding.make_workspace(binding.fp8_gated_ffn_workspace_bytes(M, self.gate_up.K, self.gate_up.N, self.down.N,
+                                                                              self.down_t is not None), dev)
+            self._workspaces[key] = (ws, M)
         return ws
 
     def forward(self, x: torch.Tensor, out_dtype=torch.bfloat16) -> torch.Tensor:
         """x bf16 [M, K] -> y [M, K_out]; h goes from one kernel to the next in its quantized form."""
-        ws = self.workspace(x.shape[0])
-        _, h, _ = binding.fp8_gated_linear(self.gate_up, x=x, act=self.act, mode=self.mode, bf16=False, quantized=True,
-                                           workspace=ws)
-        return binding.fp8_block_linear(self.down, q=h, out_dtype=out_dtype, workspace=ws)
+        return binding.fp8_gated_ffn(self.gate_up, self.down, x, act=self.act, mode=self.mode, out_dtype=out_dtype,
+                                     workspace=self.workspace(x.shape[0]))
 
     def forward_train(self, x: torch.Tensor, out_dtype=torch.bfloat16):
-        """(y, what :meth:`backward` needs)."""
-        ws = self.workspace(x.shape[0])
-        xq = binding.quantize_fp8_block(x, self.mode)
-        _, h, gu = binding.fp8_gated_linear(self.gate_up, q=xq, act=self.act, mode=self.mode, bf16=False, quantized=True,
-                                            checkpoint=True, workspace=ws)
-        return binding.fp8_block_linear(self.down, q=h, out_dtype=out_dtype, workspace=ws), SavedActivations(xq, gu, h)
+        """(y, what :meth:`backward` needs: x, gate, up and h as 8-bit checkpoints in one buffer)."""
+        return binding.fp8_gated_ffn(self.gate_up, self.down, x, act=self.act, mode=self.mode, out_dtype=out_dtype,
+                                     save=True, workspace=self.workspace(x.shape[0]))
 
-    def backward(self, dy: torch.Tensor, saved: SavedActivations, out_dtype=torch.bfloat16):
+    def backward(self, dy: torch.Tensor, saved: torch.Tensor, out_dtype=torch.bfloat16):
         """dy bf16 [M, K_out] -> (dx [M, K], dW of (gate, up) [2, F, K], dW of down [K_out, F])."""
         if self.down_t is None or self.gate_up_t is None:
             raise ValueError("the backward pass needs the transposed weights: construct the block with training=True")
-        ws = self.workspace(dy.shape[0])
-        dgu, dguq = binding.fp8_gated_linear_backward(self.down_t, saved.gu, dy=dy, act=self.act, mode=self.mode,
-                                                      workspace=ws)
-        dx = binding.fp8_block_linear(self.gate_up_t, q=dguq, out_dtype=out_dtype, workspace=ws)
-        dwgu = binding.fp8_weight_grad(dgu, saved.x, out_dtype=out_dtype, workspace=ws)
-        dwd = binding.fp8_weight_grad(dy, saved.h, out_dtype=out_dtype, workspace=ws)
-        return dx, dwgu, dwd
+        return binding.fp8_gated_ffn_backward(self.gate_up_t, self.down_t, dy, saved, act=self.act, mode=self.mode,
+                                              out_dtype=out_dtype, workspace=self.workspace(dy.shape[0]))

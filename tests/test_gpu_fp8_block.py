@@ -395,6 +395,14 @@ def test_block_step(M, mode):
     assert torch.equal(y, y0)
     dx, dwgu, dwd = ffn.backward(dyt, saved)
     ok(ffn.workspace(M))
+    # the calls it strings together give the same bits
+    xq = binding.quantize_fp8_block(xt, mode)
+    h, hq, gu = binding.fp8_gated_linear(ffn.gate_up, q=xq, mode=mode, quantized=True, checkpoint=True)
+    assert torch.equal(y, binding.fp8_block_linear(ffn.down, q=hq, out_dtype=torch.bfloat16))
+    d, dq = binding.fp8_gated_linear_backward(ffn.down_t, gu, dy=dyt, mode=mode)
+    assert torch.equal(dx, binding.fp8_block_linear(ffn.gate_up_t, q=dq, out_dtype=torch.bfloat16))
+    assert torch.equal(dwgu, binding.fp8_weight_grad(d, xq, out_dtype=torch.bfloat16))
+    assert torch.equal(dwd, binding.fp8_weight_grad(dyt, hq, out_dtype=torch.bfloat16))
 
     def fq(v):
         return R.rows_values(*R.quantize_rows(np.asarray(v, np.float32), mode))
