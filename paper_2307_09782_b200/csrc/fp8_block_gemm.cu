@@ -103,36 +103,38 @@ __device__ __forceinline__ void store_rows(const uint4* buf, uint8_t* dst, int64
   }
   __syncwarp();
 }
-template <int PIECES>
-__device__ __forceinline__ void load_rows(uint4* buf, const uint8_t* src, int64_t ld_bytes, int rows, int bytes, int lane) {
-  __syncwarp();
-  constexpr int kRowsPer = 32 / PIECES;
-#pragma unroll
-  for (int it = 0; it < PIECES; ++it) {
-    const int r = it * kRowsPer + lane / PIECES, c = lane % PIECES;
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (r < rows && c * 16 < bytes) v = __ldg(reinterpret_cast<const uint4*>(src + r * ld_bytes + c * 16));
-    buf[r * 8 + (c ^ (r & 7))] = v;
-  }
-  __syncwarp();
-}
-
-// Accumulator columns [col, col + 16 * NCH) -> run (packed pairs) += s * columns, the next 16 in flight meanwhile.
+// Accumulator columns [taddr, taddr + 32 * NCH) -> run (packed pairs) += s * columns, the next 32 in flight meanwhile.
 template <int NCH>
 __device__ __forceinline__ void promote(uint32_t taddr, uint64_t* run, float s) {
   const uint64_t s2 = pack2(s, s);
-  float nxt[16];
-  tmem_ld16(taddr, nxt);
+  float a[32], b[32];
+  tmem_ld32(taddr, a);
 #pragma unroll
-  for (int c = 0; c < NCH; ++c) {
-    float v[16];
-    tmem_ld_wait_regs<16>(nxt);
+  for (int c = 0; c < NCH; c += 2) {
+    tmem_ld_wait32(a);
+    if (c + 1 < NCH) tmem_ld32(taddr + 32 * (c + 1), b);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) v[e] = nxt[e];
-    if (c + 1 < NCH) tmem_ld16(taddr + 16 * (c + 1), nxt);
+    for (int e = 0; e < 16; ++e) run[c * 16 + e] = fma2(s2, pack2(a[2 * e], a[2 * e + 1]), run[c * 16 + e]);
+    if (c + 1 < NCH) {
+      tmem_ld_wait32(b);
+      if (c + 2 < NCH) tmem_ld32(taddr + 32 * (c + 2), a);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) run[c * 8 + e] = fma2(s2, pack2(v[2 * e], v[2 * e + 1]), run[c * 8 + e]);
+      for (int e = 0; e < 16; ++e) run[(c + 1) * 16 + e] = fma2(s2, pack2(b[2 * e], b[2 * e + 1]), run[(c + 1) * 16 + e]);
+    }
   }
+}
+
+// run[0 .. N) moves to the end: a rolled loop over N sums at a time works on run[0 .. N) and rotates, so that its code is
+// fetched once instead of once per chunk (fully unrolled, the gradient epilogue took 35 us per tile for its instructions).
+template <int N>
+__device__ __forceinline__ void rotate(uint64_t* run) {
+  uint64_t t[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) t[e] = run[e];
+#pragma unroll
+  for (int e = 0; e + N < 64; ++e) run[e] = run[e + N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) run[64 - N + e] = t[e];
 }
 
 template <int KIND, int ACT, bool F32>
@@ -304,7 +306,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
           }
         }
         const int b = count & 1;
-        if (!failed && !mbar_wait_warp(&acc_full[b], (count >> 1) & 1, s_abort)) {
+        if (!failed && !mbar_wait_all(&acc_full[b], (count >> 1) & 1, s_abort)) {
           if (lane == 0) raise_error8(p.status, s_abort, kErrEpilogue8);
           failed = true;
         }
@@ -312,10 +314,10 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         if (!failed) {
           const uint32_t t = tmem_base + b * kTileN + lane_base;
           if (KIND == kGated) {
-            promote<4>(t + half * 64, run, s0);
-            promote<4>(t + 128 + half * 64, run + 32, s1);
+            promote<2>(t + half * 64, run, s0);
+            promote<2>(t + 128 + half * 64, run + 32, s1);
           } else {
-            promote<8>(t + half * 128, run, s0);
+            promote<4>(t + half * 128, run, s0);
           }
         }
         tc_fence_before_sync();
@@ -423,68 +425,71 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
           sg = __ldg(p.cks + static_cast<int64_t>(fb) * p.M + m);
           su = __ldg(p.cks + SM + static_cast<int64_t>(fb) * p.M + m);
         }
-        const uint8_t* ck = p.ck + static_cast<int64_t>(wm0) * p.N + n0;
-        uint32_t gc[32];
-        load_rows<8>(buf, ck, p.N, rows, min(128, cols), lane);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint4 v = stage_get(buf, lane, j);
-          gc[4 * j] = v.x;
-          gc[4 * j + 1] = v.y;
-          gc[4 * j + 2] = v.z;
-          gc[4 * j + 3] = v.w;
+        // a thread reads its own row's codes, 16 of g and of u at a time (both halves of a 32-byte sector in turn), the
+        // next ones in flight; each pair of running sums (dh) is replaced by the bf16 pairs of dg and du
+        const uint4* gp = reinterpret_cast<const uint4*>(p.ck + static_cast<int64_t>(m_ok ? m : 0) * p.N + (any ? n0 : 0));
+        const uint4* up = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(gp) + MN);
+        const int pieces = m_ok && any ? min(8, cols >> 4) : 0;
+        uint4 gn = make_uint4(0u, 0u, 0u, 0u), un = gn;
+        if (pieces > 0) {
+          gn = __ldg(gp);
+          un = __ldg(up);
         }
-        load_rows<8>(buf, ck + MN, p.N, rows, min(128, cols), lane);
-        // each pair of running sums (dh) is replaced by the bf16 pairs of dg and du
         uint32_t ag = 0u, au = 0u;
-#pragma unroll
+#pragma unroll 1
         for (int j = 0; j < 8; ++j) {
-          const uint4 uv = stage_get(buf, lane, j);
-          const uint32_t uw[4] = {uv.x, uv.y, uv.z, uv.w};
+          const uint32_t gw[4] = {gn.x, gn.y, gn.z, gn.w}, uw[4] = {un.x, un.y, un.z, un.w};
+          gn = un = make_uint4(0u, 0u, 0u, 0u);
+          if (j + 1 < pieces) {
+            gn = __ldg(gp + j + 1);
+            un = __ldg(up + j + 1);
+          }
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {  // pair 8 j + e
-            const float2 gv = decode2(static_cast<uint16_t>(gc[4 * j + (e >> 1)] >> (16 * (e & 1))));
+          for (int e = 0; e < 8; ++e) {
+            const float2 gv = decode2(static_cast<uint16_t>(gw[e >> 1] >> (16 * (e & 1))));
             const float2 vv = decode2(static_cast<uint16_t>(uw[e >> 1] >> (16 * (e & 1))));
             float d0, d1, a0, a1, b0, b1;
-            unpack2(run[8 * j + e], d0, d1);
+            unpack2(run[e], d0, d1);
             act_both<ACT>(gv.x * sg, a0, b0);
             act_both<ACT>(gv.y * sg, a1, b1);
             const uint32_t dg = pack_bf16(d0 * (vv.x * su) * b0, d1 * (vv.y * su) * b1);
             const uint32_t du = pack_bf16(d0 * a0, d1 * a1);
             ag = max(ag, max((dg << 16) & 0x7FFF0000u, dg & 0x7FFF0000u));
             au = max(au, max((du << 16) & 0x7FFF0000u, du & 0x7FFF0000u));
-            run[8 * j + e] = (static_cast<uint64_t>(du) << 32) | dg;
+            run[e] = (static_cast<uint64_t>(du) << 32) | dg;
           }
+          rotate<8>(run);
         }
+        const float scg = block_scale(ag, p.pow2 != 0), scu = block_scale(au, p.pow2 != 0);
+        if (any && m_ok && !failed) {
+          p.s[static_cast<int64_t>(fb) * p.M + m] = scg;
+          p.s[SM + static_cast<int64_t>(fb) * p.M + m] = scu;
+        }
+        // (dg, du) x (first, second 64 columns)
+#pragma unroll 1
+        for (int it = 0; it < 4; ++it) {
+          const int part = it >> 1, c = it & 1;
+          const float inv = block_inv(part ? scu : scg);
+          uint32_t w[32];
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
-          const float sc = block_scale(part ? au : ag, p.pow2 != 0), inv = block_inv(sc);
-          if (any && m_ok && !failed) p.s[part * SM + static_cast<int64_t>(fb) * p.M + m] = sc;
+          for (int e = 0; e < 32; ++e) w[e] = part ? static_cast<uint32_t>(run[e] >> 32) : static_cast<uint32_t>(run[e]);
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            __syncwarp();
+          for (int j = 0; j < 8; ++j) stage_put(buf, lane, j, make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]));
+          const int64_t o = part * MN + static_cast<int64_t>(wm0) * p.N + n0 + 64 * c;
+          store_rows<8, 2>(buf, static_cast<uint8_t*>(p.y) + o * 2, static_cast<int64_t>(p.N) * 2, rows,
+                           min(128, (cols - 64 * c) * 2), true, lane);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              uint32_t w[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) w[e] = static_cast<uint32_t>(run[32 * c + 4 * j + e] >> (32 * part));
-              stage_put(buf, lane, j, make_uint4(w[0], w[1], w[2], w[3]));
-            }
-            store_rows<8, 2>(buf, static_cast<uint8_t*>(p.y) + (part * MN + static_cast<int64_t>(wm0) * p.N + n0 + 64 * c) * 2,
-                             static_cast<int64_t>(p.N) * 2, rows, min(128, (cols - 64 * c) * 2), true, lane);
-          }
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            uint32_t w[4];
+          for (int j = 0; j < 4; ++j) {
+            uint32_t o4[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const uint32_t lo = static_cast<uint32_t>(run[8 * j + 2 * e] >> (32 * part));
-              const uint32_t hi = static_cast<uint32_t>(run[8 * j + 2 * e + 1] >> (32 * part));
-              w[e] = cast4(bf16_lo(lo), bf16_hi(lo), bf16_lo(hi), bf16_hi(hi), inv);
+              const uint32_t lo = w[8 * j + 2 * e], hi = w[8 * j + 2 * e + 1];
+              o4[e] = cast4(bf16_lo(lo), bf16_hi(lo), bf16_lo(hi), bf16_hi(hi), inv);
             }
-            stage_put(buf, lane, j, make_uint4(w[0], w[1], w[2], w[3]));
+            stage_put(buf, lane, j, make_uint4(o4[0], o4[1], o4[2], o4[3]));
           }
-          store_rows<8, 1>(buf, p.q + part * MN + static_cast<int64_t>(wm0) * p.N + n0, p.N, rows, min(128, cols), true, lane);
+          store_rows<4, 1>(buf, p.q + o, p.N, rows, min(64, cols - 64 * c), true, lane);
+          rotate<32>(run);
         }
       }
     }

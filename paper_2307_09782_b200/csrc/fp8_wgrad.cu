@@ -8,12 +8,13 @@
 // Tile: 128 input features (the MMA's 128-row operand, converted once per 256 outputs) x 256 outputs, tokens by 64.
 // In memory both operands have the token index outermost, so both are MN-major for the tensor core: 64 elements
 // (128 bytes) of a token per row, 64 token rows = 8 KB per chunk of 64 columns, 128-byte swizzle.
-// Converters (4 warps, a token row and 64 features per thread) read a stage's 8 KB of codes, scale, round and write
+// Converters (a token row and 64 features per thread) read a stage's 8 KB of codes, scale, round and write
 // 16 KB of bf16 into a ring of their own; the gradient's tiles go from the copy engine to the tensor core untouched.
 // Per 64 tokens the MMAs take 512 cycles, the conversion about 180 issue slots of each SM quarter.
 //
 // Two accumulators of 256 columns: the stores of one tile overlap the sums of the next.
-// Warp roles: 0..3 epilogue, 4..7 converters, 8 producer, 9 tensor memory and MMAs.
+// Warp roles: 0..3 epilogue, 4..19 converters (four groups, each with a stage of its own), 20 producer, 21 tensor memory
+// and MMAs.
 #include "fp8_block.cuh"
 
 namespace zq {
@@ -26,7 +27,7 @@ constexpr int kGBytes = kTok * kTileN * 2;       // four chunks of 64 outputs x 
 constexpr int kXBytes = kTok * kTileK;           // codes
 constexpr int kCBytes = kTok * kTileK * 2;       // converted: two chunks of 64 features x 64 tokens
 constexpr int kChunk = kTok * 128;               // bytes of a chunk
-constexpr int kStages = 4, kConv = 3;
+constexpr int kStages = 4, kConv = 4;            // converter group c owns stage c and converted tile c
 constexpr int kOffG = 0;
 constexpr int kOffC = kOffG + kStages * kGBytes;
 constexpr int kOffX = kOffC + kConv * kCBytes;
@@ -35,7 +36,7 @@ constexpr int kNumBars = 2 * kStages + 2 * kConv + 4 + 1;
 constexpr int kOffMisc = kOffBars + kNumBars * 8;
 constexpr int kSmemBytes = kOffMisc + 16;
 static_assert(kSmemBytes <= 227 * 1024, "shared memory");
-constexpr int kConvWarp0 = 4, kProducerWarp = 8, kMmaWarp = 9, kThreads = 320;
+constexpr int kConvWarp0 = 4, kProducerWarp = 20, kMmaWarp = 21, kThreads = 704;
 
 enum { kErrProducerW = 31, kErrMmaW = 32, kErrEpilogueW = 33, kErrAlignW = 34, kErrConvertW = 35 };
 
@@ -224,30 +225,34 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
       __syncwarp();
     }
   } else if (warp >= kConvWarp0) {
-    // ---- converters: thread = token row (t % 64) and chunk of 64 features (t / 64)
-    const int t = threadIdx.x - kConvWarp0 * 32;
+    // ---- converters: group g (4 warps) takes every fourth stage; thread = token row (t % 64) and chunk of 64
+    // features (t / 64)
+    const int g = (warp - kConvWarp0) >> 2;
+    const int t = (threadIdx.x - kConvWarp0 * 32) & 127;
     const int row = t & 63, chunk = t >> 6;
     const int sw = row & 7;
+    const uint4* src = reinterpret_cast<const uint4*>(smem + kOffX + g * kXBytes + row * 128);
+    uint4* dst = reinterpret_cast<uint4*>(smem + kOffC + g * kCBytes + chunk * kChunk + row * 128);
     bool failed = !ok_start;
-    int s = 0, c = 0, n = 0;
-    uint32_t ph = 0, cph = 0;
+    int n0 = 0;  // stages before this tile
     pdl_wait();
-    for (int pos = blockIdx.x; !failed && pos < p.tiles; pos += gridDim.x) {
+    for (int pos = blockIdx.x; !failed && pos < p.tiles; pos += gridDim.x, n0 += p.steps) {
       int part, nt, kt;
       tile_of(p, pos, part, nt, kt);
       const float* sc = p.s + static_cast<int64_t>(kt) * p.M;
-      float s_next = row < p.M ? __ldg(sc + row) : 0.0f;
-      for (int i = 0; i < p.steps; ++i, ++n) {
+      int i = (g - n0) & 3;  // this group's first stage of the tile
+      int m_next = i * kTok + row;
+      float s_next = i < p.steps && m_next < p.M ? __ldg(sc + m_next) : 0.0f;
+      for (; i < p.steps; i += 4) {
         const float scale = s_next;
-        const int m_next = (i + 1) * kTok + row;
-        if (i + 1 < p.steps) s_next = m_next < p.M ? __ldg(sc + m_next) : 0.0f;
-        if (!mbar_wait_warp(&full[s], ph, s_abort) || (n >= kConv && !mbar_wait_warp(&conv_empty[c], cph ^ 1, s_abort))) {
+        m_next += 4 * kTok;
+        s_next = m_next < p.M ? __ldg(sc + m_next) : 0.0f;
+        const int use = (n0 + i) >> 2;  // use of stage g
+        if (!mbar_wait_all(&full[g], use & 1, s_abort) || (use > 0 && !mbar_wait_all(&conv_empty[g], (use - 1) & 1, s_abort))) {
           if (lane == 0) raise_error8(p.status, s_abort, kErrConvertW);
           failed = true;
           break;
         }
-        const uint4* src = reinterpret_cast<const uint4*>(smem + kOffX + s * kXBytes + row * 128);
-        uint4* dst = reinterpret_cast<uint4*>(smem + kOffC + c * kCBytes + chunk * kChunk + row * 128);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint4 v = src[(chunk * 4 + j) ^ sw];
@@ -263,15 +268,7 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
         }
         fence_proxy_async_smem();  // the tensor core reads what these stores wrote
         __syncwarp();
-        if (lane == 0) mbar_arrive(&conv_full[c]);
-        if (++s == kStages) {
-          s = 0;
-          ph ^= 1;
-        }
-        if (++c == kConv) {
-          c = 0;
-          cph ^= 1;
-        }
+        if (lane == 0) mbar_arrive(&conv_full[g]);
       }
     }
   } else {
