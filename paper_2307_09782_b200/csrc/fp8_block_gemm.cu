@@ -11,8 +11,8 @@
 // Tile: 128 tokens x 256 columns, two accumulators of 256 columns = all of tensor memory, eight epilogue warps
 // with 128 running sums per thread.
 //
-// Warp roles: 0..7 epilogue (lane quarter warp % 4, column half warp / 4), 8 producer, 9 tensor memory and MMAs
-// (10, 11 only complete their warpgroup).
+// Warp roles: 0..7 epilogue (lane quarter warp % 4, column half warp / 4), 8 producer, 9 tensor memory and MMAs,
+// 10 and 11 scales.
 // Persistent: one CTA per SM walks the tiles, blockIdx.x, + gridDim.x, ..., token tiles in groups so that the CTAs
 // running at one time share operands in L2.
 #include "fp8_block.cuh"
@@ -38,11 +38,12 @@ constexpr int kOffB = kOffA + kStages * kABytes;
 constexpr int kOffStage = kOffB + kStages * kBBytes;
 constexpr int kOffBars = kOffStage + kEpiWarps * kStageBuf;
 constexpr int kNumBars = 2 * kStages + 4 + 1;
-constexpr int kOffMisc = kOffBars + kNumBars * 8;
+constexpr int kOffScale = kOffBars + ((kNumBars * 8 + 15) / 16) * 16;  // [2][2][128] scales of a K block: accumulator, half, row
+constexpr int kOffMisc = kOffScale + 2 * 2 * kTileM * 4;
 constexpr int kSmemBytes = kOffMisc + 16;
 static_assert(kSmemBytes <= 227 * 1024, "shared memory");
 
-enum { kErrProducer8 = 21, kErrMma8 = 22, kErrEpilogue8 = 23, kErrAlign8 = 24 };
+enum { kErrProducer8 = 21, kErrMma8 = 22, kErrEpilogue8 = 23, kErrAlign8 = 24, kErrScale8 = 25 };
 
 struct P8 {
   int M, N, K;
@@ -143,9 +144,10 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBars);
   uint64_t* full = bars;                 // [stages] the stage's copies landed           (MMA waits)
   uint64_t* empty = full + kStages;      // [stages] the MMAs that read it are done       (producer waits)
-  uint64_t* acc_full = empty + kStages;  // [2] a K block's products are in the accumulator  (epilogue waits)
+  uint64_t* acc_full = empty + kStages;  // [2] a K block's products are in the accumulator, its scales in shared memory (epilogue waits)
   uint64_t* acc_empty = acc_full + 2;    // [2] the epilogue warps have read it           (MMA waits)
   uint64_t* drain_bar = acc_empty + 2;
+  float* s_scale = reinterpret_cast<float*>(smem + kOffScale);
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + kOffMisc);
   volatile int* s_abort = reinterpret_cast<volatile int*>(smem + kOffMisc + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -156,7 +158,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       mbar_init(&empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&acc_full[i], 1);
+      mbar_init(&acc_full[i], 3);  // the MMAs' commit and the two scale warps
       mbar_init(&acc_empty[i], kEpiWarps);
     }
     mbar_init(drain_bar, 1);
@@ -267,6 +269,55 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       }
       __syncwarp();
     }
+  } else if (ok_start) {
+    // ---- scale warps: one per column half (kGated: gate, up).  The products of the rows' and the columns' scales of a
+    // K block, a row per thread and quarter, loaded two blocks ahead: the epilogue warps, whose time is what the
+    // kernel waits for, find them in shared memory (their own loads, one block ahead, cost 700 of 1500 cycles a block).
+    constexpr int kAhead = 2;
+    const int h = warp - kMmaWarp - 1;
+    pdl_wait();
+    int count = 0;
+    bool ok = true;
+    for (int pos = blockIdx.x; ok && pos < tiles; pos += gridDim.x) {
+      int mt, nt;
+      tile_of(p, pos, mt, nt);
+      const int m0 = mt * kTileM + lane;
+      // block 2 nt + h of the columns (kGated: block nt of part h)
+      const int nb = KIND == kGated ? nt : min(2 * nt + h, p.nblocks - 1);
+      const int64_t part = static_cast<int64_t>(p.nblocks) * p.kblocks;
+      const float* sb = p.sb + static_cast<int64_t>(nb) * p.kblocks + (KIND == kGated ? h * part : 0);
+      float a[kAhead][4], b[kAhead];
+      auto fetch = [&](int i, int slot) {
+        const int seg = KIND == kPlain && i >= p.kblocks ? 1 : 0;  // at most two segments
+        b[slot] = __ldg(sb + seg * part + (i - seg * p.kblocks));
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          a[slot][j] = m0 + 32 * j < p.M ? __ldg(p.sa + static_cast<int64_t>(i) * p.M + m0 + 32 * j) : 0.0f;
+      };
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        if (i < kb_all) fetch(i, i);
+      for (int i0 = 0; ok && i0 < kb_all; i0 += kAhead) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          const int i = i0 + u;
+          if (ok && i < kb_all) {
+            const int buf = count & 1;
+            if (count >= 2 && !mbar_wait_all(&acc_empty[buf], ((count >> 1) - 1) & 1, s_abort)) {
+              if (lane == 0) raise_error8(p.status, s_abort, kErrScale8);
+              ok = false;
+            } else {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) s_scale[(buf * 2 + h) * kTileM + 32 * j + lane] = a[u][j] * b[u];
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&acc_full[buf]);
+              if (i + kAhead < kb_all) fetch(i + kAhead, u);
+              ++count;
+            }
+          }
+        }
+      }
+    }
   }
   } else {
     // ---- epilogue warps
@@ -283,27 +334,10 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       tile_of(p, pos, mt, nt);
       const int m0 = mt * kTileM, m = m0 + row;
       const bool m_ok = m < p.M;
-      const float* sa = p.sa + m;
-      // the scales of the columns this warp takes: block 2 nt + half (kGated: gate and up of block nt)
-      const int nb = KIND == kGated ? nt : min(2 * nt + half, p.nblocks - 1);
-      const float* sb = p.sb + static_cast<int64_t>(nb) * p.kblocks;
-      const int64_t sb_part = static_cast<int64_t>(p.nblocks) * p.kblocks;  // from one part of b to the next
       uint64_t run[64];
 #pragma unroll
       for (int e = 0; e < 64; ++e) run[e] = 0ull;
-      float sa_next = m_ok ? __ldg(sa) : 0.0f, sb_next = __ldg(sb), sc_next = KIND == kGated ? __ldg(sb + sb_part) : 0.0f;
       for (int i = 0; i < kb_all; ++i, ++count) {
-        const float s0 = sa_next * sb_next, s1 = sa_next * sc_next;
-        if (i + 1 < kb_all) {
-          if (m_ok) sa_next = __ldg(sa + static_cast<int64_t>(i + 1) * p.M);
-          if (KIND == kGated) {
-            sb_next = __ldg(sb + i + 1);
-            sc_next = __ldg(sb + sb_part + i + 1);
-          } else {
-            const int seg = (i + 1) / p.kblocks;
-            sb_next = __ldg(sb + seg * sb_part + (i + 1 - seg * p.kblocks));
-          }
-        }
         const int b = count & 1;
         if (!failed && !mbar_wait_all(&acc_full[b], (count >> 1) & 1, s_abort)) {
           if (lane == 0) raise_error8(p.status, s_abort, kErrEpilogue8);
@@ -312,6 +346,8 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         tc_fence_after_sync();
         if (!failed) {
           const uint32_t t = tmem_base + b * kTileN + lane_base;
+          const float* sc = s_scale + b * 2 * kTileM + row;
+          const float s0 = sc[(KIND == kGated ? 0 : half) * kTileM], s1 = KIND == kGated ? sc[kTileM] : 0.0f;
           if (KIND == kGated) {
             promote<4>(t + half * 64, run, s0);
             promote<4>(t + 128 + half * 64, run + 32, s1);
