@@ -8,8 +8,11 @@
 // is rounded between the blocks).
 // Orientation: token rows are the lanes (the MMA's 128-row operand), so that a thread's scale sa * sb is ONE number
 // for its 128 columns, and a promotion is one packed FMA per two columns.
-// Tile: 128 tokens x 256 columns, two accumulators of 256 columns = all of tensor memory, eight epilogue warps
-// with 128 running sums per thread.
+// Tile of a CTA: 128 tokens x 256 columns, two accumulators of 256 columns = all of tensor memory, eight epilogue
+// warps with 128 running sums per thread.  With more than 128 tokens two CTAs of a cluster share the columns
+// (cta_group::2): a pair's MMAs take 256 tokens x 128 columns of which each CTA holds 64 in its shared memory, and the two
+// column halves have accumulators, barriers and epilogue warps of their own, so that one half's waits fall into the
+// other's additions.  (A single CTA's MMAs of 128 columns read 128 bytes per cycle: 716 cycles a block instead of 480.)
 //
 // Warp roles: 0..7 epilogue (lane quarter warp % 4, column half warp / 4), 8 producer, 9 tensor memory and MMAs,
 // 10 and 11 scales.
@@ -23,9 +26,7 @@ namespace {
 
 using gemm::named_bar_sync;
 
-constexpr int kStages = 4;
-constexpr int kTileM = 128, kTileN = 256;
-constexpr int kABytes = kTileM * kBlk, kBBytes = kTileN * kBlk;
+constexpr int kTileM = 128, kTileN = 256;  // of one CTA
 constexpr int kEpiWarps = 8, kEpiThreads = 256;
 constexpr int kProducerWarp = 8, kMmaWarp = 9;
 constexpr int kThreads = 384;  // three warpgroups; the two epilogue ones take registers over from the third
@@ -33,15 +34,23 @@ constexpr int kThreads = 384;  // three warpgroups; the two epilogue ones take r
 constexpr int kEpiRegs = 224, kOtherRegs = 56;
 static_assert(256 * kEpiRegs + 128 * kOtherRegs <= kThreads * 168, "register split");
 constexpr int kStageBuf = 32 * 128;  // staging of one epilogue warp: 32 rows of 128 bytes
-constexpr int kOffA = 0;
-constexpr int kOffB = kOffA + kStages * kABytes;
-constexpr int kOffStage = kOffB + kStages * kBBytes;
-constexpr int kOffBars = kOffStage + kEpiWarps * kStageBuf;
-constexpr int kNumBars = 2 * kStages + 4 + 1;
-constexpr int kOffScale = kOffBars + ((kNumBars * 8 + 15) / 16) * 16;  // [2][2][128] scales of a K block: accumulator, half, row
-constexpr int kOffMisc = kOffScale + 2 * 2 * kTileM * 4;
-constexpr int kSmemBytes = kOffMisc + 16;
-static_assert(kSmemBytes <= 227 * 1024, "shared memory");
+template <bool PAIR>
+struct Cfg8 {
+  static constexpr int kABytes = kTileM * kBlk;
+  static constexpr int kBBytes = (PAIR ? kTileN / 2 : kTileN) * kBlk;  // a pair's CTAs hold half of the columns each
+  static constexpr int kStageBytes = kABytes + kBBytes;
+  static constexpr int kStages = PAIR ? 6 : 4;
+  static constexpr int offA = 0;
+  static constexpr int offB = offA + kStages * kABytes;
+  static constexpr int offStage = offB + kStages * kBBytes;
+  static constexpr int offBars = offStage + kEpiWarps * kStageBuf;
+  static constexpr int kNumBars = 2 * kStages + 12 + 1;
+  static constexpr int offScale = offBars + ((kNumBars * 8 + 15) / 16) * 16;  // [2 halves][2 accumulators][kScaleRow] scales of a K block
+  static constexpr int kScaleRow = kTileM + 4;  // the rows' scales, then the columns' (kGated: gate, up)
+  static constexpr int offMisc = offScale + 4 * kScaleRow * 4;
+  static constexpr int kSmemBytes = offMisc + 16;
+  static_assert(kSmemBytes <= 227 * 1024, "shared memory");
+};
 
 enum { kErrProducer8 = 21, kErrMma8 = 22, kErrEpilogue8 = 23, kErrAlign8 = 24, kErrScale8 = 25 };
 
@@ -104,24 +113,34 @@ __device__ __forceinline__ void store_rows(const uint4* buf, uint8_t* dst, int64
   }
   __syncwarp();
 }
-// Accumulator columns [taddr, taddr + 16 * NCH) -> run (packed pairs) += s * columns, the next 16 in flight meanwhile.
-// (Alone this takes 286 cycles for 128 rows x 256 columns, with 32 columns at a time 271, but those registers do not fit
-// beside the sums.)
-template <int NCH>
-__device__ __forceinline__ void promote(uint32_t taddr, uint64_t* run, float s) {
-  const uint64_t s2 = pack2(s, s);
-  float nxt[16];
-  tmem_ld16(taddr, nxt);
+// Accumulator columns -> run (packed pairs) += scale * columns, in pieces of 32 and 16 columns that alternate between two
+// register buffers, so that one is in flight while the other is added up.  (Each wait drains everything in flight; pieces
+// of 16 alone make eight waits of it, and two buffers of 32 do not fit beside 128 sums.)
+template <int N>
+__device__ __forceinline__ void add_piece(const float* v, uint64_t* run, uint64_t s2) {
 #pragma unroll
-  for (int c = 0; c < NCH; ++c) {
-    float v[16];
-    tmem_ld_wait_regs<16>(nxt);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) v[e] = nxt[e];
-    if (c + 1 < NCH) tmem_ld16(taddr + 16 * (c + 1), nxt);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) run[c * 8 + e] = fma2(s2, pack2(v[2 * e], v[2 * e + 1]), run[c * 8 + e]);
-  }
+  for (int e = 0; e < N / 2; ++e) run[e] = fma2(s2, pack2(v[2 * e], v[2 * e + 1]), run[e]);
+}
+// 128 columns: the first 64 with one scale, the others with another
+__device__ __forceinline__ void promote(uint32_t t, uint64_t* run, float s0, float s1) {
+  const uint64_t p0 = pack2(s0, s0), p1 = pack2(s1, s1);
+  float a[32], b[16];
+  tmem_ld32(t, a);
+  tmem_ld_wait32(a);
+  tmem_ld16(t + 32, b);
+  add_piece<32>(a, run, p0);
+  tmem_ld_wait_regs<16>(b);
+  tmem_ld32(t + 48, a);
+  add_piece<16>(b, run + 16, p0);
+  tmem_ld_wait32(a);
+  tmem_ld16(t + 80, b);
+  add_piece<16>(a, run + 24, p0);
+  add_piece<16>(a + 16, run + 32, p1);
+  tmem_ld_wait_regs<16>(b);
+  tmem_ld32(t + 96, a);
+  add_piece<16>(b, run + 40, p1);
+  tmem_ld_wait32(a);
+  add_piece<32>(a, run + 48, p1);
 }
 
 // run[0 .. N) moves to the end: a rolled loop over N sums at a time works on run[0 .. N) and rotates, so that its code is
@@ -137,19 +156,23 @@ __device__ __forceinline__ void rotate(uint64_t* run) {
   for (int e = 0; e < N; ++e) run[64 - N + e] = t[e];
 }
 
-template <int KIND, int ACT, bool F32>
+template <int KIND, int ACT, bool F32, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
 fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const P8 p) {
+  using C = Cfg8<PAIR>;
+  constexpr int kStages = C::kStages;
   extern __shared__ __align__(1024) uint8_t smem[];
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBars);
-  uint64_t* full = bars;                 // [stages] the stage's copies landed           (MMA waits)
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::offBars);
+  uint64_t* full = bars;                 // [stages] the stage's copies landed; PAIR: of both CTAs, the leader's counts (MMA waits)
   uint64_t* empty = full + kStages;      // [stages] the MMAs that read it are done       (producer waits)
-  uint64_t* acc_full = empty + kStages;  // [2] a K block's products are in the accumulator, its scales in shared memory (epilogue waits)
-  uint64_t* acc_empty = acc_full + 2;    // [2] the epilogue warps have read it           (MMA waits)
-  uint64_t* drain_bar = acc_empty + 2;
-  float* s_scale = reinterpret_cast<float*>(smem + kOffScale);
-  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + kOffMisc);
-  volatile int* s_abort = reinterpret_cast<volatile int*>(smem + kOffMisc + 4);
+  // per column half h and accumulator a, at 2 h + a:
+  uint64_t* acc_full = empty + kStages;  // [4] a K block's products are in the accumulator, its scales in shared memory (epilogue waits)
+  uint64_t* acc_empty = acc_full + 4;    // [4] the half's epilogue warps (PAIR: of both CTAs, the leader's counts) have read it (MMA waits)
+  uint64_t* sc_empty = acc_empty + 4;    // [4] this CTA's have                           (scale warp waits)
+  uint64_t* drain_bar = sc_empty + 4;
+  float* s_scale = reinterpret_cast<float*>(smem + C::offScale);
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + C::offMisc);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(smem + C::offMisc + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -157,9 +180,10 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
     }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&acc_full[i], 3);  // the MMAs' commit and the two scale warps
-      mbar_init(&acc_empty[i], kEpiWarps);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&acc_full[i], 2);  // the MMAs' commit and the half's scale warp
+      mbar_init(&acc_empty[i], PAIR ? kEpiWarps : kEpiWarps / 2);
+      mbar_init(&sc_empty[i], kEpiWarps / 2);
     }
     mbar_init(drain_bar, 1);
     *s_abort = 0;
@@ -170,12 +194,23 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     prefetch_tensormap(&tm_a);
     prefetch_tensormap(&tm_b);
   }
-  if (warp == kMmaWarp) tmem_alloc(s_tmem, 512);
+  if (warp == kMmaWarp) {
+    if (PAIR)
+      tmem_alloc_pair(s_tmem, 512);
+    else
+      tmem_alloc(s_tmem, 512);
+  }
   tc_fence_before_sync();
-  __syncthreads();
+  if (PAIR)
+    cluster_sync_all();  // both CTAs' barriers are initialized and their tensor memory is allocated
+  else
+    __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem_base = *s_tmem;
   const bool ok_start = *s_abort == 0;
+  const int rank = PAIR ? static_cast<int>(cluster_ctarank()) : 0;
+  const int worker = PAIR ? static_cast<int>(blockIdx.x >> 1) : static_cast<int>(blockIdx.x);
+  const int workers = PAIR ? static_cast<int>(gridDim.x >> 1) : static_cast<int>(gridDim.x);
   const int tiles = p.m_tiles * p.n_tiles;
   const int kb_all = p.segs * p.kblocks;
   if (threadIdx.x == 0) pdl_launch_dependents();
@@ -189,7 +224,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       int s = 0, issued = 0;
       uint32_t ph = 0;
       bool ok = true;
-      for (int pos = blockIdx.x; ok && pos < tiles; pos += gridDim.x) {
+      for (int pos = worker; ok && pos < tiles; pos += workers) {
         int mt, nt;
         tile_of(p, pos, mt, nt);
         for (int i = 0; i < kb_all; ++i) {
@@ -199,16 +234,30 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
             break;
           }
           if (issuer) {
-            const int seg = KIND == kPlain ? i / p.kblocks : 0, k = (i - seg * p.kblocks) * kBlk;
-            uint8_t* sb = smem + kOffB + s * kBBytes;
-            mbar_arrive_expect_tx(&full[s], kABytes + kBBytes);
-            tma_load_3d(smem + kOffA + s * kABytes, &tm_a, k, mt * kTileM, seg, &full[s]);
-            if (KIND == kGated) {  // 128 rows of the gate, the same 128 of the up projection
-              tma_load_3d(sb, &tm_b, k, nt * kBlk, 0, &full[s]);
-              tma_load_3d(sb + kBBytes / 2, &tm_b, k, nt * kBlk, 1, &full[s]);
+            const int seg = KIND == kPlain && i >= p.kblocks ? 1 : 0;  // at most two segments
+            const int k = (i - seg * p.kblocks) * kBlk;
+            uint8_t* sa = smem + C::offA + s * C::kABytes;
+            uint8_t* sb = smem + C::offB + s * C::kBBytes;
+            if (PAIR) {
+              // each CTA brings its own token rows and, of each column half, 64 columns (kGated: the leader the gate's,
+              // its peer the up projection's); all of it is counted on the leader's barrier
+              const uint32_t bar = map_to_rank(smem_u32(&full[s]), 0);
+              if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * C::kStageBytes);
+              tma_load_3d_pair(sa, &tm_a, k, (2 * mt + rank) * kTileM, seg, bar);
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+                tma_load_3d_pair(sb + h * (C::kBBytes / 2), &tm_b, k,
+                                 KIND == kGated ? nt * kBlk + h * 64 : nt * kTileN + h * kBlk + rank * 64,
+                                 KIND == kGated ? rank : seg, bar);
             } else {
-              tma_load_3d(sb, &tm_b, k, nt * kTileN, seg, &full[s]);
-              tma_load_3d(sb + kBBytes / 2, &tm_b, k, nt * kTileN + kBlk, seg, &full[s]);
+              mbar_arrive_expect_tx(&full[s], C::kStageBytes);
+              tma_load_3d(sa, &tm_a, k, mt * kTileM, seg, &full[s]);
+              // the columns by 64, in the same order
+#pragma unroll
+              for (int h = 0; h < 4; ++h)
+                tma_load_3d(sb + h * (C::kBBytes / 4), &tm_b, k,
+                            KIND == kGated ? nt * kBlk + (h >> 1) * 64 : nt * kTileN + h * 64, KIND == kGated ? h & 1 : seg,
+                            &full[s]);
             }
           }
           __syncwarp();
@@ -219,40 +268,63 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
           }
         }
       }
-      // never leave with copies still in flight
+      // never leave with copies still in flight (PAIR: the stages filled last are released by the MMAs that read them)
       for (int i = max(0, issued - kStages); i < issued; ++i) {
+        uint64_t* bar = PAIR ? &empty[i % kStages] : &full[i % kStages];
         uint32_t spin = 0;
-        while (!mbar_try_wait(&full[i % kStages], (i / kStages) & 1) && ++spin < kSpinLimit) {
+        while (!mbar_try_wait(bar, (i / kStages) & 1) && ++spin < kSpinLimit && !(PAIR && *s_abort)) {
         }
       }
     }
   } else if (warp == kMmaWarp) {
-    if (ok_start) {
+    if (ok_start && rank == 0) {
       const bool issuer = elect_one();
-      const uint64_t adesc0 = umma_desc_k128(smem_u32(smem + kOffA));
-      const uint64_t bdesc0 = umma_desc_k128(smem_u32(smem + kOffB));
-      const uint32_t idesc = umma_idesc_e4m3(kTileN);
+      const uint64_t adesc0 = umma_desc_k128(smem_u32(smem + C::offA));
+      const uint64_t bdesc0 = umma_desc_k128(smem_u32(smem + C::offB));
+      // a pair's MMAs take one column half each: 256 rows x 128 columns
+      const uint32_t idesc = PAIR ? umma_idesc_e4m3(kTileN / 2) + ((128u >> 4) << 24) : umma_idesc_e4m3(kTileN);
       int s = 0;
       uint32_t ph = 0;
       bool failed = false;
       int count = 0;  // K blocks so far: block c goes to accumulator c % 2
-      for (int pos = blockIdx.x; !failed && pos < tiles; pos += gridDim.x) {
+      for (int pos = worker; !failed && pos < tiles; pos += workers) {
         for (int i = 0; i < kb_all; ++i, ++count) {
           const int buf = count & 1;
-          if ((count >= 2 && !mbar_wait(&acc_empty[buf], ((count >> 1) - 1) & 1, s_abort)) ||
-              !mbar_wait(&full[s], ph, s_abort)) {
+          const uint32_t free_ph = ((count >> 1) - 1) & 1;
+          if (!mbar_wait(&full[s], ph, s_abort) || (count >= 2 && !mbar_wait(&acc_empty[buf], free_ph, s_abort)) ||
+              (!PAIR && count >= 2 && !mbar_wait(&acc_empty[2 + buf], free_ph, s_abort))) {
             failed = true;
             break;
           }
           tc_fence_after_sync();
-          if (issuer) {
-            const uint64_t ad = adesc0 + static_cast<uint64_t>((s * kABytes) >> 4);
-            const uint64_t bd = bdesc0 + static_cast<uint64_t>((s * kBBytes) >> 4);
+          const uint64_t ad = adesc0 + static_cast<uint64_t>((s * C::kABytes) >> 4);
+          const uint64_t bd = bdesc0 + static_cast<uint64_t>((s * C::kBBytes) >> 4);
+          const uint32_t d = tmem_base + buf * kTileN;
+          if (PAIR) {
+            if (issuer) {
 #pragma unroll
-            for (int k = 0; k < kBlk / 32; ++k)
-              umma_f8(tmem_base + buf * kTileN, ad + 2 * k, bd + 2 * k, idesc, k > 0 ? 1u : 0u);
-            umma_commit(&empty[s]);
+              for (int k = 0; k < kBlk / 32; ++k) umma_f8_pair(d, ad + 2 * k, bd + 2 * k, idesc, k > 0 ? 1u : 0u);
+              umma_commit_pair(&acc_full[buf]);
+            }
+            __syncwarp();
+            if (count >= 2 && !mbar_wait(&acc_empty[2 + buf], free_ph, s_abort)) {
+              failed = true;
+              break;
+            }
+            tc_fence_after_sync();
+            if (issuer) {
+#pragma unroll
+              for (int k = 0; k < kBlk / 32; ++k)
+                umma_f8_pair(d + kTileN / 2, ad + 2 * k, bd + ((C::kBBytes / 2) >> 4) + 2 * k, idesc, k > 0 ? 1u : 0u);
+              umma_commit_pair(&acc_full[2 + buf]);
+              umma_commit_pair(&empty[s]);
+            }
+          } else if (issuer) {
+#pragma unroll
+            for (int k = 0; k < kBlk / 32; ++k) umma_f8(d, ad + 2 * k, bd + 2 * k, idesc, k > 0 ? 1u : 0u);
             umma_commit(&acc_full[buf]);
+            umma_commit(&acc_full[2 + buf]);
+            umma_commit(&empty[s]);
           }
           __syncwarp();
           if (++s == kStages) {
@@ -263,29 +335,34 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       }
       if (failed && issuer) raise_error8(p.status, s_abort, kErrMma8);
       // tensor memory is released only when every MMA has completed, also where another role has given up
-      if (issuer) umma_commit(drain_bar);
+      if (issuer) {
+        if (PAIR)
+          umma_commit_pair(drain_bar);
+        else
+          umma_commit(drain_bar);
+      }
       uint32_t spin = 0;
       while (!mbar_try_wait(drain_bar, 0) && ++spin < kSpinLimit) {
       }
       __syncwarp();
     }
   } else if (ok_start) {
-    // ---- scale warps: one per column half (kGated: gate, up).  The products of the rows' and the columns' scales of a
-    // K block, a row per thread and quarter, loaded two blocks ahead: the epilogue warps, whose time is what the
-    // kernel waits for, find them in shared memory (their own loads, one block ahead, cost 700 of 1500 cycles a block).
+    // ---- scale warps, one per column half: the scales of a K block's 128 rows and of its columns, loaded two blocks
+    // ahead: the epilogue warps, whose time is what the kernel waits for, find them in shared memory (their own loads, one
+    // block ahead, cost 700 of 1500 cycles a block).
     constexpr int kAhead = 2;
     const int h = warp - kMmaWarp - 1;
     pdl_wait();
     int count = 0;
     bool ok = true;
-    for (int pos = blockIdx.x; ok && pos < tiles; pos += gridDim.x) {
+    for (int pos = worker; ok && pos < tiles; pos += workers) {
       int mt, nt;
       tile_of(p, pos, mt, nt);
-      const int m0 = mt * kTileM + lane;
-      // block 2 nt + h of the columns (kGated: block nt of part h)
-      const int nb = KIND == kGated ? nt : min(2 * nt + h, p.nblocks - 1);
+      const int m0 = (PAIR ? 2 * mt + rank : mt) * kTileM + lane;
+      // columns: block 2 nt + h (kGated: lane 0 block nt of the gate, lane 1 of the up projection)
       const int64_t part = static_cast<int64_t>(p.nblocks) * p.kblocks;
-      const float* sb = p.sb + static_cast<int64_t>(nb) * p.kblocks + (KIND == kGated ? h * part : 0);
+      const float* sb = p.sb + static_cast<int64_t>(KIND == kGated ? nt : min(2 * nt + h, p.nblocks - 1)) * p.kblocks +
+                        (KIND == kGated ? (lane & 1) * part : 0);
       float a[kAhead][4], b[kAhead];
       auto fetch = [&](int i, int slot) {
         const int seg = KIND == kPlain && i >= p.kblocks ? 1 : 0;  // at most two segments
@@ -302,15 +379,17 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         for (int u = 0; u < kAhead; ++u) {
           const int i = i0 + u;
           if (ok && i < kb_all) {
-            const int buf = count & 1;
-            if (count >= 2 && !mbar_wait_all(&acc_empty[buf], ((count >> 1) - 1) & 1, s_abort)) {
+            const int slot = 2 * h + (count & 1);
+            if (count >= 2 && !mbar_wait_all(&sc_empty[slot], ((count >> 1) - 1) & 1, s_abort)) {
               if (lane == 0) raise_error8(p.status, s_abort, kErrScale8);
               ok = false;
             } else {
+              float* d = s_scale + slot * C::kScaleRow;
 #pragma unroll
-              for (int j = 0; j < 4; ++j) s_scale[(buf * 2 + h) * kTileM + 32 * j + lane] = a[u][j] * b[u];
+              for (int j = 0; j < 4; ++j) d[32 * j + lane] = a[u][j];
+              if (lane < 2) d[kTileM + lane] = b[u];
               __syncwarp();
-              if (lane == 0) mbar_arrive(&acc_full[buf]);
+              if (lane == 0) mbar_arrive(&acc_full[slot]);
               if (i + kAhead < kb_all) fetch(i + kAhead, u);
               ++count;
             }
@@ -325,40 +404,40 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     const int quarter = warp & 3, half = warp >> 2;
     const int row = quarter * 32 + lane;
     const uint32_t lane_base = static_cast<uint32_t>(quarter * 32) << 16;
-    uint4* buf = reinterpret_cast<uint4*>(smem + kOffStage + warp * kStageBuf);
+    uint4* buf = reinterpret_cast<uint4*>(smem + C::offStage + warp * kStageBuf);
     bool failed = !ok_start;
     int count = 0;
     pdl_wait();
-    for (int pos = blockIdx.x; pos < tiles; pos += gridDim.x) {
-      int mt, nt;
-      tile_of(p, pos, mt, nt);
-      const int m0 = mt * kTileM, m = m0 + row;
-      const bool m_ok = m < p.M;
+    for (int pos = worker; pos < tiles; pos += workers) {
       uint64_t run[64];
 #pragma unroll
       for (int e = 0; e < 64; ++e) run[e] = 0ull;
       for (int i = 0; i < kb_all; ++i, ++count) {
-        const int b = count & 1;
+        const int b = 2 * half + (count & 1);
         if (!failed && !mbar_wait_all(&acc_full[b], (count >> 1) & 1, s_abort)) {
           if (lane == 0) raise_error8(p.status, s_abort, kErrEpilogue8);
           failed = true;
         }
         tc_fence_after_sync();
         if (!failed) {
-          const uint32_t t = tmem_base + b * kTileN + lane_base;
-          const float* sc = s_scale + b * 2 * kTileM + row;
-          const float s0 = sc[(KIND == kGated ? 0 : half) * kTileM], s1 = KIND == kGated ? sc[kTileM] : 0.0f;
-          if (KIND == kGated) {
-            promote<4>(t + half * 64, run, s0);
-            promote<4>(t + 128 + half * 64, run + 32, s1);
-          } else {
-            promote<8>(t + half * 128, run, s0);
-          }
+          const float* sc = s_scale + b * C::kScaleRow;
+          const float sr = sc[row], s0 = sr * sc[kTileM], s1 = KIND == kGated ? sr * sc[kTileM + 1] : s0;
+          promote(tmem_base + (count & 1) * kTileN + half * (kTileN / 2) + lane_base, run, s0, s1);
         }
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0 && !failed) mbar_arrive(&acc_empty[b]);
+        if (lane == 0 && !failed) {
+          if (PAIR)
+            mbar_arrive_cluster_relaxed(map_to_rank(smem_u32(&acc_empty[b]), 0));
+          else
+            mbar_arrive(&acc_empty[b]);
+          mbar_arrive(&sc_empty[b]);
+        }
       }
+      int mt, nt;
+      tile_of(p, pos, mt, nt);
+      const int m0 = (PAIR ? 2 * mt + rank : mt) * kTileM, m = m0 + row;
+      const bool m_ok = m < p.M;
       const int wm0 = m0 + quarter * 32;
       const int rows = failed ? 0 : min(32, p.M - wm0);  // may be <= 0
 
@@ -392,7 +471,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         float* u = g + 64;
         const int64_t MN = static_cast<int64_t>(p.M) * p.N, SM = static_cast<int64_t>(p.nblocks) * p.M;
         float* mine = reinterpret_cast<float*>(buf);
-        const float* other = reinterpret_cast<const float*>(smem + kOffStage + (warp ^ 4) * kStageBuf);
+        const float* other = reinterpret_cast<const float*>(smem + C::offStage + (warp ^ 4) * kStageBuf);
         // columns beyond N hold zeros (the copy engine filled the operand with zeros): they do not move a maximum
         if (p.ck) {
           uint32_t ag = 0u, au = 0u;
@@ -460,103 +539,156 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
           sg = __ldg(p.cks + static_cast<int64_t>(fb) * p.M + m);
           su = __ldg(p.cks + SM + static_cast<int64_t>(fb) * p.M + m);
         }
-        // a thread reads its own row's codes, 16 of g and of u at a time (both halves of a 32-byte sector in turn), the
-        // next ones in flight; each pair of running sums (dh) is replaced by the bf16 pairs of dg and du
-        const uint4* gp = reinterpret_cast<const uint4*>(p.ck + static_cast<int64_t>(m_ok ? m : 0) * p.N + (any ? n0 : 0));
-        const uint4* up = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(gp) + MN);
-        const int pieces = m_ok && any ? min(8, cols >> 4) : 0;
-        uint4 gn = make_uint4(0u, 0u, 0u, 0u), un = gn;
-        if (pieces > 0) {
-          gn = __ldg(gp);
-          un = __ldg(up);
-        }
-        uint32_t ag = 0u, au = 0u;
+        // 32 columns at a time through the staging buffer (dh in FP32), so that eight lanes share a row: they read the
+        // codes of g and u and write dg and du in whole sectors.  The bf16 pairs of dg and du take the place of the sums
+        // they come from; a rolled loop, since its code unrolled is more than the instruction caches hold.
+        const int rr = lane >> 3, cc = lane & 7;  // rows rr, rr + 4, ...; columns 4 cc .. 4 cc + 3 of the 32
+        const uint8_t* ck = p.ck + static_cast<int64_t>(wm0) * p.N + n0 + 4 * cc;
+        uint8_t* yd = static_cast<uint8_t*>(p.y) + (static_cast<int64_t>(wm0) * p.N + n0 + 4 * cc) * 2;
+        uint32_t ag[8], au[8];
+#pragma unroll
+        for (int it = 0; it < 8; ++it) ag[it] = au[it] = 0u;
 #pragma unroll 1
-        for (int j = 0; j < 8; ++j) {
-          const uint32_t gw[4] = {gn.x, gn.y, gn.z, gn.w}, uw[4] = {un.x, un.y, un.z, un.w};
-          gn = un = make_uint4(0u, 0u, 0u, 0u);
-          if (j + 1 < pieces) {
-            gn = __ldg(gp + j + 1);
-            un = __ldg(up + j + 1);
-          }
+        for (int c = 0; c < 4; ++c) {
+          uint32_t gc[8], uc[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float2 gv = decode2(static_cast<uint16_t>(gw[e >> 1] >> (16 * (e & 1))));
-            const float2 vv = decode2(static_cast<uint16_t>(uw[e >> 1] >> (16 * (e & 1))));
-            float d0, d1, a0, a1, b0, b1;
-            unpack2(run[e], d0, d1);
-            act_both<ACT>(gv.x * sg, a0, b0);
-            act_both<ACT>(gv.y * sg, a1, b1);
-            const uint32_t dg = pack_bf16(d0 * (vv.x * su) * b0, d1 * (vv.y * su) * b1);
-            const uint32_t du = pack_bf16(d0 * a0, d1 * a1);
-            ag = max(ag, max((dg << 16) & 0x7FFF0000u, dg & 0x7FFF0000u));
-            au = max(au, max((du << 16) & 0x7FFF0000u, du & 0x7FFF0000u));
-            run[e] = (static_cast<uint64_t>(du) << 32) | dg;
-          }
-          rotate<8>(run);
-        }
-        const float scg = block_scale(ag, p.pow2 != 0), scu = block_scale(au, p.pow2 != 0);
-        if (any && m_ok && !failed) {
-          p.s[static_cast<int64_t>(fb) * p.M + m] = scg;
-          p.s[SM + static_cast<int64_t>(fb) * p.M + m] = scu;
-        }
-        // (dg, du) x (first, second 64 columns)
-#pragma unroll 1
-        for (int it = 0; it < 4; ++it) {
-          const int part = it >> 1, c = it & 1;
-          const float inv = block_inv(part ? scu : scg);
-          uint32_t w[32];
-#pragma unroll
-          for (int e = 0; e < 32; ++e) w[e] = part ? static_cast<uint32_t>(run[e] >> 32) : static_cast<uint32_t>(run[e]);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) stage_put(buf, lane, j, make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]));
-          const int64_t o = part * MN + static_cast<int64_t>(wm0) * p.N + n0 + 64 * c;
-          store_rows<8, 2>(buf, static_cast<uint8_t*>(p.y) + o * 2, static_cast<int64_t>(p.N) * 2, rows,
-                           min(128, (cols - 64 * c) * 2), true, lane);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t o4[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t lo = w[8 * j + 2 * e], hi = w[8 * j + 2 * e + 1];
-              o4[e] = cast4(bf16_lo(lo), bf16_hi(lo), bf16_lo(hi), bf16_hi(hi), inv);
+          for (int it = 0; it < 8; ++it) {
+            const int r = it * 4 + rr;
+            gc[it] = uc[it] = 0u;
+            if (r < rows && 32 * c + 4 * cc < cols) {  // N is a multiple of 16: the four are inside or outside together
+              gc[it] = __ldg(reinterpret_cast<const uint32_t*>(ck + static_cast<int64_t>(r) * p.N + 32 * c));
+              uc[it] = __ldg(reinterpret_cast<const uint32_t*>(ck + MN + static_cast<int64_t>(r) * p.N + 32 * c));
             }
-            stage_put(buf, lane, j, make_uint4(o4[0], o4[1], o4[2], o4[3]));
           }
-          store_rows<4, 1>(buf, p.q + o, p.N, rows, min(64, cols - 64 * c), true, lane);
-          rotate<32>(run);
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            float f[4];
+            unpack2(run[2 * j], f[0], f[1]);
+            unpack2(run[2 * j + 1], f[2], f[3]);
+            stage_put(buf, lane, j, make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])));
+          }
+          __syncwarp();
+#pragma unroll
+          for (int it = 0; it < 8; ++it) {
+            const int r = it * 4 + rr;
+            const uint4 dv = stage_get(buf, r, cc);
+            const float d[4] = {__uint_as_float(dv.x), __uint_as_float(dv.y), __uint_as_float(dv.z), __uint_as_float(dv.w)};
+            const float g_s = __shfl_sync(0xFFFFFFFFu, sg, r), u_s = __shfl_sync(0xFFFFFFFFu, su, r);
+            uint32_t dg[2], du[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float2 gv = decode2(static_cast<uint16_t>(gc[it] >> (16 * e)));
+              const float2 vv = decode2(static_cast<uint16_t>(uc[it] >> (16 * e)));
+              float a0, a1, b0, b1;
+              act_both<ACT>(gv.x * g_s, a0, b0);
+              act_both<ACT>(gv.y * g_s, a1, b1);
+              dg[e] = pack_bf16(d[2 * e] * (vv.x * u_s) * b0, d[2 * e + 1] * (vv.y * u_s) * b1);
+              du[e] = pack_bf16(d[2 * e] * a0, d[2 * e + 1] * a1);
+              ag[it] = max(ag[it], max((dg[e] << 16) & 0x7FFF0000u, dg[e] & 0x7FFF0000u));
+              au[it] = max(au[it], max((du[e] << 16) & 0x7FFF0000u, du[e] & 0x7FFF0000u));
+            }
+            run[2 * it] = (static_cast<uint64_t>(dg[1]) << 32) | dg[0];
+            run[2 * it + 1] = (static_cast<uint64_t>(du[1]) << 32) | du[0];
+            if (r < rows && 32 * c + 4 * cc < cols) {
+              uint8_t* yr = yd + (static_cast<int64_t>(r) * p.N + 32 * c) * 2;
+              *reinterpret_cast<uint2*>(yr) = make_uint2(dg[0], dg[1]);
+              *reinterpret_cast<uint2*>(yr + MN * 2) = make_uint2(du[0], du[1]);
+            }
+          }
+          rotate<16>(run);
+        }
+        float ig[8], iu[8];
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+#pragma unroll
+          for (int o = 4; o; o >>= 1) {
+            ag[it] = max(ag[it], __shfl_xor_sync(0xFFFFFFFFu, ag[it], o));
+            au[it] = max(au[it], __shfl_xor_sync(0xFFFFFFFFu, au[it], o));
+          }
+          const int r = it * 4 + rr;
+          const float scg = block_scale(ag[it], p.pow2 != 0), scu = block_scale(au[it], p.pow2 != 0);
+          if (any && r < rows && cc == 0) {
+            float* sd = p.s + static_cast<int64_t>(fb) * p.M + wm0 + r;
+            sd[0] = scg;
+            sd[SM] = scu;
+          }
+          ig[it] = block_inv(scg);
+          iu[it] = block_inv(scu);
+        }
+        uint8_t* qd = p.q + static_cast<int64_t>(wm0) * p.N + n0 + 4 * cc;
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+#pragma unroll
+          for (int it = 0; it < 8; ++it) {
+            const int r = it * 4 + rr;
+            if (r < rows && 32 * c + 4 * cc < cols) {
+              const uint32_t g0 = static_cast<uint32_t>(run[2 * it]), g1 = static_cast<uint32_t>(run[2 * it] >> 32);
+              const uint32_t u0 = static_cast<uint32_t>(run[2 * it + 1]), u1 = static_cast<uint32_t>(run[2 * it + 1] >> 32);
+              uint8_t* qr = qd + static_cast<int64_t>(r) * p.N + 32 * c;
+              *reinterpret_cast<uint32_t*>(qr) = cast4(bf16_lo(g0), bf16_hi(g0), bf16_lo(g1), bf16_hi(g1), ig[it]);
+              *reinterpret_cast<uint32_t*>(qr + MN) = cast4(bf16_lo(u0), bf16_hi(u0), bf16_lo(u1), bf16_hi(u1), iu[it]);
+            }
+          }
+          rotate<16>(run);
         }
       }
     }
   }
 
   tc_fence_before_sync();
-  __syncthreads();
+  if (PAIR)
+    cluster_sync_all();  // both CTAs are done with both CTAs' tensor memory and barriers
+  else
+    __syncthreads();
   if (warp == kMmaWarp) {
     tc_fence_after_sync();
-    tmem_dealloc(tmem_base, 512);
+    if (PAIR)
+      tmem_dealloc_pair(tmem_base, 512);
+    else
+      tmem_dealloc(tmem_base, 512);
   }
 }
 
-template <int KIND, int ACT, bool F32>
-int launch_cfg(const CUtensorMap& ta, const CUtensorMap& tb, const P8& p, unsigned grid, cudaStream_t st) {
+template <int KIND, int ACT, bool F32, bool PAIR>
+int launch_cfg(const CUtensorMap& ta, const CUtensorMap& tb, const P8& p, cudaStream_t st) {
   static std::once_flag once;
   static cudaError_t attr = cudaSuccess;
   std::call_once(once, [] {
-    attr = cudaFuncSetAttribute(fp8_block_gemm_kernel<KIND, ACT, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    attr = cudaFuncSetAttribute(fp8_block_gemm_kernel<KIND, ACT, F32, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                Cfg8<PAIR>::kSmemBytes);
   });
   if (attr != cudaSuccess) return ZQ_ERR_CUDA;
-  const cudaError_t e = launch_chained(fp8_block_gemm_kernel<KIND, ACT, F32>, dim3(grid), dim3(kThreads), kSmemBytes, st, false,
-                                       ta, tb, p);
+  const int tiles = p.m_tiles * p.n_tiles, slots = PAIR ? sm_count() / 2 : sm_count();
+  const unsigned workers = static_cast<unsigned>(tiles < slots ? tiles : slots);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(PAIR ? 2 * workers : workers);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Cfg8<PAIR>::kSmemBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = PAIR ? 2 : 1;
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, fp8_block_gemm_kernel<KIND, ACT, F32, PAIR>, ta, tb, p);
   count_launch();
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
 }
 
+template <int KIND, int ACT, bool F32>
+int launch_pair(bool pair, const CUtensorMap& ta, const CUtensorMap& tb, const P8& p, cudaStream_t st) {
+  return pair ? launch_cfg<KIND, ACT, F32, true>(ta, tb, p, st) : launch_cfg<KIND, ACT, F32, false>(ta, tb, p, st);
+}
 template <int KIND>
-int launch_act(int act, const CUtensorMap& ta, const CUtensorMap& tb, const P8& p, unsigned grid, cudaStream_t st) {
-  if (act == ZQ_ACT_SILU) return launch_cfg<KIND, ZQ_ACT_SILU, false>(ta, tb, p, grid, st);
-  if (act == ZQ_ACT_GELU_TANH) return launch_cfg<KIND, ZQ_ACT_GELU_TANH, false>(ta, tb, p, grid, st);
-  return launch_cfg<KIND, ZQ_ACT_RELU, false>(ta, tb, p, grid, st);
+int launch_act(int act, bool pair, const CUtensorMap& ta, const CUtensorMap& tb, const P8& p, cudaStream_t st) {
+  if (act == ZQ_ACT_SILU) return launch_pair<KIND, ZQ_ACT_SILU, false>(pair, ta, tb, p, st);
+  if (act == ZQ_ACT_GELU_TANH) return launch_pair<KIND, ZQ_ACT_GELU_TANH, false>(pair, ta, tb, p, st);
+  return launch_pair<KIND, ZQ_ACT_RELU, false>(pair, ta, tb, p, st);
 }
 
 }  // namespace
@@ -569,9 +701,11 @@ int launch_block_gemm(const GemmArgs8& a, cudaStream_t st) {
   p.kblocks = static_cast<int>(blocks_of(a.K));
   p.segs = a.kind == kPlain ? a.parts : 1;
   p.nblocks = static_cast<int>(blocks_of(a.N));
-  p.m_tiles = static_cast<int>((a.M + kTileM - 1) / kTileM);
+  const bool pair = a.M > kTileM;  // otherwise the second CTA of a pair would have no rows
+  const int64_t tile_rows = pair ? 2 * kTileM : kTileM;
+  p.m_tiles = static_cast<int>((a.M + tile_rows - 1) / tile_rows);
   p.n_tiles = a.kind == kGated ? p.nblocks : static_cast<int>((a.N + kTileN - 1) / kTileN);
-  p.m_group = 16;
+  p.m_group = pair ? 8 : 16;
   const int64_t tiles = static_cast<int64_t>(p.m_tiles) * p.n_tiles;
   if (tiles > 0x3FFFFFFF) return ZQ_ERR_SHAPE;
   p.sa = a.sa;
@@ -588,13 +722,12 @@ int launch_block_gemm(const GemmArgs8& a, cudaStream_t st) {
   CUtensorMap ta, tb;
   if (!make_code_map(&ta, a.a, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.M), static_cast<uint64_t>(p.segs), kTileM) ||
       !make_code_map(&tb, a.b, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.N),
-                     a.kind == kGated ? 2u : static_cast<uint64_t>(p.segs), kBlk))
+                     a.kind == kGated ? 2u : static_cast<uint64_t>(p.segs), 64))
     return ZQ_ERR_CUDA;
-  const unsigned grid = static_cast<unsigned>(tiles < sm_count() ? tiles : sm_count());
-  if (a.kind == kGated) return launch_act<kGated>(a.act, ta, tb, p, grid, st);
-  if (a.kind == kGatedBwd) return launch_act<kGatedBwd>(a.act, ta, tb, p, grid, st);
-  return a.ydt == ZQ_OUT_F32 ? launch_cfg<kPlain, ZQ_ACT_RELU, true>(ta, tb, p, grid, st)
-                             : launch_cfg<kPlain, ZQ_ACT_RELU, false>(ta, tb, p, grid, st);
+  if (a.kind == kGated) return launch_act<kGated>(a.act, pair, ta, tb, p, st);
+  if (a.kind == kGatedBwd) return launch_act<kGatedBwd>(a.act, pair, ta, tb, p, st);
+  return a.ydt == ZQ_OUT_F32 ? launch_pair<kPlain, ZQ_ACT_RELU, true>(pair, ta, tb, p, st)
+                             : launch_pair<kPlain, ZQ_ACT_RELU, false>(pair, ta, tb, p, st);
 }
 
 }  // namespace fp8b
