@@ -9,6 +9,9 @@
 // tokens that are its share, in rank order (the same result every time), and finishes them: one launch, no
 // scratch in global memory.
 //
+// A pipeline stage is a K block: weight tile, token tile, token scales and an accumulator of its own in tensor memory, so
+// that the roles meet at three barriers per block and run up to kStages blocks apart (with two accumulators for all
+// stages their hand-over took 1.1 us per block whatever the copies took).
 // The tensor core adds up one block of 128; the epilogue warps multiply it by the block's scale (of the weight
 // tile, one number; of the tokens, one per column, read from shared memory) and add it to running sums in registers.
 //
@@ -63,22 +66,23 @@ struct FewCfg {
   static constexpr int kSmemEach = 226 * 1024 / kCtas - 1024;
   static constexpr int kMisc = 1024 + 4 * BM * 12;
   static constexpr int kStagesFit = (kSmemEach - kMisc) / kStageBytes;
-  static constexpr int kStages = kStagesFit > 8 ? 8 : kStagesFit;
+  // a stage has its accumulator in tensor memory: 512 columns for all CTAs of an SM
+  static constexpr int kStagesTmem = 512 / kCtas / (kMats * BM);
+  static constexpr int kStages = gemm::cmin(8, gemm::cmin(kStagesFit, kStagesTmem));
   static constexpr int kRedBytes = kMats * BM * 128 * 4;  // partial sums, in the stages' memory once they are done
-  static constexpr int kNB = 2;                           // accumulators
-  static constexpr int kCols = kNB * kMats * BM;
-  static constexpr int kTmemCols = kCols <= 32 ? 32 : (kCols <= 64 ? 64 : (kCols <= 128 ? 128 : 256));
+  static constexpr int kCols = kStages * kMats * BM;
+  static constexpr int kTmemCols = kCols <= 32 ? 32 : (kCols <= 64 ? 64 : (kCols <= 128 ? 128 : (kCols <= 256 ? 256 : 512)));
   static constexpr int offTok = kStages * kWBytes;
   static constexpr int offSc = offTok + kStages * kTokBytes;  // [stages][BM] token scales
   static constexpr int offMax = offSc + kStages * BM * 4;     // [kMats][4] maxima of the final step
   static constexpr int offBars = offMax + 64;
-  static constexpr int kNumBars = 3 * kStages + 2 * kNB + 1;
+  static constexpr int kNumBars = 4 * kStages + 1;
   static constexpr int offMisc = offBars + kNumBars * 8;
   static constexpr int kSmemBytes = offMisc + 16;
   static_assert(kStages >= 3, "pipeline depth");
   static_assert(kRedBytes <= offSc, "the partial sums must fit the stages");
   static_assert(kSmemBytes <= kSmemEach, "shared memory");
-  static_assert(kTmemCols * kCtas <= 512 && kCols <= 256, "tensor memory");
+  static_assert(kTmemCols * kCtas <= 512, "tensor memory");
   static_assert((BM * 4) % 16 == 0 && kTokBytes % 1024 == 0, "alignment");
 };
 
@@ -100,12 +104,11 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   constexpr int NS = C::kStages;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::offBars);
-  uint64_t* full = bars;                // [NS] the copies of the stage landed              (MMA waits)
-  uint64_t* tok_full = full + NS;       // [NS] token codes (RAW) and scales are written    (MMA, epilogue wait)
-  uint64_t* empty = tok_full + NS;      // [NS] MMAs done and scales read                   (producer, quantizer wait)
-  uint64_t* acc_full = empty + NS;      // [NB] a K block's products are complete           (epilogue waits)
-  uint64_t* acc_empty = acc_full + C::kNB;
-  uint64_t* drain_bar = acc_empty + C::kNB;
+  uint64_t* full = bars;                // [NS] the copies of the stage landed                        (MMA waits)
+  uint64_t* tok_full = full + NS;       // [NS] RAW: the token codes are written                      (MMA waits)
+  uint64_t* acc_full = tok_full + NS;   // [NS] the stage's products are complete, its token scales written (epilogue waits)
+  uint64_t* empty = acc_full + NS;      // [NS] the epilogue warps have read products and scales      (producer, quantizer wait)
+  uint64_t* drain_bar = empty + NS;
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + C::offMisc);
   volatile int* s_abort = reinterpret_cast<volatile int*>(smem + C::offMisc + 4);
   float* s_sc = reinterpret_cast<float*>(smem + C::offSc);
@@ -116,11 +119,8 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     for (int i = 0; i < NS; ++i) {
       mbar_init(&full[i], 1);
       mbar_init(&tok_full[i], 1);
-      mbar_init(&empty[i], 1 + C::kEpiWarps);
-    }
-    for (int i = 0; i < C::kNB; ++i) {
-      mbar_init(&acc_full[i], 1);
-      mbar_init(&acc_empty[i], C::kEpiWarps);
+      mbar_init(&acc_full[i], 2);  // the MMAs' commit and the warp that wrote the scales
+      mbar_init(&empty[i], C::kEpiWarps);
     }
     mbar_init(drain_bar, 1);
     *s_abort = 0;
@@ -212,9 +212,8 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       uint32_t ph = 0;
       bool failed = false;
       for (int i = 0; i < nkb; ++i) {
-        const int buf = i % C::kNB;
-        if ((i >= C::kNB && !mbar_wait(&acc_empty[buf], ((i / C::kNB) - 1) & 1, s_abort)) ||
-            !mbar_wait(&full[s], ph, s_abort) || !mbar_wait(&tok_full[s], ph, s_abort)) {
+        // (the stage's accumulator is free: the producer has refilled the stage after the epilogue had read it)
+        if (!mbar_wait(&full[s], ph, s_abort) || (RAW && !mbar_wait(&tok_full[s], ph, s_abort))) {
           failed = true;
           break;
         }
@@ -226,10 +225,9 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
           for (int mat = 0; mat < C::kMats; ++mat)
 #pragma unroll
             for (int k = 0; k < kBlk / 32; ++k)
-              umma_f8(tmem_base + (buf * C::kMats + mat) * BM, ad + ((mat * 128 * kBlk) >> 4) + 2 * k, bd + 2 * k, idesc,
+              umma_f8(tmem_base + (s * C::kMats + mat) * BM, ad + ((mat * 128 * kBlk) >> 4) + 2 * k, bd + 2 * k, idesc,
                       k > 0 ? 1u : 0u);
-          umma_commit(&empty[s]);
-          umma_commit(&acc_full[buf]);
+          umma_commit(&acc_full[s]);
         }
         __syncwarp();
         if (++s == NS) {
@@ -281,7 +279,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         for (int j = 0; j < kPairs; ++j) v[j] = nxt[j];
         i_next = next_own(i);
         if (i_next < nkb) fetch(kb0 + i_next);
-        if (i >= NS && !mbar_wait_warp(&empty[s], ((i / NS) - 1) & 1, s_abort)) {
+        if (i >= NS && !mbar_wait_all(&empty[s], ((i / NS) - 1) & 1, s_abort)) {
           if (lane == 0) raise_error8(p.status, s_abort, kErrQuantF);
           break;
         }
@@ -307,7 +305,10 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         }
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&tok_full[s]);
+        if (lane == 0) {
+          mbar_arrive(&tok_full[s]);
+          mbar_arrive(&acc_full[s]);
+        }
       }
     } else if (qw == 0) {
       int s = 0;
@@ -317,7 +318,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         float v[BM / 32 + 1];
 #pragma unroll
         for (int c = 0; c < BM; c += 32) v[c / 32] = c + lane < m_here ? __ldg(src + c + lane) : 0.0f;
-        if (i >= NS && !mbar_wait_warp(&empty[s], ph ^ 1, s_abort)) {
+        if (i >= NS && !mbar_wait_all(&empty[s], ph ^ 1, s_abort)) {
           if (lane == 0) raise_error8(p.status, s_abort, kErrQuantF);
           break;
         }
@@ -325,7 +326,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         for (int c = 0; c < BM; c += 32)
           if (c + lane < BM) s_sc[s * BM + c + lane] = v[c / 32];
         __syncwarp();
-        if (lane == 0) mbar_arrive(&tok_full[s]);
+        if (lane == 0) mbar_arrive(&acc_full[s]);
         if (++s == NS) {
           s = 0;
           ph ^= 1;
@@ -350,15 +351,13 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     for (int i = 0; i < nkb; ++i) {
       const float sw = sw_next;
       if (i + 1 < nkb) sw_next = weight_scale(kb0 + i + 1);
-      const int buf = i % C::kNB;
-      if (!failed && (!mbar_wait_warp(&tok_full[s], ph, s_abort) ||
-                      !mbar_wait_warp(&acc_full[buf], (i / C::kNB) & 1, s_abort))) {
+      if (!failed && !mbar_wait_all(&acc_full[s], ph, s_abort)) {
         if (lane == 0) raise_error8(p.status, s_abort, kErrEpilogueF);
         failed = true;
       }
       tc_fence_after_sync();
       if (!failed) {
-        const uint32_t t = tmem_base + (buf * C::kMats + mat) * BM + lane_base;
+        const uint32_t t = tmem_base + (s * C::kMats + mat) * BM + lane_base;
         const float4* sc = reinterpret_cast<const float4*>(s_sc + s * BM);
         float nxt[16];
         tmem_ld16(t, nxt);
@@ -383,10 +382,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       __syncwarp();
       // a warp that has given up counts itself in nowhere: nobody may take what it has not waited for as free
       if (failed) break;
-      if (lane == 0) {
-        mbar_arrive(&acc_empty[buf]);
-        mbar_arrive(&empty[s]);
-      }
+      if (lane == 0) mbar_arrive(&empty[s]);
       if (++s == NS) {
         s = 0;
         ph ^= 1;
