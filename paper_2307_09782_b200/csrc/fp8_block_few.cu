@@ -62,7 +62,7 @@ struct FewCfg {
   static constexpr int kWBytes = kMats * 128 * kBlk, kTokBytes = BM * kBlk;
   static constexpr int kStageBytes = kWBytes + kTokBytes;
   // CTAs per SM wanted, and with them the stages that fit
-  static constexpr int kCtas = GATED ? (BM <= 32 ? 2 : 1) : (BM <= 32 ? 3 : 2);
+  static constexpr int kCtas = GATED && BM > 32 ? 1 : 2;
   static constexpr int kSmemEach = 226 * 1024 / kCtas - 1024;
   static constexpr int kMisc = 1024 + 4 * BM * 12;
   static constexpr int kStagesFit = (kSmemEach - kMisc) / kStageBytes;
@@ -76,7 +76,7 @@ struct FewCfg {
   static constexpr int offSc = offTok + kStages * kTokBytes;  // [stages][BM] token scales
   static constexpr int offMax = offSc + kStages * BM * 4;     // [kMats][4] maxima of the final step
   static constexpr int offBars = offMax + 64;
-  static constexpr int kNumBars = 4 * kStages + 1;
+  static constexpr int kNumBars = 5 * kStages + 1;
   static constexpr int offMisc = offBars + kNumBars * 8;
   static constexpr int kSmemBytes = offMisc + 16;
   static_assert(kStages >= 3, "pipeline depth");
@@ -107,8 +107,9 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   uint64_t* full = bars;                // [NS] the copies of the stage landed                        (MMA waits)
   uint64_t* tok_full = full + NS;       // [NS] RAW: the token codes are written                      (MMA waits)
   uint64_t* acc_full = tok_full + NS;   // [NS] the stage's products are complete, its token scales written (epilogue waits)
-  uint64_t* empty = acc_full + NS;      // [NS] the epilogue warps have read products and scales      (producer, quantizer wait)
-  uint64_t* drain_bar = empty + NS;
+  uint64_t* empty = acc_full + NS;      // [NS] the MMAs that read the stage are done                  (producer waits)
+  uint64_t* acc_empty = empty + NS;     // [NS] the epilogue warps have read products and scales      (MMA, quantizer wait)
+  uint64_t* drain_bar = acc_empty + NS;
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + C::offMisc);
   volatile int* s_abort = reinterpret_cast<volatile int*>(smem + C::offMisc + 4);
   float* s_sc = reinterpret_cast<float*>(smem + C::offSc);
@@ -120,7 +121,8 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       mbar_init(&full[i], 1);
       mbar_init(&tok_full[i], 1);
       mbar_init(&acc_full[i], 2);  // the MMAs' commit and the warp that wrote the scales
-      mbar_init(&empty[i], C::kEpiWarps);
+      mbar_init(&empty[i], 1);
+      mbar_init(&acc_empty[i], C::kEpiWarps);
     }
     mbar_init(drain_bar, 1);
     *s_abort = 0;
@@ -212,8 +214,8 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       uint32_t ph = 0;
       bool failed = false;
       for (int i = 0; i < nkb; ++i) {
-        // (the stage's accumulator is free: the producer has refilled the stage after the epilogue had read it)
-        if (!mbar_wait(&full[s], ph, s_abort) || (RAW && !mbar_wait(&tok_full[s], ph, s_abort))) {
+        if ((i >= NS && !mbar_wait(&acc_empty[s], ph ^ 1, s_abort)) || !mbar_wait(&full[s], ph, s_abort) ||
+            (RAW && !mbar_wait(&tok_full[s], ph, s_abort))) {
           failed = true;
           break;
         }
@@ -228,6 +230,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
               umma_f8(tmem_base + (s * C::kMats + mat) * BM, ad + ((mat * 128 * kBlk) >> 4) + 2 * k, bd + 2 * k, idesc,
                       k > 0 ? 1u : 0u);
           umma_commit(&acc_full[s]);
+          umma_commit(&empty[s]);
         }
         __syncwarp();
         if (++s == NS) {
@@ -279,7 +282,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         for (int j = 0; j < kPairs; ++j) v[j] = nxt[j];
         i_next = next_own(i);
         if (i_next < nkb) fetch(kb0 + i_next);
-        if (i >= NS && !mbar_wait_all(&empty[s], ((i / NS) - 1) & 1, s_abort)) {
+        if (i >= NS && !mbar_wait_all(&acc_empty[s], ((i / NS) - 1) & 1, s_abort)) {
           if (lane == 0) raise_error8(p.status, s_abort, kErrQuantF);
           break;
         }
@@ -318,7 +321,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         float v[BM / 32 + 1];
 #pragma unroll
         for (int c = 0; c < BM; c += 32) v[c / 32] = c + lane < m_here ? __ldg(src + c + lane) : 0.0f;
-        if (i >= NS && !mbar_wait_all(&empty[s], ph ^ 1, s_abort)) {
+        if (i >= NS && !mbar_wait_all(&acc_empty[s], ph ^ 1, s_abort)) {
           if (lane == 0) raise_error8(p.status, s_abort, kErrQuantF);
           break;
         }
@@ -382,7 +385,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       __syncwarp();
       // a warp that has given up counts itself in nowhere: nobody may take what it has not waited for as free
       if (failed) break;
-      if (lane == 0) mbar_arrive(&empty[s]);
+      if (lane == 0) mbar_arrive(&acc_empty[s]);
       if (++s == NS) {
         s = 0;
         ph ^= 1;
