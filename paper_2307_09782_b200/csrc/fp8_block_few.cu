@@ -150,9 +150,9 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   const int nkb = kb1 - kb0;
   const int m_here = min(BM, p.M - m0);
 
-  float run[BM];  // epilogue warps
+  uint64_t run[BM / 2];  // epilogue warps: one channel's sums, tokens in pairs
 #pragma unroll
-  for (int c = 0; c < BM; ++c) run[c] = 0.0f;
+  for (int c = 0; c < BM / 2; ++c) run[c] = 0ull;
 
   if (warp == C::kProducerWarp) {
     if (ok_start) {
@@ -251,19 +251,18 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     const int qw = warp - C::kQuantWarp0;
     if (RAW) {
       // A warp takes the K blocks of the stages that are its own (stage % 4 == qw): 16 lanes per token row, two rows at a
-      // time.  Its next block's x is on its way while this one is cast, so that up to four blocks are under way at a
-      // time.  A stage belongs to one warp because a parity wait tells only two neighbouring phases of a barrier apart:
+      // time, so that four blocks are under way at a time.  A stage belongs to one warp because a parity wait tells only two neighbouring phases of a barrier apart:
       // whoever waits for a stage has to see every use of it.
       constexpr int kPairs = BM / 2;
       const int hl = lane & 15, r0 = lane >> 4;
-      uint4 nxt[kPairs];
+      uint4 v[kPairs];
       auto fetch = [&](int kb) {
         const int k = kb * kBlk + hl * 8;
 #pragma unroll
         for (int j = 0; j < kPairs; ++j) {
           const int r = r0 + 2 * j;
-          nxt[j] = make_uint4(0u, 0u, 0u, 0u);
-          if (r < m_here && k < p.K) nxt[j] = __ldg(reinterpret_cast<const uint4*>(p.x + static_cast<int64_t>(m0 + r) * p.ldx + k));
+          v[j] = make_uint4(0u, 0u, 0u, 0u);
+          if (r < m_here && k < p.K) v[j] = __ldg(reinterpret_cast<const uint4*>(p.x + static_cast<int64_t>(m0 + r) * p.ldx + k));
         }
       };
       auto next_own = [&](int i) {
@@ -273,15 +272,11 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       };
       int i_next = qw;
       if (qw >= NS) i_next = nkb;  // fewer stages than warps: nothing to do
-      if (ok_start && i_next < nkb) fetch(kb0 + i_next);
       while (ok_start && i_next < nkb) {
         const int i = i_next;
         const int s = i % NS;
-        uint4 v[kPairs];
-#pragma unroll
-        for (int j = 0; j < kPairs; ++j) v[j] = nxt[j];
         i_next = next_own(i);
-        if (i_next < nkb) fetch(kb0 + i_next);
+        fetch(kb0 + i);
         if (i >= NS && !mbar_wait_all(&acc_empty[s], ((i / NS) - 1) & 1, s_abort)) {
           if (lane == 0) raise_error8(p.status, s_abort, kErrQuantF);
           break;
@@ -361,7 +356,8 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       tc_fence_after_sync();
       if (!failed) {
         const uint32_t t = tmem_base + (s * C::kMats + mat) * BM + lane_base;
-        const float4* sc = reinterpret_cast<const float4*>(s_sc + s * BM);
+        const ulonglong2* sc = reinterpret_cast<const ulonglong2*>(s_sc + s * BM);  // pairs of tokens
+        const uint64_t sw2 = pack2(sw, sw);
         float nxt[16];
         tmem_ld16(t, nxt);
 #pragma unroll
@@ -373,11 +369,9 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
           if (c + 16 < BM) tmem_ld16(t + c + 16, nxt);
 #pragma unroll
           for (int e = 0; e < 16; e += 4) {
-            const float4 f = sc[(c + e) / 4];
-            run[c + e] = fmaf(f.x * sw, v[e], run[c + e]);
-            run[c + e + 1] = fmaf(f.y * sw, v[e + 1], run[c + e + 1]);
-            run[c + e + 2] = fmaf(f.z * sw, v[e + 2], run[c + e + 2]);
-            run[c + e + 3] = fmaf(f.w * sw, v[e + 3], run[c + e + 3]);
+            const ulonglong2 f = sc[(c + e) / 4];
+            run[(c + e) / 2] = fma2(mul2(f.x, sw2), pack2(v[e], v[e + 1]), run[(c + e) / 2]);
+            run[(c + e) / 2 + 1] = fma2(mul2(f.y, sw2), pack2(v[e + 2], v[e + 3]), run[(c + e) / 2 + 1]);
           }
         }
       }
@@ -401,7 +395,13 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   float* red = reinterpret_cast<float*>(smem);  // [kMats][BM][128]
   if (warp < C::kEpiWarps) {
 #pragma unroll
-    for (int c = 0; c < BM; ++c) red[((warp >> 2) * BM + c) * 128 + (warp & 3) * 32 + lane] = run[c];
+    for (int c = 0; c < BM / 2; ++c) {
+      float lo, hi;
+      unpack2(run[c], lo, hi);
+      float* r = red + ((warp >> 2) * BM + 2 * c) * 128 + (warp & 3) * 32 + lane;
+      r[0] = lo;
+      r[128] = hi;
+    }
   }
   cluster_sync_all();
   if (warp < C::kEpiWarps && *s_abort == 0) {
@@ -417,8 +417,12 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       float v[C::kMats];
 #pragma unroll
       for (int mat = 0; mat < C::kMats; ++mat) {
-        v[mat] = 0.0f;
-        for (int r = 0; r < p.cluster; ++r) v[mat] += ld_cluster(map_to_rank(base + (mat * BM + c) * 512, r));
+        float part[8];  // all ranks' sums on their way before the first is added
+#pragma unroll
+        for (int r = 0; r < 8; ++r) part[r] = r < p.cluster ? ld_cluster(map_to_rank(base + (mat * BM + c) * 512, r)) : 0.0f;
+        v[mat] = part[0];
+#pragma unroll
+        for (int r = 1; r < 8; ++r) v[mat] += part[r];
       }
       if (!GATED) {
         if (n_ok) {
@@ -457,7 +461,8 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       }
     }
   }
-  cluster_sync_all();  // nobody leaves while a peer reads its sums
+  // nobody leaves while a peer reads its sums (nothing is published here: a relaxed arrival)
+  asm volatile("barrier.cluster.arrive.relaxed;\n\tbarrier.cluster.wait;" ::: "memory");
 }
 
 template <int BM, bool GATED, bool RAW>
