@@ -21,8 +21,8 @@
 // those of zq_quantize_fp8_block.  With more tokens the cast of a K block in every CTA takes longer than its weights'
 // way from HBM (32 tokens, 7168 -> 28672: 134 us), and a separate quantizer costs less.
 //
-// Warp roles: 0..3 epilogue (kGated: 0..3 gate, 4..7 up), then 4 quantizer warps (without RAW the first of them
-// copies the tokens' scales), 1 producer, 1 tensor memory and MMAs.
+// Warp roles: 0..3 epilogue (kGated: 0..3 gate, 4..7 up), then 4 quantizer warps (without RAW they
+// bring the tokens' scales; the weight tiles' scales in both forms), 1 producer, 1 tensor memory and MMAs.
 #include "fp8_block.cuh"
 
 namespace zq {
@@ -74,7 +74,8 @@ struct FewCfg {
   static constexpr int kTmemCols = kCols <= 32 ? 32 : (kCols <= 64 ? 64 : (kCols <= 128 ? 128 : (kCols <= 256 ? 256 : 512)));
   static constexpr int offTok = kStages * kWBytes;
   static constexpr int offSc = offTok + kStages * kTokBytes;  // [stages][BM] token scales
-  static constexpr int offMax = offSc + kStages * BM * 4;     // [kMats][4] maxima of the final step
+  static constexpr int offSw = offSc + kStages * BM * 4;      // [stages][2] scales of the weight tiles
+  static constexpr int offMax = offSw + kStages * 8;          // [kMats][4] maxima of the final step
   static constexpr int offBars = offMax + 64;
   static constexpr int kNumBars = 5 * kStages + 1;
   static constexpr int offMisc = offBars + kNumBars * 8;
@@ -113,6 +114,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + C::offMisc);
   volatile int* s_abort = reinterpret_cast<volatile int*>(smem + C::offMisc + 4);
   float* s_sc = reinterpret_cast<float*>(smem + C::offSc);
+  float* s_sw = reinterpret_cast<float*>(smem + C::offSw);
   uint32_t* s_max = reinterpret_cast<uint32_t*>(smem + C::offMax);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -247,12 +249,26 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       __syncwarp();
     }
   } else if (warp >= C::kQuantWarp0) {
-    pdl_wait();
     const int qw = warp - C::kQuantWarp0;
+    // A warp takes the K blocks of the stages that are its own (stage % 4 == qw), so that four blocks are under way at a
+    // time.  A stage belongs to one warp because a parity wait tells only two neighbouring phases of a barrier apart:
+    // whoever waits for a stage has to see every use of it.
+    auto next_own = [&](int i) {
+      do ++i;
+      while ((i % NS) % C::kQuantWarps != qw);
+      return i;
+    };
+    int i_next = ok_start && qw < NS ? qw : nkb;  // with fewer stages than warps some have nothing to do
+    // the weight tiles' scales of a K block, one per lane 0 .. kMats - 1
+    auto weight_scale = [&](int kb) {
+      const int seg = kb / p.kblocks;
+      const int64_t part = static_cast<int64_t>(p.nblocks) * p.kblocks;
+      return lane < C::kMats ? __ldg(p.sb + (GATED ? lane : seg) * part + static_cast<int64_t>(nt) * p.kblocks + (kb - seg * p.kblocks))
+                             : 0.0f;
+    };
+    pdl_wait();
     if (RAW) {
-      // A warp takes the K blocks of the stages that are its own (stage % 4 == qw): 16 lanes per token row, two rows at a
-      // time, so that four blocks are under way at a time.  A stage belongs to one warp because a parity wait tells only two neighbouring phases of a barrier apart:
-      // whoever waits for a stage has to see every use of it.
+      // 16 lanes per token row, two rows at a time
       constexpr int kPairs = BM / 2;
       const int hl = lane & 15, r0 = lane >> 4;
       uint4 v[kPairs];
@@ -265,18 +281,12 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
           if (r < m_here && k < p.K) v[j] = __ldg(reinterpret_cast<const uint4*>(p.x + static_cast<int64_t>(m0 + r) * p.ldx + k));
         }
       };
-      auto next_own = [&](int i) {
-        do ++i;
-        while ((i % NS) % C::kQuantWarps != qw);
-        return i;
-      };
-      int i_next = qw;
-      if (qw >= NS) i_next = nkb;  // fewer stages than warps: nothing to do
-      while (ok_start && i_next < nkb) {
+      while (i_next < nkb) {
         const int i = i_next;
         const int s = i % NS;
         i_next = next_own(i);
         fetch(kb0 + i);
+        const float sw = weight_scale(kb0 + i);
         if (i >= NS && !mbar_wait_all(&acc_empty[s], ((i / NS) - 1) & 1, s_abort)) {
           if (lane == 0) raise_error8(p.status, s_abort, kErrQuantF);
           break;
@@ -301,6 +311,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
             }
           }
         }
+        if (lane < C::kMats) s_sw[2 * s + lane] = sw;
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
@@ -308,27 +319,26 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
           mbar_arrive(&acc_full[s]);
         }
       }
-    } else if (qw == 0) {
-      int s = 0;
-      uint32_t ph = 0;
-      for (int i = 0; ok_start && i < nkb; ++i) {
+    } else {
+      while (i_next < nkb) {
+        const int i = i_next;
+        const int s = i % NS;
+        i_next = next_own(i);
         const float* src = p.sa + static_cast<int64_t>(kb0 + i) * p.M + m0;  // [segs][kblocks][M]
         float v[BM / 32 + 1];
 #pragma unroll
         for (int c = 0; c < BM; c += 32) v[c / 32] = c + lane < m_here ? __ldg(src + c + lane) : 0.0f;
-        if (i >= NS && !mbar_wait_all(&acc_empty[s], ph ^ 1, s_abort)) {
+        const float sw = weight_scale(kb0 + i);
+        if (i >= NS && !mbar_wait_all(&acc_empty[s], ((i / NS) - 1) & 1, s_abort)) {
           if (lane == 0) raise_error8(p.status, s_abort, kErrQuantF);
           break;
         }
 #pragma unroll
         for (int c = 0; c < BM; c += 32)
           if (c + lane < BM) s_sc[s * BM + c + lane] = v[c / 32];
+        if (lane < C::kMats) s_sw[2 * s + lane] = sw;
         __syncwarp();
         if (lane == 0) mbar_arrive(&acc_full[s]);
-        if (++s == NS) {
-          s = 0;
-          ph ^= 1;
-        }
       }
     }
   } else {
@@ -338,17 +348,8 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     bool failed = !ok_start;
     int s = 0;
     uint32_t ph = 0;
-    const float* sb0 = p.sb + static_cast<int64_t>(nt) * p.kblocks;
-    const int64_t sb_part = static_cast<int64_t>(p.nblocks) * p.kblocks;
-    auto weight_scale = [&](int kb) {
-      const int seg = kb / p.kblocks;
-      return __ldg(sb0 + (GATED ? mat : seg) * sb_part + (kb - seg * p.kblocks));
-    };
-    float sw_next = nkb > 0 ? weight_scale(kb0) : 0.0f;
     pdl_wait();
     for (int i = 0; i < nkb; ++i) {
-      const float sw = sw_next;
-      if (i + 1 < nkb) sw_next = weight_scale(kb0 + i + 1);
       if (!failed && !mbar_wait_all(&acc_full[s], ph, s_abort)) {
         if (lane == 0) raise_error8(p.status, s_abort, kErrEpilogueF);
         failed = true;
@@ -357,6 +358,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       if (!failed) {
         const uint32_t t = tmem_base + (s * C::kMats + mat) * BM + lane_base;
         const ulonglong2* sc = reinterpret_cast<const ulonglong2*>(s_sc + s * BM);  // pairs of tokens
+        const float sw = s_sw[2 * s + mat];
         const uint64_t sw2 = pack2(sw, sw);
         float nxt[16];
         tmem_ld16(t, nxt);
