@@ -29,8 +29,6 @@ namespace zq {
 namespace fp8b {
 namespace {
 
-using gemm::named_bar_sync;
-
 enum { kErrProducerF = 41, kErrMmaF = 42, kErrEpilogueF = 43, kErrAlignF = 44, kErrQuantF = 45 };
 
 struct PF {
@@ -43,7 +41,7 @@ struct PF {
   int64_t ldx;
   void* y;
   int64_t ldy;
-  int y_f32;
+  int y_f32, y_vec;  // y_vec: four neighbouring outputs can be stored at once
   uint8_t* q;
   float* s;
   uint8_t* ck;
@@ -75,8 +73,7 @@ struct FewCfg {
   static constexpr int offTok = kStages * kWBytes;
   static constexpr int offSc = offTok + kStages * kTokBytes;  // [stages][BM] token scales
   static constexpr int offSw = offSc + kStages * BM * 4;      // [stages][2] scales of the weight tiles
-  static constexpr int offMax = offSw + kStages * 8;          // [kMats][4] maxima of the final step
-  static constexpr int offBars = offMax + 64;
+  static constexpr int offBars = offSw + kStages * 8;
   static constexpr int kNumBars = 5 * kStages + 1;
   static constexpr int offMisc = offBars + kNumBars * 8;
   static constexpr int kSmemBytes = offMisc + 16;
@@ -87,10 +84,28 @@ struct FewCfg {
   static_assert((BM * 4) % 16 == 0 && kTokBytes % 1024 == 0, "alignment");
 };
 
-__device__ __forceinline__ float ld_cluster(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
+}
+__device__ __forceinline__ void store_bf16x4(__nv_bfloat16* y, const float* v, int n_here, bool vec) {
+  if (vec && n_here >= 4) {
+    *reinterpret_cast<uint2*>(y) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < n_here) y[e] = __float2bfloat16_rn(v[e]);
+  }
+}
+// One warp, one block: scale and codes of 128 values, four per lane (their number is a multiple of 16).
+__device__ __forceinline__ void quantize_token(const float* v, uint8_t* q, float* s, int n_here, bool pow2, int lane) {
+  uint32_t a = max(max(abs_bits(v[0]), abs_bits(v[1])), max(abs_bits(v[2]), abs_bits(v[3])));
+#pragma unroll
+  for (int o = 16; o; o >>= 1) a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
+  const float sc = block_scale(a, pow2), inv = block_inv(sc);
+  if (n_here >= 4) *reinterpret_cast<uint32_t*>(q) = cast4(v[0], v[1], v[2], v[3], inv);
+  if (lane == 0) *s = sc;
 }
 __device__ __forceinline__ float act_any(int act, float v) {
   if (act == ZQ_ACT_SILU) return act_value<ZQ_ACT_SILU>(v);
@@ -115,7 +130,6 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   volatile int* s_abort = reinterpret_cast<volatile int*>(smem + C::offMisc + 4);
   float* s_sc = reinterpret_cast<float*>(smem + C::offSc);
   float* s_sw = reinterpret_cast<float*>(smem + C::offSw);
-  uint32_t* s_max = reinterpret_cast<uint32_t*>(smem + C::offMax);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -407,58 +421,59 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   }
   cluster_sync_all();
   if (warp < C::kEpiWarps && *s_abort == 0) {
-    // group g of 128 threads finishes tokens rank * per + g, + groups, ...; thread = channel
-    const int grp = warp >> 2, ch = (warp & 3) * 32 + lane;
-    const int n = nt * kBlk + ch;
-    const bool n_ok = n < p.N;
+    // a warp finishes one token at a time (rank * per + warp, + kEpiWarps, ...), a lane four neighbouring channels
+    const int n = nt * kBlk + 4 * lane;
+    const int n_here = p.N - n;  // may be <= 0
     const int per = BM / p.cluster;
     const int c_end = min(m_here, (rank + 1) * per);
-    const uint32_t base = smem_u32(red) + ch * 4;
-    for (int c = rank * per + grp; c < c_end; c += C::kMats) {
+    const uint32_t base = smem_u32(red) + lane * 16;
+    for (int c = rank * per + warp; c < c_end; c += C::kEpiWarps) {
       const int64_t m = m0 + c;
-      float v[C::kMats];
+      float v[C::kMats][4];
 #pragma unroll
       for (int mat = 0; mat < C::kMats; ++mat) {
-        float part[8];  // all ranks' sums on their way before the first is added
+        float4 part[8];  // all ranks' sums on their way before the first is added
 #pragma unroll
-        for (int r = 0; r < 8; ++r) part[r] = r < p.cluster ? ld_cluster(map_to_rank(base + (mat * BM + c) * 512, r)) : 0.0f;
-        v[mat] = part[0];
+        for (int r = 0; r < 8; ++r)
+          part[r] = r < p.cluster ? ld_cluster4(map_to_rank(base + (mat * BM + c) * 512, r)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        v[mat][0] = part[0].x;
+        v[mat][1] = part[0].y;
+        v[mat][2] = part[0].z;
+        v[mat][3] = part[0].w;
 #pragma unroll
-        for (int r = 1; r < 8; ++r) v[mat] += part[r];
+        for (int r = 1; r < 8; ++r) {
+          v[mat][0] += part[r].x;
+          v[mat][1] += part[r].y;
+          v[mat][2] += part[r].z;
+          v[mat][3] += part[r].w;
+        }
       }
       if (!GATED) {
-        if (n_ok) {
-          if (p.y_f32)
-            static_cast<float*>(p.y)[m * p.ldy + n] = v[0];
-          else
-            static_cast<__nv_bfloat16*>(p.y)[m * p.ldy + n] = __float2bfloat16_rn(v[0]);
+        if (p.y_f32) {
+          float* y = static_cast<float*>(p.y) + m * p.ldy + n;
+          if (p.y_vec && n_here >= 4) {
+            *reinterpret_cast<float4*>(y) = make_float4(v[0][0], v[0][1], v[0][2], v[0][3]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (e < n_here) y[e] = v[0][e];
+          }
+        } else {
+          store_bf16x4(static_cast<__nv_bfloat16*>(p.y) + m * p.ldy + n, v[0], n_here, p.y_vec != 0);
         }
       } else {
-        const float g = v[0], u = v[C::kMats - 1];
+        float* g = v[0];
+        float* u = v[C::kMats - 1];
         // channels past N hold zeros (the copy engine filled their weights with zeros)
-        const float h = act_any(p.act, g) * u;
-        if (p.y && n_ok) static_cast<__nv_bfloat16*>(p.y)[m * p.ldy + n] = __float2bfloat16_rn(h);
-        if (p.q || p.ck) {
-          uint32_t a[3] = {abs_bits(h), abs_bits(g), abs_bits(u)};
-          uint32_t* mx = s_max + grp * 8;
+        float h[4];
 #pragma unroll
-          for (int j = 0; j < 3; ++j) {
-            if (j > 0 && !p.ck) break;
-            uint32_t b = a[j];
-#pragma unroll
-            for (int o = 16; o; o >>= 1) b = max(b, __shfl_xor_sync(0xFFFFFFFFu, b, o));
-            if (lane == 0) mx[warp & 3] = b;
-            named_bar_sync(1 + grp, 128);
-            b = max(max(mx[0], mx[1]), max(mx[2], mx[3]));
-            named_bar_sync(1 + grp, 128);
-            uint8_t* qd = j == 0 ? p.q : p.ck + (j - 1) * static_cast<int64_t>(p.M) * p.N;
-            float* sd = j == 0 ? p.s : p.cks + (j - 1) * static_cast<int64_t>(p.nblocks) * p.M;
-            if (j == 0 && !p.q) continue;
-            const float sc = block_scale(b, p.pow2 != 0), inv = block_inv(sc);
-            const float w = j == 0 ? h : (j == 1 ? g : u);
-            if (n_ok) qd[m * p.N + n] = static_cast<uint8_t>(cvt_e4m3x2(__fmul_rn(w, inv), 0.0f) & 0xFF);
-            if (ch == 0) sd[static_cast<int64_t>(nt) * p.M + m] = sc;
-          }
+        for (int e = 0; e < 4; ++e) h[e] = act_any(p.act, g[e]) * u[e];
+        if (p.y) store_bf16x4(static_cast<__nv_bfloat16*>(p.y) + m * p.ldy + n, h, n_here, p.y_vec != 0);
+        const int64_t MN = static_cast<int64_t>(p.M) * p.N, SM = static_cast<int64_t>(p.nblocks) * p.M;
+        if (p.q) quantize_token(h, p.q + m * p.N + n, p.s + static_cast<int64_t>(nt) * p.M + m, n_here, p.pow2 != 0, lane);
+        if (p.ck) {
+          quantize_token(g, p.ck + m * p.N + n, p.cks + static_cast<int64_t>(nt) * p.M + m, n_here, p.pow2 != 0, lane);
+          quantize_token(u, p.ck + MN + m * p.N + n, p.cks + SM + static_cast<int64_t>(nt) * p.M + m, n_here, p.pow2 != 0, lane);
         }
       }
     }
@@ -522,6 +537,7 @@ int launch_block_few(const GemmArgs8& a, cudaStream_t st) {
   p.y = a.y;
   p.ldy = a.ldy;
   p.y_f32 = a.ydt == ZQ_OUT_F32;
+  p.y_vec = (reinterpret_cast<uintptr_t>(a.y) & (p.y_f32 ? 15u : 7u)) == 0 && a.ldy % 4 == 0;
   p.q = a.q;
   p.s = a.s;
   p.ck = a.ck;
