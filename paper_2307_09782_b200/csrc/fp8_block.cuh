@@ -50,9 +50,8 @@ int launch_quantize_weight_block(const float* w, int64_t N, int64_t K, int mode,
 int launch_transpose_weight_block(const uint8_t* q, const float* s, int64_t N, int64_t K, uint8_t* qt, float* st_,
                                   cudaStream_t st);
 int launch_block_gemm(const GemmArgs8& a, cudaStream_t st);  // many tokens
-constexpr int64_t kFewTokens = 64;
-bool few_takes(const GemmArgs8& a);
-bool few_takes_raw(const GemmArgs8& a);
+bool few_takes(const GemmArgs8& a);      // which of the two
+bool few_takes_raw(const GemmArgs8& a);  // whether launch_block_few quantizes raw activations itself
 int launch_block_few(const GemmArgs8& a, cudaStream_t st);   // few tokens
 struct WgradArgs {
   const void* g;     // bf16 [parts] x [M][ldg], g_stride elements apart

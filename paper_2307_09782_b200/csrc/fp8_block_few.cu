@@ -518,8 +518,41 @@ constexpr int ctas_per_sm(bool gated) {
 
 }  // namespace
 
-bool few_takes(const GemmArgs8& a) { return a.kind != kGatedBwd && a.M <= kFewTokens; }
-bool few_takes_raw(const GemmArgs8& a) { return few_takes(a) && a.M <= 16; }
+namespace {
+
+int few_width(int64_t M) { return M <= 16 ? 16 : (M <= 32 ? 32 : 64); }
+int few_slots(int bm, bool gated) {
+  return sm_count() * (bm == 16 ? ctas_per_sm<16>(gated) : (bm == 32 ? ctas_per_sm<32>(gated) : ctas_per_sm<64>(gated)));
+}
+// The widest cluster with which all CTAs are resident at once and none has fewer than two K blocks.
+int few_cluster(int64_t tiles, int64_t kb_all, int slots) {
+  int c = 1;
+  while (c < 8 && tiles * c * 2 <= slots && kb_all >= c * 4) c *= 2;
+  return c;
+}
+
+}  // namespace
+
+// Which of the two kernels.  Up to 32 tokens this one: it streams the weights at 0.8 - 0.9 of the copy bandwidth.  Beyond, the
+// one that is expected to be done first.  Here a CTA with 64 tokens takes 0.75 us per K block (gated: 0.85), all of it in
+// `waves`, and 4 us more; the other kernel 0.6 us per K block of a tile of 128 x 256 and 2 us more.  Measured (us, this
+// kernel / the other): 64 tokens 4096 -> 4096 9.7 / 19.6, 17920 -> 6656 29 / 71, 7168 -> 28672 44.5 / 39.6, gated 4096 ->
+// 11008 29 / 23.5; 256 tokens 4096 -> 4096 17 / 22, 11008 -> 4096 35 / 50; 512 tokens 4096 -> 4096 28 / 22.
+bool few_takes(const GemmArgs8& a) {
+  if (a.kind == kGatedBwd) return false;
+  if (a.M <= 32) return true;
+  const bool gated = a.kind == kGated;
+  const int64_t kb = blocks_of(a.K) * (gated ? 1 : a.parts), nb = blocks_of(a.N);
+  const int slots = few_slots(64, gated);
+  const int64_t tiles = (a.M + 63) / 64 * nb;
+  const int c = few_cluster(tiles, kb, slots);
+  const int64_t waves = (tiles * c + slots - 1) / slots;
+  const int64_t here = 4000 + waves * ((kb + c - 1) / c) * (gated ? 850 : 750);
+  const int64_t cols = gated ? nb : (a.N + 255) / 256;
+  const int64_t rounds = ((a.M + 127) / 128 * cols + sm_count() - 1) / sm_count();
+  return here < 2000 + rounds * kb * 600;
+}
+bool few_takes_raw(const GemmArgs8& a) { return a.M <= 16 && a.kind != kGatedBwd; }
 
 int launch_block_few(const GemmArgs8& a, cudaStream_t st) {
   const bool gated = a.kind == kGated, raw = a.x != nullptr;
@@ -545,11 +578,11 @@ int launch_block_few(const GemmArgs8& a, cudaStream_t st) {
   p.act = a.act;
   p.pow2 = a.mode == ZQ_SCALE_M1;
   p.status = a.status;
-  const int bm = a.M <= 16 ? 16 : (a.M <= 32 ? 32 : 64);
-  const int slots = sm_count() * (bm == 16 ? ctas_per_sm<16>(gated) : (bm == 32 ? ctas_per_sm<32>(gated) : ctas_per_sm<64>(gated)));
-  // the widest cluster with which all CTAs are resident at once and none has fewer than two K blocks
-  p.cluster = 1;
-  while (p.cluster < 8 && p.n_tiles * p.cluster * 2 <= slots && p.segs * p.kblocks >= p.cluster * 4) p.cluster *= 2;
+  const int bm = few_width(a.M);
+  const int64_t m_tiles64 = (a.M + bm - 1) / bm;
+  if (m_tiles64 > 65535) return ZQ_ERR_SHAPE;
+  const int m_tiles = static_cast<int>(m_tiles64);
+  p.cluster = few_cluster(m_tiles64 * p.n_tiles, static_cast<int64_t>(p.segs) * p.kblocks, few_slots(bm, gated));
   if (static_cast<int64_t>(p.n_tiles) * p.cluster > 0x7FFFFFFF) return ZQ_ERR_SHAPE;
   CUtensorMap tw, tq;
   if (!make_code_map(&tw, a.b, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.N),
@@ -561,15 +594,15 @@ int launch_block_few(const GemmArgs8& a, cudaStream_t st) {
                           static_cast<uint32_t>(bm)))
     return ZQ_ERR_CUDA;
   if (gated) {
-    if (raw) return launch_cfg<16, true, true>(tw, tq, p, 1, st);
-    if (bm == 16) return launch_cfg<16, true, false>(tw, tq, p, 1, st);
-    if (bm == 32) return launch_cfg<32, true, false>(tw, tq, p, 1, st);
-    return launch_cfg<64, true, false>(tw, tq, p, 1, st);
+    if (raw) return launch_cfg<16, true, true>(tw, tq, p, m_tiles, st);
+    if (bm == 16) return launch_cfg<16, true, false>(tw, tq, p, m_tiles, st);
+    if (bm == 32) return launch_cfg<32, true, false>(tw, tq, p, m_tiles, st);
+    return launch_cfg<64, true, false>(tw, tq, p, m_tiles, st);
   }
-  if (raw) return launch_cfg<16, false, true>(tw, tq, p, 1, st);
-  if (bm == 16) return launch_cfg<16, false, false>(tw, tq, p, 1, st);
-  if (bm == 32) return launch_cfg<32, false, false>(tw, tq, p, 1, st);
-  return launch_cfg<64, false, false>(tw, tq, p, 1, st);
+  if (raw) return launch_cfg<16, false, true>(tw, tq, p, m_tiles, st);
+  if (bm == 16) return launch_cfg<16, false, false>(tw, tq, p, m_tiles, st);
+  if (bm == 32) return launch_cfg<32, false, false>(tw, tq, p, m_tiles, st);
+  return launch_cfg<64, false, false>(tw, tq, p, m_tiles, st);
 }
 
 }  // namespace fp8b

@@ -86,33 +86,51 @@ __device__ __forceinline__ void tile_of(const P8& p, int pos, int& mt, int& nt) 
 __device__ __forceinline__ void stage_put(uint4* buf, int lane, int piece, uint4 v) { buf[lane * 8 + (piece ^ (lane & 7))] = v; }
 __device__ __forceinline__ uint4 stage_get(const uint4* buf, int row, int piece) { return buf[row * 8 + (piece ^ (row & 7))]; }
 
-// Staged rows -> global memory, `rows` of them and `bytes` of each; ES: element size for the ragged and unaligned ends.
+// Staged rows -> global memory, `rows` of them and `bytes` of each; ES: element size.  Rows that do not start on 16-byte
+// boundaries are written row by row, neighbouring lanes neighbouring elements.
 template <int PIECES, int ES>
 __device__ __forceinline__ void store_rows(const uint4* buf, uint8_t* dst, int64_t ld_bytes, int rows, int bytes, bool vec,
                                            int lane) {
   __syncwarp();
-  constexpr int kRowsPer = 32 / PIECES;
+  if (vec) {
+    constexpr int kRowsPer = 32 / PIECES;
 #pragma unroll
-  for (int it = 0; it < PIECES; ++it) {
-    const int r = it * kRowsPer + lane / PIECES, c = lane % PIECES;
-    if (r < rows && c * 16 < bytes) {
-      const uint4 v = stage_get(buf, r, c);
-      uint8_t* d = dst + r * ld_bytes + c * 16;
-      if (vec && c * 16 + 16 <= bytes) {
-        *reinterpret_cast<uint4*>(d) = v;
-      } else {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    for (int it = 0; it < PIECES; ++it) {
+      const int r = it * kRowsPer + lane / PIECES, c = lane % PIECES;
+      if (r < rows && c * 16 < bytes) {
+        const uint4 v = stage_get(buf, r, c);
+        uint8_t* d = dst + r * ld_bytes + c * 16;
+        if (ES == 1 || c * 16 + 16 <= bytes) {  // (rows of codes are multiples of 16 bytes)
+          *reinterpret_cast<uint4*>(d) = v;
+        } else {
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int e = 0; e < 16 / ES; ++e)
-          if (c * 16 + e * ES < bytes) {
-            if (ES == 4) reinterpret_cast<uint32_t*>(d)[e] = w[e];
-            if (ES == 2) reinterpret_cast<uint16_t*>(d)[e] = static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)));
-          }
+          for (int e = 0; e < 16 / ES; ++e)
+            if (c * 16 + e * ES < bytes) {
+              if (ES == 4) reinterpret_cast<uint32_t*>(d)[e] = w[e];
+              if (ES == 2) reinterpret_cast<uint16_t*>(d)[e] = static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)));
+            }
+        }
+      }
+    }
+  } else if (ES > 1) {
+#pragma unroll 1
+    for (int r = 0; r < rows; ++r) {
+      uint8_t* d = dst + r * ld_bytes;
+#pragma unroll
+      for (int o = 0; o < PIECES * 16; o += 32 * ES) {
+        const int at = o + lane * ES;  // byte of the row
+        const uint8_t* src = reinterpret_cast<const uint8_t*>(buf + r * 8 + ((at >> 4) ^ (r & 7))) + (at & 15);
+        if (at < bytes) {
+          if (ES == 4) *reinterpret_cast<uint32_t*>(d + at) = *reinterpret_cast<const uint32_t*>(src);
+          if (ES == 2) *reinterpret_cast<uint16_t*>(d + at) = *reinterpret_cast<const uint16_t*>(src);
+        }
       }
     }
   }
   __syncwarp();
 }
+
 // Accumulator columns -> run (packed pairs) += scale * columns, in pieces of 32 and 16 columns that alternate between two
 // register buffers, so that one is in flight while the other is added up.  (Each wait drains everything in flight; pieces
 // of 16 alone make eight waits of it, and two buffers of 32 do not fit beside 128 sums.)
