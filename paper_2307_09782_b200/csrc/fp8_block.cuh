@@ -166,23 +166,6 @@ __device__ __forceinline__ bool mbar_wait_all(uint64_t* bar, uint32_t parity, vo
   return __all_sync(0xFFFFFFFFu, ok);
 }
 
-// The pair form of the E4M3 MMA: 256 rows (128 in each CTA), each CTA holding half of the N rows of B.
-__device__ __forceinline__ void umma_f8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
-                                             uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-
-// Arrive on a barrier of any CTA of the cluster without publishing memory: what it hands over is tensor memory that has been
-// read (the loads are waited for), and a release at cluster scope waits about 1000 cycles for the warp's other stores.
-__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
-  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-
 __device__ __forceinline__ void raise_error8(int* status, volatile int* abort_flag, int detail) {
   *abort_flag = 1;
   if (atomicCAS(status, 0, ZQ_ERR_DEVICE_TIMEOUT) == 0) status[1] = detail;

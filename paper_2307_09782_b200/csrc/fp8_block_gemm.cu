@@ -8,11 +8,16 @@
 // is rounded between the blocks).
 // Orientation: token rows are the lanes (the MMA's 128-row operand), so that a thread's scale sa * sb is ONE number
 // for its 128 columns, and a promotion is one packed FMA per two columns.
-// Tile of a CTA: 128 tokens x 256 columns, two accumulators of 256 columns = all of tensor memory, eight epilogue
-// warps with 128 running sums per thread.  With more than 128 tokens two CTAs of a cluster share the columns
-// (cta_group::2): a pair's MMAs take 256 tokens x 128 columns of which each CTA holds 64 in its shared memory, and the two
-// column halves have accumulators, barriers and epilogue warps of their own, so that one half's waits fall into the
-// other's additions.  (A single CTA's MMAs of 128 columns read 128 bytes per cycle: 716 cycles a block instead of 480.)
+// Tile: 128 tokens x 256 columns, two accumulators of 256 columns = all of tensor memory, eight epilogue warps with 128
+// running sums per thread.  The two column halves (four warps each) give their accumulators back separately.
+//
+// What bounds it: the way of an accumulator from the MMAs to the epilogue warps and back.  Per K block the MMAs take 480
+// cycles, the promotion 460 (286 alone; tensor memory serves both), and commit, waits and hand-over 350: about 870 with two
+// accumulators, 59 % of the tensor core's cycles.  Tried and not faster: CTA pairs with four accumulators of 128
+// columns (the same time; with single CTAs MMAs of 128 columns read the token operand twice, 716 cycles), sixteen epilogue
+// warps (5 % faster without the gated epilogues, which then spill), polling instead of parked waits (slower).
+// No spills: with 227 KB of shared memory the first-level cache holds none of them; 100 bytes per thread in the gradient's
+// epilogue doubled the kernel's time.
 //
 // Warp roles: 0..7 epilogue (lane quarter warp % 4, column half warp / 4), 8 producer, 9 tensor memory and MMAs,
 // 10 and 11 scales.
@@ -30,27 +35,25 @@ constexpr int kTileM = 128, kTileN = 256;  // of one CTA
 constexpr int kEpiWarps = 8, kEpiThreads = 256;
 constexpr int kProducerWarp = 8, kMmaWarp = 9;
 constexpr int kThreads = 384;  // three warpgroups; the two epilogue ones take registers over from the third
-// 384 threads start with 168 registers each: 2 x 128 x 224 + 128 x 56 is what the block was given
-constexpr int kEpiRegs = 224, kOtherRegs = 56;
-static_assert(256 * kEpiRegs + 128 * kOtherRegs <= kThreads * 168, "register split");
-constexpr int kStageBuf = 32 * 128;  // staging of one epilogue warp: 32 rows of 128 bytes
-template <bool PAIR>
-struct Cfg8 {
-  static constexpr int kABytes = kTileM * kBlk;
-  static constexpr int kBBytes = (PAIR ? kTileN / 2 : kTileN) * kBlk;  // a pair's CTAs hold half of the columns each
-  static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kStages = PAIR ? 6 : 4;
-  static constexpr int offA = 0;
-  static constexpr int offB = offA + kStages * kABytes;
-  static constexpr int offStage = offB + kStages * kBBytes;
-  static constexpr int offBars = offStage + kEpiWarps * kStageBuf;
-  static constexpr int kNumBars = 2 * kStages + 12 + 1;
-  static constexpr int offScale = offBars + ((kNumBars * 8 + 15) / 16) * 16;  // [2 halves][2 accumulators][kScaleRow] scales of a K block
-  static constexpr int kScaleRow = kTileM + 4;  // the rows' scales, then the columns' (kGated: gate, up)
-  static constexpr int offMisc = offScale + 4 * kScaleRow * 4;
-  static constexpr int kSmemBytes = offMisc + 16;
-  static_assert(kSmemBytes <= 227 * 1024, "shared memory");
+// 384 threads start with 168 registers each; 2 x 128 x epilogue + 128 x other is what the block was given
+template <int KIND>
+struct Regs {
+  static constexpr int kEpi = KIND == kGatedBwd ? 232 : (KIND == kGated ? 216 : 224);
+  static constexpr int kOther = 3 * 168 - 2 * kEpi;
 };
+constexpr int kStageBuf = 32 * 128;  // staging of one epilogue warp: 32 rows of 128 bytes
+constexpr int kStages = 4;
+constexpr int kABytes = kTileM * kBlk, kBBytes = kTileN * kBlk;
+constexpr int kOffA = 0;
+constexpr int kOffB = kOffA + kStages * kABytes;
+constexpr int kOffStage = kOffB + kStages * kBBytes;
+constexpr int kOffBars = kOffStage + kEpiWarps * kStageBuf;
+constexpr int kNumBars = 2 * kStages + 8 + 1;
+constexpr int kOffScale = kOffBars + ((kNumBars * 8 + 15) / 16) * 16;  // [2 halves][2 accumulators][kScaleRow] scales of a K block
+constexpr int kScaleRow = kTileM + 4;  // the rows' scales, then the columns' (kGated: gate, up)
+constexpr int kOffMisc = kOffScale + 4 * kScaleRow * 4;
+constexpr int kSmemBytes = kOffMisc + 16;
+static_assert(kSmemBytes <= 227 * 1024, "shared memory");
 
 enum { kErrProducer8 = 21, kErrMma8 = 22, kErrEpilogue8 = 23, kErrAlign8 = 24, kErrScale8 = 25 };
 
@@ -174,23 +177,20 @@ __device__ __forceinline__ void rotate(uint64_t* run) {
   for (int e = 0; e < N; ++e) run[64 - N + e] = t[e];
 }
 
-template <int KIND, int ACT, bool F32, bool PAIR>
+template <int KIND, int ACT, bool F32>
 __global__ void __launch_bounds__(kThreads, 1)
 fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const P8 p) {
-  using C = Cfg8<PAIR>;
-  constexpr int kStages = C::kStages;
   extern __shared__ __align__(1024) uint8_t smem[];
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::offBars);
-  uint64_t* full = bars;                 // [stages] the stage's copies landed; PAIR: of both CTAs, the leader's counts (MMA waits)
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBars);
+  uint64_t* full = bars;                 // [stages] the stage's copies landed           (MMA waits)
   uint64_t* empty = full + kStages;      // [stages] the MMAs that read it are done       (producer waits)
   // per column half h and accumulator a, at 2 h + a:
   uint64_t* acc_full = empty + kStages;  // [4] a K block's products are in the accumulator, its scales in shared memory (epilogue waits)
-  uint64_t* acc_empty = acc_full + 4;    // [4] the half's epilogue warps (PAIR: of both CTAs, the leader's counts) have read it (MMA waits)
-  uint64_t* sc_empty = acc_empty + 4;    // [4] this CTA's have                           (scale warp waits)
-  uint64_t* drain_bar = sc_empty + 4;
-  float* s_scale = reinterpret_cast<float*>(smem + C::offScale);
-  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + C::offMisc);
-  volatile int* s_abort = reinterpret_cast<volatile int*>(smem + C::offMisc + 4);
+  uint64_t* acc_empty = acc_full + 4;    // [4] the half's epilogue warps have read it (MMA, scale warp wait)
+  uint64_t* drain_bar = acc_empty + 4;
+  float* s_scale = reinterpret_cast<float*>(smem + kOffScale);
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + kOffMisc);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(smem + kOffMisc + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -200,8 +200,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(&acc_full[i], 2);  // the MMAs' commit and the half's scale warp
-      mbar_init(&acc_empty[i], PAIR ? kEpiWarps : kEpiWarps / 2);
-      mbar_init(&sc_empty[i], kEpiWarps / 2);
+      mbar_init(&acc_empty[i], kEpiWarps / 2);
     }
     mbar_init(drain_bar, 1);
     *s_abort = 0;
@@ -212,29 +211,18 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     prefetch_tensormap(&tm_a);
     prefetch_tensormap(&tm_b);
   }
-  if (warp == kMmaWarp) {
-    if (PAIR)
-      tmem_alloc_pair(s_tmem, 512);
-    else
-      tmem_alloc(s_tmem, 512);
-  }
+  if (warp == kMmaWarp) tmem_alloc(s_tmem, 512);
   tc_fence_before_sync();
-  if (PAIR)
-    cluster_sync_all();  // both CTAs' barriers are initialized and their tensor memory is allocated
-  else
-    __syncthreads();
+  __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem_base = *s_tmem;
   const bool ok_start = *s_abort == 0;
-  const int rank = PAIR ? static_cast<int>(cluster_ctarank()) : 0;
-  const int worker = PAIR ? static_cast<int>(blockIdx.x >> 1) : static_cast<int>(blockIdx.x);
-  const int workers = PAIR ? static_cast<int>(gridDim.x >> 1) : static_cast<int>(gridDim.x);
   const int tiles = p.m_tiles * p.n_tiles;
   const int kb_all = p.segs * p.kblocks;
   if (threadIdx.x == 0) pdl_launch_dependents();
 
   if (warp >= kEpiWarps) {
-  regs_give<kOtherRegs>();
+  regs_give<Regs<KIND>::kOther>();
   if (warp == kProducerWarp) {
     if (ok_start) {
       const bool issuer = elect_one();
@@ -242,7 +230,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       int s = 0, issued = 0;
       uint32_t ph = 0;
       bool ok = true;
-      for (int pos = worker; ok && pos < tiles; pos += workers) {
+      for (int pos = blockIdx.x; ok && pos < tiles; pos += gridDim.x) {
         int mt, nt;
         tile_of(p, pos, mt, nt);
         for (int i = 0; i < kb_all; ++i) {
@@ -254,28 +242,17 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
           if (issuer) {
             const int seg = KIND == kPlain && i >= p.kblocks ? 1 : 0;  // at most two segments
             const int k = (i - seg * p.kblocks) * kBlk;
-            uint8_t* sa = smem + C::offA + s * C::kABytes;
-            uint8_t* sb = smem + C::offB + s * C::kBBytes;
-            if (PAIR) {
-              // each CTA brings its own token rows and, of each column half, 64 columns (kGated: the leader the gate's,
-              // its peer the up projection's); all of it is counted on the leader's barrier
-              const uint32_t bar = map_to_rank(smem_u32(&full[s]), 0);
-              if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * C::kStageBytes);
-              tma_load_3d_pair(sa, &tm_a, k, (2 * mt + rank) * kTileM, seg, bar);
-#pragma unroll
-              for (int h = 0; h < 2; ++h)
-                tma_load_3d_pair(sb + h * (C::kBBytes / 2), &tm_b, k,
-                                 KIND == kGated ? nt * kBlk + h * 64 : nt * kTileN + h * kBlk + rank * 64,
-                                 KIND == kGated ? rank : seg, bar);
-            } else {
-              mbar_arrive_expect_tx(&full[s], C::kStageBytes);
-              tma_load_3d(sa, &tm_a, k, mt * kTileM, seg, &full[s]);
-              // the columns by 64, in the same order
+            uint8_t* sa = smem + kOffA + s * kABytes;
+            uint8_t* sb = smem + kOffB + s * kBBytes;
+            mbar_arrive_expect_tx(&full[s], kABytes + kBBytes);
+            tma_load_3d(sa, &tm_a, k, mt * kTileM, seg, &full[s]);
+            // the columns; kGated: per column half 64 of the gate and the same 64 of the up projection
+            if (KIND == kGated) {
 #pragma unroll
               for (int h = 0; h < 4; ++h)
-                tma_load_3d(sb + h * (C::kBBytes / 4), &tm_b, k,
-                            KIND == kGated ? nt * kBlk + (h >> 1) * 64 : nt * kTileN + h * 64, KIND == kGated ? h & 1 : seg,
-                            &full[s]);
+                tma_load_3d(sb + h * (kBBytes / 4), &tm_b, k, nt * kBlk + (h >> 1) * 64, h & 1, &full[s]);
+            } else {
+              tma_load_3d(sb, &tm_b, k, nt * kTileN, seg, &full[s]);
             }
           }
           __syncwarp();
@@ -286,58 +263,37 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
           }
         }
       }
-      // never leave with copies still in flight (PAIR: the stages filled last are released by the MMAs that read them)
+      // never leave with copies still in flight
       for (int i = max(0, issued - kStages); i < issued; ++i) {
-        uint64_t* bar = PAIR ? &empty[i % kStages] : &full[i % kStages];
         uint32_t spin = 0;
-        while (!mbar_try_wait(bar, (i / kStages) & 1) && ++spin < kSpinLimit && !(PAIR && *s_abort)) {
+        while (!mbar_try_wait(&full[i % kStages], (i / kStages) & 1) && ++spin < kSpinLimit) {
         }
       }
     }
   } else if (warp == kMmaWarp) {
-    if (ok_start && rank == 0) {
+    if (ok_start) {
       const bool issuer = elect_one();
-      const uint64_t adesc0 = umma_desc_k128(smem_u32(smem + C::offA));
-      const uint64_t bdesc0 = umma_desc_k128(smem_u32(smem + C::offB));
-      // a pair's MMAs take one column half each: 256 rows x 128 columns
-      const uint32_t idesc = PAIR ? umma_idesc_e4m3(kTileN / 2) + ((128u >> 4) << 24) : umma_idesc_e4m3(kTileN);
+      const uint64_t adesc0 = umma_desc_k128(smem_u32(smem + kOffA));
+      const uint64_t bdesc0 = umma_desc_k128(smem_u32(smem + kOffB));
+      const uint32_t idesc = umma_idesc_e4m3(kTileN);
       int s = 0;
       uint32_t ph = 0;
       bool failed = false;
       int count = 0;  // K blocks so far: block c goes to accumulator c % 2
-      for (int pos = worker; !failed && pos < tiles; pos += workers) {
+      for (int pos = blockIdx.x; !failed && pos < tiles; pos += gridDim.x) {
         for (int i = 0; i < kb_all; ++i, ++count) {
           const int buf = count & 1;
           const uint32_t free_ph = ((count >> 1) - 1) & 1;
           if (!mbar_wait(&full[s], ph, s_abort) || (count >= 2 && !mbar_wait(&acc_empty[buf], free_ph, s_abort)) ||
-              (!PAIR && count >= 2 && !mbar_wait(&acc_empty[2 + buf], free_ph, s_abort))) {
+              (count >= 2 && !mbar_wait(&acc_empty[2 + buf], free_ph, s_abort))) {
             failed = true;
             break;
           }
           tc_fence_after_sync();
-          const uint64_t ad = adesc0 + static_cast<uint64_t>((s * C::kABytes) >> 4);
-          const uint64_t bd = bdesc0 + static_cast<uint64_t>((s * C::kBBytes) >> 4);
+          const uint64_t ad = adesc0 + static_cast<uint64_t>((s * kABytes) >> 4);
+          const uint64_t bd = bdesc0 + static_cast<uint64_t>((s * kBBytes) >> 4);
           const uint32_t d = tmem_base + buf * kTileN;
-          if (PAIR) {
-            if (issuer) {
-#pragma unroll
-              for (int k = 0; k < kBlk / 32; ++k) umma_f8_pair(d, ad + 2 * k, bd + 2 * k, idesc, k > 0 ? 1u : 0u);
-              umma_commit_pair(&acc_full[buf]);
-            }
-            __syncwarp();
-            if (count >= 2 && !mbar_wait(&acc_empty[2 + buf], free_ph, s_abort)) {
-              failed = true;
-              break;
-            }
-            tc_fence_after_sync();
-            if (issuer) {
-#pragma unroll
-              for (int k = 0; k < kBlk / 32; ++k)
-                umma_f8_pair(d + kTileN / 2, ad + 2 * k, bd + ((C::kBBytes / 2) >> 4) + 2 * k, idesc, k > 0 ? 1u : 0u);
-              umma_commit_pair(&acc_full[2 + buf]);
-              umma_commit_pair(&empty[s]);
-            }
-          } else if (issuer) {
+          if (issuer) {
 #pragma unroll
             for (int k = 0; k < kBlk / 32; ++k) umma_f8(d, ad + 2 * k, bd + 2 * k, idesc, k > 0 ? 1u : 0u);
             umma_commit(&acc_full[buf]);
@@ -353,12 +309,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       }
       if (failed && issuer) raise_error8(p.status, s_abort, kErrMma8);
       // tensor memory is released only when every MMA has completed, also where another role has given up
-      if (issuer) {
-        if (PAIR)
-          umma_commit_pair(drain_bar);
-        else
-          umma_commit(drain_bar);
-      }
+      if (issuer) umma_commit(drain_bar);
       uint32_t spin = 0;
       while (!mbar_try_wait(drain_bar, 0) && ++spin < kSpinLimit) {
       }
@@ -373,10 +324,10 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     pdl_wait();
     int count = 0;
     bool ok = true;
-    for (int pos = worker; ok && pos < tiles; pos += workers) {
+    for (int pos = blockIdx.x; ok && pos < tiles; pos += gridDim.x) {
       int mt, nt;
       tile_of(p, pos, mt, nt);
-      const int m0 = (PAIR ? 2 * mt + rank : mt) * kTileM + lane;
+      const int m0 = mt * kTileM + lane;
       // columns: block 2 nt + h (kGated: lane 0 block nt of the gate, lane 1 of the up projection)
       const int64_t part = static_cast<int64_t>(p.nblocks) * p.kblocks;
       const float* sb = p.sb + static_cast<int64_t>(KIND == kGated ? nt : min(2 * nt + h, p.nblocks - 1)) * p.kblocks +
@@ -398,11 +349,11 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
           const int i = i0 + u;
           if (ok && i < kb_all) {
             const int slot = 2 * h + (count & 1);
-            if (count >= 2 && !mbar_wait_all(&sc_empty[slot], ((count >> 1) - 1) & 1, s_abort)) {
+            if (count >= 2 && !mbar_wait_all(&acc_empty[slot], ((count >> 1) - 1) & 1, s_abort)) {
               if (lane == 0) raise_error8(p.status, s_abort, kErrScale8);
               ok = false;
             } else {
-              float* d = s_scale + slot * C::kScaleRow;
+              float* d = s_scale + slot * kScaleRow;
 #pragma unroll
               for (int j = 0; j < 4; ++j) d[32 * j + lane] = a[u][j];
               if (lane < 2) d[kTileM + lane] = b[u];
@@ -418,15 +369,15 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   }
   } else {
     // ---- epilogue warps
-    regs_take<kEpiRegs>();
+    regs_take<Regs<KIND>::kEpi>();
     const int quarter = warp & 3, half = warp >> 2;
     const int row = quarter * 32 + lane;
     const uint32_t lane_base = static_cast<uint32_t>(quarter * 32) << 16;
-    uint4* buf = reinterpret_cast<uint4*>(smem + C::offStage + warp * kStageBuf);
+    uint4* buf = reinterpret_cast<uint4*>(smem + kOffStage + warp * kStageBuf);
     bool failed = !ok_start;
     int count = 0;
     pdl_wait();
-    for (int pos = worker; pos < tiles; pos += workers) {
+    for (int pos = blockIdx.x; pos < tiles; pos += gridDim.x) {
       uint64_t run[64];
 #pragma unroll
       for (int e = 0; e < 64; ++e) run[e] = 0ull;
@@ -438,23 +389,17 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         }
         tc_fence_after_sync();
         if (!failed) {
-          const float* sc = s_scale + b * C::kScaleRow;
+          const float* sc = s_scale + b * kScaleRow;
           const float sr = sc[row], s0 = sr * sc[kTileM], s1 = KIND == kGated ? sr * sc[kTileM + 1] : s0;
           promote(tmem_base + (count & 1) * kTileN + half * (kTileN / 2) + lane_base, run, s0, s1);
         }
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0 && !failed) {
-          if (PAIR)
-            mbar_arrive_cluster_relaxed(map_to_rank(smem_u32(&acc_empty[b]), 0));
-          else
-            mbar_arrive(&acc_empty[b]);
-          mbar_arrive(&sc_empty[b]);
-        }
+        if (lane == 0 && !failed) mbar_arrive(&acc_empty[b]);
       }
       int mt, nt;
       tile_of(p, pos, mt, nt);
-      const int m0 = (PAIR ? 2 * mt + rank : mt) * kTileM, m = m0 + row;
+      const int m0 = mt * kTileM, m = m0 + row;
       const bool m_ok = m < p.M;
       const int wm0 = m0 + quarter * 32;
       const int rows = failed ? 0 : min(32, p.M - wm0);  // may be <= 0
@@ -489,7 +434,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         float* u = g + 64;
         const int64_t MN = static_cast<int64_t>(p.M) * p.N, SM = static_cast<int64_t>(p.nblocks) * p.M;
         float* mine = reinterpret_cast<float*>(buf);
-        const float* other = reinterpret_cast<const float*>(smem + C::offStage + (warp ^ 4) * kStageBuf);
+        const float* other = reinterpret_cast<const float*>(smem + kOffStage + (warp ^ 4) * kStageBuf);
         // columns beyond N hold zeros (the copy engine filled the operand with zeros): they do not move a maximum
         if (p.ck) {
           uint32_t ag = 0u, au = 0u;
@@ -655,58 +600,34 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   }
 
   tc_fence_before_sync();
-  if (PAIR)
-    cluster_sync_all();  // both CTAs are done with both CTAs' tensor memory and barriers
-  else
-    __syncthreads();
+  __syncthreads();
   if (warp == kMmaWarp) {
     tc_fence_after_sync();
-    if (PAIR)
-      tmem_dealloc_pair(tmem_base, 512);
-    else
-      tmem_dealloc(tmem_base, 512);
+    tmem_dealloc(tmem_base, 512);
   }
 }
 
-template <int KIND, int ACT, bool F32, bool PAIR>
+template <int KIND, int ACT, bool F32>
 int launch_cfg(const CUtensorMap& ta, const CUtensorMap& tb, const P8& p, cudaStream_t st) {
   static std::once_flag once;
   static cudaError_t attr = cudaSuccess;
   std::call_once(once, [] {
-    attr = cudaFuncSetAttribute(fp8_block_gemm_kernel<KIND, ACT, F32, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                Cfg8<PAIR>::kSmemBytes);
+    attr = cudaFuncSetAttribute(fp8_block_gemm_kernel<KIND, ACT, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   });
   if (attr != cudaSuccess) return ZQ_ERR_CUDA;
-  const int tiles = p.m_tiles * p.n_tiles, slots = PAIR ? sm_count() / 2 : sm_count();
-  const unsigned workers = static_cast<unsigned>(tiles < slots ? tiles : slots);
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(PAIR ? 2 * workers : workers);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = Cfg8<PAIR>::kSmemBytes;
-  cfg.stream = st;
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = PAIR ? 2 : 1;
-  at[1].val.clusterDim.y = 1;
-  at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 2;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, fp8_block_gemm_kernel<KIND, ACT, F32, PAIR>, ta, tb, p);
+  const int tiles = p.m_tiles * p.n_tiles;
+  const unsigned grid = static_cast<unsigned>(tiles < sm_count() ? tiles : sm_count());
+  const cudaError_t e = launch_chained(fp8_block_gemm_kernel<KIND, ACT, F32>, dim3(grid), dim3(kThreads), kSmemBytes, st, false,
+                                       ta, tb, p);
   count_launch();
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
 }
 
-template <int KIND, int ACT, bool F32>
-int launch_pair(bool pair, const CUtensorMap& ta, const CUtensorMap& tb, const P8& p, cudaStream_t st) {
-  return pair ? launch_cfg<KIND, ACT, F32, true>(ta, tb, p, st) : launch_cfg<KIND, ACT, F32, false>(ta, tb, p, st);
-}
 template <int KIND>
-int launch_act(int act, bool pair, const CUtensorMap& ta, const CUtensorMap& tb, const P8& p, cudaStream_t st) {
-  if (act == ZQ_ACT_SILU) return launch_pair<KIND, ZQ_ACT_SILU, false>(pair, ta, tb, p, st);
-  if (act == ZQ_ACT_GELU_TANH) return launch_pair<KIND, ZQ_ACT_GELU_TANH, false>(pair, ta, tb, p, st);
-  return launch_pair<KIND, ZQ_ACT_RELU, false>(pair, ta, tb, p, st);
+int launch_act(int act, const CUtensorMap& ta, const CUtensorMap& tb, const P8& p, cudaStream_t st) {
+  if (act == ZQ_ACT_SILU) return launch_cfg<KIND, ZQ_ACT_SILU, false>(ta, tb, p, st);
+  if (act == ZQ_ACT_GELU_TANH) return launch_cfg<KIND, ZQ_ACT_GELU_TANH, false>(ta, tb, p, st);
+  return launch_cfg<KIND, ZQ_ACT_RELU, false>(ta, tb, p, st);
 }
 
 }  // namespace
@@ -719,11 +640,9 @@ int launch_block_gemm(const GemmArgs8& a, cudaStream_t st) {
   p.kblocks = static_cast<int>(blocks_of(a.K));
   p.segs = a.kind == kPlain ? a.parts : 1;
   p.nblocks = static_cast<int>(blocks_of(a.N));
-  const bool pair = a.M > kTileM;  // otherwise the second CTA of a pair would have no rows
-  const int64_t tile_rows = pair ? 2 * kTileM : kTileM;
-  p.m_tiles = static_cast<int>((a.M + tile_rows - 1) / tile_rows);
+  p.m_tiles = static_cast<int>((a.M + kTileM - 1) / kTileM);
   p.n_tiles = a.kind == kGated ? p.nblocks : static_cast<int>((a.N + kTileN - 1) / kTileN);
-  p.m_group = pair ? 8 : 16;
+  p.m_group = 16;
   const int64_t tiles = static_cast<int64_t>(p.m_tiles) * p.n_tiles;
   if (tiles > 0x3FFFFFFF) return ZQ_ERR_SHAPE;
   p.sa = a.sa;
@@ -740,12 +659,12 @@ int launch_block_gemm(const GemmArgs8& a, cudaStream_t st) {
   CUtensorMap ta, tb;
   if (!make_code_map(&ta, a.a, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.M), static_cast<uint64_t>(p.segs), kTileM) ||
       !make_code_map(&tb, a.b, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.N),
-                     a.kind == kGated ? 2u : static_cast<uint64_t>(p.segs), 64))
+                     a.kind == kGated ? 2u : static_cast<uint64_t>(p.segs), a.kind == kGated ? 64 : kTileN))
     return ZQ_ERR_CUDA;
-  if (a.kind == kGated) return launch_act<kGated>(a.act, pair, ta, tb, p, st);
-  if (a.kind == kGatedBwd) return launch_act<kGatedBwd>(a.act, pair, ta, tb, p, st);
-  return a.ydt == ZQ_OUT_F32 ? launch_pair<kPlain, ZQ_ACT_RELU, true>(pair, ta, tb, p, st)
-                             : launch_pair<kPlain, ZQ_ACT_RELU, false>(pair, ta, tb, p, st);
+  if (a.kind == kGated) return launch_act<kGated>(a.act, ta, tb, p, st);
+  if (a.kind == kGatedBwd) return launch_act<kGatedBwd>(a.act, ta, tb, p, st);
+  return a.ydt == ZQ_OUT_F32 ? launch_cfg<kPlain, ZQ_ACT_RELU, true>(ta, tb, p, st)
+                             : launch_cfg<kPlain, ZQ_ACT_RELU, false>(ta, tb, p, st);
 }
 
 }  // namespace fp8b
