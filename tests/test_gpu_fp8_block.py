@@ -422,3 +422,40 @@ def test_block_step(M, mode):
         v = host(got[k].float()).astype(np.float64)
         rel = np.linalg.norm(v - r) / np.linalg.norm(r)
         assert rel <= 2.0 ** -9 + 4e-3, (k, rel)
+
+
+def test_example_trains_and_serves():
+    """The example's loop lowers its loss, and its single-token passes agree with the batch to bf16 rounding."""
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "gated_ffn_fp8.py")
+    spec = importlib.util.spec_from_file_location("gated_ffn_fp8_example", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    losses, ffn, x = ex.train(128, 256, 384, 25, log=None)
+    assert losses[-1] < 0.7 * losses[0]
+    whole = ffn.forward(x).float()
+    one = torch.cat([ffn.forward(x[i:i + 1]) for i in range(4)]).float()
+    # the sums differ in order only; a code of h in between can flip by one step (2^-3 of one of 384 terms)
+    assert ((one - whole[:4]).norm() / whole[:4].norm()) < 2.0 ** -8 + 4e-3
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^31 codes and 2^32 bytes of activations: the last rows come out like a call on them alone."""
+    M, K, N = 70_001, 32_768, 16
+    x = torch.randn((1, K), device=dev()).to(torch.bfloat16).expand(M, K).contiguous()
+    x[-3:] = torch.randn((3, K), device=dev()).to(torch.bfloat16)
+    w, _ = weight(1, N, K, "none")
+    q, ql = binding.quantize_fp8_block(x), binding.quantize_fp8_block(x[-3:])
+    assert torch.equal(q.codes[-3:], ql.codes) and torch.equal(q.scale[:, -3:], ql.scale)
+    y = binding.fp8_block_linear(w, q=q)
+    yl = binding.fp8_block_linear(w, q=ql)
+    assert torch.equal(y[0], y[1]) and torch.equal(y[0], y[-4])
+    S = ql.values().abs() @ w.values().abs().t()
+    assert ((y[-3:] - yl).abs() <= 2 * sum_tol(S, K)).all()
+    g = torch.zeros((M, 8), dtype=torch.bfloat16, device=dev())
+    g[-3:] = 1.0
+    dw = binding.fp8_weight_grad(g, q)
+    dl = binding.fp8_weight_grad(g[-3:].contiguous(), ql)
+    assert ((dw - dl).abs() <= 2.0 ** -20 * ql.values().abs().sum(0)).all()
