@@ -12,8 +12,9 @@
 // 16 KB of bf16 into a ring of their own; the gradient's tiles go from the copy engine to the tensor core untouched.
 // Per 64 tokens the MMAs take 512 cycles, the conversion about 180 issue slots of each SM quarter.
 //
-// Two accumulators of 256 columns: the stores of one tile overlap the sums of the next.
-// Warp roles: 0..3 epilogue, 4..19 converters (four groups, each with a stage of its own), 20 producer, 21 tensor memory
+// Two accumulators of 256 columns: bf16 results take them in turn, so that the stores of one tile overlap the sums of the
+// next; FP32 results use the second for running sums (see kFold).
+// Warp roles: 0..7 epilogue, 8..23 converters (four groups, each with a stage of its own), 24 producer, 25 tensor memory
 // and MMAs.
 #include "fp8_block.cuh"
 
@@ -36,7 +37,12 @@ constexpr int kNumBars = 2 * kStages + 2 * kConv + 4 + 1;
 constexpr int kOffMisc = kOffBars + kNumBars * 8;
 constexpr int kSmemBytes = kOffMisc + 16;
 static_assert(kSmemBytes <= 227 * 1024, "shared memory");
-constexpr int kConvWarp0 = 4, kProducerWarp = 20, kMmaWarp = 21, kThreads = 704;
+constexpr int kEpiWarps = 8;
+constexpr int kConvWarp0 = 8, kProducerWarp = 24, kMmaWarp = 25, kThreads = 832;
+// Stages whose products go to one accumulator before it is folded into the running sums (FP32 results only).  The tensor
+// core rounds every addition to its accumulator towards zero: over 16384 tokens that adds up to 8.5e-6 of the result,
+// over 2048 to 6e-7 at most, the size of the rounding errors of an FP32 sum; a fold holds the MMAs up for about 800 cycles.
+constexpr int kFold = 32;
 
 enum { kErrProducerW = 31, kErrMmaW = 32, kErrEpilogueW = 33, kErrAlignW = 34, kErrConvertW = 35 };
 
@@ -117,7 +123,7 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&acc_full[i], 1);
-      mbar_init(&acc_empty[i], 4);
+      mbar_init(&acc_empty[i], kEpiWarps);
     }
     mbar_init(drain_bar, 1);
     *s_abort = 0;
@@ -180,16 +186,22 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
       const uint64_t adesc0 = desc_mn128(smem_u32(smem + kOffC));
       const uint64_t bdesc0 = desc_mn128(smem_u32(smem + kOffG));
       const uint32_t idesc = idesc_bf16_mn(kTileN);
-      int s = 0, c = 0, tile = 0;
+      int s = 0, c = 0, sum = 0;  // sum: accumulations begun
       uint32_t ph = 0, cph = 0;
       bool failed = false;
-      for (int pos = blockIdx.x; !failed && pos < p.tiles; pos += gridDim.x, ++tile) {
-        const int buf = tile & 1;
-        if (tile >= 2 && !mbar_wait(&acc_empty[buf], ((tile >> 1) - 1) & 1, s_abort)) {
-          failed = true;
-          break;
-        }
+      for (int pos = blockIdx.x; !failed && pos < p.tiles; pos += gridDim.x) {
         for (int i = 0; i < p.steps; ++i) {
+          const bool begin = F32 ? i % kFold == 0 : i == 0, end = i + 1 == p.steps || (F32 && (i + 1) % kFold == 0);
+          if (begin) {
+            // FP32: always the first accumulator, the second holds the running sums; bf16: in turn
+            const int uses = F32 ? sum : sum >> 1;  // of this accumulator before
+            if (uses > 0 && !mbar_wait(&acc_empty[F32 ? 0 : sum & 1], (uses - 1) & 1, s_abort)) {
+              failed = true;
+              break;
+            }
+            ++sum;
+          }
+          const int buf = F32 ? 0 : (sum - 1) & 1;
           if (!mbar_wait(&full[s], ph, s_abort) || !mbar_wait(&conv_full[c], cph, s_abort)) {
             failed = true;
             break;
@@ -200,10 +212,10 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
             const uint64_t bd = bdesc0 + static_cast<uint64_t>((s * kGBytes) >> 4);
 #pragma unroll
             for (int k = 0; k < kTok / 16; ++k)  // 16 token rows of 128 bytes further
-              umma_f16(tmem_base + buf * kTileN, ad + k * (2048 >> 4), bd + k * (2048 >> 4), idesc, (i > 0 || k > 0) ? 1u : 0u);
+              umma_f16(tmem_base + buf * kTileN, ad + k * (2048 >> 4), bd + k * (2048 >> 4), idesc, (!begin || k > 0) ? 1u : 0u);
             umma_commit(&empty[s]);
             umma_commit(&conv_empty[c]);
-            if (i + 1 == p.steps) umma_commit(&acc_full[buf]);
+            if (end) umma_commit(&acc_full[buf]);
           }
           __syncwarp();
           if (++s == kStages) {
@@ -253,7 +265,7 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
           failed = true;
           break;
         }
-#pragma unroll
+#pragma unroll 2
         for (int j = 0; j < 4; ++j) {
           const uint4 v = src[(chunk * 4 + j) ^ sw];
           const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -272,28 +284,57 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
       }
     }
   } else {
-    // ---- epilogue: thread = input feature; a column is one output channel, 32 neighbouring features per warp
+    // ---- epilogue: thread = input feature and column half; a column is one output channel, 32 neighbouring features
+    // per warp
     bool failed = !ok_start;
-    const uint32_t lane_base = static_cast<uint32_t>(warp * 32) << 16;
-    int tile = 0;
+    constexpr int kCols = kTileN / 2;
+    const int half = warp >> 2;
+    const uint32_t lane_base = (static_cast<uint32_t>((warp & 3) * 32) << 16) + half * kCols;
+    int sum = 0;
     pdl_wait();
-    for (int pos = blockIdx.x; !failed && pos < p.tiles; pos += gridDim.x, ++tile) {
+    for (int pos = blockIdx.x; !failed && pos < p.tiles; pos += gridDim.x) {
       int part, nt, kt;
       tile_of(p, pos, part, nt, kt);
-      const int buf = tile & 1;
-      if (!mbar_wait_warp(&acc_full[buf], (tile >> 1) & 1, s_abort)) {
-        if (lane == 0) raise_error8(p.status, s_abort, kErrEpilogueW);
-        failed = true;
-        break;
+      const int folds = F32 ? (p.steps + kFold - 1) / kFold : 1;
+      for (int f = 0; f < folds; ++f, ++sum) {
+        const int buf = F32 ? 0 : sum & 1;
+        if (!mbar_wait_all(&acc_full[buf], (F32 ? sum : sum >> 1) & 1, s_abort)) {
+          if (lane == 0) raise_error8(p.status, s_abort, kErrEpilogueW);
+          failed = true;
+          break;
+        }
+        tc_fence_after_sync();
+        if (F32) {
+          // into the running sums (of the same lanes and columns: no other warp touches them), then the MMAs may go on
+          const uint32_t ta = tmem_base + lane_base, tr = ta + kTileN;
+#pragma unroll 1
+          for (int c = 0; c < kCols; c += 16) {
+            float v[16], r[16];
+            tmem_ld16(ta + c, v);
+            if (f > 0) tmem_ld16(tr + c, r);
+            tmem_ld_wait_regs<16>(v);
+            if (f > 0) {
+              tmem_ld_wait_regs<16>(r);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) v[e] += r[e];
+            }
+            tmem_st16(tr + c, reinterpret_cast<const uint32_t*>(v));
+          }
+          tmem_st_wait();
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&acc_empty[0]);
+        }
       }
-      tc_fence_after_sync();
-      const int k = kt * kTileK + warp * 32 + lane;
-      const int n0 = nt * kTileN;
+      if (failed) break;
+      const int k = kt * kTileK + (warp & 3) * 32 + lane;
+      const int n0 = nt * kTileN + half * kCols;
       const int cols = k < p.K ? p.N - n0 : 0;
       const int64_t base = (static_cast<int64_t>(part) * p.N + n0) * p.K + k;
+      const int buf = F32 ? 1 : (sum - 1) & 1;
       const uint32_t ta = tmem_base + buf * kTileN + lane_base;
 #pragma unroll 1
-      for (int c = 0; c < kTileN; c += 16) {
+      for (int c = 0; c < kCols; c += 16) {
         float v[16];
         tmem_ld16(ta + c, v);
         tmem_ld_wait_regs<16>(v);
@@ -307,9 +348,11 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
               static_cast<__nv_bfloat16*>(p.dw)[o] = __float2bfloat16_rn(v[e]);
           }
       }
-      tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&acc_empty[buf]);
+      if (!F32) {
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&acc_empty[buf]);
+      }
     }
   }
 
