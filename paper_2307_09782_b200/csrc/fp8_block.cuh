@@ -113,6 +113,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
 // The activations.  SiLU and the tanh form of GELU are both v * sigmoid(w(v)), with w = v and
 // w = 2 sqrt(2 / pi) (v + 0.044715 v^3), since (1 + tanh z) / 2 = sigmoid(2 z).  1 / (1 + exp(-w)) with the fast
 // exponential and division is good to about 1e-6 relative: 2^-13 of a bf16 rounding step.

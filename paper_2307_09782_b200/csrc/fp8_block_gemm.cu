@@ -378,6 +378,21 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     int count = 0;
     pdl_wait();
     for (int pos = blockIdx.x; pos < tiles; pos += gridDim.x) {
+      if (KIND == kGatedBwd) {
+        // the checkpoint's codes that this tile's epilogue will read: on their way to L2 while the MMAs run
+        int mt, nt;
+        tile_of(p, pos, mt, nt);
+        const int m = mt * kTileM + row, n0 = (2 * nt + half) * kBlk;
+        if (m < p.M && n0 < p.N) {
+          const uint8_t* g = p.ck + static_cast<int64_t>(m) * p.N + n0;
+          const uint8_t* u = g + static_cast<int64_t>(p.M) * p.N;
+          const int last = min(kBlk, p.N - n0) - 1;  // a row's codes can lie in two lines
+          prefetch_l2(g);
+          prefetch_l2(g + last);
+          prefetch_l2(u);
+          prefetch_l2(u + last);
+        }
+      }
       uint64_t run[64];
 #pragma unroll
       for (int e = 0; e < 64; ++e) run[e] = 0ull;
@@ -511,18 +526,28 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         uint32_t ag[8], au[8];
 #pragma unroll
         for (int it = 0; it < 8; ++it) ag[it] = au[it] = 0u;
+        uint32_t gn[8], un[8];  // the next 32 columns' codes
+        auto fetch = [&](int c) {
+#pragma unroll
+          for (int it = 0; it < 8; ++it) {
+            const int r = it * 4 + rr;
+            gn[it] = un[it] = 0u;
+            if (r < rows && 32 * c + 4 * cc < cols) {  // N is a multiple of 16: the four are inside or outside together
+              gn[it] = __ldg(reinterpret_cast<const uint32_t*>(ck + static_cast<int64_t>(r) * p.N + 32 * c));
+              un[it] = __ldg(reinterpret_cast<const uint32_t*>(ck + MN + static_cast<int64_t>(r) * p.N + 32 * c));
+            }
+          }
+        };
+        fetch(0);
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           uint32_t gc[8], uc[8];
 #pragma unroll
           for (int it = 0; it < 8; ++it) {
-            const int r = it * 4 + rr;
-            gc[it] = uc[it] = 0u;
-            if (r < rows && 32 * c + 4 * cc < cols) {  // N is a multiple of 16: the four are inside or outside together
-              gc[it] = __ldg(reinterpret_cast<const uint32_t*>(ck + static_cast<int64_t>(r) * p.N + 32 * c));
-              uc[it] = __ldg(reinterpret_cast<const uint32_t*>(ck + MN + static_cast<int64_t>(r) * p.N + 32 * c));
-            }
+            gc[it] = gn[it];
+            uc[it] = un[it];
           }
+          if (c < 3) fetch(c + 1);
           __syncwarp();
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
