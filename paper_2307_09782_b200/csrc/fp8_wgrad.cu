@@ -265,7 +265,7 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
           failed = true;
           break;
         }
-#pragma unroll 2
+#pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint4 v = src[(chunk * 4 + j) ^ sw];
           const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -334,12 +334,12 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
       const int buf = F32 ? 1 : (sum - 1) & 1;
       const uint32_t ta = tmem_base + buf * kTileN + lane_base;
 #pragma unroll 1
-      for (int c = 0; c < kCols; c += 16) {
-        float v[16];
-        tmem_ld16(ta + c, v);
-        tmem_ld_wait_regs<16>(v);
+      for (int c = 0; c < kCols; c += 8) {
+        float v[8];
+        tmem_ld8(ta + c, v);
+        tmem_ld_wait_regs<8>(v);
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
+        for (int e = 0; e < 8; ++e)
           if (c + e < cols) {
             const int64_t o = base + static_cast<int64_t>(c + e) * p.K;
             if (F32)
