@@ -49,20 +49,30 @@ enum { kErrProducerW = 31, kErrMmaW = 32, kErrEpilogueW = 33, kErrAlignW = 34, k
 struct PW {
   int M, N, K;
   int steps;  // stages per tile
-  int k_tiles, n_tiles, tiles, n_group;
+  int k_tiles, n_tiles, n_group;
+  int whole, tiles;  // tiles 128 x 256, and with the halves (128 x 128) of the others
   const float* s;
   void* dw;
   int* status;
 };
 
-__device__ __forceinline__ void tile_of(const PW& p, int pos, int& part, int& nt, int& kt) {
+// Position of the launch order -> part, block of features, first output, and whether the tile has 256 outputs or 128.
+// (The tiles of the last, incomplete round are cut in halves where those fit one round: 512 tiles on 148 SMs are three
+// rounds and 136 halves instead of four rounds.)
+__device__ __forceinline__ void tile_of(const PW& p, int pos, int& part, int& kt, int& n0, bool& wide) {
+  int cut = 0;
+  wide = pos < p.whole;
+  if (!wide) {
+    cut = (pos - p.whole) & 1;
+    pos = p.whole + ((pos - p.whole) >> 1);
+  }
   const int per_part = p.n_tiles * p.k_tiles;
   part = pos / per_part;
   pos -= part * per_part;
   const int per_group = p.n_group * p.k_tiles;
   const int g = pos / per_group, within = pos - g * per_group;
   const int gn = min(p.n_group, p.n_tiles - g * p.n_group);
-  nt = g * p.n_group + within % gn;
+  n0 = (g * p.n_group + within % gn) * kTileN + cut * (kTileN / 2);
   kt = within / gn;
 }
 
@@ -150,8 +160,9 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
       uint32_t ph = 0;
       bool ok = true;
       for (int pos = blockIdx.x; ok && pos < p.tiles; pos += gridDim.x) {
-        int part, nt, kt;
-        tile_of(p, pos, part, nt, kt);
+        int part, kt, n0;
+        bool wide;
+        tile_of(p, pos, part, kt, n0, wide);
         for (int i = 0; i < p.steps; ++i) {
           if (issued >= kStages && !mbar_wait(&empty[s], ph ^ 1, s_abort)) {
             if (issuer) raise_error8(p.status, s_abort, kErrProducerW);
@@ -159,11 +170,11 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
             break;
           }
           if (issuer) {
-            mbar_arrive_expect_tx(&full[s], kGBytes + kXBytes);
+            mbar_arrive_expect_tx(&full[s], (wide ? kGBytes : kGBytes / 2) + kXBytes);
             tma_load_3d(smem + kOffX + s * kXBytes, &tm_x, kt * kTileK, i * kTok, 0, &full[s]);
 #pragma unroll
             for (int c = 0; c < 4; ++c)
-              tma_load_3d(smem + kOffG + s * kGBytes + c * kChunk, &tm_g, nt * kTileN + c * 64, i * kTok, part, &full[s]);
+              if (c < 2 || wide) tma_load_3d(smem + kOffG + s * kGBytes + c * kChunk, &tm_g, n0 + c * 64, i * kTok, part, &full[s]);
           }
           __syncwarp();
           ++issued;
@@ -185,11 +196,11 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
       const bool issuer = elect_one();
       const uint64_t adesc0 = desc_mn128(smem_u32(smem + kOffC));
       const uint64_t bdesc0 = desc_mn128(smem_u32(smem + kOffG));
-      const uint32_t idesc = idesc_bf16_mn(kTileN);
       int s = 0, c = 0, sum = 0;  // sum: accumulations begun
       uint32_t ph = 0, cph = 0;
       bool failed = false;
       for (int pos = blockIdx.x; !failed && pos < p.tiles; pos += gridDim.x) {
+        const uint32_t idesc = idesc_bf16_mn(pos < p.whole ? kTileN : kTileN / 2);
         for (int i = 0; i < p.steps; ++i) {
           const bool begin = F32 ? i % kFold == 0 : i == 0, end = i + 1 == p.steps || (F32 && (i + 1) % kFold == 0);
           if (begin) {
@@ -249,8 +260,9 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
     int n0 = 0;  // stages before this tile
     pdl_wait();
     for (int pos = blockIdx.x; !failed && pos < p.tiles; pos += gridDim.x, n0 += p.steps) {
-      int part, nt, kt;
-      tile_of(p, pos, part, nt, kt);
+      int part, kt, n_unused;
+      bool wide;
+      tile_of(p, pos, part, kt, n_unused, wide);
       const float* sc = p.s + static_cast<int64_t>(kt) * p.M;
       int i = (g - n0) & 3;  // this group's first stage of the tile
       int m_next = i * kTok + row;
@@ -293,8 +305,10 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
     int sum = 0;
     pdl_wait();
     for (int pos = blockIdx.x; !failed && pos < p.tiles; pos += gridDim.x) {
-      int part, nt, kt;
-      tile_of(p, pos, part, nt, kt);
+      int part, kt, n0;
+      bool wide;
+      tile_of(p, pos, part, kt, n0, wide);
+      const bool mine = wide || half == 0;  // a tile of 128 outputs has the first half's columns only
       const int folds = F32 ? (p.steps + kFold - 1) / kFold : 1;
       for (int f = 0; f < folds; ++f, ++sum) {
         const int buf = F32 ? 0 : sum & 1;
@@ -308,7 +322,7 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
           // into the running sums (of the same lanes and columns: no other warp touches them), then the MMAs may go on
           const uint32_t ta = tmem_base + lane_base, tr = ta + kTileN;
 #pragma unroll 1
-          for (int c = 0; c < kCols; c += 16) {
+          for (int c = 0; mine && c < kCols; c += 16) {
             float v[16], r[16];
             tmem_ld16(ta + c, v);
             if (f > 0) tmem_ld16(tr + c, r);
@@ -328,13 +342,13 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
       }
       if (failed) break;
       const int k = kt * kTileK + (warp & 3) * 32 + lane;
-      const int n0 = nt * kTileN + half * kCols;
+      n0 += half * kCols;
       const int cols = k < p.K ? p.N - n0 : 0;
       const int64_t base = (static_cast<int64_t>(part) * p.N + n0) * p.K + k;
       const int buf = F32 ? 1 : (sum - 1) & 1;
       const uint32_t ta = tmem_base + buf * kTileN + lane_base;
 #pragma unroll 1
-      for (int c = 0; c < kCols; c += 8) {
+      for (int c = 0; mine && c < kCols; c += 8) {
         float v[8];
         tmem_ld8(ta + c, v);
         tmem_ld_wait_regs<8>(v);
@@ -404,7 +418,9 @@ int launch_wgrad(const WgradArgs& a, cudaStream_t st) {
   p.n_group = 8;
   const int64_t tiles = static_cast<int64_t>(p.k_tiles) * p.n_tiles * a.parts;
   if (tiles > 0x3FFFFFFF) return ZQ_ERR_SHAPE;
-  p.tiles = static_cast<int>(tiles);
+  const int sms = sm_count(), tail = static_cast<int>(tiles % sms);
+  p.whole = static_cast<int>(2 * tail <= sms ? tiles - tail : tiles);
+  p.tiles = static_cast<int>(p.whole + 2 * (tiles - p.whole));
   p.s = a.s;
   p.dw = a.dw;
   p.status = a.status;
@@ -412,7 +428,7 @@ int launch_wgrad(const WgradArgs& a, cudaStream_t st) {
   if (!make_grad_map(&tg, a) ||
       !make_code_map(&tx, a.q, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.M), 1, kTok))
     return ZQ_ERR_CUDA;
-  const unsigned grid = static_cast<unsigned>(tiles < sm_count() ? tiles : sm_count());
+  const unsigned grid = static_cast<unsigned>(p.tiles < sms ? p.tiles : sms);
   return a.dwdt == ZQ_OUT_F32 ? launch_cfg<true>(tg, tx, p, grid, st) : launch_cfg<false>(tg, tx, p, grid, st);
 }
 
