@@ -478,8 +478,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       }
     }
   }
-  // nobody leaves while a peer reads its sums (nothing is published here: a relaxed arrival)
-  asm volatile("barrier.cluster.arrive.relaxed;\n\tbarrier.cluster.wait;" ::: "memory");
+  cluster_leave();  // nobody leaves while a peer reads its sums
 }
 
 template <int BM, bool GATED, bool RAW>
@@ -492,21 +491,9 @@ int launch_cfg(const CUtensorMap& tw, const CUtensorMap& tq, const PF& p, int m_
                                     C::kSmemBytes);
   });
   if (attr_err != cudaSuccess) return ZQ_ERR_CUDA;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(p.n_tiles * p.cluster), static_cast<unsigned>(m_tiles));
-  cfg.blockDim = dim3(C::kThreads);
-  cfg.dynamicSmemBytes = C::kSmemBytes;
-  cfg.stream = st;
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = static_cast<unsigned>(p.cluster);
-  at[1].val.clusterDim.y = 1;
-  at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 2;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, fp8_block_few_kernel<BM, GATED, RAW>, tw, tq, p);
+  const cudaError_t e = launch_clustered(fp8_block_few_kernel<BM, GATED, RAW>,
+                                         dim3(static_cast<unsigned>(p.n_tiles * p.cluster), static_cast<unsigned>(m_tiles)),
+                                         dim3(C::kThreads), C::kSmemBytes, st, p.cluster, tw, tq, p);
   count_launch();
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
 }

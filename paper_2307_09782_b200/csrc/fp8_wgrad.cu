@@ -12,6 +12,8 @@
 // 16 KB of bf16 into a ring of their own; the gradient's tiles go from the copy engine to the tensor core untouched.
 // Per 64 tokens the MMAs take 512 cycles, the conversion about 180 issue slots of each SM quarter.
 //
+// With few tiles and many tokens a cluster of up to 8 CTAs shares a tile's tokens; its partial sums meet through
+// distributed shared memory.
 // Two accumulators of 256 columns: bf16 results take them in turn, so that the stores of one tile overlap the sums of the
 // next; FP32 results use the second for running sums (see kFold).
 // Warp roles: 0..7 epilogue, 8..23 converters (four groups, each with a stage of its own), 24 producer, 25 tensor memory
@@ -48,7 +50,8 @@ enum { kErrProducerW = 31, kErrMmaW = 32, kErrEpilogueW = 33, kErrAlignW = 34, k
 
 struct PW {
   int M, N, K;
-  int steps;  // stages per tile
+  int steps;    // stages (of 64 tokens) per tile
+  int cluster;  // CTAs that share a tile's tokens
   int k_tiles, n_tiles, n_group;
   int whole, tiles;  // tiles 128 x 256, and with the halves (128 x 128) of the others
   const float* s;
@@ -151,6 +154,11 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
   const uint32_t tmem_base = *s_tmem;
   const bool ok_start = *s_abort == 0;
   if (threadIdx.x == 0) pdl_launch_dependents();
+  // this CTA's tiles: pos0, + stride, ...; of each the stages step0 .. step0 + steps - 1
+  const int rank = static_cast<int>(blockIdx.x) % p.cluster;
+  const int pos0 = static_cast<int>(blockIdx.x) / p.cluster, stride = static_cast<int>(gridDim.x) / p.cluster;
+  const int step0 = static_cast<int>(static_cast<int64_t>(p.steps) * rank / p.cluster);
+  const int steps = static_cast<int>(static_cast<int64_t>(p.steps) * (rank + 1) / p.cluster) - step0;
 
   if (warp == kProducerWarp) {
     if (ok_start) {
@@ -159,11 +167,11 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
       int s = 0, issued = 0;
       uint32_t ph = 0;
       bool ok = true;
-      for (int pos = blockIdx.x; ok && pos < p.tiles; pos += gridDim.x) {
+      for (int pos = pos0; ok && pos < p.tiles; pos += stride) {
         int part, kt, n0;
         bool wide;
         tile_of(p, pos, part, kt, n0, wide);
-        for (int i = 0; i < p.steps; ++i) {
+        for (int i = 0; i < steps; ++i) {
           if (issued >= kStages && !mbar_wait(&empty[s], ph ^ 1, s_abort)) {
             if (issuer) raise_error8(p.status, s_abort, kErrProducerW);
             ok = false;
@@ -171,10 +179,10 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
           }
           if (issuer) {
             mbar_arrive_expect_tx(&full[s], (wide ? kGBytes : kGBytes / 2) + kXBytes);
-            tma_load_3d(smem + kOffX + s * kXBytes, &tm_x, kt * kTileK, i * kTok, 0, &full[s]);
+            tma_load_3d(smem + kOffX + s * kXBytes, &tm_x, kt * kTileK, (step0 + i) * kTok, 0, &full[s]);
 #pragma unroll
             for (int c = 0; c < 4; ++c)
-              if (c < 2 || wide) tma_load_3d(smem + kOffG + s * kGBytes + c * kChunk, &tm_g, n0 + c * 64, i * kTok, part, &full[s]);
+              if (c < 2 || wide) tma_load_3d(smem + kOffG + s * kGBytes + c * kChunk, &tm_g, n0 + c * 64, (step0 + i) * kTok, part, &full[s]);
           }
           __syncwarp();
           ++issued;
@@ -199,10 +207,10 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
       int s = 0, c = 0, sum = 0;  // sum: accumulations begun
       uint32_t ph = 0, cph = 0;
       bool failed = false;
-      for (int pos = blockIdx.x; !failed && pos < p.tiles; pos += gridDim.x) {
+      for (int pos = pos0; !failed && pos < p.tiles; pos += stride) {
         const uint32_t idesc = idesc_bf16_mn(pos < p.whole ? kTileN : kTileN / 2);
-        for (int i = 0; i < p.steps; ++i) {
-          const bool begin = F32 ? i % kFold == 0 : i == 0, end = i + 1 == p.steps || (F32 && (i + 1) % kFold == 0);
+        for (int i = 0; i < steps; ++i) {
+          const bool begin = F32 ? i % kFold == 0 : i == 0, end = i + 1 == steps || (F32 && (i + 1) % kFold == 0);
           if (begin) {
             // FP32: always the first accumulator, the second holds the running sums; bf16: in turn
             const int uses = F32 ? sum : sum >> 1;  // of this accumulator before
@@ -259,15 +267,15 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
     bool failed = !ok_start;
     int n0 = 0;  // stages before this tile
     pdl_wait();
-    for (int pos = blockIdx.x; !failed && pos < p.tiles; pos += gridDim.x, n0 += p.steps) {
+    for (int pos = pos0; !failed && pos < p.tiles; pos += stride, n0 += steps) {
       int part, kt, n_unused;
       bool wide;
       tile_of(p, pos, part, kt, n_unused, wide);
       const float* sc = p.s + static_cast<int64_t>(kt) * p.M;
       int i = (g - n0) & 3;  // this group's first stage of the tile
-      int m_next = i * kTok + row;
-      float s_next = i < p.steps && m_next < p.M ? __ldg(sc + m_next) : 0.0f;
-      for (; i < p.steps; i += 4) {
+      int m_next = (step0 + i) * kTok + row;
+      float s_next = i < steps && m_next < p.M ? __ldg(sc + m_next) : 0.0f;
+      for (; i < steps; i += 4) {
         const float scale = s_next;
         m_next += 4 * kTok;
         s_next = m_next < p.M ? __ldg(sc + m_next) : 0.0f;
@@ -304,12 +312,12 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
     const uint32_t lane_base = (static_cast<uint32_t>((warp & 3) * 32) << 16) + half * kCols;
     int sum = 0;
     pdl_wait();
-    for (int pos = blockIdx.x; !failed && pos < p.tiles; pos += gridDim.x) {
+    for (int pos = pos0; !failed && pos < p.tiles; pos += stride) {
       int part, kt, n0;
       bool wide;
       tile_of(p, pos, part, kt, n0, wide);
       const bool mine = wide || half == 0;  // a tile of 128 outputs has the first half's columns only
-      const int folds = F32 ? (p.steps + kFold - 1) / kFold : 1;
+      const int folds = F32 ? (steps + kFold - 1) / kFold : 1;
       for (int f = 0; f < folds; ++f, ++sum) {
         const int buf = F32 ? 0 : sum & 1;
         if (!mbar_wait_all(&acc_full[buf], (F32 ? sum : sum >> 1) & 1, s_abort)) {
@@ -347,6 +355,20 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
       const int64_t base = (static_cast<int64_t>(part) * p.N + n0) * p.K + k;
       const int buf = F32 ? 1 : (sum - 1) & 1;
       const uint32_t ta = tmem_base + buf * kTileN + lane_base;
+      if (p.cluster > 1) {
+        // partial sums of the cluster's CTAs (128 outputs x 128 features, in the stages' memory, which is done with): they
+        // meet below
+        float* red = reinterpret_cast<float*>(smem) + (warp & 3) * 32 + lane;
+#pragma unroll 1
+        for (int c = 0; mine && c < kCols; c += 8) {
+          float v[8];
+          tmem_ld8(ta + c, v);
+          tmem_ld_wait_regs<8>(v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) red[(c + e) * kTileK] = v[e];
+        }
+        break;  // a cluster has one tile
+      }
 #pragma unroll 1
       for (int c = 0; mine && c < kCols; c += 8) {
         float v[8];
@@ -376,6 +398,31 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
     tc_fence_after_sync();
     tmem_dealloc(tmem_base, 512);
   }
+  if (p.cluster > 1) {
+    // rank r adds up outputs r * per .. of the tile, in rank order (the same result every time), and stores them
+    cluster_sync_all();
+    int part, kt, n0;
+    bool wide;
+    tile_of(p, pos0, part, kt, n0, wide);
+    const int per = (kTileN / 2) / p.cluster;
+    const int f = threadIdx.x & (kTileK - 1), k = kt * kTileK + f;
+    if (*s_abort == 0 && k < p.K && threadIdx.x < 6 * kTileK) {
+      for (int c = rank * per + static_cast<int>(threadIdx.x >> 7); c < (rank + 1) * per && n0 + c < p.N; c += 6) {
+        const uint32_t at = smem_u32(smem) + (c * kTileK + f) * 4;
+        float v[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] = r < p.cluster ? ld_cluster(map_to_rank(at, r)) : 0.0f;
+#pragma unroll
+        for (int r = 1; r < 8; ++r) v[0] += v[r];
+        const int64_t o = (static_cast<int64_t>(part) * p.N + n0 + c) * p.K + k;
+        if (F32)
+          static_cast<float*>(p.dw)[o] = v[0];
+        else
+          static_cast<__nv_bfloat16*>(p.dw)[o] = __float2bfloat16_rn(v[0]);
+      }
+    }
+    cluster_leave();  // nobody leaves while a peer reads its sums
+  }
 }
 
 // G as a 3-D tensor [parts][M][N] of bf16, boxes of 64 elements x 64 tokens.
@@ -400,7 +447,7 @@ int launch_cfg(const CUtensorMap& tg, const CUtensorMap& tx, const PW& p, unsign
     attr = cudaFuncSetAttribute(fp8_wgrad_kernel<F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   });
   if (attr != cudaSuccess) return ZQ_ERR_CUDA;
-  const cudaError_t e = launch_chained(fp8_wgrad_kernel<F32>, dim3(grid), dim3(kThreads), kSmemBytes, st, false, tg, tx, p);
+  const cudaError_t e = launch_clustered(fp8_wgrad_kernel<F32>, dim3(grid), dim3(kThreads), kSmemBytes, st, p.cluster, tg, tx, p);
   count_launch();
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
 }
@@ -421,6 +468,9 @@ int launch_wgrad(const WgradArgs& a, cudaStream_t st) {
   const int sms = sm_count(), tail = static_cast<int>(tiles % sms);
   p.whole = static_cast<int>(2 * tail <= sms ? tiles - tail : tiles);
   p.tiles = static_cast<int>(p.whole + 2 * (tiles - p.whole));
+  // few tiles and many tokens: a cluster shares a tile's tokens, at least 512 of them each
+  p.cluster = 1;
+  while (p.cluster < 8 && p.whole == 0 && p.tiles * p.cluster * 2 <= sms && p.steps >= p.cluster * 16) p.cluster *= 2;
   p.s = a.s;
   p.dw = a.dw;
   p.status = a.status;
@@ -428,7 +478,7 @@ int launch_wgrad(const WgradArgs& a, cudaStream_t st) {
   if (!make_grad_map(&tg, a) ||
       !make_code_map(&tx, a.q, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.M), 1, kTok))
     return ZQ_ERR_CUDA;
-  const unsigned grid = static_cast<unsigned>(p.tiles < sms ? p.tiles : sms);
+  const unsigned grid = static_cast<unsigned>(p.tiles * p.cluster < sms ? p.tiles * p.cluster : sms);
   return a.dwdt == ZQ_OUT_F32 ? launch_cfg<true>(tg, tx, p, grid, st) : launch_cfg<false>(tg, tx, p, grid, st);
 }
 
