@@ -320,7 +320,7 @@ def test_backward_against_differences(kind):
 # ---- weight gradient -------------------------------------------------------------------------------------------------
 WGRAD = [(1, 16, 1, 1), (3, 128, 128, 1), (64, 144, 100, 1), (65, 272, 257, 1), (333, 768, 144, 1), (200, 400, 130, 2),
          (1000, 256, 512, 1), (129, 528, 8, 3),
-         (2100, 144, 40, 1), (4500, 272, 300, 1), (8200, 128, 130, 1)]  # few tiles, many tokens: clusters of 2, 4, 8
+         (2100, 144, 40, 1), (4500, 272, 300, 1), (8200, 128, 130, 1), (2100, 1552, 1500, 1)]  # few tiles, many tokens: clusters of 2, 4, 8
 
 
 @pytest.mark.parametrize("M,K,N,parts", WGRAD)
