@@ -414,8 +414,8 @@ def quantize_fp8_block(x: torch.Tensor, mode="none") -> Fp8Block:
     """x: bf16 [M, K] (row stride allowed); ``mode`` "none" (FP32 scales) or "M1" (powers of two)."""
     ldx = _rows(x, "x")
     M, K = x.shape
-    q = torch.empty((M, K), dtype=torch.uint8, device=x.device)
-    s = torch.empty((_blocks(K), M), dtype=torch.float32, device=x.device)
+    q = x.new_empty((M, K), dtype=torch.uint8)
+    s = x.new_empty(((K + 127) // 128, M), dtype=torch.float32)
     _check(lib().zq_quantize_fp8_block(_ptr(x), M, K, ldx, _mode(mode), _ptr(q), _ptr(s), _stream()),
            "zq_quantize_fp8_block")
     return Fp8Block(q, s)
@@ -475,11 +475,11 @@ def _fp8_workspace(workspace, M: int, K: int, device):
     """The caller's workspace, or one that is kept per device and stream and grown on demand."""
     if workspace is not None:
         return workspace
-    key = (device, _stream())
-    need = lib().zq_fp8_block_workspace_bytes(M, K)
-    ws = _fp8_workspaces.get(key)
-    if ws is None or ws.numel() < need:
-        ws = _fp8_workspaces[key] = make_workspace(need, device)
+    key = (device.index, _stream())
+    ws, most = _fp8_workspaces.get(key, (None, -1))
+    if most < M * (K + 128):  # codes, scales and some slack: a bound that needs no call
+        ws, most = make_workspace(lib().zq_fp8_block_workspace_bytes(M, K), device), M * (K + 128)
+        _fp8_workspaces[key] = ws, most
     return ws
 
 
@@ -489,11 +489,12 @@ def fp8_block_linear(w: Fp8Weight, *, x=None, q: Optional[Fp8Block] = None, mode
     ``w.parts`` = 2 the sum over two pairs of operands (``q`` then holds two as well)."""
     codes, scale, x, ldx, M = _activations(x, q, w.K, w.parts)
     if y is None:
-        y = torch.empty((M, w.N), dtype=out_dtype, device=w.codes.device)
+        y = w.scale.new_empty((M, w.N), dtype=out_dtype)
     elif y.shape != (M, w.N) or y.dtype not in (torch.float32, torch.bfloat16) or (w.N > 1 and y.stride(1) != 1):
         raise ValueError(f"y: a float32 or bf16 [{M}, {w.N}] matrix with contiguous rows is needed")
     ydt = OUT_F32 if y.dtype == torch.float32 else OUT_BF16
-    workspace = _fp8_workspace(workspace, M, w.K, w.codes.device)
+    if workspace is None:
+        workspace = _fp8_workspace(None, M, w.K, w.codes.device)
     _check(lib().zq_fp8_block_linear(_ptr(codes), _ptr(scale), _ptr(x), ldx, _mode(mode), w.parts, M, w.N, w.K,
                                      _ptr(w.codes), _ptr(w.scale), _ptr(y), ydt, y.stride(0) if M > 1 else w.N,
                                      _ptr(workspace), workspace.numel(), _stream()), "zq_fp8_block_linear")
@@ -558,12 +559,13 @@ def fp8_weight_grad(g: torch.Tensor, q: Fp8Block, *, out_dtype=torch.float32,
     g0 = g[0] if g.dim() == 3 else g
     ldg = _rows(g0, "g")
     M, N = g0.shape
-    codes, scale, _, _, Mq = _activations(None, q, q.codes.shape[-1], 1)
+    K = q.codes.shape[-1]
+    codes, scale, _, _, Mq = _activations(None, q, K, 1)
     if Mq != M:
         raise ValueError(f"g has {M} rows, the checkpoint {Mq}")
-    K = codes.shape[-1]
-    dw = torch.empty((parts, N, K) if g.dim() == 3 else (N, K), dtype=out_dtype, device=g.device)
-    workspace = _fp8_workspace(workspace, 0, 16, g.device)
+    dw = g.new_empty((parts, N, K) if g.dim() == 3 else (N, K), dtype=out_dtype)
+    if workspace is None:
+        workspace = _fp8_workspace(None, 0, 16, g.device)
     _check(lib().zq_fp8_weight_grad(_ptr(g), ldg, g.stride(0) if g.dim() == 3 else 0, parts, _ptr(codes), _ptr(scale),
                                     M, N, K, _ptr(dw), OUT_F32 if out_dtype == torch.float32 else OUT_BF16,
                                     _ptr(workspace), workspace.numel(), _stream()), "zq_fp8_weight_grad")
