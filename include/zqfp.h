@@ -370,7 +370,9 @@ size_t zq_fp8_block_workspace_bytes(int64_t M, int64_t K);
  * parts : 1, or 2 for a sum over two pairs of operands (the input gradient of two projections of the same input)
  * q, s  : activations [parts][M, K] and their scales [parts][ceil(K/128), M]; or x_bf16 [M, ldx] (parts == 1,
  *         q = s = NULL), which the call quantizes with `mode`
- * w, ws : weights [parts][N, K] and scales [parts][ceil(N/128), ceil(K/128)]
+ * w, ws : weights [parts][N, K] and scales [parts][ceil(N/128), ceil(K/128)].  The kernel may copy its first weight tiles
+ *         while the kernel ahead of it in the stream still runs (as for the W4A8 layer): weights are the layer's
+ *         own data, written by the two entry points above or by kernels launched in the ordinary way
  * y     : out [M, ldy], FP32 or bf16 (ydt), element-aligned, ldy >= N; any N
  * The products of a block are summed by the tensor core, scaled and summed over the blocks in FP32; results do not
  * vary from run to run.  M == 0 or N == 0 is a no-op.
@@ -416,7 +418,8 @@ int zq_fp8_gated_linear_backward(const uint8_t* q, const float* s, const void* d
 /*
  * Weight gradient from an 8-bit activation checkpoint:  dW[p][n, k] = sum_m G[p][m, n] bf16(code[m, k] s[k/128, m])
  * (the rounding to bf16 is none with power-of-two scales), summed in FP32.
- * G    : bf16, parts (1 .. 64) matrices [M, ldg], g_stride elements apart; ldg >= N; ldg and g_stride multiples of 8
+ * G    : bf16, parts (1 .. 64) matrices [M, ldg], g_stride elements apart (not 0 with several); ldg >= N; ldg and
+ *        g_stride multiples of 8
  * q, s : the checkpoint, [M, K] and [ceil(K/128), M]
  * dw   : out, [parts][N, K] dense, FP32 or bf16, 16-byte aligned; any N.  M == 0 gives zeros.
  */

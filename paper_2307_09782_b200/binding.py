@@ -392,6 +392,13 @@ def _expect(t: torch.Tensor, dtype, name: str):
         raise ValueError(f"{name}: a contiguous {dtype} tensor is needed, got {t.dtype}, strides {t.stride()}")
 
 
+def _on_gpu(*tensors: torch.Tensor):
+    """The library takes device pointers: a tensor in host memory must not get that far."""
+    for t in tensors:
+        if not t.is_cuda:
+            raise ValueError(f"a CUDA tensor is needed, got one of {tuple(t.shape)} on {t.device}")
+
+
 def _rows(x: torch.Tensor, name: str) -> int:
     """The row stride of a bf16 matrix whose rows are contiguous."""
     if x.dtype != torch.bfloat16 or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
@@ -413,6 +420,7 @@ def _blocks(n: int) -> int:
 def quantize_fp8_block(x: torch.Tensor, mode="none") -> Fp8Block:
     """x: bf16 [M, K] (row stride allowed); ``mode`` "none" (FP32 scales) or "M1" (powers of two)."""
     ldx = _rows(x, "x")
+    _on_gpu(x)
     M, K = x.shape
     q = x.new_empty((M, K), dtype=torch.uint8)
     s = x.new_empty(((K + 127) // 128, M), dtype=torch.float32)
@@ -424,6 +432,7 @@ def quantize_fp8_block(x: torch.Tensor, mode="none") -> Fp8Block:
 def quantize_weight_fp8_block(W: torch.Tensor, mode="none") -> Fp8Weight:
     """W: float32 [N, K] or [parts, N, K], contiguous."""
     _expect(W, torch.float32, "W")
+    _on_gpu(W)
     parts = W.shape[0] if W.dim() == 3 else 1
     N, K = W.shape[-2:]
     lead = W.shape[:-2] if parts > 1 else ()
@@ -438,6 +447,7 @@ def quantize_weight_fp8_block(W: torch.Tensor, mode="none") -> Fp8Weight:
 
 def transpose_fp8_weight(w: Fp8Weight) -> Fp8Weight:
     """The transposed weight (of each part): [N, K] -> [K, N]."""
+    _on_gpu(w.codes, w.scale)
     lead = (w.parts,) if w.parts > 1 else ()
     nb, kb = _blocks(w.N), _blocks(w.K)
     q = torch.empty((*lead, w.K, w.N), dtype=torch.uint8, device=w.codes.device)
@@ -458,6 +468,7 @@ def _activations(x, q, K: int, parts: int):
         ldx = _rows(x, "x")
         if x.shape[1] != K:
             raise ValueError(f"x has {x.shape[1]} features, the weight {K}")
+        _on_gpu(x)
         return None, None, x, ldx, x.shape[0]
     _expect(q.codes, torch.uint8, "q.codes")
     _expect(q.scale, torch.float32, "q.scale")
@@ -465,6 +476,7 @@ def _activations(x, q, K: int, parts: int):
     lead = (parts,) if parts > 1 else ()
     if tuple(q.codes.shape) != (*lead, M, K) or tuple(q.scale.shape) != (*lead, _blocks(K), M):
         raise ValueError(f"codes {tuple(q.codes.shape)} / scales {tuple(q.scale.shape)} do not fit {parts} x [M, {K}]")
+    _on_gpu(q.codes, q.scale)
     return q.codes, q.scale, None, K, M
 
 
@@ -488,6 +500,7 @@ def fp8_block_linear(w: Fp8Weight, *, x=None, q: Optional[Fp8Block] = None, mode
     """y [M, N] = the linear layer; activations raw (bf16 ``x``, quantized with ``mode``) or quantized (``q``).  With
     ``w.parts`` = 2 the sum over two pairs of operands (``q`` then holds two as well)."""
     codes, scale, x, ldx, M = _activations(x, q, w.K, w.parts)
+    _on_gpu(w.codes, w.scale)
     if y is None:
         y = w.scale.new_empty((M, w.N), dtype=out_dtype)
     elif y.shape != (M, w.N) or y.dtype not in (torch.float32, torch.bfloat16) or (w.N > 1 and y.stride(1) != 1):
@@ -495,6 +508,7 @@ def fp8_block_linear(w: Fp8Weight, *, x=None, q: Optional[Fp8Block] = None, mode
     ydt = OUT_F32 if y.dtype == torch.float32 else OUT_BF16
     if workspace is None:
         workspace = _fp8_workspace(None, M, w.K, w.codes.device)
+    _on_gpu(y, workspace)
     _check(lib().zq_fp8_block_linear(_ptr(codes), _ptr(scale), _ptr(x), ldx, _mode(mode), w.parts, M, w.N, w.K,
                                      _ptr(w.codes), _ptr(w.scale), _ptr(y), ydt, y.stride(0) if M > 1 else w.N,
                                      _ptr(workspace), workspace.numel(), _stream()), "zq_fp8_block_linear")
@@ -512,6 +526,7 @@ def fp8_gated_linear(w: Fp8Weight, *, x=None, q: Optional[Fp8Block] = None, act=
     if w.parts != 2:
         raise ValueError("the gated layer takes the stacked (gate, up) weights: parts = 2")
     codes, scale, x, ldx, M = _activations(x, q, w.K, 1)
+    _on_gpu(w.codes, w.scale)
     F, dev, fb = w.N, w.codes.device, _blocks(w.N)
     h = torch.empty((M, F), dtype=torch.bfloat16, device=dev) if bf16 else None
     hq = gu = None
@@ -533,7 +548,10 @@ def fp8_gated_linear_backward(wt: Fp8Weight, gu: Fp8Block, *, dy=None, q: Option
                               mode="none", workspace: Optional[torch.Tensor] = None):
     """Gradients of g and u from the gradient of the block's output (bf16 ``dy`` or quantized ``q``), the transposed down
     projection ``wt`` and the checkpoint ``gu``.  Returns (bf16 [2, M, F], the same quantized)."""
+    if wt.parts != 1:
+        raise ValueError("the backward pass takes one transposed down projection: parts = 1")
     codes, scale, dy, lddy, M = _activations(dy, q, wt.K, 1)
+    _on_gpu(wt.codes, wt.scale, gu.codes, gu.scale)
     F, dev, fb = wt.N, wt.codes.device, _blocks(wt.N)
     if tuple(gu.codes.shape) != (2, M, F) or tuple(gu.scale.shape) != (2, fb, M):
         raise ValueError(f"the checkpoint {tuple(gu.codes.shape)} does not fit [2, {M}, {F}]")
@@ -558,6 +576,7 @@ def fp8_weight_grad(g: torch.Tensor, q: Fp8Block, *, out_dtype=torch.float32,
     parts = g.shape[0] if g.dim() == 3 else 1
     g0 = g[0] if g.dim() == 3 else g
     ldg = _rows(g0, "g")
+    _on_gpu(g)
     M, N = g0.shape
     K = q.codes.shape[-1]
     codes, scale, _, _, Mq = _activations(None, q, K, 1)
@@ -590,6 +609,7 @@ def fp8_gated_ffn(gate_up: Fp8Weight, down: Fp8Weight, x: torch.Tensor, *, act="
     if gate_up.parts != 2 or down.parts != 1 or gate_up.K != K or down.K != F:
         raise ValueError(f"x [{M}, {K}], gate_up {gate_up.parts} x [{F}, {gate_up.K}] and down [{N}, {down.K}] do not belong "
                          "together")
+    _on_gpu(x, gate_up.codes, gate_up.scale, down.codes, down.scale)
     y = torch.empty((M, N), dtype=out_dtype, device=x.device)
     saved = torch.empty((fp8_gated_ffn_saved_bytes(M, K, F),), dtype=torch.uint8, device=x.device) if save else None
     _check(lib().zq_fp8_gated_ffn(x.data_ptr(), ldx, _mode(mode), M, K, F, N, gate_up.codes.data_ptr(),
@@ -612,6 +632,7 @@ def fp8_gated_ffn_backward(gate_up_t: Fp8Weight, down_t: Fp8Weight, dy: torch.Te
     _expect(saved, torch.uint8, "saved")
     if saved.numel() != fp8_gated_ffn_saved_bytes(M, K, F):
         raise ValueError(f"what was saved ({saved.numel()} bytes) is not of {M} tokens")
+    _on_gpu(dy, saved, gate_up_t.codes, gate_up_t.scale, down_t.codes, down_t.scale)
     dev = dy.device
     dx = torch.empty((M, K), dtype=out_dtype, device=dev)
     dwgu = torch.empty((2, F, K), dtype=out_dtype, device=dev)

@@ -21,7 +21,7 @@
 // those of zq_quantize_fp8_block.  With more tokens the cast of a K block in every CTA takes longer than its weights'
 // way from HBM (32 tokens, 7168 -> 28672: 134 us), and a separate quantizer costs less.
 //
-// Warp roles: 0..3 epilogue (kGated: 0..3 gate, 4..7 up), then 4 quantizer warps (without RAW they
+// Warp roles: epilogue (four warps per matrix, with 64 tokens eight: each takes 32 tokens), then 4 quantizer warps (without RAW they
 // bring the tokens' scales; the weight tiles' scales in both forms), 1 producer, 1 tensor memory and MMAs.
 #include "fp8_block.cuh"
 
@@ -53,7 +53,9 @@ struct PF {
 template <int BM, bool GATED>
 struct FewCfg {
   static constexpr int kMats = GATED ? 2 : 1;
-  static constexpr int kEpiWarps = 4 * kMats;
+  static constexpr int kSplit = BM == 64 ? 2 : 1;  // warps that share a channel's tokens
+  static constexpr int kCols1 = BM / kSplit;                 // tokens per epilogue thread
+  static constexpr int kEpiWarps = 4 * kMats * kSplit;
   static constexpr int kQuantWarp0 = kEpiWarps, kQuantWarps = 4;
   static constexpr int kProducerWarp = kEpiWarps + 4, kMmaWarp = kEpiWarps + 5;
   static constexpr int kThreads = 32 * (kEpiWarps + 6);
@@ -166,9 +168,9 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   const int nkb = kb1 - kb0;
   const int m_here = min(BM, p.M - m0);
 
-  uint64_t run[BM / 2];  // epilogue warps: one channel's sums, tokens in pairs
+  uint64_t run[C::kCols1 / 2];  // epilogue warps: one channel's sums, tokens in pairs
 #pragma unroll
-  for (int c = 0; c < BM / 2; ++c) run[c] = 0ull;
+  for (int c = 0; c < C::kCols1 / 2; ++c) run[c] = 0ull;
 
   if (warp == C::kProducerWarp) {
     if (ok_start) {
@@ -357,7 +359,8 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     }
   } else {
     // ---- epilogue warps: running sums of one channel and all tokens
-    const int mat = warp >> 2;
+    const int mat = (warp >> 2) / C::kSplit;
+    const int col0 = (warp >> 2) % C::kSplit * C::kCols1;  // first of this warp's tokens
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     bool failed = !ok_start;
     int s = 0;
@@ -370,19 +373,19 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       }
       tc_fence_after_sync();
       if (!failed) {
-        const uint32_t t = tmem_base + (s * C::kMats + mat) * BM + lane_base;
-        const ulonglong2* sc = reinterpret_cast<const ulonglong2*>(s_sc + s * BM);  // pairs of tokens
+        const uint32_t t = tmem_base + (s * C::kMats + mat) * BM + col0 + lane_base;
+        const ulonglong2* sc = reinterpret_cast<const ulonglong2*>(s_sc + s * BM + col0);  // pairs of tokens
         const float sw = s_sw[2 * s + mat];
         const uint64_t sw2 = pack2(sw, sw);
         float nxt[16];
         tmem_ld16(t, nxt);
 #pragma unroll
-        for (int c = 0; c < BM; c += 16) {
+        for (int c = 0; c < C::kCols1; c += 16) {
           float v[16];
           tmem_ld_wait_regs<16>(nxt);
 #pragma unroll
           for (int e = 0; e < 16; ++e) v[e] = nxt[e];
-          if (c + 16 < BM) tmem_ld16(t + c + 16, nxt);
+          if (c + 16 < C::kCols1) tmem_ld16(t + c + 16, nxt);
 #pragma unroll
           for (int e = 0; e < 16; e += 4) {
             const ulonglong2 f = sc[(c + e) / 4];
@@ -411,10 +414,11 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   float* red = reinterpret_cast<float*>(smem);  // [kMats][BM][128]
   if (warp < C::kEpiWarps) {
 #pragma unroll
-    for (int c = 0; c < BM / 2; ++c) {
+    for (int c = 0; c < C::kCols1 / 2; ++c) {
       float lo, hi;
       unpack2(run[c], lo, hi);
-      float* r = red + ((warp >> 2) * BM + 2 * c) * 128 + (warp & 3) * 32 + lane;
+      // [kMats][BM][128]: a matrix's tokens, by the warps that share them, one after the other
+      float* r = red + ((warp >> 2) * C::kCols1 + 2 * c) * 128 + (warp & 3) * 32 + lane;
       r[0] = lo;
       r[128] = hi;
     }

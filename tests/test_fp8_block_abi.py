@@ -97,6 +97,7 @@ def test_weight_grad_refusals(L):
         return L.zq_fp8_weight_grad(g, ldg, stride, parts, q, s, M, N, K, dw, dt, work, nws, None)
 
     assert call(dt=2) == ERR_MODE
+    assert call(parts=2, stride=0) == ERR_SHAPE  # several parts in one place
     assert call(ldg=7) == ERR_SHAPE and call(parts=0) == ERR_SHAPE and call(parts=65) == ERR_SHAPE and call(K=40) == ERR_SHAPE
     assert call(g=NULL) == ERR_NULL and call(q=NULL) == ERR_NULL and call(dw=NULL) == ERR_NULL
     assert call(N=4, ldg=12) == ERR_ALIGN and call(stride=4, parts=2) == ERR_ALIGN and call(dw=ODD) == ERR_ALIGN
@@ -164,6 +165,13 @@ def test_binding_refusals(L):
         binding.fp8_gated_linear(w, x=torch.zeros((4, 64), dtype=bf))  # one projection, two are needed
     with pytest.raises(ValueError):
         binding.fp8_weight_grad(torch.zeros((5, 8), dtype=bf), binding.Fp8Block(torch.zeros((4, 64), dtype=u8), torch.ones((1, 4))))
+    x = torch.zeros((4, 64), dtype=bf)  # fits, but in host memory
+    for call in (lambda: binding.quantize_fp8_block(x), lambda: binding.fp8_block_linear(w, x=x),
+                 lambda: binding.transpose_fp8_weight(w), lambda: binding.quantize_weight_fp8_block(torch.zeros((32, 64))),
+                 lambda: binding.fp8_weight_grad(torch.zeros((4, 8), dtype=bf),
+                                                 binding.Fp8Block(torch.zeros((4, 64), dtype=u8), torch.ones((1, 4))))):
+        with pytest.raises(ValueError, match="CUDA"):
+            call()
     gu = binding.Fp8Weight(torch.zeros((2, 32, 64), dtype=u8), torch.ones((2, 1, 1)), 32, 64, parts=2)
     with pytest.raises(ValueError):
         gated_ffn.GatedFfnFp8(gu, w)  # down has 64 features, the gated layer 32
