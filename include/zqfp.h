@@ -342,18 +342,24 @@ int zq_w4a8_linear_noalloc_status(int* detail, void* stream);
  *   ZQ_SCALE_NONE: s = max(fl32(a / 448), 2^-126)
  *   ZQ_SCALE_M1  : that, rounded up to a power of two (as M1 does for weight groups)
  *   code = RNE_E4M3(fl32(x * fl32(1 / s))), saturating at +-448.
- * ZQ_SCALE_M2 is refused (ZQ_ERR_MODE).  K (features) is a multiple of 16 throughout; codes are 16-byte aligned.
+ * `mode` is one of these two rules, for what the call itself quantizes (ZQ_SCALE_M2 is refused with ZQ_ERR_MODE), and,
+ * where the call multiplies, may carry a promise: ZQ_SCALES_POW2 or'ed to it says that every scale the call is GIVEN, of
+ * weights and of quantized activations, is a power of two (or NaN).  With many tokens and a bf16 or quantized result
+ * the tensor core then applies the scales itself; the sums are the same up to the order and rounding of FP32
+ * additions.  A broken promise gives wrong results.  With ZQ_SCALE_NONE and raw activations it is refused
+ * (ZQ_ERR_MODE).  K (features) is a multiple of 16 throughout; codes are 16-byte aligned.
  */
+#define ZQ_SCALES_POW2 16
 
 /*
  * x : bf16 [M, ldx], 16-byte aligned, ldx >= K, ldx % 8 == 0;  q : out, E4M3 [M, K];  s : out, FP32 [ceil(K/128), M].
  * This is also how an activation is kept as an 8-bit checkpoint (1.03 bytes per element instead of 2); with
  * ZQ_SCALE_M1 every code * scale is a bf16 number, so that reading it back rounds nothing.  M == 0 is a no-op.
  */
-int zq_quantize_fp8_block(const void* x_bf16, int64_t M, int64_t K, int64_t ldx, zq_scale_mode mode, uint8_t* q,
+int zq_quantize_fp8_block(const void* x_bf16, int64_t M, int64_t K, int64_t ldx, int mode, uint8_t* q,
                           float* s, void* stream);
 /* W : FP32 [N, K] dense, 16-byte aligned;  q : out, E4M3 [N, K];  s : out, FP32 [ceil(N/128), ceil(K/128)]. */
-int zq_quantize_weight_fp8_block(const float* W, int64_t N, int64_t K, zq_scale_mode mode, uint8_t* q, float* s,
+int zq_quantize_weight_fp8_block(const float* W, int64_t N, int64_t K, int mode, uint8_t* q, float* s,
                                  void* stream);
 /* Codes [N, K] and scales of a weight -> codes [K, N] and scales of its transpose, what the gradient with respect to
  * the layer's input multiplies by (laid out once per weight).  N % 16 == 0. */
@@ -377,7 +383,7 @@ size_t zq_fp8_block_workspace_bytes(int64_t M, int64_t K);
  * The products of a block are summed by the tensor core, scaled and summed over the blocks in FP32; results do not
  * vary from run to run.  M == 0 or N == 0 is a no-op.
  */
-int zq_fp8_block_linear(const uint8_t* q, const float* s, const void* x_bf16, int64_t ldx, zq_scale_mode mode,
+int zq_fp8_block_linear(const uint8_t* q, const float* s, const void* x_bf16, int64_t ldx, int mode,
                         int parts, int64_t M, int64_t N, int64_t K, const uint8_t* w, const float* ws, void* y,
                         zq_out_dtype ydt, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
 
@@ -394,7 +400,7 @@ typedef enum { ZQ_ACT_SILU = 0, ZQ_ACT_GELU_TANH = 1, ZQ_ACT_RELU = 2 } zq_activ
  * gu, gus : out or NULL: g and u quantized with `mode`, [2][M, F] and [2][ceil(F/128), M], kept for the backward pass
  * Activations, mode, workspace as zq_fp8_block_linear.
  */
-int zq_fp8_gated_linear(const uint8_t* q, const float* s, const void* x_bf16, int64_t ldx, zq_scale_mode mode,
+int zq_fp8_gated_linear(const uint8_t* q, const float* s, const void* x_bf16, int64_t ldx, int mode,
                         int64_t M, int64_t F, int64_t K, const uint8_t* w, const float* ws, zq_activation act,
                         void* h_bf16, int64_t ldh, uint8_t* hq, float* hs, uint8_t* gu, float* gus, void* workspace,
                         size_t workspace_bytes, void* stream);
@@ -410,7 +416,7 @@ int zq_fp8_gated_linear(const uint8_t* q, const float* s, const void* x_bf16, in
  * dW = zq_fp8_weight_grad of dgu_bf16 and the checkpoint of x.
  */
 int zq_fp8_gated_linear_backward(const uint8_t* q, const float* s, const void* dy_bf16, int64_t lddy,
-                                 zq_scale_mode mode, int64_t M, int64_t F, int64_t K, const uint8_t* wt,
+                                 int mode, int64_t M, int64_t F, int64_t K, const uint8_t* wt,
                                  const float* wts, zq_activation act, const uint8_t* gu, const float* gus,
                                  void* dgu_bf16, uint8_t* dguq, float* dgus, void* workspace, size_t workspace_bytes,
                                  void* stream);
@@ -439,7 +445,7 @@ int zq_fp8_weight_grad(const void* g_bf16, int64_t ldg, int64_t g_stride, int pa
  */
 size_t zq_fp8_gated_ffn_saved_bytes(int64_t M, int64_t K, int64_t F);
 size_t zq_fp8_gated_ffn_workspace_bytes(int64_t M, int64_t K, int64_t F, int64_t N, int training);
-int zq_fp8_gated_ffn(const void* x_bf16, int64_t ldx, zq_scale_mode mode, int64_t M, int64_t K, int64_t F, int64_t N,
+int zq_fp8_gated_ffn(const void* x_bf16, int64_t ldx, int mode, int64_t M, int64_t K, int64_t F, int64_t N,
                      const uint8_t* gate_up, const float* gate_ups, const uint8_t* down, const float* downs,
                      zq_activation act, void* y, zq_out_dtype ydt, int64_t ldy, void* saved, void* workspace,
                      size_t workspace_bytes, void* stream);
@@ -448,7 +454,7 @@ int zq_fp8_gated_ffn(const void* x_bf16, int64_t ldx, zq_scale_mode mode, int64_
  * dense.  gate_up_t : [2][K, F] and down_t : [F, N], the transposed weights (so K % 16 == 0 and N % 16 == 0);
  * workspace with training = 1.
  */
-int zq_fp8_gated_ffn_backward(const void* dy_bf16, int64_t lddy, zq_scale_mode mode, int64_t M, int64_t K, int64_t F,
+int zq_fp8_gated_ffn_backward(const void* dy_bf16, int64_t lddy, int mode, int64_t M, int64_t K, int64_t F,
                               int64_t N, const void* saved, const uint8_t* gate_up_t, const float* gate_up_ts,
                               const uint8_t* down_t, const float* down_ts, zq_activation act, void* dx, void* dw_gate_up,
                               void* dw_down, zq_out_dtype dt, void* workspace, size_t workspace_bytes, void* stream);

@@ -355,6 +355,7 @@ class Fp8Block:
     """Activations as E4M3 codes with one scale per row and 128 features (``zq_quantize_fp8_block``)."""
     codes: torch.Tensor   # uint8 [M, K] (or [parts, M, K])
     scale: torch.Tensor   # float32 [ceil(K / 128), M] (or [parts, ...]): the row index is innermost
+    pow2: bool = False    # the scales are known to be powers of two (mode "M1")
 
     def values(self) -> torch.Tensor:
         """The FP32 values the codes stand for (a convenience for inspection, not a hot path)."""
@@ -372,6 +373,7 @@ class Fp8Weight:
     N: int
     K: int
     parts: int = 1
+    pow2: Optional[bool] = None   # whether all scales are powers of two; None: looked up once, here
 
     def __post_init__(self):
         lead = (self.parts,) if self.parts > 1 else ()
@@ -381,6 +383,8 @@ class Fp8Weight:
                              f"{self.parts} x [{self.N}, {self.K}]")
         _expect(self.codes, torch.uint8, "codes")
         _expect(self.scale, torch.float32, "scale")
+        if self.pow2 is None:  # a mantissa of zero
+            self.pow2 = bool(((self.scale.view(torch.int32) & 0x7FFFFF) == 0).all()) if self.scale.is_cuda else False
 
     def values(self) -> torch.Tensor:
         s = self.scale.repeat_interleave(128, -1)[..., :self.K].repeat_interleave(128, -2)[..., :self.N, :]
@@ -426,7 +430,7 @@ def quantize_fp8_block(x: torch.Tensor, mode="none") -> Fp8Block:
     s = x.new_empty(((K + 127) // 128, M), dtype=torch.float32)
     _check(lib().zq_quantize_fp8_block(_ptr(x), M, K, ldx, _mode(mode), _ptr(q), _ptr(s), _stream()),
            "zq_quantize_fp8_block")
-    return Fp8Block(q, s)
+    return Fp8Block(q, s, _mode(mode) == SCALE_M1)
 
 
 def quantize_weight_fp8_block(W: torch.Tensor, mode="none") -> Fp8Weight:
@@ -442,7 +446,7 @@ def quantize_weight_fp8_block(W: torch.Tensor, mode="none") -> Fp8Weight:
         Wi, qi, si = (W.view(parts, N, K)[i], q.view(parts, N, K)[i], s.view(parts, _blocks(N), _blocks(K))[i])
         _check(lib().zq_quantize_weight_fp8_block(_ptr(Wi), N, K, _mode(mode), _ptr(qi), _ptr(si), _stream()),
                "zq_quantize_weight_fp8_block")
-    return Fp8Weight(q, s, N, K, parts)
+    return Fp8Weight(q, s, N, K, parts, _mode(mode) == SCALE_M1)
 
 
 def transpose_fp8_weight(w: Fp8Weight) -> Fp8Weight:
@@ -457,7 +461,7 @@ def transpose_fp8_weight(w: Fp8Weight) -> Fp8Weight:
             _ptr(w.codes.view(w.parts, w.N, w.K)[i]), _ptr(w.scale.view(w.parts, nb, kb)[i]), w.N, w.K,
             _ptr(q.view(w.parts, w.K, w.N)[i]), _ptr(s.view(w.parts, kb, nb)[i]), _stream()),
             "zq_transpose_weight_fp8_block")
-    return Fp8Weight(q, s, w.K, w.N, w.parts)
+    return Fp8Weight(q, s, w.K, w.N, w.parts, w.pow2)
 
 
 def _activations(x, q, K: int, parts: int):
@@ -478,6 +482,15 @@ def _activations(x, q, K: int, parts: int):
         raise ValueError(f"codes {tuple(q.codes.shape)} / scales {tuple(q.scale.shape)} do not fit {parts} x [M, {K}]")
     _on_gpu(q.codes, q.scale)
     return q.codes, q.scale, None, K, M
+
+
+SCALES_POW2 = 16
+
+
+def _scales(mode, w: Fp8Weight, q: Optional[Fp8Block]) -> int:
+    """The scale rule, with the promise of ``ZQ_SCALES_POW2`` where every scale the call is given is a power of two."""
+    m = _mode(mode)
+    return m | SCALES_POW2 if w.pow2 and (m == SCALE_M1 if q is None else q.pow2) else m
 
 
 _fp8_workspaces = {}
@@ -509,7 +522,7 @@ def fp8_block_linear(w: Fp8Weight, *, x=None, q: Optional[Fp8Block] = None, mode
     if workspace is None:
         workspace = _fp8_workspace(None, M, w.K, w.codes.device)
     _on_gpu(y, workspace)
-    _check(lib().zq_fp8_block_linear(_ptr(codes), _ptr(scale), _ptr(x), ldx, _mode(mode), w.parts, M, w.N, w.K,
+    _check(lib().zq_fp8_block_linear(_ptr(codes), _ptr(scale), _ptr(x), ldx, _scales(mode, w, q), w.parts, M, w.N, w.K,
                                      _ptr(w.codes), _ptr(w.scale), _ptr(y), ydt, y.stride(0) if M > 1 else w.N,
                                      _ptr(workspace), workspace.numel(), _stream()), "zq_fp8_block_linear")
     return y
@@ -532,12 +545,12 @@ def fp8_gated_linear(w: Fp8Weight, *, x=None, q: Optional[Fp8Block] = None, act=
     hq = gu = None
     if quantized:
         hq = Fp8Block(torch.empty((M, F), dtype=torch.uint8, device=dev),
-                      torch.empty((fb, M), dtype=torch.float32, device=dev))
+                      torch.empty((fb, M), dtype=torch.float32, device=dev), _mode(mode) == SCALE_M1)
     if checkpoint:
         gu = Fp8Block(torch.empty((2, M, F), dtype=torch.uint8, device=dev),
-                      torch.empty((2, fb, M), dtype=torch.float32, device=dev))
+                      torch.empty((2, fb, M), dtype=torch.float32, device=dev), _mode(mode) == SCALE_M1)
     workspace = _fp8_workspace(workspace, M, w.K, dev)
-    _check(lib().zq_fp8_gated_linear(_ptr(codes), _ptr(scale), _ptr(x), ldx, _mode(mode), M, F, w.K, _ptr(w.codes),
+    _check(lib().zq_fp8_gated_linear(_ptr(codes), _ptr(scale), _ptr(x), ldx, _scales(mode, w, q), M, F, w.K, _ptr(w.codes),
                                      _ptr(w.scale), _act(act), _ptr(h), F, _ptr(hq and hq.codes), _ptr(hq and hq.scale),
                                      _ptr(gu and gu.codes), _ptr(gu and gu.scale), _ptr(workspace), workspace.numel(),
                                      _stream()), "zq_fp8_gated_linear")
@@ -559,9 +572,9 @@ def fp8_gated_linear_backward(wt: Fp8Weight, gu: Fp8Block, *, dy=None, q: Option
     _expect(gu.scale, torch.float32, "gu.scale")
     d = torch.empty((2, M, F), dtype=torch.bfloat16, device=dev)
     dq = Fp8Block(torch.empty((2, M, F), dtype=torch.uint8, device=dev),
-                  torch.empty((2, fb, M), dtype=torch.float32, device=dev))
+                  torch.empty((2, fb, M), dtype=torch.float32, device=dev), _mode(mode) == SCALE_M1)
     workspace = _fp8_workspace(workspace, M, wt.K, dev)
-    _check(lib().zq_fp8_gated_linear_backward(_ptr(codes), _ptr(scale), _ptr(dy), lddy, _mode(mode), M, F, wt.K,
+    _check(lib().zq_fp8_gated_linear_backward(_ptr(codes), _ptr(scale), _ptr(dy), lddy, _scales(mode, wt, q), M, F, wt.K,
                                               _ptr(wt.codes), _ptr(wt.scale), _act(act), _ptr(gu.codes),
                                               _ptr(gu.scale), _ptr(d), _ptr(dq.codes), _ptr(dq.scale),
                                               _ptr(workspace), workspace.numel(), _stream()),
@@ -612,7 +625,7 @@ def fp8_gated_ffn(gate_up: Fp8Weight, down: Fp8Weight, x: torch.Tensor, *, act="
     _on_gpu(x, gate_up.codes, gate_up.scale, down.codes, down.scale)
     y = torch.empty((M, N), dtype=out_dtype, device=x.device)
     saved = torch.empty((fp8_gated_ffn_saved_bytes(M, K, F),), dtype=torch.uint8, device=x.device) if save else None
-    _check(lib().zq_fp8_gated_ffn(x.data_ptr(), ldx, _mode(mode), M, K, F, N, gate_up.codes.data_ptr(),
+    _check(lib().zq_fp8_gated_ffn(x.data_ptr(), ldx, _scales(mode, gate_up, None) if down.pow2 else _mode(mode), M, K, F, N, gate_up.codes.data_ptr(),
                                   gate_up.scale.data_ptr(), down.codes.data_ptr(), down.scale.data_ptr(), _act(act),
                                   y.data_ptr(), OUT_F32 if out_dtype == torch.float32 else OUT_BF16, N, _ptr(saved),
                                   workspace.data_ptr(), workspace.numel(), _stream()), "zq_fp8_gated_ffn")
@@ -637,7 +650,8 @@ def fp8_gated_ffn_backward(gate_up_t: Fp8Weight, down_t: Fp8Weight, dy: torch.Te
     dx = torch.empty((M, K), dtype=out_dtype, device=dev)
     dwgu = torch.empty((2, F, K), dtype=out_dtype, device=dev)
     dwd = torch.empty((N, F), dtype=out_dtype, device=dev)
-    _check(lib().zq_fp8_gated_ffn_backward(dy.data_ptr(), lddy, _mode(mode), M, K, F, N, saved.data_ptr(),
+    _check(lib().zq_fp8_gated_ffn_backward(dy.data_ptr(), lddy,
+                                           _scales(mode, gate_up_t, None) if down_t.pow2 else _mode(mode), M, K, F, N, saved.data_ptr(),
                                            gate_up_t.codes.data_ptr(), gate_up_t.scale.data_ptr(),
                                            down_t.codes.data_ptr(), down_t.scale.data_ptr(), _act(act), dx.data_ptr(),
                                            dwgu.data_ptr(), dwd.data_ptr(),

@@ -31,6 +31,7 @@ struct GemmArgs8 {
   int64_t M, N, K;
   int parts;         // segments of the K sum (kPlain)
   int kind, act, mode;
+  int pow2_scales;   // sa and sb are powers of two: the tensor core can apply them itself
   void* y;           // kPlain: [M][ldy] FP32 or bf16; kGated: h bf16 [M][ldy] or NULL; kGatedBwd: bf16 [2][M][N]
   int ydt;
   int64_t ldy;
@@ -189,6 +190,10 @@ __device__ __forceinline__ bool mbar_wait_all(uint64_t* bar, uint32_t parity, vo
   return __all_sync(0xFFFFFFFFu, ok);
 }
 
+// Four 32-bit columns of this thread's tensor-memory lane.
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(a), "r"(b), "r"(c), "r"(d));
+}
 __device__ __forceinline__ float ld_cluster(uint32_t addr) {
   float v;
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");

@@ -9,7 +9,12 @@ namespace {
 
 inline bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
-bool scale_rule_ok(int mode) { return mode == ZQ_SCALE_NONE || mode == ZQ_SCALE_M1; }
+int rule_of(int mode) { return mode & ~ZQ_SCALES_POW2; }
+// raw: the call quantizes an operand itself, by a rule that has to keep the promise of ZQ_SCALES_POW2
+bool scale_rule_ok(int mode, bool raw = false) {
+  const int rule = rule_of(mode);
+  return (rule == ZQ_SCALE_NONE && !(raw && mode != rule)) || rule == ZQ_SCALE_M1;
+}
 bool act_ok(int act) { return act == ZQ_ACT_SILU || act == ZQ_ACT_GELU_TANH || act == ZQ_ACT_RELU; }
 constexpr int64_t kMaxRows = 0x7FFFFF00;
 bool rows_ok(int64_t n) { return n >= 0 && n <= kMaxRows; }
@@ -72,9 +77,9 @@ int check_activations(const uint8_t* q, const float* s, const void* x, int64_t l
 
 extern "C" {
 
-int zq_quantize_fp8_block(const void* x, int64_t M, int64_t K, int64_t ldx, zq_scale_mode mode, uint8_t* q, float* s,
+int zq_quantize_fp8_block(const void* x, int64_t M, int64_t K, int64_t ldx, int mode, uint8_t* q, float* s,
                           void* stream) {
-  if (!scale_rule_ok(mode)) return ZQ_ERR_MODE;
+  if (mode != rule_of(mode) || !scale_rule_ok(mode)) return ZQ_ERR_MODE;
   if (!rows_ok(M) || !k_ok(K) || ldx < K) return ZQ_ERR_SHAPE;
   if (M == 0) return ZQ_OK;
   if (!x || !q || !s) return ZQ_ERR_NULL;
@@ -83,9 +88,9 @@ int zq_quantize_fp8_block(const void* x, int64_t M, int64_t K, int64_t ldx, zq_s
   return launch_quantize_block(x, M, K, ldx, mode, q, s, static_cast<cudaStream_t>(stream));
 }
 
-int zq_quantize_weight_fp8_block(const float* W, int64_t N, int64_t K, zq_scale_mode mode, uint8_t* q, float* s,
+int zq_quantize_weight_fp8_block(const float* W, int64_t N, int64_t K, int mode, uint8_t* q, float* s,
                                  void* stream) {
-  if (!scale_rule_ok(mode)) return ZQ_ERR_MODE;
+  if (mode != rule_of(mode) || !scale_rule_ok(mode)) return ZQ_ERR_MODE;
   if (!rows_ok(N) || !k_ok(K)) return ZQ_ERR_SHAPE;
   if (N == 0) return ZQ_OK;
   if (!W || !q || !s) return ZQ_ERR_NULL;
@@ -109,10 +114,10 @@ size_t zq_fp8_block_workspace_bytes(int64_t M, int64_t K) {
   return ws8(M, K).total;
 }
 
-int zq_fp8_block_linear(const uint8_t* q, const float* s, const void* x_bf16, int64_t ldx, zq_scale_mode mode, int parts,
+int zq_fp8_block_linear(const uint8_t* q, const float* s, const void* x_bf16, int64_t ldx, int mode, int parts,
                         int64_t M, int64_t N, int64_t K, const uint8_t* w, const float* ws, void* y, zq_out_dtype ydt,
                         int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!scale_rule_ok(mode) || (ydt != ZQ_OUT_F32 && ydt != ZQ_OUT_BF16)) return ZQ_ERR_MODE;
+  if (!scale_rule_ok(mode, x_bf16 != nullptr) || (ydt != ZQ_OUT_F32 && ydt != ZQ_OUT_BF16)) return ZQ_ERR_MODE;
   if (!rows_ok(M) || !rows_ok(N) || !k_ok(K) || ldy < N || parts < 1 || parts > 2 || (x_bf16 && parts != 1))
     return ZQ_ERR_SHAPE;
   if (M == 0 || N == 0) return ZQ_OK;
@@ -128,18 +133,19 @@ int zq_fp8_block_linear(const uint8_t* q, const float* s, const void* x_bf16, in
   a.K = K;
   a.parts = parts;
   a.kind = kPlain;
-  a.mode = mode;
+  a.mode = rule_of(mode);
+  a.pow2_scales = mode != a.mode;
   a.y = y;
   a.ydt = ydt;
   a.ldy = ldy;
   return launch(a, q, s, x_bf16, ldx, workspace, workspace_bytes, stream);
 }
 
-int zq_fp8_gated_linear(const uint8_t* q, const float* s, const void* x_bf16, int64_t ldx, zq_scale_mode mode, int64_t M,
+int zq_fp8_gated_linear(const uint8_t* q, const float* s, const void* x_bf16, int64_t ldx, int mode, int64_t M,
                         int64_t F, int64_t K, const uint8_t* w, const float* ws, zq_activation act, void* h_bf16,
                         int64_t ldh, uint8_t* hq, float* hs, uint8_t* gu, float* gus, void* workspace,
                         size_t workspace_bytes, void* stream) {
-  if (!scale_rule_ok(mode) || !act_ok(act)) return ZQ_ERR_MODE;
+  if (!scale_rule_ok(mode, x_bf16 != nullptr) || !act_ok(act)) return ZQ_ERR_MODE;
   if (!rows_ok(M) || !rows_ok(F) || F % 16 || !k_ok(K) || (h_bf16 && ldh < F)) return ZQ_ERR_SHAPE;
   if (M == 0 || F == 0) return ZQ_OK;
   if (!w || !ws || (!h_bf16 && !hq) || (hq && !hs) || (gu && !gus)) return ZQ_ERR_NULL;
@@ -155,7 +161,8 @@ int zq_fp8_gated_linear(const uint8_t* q, const float* s, const void* x_bf16, in
   a.parts = 1;
   a.kind = kGated;
   a.act = act;
-  a.mode = mode;
+  a.mode = rule_of(mode);
+  a.pow2_scales = mode != a.mode;
   a.y = h_bf16;
   a.ydt = ZQ_OUT_BF16;
   a.ldy = ldh;
@@ -166,11 +173,11 @@ int zq_fp8_gated_linear(const uint8_t* q, const float* s, const void* x_bf16, in
   return launch(a, q, s, x_bf16, ldx, workspace, workspace_bytes, stream);
 }
 
-int zq_fp8_gated_linear_backward(const uint8_t* q, const float* s, const void* dy_bf16, int64_t lddy, zq_scale_mode mode,
+int zq_fp8_gated_linear_backward(const uint8_t* q, const float* s, const void* dy_bf16, int64_t lddy, int mode,
                                  int64_t M, int64_t F, int64_t K, const uint8_t* wt, const float* wts, zq_activation act,
                                  const uint8_t* gu, const float* gus, void* dgu_bf16, uint8_t* dguq, float* dgus,
                                  void* workspace, size_t workspace_bytes, void* stream) {
-  if (!scale_rule_ok(mode) || !act_ok(act)) return ZQ_ERR_MODE;
+  if (!scale_rule_ok(mode, dy_bf16 != nullptr) || !act_ok(act)) return ZQ_ERR_MODE;
   if (!rows_ok(M) || !rows_ok(F) || F % 16 || !k_ok(K)) return ZQ_ERR_SHAPE;
   if (M == 0 || F == 0) return ZQ_OK;
   if (!wt || !wts || !gu || !gus || !dgu_bf16 || !dguq || !dgus) return ZQ_ERR_NULL;
@@ -186,7 +193,8 @@ int zq_fp8_gated_linear_backward(const uint8_t* q, const float* s, const void* d
   a.parts = 1;
   a.kind = kGatedBwd;
   a.act = act;
-  a.mode = mode;
+  a.mode = rule_of(mode);
+  a.pow2_scales = mode != a.mode;
   a.y = dgu_bf16;
   a.ydt = ZQ_OUT_BF16;
   a.ldy = F;
@@ -281,12 +289,12 @@ size_t zq_fp8_gated_ffn_workspace_bytes(int64_t M, int64_t K, int64_t F, int64_t
   return ws_ffn(M, K, F, N, training != 0).total;
 }
 
-int zq_fp8_gated_ffn(const void* x, int64_t ldx, zq_scale_mode mode, int64_t M, int64_t K, int64_t F, int64_t N,
+int zq_fp8_gated_ffn(const void* x, int64_t ldx, int mode, int64_t M, int64_t K, int64_t F, int64_t N,
                      const uint8_t* gate_up, const float* gate_ups, const uint8_t* down, const float* downs,
                      zq_activation act, void* y, zq_out_dtype ydt, int64_t ldy, void* saved, void* workspace,
                      size_t workspace_bytes, void* stream) {
   // everything the second call would refuse is refused before the first one launches
-  if (!scale_rule_ok(mode) || !act_ok(act) || (ydt != ZQ_OUT_F32 && ydt != ZQ_OUT_BF16)) return ZQ_ERR_MODE;
+  if (!scale_rule_ok(mode, true) || !act_ok(act) || (ydt != ZQ_OUT_F32 && ydt != ZQ_OUT_BF16)) return ZQ_ERR_MODE;
   if (!ffn_sizes_ok(M, K, F, N) || ldx < K || ldy < N) return ZQ_ERR_SHAPE;
   if (M == 0) return ZQ_OK;
   if (!x || !gate_up || !gate_ups || (N > 0 && (!down || !downs || !y))) return ZQ_ERR_NULL;
@@ -313,7 +321,7 @@ int zq_fp8_gated_ffn(const void* x, int64_t ldx, zq_scale_mode mode, int64_t M, 
   float* xs = reinterpret_cast<float*>(sv + v.xs);
   uint8_t* hq = sv + v.hq;
   float* hs = reinterpret_cast<float*>(sv + v.hs);
-  if (int e = zq_quantize_fp8_block(x, M, K, ldx, mode, xq, xs, stream)) return e;
+  if (int e = zq_quantize_fp8_block(x, M, K, ldx, rule_of(mode), xq, xs, stream)) return e;
   if (int e = zq_fp8_gated_linear(xq, xs, nullptr, 0, mode, M, F, K, gate_up, gate_ups, act, nullptr, 0, hq, hs, sv + v.gu,
                                   reinterpret_cast<float*>(sv + v.gus), workspace, workspace_bytes, stream))
     return e;
@@ -321,11 +329,11 @@ int zq_fp8_gated_ffn(const void* x, int64_t ldx, zq_scale_mode mode, int64_t M, 
                              stream);
 }
 
-int zq_fp8_gated_ffn_backward(const void* dy, int64_t lddy, zq_scale_mode mode, int64_t M, int64_t K, int64_t F, int64_t N,
+int zq_fp8_gated_ffn_backward(const void* dy, int64_t lddy, int mode, int64_t M, int64_t K, int64_t F, int64_t N,
                               const void* saved, const uint8_t* gate_up_t, const float* gate_up_ts, const uint8_t* down_t,
                               const float* down_ts, zq_activation act, void* dx, void* dw_gate_up, void* dw_down,
                               zq_out_dtype dt, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!scale_rule_ok(mode) || !act_ok(act) || (dt != ZQ_OUT_F32 && dt != ZQ_OUT_BF16)) return ZQ_ERR_MODE;
+  if (!scale_rule_ok(mode, true) || !act_ok(act) || (dt != ZQ_OUT_F32 && dt != ZQ_OUT_BF16)) return ZQ_ERR_MODE;
   if (!ffn_sizes_ok(M, K, F, N) || !k_ok(N) || lddy < N) return ZQ_ERR_SHAPE;
   if (!dw_gate_up || !dw_down || (M > 0 && (!dy || !saved || !gate_up_t || !gate_up_ts || !down_t || !down_ts || !dx)))
     return ZQ_ERR_NULL;

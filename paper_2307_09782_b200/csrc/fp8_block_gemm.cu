@@ -36,11 +36,15 @@ constexpr int kEpiWarps = 8, kEpiThreads = 256;
 constexpr int kProducerWarp = 8, kMmaWarp = 9;
 constexpr int kThreads = 384;  // three warpgroups; the two epilogue ones take registers over from the third
 // 384 threads start with 168 registers each; 2 x 128 x epilogue + 128 x other is what the block was given
-template <int KIND>
+// With block scales in the tensor core (MX) there are 512 threads with 128 registers each, and a second other warpgroup.
+template <int KIND, bool MX>
 struct Regs {
-  static constexpr int kEpi = KIND == kGatedBwd ? 232 : (KIND == kGated ? 216 : 224);
-  static constexpr int kOther = 3 * 168 - 2 * kEpi;
+  static constexpr int kEpi = MX ? (KIND == kGatedBwd ? 208 : 192) : (KIND == kGatedBwd ? 232 : (KIND == kGated ? 216 : 224));
+  static constexpr int kOther = MX ? (4 * 128 - 2 * kEpi) / 2 : 3 * 168 - 2 * kEpi;
 };
+constexpr int threads_of(bool mx) { return mx ? 512 : kThreads; }
+constexpr int kSfWarp0 = 12;    // MX: 12..15 write the block scales, one per lane quarter of tensor memory
+constexpr int kSfCol0 = kTileN; // MX: one accumulator, then 16 columns of scales per stage (4 rows' blocks, 8 columns' blocks)
 constexpr int kStageBuf = 32 * 128;  // staging of one epilogue warp: 32 rows of 128 bytes
 constexpr int kStages = 4;
 constexpr int kABytes = kTileM * kBlk, kBBytes = kTileN * kBlk;
@@ -48,7 +52,7 @@ constexpr int kOffA = 0;
 constexpr int kOffB = kOffA + kStages * kABytes;
 constexpr int kOffStage = kOffB + kStages * kBBytes;
 constexpr int kOffBars = kOffStage + kEpiWarps * kStageBuf;
-constexpr int kNumBars = 2 * kStages + 8 + 1;
+constexpr int kNumBars = 3 * kStages + 8 + 1;
 constexpr int kOffScale = kOffBars + ((kNumBars * 8 + 15) / 16) * 16;  // [2 halves][2 accumulators][kScaleRow] scales of a K block
 constexpr int kScaleRow = kTileM + 4;  // the rows' scales, then the columns' (kGated: gate, up)
 constexpr int kOffMisc = kOffScale + 4 * kScaleRow * 4;
@@ -177,8 +181,8 @@ __device__ __forceinline__ void rotate(uint64_t* run) {
   for (int e = 0; e < N; ++e) run[64 - N + e] = t[e];
 }
 
-template <int KIND, int ACT, bool F32>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int KIND, int ACT, bool F32, bool MX>
+__global__ void __launch_bounds__(threads_of(MX), 1)
 fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const P8 p) {
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBars);
@@ -187,7 +191,8 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   // per column half h and accumulator a, at 2 h + a:
   uint64_t* acc_full = empty + kStages;  // [4] a K block's products are in the accumulator, its scales in shared memory (epilogue waits)
   uint64_t* acc_empty = acc_full + 4;    // [4] the half's epilogue warps have read it (MMA, scale warp wait)
-  uint64_t* drain_bar = acc_empty + 4;
+  uint64_t* sf_full = acc_empty + 4;     // [stages] MX: the stage's block scales are in tensor memory (MMA waits)
+  uint64_t* drain_bar = sf_full + kStages;
   float* s_scale = reinterpret_cast<float*>(smem + kOffScale);
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + kOffMisc);
   volatile int* s_abort = reinterpret_cast<volatile int*>(smem + kOffMisc + 4);
@@ -197,10 +202,11 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
+      mbar_init(&sf_full[i], 4);
     }
     for (int i = 0; i < 4; ++i) {
-      mbar_init(&acc_full[i], 2);  // the MMAs' commit and the half's scale warp
-      mbar_init(&acc_empty[i], kEpiWarps / 2);
+      mbar_init(&acc_full[i], MX ? 1 : 2);  // the MMAs' commit and the half's scale warp
+      mbar_init(&acc_empty[i], MX ? kEpiWarps : kEpiWarps / 2);
     }
     mbar_init(drain_bar, 1);
     *s_abort = 0;
@@ -222,7 +228,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   if (threadIdx.x == 0) pdl_launch_dependents();
 
   if (warp >= kEpiWarps) {
-  regs_give<Regs<KIND>::kOther>();
+  regs_give<Regs<KIND, MX>::kOther>();
   if (warp == kProducerWarp) {
     if (ok_start) {
       const bool issuer = elect_one();
@@ -275,16 +281,23 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       const bool issuer = elect_one();
       const uint64_t adesc0 = umma_desc_k128(smem_u32(smem + kOffA));
       const uint64_t bdesc0 = umma_desc_k128(smem_u32(smem + kOffB));
-      const uint32_t idesc = umma_idesc_e4m3(kTileN);
+      const uint32_t idesc = MX ? umma_idesc_mx_e4m3_e4m3(kTileN, 0, 0) : umma_idesc_e4m3(kTileN);
       int s = 0;
       uint32_t ph = 0;
       bool failed = false;
       int count = 0;  // K blocks so far: block c goes to accumulator c % 2
-      for (int pos = blockIdx.x; !failed && pos < tiles; pos += gridDim.x) {
+      int tile = 0;
+      for (int pos = blockIdx.x; !failed && pos < tiles; pos += gridDim.x, ++tile) {
         for (int i = 0; i < kb_all; ++i, ++count) {
-          const int buf = count & 1;
+          const int buf = MX ? 0 : count & 1;
           const uint32_t free_ph = ((count >> 1) - 1) & 1;
-          if (!mbar_wait(&full[s], ph, s_abort) || (count >= 2 && !mbar_wait(&acc_empty[buf], free_ph, s_abort)) ||
+          if (MX) {
+            if ((i == 0 && tile > 0 && !mbar_wait(&acc_empty[0], (tile - 1) & 1, s_abort)) || !mbar_wait(&full[s], ph, s_abort) ||
+                !mbar_wait(&sf_full[s], ph, s_abort)) {
+              failed = true;
+              break;
+            }
+          } else if (!mbar_wait(&full[s], ph, s_abort) || (count >= 2 && !mbar_wait(&acc_empty[buf], free_ph, s_abort)) ||
               (count >= 2 && !mbar_wait(&acc_empty[2 + buf], free_ph, s_abort))) {
             failed = true;
             break;
@@ -293,7 +306,16 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
           const uint64_t ad = adesc0 + static_cast<uint64_t>((s * kABytes) >> 4);
           const uint64_t bd = bdesc0 + static_cast<uint64_t>((s * kBBytes) >> 4);
           const uint32_t d = tmem_base + buf * kTileN;
-          if (issuer) {
+          if (MX) {
+            if (issuer) {
+              const uint32_t sf = tmem_base + kSfCol0 + 16 * s;
+#pragma unroll
+              for (int k = 0; k < kBlk / 32; ++k)
+                umma_mxf8f6f4(d, ad + 2 * k, bd + 2 * k, idesc, sf, sf + 4, (i > 0 || k > 0) ? 1u : 0u);
+              if (i + 1 == kb_all) umma_commit(&acc_full[0]);
+              umma_commit(&empty[s]);
+            }
+          } else if (issuer) {
 #pragma unroll
             for (int k = 0; k < kBlk / 32; ++k) umma_f8(d, ad + 2 * k, bd + 2 * k, idesc, k > 0 ? 1u : 0u);
             umma_commit(&acc_full[buf]);
@@ -314,6 +336,78 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       while (!mbar_try_wait(drain_bar, 0) && ++spin < kSpinLimit) {
       }
       __syncwarp();
+    }
+  } else if (MX) {
+    if (ok_start && warp >= kSfWarp0) {
+      // ---- block scales (powers of two) as E8M0 bytes, the same for the four blocks of 32 that a K block has: rows l, l + 32,
+      // l + 64, l + 96 of the tokens in lane l of four columns, the columns' likewise in eight; every lane quarter of
+      // tensor memory holds a copy, which its warp writes.  Loaded two blocks ahead.
+      constexpr int kAhead = 2;
+      pdl_wait();
+      int s = 0, issued = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+      for (int pos = blockIdx.x; ok && pos < tiles; pos += gridDim.x) {
+        int mt, nt;
+        tile_of(p, pos, mt, nt);
+        const int m0 = mt * kTileM + lane;
+        const int64_t part = static_cast<int64_t>(p.nblocks) * p.kblocks;
+        // kGated: columns 0..63 and 128..191 are the gate's, the others the up projection's
+        const float* sb0 = p.sb + static_cast<int64_t>(KIND == kGated ? nt : 2 * nt) * p.kblocks;
+        const float* sb1 = KIND == kGated ? sb0 + part : p.sb + static_cast<int64_t>(min(2 * nt + 1, p.nblocks - 1)) * p.kblocks;
+        uint32_t a[kAhead][4], b[kAhead][2];
+        auto byte4 = [](float v) { return ((__float_as_uint(v) >> 23) & 0xFFu) * 0x01010101u; };
+        const float* sa = p.sa + m0;
+        auto fetch = [&](int i, int slot) {  // called for i = 0, 1, 2, ...
+          if (KIND == kPlain && i == p.kblocks) {  // the second segment
+            sb0 += part - p.kblocks;
+            sb1 += part - p.kblocks;
+          }
+          b[slot][0] = byte4(__ldg(sb0++));
+          b[slot][1] = byte4(__ldg(sb1++));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) a[slot][j] = byte4(m0 + 32 * j < p.M ? __ldg(sa + 32 * j) : 1.0f);
+          sa += p.M;
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+          if (i < kb_all) fetch(i, i);
+        for (int i0 = 0; ok && i0 < kb_all; i0 += kAhead) {
+#pragma unroll
+          for (int u = 0; u < kAhead; ++u) {
+            const int i = i0 + u;
+            if (ok && i < kb_all) {
+              // (the MMAs that read the stage's scales last are those that release its shared memory)
+              if (issued >= kStages && !mbar_wait_all(&empty[s], ph ^ 1, s_abort)) {
+                if (lane == 0) raise_error8(p.status, s_abort, kErrScale8);
+                ok = false;
+              } else {
+                tc_fence_after_sync();
+                const uint32_t t = tmem_base + kSfCol0 + 16 * s + lane_base, b0 = b[u][0], b1 = b[u][1];
+                tmem_st4(t, a[u][0], a[u][1], a[u][2], a[u][3]);
+                if (KIND == kGated) {
+                  tmem_st4(t + 4, b0, b0, b1, b1);
+                  tmem_st4(t + 8, b0, b0, b1, b1);
+                } else {
+                  tmem_st4(t + 4, b0, b0, b0, b0);
+                  tmem_st4(t + 8, b1, b1, b1, b1);
+                }
+                tmem_st_wait();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sf_full[s]);
+                if (i + kAhead < kb_all) fetch(i + kAhead, u);
+                ++issued;
+                if (++s == kStages) {
+                  s = 0;
+                  ph ^= 1;
+                }
+              }
+            }
+          }
+        }
+      }
     }
   } else if (ok_start) {
     // ---- scale warps, one per column half: the scales of a K block's 128 rows and of its columns, loaded two blocks
@@ -369,7 +463,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   }
   } else {
     // ---- epilogue warps
-    regs_take<Regs<KIND>::kEpi>();
+    regs_take<Regs<KIND, MX>::kEpi>();
     const int quarter = warp & 3, half = warp >> 2;
     const int row = quarter * 32 + lane;
     const uint32_t lane_base = static_cast<uint32_t>(quarter * 32) << 16;
@@ -396,7 +490,29 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       uint64_t run[64];
 #pragma unroll
       for (int e = 0; e < 64; ++e) run[e] = 0ull;
-      for (int i = 0; i < kb_all; ++i, ++count) {
+      if (MX) {
+        // the tile's sums, complete: into registers, and the MMAs of the next tile may begin
+        if (!failed && !mbar_wait_all(&acc_full[0], count & 1, s_abort)) {
+          if (lane == 0) raise_error8(p.status, s_abort, kErrEpilogue8);
+          failed = true;
+        }
+        ++count;
+        tc_fence_after_sync();
+        if (!failed) {
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            float v[16];
+            tmem_ld16(tmem_base + half * (kTileN / 2) + 16 * c + lane_base, v);
+            tmem_ld_wait_regs<16>(v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) run[8 * c + e] = pack2(v[2 * e], v[2 * e + 1]);
+          }
+        }
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0 && !failed) mbar_arrive(&acc_empty[0]);
+      }
+      for (int i = 0; !MX && i < kb_all; ++i, ++count) {
         const int b = 2 * half + (count & 1);
         if (!failed && !mbar_wait_all(&acc_full[b], (count >> 1) & 1, s_abort)) {
           if (lane == 0) raise_error8(p.status, s_abort, kErrEpilogue8);
@@ -526,7 +642,9 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         uint32_t ag[8], au[8];
 #pragma unroll
         for (int it = 0; it < 8; ++it) ag[it] = au[it] = 0u;
-        uint32_t gn[8], un[8];  // the next 32 columns' codes
+        // the next 32 columns' codes, on their way while these are worked on (MX: the MMAs do not wait for this epilogue, and
+        // its warps have no registers to spare)
+        uint32_t gn[8], un[8];
         auto fetch = [&](int c) {
 #pragma unroll
           for (int it = 0; it < 8; ++it) {
@@ -538,16 +656,17 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
             }
           }
         };
-        fetch(0);
+        if (!MX) fetch(0);
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
+          if (MX) fetch(c);
           uint32_t gc[8], uc[8];
 #pragma unroll
           for (int it = 0; it < 8; ++it) {
             gc[it] = gn[it];
             uc[it] = un[it];
           }
-          if (c < 3) fetch(c + 1);
+          if (!MX && c < 3) fetch(c + 1);
           __syncwarp();
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
@@ -632,27 +751,31 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   }
 }
 
-template <int KIND, int ACT, bool F32>
+template <int KIND, int ACT, bool F32, bool MX>
 int launch_cfg(const CUtensorMap& ta, const CUtensorMap& tb, const P8& p, cudaStream_t st) {
   static std::once_flag once;
   static cudaError_t attr = cudaSuccess;
   std::call_once(once, [] {
-    attr = cudaFuncSetAttribute(fp8_block_gemm_kernel<KIND, ACT, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    attr = cudaFuncSetAttribute(fp8_block_gemm_kernel<KIND, ACT, F32, MX>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   });
   if (attr != cudaSuccess) return ZQ_ERR_CUDA;
   const int tiles = p.m_tiles * p.n_tiles;
   const unsigned grid = static_cast<unsigned>(tiles < sm_count() ? tiles : sm_count());
-  const cudaError_t e = launch_chained(fp8_block_gemm_kernel<KIND, ACT, F32>, dim3(grid), dim3(kThreads), kSmemBytes, st, false,
+  const cudaError_t e = launch_chained(fp8_block_gemm_kernel<KIND, ACT, F32, MX>, dim3(grid), dim3(threads_of(MX)), kSmemBytes, st, false,
                                        ta, tb, p);
   count_launch();
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
 }
 
+template <int KIND, int ACT>
+int launch_mx(bool mx, const CUtensorMap& ta, const CUtensorMap& tb, const P8& p, cudaStream_t st) {
+  return mx ? launch_cfg<KIND, ACT, false, true>(ta, tb, p, st) : launch_cfg<KIND, ACT, false, false>(ta, tb, p, st);
+}
 template <int KIND>
-int launch_act(int act, const CUtensorMap& ta, const CUtensorMap& tb, const P8& p, cudaStream_t st) {
-  if (act == ZQ_ACT_SILU) return launch_cfg<KIND, ZQ_ACT_SILU, false>(ta, tb, p, st);
-  if (act == ZQ_ACT_GELU_TANH) return launch_cfg<KIND, ZQ_ACT_GELU_TANH, false>(ta, tb, p, st);
-  return launch_cfg<KIND, ZQ_ACT_RELU, false>(ta, tb, p, st);
+int launch_act(int act, bool mx, const CUtensorMap& ta, const CUtensorMap& tb, const P8& p, cudaStream_t st) {
+  if (act == ZQ_ACT_SILU) return launch_mx<KIND, ZQ_ACT_SILU>(mx, ta, tb, p, st);
+  if (act == ZQ_ACT_GELU_TANH) return launch_mx<KIND, ZQ_ACT_GELU_TANH>(mx, ta, tb, p, st);
+  return launch_mx<KIND, ZQ_ACT_RELU>(mx, ta, tb, p, st);
 }
 
 }  // namespace
@@ -686,10 +809,12 @@ int launch_block_gemm(const GemmArgs8& a, cudaStream_t st) {
       !make_code_map(&tb, a.b, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.N),
                      a.kind == kGated ? 2u : static_cast<uint64_t>(p.segs), a.kind == kGated ? 64 : kTileN))
     return ZQ_ERR_CUDA;
-  if (a.kind == kGated) return launch_act<kGated>(a.act, ta, tb, p, st);
-  if (a.kind == kGatedBwd) return launch_act<kGatedBwd>(a.act, ta, tb, p, st);
-  return a.ydt == ZQ_OUT_F32 ? launch_cfg<kPlain, ZQ_ACT_RELU, true>(ta, tb, p, st)
-                             : launch_cfg<kPlain, ZQ_ACT_RELU, false>(ta, tb, p, st);
+  // FP32 results keep the promotion: the tensor core rounds its running sum towards zero, about 1e-8 of it per block
+  const bool mx = a.pow2_scales && a.ydt != ZQ_OUT_F32;
+  if (a.kind == kGated) return launch_act<kGated>(a.act, mx, ta, tb, p, st);
+  if (a.kind == kGatedBwd) return launch_act<kGatedBwd>(a.act, mx, ta, tb, p, st);
+  return a.ydt == ZQ_OUT_F32 ? launch_cfg<kPlain, ZQ_ACT_RELU, true, false>(ta, tb, p, st)
+                             : launch_mx<kPlain, ZQ_ACT_RELU>(mx, ta, tb, p, st);
 }
 
 }  // namespace fp8b
