@@ -373,7 +373,8 @@ class Fp8Weight:
     N: int
     K: int
     parts: int = 1
-    pow2: Optional[bool] = None   # whether all scales are powers of two; None: looked up once, here
+    pow2: Optional[bool] = None   # whether all scales are powers of two; None: looked up once, here (set it anew where
+                                  # the scales are changed in place)
 
     def __post_init__(self):
         lead = (self.parts,) if self.parts > 1 else ()
@@ -383,8 +384,9 @@ class Fp8Weight:
                              f"{self.parts} x [{self.N}, {self.K}]")
         _expect(self.codes, torch.uint8, "codes")
         _expect(self.scale, torch.float32, "scale")
-        if self.pow2 is None:  # a mantissa of zero
-            self.pow2 = bool(((self.scale.view(torch.int32) & 0x7FFFFF) == 0).all()) if self.scale.is_cuda else False
+        if self.pow2 is None:  # positive, finite, no zero, a mantissa of zero
+            bits = self.scale.view(torch.int32)
+            self.pow2 = self.scale.is_cuda and bool((((bits & 0x7FFFFF) == 0) & (bits > 0) & (bits < 0x7F800000)).all())
 
     def values(self) -> torch.Tensor:
         s = self.scale.repeat_interleave(128, -1)[..., :self.K].repeat_interleave(128, -2)[..., :self.N, :]

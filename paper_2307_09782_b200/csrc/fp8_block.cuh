@@ -190,6 +190,12 @@ __device__ __forceinline__ bool mbar_wait_all(uint64_t* bar, uint32_t parity, vo
   return __all_sync(0xFFFFFFFFu, ok);
 }
 
+// Arrive on the leader's barrier of a CTA pair for what has been done to tensor memory (the loads or stores are waited for and
+// fenced): nothing in other memory is published, and a release at cluster scope would wait for the warp's other accesses,
+// about 1000 cycles.
+__device__ __forceinline__ void mbar_arrive_tmem(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_to_rank(smem_u32(bar), 0)) : "memory");
+}
 // Four 32-bit columns of this thread's tensor-memory lane.
 __device__ __forceinline__ void tmem_st4(uint32_t taddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(a), "r"(b), "r"(c), "r"(d));

@@ -19,10 +19,22 @@
 // No spills: with 227 KB of shared memory the first-level cache holds none of them; 100 bytes per thread in the gradient's
 // epilogue doubled the kernel's time.
 //
-// Warp roles: 0..7 epilogue (lane quarter warp % 4, column half warp / 4), 8 producer, 9 tensor memory and MMAs,
-// 10 and 11 scales.
-// Persistent: one CTA per SM walks the tiles, blockIdx.x, + gridDim.x, ..., token tiles in groups so that the CTAs
-// running at one time share operands in L2.
+//
+// Powers of two (MX): where all scales are (rule M1 on both sides, the caller's promise), they are E8M0 bytes that the
+// tensor core multiplies in by itself, exactly: one accumulator takes all of K, nothing is promoted, and the epilogue, with
+// the sums in registers, runs behind the next tile's MMAs.  A K block's scale stands for the four blocks of 32 that the MMA
+// has in it; four warps write the bytes straight into tensor memory (tcgen05.st), stage by stage: no second operand
+// format.  A pair of CTAs takes 256 tokens x 256 columns, so that a CTA loads half of the columns and has six stages.
+// Measured, us, promotion -> MX (2048 tokens unless said): product 4096 -> 11008 93 -> 68; 8192 tokens 7168 -> 28672 1640 -> 1230
+// (2.7 PFLOP/s); gated layer 4096 -> 11008 191 -> 145; gradient 176 -> 128, its epilogue bound.  What the steps gave, on the
+// product: single CTAs 86; pairs 84; scales loaded four K blocks ahead and made bytes only when used 73 (with two ahead, the
+// loads' latency set the pace); sums out of tensor memory with one wait 68.
+// What bounds MX: at 2.7 PFLOP/s and the clock that the power cap leaves (1.6 - 1.7 GHz) the MMAs run about 2/3 of the time.
+//
+// Warp roles: 0..7 epilogue (lane quarter warp % 4, column half warp / 4), 8 producer, 9 tensor memory and MMAs (MX: the
+// leader's for both CTAs), 10 and 11 scales, MX: 12..15 scales.
+// Persistent: one CTA per SM (MX: one pair per two) walks the tiles, blockIdx.x, + gridDim.x, ..., token tiles in groups so that
+// the CTAs running at one time share operands in L2.
 #include "fp8_block.cuh"
 
 namespace zq {
@@ -46,13 +58,14 @@ constexpr int threads_of(bool mx) { return mx ? 512 : kThreads; }
 constexpr int kSfWarp0 = 12;    // MX: 12..15 write the block scales, one per lane quarter of tensor memory
 constexpr int kSfCol0 = kTileN; // MX: one accumulator, then 16 columns of scales per stage (4 rows' blocks, 8 columns' blocks)
 constexpr int kStageBuf = 32 * 128;  // staging of one epilogue warp: 32 rows of 128 bytes
-constexpr int kStages = 4;
-constexpr int kABytes = kTileM * kBlk, kBBytes = kTileN * kBlk;
-constexpr int kOffA = 0;
-constexpr int kOffB = kOffA + kStages * kABytes;
-constexpr int kOffStage = kOffB + kStages * kBBytes;
+// MX: the two CTAs of a pair bring half of the columns each, so that more stages fit
+__host__ __device__ constexpr int stages_of(bool mx) { return mx ? 6 : 4; }
+constexpr int kABytes = kTileM * kBlk;
+__host__ __device__ constexpr int b_bytes_of(bool mx) { return (mx ? kTileN / 2 : kTileN) * kBlk; }
+constexpr int kOffStage = 4 * (kABytes + b_bytes_of(false));
+static_assert(kOffStage == 6 * (kABytes + b_bytes_of(true)), "the stages of both forms take the same room");
 constexpr int kOffBars = kOffStage + kEpiWarps * kStageBuf;
-constexpr int kNumBars = 3 * kStages + 8 + 1;
+constexpr int kNumBars = 3 * 6 + 8 + 1;
 constexpr int kOffScale = kOffBars + ((kNumBars * 8 + 15) / 16) * 16;  // [2 halves][2 accumulators][kScaleRow] scales of a K block
 constexpr int kScaleRow = kTileM + 4;  // the rows' scales, then the columns' (kGated: gate, up)
 constexpr int kOffMisc = kOffScale + 4 * kScaleRow * 4;
@@ -184,9 +197,11 @@ __device__ __forceinline__ void rotate(uint64_t* run) {
 template <int KIND, int ACT, bool F32, bool MX>
 __global__ void __launch_bounds__(threads_of(MX), 1)
 fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const P8 p) {
+  constexpr int kStages = stages_of(MX), kBBytes = b_bytes_of(MX);
+  constexpr int kOffA = 0, kOffB = kStages * kABytes;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBars);
-  uint64_t* full = bars;                 // [stages] the stage's copies landed           (MMA waits)
+  uint64_t* full = bars;                 // [stages] the stage's copies landed; MX: both CTAs', the leader's counts (MMA waits)
   uint64_t* empty = full + kStages;      // [stages] the MMAs that read it are done       (producer waits)
   // per column half h and accumulator a, at 2 h + a:
   uint64_t* acc_full = empty + kStages;  // [4] a K block's products are in the accumulator, its scales in shared memory (epilogue waits)
@@ -202,11 +217,11 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
-      mbar_init(&sf_full[i], 4);
+      mbar_init(&sf_full[i], 8);  // four warps of each CTA, the leader's counts
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(&acc_full[i], MX ? 1 : 2);  // the MMAs' commit and the half's scale warp
-      mbar_init(&acc_empty[i], MX ? kEpiWarps : kEpiWarps / 2);
+      mbar_init(&acc_empty[i], MX ? 2 * kEpiWarps : kEpiWarps / 2);  // MX: both CTAs' warps, the leader's counts
     }
     mbar_init(drain_bar, 1);
     *s_abort = 0;
@@ -217,12 +232,24 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     prefetch_tensormap(&tm_a);
     prefetch_tensormap(&tm_b);
   }
-  if (warp == kMmaWarp) tmem_alloc(s_tmem, 512);
+  if (warp == kMmaWarp) {
+    if (MX)
+      tmem_alloc_pair(s_tmem, 512);
+    else
+      tmem_alloc(s_tmem, 512);
+  }
   tc_fence_before_sync();
-  __syncthreads();
+  if (MX)
+    cluster_sync_all();  // both CTAs' barriers are initialized and their tensor memory is allocated
+  else
+    __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem_base = *s_tmem;
   const bool ok_start = *s_abort == 0;
+  // MX: a pair of CTAs takes a tile of 256 rows, 128 each
+  const int rank = MX ? static_cast<int>(cluster_ctarank()) : 0;
+  const int pos0 = MX ? static_cast<int>(blockIdx.x >> 1) : static_cast<int>(blockIdx.x);
+  const int stride = MX ? static_cast<int>(gridDim.x >> 1) : static_cast<int>(gridDim.x);
   const int tiles = p.m_tiles * p.n_tiles;
   const int kb_all = p.segs * p.kblocks;
   if (threadIdx.x == 0) pdl_launch_dependents();
@@ -236,7 +263,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       int s = 0, issued = 0;
       uint32_t ph = 0;
       bool ok = true;
-      for (int pos = blockIdx.x; ok && pos < tiles; pos += gridDim.x) {
+      for (int pos = pos0; ok && pos < tiles; pos += stride) {
         int mt, nt;
         tile_of(p, pos, mt, nt);
         for (int i = 0; i < kb_all; ++i) {
@@ -250,10 +277,24 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
             const int k = (i - seg * p.kblocks) * kBlk;
             uint8_t* sa = smem + kOffA + s * kABytes;
             uint8_t* sb = smem + kOffB + s * kBBytes;
-            mbar_arrive_expect_tx(&full[s], kABytes + kBBytes);
-            tma_load_3d(sa, &tm_a, k, mt * kTileM, seg, &full[s]);
             // the columns; kGated: per column half 64 of the gate and the same 64 of the up projection
-            if (KIND == kGated) {
+            if (MX) {
+              const uint32_t bar = map_to_rank(smem_u32(&full[s]), 0);
+              if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * (kABytes + kBBytes));
+              tma_load_3d_pair(sa, &tm_a, k, (2 * mt + rank) * kTileM, seg, bar);
+              if (KIND == kGated) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                  tma_load_3d_pair(sb + h * (kBBytes / 2), &tm_b, k, nt * kBlk + rank * 64, h, bar);
+              } else {
+                tma_load_3d_pair(sb, &tm_b, k, nt * kTileN + rank * kBlk, seg, bar);
+              }
+            } else {
+              mbar_arrive_expect_tx(&full[s], kABytes + kBBytes);
+              tma_load_3d(sa, &tm_a, k, mt * kTileM, seg, &full[s]);
+            }
+            if (MX) {
+            } else if (KIND == kGated) {
 #pragma unroll
               for (int h = 0; h < 4; ++h)
                 tma_load_3d(sb + h * (kBBytes / 4), &tm_b, k, nt * kBlk + (h >> 1) * 64, h & 1, &full[s]);
@@ -269,25 +310,28 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
           }
         }
       }
-      // never leave with copies still in flight
+      // never leave with copies still in flight (MX: the leader's barriers count them; the other CTA sees the stages that it
+      // filled last released by the MMAs that read them)
       for (int i = max(0, issued - kStages); i < issued; ++i) {
+        uint64_t* bar = (rank == 0 ? full : empty) + i % kStages;
         uint32_t spin = 0;
-        while (!mbar_try_wait(&full[i % kStages], (i / kStages) & 1) && ++spin < kSpinLimit) {
+        while (!mbar_try_wait(bar, (i / kStages) & 1) && ++spin < kSpinLimit) {
         }
       }
     }
   } else if (warp == kMmaWarp) {
-    if (ok_start) {
+    if (ok_start && rank == 0) {
       const bool issuer = elect_one();
       const uint64_t adesc0 = umma_desc_k128(smem_u32(smem + kOffA));
       const uint64_t bdesc0 = umma_desc_k128(smem_u32(smem + kOffB));
-      const uint32_t idesc = MX ? umma_idesc_mx_e4m3_e4m3(kTileN, 0, 0) : umma_idesc_e4m3(kTileN);
+      // MX: 256 rows, 128 in each CTA
+      const uint32_t idesc = MX ? umma_idesc_mx_e4m3_e4m3(kTileN, 0, 0) + ((128u >> 4) << 24) : umma_idesc_e4m3(kTileN);
       int s = 0;
       uint32_t ph = 0;
       bool failed = false;
       int count = 0;  // K blocks so far: block c goes to accumulator c % 2
       int tile = 0;
-      for (int pos = blockIdx.x; !failed && pos < tiles; pos += gridDim.x, ++tile) {
+      for (int pos = pos0; !failed && pos < tiles; pos += stride, ++tile) {
         for (int i = 0; i < kb_all; ++i, ++count) {
           const int buf = MX ? 0 : count & 1;
           const uint32_t free_ph = ((count >> 1) - 1) & 1;
@@ -311,9 +355,9 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
               const uint32_t sf = tmem_base + kSfCol0 + 16 * s;
 #pragma unroll
               for (int k = 0; k < kBlk / 32; ++k)
-                umma_mxf8f6f4(d, ad + 2 * k, bd + 2 * k, idesc, sf, sf + 4, (i > 0 || k > 0) ? 1u : 0u);
-              if (i + 1 == kb_all) umma_commit(&acc_full[0]);
-              umma_commit(&empty[s]);
+                umma_mxf8f6f4_pair(d, ad + 2 * k, bd + 2 * k, idesc, sf, sf + 4, (i > 0 || k > 0) ? 1u : 0u);
+              if (i + 1 == kb_all) umma_commit_pair(&acc_full[0]);
+              umma_commit_pair(&empty[s]);
             }
           } else if (issuer) {
 #pragma unroll
@@ -331,7 +375,14 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       }
       if (failed && issuer) raise_error8(p.status, s_abort, kErrMma8);
       // tensor memory is released only when every MMA has completed, also where another role has given up
-      if (issuer) umma_commit(drain_bar);
+      if (issuer) {
+        if (MX)
+          umma_commit_pair(drain_bar);
+        else
+          umma_commit(drain_bar);
+      }
+    }
+    if (ok_start) {  // (MX: in both CTAs, so that neither ends before the commit has arrived at it)
       uint32_t spin = 0;
       while (!mbar_try_wait(drain_bar, 0) && ++spin < kSpinLimit) {
       }
@@ -341,22 +392,22 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     if (ok_start && warp >= kSfWarp0) {
       // ---- block scales (powers of two) as E8M0 bytes, the same for the four blocks of 32 that a K block has: rows l, l + 32,
       // l + 64, l + 96 of the tokens in lane l of four columns, the columns' likewise in eight; every lane quarter of
-      // tensor memory holds a copy, which its warp writes.  Loaded two blocks ahead.
-      constexpr int kAhead = 2;
+      // tensor memory holds a copy, which its warp writes.  Loaded four blocks ahead.
+      constexpr int kAhead = 4;
       pdl_wait();
       int s = 0, issued = 0;
       uint32_t ph = 0;
       bool ok = true;
       const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
-      for (int pos = blockIdx.x; ok && pos < tiles; pos += gridDim.x) {
+      for (int pos = pos0; ok && pos < tiles; pos += stride) {
         int mt, nt;
         tile_of(p, pos, mt, nt);
-        const int m0 = mt * kTileM + lane;
+        const int m0 = (2 * mt + rank) * kTileM + lane;
         const int64_t part = static_cast<int64_t>(p.nblocks) * p.kblocks;
         // kGated: columns 0..63 and 128..191 are the gate's, the others the up projection's
         const float* sb0 = p.sb + static_cast<int64_t>(KIND == kGated ? nt : 2 * nt) * p.kblocks;
         const float* sb1 = KIND == kGated ? sb0 + part : p.sb + static_cast<int64_t>(min(2 * nt + 1, p.nblocks - 1)) * p.kblocks;
-        uint32_t a[kAhead][4], b[kAhead][2];
+        float a[kAhead][4], b[kAhead][2];  // (made bytes when they are used: nothing waits for a load before that)
         auto byte4 = [](float v) { return ((__float_as_uint(v) >> 23) & 0xFFu) * 0x01010101u; };
         const float* sa = p.sa + m0;
         auto fetch = [&](int i, int slot) {  // called for i = 0, 1, 2, ...
@@ -364,10 +415,10 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
             sb0 += part - p.kblocks;
             sb1 += part - p.kblocks;
           }
-          b[slot][0] = byte4(__ldg(sb0++));
-          b[slot][1] = byte4(__ldg(sb1++));
+          b[slot][0] = __ldg(sb0++);
+          b[slot][1] = __ldg(sb1++);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) a[slot][j] = byte4(m0 + 32 * j < p.M ? __ldg(sa + 32 * j) : 1.0f);
+          for (int j = 0; j < 4; ++j) a[slot][j] = m0 + 32 * j < p.M ? __ldg(sa + 32 * j) : 1.0f;
           sa += p.M;
         };
 #pragma unroll
@@ -384,8 +435,8 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
                 ok = false;
               } else {
                 tc_fence_after_sync();
-                const uint32_t t = tmem_base + kSfCol0 + 16 * s + lane_base, b0 = b[u][0], b1 = b[u][1];
-                tmem_st4(t, a[u][0], a[u][1], a[u][2], a[u][3]);
+                const uint32_t t = tmem_base + kSfCol0 + 16 * s + lane_base, b0 = byte4(b[u][0]), b1 = byte4(b[u][1]);
+                tmem_st4(t, byte4(a[u][0]), byte4(a[u][1]), byte4(a[u][2]), byte4(a[u][3]));
                 if (KIND == kGated) {
                   tmem_st4(t + 4, b0, b0, b1, b1);
                   tmem_st4(t + 8, b0, b0, b1, b1);
@@ -396,7 +447,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
                 tmem_st_wait();
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&sf_full[s]);
+                if (lane == 0) mbar_arrive_tmem(&sf_full[s]);
                 if (i + kAhead < kb_all) fetch(i + kAhead, u);
                 ++issued;
                 if (++s == kStages) {
@@ -418,7 +469,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     pdl_wait();
     int count = 0;
     bool ok = true;
-    for (int pos = blockIdx.x; ok && pos < tiles; pos += gridDim.x) {
+    for (int pos = pos0; ok && pos < tiles; pos += stride) {
       int mt, nt;
       tile_of(p, pos, mt, nt);
       const int m0 = mt * kTileM + lane;
@@ -471,12 +522,12 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     bool failed = !ok_start;
     int count = 0;
     pdl_wait();
-    for (int pos = blockIdx.x; pos < tiles; pos += gridDim.x) {
+    for (int pos = pos0; pos < tiles; pos += stride) {
       if (KIND == kGatedBwd) {
         // the checkpoint's codes that this tile's epilogue will read: on their way to L2 while the MMAs run
         int mt, nt;
         tile_of(p, pos, mt, nt);
-        const int m = mt * kTileM + row, n0 = (2 * nt + half) * kBlk;
+        const int m = (MX ? 2 * mt + rank : mt) * kTileM + row, n0 = (2 * nt + half) * kBlk;
         if (m < p.M && n0 < p.N) {
           const uint8_t* g = p.ck + static_cast<int64_t>(m) * p.N + n0;
           const uint8_t* u = g + static_cast<int64_t>(p.M) * p.N;
@@ -499,18 +550,31 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         ++count;
         tc_fence_after_sync();
         if (!failed) {
+          const uint32_t t = tmem_base + half * (kTileN / 2) + lane_base;
+          if (KIND == kGatedBwd) {  // (its registers hold no more than 16 columns in flight; all at once, they spill: 138 for 128 us)
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            float v[16];
-            tmem_ld16(tmem_base + half * (kTileN / 2) + 16 * c + lane_base, v);
-            tmem_ld_wait_regs<16>(v);
+            for (int c = 0; c < 8; ++c) {
+              float v[16];
+              tmem_ld16(t + 16 * c, v);
+              tmem_ld_wait_regs<16>(v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) run[8 * c + e] = pack2(v[2 * e], v[2 * e + 1]);
+              for (int e = 0; e < 8; ++e) run[8 * c + e] = pack2(v[2 * e], v[2 * e + 1]);
+            }
+          } else {
+            float v[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld32(t + 32 * c, v[c]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              tmem_ld_wait32(v[c]);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) run[16 * c + e] = pack2(v[c][2 * e], v[c][2 * e + 1]);
+            }
           }
         }
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0 && !failed) mbar_arrive(&acc_empty[0]);
+        if (lane == 0 && !failed) mbar_arrive_tmem(&acc_empty[0]);
       }
       for (int i = 0; !MX && i < kb_all; ++i, ++count) {
         const int b = 2 * half + (count & 1);
@@ -530,7 +594,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       }
       int mt, nt;
       tile_of(p, pos, mt, nt);
-      const int m0 = mt * kTileM, m = m0 + row;
+      const int m0 = (MX ? 2 * mt + rank : mt) * kTileM, m = m0 + row;
       const bool m_ok = m < p.M;
       const int wm0 = m0 + quarter * 32;
       const int rows = failed ? 0 : min(32, p.M - wm0);  // may be <= 0
@@ -744,10 +808,16 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   }
 
   tc_fence_before_sync();
-  __syncthreads();
+  if (MX)
+    cluster_sync_all();  // both CTAs are done with both CTAs' tensor memory and barriers
+  else
+    __syncthreads();
   if (warp == kMmaWarp) {
     tc_fence_after_sync();
-    tmem_dealloc(tmem_base, 512);
+    if (MX)
+      tmem_dealloc_pair(tmem_base, 512);
+    else
+      tmem_dealloc(tmem_base, 512);
   }
 }
 
@@ -759,9 +829,9 @@ int launch_cfg(const CUtensorMap& ta, const CUtensorMap& tb, const P8& p, cudaSt
     attr = cudaFuncSetAttribute(fp8_block_gemm_kernel<KIND, ACT, F32, MX>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   });
   if (attr != cudaSuccess) return ZQ_ERR_CUDA;
-  const int tiles = p.m_tiles * p.n_tiles;
-  const unsigned grid = static_cast<unsigned>(tiles < sm_count() ? tiles : sm_count());
-  const cudaError_t e = launch_chained(fp8_block_gemm_kernel<KIND, ACT, F32, MX>, dim3(grid), dim3(threads_of(MX)), kSmemBytes, st, false,
+  const int tiles = p.m_tiles * p.n_tiles, slots = MX ? sm_count() / 2 : sm_count();
+  const unsigned grid = (MX ? 2u : 1u) * static_cast<unsigned>(tiles < slots ? tiles : slots);
+  const cudaError_t e = launch_clustered(fp8_block_gemm_kernel<KIND, ACT, F32, MX>, dim3(grid), dim3(threads_of(MX)), kSmemBytes, st, MX ? 2 : 1,
                                        ta, tb, p);
   count_launch();
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
@@ -788,9 +858,17 @@ int launch_block_gemm(const GemmArgs8& a, cudaStream_t st) {
   p.kblocks = static_cast<int>(blocks_of(a.K));
   p.segs = a.kind == kPlain ? a.parts : 1;
   p.nblocks = static_cast<int>(blocks_of(a.N));
-  p.m_tiles = static_cast<int>((a.M + kTileM - 1) / kTileM);
   p.n_tiles = a.kind == kGated ? p.nblocks : static_cast<int>((a.N + kTileN - 1) / kTileN);
-  p.m_group = 16;
+  // FP32 results keep the promotion: the tensor core rounds its running sum towards zero, about 1e-8 of it per block.  A
+  // round of tiles takes the pairs 3/4 of the single CTAs' time, but the last pair of an odd number of token tiles has an idle
+  // half.  Measured, us, single CTAs / pairs: 128 tokens, 7168 -> 28672 (1 and 2 rounds) 44 / 54; 384 tokens, 4096 -> 11008 (1 and
+  // 2) 21 / 27; 256 tokens (1 and 1) 20.7 / 16.6; 1024 tokens, 4096 -> 4096 (1 and 1) 20.6 / 17.3; 640 tokens (2 and 2) 38.6 / 29.4.
+  const int64_t mt1 = (a.M + kTileM - 1) / kTileM, mt2 = (mt1 + 1) / 2;
+  const int64_t rounds1 = (mt1 * p.n_tiles + sm_count() - 1) / sm_count();
+  const int64_t rounds2 = (mt2 * p.n_tiles + sm_count() / 2 - 1) / (sm_count() / 2);
+  const bool mx = a.pow2_scales && a.ydt != ZQ_OUT_F32 && 3 * rounds2 <= 4 * rounds1;
+  p.m_tiles = static_cast<int>(mx ? mt2 : mt1);
+  p.m_group = mx ? 8 : 16;
   const int64_t tiles = static_cast<int64_t>(p.m_tiles) * p.n_tiles;
   if (tiles > 0x3FFFFFFF) return ZQ_ERR_SHAPE;
   p.sa = a.sa;
@@ -807,10 +885,8 @@ int launch_block_gemm(const GemmArgs8& a, cudaStream_t st) {
   CUtensorMap ta, tb;
   if (!make_code_map(&ta, a.a, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.M), static_cast<uint64_t>(p.segs), kTileM) ||
       !make_code_map(&tb, a.b, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.N),
-                     a.kind == kGated ? 2u : static_cast<uint64_t>(p.segs), a.kind == kGated ? 64 : kTileN))
+                     a.kind == kGated ? 2u : static_cast<uint64_t>(p.segs), a.kind == kGated ? 64 : (mx ? kBlk : kTileN)))
     return ZQ_ERR_CUDA;
-  // FP32 results keep the promotion: the tensor core rounds its running sum towards zero, about 1e-8 of it per block
-  const bool mx = a.pow2_scales && a.ydt != ZQ_OUT_F32;
   if (a.kind == kGated) return launch_act<kGated>(a.act, mx, ta, tb, p, st);
   if (a.kind == kGatedBwd) return launch_act<kGatedBwd>(a.act, mx, ta, tb, p, st);
   return a.ydt == ZQ_OUT_F32 ? launch_cfg<kPlain, ZQ_ACT_RELU, true, false>(ta, tb, p, st)

@@ -214,3 +214,34 @@ def test_ref_activation_derivative(kind):
     e = 1e-6
     fd = (R.act(v + e, kind)[0] - R.act(v - e, kind)[0]) / (2 * e)
     assert np.abs(fd - R.act(v, kind)[1]).max() < 1e-8
+
+
+def test_promise_of_powers_of_two(L):
+    """Where the promise may be made, and where it is refused."""
+    P2 = binding.SCALES_POW2
+    assert L.zq_quantize_fp8_block(P, 4, 64, 64, M1 | P2, P, P, None) == ERR_MODE      # nothing is given that has scales
+    assert L.zq_quantize_weight_fp8_block(P, 4, 64, M1 | P2, P, P, None) == ERR_MODE
+    ws = binding.fp8_block_linear_workspace_bytes(4, 8, 64)
+
+    def call(mode, q=P, s=P, x=NULL, ldx=0, work=P, nws=ws):
+        return L.zq_fp8_block_linear(q, s, x, ldx, mode, 1, 4, 8, 64, P, P, P, 0, 8, work, nws, None)
+
+    raw = dict(q=NULL, s=NULL, x=P, ldx=64)
+    assert call(M2 | P2) == ERR_MODE and call(P2 << 1) == ERR_MODE and call(-1) == ERR_MODE
+    assert call(NONE | P2, **raw) == ERR_MODE                      # the call's own scales would not be powers of two
+    # accepted as far as the mode goes: the next check answers
+    assert call(M1 | P2, **raw, work=NULL) in (ERR_NULL, ERR_WS) and call(NONE | P2, work=NULL) in (ERR_NULL, ERR_WS)
+
+
+def test_promise_of_the_binding():
+    """The binding promises what it knows: of a weight on the CPU nothing."""
+    codes = torch.zeros((128, 128), dtype=torch.uint8)
+    assert binding.Fp8Weight(codes, torch.ones((1, 1)), 128, 128).pow2 is False
+    w = binding.Fp8Weight(codes, torch.ones((1, 1)), 128, 128, pow2=True)
+    assert binding._scales("M1", w, None) == M1 | binding.SCALES_POW2 and binding._scales("none", w, None) == NONE
+    q = binding.Fp8Block(codes, torch.ones((1, 128)))
+    assert binding._scales("M1", w, q) == M1                       # given activations of unknown scales
+    q.pow2 = True
+    assert binding._scales("none", w, q) == NONE | binding.SCALES_POW2
+    w.pow2 = False
+    assert binding._scales("M1", w, q) == M1
