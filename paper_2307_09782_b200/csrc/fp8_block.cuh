@@ -138,30 +138,70 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 __device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 // The activations.  SiLU and the tanh form of GELU are both v * sigmoid(w(v)), with w = v and
-// w = 2 sqrt(2 / pi) (v + 0.044715 v^3), since (1 + tanh z) / 2 = sigmoid(2 z).  1 / (1 + exp(-w)) with the fast
-// exponential and division is good to about 1e-6 relative: 2^-13 of a bf16 rounding step.
+// w = 2 sqrt(2 / pi) (v + 0.044715 v^3), since (1 + tanh z) / 2 = sigmoid(2 z).  1 / (1 + 2^(-w / ln 2)) with the special
+// function unit's power of two and reciprocal is good to about 1e-6 relative: 2^-13 of a bf16 rounding step.  A power that
+// overflows gives 0, one that underflows 1, a NaN stays one.
+__device__ __forceinline__ float sfu_ex2(float v) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float sfu_rcp(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+constexpr float kSiluC = -1.4426950408889634f;                        // -1 / ln 2
+constexpr float kGeluC = -1.4426950408889634f * 1.5957691216057308f;  // times 2 sqrt(2 / pi)
 template <int ACT>
 __device__ __forceinline__ float act_sigmoid(float v) {
-  const float w = ACT == ZQ_ACT_SILU ? v : 1.5957691216057308f * v * fmaf(0.044715f * v, v, 1.0f);
-  return __fdividef(1.0f, 1.0f + __expf(-w));
+  const float t = ACT == ZQ_ACT_SILU ? kSiluC * v : v * fmaf(kGeluC * 0.044715f, v * v, kGeluC);
+  return sfu_rcp(1.0f + sfu_ex2(t));
 }
 template <int ACT>
 __device__ __forceinline__ float act_value(float v) {
   if (ACT == ZQ_ACT_RELU) return v < 0.0f ? 0.0f : v;  // keeps NaN
   return v * act_sigmoid<ACT>(v);
 }
+__device__ __forceinline__ uint64_t twice(float v) { return pack2(v, v); }
+// Two values at a time: packed arithmetic (one instruction for both), the special function unit for each.
+template <int ACT>
+__device__ __forceinline__ uint64_t act_sigmoid2(uint64_t v, uint64_t v2) {  // v2: v^2 (GELU)
+  const uint64_t t = ACT == ZQ_ACT_SILU ? mul2(v, twice(kSiluC)) : mul2(v, fma2(v2, twice(kGeluC * 0.044715f), twice(kGeluC)));
+  float t0, t1;
+  unpack2(t, t0, t1);
+  unpack2(fma2(pack2(sfu_ex2(t0), sfu_ex2(t1)), twice(1.0f), twice(1.0f)), t0, t1);
+  return pack2(sfu_rcp(t0), sfu_rcp(t1));
+}
 // value and derivative: v p and p + v p (1 - p) w'
 template <int ACT>
-__device__ __forceinline__ void act_both(float v, float& value, float& slope) {
+__device__ __forceinline__ void act_both2(uint64_t v, uint64_t& value, uint64_t& slope) {
   if (ACT == ZQ_ACT_RELU) {
-    value = v < 0.0f ? 0.0f : v;
-    slope = v > 0.0f ? 1.0f : 0.0f;
+    float a, b;
+    unpack2(v, a, b);
+    value = pack2(act_value<ACT>(a), act_value<ACT>(b));
+    slope = pack2(a > 0.0f ? 1.0f : 0.0f, b > 0.0f ? 1.0f : 0.0f);
     return;
   }
-  const float p = act_sigmoid<ACT>(v);
-  const float dw = ACT == ZQ_ACT_SILU ? 1.0f : 1.5957691216057308f * fmaf(0.134145f * v, v, 1.0f);
-  value = v * p;
-  slope = fmaf(value * (1.0f - p), dw, p);
+  uint64_t v2 = 0ull;
+  if (ACT == ZQ_ACT_GELU_TANH) {  // from |v| = 100 on p is 0 or 1 and (1 - p) or v p zero: v^2 must not overflow beside them
+    float a, b;
+    unpack2(mul2(v, v), a, b);
+    v2 = pack2(fminf(a, 1e4f), fminf(b, 1e4f));
+  }
+  const uint64_t p = act_sigmoid2<ACT>(v, v2);
+  value = mul2(v, p);
+  const uint64_t q = fma2(p, twice(-1.0f), twice(1.0f));
+  if (ACT == ZQ_ACT_SILU)
+    slope = fma2(value, q, p);
+  else
+    slope = fma2(mul2(value, q), fma2(v2, twice(1.5957691216057308f * 0.134145f), twice(1.5957691216057308f)), p);
+}
+// Larger of two pairs of 16-bit unsigned numbers.
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
 }
 
 // Registers per thread from here on, for a whole warpgroup (each warp of it executes one of these).

@@ -25,8 +25,8 @@
 // the sums in registers, runs behind the next tile's MMAs.  A K block's scale stands for the four blocks of 32 that the MMA
 // has in it; four warps write the bytes straight into tensor memory (tcgen05.st), stage by stage: no second operand
 // format.  A pair of CTAs takes 256 tokens x 256 columns, so that a CTA loads half of the columns and has six stages.
-// Measured, us, promotion -> MX (2048 tokens unless said): product 4096 -> 11008 93 -> 68; 8192 tokens 7168 -> 28672 1640 -> 1230
-// (2.7 PFLOP/s); gated layer 4096 -> 11008 191 -> 145; gradient 176 -> 128, its epilogue bound.  What the steps gave, on the
+// Measured, us, promotion -> MX (2048 tokens unless said): product 4096 -> 11008 93 -> 68; 8192 tokens 7168 -> 28672 1640 -> 1220
+// (2.7 PFLOP/s); gated layer 4096 -> 11008 191 -> 145; gradient 170 -> 124, its epilogue bound.  What the steps gave, on the
 // product: single CTAs 86; pairs 84; scales loaded four K blocks ahead and made bytes only when used 73 (with two ahead, the
 // loads' latency set the pace); sums out of tensor memory with one wait 68.
 // What bounds MX: at 2.7 PFLOP/s and the clock that the power cap leaves (1.6 - 1.7 GHz) the MMAs run about 2/3 of the time.
@@ -551,7 +551,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         tc_fence_after_sync();
         if (!failed) {
           const uint32_t t = tmem_base + half * (kTileN / 2) + lane_base;
-          if (KIND == kGatedBwd) {  // (its registers hold no more than 16 columns in flight; all at once, they spill: 138 for 128 us)
+          if (KIND == kGatedBwd) {  // (its registers hold no more than 16 columns in flight; all at once, they spill: 138 us for 128)
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
               float v[16];
@@ -744,21 +744,25 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
           for (int it = 0; it < 8; ++it) {
             const int r = it * 4 + rr;
             const uint4 dv = stage_get(buf, r, cc);
-            const float d[4] = {__uint_as_float(dv.x), __uint_as_float(dv.y), __uint_as_float(dv.z), __uint_as_float(dv.w)};
-            const float g_s = __shfl_sync(0xFFFFFFFFu, sg, r), u_s = __shfl_sync(0xFFFFFFFFu, su, r);
+            const uint64_t d[2] = {pack2(__uint_as_float(dv.x), __uint_as_float(dv.y)),
+                                   pack2(__uint_as_float(dv.z), __uint_as_float(dv.w))};
+            const uint64_t g_s = twice(__shfl_sync(0xFFFFFFFFu, sg, r)), u_s = twice(__shfl_sync(0xFFFFFFFFu, su, r));
             uint32_t dg[2], du[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const float2 gv = decode2(static_cast<uint16_t>(gc[it] >> (16 * e)));
               const float2 vv = decode2(static_cast<uint16_t>(uc[it] >> (16 * e)));
-              float a0, a1, b0, b1;
-              act_both<ACT>(gv.x * g_s, a0, b0);
-              act_both<ACT>(gv.y * g_s, a1, b1);
-              dg[e] = pack_bf16(d[2 * e] * (vv.x * u_s) * b0, d[2 * e + 1] * (vv.y * u_s) * b1);
-              du[e] = pack_bf16(d[2 * e] * a0, d[2 * e + 1] * a1);
-              ag[it] = max(ag[it], max((dg[e] << 16) & 0x7FFF0000u, dg[e] & 0x7FFF0000u));
-              au[it] = max(au[it], max((du[e] << 16) & 0x7FFF0000u, du[e] & 0x7FFF0000u));
+              uint64_t a, b;
+              act_both2<ACT>(mul2(pack2(gv.x, gv.y), g_s), a, b);
+              float x0, x1;
+              unpack2(mul2(mul2(d[e], mul2(pack2(vv.x, vv.y), u_s)), b), x0, x1);
+              dg[e] = pack_bf16(x0, x1);
+              unpack2(mul2(d[e], a), x0, x1);
+              du[e] = pack_bf16(x0, x1);
             }
+            // (absolute values of bf16 numbers order like their bits)
+            ag[it] = max_u16x2(ag[it], max_u16x2(dg[0] & 0x7FFF7FFFu, dg[1] & 0x7FFF7FFFu));
+            au[it] = max_u16x2(au[it], max_u16x2(du[0] & 0x7FFF7FFFu, du[1] & 0x7FFF7FFFu));
             run[2 * it] = (static_cast<uint64_t>(dg[1]) << 32) | dg[0];
             run[2 * it + 1] = (static_cast<uint64_t>(du[1]) << 32) | du[0];
             if (r < rows && 32 * c + 4 * cc < cols) {
@@ -774,9 +778,11 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         for (int it = 0; it < 8; ++it) {
 #pragma unroll
           for (int o = 4; o; o >>= 1) {
-            ag[it] = max(ag[it], __shfl_xor_sync(0xFFFFFFFFu, ag[it], o));
-            au[it] = max(au[it], __shfl_xor_sync(0xFFFFFFFFu, au[it], o));
+            ag[it] = max_u16x2(ag[it], __shfl_xor_sync(0xFFFFFFFFu, ag[it], o));
+            au[it] = max_u16x2(au[it], __shfl_xor_sync(0xFFFFFFFFu, au[it], o));
           }
+          ag[it] = max(ag[it] << 16, ag[it] & 0xFFFF0000u);
+          au[it] = max(au[it] << 16, au[it] & 0xFFFF0000u);
           const int r = it * 4 + rr;
           const float scg = block_scale(ag[it], p.pow2 != 0), scu = block_scale(au[it], p.pow2 != 0);
           if (any && r < rows && cc == 0) {

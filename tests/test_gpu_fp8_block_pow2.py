@@ -149,3 +149,25 @@ def test_gated_and_backward(M, K, F, kind):
     for i in (0, 1):
         q = binding.quantize_fp8_block(d[i], "M1")
         assert torch.equal(q.codes, dq.codes[i]) and torch.equal(q.scale, dq.scale[i])
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu_tanh", "relu"])
+@pytest.mark.parametrize("M,mode", [(5, "none"), (5, "M1"), (150, "M1")])
+def test_gradient_far_out(M, mode, kind):
+    """Far from zero the derivative is 0 or 1, also where the square of the argument overflows."""
+    K, F = 144, 272
+    rng = np.random.default_rng(M)
+    dy = R.bf16(rng.standard_normal((M, K)) * 0.01)
+    g, u = R.bf16(rng.standard_normal((M, F)) * 200), R.bf16(rng.standard_normal((M, F)))
+    g[0], g[1], g[2, :128], g[2, 128:] = 1e20, -1e20, 90.0, -3e36
+    wt, (wv,) = weight(F, F, K, mode)
+    gq, uq = (binding.quantize_fp8_block(bf16_tensor(v), mode) for v in (g, u))
+    gu = binding.Fp8Block(torch.stack([gq.codes, uq.codes]), torch.stack([gq.scale, uq.scale]))
+    d, _ = binding.fp8_gated_linear_backward(wt, gu, dy=bf16_tensor(dy), act=kind, mode=mode)
+    dyv = R.rows_values(*R.quantize_rows(dy, mode))
+    dh, t = dyv @ wv.T, (134 + 2 * blocks(K)) * 2.0 ** -23 * (np.abs(dyv) @ np.abs(wv).T)
+    gv, uv = quantized_values(gu, 0), quantized_values(gu, 1)
+    a, da = R.act(gv, kind)
+    ea = 2.0 ** -18 * np.maximum(1.0, np.abs(gv))
+    check_values(d[0], dh * uv * da, t * np.abs(uv * da) + (np.abs(dh) + t) * np.abs(uv) * ea, True)
+    check_values(d[1], dh * a, t * np.abs(a) + (np.abs(dh) + t) * ea, True)
