@@ -26,7 +26,7 @@
 // has in it; four warps write the bytes straight into tensor memory (tcgen05.st), stage by stage: no second operand
 // format.  A pair of CTAs takes 256 tokens x 256 columns, so that a CTA loads half of the columns and has six stages.
 // Measured, us, promotion -> MX (2048 tokens unless said): product 4096 -> 11008 93 -> 68; 8192 tokens 7168 -> 28672 1640 -> 1220
-// (2.7 PFLOP/s); gated layer 4096 -> 11008 191 -> 145; gradient 170 -> 124, its epilogue bound.  What the steps gave, on the
+// (2.7 PFLOP/s); gated layer 4096 -> 11008 191 -> 145; gradient 170 -> 121, its epilogue bound.  What the steps gave, on the
 // product: single CTAs 86; pairs 84; scales loaded four K blocks ahead and made bytes only when used 73 (with two ahead, the
 // loads' latency set the pace); sums out of tensor memory with one wait 68.
 // What bounds MX: at 2.7 PFLOP/s and the clock that the power cap leaves (1.6 - 1.7 GHz) the MMAs run about 2/3 of the time.
@@ -703,9 +703,6 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         const int rr = lane >> 3, cc = lane & 7;  // rows rr, rr + 4, ...; columns 4 cc .. 4 cc + 3 of the 32
         const uint8_t* ck = p.ck + static_cast<int64_t>(wm0) * p.N + n0 + 4 * cc;
         uint8_t* yd = static_cast<uint8_t*>(p.y) + (static_cast<int64_t>(wm0) * p.N + n0 + 4 * cc) * 2;
-        uint32_t ag[8], au[8];
-#pragma unroll
-        for (int it = 0; it < 8; ++it) ag[it] = au[it] = 0u;
         // the next 32 columns' codes, on their way while these are worked on (MX: the MMAs do not wait for this epilogue, and
         // its warps have no registers to spare)
         uint32_t gn[8], un[8];
@@ -760,38 +757,53 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
               unpack2(mul2(d[e], a), x0, x1);
               du[e] = pack_bf16(x0, x1);
             }
-            // (absolute values of bf16 numbers order like their bits)
-            ag[it] = max_u16x2(ag[it], max_u16x2(dg[0] & 0x7FFF7FFFu, dg[1] & 0x7FFF7FFFu));
-            au[it] = max_u16x2(au[it], max_u16x2(du[0] & 0x7FFF7FFFu, du[1] & 0x7FFF7FFFu));
             run[2 * it] = (static_cast<uint64_t>(dg[1]) << 32) | dg[0];
             run[2 * it + 1] = (static_cast<uint64_t>(du[1]) << 32) | du[0];
             if (r < rows && 32 * c + 4 * cc < cols) {
               uint8_t* yr = yd + (static_cast<int64_t>(r) * p.N + 32 * c) * 2;
-              *reinterpret_cast<uint2*>(yr) = make_uint2(dg[0], dg[1]);
-              *reinterpret_cast<uint2*>(yr + MN * 2) = make_uint2(du[0], du[1]);
+              *reinterpret_cast<uint64_t*>(yr) = run[2 * it];
+              *reinterpret_cast<uint64_t*>(yr + MN * 2) = run[2 * it + 1];
             }
           }
           rotate<16>(run);
         }
+        // The rows' maxima, from the finished pairs (kept up to date in the loop above they would be more registers than it
+        // has): of bf16 numbers, whose absolute values order like their bits, g's in the lower half of a word, u's in the upper.
+        uint32_t top[8];
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+          uint32_t ag = 0u, au = 0u;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const uint64_t vg = run[16 * c + 2 * it], vu = run[16 * c + 2 * it + 1];
+            ag = max_u16x2(ag, max_u16x2(static_cast<uint32_t>(vg) & 0x7FFF7FFFu, static_cast<uint32_t>(vg >> 32) & 0x7FFF7FFFu));
+            au = max_u16x2(au, max_u16x2(static_cast<uint32_t>(vu) & 0x7FFF7FFFu, static_cast<uint32_t>(vu >> 32) & 0x7FFF7FFFu));
+          }
+          top[it] = max_u16x2(__byte_perm(ag, au, 0x5410), __byte_perm(ag, au, 0x7632));
+        }
+        // over the eight lanes of a row: each exchange halves the rows that a lane still has, until lane cc has row 4 cc + rr,
+        // whose two scales it computes and hands round
+#pragma unroll
+        for (int o = 4; o; o >>= 1) {
+          const bool upper = (cc & o) != 0;
+#pragma unroll
+          for (int e = 0; e < o; ++e) {
+            const uint32_t give = upper ? top[e] : top[e + o], keep = upper ? top[e + o] : top[e];
+            top[e] = max_u16x2(keep, __shfl_xor_sync(0xFFFFFFFFu, give, o));
+          }
+        }
+        const float scg = block_scale(top[0] << 16, p.pow2 != 0), scu = block_scale(top[0] & 0xFFFF0000u, p.pow2 != 0);
+        if (any && 4 * cc + rr < rows) {
+          float* sd = p.s + static_cast<int64_t>(fb) * p.M + wm0 + 4 * cc + rr;
+          sd[0] = scg;
+          sd[SM] = scu;
+        }
+        const float invg = block_inv(scg), invu = block_inv(scu);
         float ig[8], iu[8];
 #pragma unroll
         for (int it = 0; it < 8; ++it) {
-#pragma unroll
-          for (int o = 4; o; o >>= 1) {
-            ag[it] = max_u16x2(ag[it], __shfl_xor_sync(0xFFFFFFFFu, ag[it], o));
-            au[it] = max_u16x2(au[it], __shfl_xor_sync(0xFFFFFFFFu, au[it], o));
-          }
-          ag[it] = max(ag[it] << 16, ag[it] & 0xFFFF0000u);
-          au[it] = max(au[it] << 16, au[it] & 0xFFFF0000u);
-          const int r = it * 4 + rr;
-          const float scg = block_scale(ag[it], p.pow2 != 0), scu = block_scale(au[it], p.pow2 != 0);
-          if (any && r < rows && cc == 0) {
-            float* sd = p.s + static_cast<int64_t>(fb) * p.M + wm0 + r;
-            sd[0] = scg;
-            sd[SM] = scu;
-          }
-          ig[it] = block_inv(scg);
-          iu[it] = block_inv(scu);
+          ig[it] = __shfl_sync(0xFFFFFFFFu, invg, 8 * rr + it);
+          iu[it] = __shfl_sync(0xFFFFFFFFu, invu, 8 * rr + it);
         }
         uint8_t* qd = p.q + static_cast<int64_t>(wm0) * p.N + n0 + 4 * cc;
 #pragma unroll 1
@@ -799,12 +811,14 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
 #pragma unroll
           for (int it = 0; it < 8; ++it) {
             const int r = it * 4 + rr;
+            const uint32_t g0 = static_cast<uint32_t>(run[2 * it]), g1 = static_cast<uint32_t>(run[2 * it] >> 32);
+            const uint32_t u0 = static_cast<uint32_t>(run[2 * it + 1]), u1 = static_cast<uint32_t>(run[2 * it + 1] >> 32);
+            const uint32_t qg = cast4(bf16_lo(g0), bf16_hi(g0), bf16_lo(g1), bf16_hi(g1), ig[it]);
+            const uint32_t qu = cast4(bf16_lo(u0), bf16_hi(u0), bf16_lo(u1), bf16_hi(u1), iu[it]);
             if (r < rows && 32 * c + 4 * cc < cols) {
-              const uint32_t g0 = static_cast<uint32_t>(run[2 * it]), g1 = static_cast<uint32_t>(run[2 * it] >> 32);
-              const uint32_t u0 = static_cast<uint32_t>(run[2 * it + 1]), u1 = static_cast<uint32_t>(run[2 * it + 1] >> 32);
               uint8_t* qr = qd + static_cast<int64_t>(r) * p.N + 32 * c;
-              *reinterpret_cast<uint32_t*>(qr) = cast4(bf16_lo(g0), bf16_hi(g0), bf16_lo(g1), bf16_hi(g1), ig[it]);
-              *reinterpret_cast<uint32_t*>(qr + MN) = cast4(bf16_lo(u0), bf16_hi(u0), bf16_lo(u1), bf16_hi(u1), iu[it]);
+              *reinterpret_cast<uint32_t*>(qr) = qg;
+              *reinterpret_cast<uint32_t*>(qr + MN) = qu;
             }
           }
           rotate<16>(run);
