@@ -423,6 +423,15 @@ def _blocks(n: int) -> int:
     return (n + 127) // 128
 
 
+def _out_type(dtype) -> int:
+    """The library's name for a result type.  Any other type would be written as bf16: wrong bits, or beyond its end."""
+    if dtype is torch.bfloat16:
+        return OUT_BF16
+    if dtype is torch.float32:
+        return OUT_F32
+    raise ValueError(f"out_dtype: torch.float32 or torch.bfloat16 is needed, got {dtype}")
+
+
 def quantize_fp8_block(x: torch.Tensor, mode="none") -> Fp8Block:
     """x: bf16 [M, K] (row stride allowed); ``mode`` "none" (FP32 scales) or "M1" (powers of two)."""
     ldx = _rows(x, "x")
@@ -514,13 +523,13 @@ def fp8_block_linear(w: Fp8Weight, *, x=None, q: Optional[Fp8Block] = None, mode
                      workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y [M, N] = the linear layer; activations raw (bf16 ``x``, quantized with ``mode``) or quantized (``q``).  With
     ``w.parts`` = 2 the sum over two pairs of operands (``q`` then holds two as well)."""
+    ydt = _out_type(out_dtype if y is None else y.dtype)
     codes, scale, x, ldx, M = _activations(x, q, w.K, w.parts)
     _on_gpu(w.codes, w.scale)
     if y is None:
         y = w.scale.new_empty((M, w.N), dtype=out_dtype)
-    elif y.shape != (M, w.N) or y.dtype not in (torch.float32, torch.bfloat16) or (w.N > 1 and y.stride(1) != 1):
-        raise ValueError(f"y: a float32 or bf16 [{M}, {w.N}] matrix with contiguous rows is needed")
-    ydt = OUT_F32 if y.dtype == torch.float32 else OUT_BF16
+    elif y.shape != (M, w.N) or (w.N > 1 and y.stride(1) != 1):
+        raise ValueError(f"y: a [{M}, {w.N}] matrix with contiguous rows is needed")
     if workspace is None:
         workspace = _fp8_workspace(None, M, w.K, w.codes.device)
     _on_gpu(y, workspace)
@@ -588,6 +597,7 @@ def fp8_weight_grad(g: torch.Tensor, q: Fp8Block, *, out_dtype=torch.float32,
                     workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dW = g^T x^ with the checkpoint ``q`` of x.  g: bf16 [M, N] (row stride allowed) -> [N, K]; or contiguous
     [parts, M, N] -> [parts, N, K]."""
+    dwdt = _out_type(out_dtype)
     parts = g.shape[0] if g.dim() == 3 else 1
     g0 = g[0] if g.dim() == 3 else g
     ldg = _rows(g0, "g")
@@ -601,8 +611,7 @@ def fp8_weight_grad(g: torch.Tensor, q: Fp8Block, *, out_dtype=torch.float32,
     if workspace is None:
         workspace = _fp8_workspace(None, 0, 16, g.device)
     _check(lib().zq_fp8_weight_grad(_ptr(g), ldg, g.stride(0) if g.dim() == 3 else 0, parts, _ptr(codes), _ptr(scale),
-                                    M, N, K, _ptr(dw), OUT_F32 if out_dtype == torch.float32 else OUT_BF16,
-                                    _ptr(workspace), workspace.numel(), _stream()), "zq_fp8_weight_grad")
+                                    M, N, K, _ptr(dw), dwdt, _ptr(workspace), workspace.numel(), _stream()), "zq_fp8_weight_grad")
     return dw
 
 
@@ -618,6 +627,7 @@ def fp8_gated_ffn(gate_up: Fp8Weight, down: Fp8Weight, x: torch.Tensor, *, act="
                   out_dtype=torch.bfloat16, save=False, workspace: torch.Tensor):
     """The gated feed-forward block in one call: y = (act(x Wg^T) * (x Wu^T)) Wd^T.  With ``save`` returns (y, the uint8
     buffer that :func:`fp8_gated_ffn_backward` reads), else y."""
+    ydt = _out_type(out_dtype)
     ldx = _rows(x, "x")
     M, K = x.shape
     F, N = gate_up.N, down.N
@@ -629,7 +639,7 @@ def fp8_gated_ffn(gate_up: Fp8Weight, down: Fp8Weight, x: torch.Tensor, *, act="
     saved = torch.empty((fp8_gated_ffn_saved_bytes(M, K, F),), dtype=torch.uint8, device=x.device) if save else None
     _check(lib().zq_fp8_gated_ffn(x.data_ptr(), ldx, _scales(mode, gate_up, None) if down.pow2 else _mode(mode), M, K, F, N, gate_up.codes.data_ptr(),
                                   gate_up.scale.data_ptr(), down.codes.data_ptr(), down.scale.data_ptr(), _act(act),
-                                  y.data_ptr(), OUT_F32 if out_dtype == torch.float32 else OUT_BF16, N, _ptr(saved),
+                                  y.data_ptr(), ydt, N, _ptr(saved),
                                   workspace.data_ptr(), workspace.numel(), _stream()), "zq_fp8_gated_ffn")
     return (y, saved) if save else y
 
@@ -638,6 +648,7 @@ def fp8_gated_ffn_backward(gate_up_t: Fp8Weight, down_t: Fp8Weight, dy: torch.Te
                            mode="none", out_dtype=torch.bfloat16, workspace: torch.Tensor):
     """(dx [M, K], dW of (gate, up) [2, F, K], dW of down [N, F]) from dy bf16 [M, N], the transposed weights and what
     :func:`fp8_gated_ffn` saved."""
+    dt = _out_type(out_dtype)
     lddy = _rows(dy, "dy")
     M, N = dy.shape
     F, K = down_t.N, gate_up_t.N
@@ -657,6 +668,6 @@ def fp8_gated_ffn_backward(gate_up_t: Fp8Weight, down_t: Fp8Weight, dy: torch.Te
                                            gate_up_t.codes.data_ptr(), gate_up_t.scale.data_ptr(),
                                            down_t.codes.data_ptr(), down_t.scale.data_ptr(), _act(act), dx.data_ptr(),
                                            dwgu.data_ptr(), dwd.data_ptr(),
-                                           OUT_F32 if out_dtype == torch.float32 else OUT_BF16, workspace.data_ptr(),
+                                           dt, workspace.data_ptr(),
                                            workspace.numel(), _stream()), "zq_fp8_gated_ffn_backward")
     return dx, dwgu, dwd

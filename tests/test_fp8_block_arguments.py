@@ -1,0 +1,50 @@
+"""Arguments that the binding of the FP8 operators must refuse, or look after, before anything is launched (no GPU needed)."""
+import pytest
+import torch
+
+import __graft_entry__ as entry
+from paper_2307_09782_b200 import binding, gated_ffn
+
+u8, f32, bf = torch.uint8, torch.float32, torch.bfloat16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def L():
+    entry.build()
+    return binding.lib()
+
+
+def weight(N, K, parts=1, **kw):
+    lead = (parts,) if parts > 1 else ()
+    nb, kb = (N + 127) // 128, (K + 127) // 128
+    return binding.Fp8Weight(torch.zeros((*lead, N, K), dtype=u8), torch.ones((*lead, nb, kb)), N, K, parts, **kw)
+
+
+# ---- result types ----------------------------------------------------------------------------------------------------
+OTHER_TYPES = [torch.float16, torch.float64, torch.uint8, torch.float8_e4m3fn, torch.int32]
+
+
+@pytest.mark.parametrize("dtype", OTHER_TYPES)
+def test_result_types(dtype):
+    """The library writes FP32 or bf16: into a tensor of another type it would write wrong bits, or beyond its end."""
+    x = torch.zeros((4, 64), dtype=bf)
+    work = torch.zeros(256, dtype=u8)
+    gu, down = weight(32, 64, 2), weight(64, 32)
+    gut, dnt = weight(64, 32, 2), weight(32, 64)
+    saved = torch.zeros(binding.fp8_gated_ffn_saved_bytes(4, 64, 32), dtype=u8)
+    ffn = gated_ffn.GatedFfnFp8(gu, down)
+    ffn.gate_up_t, ffn.down_t = gut, dnt
+    ffn.workspace = lambda M: work
+    calls = [lambda: binding.fp8_block_linear(weight(32, 64), x=x, out_dtype=dtype, workspace=work),
+             lambda: binding.fp8_block_linear(weight(32, 64), x=x, y=torch.zeros((4, 32)).to(dtype), workspace=work),
+             lambda: binding.fp8_weight_grad(torch.zeros((4, 8), dtype=bf), binding.Fp8Block(torch.zeros((4, 64), dtype=u8),
+                                                                                             torch.ones((1, 4))),
+                                             out_dtype=dtype, workspace=work),
+             lambda: binding.fp8_gated_ffn(gu, down, x, out_dtype=dtype, workspace=work),
+             lambda: binding.fp8_gated_ffn_backward(gut, dnt, x, saved, out_dtype=dtype, workspace=work),
+             lambda: ffn.forward(x, out_dtype=dtype), lambda: ffn.forward_train(x, out_dtype=dtype),
+             lambda: ffn.backward(x, saved, out_dtype=dtype)]
+    for i, call in enumerate(calls):
+        with pytest.raises(ValueError, match="out_dtype"):
+            call()
+            pytest.fail(str(i))
