@@ -165,6 +165,15 @@ def _check(status: int, where: str):
         raise ZqError(status, where)
 
 
+def _out_type(dtype) -> int:
+    """The library's name for a result type.  Any other type would be written as bf16: wrong bits, or beyond its end."""
+    if dtype is torch.bfloat16:
+        return OUT_BF16
+    if dtype is torch.float32:
+        return OUT_F32
+    raise ValueError(f"out_dtype: torch.float32 or torch.bfloat16 is needed, got {dtype}")
+
+
 def packed_weight_sizes(N: int, K: int, group: int, mode, layout=WEIGHTS_CAST):
     a, b, c = C.c_size_t(), C.c_size_t(), C.c_size_t()
     _check(lib().zq_packed_weight_sizes(N, K, group, _mode(mode), _layout(layout), C.byref(a), C.byref(b),
@@ -265,9 +274,9 @@ def w4a8_linear(w: PackedWeight, *, q=None, sx=None, t=None, x=None, U=None, V=N
     r = 0 if U is None else U.shape[1]
     if workspace is None:
         workspace = make_workspace(linear_workspace_bytes(M, N, K, r), codes.device)
+    ydt = _out_type(out_dtype if y is None else y.dtype)
     if y is None:
         y = torch.empty((M, N), dtype=out_dtype, device=codes.device)
-    ydt = OUT_F32 if y.dtype == torch.float32 else OUT_BF16
     ldy = y.stride(0) if M > 1 else N
     if relu or y_absmax is not None:
         assert y_absmax is None or (y_absmax.dtype == torch.float32 and y_absmax.is_contiguous() and
@@ -290,9 +299,9 @@ def w4a8_linear_noalloc(w: PackedWeight, *, q, sx, t=None, U=None, y=None, out_d
     assert w.layout == WEIGHTS_CAST, "zq_w4a8_linear_noalloc takes weights in the cast layout"
     M = q.shape[0]
     r = 0 if U is None else U.shape[1]
+    ydt = _out_type(out_dtype if y is None else y.dtype)
     if y is None:
         y = torch.empty((M, N), dtype=out_dtype, device=codes.device)
-    ydt = OUT_F32 if y.dtype == torch.float32 else OUT_BF16
     ldy = y.stride(0) if M > 1 else N
     _check(lib().zq_w4a8_linear_noalloc(_ptr(q), _ptr(sx), M, N, K, group, _mode(mode), _ptr(codes), _ptr(shift),
                                         _ptr(scale), _ptr(U), _ptr(t), r, _ptr(y), ydt, ldy, _stream()),
@@ -421,15 +430,6 @@ def fp8_block_linear_workspace_bytes(M: int, N: int, K: int) -> int:
 
 def _blocks(n: int) -> int:
     return (n + 127) // 128
-
-
-def _out_type(dtype) -> int:
-    """The library's name for a result type.  Any other type would be written as bf16: wrong bits, or beyond its end."""
-    if dtype is torch.bfloat16:
-        return OUT_BF16
-    if dtype is torch.float32:
-        return OUT_F32
-    raise ValueError(f"out_dtype: torch.float32 or torch.bfloat16 is needed, got {dtype}")
 
 
 def quantize_fp8_block(x: torch.Tensor, mode="none") -> Fp8Block:

@@ -48,3 +48,16 @@ def test_result_types(dtype):
         with pytest.raises(ValueError, match="out_dtype"):
             call()
             pytest.fail(str(i))
+
+
+@pytest.mark.parametrize("dtype", OTHER_TYPES)
+def test_result_types_w4a8(dtype):
+    w = binding.PackedWeight(torch.zeros(8704, dtype=u8), torch.zeros((128, 1), dtype=u8), torch.ones(128), 128, 128, 128,
+                             binding.SCALE_M2)
+    q, sx, work = torch.zeros((4, 128), dtype=u8), torch.ones(4), torch.zeros(256, dtype=u8)
+    y = torch.zeros((4, 128)).to(dtype)
+    for call in (lambda **kw: binding.w4a8_linear(w, q=q, sx=sx, workspace=work, **kw),
+                 lambda **kw: binding.w4a8_linear_noalloc(w, q=q, sx=sx, **kw)):
+        for kw in (dict(out_dtype=dtype), dict(y=y)):
+            with pytest.raises(ValueError, match="out_dtype"):
+                call(**kw)
