@@ -19,6 +19,7 @@
 // Warp roles: 0..7 epilogue, 8..23 converters (four groups, each with a stage of its own), 24 producer, 25 tensor memory
 // and MMAs.
 #include "fp8_block.cuh"
+#include "fp8_index.h"
 
 namespace zq {
 namespace fp8b {
@@ -274,12 +275,14 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
       tile_of(p, pos, part, kt, n_unused, wide);
       const float* sc = p.s + static_cast<int64_t>(kt) * p.M;
       int i = (g - n0) & 3;  // this group's first stage of the tile
-      int m_next = (step0 + i) * kTok + row;
-      float s_next = i < steps && m_next < p.M ? __ldg(sc + m_next) : 0.0f;
+      auto fetch = [&](int stage) {
+        const int m = stage_token(step0, stage, steps, row, p.M);
+        return m >= 0 ? __ldg(sc + m) : 0.0f;
+      };
+      float s_next = fetch(i);
       for (; i < steps; i += 4) {
         const float scale = s_next;
-        m_next += 4 * kTok;
-        s_next = m_next < p.M ? __ldg(sc + m_next) : 0.0f;
+        s_next = fetch(i + 4);
         const int use = (n0 + i) >> 2;  // use of stage g
         if (!mbar_wait_all(&full[g], use & 1, s_abort) || (use > 0 && !mbar_wait_all(&conv_empty[g], (use - 1) & 1, s_abort))) {
           if (lane == 0) raise_error8(p.status, s_abort, kErrConvertW);
