@@ -376,9 +376,8 @@ size_t zq_fp8_block_workspace_bytes(int64_t M, int64_t K);
  * parts : 1, or 2 for a sum over two pairs of operands (the input gradient of two projections of the same input)
  * q, s  : activations [parts][M, K] and their scales [parts][ceil(K/128), M]; or x_bf16 [M, ldx] (parts == 1,
  *         q = s = NULL), which the call quantizes with `mode`
- * w, ws : weights [parts][N, K] and scales [parts][ceil(N/128), ceil(K/128)].  The kernel may copy its first weight tiles
- *         while the kernel ahead of it in the stream still runs (as for the W4A8 layer): weights are the layer's
- *         own data, written by the two entry points above or by kernels launched in the ordinary way
+ * w, ws : weights [parts][N, K] and scales [parts][ceil(N/128), ceil(K/128)]; read after everything ahead in the stream has
+ *         ended, whatever wrote them
  * y     : out [M, ldy], FP32 or bf16 (ydt), element-aligned, ldy >= N; any N
  * The products of a block are summed by the tensor core, scaled and summed over the blocks in FP32; results do not
  * vary from run to run.  M == 0 or N == 0 is a no-op.

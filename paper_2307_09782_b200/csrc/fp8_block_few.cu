@@ -175,26 +175,28 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   if (warp == C::kProducerWarp) {
     if (ok_start) {
       const bool issuer = elect_one();
-      auto issue_weights = [&](int s, int kb) {
+      auto issue = [&](int s, int kb) {
         if (!issuer) return;
         const int seg = kb / p.kblocks, k = (kb - seg * p.kblocks) * kBlk;
         uint8_t* d = smem + s * C::kWBytes;
         mbar_arrive_expect_tx(&full[s], C::kWBytes + (RAW ? 0 : C::kTokBytes));
         tma_load_3d(d, &tm_w, k, nt * kBlk, GATED ? 0 : seg, &full[s]);
         if (GATED) tma_load_3d(d + C::kWBytes / 2, &tm_w, k, nt * kBlk, 1, &full[s]);
+        if (!RAW) tma_load_3d(smem + C::offTok + s * C::kTokBytes, &tm_q, k, m0, seg, &full[s]);
       };
-      auto issue_tokens = [&](int s, int kb) {
-        if (RAW || !issuer) return;
-        const int seg = kb / p.kblocks, k = (kb - seg * p.kblocks) * kBlk;
-        tma_load_3d(smem + C::offTok + s * C::kTokBytes, &tm_q, k, m0, seg, &full[s]);
-      };
-      // weights are the layer's own read-only data: their first copies go out before the wait for the kernel ahead
-      // in the stream, whose output the tokens may be
+      // The first weight tiles are fetched to L2 while the kernel ahead in the stream may still run.  They are copied from there
+      // after the wait for it, and not before: it may be the kernel that writes the weights, or that followed it, and until then
+      // nothing orders its stores before the copies.
       const int first = min(NS, nkb);
-      for (int i = 0; i < first; ++i) issue_weights(i, kb0 + i);
+      for (int i = 0; i < first; ++i) {
+        if (!issuer) continue;
+        const int kb = kb0 + i, seg = kb / p.kblocks, k = (kb - seg * p.kblocks) * kBlk;
+        tma_prefetch_3d(&tm_w, k, nt * kBlk, GATED ? 0 : seg);
+        if (GATED) tma_prefetch_3d(&tm_w, k, nt * kBlk, 1);
+      }
       __syncwarp();
       pdl_wait();
-      for (int i = 0; i < first; ++i) issue_tokens(i, kb0 + i);
+      for (int i = 0; i < first; ++i) issue(i, kb0 + i);
       __syncwarp();
       bool ok = true;
       int s = first == NS ? 0 : first, issued = first;
@@ -205,8 +207,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
           ok = false;
           break;
         }
-        issue_weights(s, kb0 + i);
-        issue_tokens(s, kb0 + i);
+        issue(s, kb0 + i);
         __syncwarp();
         ++issued;
         if (++s == NS) {

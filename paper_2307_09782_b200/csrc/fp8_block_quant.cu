@@ -49,14 +49,6 @@ quantize_block_kernel(const __nv_bfloat16* __restrict__ x, int M, int K, int64_t
   }
 }
 
-// The product kernels start copying their weights before they wait for the kernel ahead in the stream.  That kernel may be one
-// of the two below, whose CTAs have then finished: what they wrote is made visible to the device, and to the copy engine,
-// before each of them ends.
-__device__ __forceinline__ void publish_weights() {
-  __threadfence();
-  asm volatile("fence.proxy.async.global;" ::: "memory");
-}
-
 // One CTA per 128 x 128 block, kept in registers between the maximum and the cast.
 __global__ void __launch_bounds__(256)
 quantize_weight_block_kernel(const float* __restrict__ w, int64_t N, int64_t K, int64_t kblocks, bool pow2,
@@ -88,7 +80,6 @@ quantize_weight_block_kernel(const float* __restrict__ w, int64_t N, int64_t K, 
     const int64_t n = nb * kBlk + i * 8 + row;
     if (n < N && k < K) *reinterpret_cast<uint32_t*>(q + n * K + k) = cast4(v[i].x, v[i].y, v[i].z, v[i].w, inv);
   }
-  publish_weights();
 }
 
 // 128 x 128 tile through shared memory: 16-byte loads along K, 16-byte stores along N.
@@ -122,7 +113,6 @@ transpose_weight_block_kernel(const uint8_t* __restrict__ q, const float* __rest
       *reinterpret_cast<uint4*>(qt + k * N + n) = make_uint4(o[0], o[1], o[2], o[3]);
     }
   }
-  publish_weights();
 }
 
 inline int launched(cudaError_t e) {
