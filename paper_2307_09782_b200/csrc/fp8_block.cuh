@@ -135,6 +135,25 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
+// Loads of data that the kernel ahead in the stream may have written.  With programmatic launches that kernel can still run
+// when this one begins.  So the read-only path, which is for data that nobody writes while the kernel lasts, is not for them
+// (the compiler may move such a load above the wait for that kernel as well), nor are lines that the first-level cache may hold
+// from before the wait: they go to L2, and stay in order with the wait.
+__device__ __forceinline__ float load_chained(const float* p) {
+  float v;
+  asm volatile("ld.global.cg.f32 %0, [%1];" : "=f"(v) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint32_t load_chained(const uint32_t* p) {
+  uint32_t v;
+  asm volatile("ld.global.cg.u32 %0, [%1];" : "=r"(v) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint4 load_chained(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.cg.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
 // A tile of a 3-D tensor map on its way to L2.  It reads nothing: whatever is written to the tile afterwards is what a copy
 // after that write gets.
 __device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* m, int c0, int c1, int c2) {

@@ -280,7 +280,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     auto weight_scale = [&](int kb) {
       const int seg = kb / p.kblocks;
       const int64_t part = static_cast<int64_t>(p.nblocks) * p.kblocks;
-      return lane < C::kMats ? __ldg(p.sb + (GATED ? lane : seg) * part + static_cast<int64_t>(nt) * p.kblocks + (kb - seg * p.kblocks))
+      return lane < C::kMats ? load_chained(p.sb + (GATED ? lane : seg) * part + static_cast<int64_t>(nt) * p.kblocks + (kb - seg * p.kblocks))
                              : 0.0f;
     };
     pdl_wait();
@@ -295,7 +295,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         for (int j = 0; j < kPairs; ++j) {
           const int r = r0 + 2 * j;
           v[j] = make_uint4(0u, 0u, 0u, 0u);
-          if (r < m_here && k < p.K) v[j] = __ldg(reinterpret_cast<const uint4*>(p.x + static_cast<int64_t>(m0 + r) * p.ldx + k));
+          if (r < m_here && k < p.K) v[j] = load_chained(reinterpret_cast<const uint4*>(p.x + static_cast<int64_t>(m0 + r) * p.ldx + k));
         }
       };
       while (i_next < nkb) {
@@ -344,7 +344,7 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         const float* src = p.sa + static_cast<int64_t>(kb0 + i) * p.M + m0;  // [segs][kblocks][M]
         float v[BM / 32 + 1];
 #pragma unroll
-        for (int c = 0; c < BM; c += 32) v[c / 32] = c + lane < m_here ? __ldg(src + c + lane) : 0.0f;
+        for (int c = 0; c < BM; c += 32) v[c / 32] = c + lane < m_here ? load_chained(src + c + lane) : 0.0f;
         const float sw = weight_scale(kb0 + i);
         if (i >= NS && !mbar_wait_all(&acc_empty[s], ((i / NS) - 1) & 1, s_abort)) {
           if (lane == 0) raise_error8(p.status, s_abort, kErrQuantF);

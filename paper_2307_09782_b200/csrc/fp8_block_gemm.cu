@@ -415,10 +415,10 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
             sb0 += part - p.kblocks;
             sb1 += part - p.kblocks;
           }
-          b[slot][0] = __ldg(sb0++);
-          b[slot][1] = __ldg(sb1++);
+          b[slot][0] = load_chained(sb0++);
+          b[slot][1] = load_chained(sb1++);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) a[slot][j] = m0 + 32 * j < p.M ? __ldg(sa + 32 * j) : 1.0f;
+          for (int j = 0; j < 4; ++j) a[slot][j] = m0 + 32 * j < p.M ? load_chained(sa + 32 * j) : 1.0f;
           sa += p.M;
         };
 #pragma unroll
@@ -480,10 +480,10 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       float a[kAhead][4], b[kAhead];
       auto fetch = [&](int i, int slot) {
         const int seg = KIND == kPlain && i >= p.kblocks ? 1 : 0;  // at most two segments
-        b[slot] = __ldg(sb + seg * part + (i - seg * p.kblocks));
+        b[slot] = load_chained(sb + seg * part + (i - seg * p.kblocks));
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          a[slot][j] = m0 + 32 * j < p.M ? __ldg(p.sa + static_cast<int64_t>(i) * p.M + m0 + 32 * j) : 0.0f;
+          a[slot][j] = m0 + 32 * j < p.M ? load_chained(p.sa + static_cast<int64_t>(i) * p.M + m0 + 32 * j) : 0.0f;
       };
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
@@ -694,8 +694,8 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         const bool any = cols > 0;
         float sg = 0.0f, su = 0.0f;
         if (any && m_ok) {
-          sg = __ldg(p.cks + static_cast<int64_t>(fb) * p.M + m);
-          su = __ldg(p.cks + SM + static_cast<int64_t>(fb) * p.M + m);
+          sg = load_chained(p.cks + static_cast<int64_t>(fb) * p.M + m);
+          su = load_chained(p.cks + SM + static_cast<int64_t>(fb) * p.M + m);
         }
         // 32 columns at a time through the staging buffer (dh in FP32), so that eight lanes share a row: they read the
         // codes of g and u and write dg and du in whole sectors.  The bf16 pairs of dg and du take the place of the sums
@@ -712,8 +712,8 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
             const int r = it * 4 + rr;
             gn[it] = un[it] = 0u;
             if (r < rows && 32 * c + 4 * cc < cols) {  // N is a multiple of 16: the four are inside or outside together
-              gn[it] = __ldg(reinterpret_cast<const uint32_t*>(ck + static_cast<int64_t>(r) * p.N + 32 * c));
-              un[it] = __ldg(reinterpret_cast<const uint32_t*>(ck + MN + static_cast<int64_t>(r) * p.N + 32 * c));
+              gn[it] = load_chained(reinterpret_cast<const uint32_t*>(ck + static_cast<int64_t>(r) * p.N + 32 * c));
+              un[it] = load_chained(reinterpret_cast<const uint32_t*>(ck + MN + static_cast<int64_t>(r) * p.N + 32 * c));
             }
           }
         };

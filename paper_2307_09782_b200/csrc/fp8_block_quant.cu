@@ -17,8 +17,7 @@ constexpr int kQuantGroups = kQuantThreads / 16;
 // neighbouring rows, so that their scales (stored with the row index innermost) share sectors.
 template <int U>
 __global__ void __launch_bounds__(kQuantThreads)
-quantize_block_kernel(const __nv_bfloat16* __restrict__ x, int M, int K, int64_t ldx, int kblocks, bool pow2,
-                      uint8_t* __restrict__ q, float* __restrict__ s) {
+quantize_block_kernel(const __nv_bfloat16* x, int M, int K, int64_t ldx, int kblocks, bool pow2, uint8_t* q, float* s) {
   pdl_launch_dependents();
   const int64_t task = static_cast<int64_t>(blockIdx.x) * kQuantGroups + (threadIdx.x >> 4);
   const int lane = threadIdx.x & 15;
@@ -32,7 +31,7 @@ quantize_block_kernel(const __nv_bfloat16* __restrict__ x, int M, int K, int64_t
   for (int u = 0; u < U; ++u) {
     const int k = (kb0 + u) * kBlk + lane * 8;
     v[u] = make_uint4(0u, 0u, 0u, 0u);
-    if (row_ok && k < K) v[u] = __ldg(reinterpret_cast<const uint4*>(xr + k));
+    if (row_ok && k < K) v[u] = load_chained(reinterpret_cast<const uint4*>(xr + k));
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {

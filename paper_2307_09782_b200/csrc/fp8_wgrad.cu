@@ -277,7 +277,7 @@ fp8_wgrad_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant
       int i = (g - n0) & 3;  // this group's first stage of the tile
       auto fetch = [&](int stage) {
         const int m = stage_token(step0, stage, steps, row, p.M);
-        return m >= 0 ? __ldg(sc + m) : 0.0f;
+        return m >= 0 ? load_chained(sc + m) : 0.0f;
       };
       float s_next = fetch(i);
       for (; i < steps; i += 4) {

@@ -36,3 +36,14 @@ def test_weight_gradient_rows(tmp_path):
       }
     }"""
     run(tmp_path, body)
+
+
+def test_chained_kernels_load_through_l2():
+    """The kernels that are launched before the one ahead has ended never use the read-only path, whose loads may see what was
+    there before (and may be moved ahead of the wait)."""
+    for name in ("fp8_block_few.cu", "fp8_block_gemm.cu", "fp8_wgrad.cu"):
+        text = open(os.path.join(CSRC, name)).read()
+        assert "__ldg(" not in text and "__restrict__" not in text and "load_chained(" in text, name
+    text = open(os.path.join(CSRC, "fp8_block_quant.cu")).read()
+    chained = text[text.index("\nquantize_block_kernel("):text.index("// One CTA per 128 x 128 block")]
+    assert "__ldg(" not in chained and "__restrict__" not in chained and "pdl_wait();" in chained

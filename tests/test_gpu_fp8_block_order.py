@@ -7,7 +7,7 @@ import torch
 
 import fp8_ref as R
 from gpu_util import dev
-from paper_2307_09782_b200 import binding
+from paper_2307_09782_b200 import binding, gated_ffn
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +61,44 @@ def test_weights_rewritten_just_before(M, raw, gated):
     assert binding.device_status(ws) == (0, 0)
     for i, y in enumerate(got):
         assert torch.equal(y, want[i % 3]), i
+
+
+@pytest.mark.parametrize("M", [1, 20, 200])
+@pytest.mark.parametrize("mode", ["none", "M1"])
+def test_calls_in_a_row(M, mode):
+    """Training and serving passes of two blocks one after the other on the same buffers, each reading what the kernel just ahead
+    wrote: the same bits as with the device waited for in between."""
+    K, F = 512, 720
+    gen = torch.Generator(device="cuda").manual_seed(M)
+
+    def normal(*shape, std=1.0):
+        return torch.randn(shape, generator=gen, device=dev()) * std
+
+    blocks = [gated_ffn.GatedFfnFp8.from_weights(normal(F, K, std=0.05), normal(F, K, std=0.05), normal(K, F, std=0.05), mode=mode,
+                                                 training=True) for _ in range(2)]
+    for b in blocks[1:]:
+        b._workspaces = blocks[0]._workspaces  # one workspace for both: what a call leaves there the next one overwrites
+    xs = [normal(M, K).to(torch.bfloat16) for _ in range(2)]
+
+    def chain(wait):
+        out = []
+        for i in range(12):
+            x = xs[i % 2]
+            keep = []
+            for b in blocks:
+                x, saved = b.forward_train(x)
+                keep.append(saved)
+                wait()
+            dy = x
+            for b, saved in zip(reversed(blocks), reversed(keep)):
+                dy, dgu, dd = b.backward(dy, saved)
+                out += [dgu, dd]
+                wait()
+            out += [x, dy, blocks[0].forward(dy)]
+            wait()
+        torch.cuda.synchronize()
+        return out
+
+    want = chain(torch.cuda.synchronize)
+    for i, (a, b) in enumerate(zip(want, chain(lambda: None))):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16)), i
