@@ -505,6 +505,15 @@ def _scales(mode, w: Fp8Weight, q: Optional[Fp8Block]) -> int:
 
 
 _fp8_workspaces = {}
+_fp8_head = 0
+
+
+def _fp8_workspace_need(M: int, K: int) -> int:
+    """``zq_fp8_block_workspace_bytes`` without a call into the library: a head, the codes, the scales, each rounded up to 256."""
+    global _fp8_head
+    if _fp8_head == 0:
+        _fp8_head = int(lib().zq_fp8_block_workspace_bytes(0, 16))
+    return _fp8_head + (M * K + 255) // 256 * 256 + (4 * M * _blocks(K) + 255) // 256 * 256
 
 
 def _fp8_workspace(workspace, M: int, K: int, device):
@@ -512,10 +521,9 @@ def _fp8_workspace(workspace, M: int, K: int, device):
     if workspace is not None:
         return workspace
     key = (device.index, _stream())
-    ws, most = _fp8_workspaces.get(key, (None, -1))
-    if most < M * (K + 128):  # codes, scales and some slack: a bound that needs no call
-        ws, most = make_workspace(lib().zq_fp8_block_workspace_bytes(M, K), device), M * (K + 128)
-        _fp8_workspaces[key] = ws, most
+    ws, need = _fp8_workspaces.get(key), _fp8_workspace_need(M, K)
+    if ws is None or ws.numel() < need:
+        ws = _fp8_workspaces[key] = make_workspace(need, device)
     return ws
 
 

@@ -61,3 +61,30 @@ def test_result_types_w4a8(dtype):
         for kw in (dict(out_dtype=dtype), dict(y=y)):
             with pytest.raises(ValueError, match="out_dtype"):
                 call(**kw)
+
+
+# ---- workspaces that are kept ------------------------------------------------------------------------------------------
+@pytest.fixture
+def kept(monkeypatch):
+    """The workspaces that the binding keeps, on the CPU, from an empty start."""
+    monkeypatch.setattr(binding, "_stream", lambda: 0)
+    monkeypatch.setattr(binding, "make_workspace", lambda n, device=None: torch.zeros(n, dtype=u8))
+    monkeypatch.setattr(binding, "_fp8_workspaces", type(binding._fp8_workspaces)())
+    return torch.device("cpu")
+
+
+SEQUENCES = [[(2048, 512), (300, 4096)], [(100, 1024), (27, 4096)], [(8192, 7168), (2075, 28672)], [(8192, 256), (700, 4096)],
+             [(1000, 16), (1, 100_000)], [(0, 16), (1, 16), (3, 128), (2, 4096), (1, 8192), (64, 16)]]
+
+
+@pytest.mark.parametrize("calls", SEQUENCES)
+def test_kept_workspace_is_large_enough(kept, L, calls):
+    for M, K in calls:
+        ws = binding._fp8_workspace(None, M, K, kept)
+        assert ws.numel() >= L.zq_fp8_block_workspace_bytes(M, K), (M, K)
+
+
+def test_workspace_need(L):
+    for M in (0, 1, 2, 7, 64, 333, 4096, 100_003):
+        for K in (16, 128, 144, 4096, 11008, 28672):
+            assert binding._fp8_workspace_need(M, K) == L.zq_fp8_block_workspace_bytes(M, K)
