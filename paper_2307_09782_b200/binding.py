@@ -160,6 +160,11 @@ def _stream():
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
+def _capturing() -> bool:
+    """Whether calls on the current stream are being captured into a CUDA graph."""
+    return torch._C._cuda_isCurrentStreamCapturing()
+
+
 def _check(status: int, where: str):
     if status != 0:
         raise ZqError(status, where)
@@ -517,11 +522,16 @@ def _fp8_workspace_need(M: int, K: int) -> int:
 
 
 def _fp8_workspace(workspace, M: int, K: int, device):
-    """The caller's workspace, or one that is kept per device and stream and grown on demand."""
+    """The caller's workspace, or one that is kept per device and stream and grown on demand.  A call that is captured into a
+    CUDA graph gets one of its own, in the graph's memory: a graph lasts longer than a kept one, which is given back when it
+    has to grow, and may be replayed on any stream."""
     if workspace is not None:
         return workspace
+    need = _fp8_workspace_need(M, K)
+    if _capturing():
+        return make_workspace(need, device)
     key = (device.index, _stream())
-    ws, need = _fp8_workspaces.get(key), _fp8_workspace_need(M, K)
+    ws = _fp8_workspaces.get(key)
     if ws is None or ws.numel() < need:
         ws = _fp8_workspaces[key] = make_workspace(need, device)
     return ws

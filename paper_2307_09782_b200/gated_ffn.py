@@ -17,7 +17,8 @@ class GatedFfnFp8:
 
     ``mode``: how activations are scaled, "none" (FP32 scales) or "M1" (powers of two, which the 8-bit checkpoints
     turn back into bf16 without rounding: the one to train with).  ``training`` lays the transposed weights out as well.
-    A block keeps one workspace per stream and device it is used on, grown on demand.
+    A block keeps one workspace per stream and device it is used on, grown on demand; a call that is captured into a CUDA graph
+    gets one of its own, in the graph's memory.
     """
 
     def __init__(self, gate_up: Fp8Weight, down: Fp8Weight, act: str = "silu", mode: str = "none", training: bool = False):
@@ -39,13 +40,17 @@ class GatedFfnFp8:
         return cls(binding.quantize_weight_fp8_block(torch.stack([gate, up]), mode),
                    binding.quantize_weight_fp8_block(down.contiguous(), mode), **kw)
 
+    def _new_workspace(self, M: int) -> torch.Tensor:
+        return binding.make_workspace(binding.fp8_gated_ffn_workspace_bytes(M, self.gate_up.K, self.gate_up.N, self.down.N,
+                                                                            self.down_t is not None), self.down.codes.device)
+
     def workspace(self, M: int) -> torch.Tensor:
-        dev = self.down.codes.device
-        key = (dev, binding._stream())
+        if binding._capturing():
+            return self._new_workspace(M)
+        key = (self.down.codes.device, binding._stream())
         ws, rows = self._workspaces.get(key, (None, -1))
         if rows < M:
-            ws = binding.make_workspace(binding.fp8_gated_ffn_workspace_bytes(M, self.gate_up.K, self.gate_up.N, self.down.N,
-                                                                              self.down_t is not None), dev)
+            ws = self._new_workspace(M)
             self._workspaces[key] = (ws, M)
         return ws
 

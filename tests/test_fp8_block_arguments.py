@@ -68,6 +68,7 @@ def test_result_types_w4a8(dtype):
 def kept(monkeypatch):
     """The workspaces that the binding keeps, on the CPU, from an empty start."""
     monkeypatch.setattr(binding, "_stream", lambda: 0)
+    monkeypatch.setattr(binding, "_capturing", lambda: False, raising=False)
     monkeypatch.setattr(binding, "make_workspace", lambda n, device=None: torch.zeros(n, dtype=u8))
     monkeypatch.setattr(binding, "_fp8_workspaces", type(binding._fp8_workspaces)())
     return torch.device("cpu")
@@ -88,3 +89,16 @@ def test_workspace_need(L):
     for M in (0, 1, 2, 7, 64, 333, 4096, 100_003):
         for K in (16, 128, 144, 4096, 11008, 28672):
             assert binding._fp8_workspace_need(M, K) == L.zq_fp8_block_workspace_bytes(M, K)
+
+
+def test_captured_calls_keep_nothing(kept, monkeypatch):
+    """A captured call's workspace is neither the kept one, which may be given back while the graph lives, nor kept."""
+    monkeypatch.setattr(binding, "_capturing", lambda: False)
+    ffn = gated_ffn.GatedFfnFp8(weight(32, 64, 2), weight(64, 32))
+    eager = binding._fp8_workspace(None, 8, 64, kept), ffn.workspace(8)
+    monkeypatch.setattr(binding, "_capturing", lambda: True)
+    captured = [binding._fp8_workspace(None, 8, 64, kept), ffn.workspace(8), binding._fp8_workspace(None, 8, 64, kept),
+                ffn.workspace(8)]
+    assert len({t.data_ptr() for t in (*eager, *captured)}) == 6
+    monkeypatch.setattr(binding, "_capturing", lambda: False)
+    assert binding._fp8_workspace(None, 8, 64, kept) is eager[0] and ffn.workspace(8) is eager[1]

@@ -21,3 +21,35 @@ def test_kept_workspace_over_sizes():
             y = binding.fp8_block_linear(w[K], x=x)
             assert torch.equal(y, binding.fp8_block_linear(w[K], q=binding.quantize_fp8_block(x))), (M, K)
         torch.cuda.synchronize()
+
+
+def test_captured_calls():
+    """A graph captured on a stream where the same calls ran before, replayed after those calls' workspaces have grown: it
+    computes on new inputs, and writes to nothing but its own memory."""
+    K, F, M = 512, 720, 24
+    ffn = gated_ffn.GatedFfnFp8.from_weights(*[torch.randn(s, device=dev()) * 0.05 for s in ((F, K), (F, K), (K, F))], mode="M1")
+    down = binding.quantize_weight_fp8_block(torch.randn((K, K), device=dev()) * 0.05)
+    x = torch.randn((M, K), device=dev()).to(torch.bfloat16)
+    big = torch.randn((3000, K), device=dev()).to(torch.bfloat16)
+    s = torch.cuda.Stream()
+
+    def both(v):
+        return binding.fp8_block_linear(down, x=ffn.forward(v), out_dtype=torch.bfloat16)
+
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        both(x)
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        y = both(x)
+    with torch.cuda.stream(s):
+        both(big)  # the kept workspaces grow: the old ones go back to the allocator
+        fill = [torch.full((1 << 18,), 7, dtype=torch.uint8, device=dev()) for _ in range(64)]
+    s.synchronize()
+    for v in (x.clone(), torch.randn_like(x)):
+        x.copy_(v)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, both(v))
+    assert all(bool((f == 7).all()) for f in fill)
