@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import threading
 from dataclasses import dataclass
 from typing import Optional
 
@@ -509,7 +510,18 @@ def _scales(mode, w: Fp8Weight, q: Optional[Fp8Block]) -> int:
     return m | SCALES_POW2 if w.pow2 and (m == SCALE_M1 if q is None else q.pow2) else m
 
 
-_fp8_workspaces = {}
+class KeptWorkspaces(threading.local):
+    """Workspaces that outlast a call, each thread's own: the library is called without the interpreter's lock, so the kernels of
+    two threads' calls can mix on a stream that they share.  Copies and pickles start empty."""
+
+    def __init__(self):
+        self.of = {}
+
+    def __reduce__(self):
+        return KeptWorkspaces, ()
+
+
+_fp8_workspaces = KeptWorkspaces()
 _fp8_head = 0
 
 
@@ -522,7 +534,7 @@ def _fp8_workspace_need(M: int, K: int) -> int:
 
 
 def _fp8_workspace(workspace, M: int, K: int, device):
-    """The caller's workspace, or one that is kept per device and stream and grown on demand.  A call that is captured into a
+    """The caller's workspace, or one that is kept per thread, device and stream and grown on demand.  A call that is captured into a
     CUDA graph gets one of its own, in the graph's memory: a graph lasts longer than a kept one, which is given back when it
     has to grow, and may be replayed on any stream."""
     if workspace is not None:
@@ -531,9 +543,10 @@ def _fp8_workspace(workspace, M: int, K: int, device):
     if _capturing():
         return make_workspace(need, device)
     key = (device.index, _stream())
-    ws = _fp8_workspaces.get(key)
+    kept = _fp8_workspaces.of
+    ws = kept.get(key)
     if ws is None or ws.numel() < need:
-        ws = _fp8_workspaces[key] = make_workspace(need, device)
+        ws = kept[key] = make_workspace(need, device)
     return ws
 
 

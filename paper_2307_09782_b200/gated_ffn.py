@@ -17,7 +17,7 @@ class GatedFfnFp8:
 
     ``mode``: how activations are scaled, "none" (FP32 scales) or "M1" (powers of two, which the 8-bit checkpoints
     turn back into bf16 without rounding: the one to train with).  ``training`` lays the transposed weights out as well.
-    A block keeps one workspace per stream and device it is used on, grown on demand; a call that is captured into a CUDA graph
+    A block keeps one workspace per thread, stream and device it is used on, grown on demand; a call that is captured into a CUDA graph
     gets one of its own, in the graph's memory.
     """
 
@@ -28,7 +28,7 @@ class GatedFfnFp8:
         self.gate_up, self.down, self.act, self.mode = gate_up, down, act, mode
         self.gate_up_t: Optional[Fp8Weight] = None
         self.down_t: Optional[Fp8Weight] = None
-        self._workspaces = {}
+        self._workspaces = binding.KeptWorkspaces()
         if training:
             self.gate_up_t = binding.transpose_fp8_weight(gate_up)
             self.down_t = binding.transpose_fp8_weight(down)
@@ -48,10 +48,11 @@ class GatedFfnFp8:
         if binding._capturing():
             return self._new_workspace(M)
         key = (self.down.codes.device, binding._stream())
-        ws, rows = self._workspaces.get(key, (None, -1))
+        kept = self._workspaces.of
+        ws, rows = kept.get(key, (None, -1))
         if rows < M:
             ws = self._new_workspace(M)
-            self._workspaces[key] = (ws, M)
+            kept[key] = (ws, M)
         return ws
 
     def forward(self, x: torch.Tensor, out_dtype=torch.bfloat16) -> torch.Tensor:

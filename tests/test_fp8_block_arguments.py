@@ -1,4 +1,8 @@
 """Arguments that the binding of the FP8 operators must refuse, or look after, before anything is launched (no GPU needed)."""
+import copy
+import pickle
+import threading
+
 import pytest
 import torch
 
@@ -102,3 +106,26 @@ def test_captured_calls_keep_nothing(kept, monkeypatch):
     assert len({t.data_ptr() for t in (*eager, *captured)}) == 6
     monkeypatch.setattr(binding, "_capturing", lambda: False)
     assert binding._fp8_workspace(None, 8, 64, kept) is eager[0] and ffn.workspace(8) is eager[1]
+
+
+def test_threads_share_no_workspace(kept):
+    """Threads can share a stream (all start on the default one) and their calls' kernels mix there."""
+    ffn = gated_ffn.GatedFfnFp8(weight(32, 64, 2), weight(64, 32))
+
+    def both():
+        return binding._fp8_workspace(None, 8, 64, kept), ffn.workspace(8)
+
+    mine, others = both(), []
+    t = threading.Thread(target=lambda: others.extend([*both(), *both()]))
+    t.start()
+    t.join()
+    assert others[0] is others[2] and others[1] is others[3]
+    assert len({b.data_ptr() for b in (*mine, *others)}) == 4
+    assert both()[0] is mine[0] and both()[1] is mine[1]
+
+
+def test_block_can_be_copied(kept):
+    ffn = gated_ffn.GatedFfnFp8(weight(32, 64, 2), weight(64, 32))
+    ws = ffn.workspace(8)
+    for other in (copy.deepcopy(ffn), pickle.loads(pickle.dumps(ffn))):
+        assert torch.equal(other.down.codes, ffn.down.codes) and other.workspace(8).data_ptr() != ws.data_ptr()

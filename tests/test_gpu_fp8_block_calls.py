@@ -1,5 +1,7 @@
 """How the FP8 operators are called: sizes one after the other without a workspace of the caller's, empty batches, results of
 more bytes than 32 bits count, stream capture, threads, scales that change in place."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -53,3 +55,32 @@ def test_captured_calls():
         torch.cuda.synchronize()
         assert torch.equal(y, both(v))
     assert all(bool((f == 7).all()) for f in fill)
+
+
+def test_threads_on_one_stream():
+    """Two threads use one block on the same stream, each with its own tokens."""
+    K, F, M = 512, 720, 40
+    ffn = gated_ffn.GatedFfnFp8.from_weights(*[torch.randn(s, device=dev()) * 0.05 for s in ((F, K), (F, K), (K, F))])
+    xs = [torch.randn((M, K), device=dev()).to(torch.bfloat16) for _ in range(2)]
+
+    def call(x):
+        y = ffn.forward(x)
+        return y, binding.fp8_block_linear(ffn.down, x=torch.nn.functional.pad(y, (0, F - K)), out_dtype=torch.bfloat16)
+
+    want = [call(x) for x in xs]
+    torch.cuda.synchronize()
+    got = [[], []]
+
+    def work(i):
+        for _ in range(200):
+            got[i].append(call(xs[i]))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert len(got[i]) == 200
+        assert all(torch.equal(a, b) for pair in got[i] for a, b in zip(pair, want[i]))
