@@ -365,8 +365,26 @@ def device_status(workspace: torch.Tensor):
 
 # ---- FP8 with block scales --------------------------------------------------------------------------
 
+def _version(t: torch.Tensor) -> int:
+    """A number that changes when torch writes to a tensor (inference tensors have none)."""
+    return -1 if t.is_inference() else t._version
+
+
+class _ScalesPow2:
+    """``pow2``: whether all scales are powers of two, as far as it is known: of these scales, as they were written last.  (Writes
+    that torch does not count, through ``.data``, by a kernel of one's own or to an inference tensor, are the caller's to
+    tell: set ``pow2`` anew.)"""
+
+    def _known_pow2(self) -> Optional[bool]:
+        scale, version, value = self._pow2
+        return value if scale is self.scale and version == _version(scale) else None
+
+    def _set_pow2(self, value: Optional[bool]):
+        self._pow2 = self.scale, _version(self.scale), value
+
+
 @dataclass
-class Fp8Block:
+class Fp8Block(_ScalesPow2):
     """Activations as E4M3 codes with one scale per row and 128 features (``zq_quantize_fp8_block``)."""
     codes: torch.Tensor   # uint8 [M, K] (or [parts, M, K])
     scale: torch.Tensor   # float32 [ceil(K / 128), M] (or [parts, ...]): the row index is innermost
@@ -379,8 +397,11 @@ class Fp8Block:
         return self.codes.view(torch.float8_e4m3fn).float() * s
 
 
+Fp8Block.pow2 = property(lambda self: bool(self._known_pow2()), _ScalesPow2._set_pow2)
+
+
 @dataclass
-class Fp8Weight:
+class Fp8Weight(_ScalesPow2):
     """Weights as E4M3 codes with one scale per 128 x 128 block (``zq_quantize_weight_fp8_block``); ``parts`` = 2 for the
     stacked gate and up projections."""
     codes: torch.Tensor   # uint8 [N, K] or [parts, N, K]
@@ -388,8 +409,7 @@ class Fp8Weight:
     N: int
     K: int
     parts: int = 1
-    pow2: Optional[bool] = None   # whether all scales are powers of two; None: looked up once, here (set it anew where
-                                  # the scales are changed in place)
+    pow2: Optional[bool] = None   # whether all scales are powers of two; None: looked up when it is first needed
 
     def __post_init__(self):
         lead = (self.parts,) if self.parts > 1 else ()
@@ -399,13 +419,22 @@ class Fp8Weight:
                              f"{self.parts} x [{self.N}, {self.K}]")
         _expect(self.codes, torch.uint8, "codes")
         _expect(self.scale, torch.float32, "scale")
-        if self.pow2 is None:  # positive, finite, no zero, a mantissa of zero
-            bits = self.scale.view(torch.int32)
-            self.pow2 = self.scale.is_cuda and bool((((bits & 0x7FFFFF) == 0) & (bits > 0) & (bits < 0x7F800000)).all())
+
+    def _look_up_pow2(self) -> bool:
+        value = self._known_pow2()
+        if value is None:
+            if not self.scale.is_cuda or _capturing():  # (a capture cannot wait for the answer)
+                return False
+            bits = self.scale.view(torch.int32)  # positive, finite, no zero, a mantissa of zero
+            self.pow2 = value = bool((((bits & 0x7FFFFF) == 0) & (bits > 0) & (bits < 0x7F800000)).all())
+        return value
 
     def values(self) -> torch.Tensor:
         s = self.scale.repeat_interleave(128, -1)[..., :self.K].repeat_interleave(128, -2)[..., :self.N, :]
         return self.codes.view(torch.float8_e4m3fn).float() * s
+
+
+Fp8Weight.pow2 = property(Fp8Weight._look_up_pow2, _ScalesPow2._set_pow2)
 
 
 def _expect(t: torch.Tensor, dtype, name: str):
@@ -478,7 +507,7 @@ def transpose_fp8_weight(w: Fp8Weight) -> Fp8Weight:
             _ptr(w.codes.view(w.parts, w.N, w.K)[i]), _ptr(w.scale.view(w.parts, nb, kb)[i]), w.N, w.K,
             _ptr(q.view(w.parts, w.K, w.N)[i]), _ptr(s.view(w.parts, kb, nb)[i]), _stream()),
             "zq_transpose_weight_fp8_block")
-    return Fp8Weight(q, s, w.K, w.N, w.parts, w.pow2)
+    return Fp8Weight(q, s, w.K, w.N, w.parts, w._known_pow2())
 
 
 def _activations(x, q, K: int, parts: int):
@@ -507,7 +536,12 @@ SCALES_POW2 = 16
 def _scales(mode, w: Fp8Weight, q: Optional[Fp8Block]) -> int:
     """The scale rule, with the promise of ``ZQ_SCALES_POW2`` where every scale the call is given is a power of two."""
     m = _mode(mode)
-    return m | SCALES_POW2 if w.pow2 and (m == SCALE_M1 if q is None else q.pow2) else m
+    return m | SCALES_POW2 if (m == SCALE_M1 if q is None else q.pow2) and w.pow2 else m
+
+
+def _ffn_scales(mode, gate_up: Fp8Weight, down: Fp8Weight) -> int:
+    m = _scales(mode, gate_up, None)
+    return m if m & SCALES_POW2 and down.pow2 else _mode(mode)
 
 
 class KeptWorkspaces(threading.local):
@@ -668,7 +702,7 @@ def fp8_gated_ffn(gate_up: Fp8Weight, down: Fp8Weight, x: torch.Tensor, *, act="
     _on_gpu(x, gate_up.codes, gate_up.scale, down.codes, down.scale)
     y = torch.empty((M, N), dtype=out_dtype, device=x.device)
     saved = torch.empty((fp8_gated_ffn_saved_bytes(M, K, F),), dtype=torch.uint8, device=x.device) if save else None
-    _check(lib().zq_fp8_gated_ffn(x.data_ptr(), ldx, _scales(mode, gate_up, None) if down.pow2 else _mode(mode), M, K, F, N, gate_up.codes.data_ptr(),
+    _check(lib().zq_fp8_gated_ffn(x.data_ptr(), ldx, _ffn_scales(mode, gate_up, down), M, K, F, N, gate_up.codes.data_ptr(),
                                   gate_up.scale.data_ptr(), down.codes.data_ptr(), down.scale.data_ptr(), _act(act),
                                   y.data_ptr(), ydt, N, _ptr(saved),
                                   workspace.data_ptr(), workspace.numel(), _stream()), "zq_fp8_gated_ffn")
@@ -695,7 +729,7 @@ def fp8_gated_ffn_backward(gate_up_t: Fp8Weight, down_t: Fp8Weight, dy: torch.Te
     dwgu = torch.empty((2, F, K), dtype=out_dtype, device=dev)
     dwd = torch.empty((N, F), dtype=out_dtype, device=dev)
     _check(lib().zq_fp8_gated_ffn_backward(dy.data_ptr(), lddy,
-                                           _scales(mode, gate_up_t, None) if down_t.pow2 else _mode(mode), M, K, F, N, saved.data_ptr(),
+                                           _ffn_scales(mode, gate_up_t, down_t), M, K, F, N, saved.data_ptr(),
                                            gate_up_t.codes.data_ptr(), gate_up_t.scale.data_ptr(),
                                            down_t.codes.data_ptr(), down_t.scale.data_ptr(), _act(act), dx.data_ptr(),
                                            dwgu.data_ptr(), dwd.data_ptr(),

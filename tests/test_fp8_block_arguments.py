@@ -129,3 +129,36 @@ def test_block_can_be_copied(kept):
     ws = ffn.workspace(8)
     for other in (copy.deepcopy(ffn), pickle.loads(pickle.dumps(ffn))):
         assert torch.equal(other.down.codes, ffn.down.codes) and other.workspace(8).data_ptr() != ws.data_ptr()
+
+
+# ---- scales that change ------------------------------------------------------------------------------------------------
+def test_promise_ends_with_a_write(monkeypatch):
+    """What is known of scales holds until they are written to, or others take their place."""
+    monkeypatch.setattr(binding, "_capturing", lambda: False, raising=False)
+    P2 = binding.SCALES_POW2
+    writes = [lambda t: t.mul_(1.5), lambda t: t.copy_(torch.full_like(t, 3.0)), lambda t: t[0].fill_(0.7), lambda t: t.view(-1).add_(1)]
+    for write in writes:
+        w, q = weight(128, 128, pow2=True), binding.Fp8Block(torch.zeros((4, 128), dtype=u8), torch.ones((1, 4)), True)
+        down = weight(128, 128, pow2=True)
+        assert binding._scales("M1", w, None) == binding.SCALE_M1 | P2 and binding._scales("none", w, q) == P2
+        write(q.scale)
+        assert not q.pow2 and binding._scales("none", w, q) == 0
+        q.pow2 = True  # told anew
+        assert binding._scales("none", w, q) == P2
+        write(w.scale)
+        assert not w.pow2 and binding._scales("M1", w, None) == binding.SCALE_M1 and binding._scales("none", w, q) == 0
+        assert binding._ffn_scales("M1", down, w) == binding.SCALE_M1 and binding._ffn_scales("M1", w, down) == binding.SCALE_M1
+        w.scale = torch.ones((1, 1))
+        w.pow2 = True
+        assert binding._ffn_scales("M1", down, w) == binding.SCALE_M1 | P2
+        w.scale = torch.full((1, 1), 1.5)
+        assert not w.pow2
+        q.scale = torch.full((1, 4), 1.5)
+        assert not q.pow2
+
+
+def test_promise_in_inference_mode():
+    with torch.inference_mode():
+        w = weight(128, 128, pow2=True)
+        assert binding._scales("M1", w, None) == binding.SCALE_M1 | binding.SCALES_POW2
+    assert w.pow2 is True

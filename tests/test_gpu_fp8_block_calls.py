@@ -84,3 +84,36 @@ def test_threads_on_one_stream():
     for i in range(2):
         assert len(got[i]) == 200
         assert all(torch.equal(a, b) for pair in got[i] for a, b in zip(pair, want[i]))
+
+
+def test_scales_written_in_place():
+    """Scales that were powers of two and are no more, and back: every call multiplies by the scales of its time."""
+    M, K, N = 300, 528, 400
+    x = acts(1, M, K)
+    w, _ = weight(2, N, K, "M1")
+    xv, xt = R.rows_values(*R.quantize_rows(x, "M1")), bf16_tensor(x)
+    pow2 = w.scale.clone()
+    first = binding.fp8_block_linear(w, x=xt, mode="M1", out_dtype=torch.bfloat16)
+    for factor in (1.5, 0.3, 1.0):
+        w.scale.copy_(pow2 * factor)
+        wv = R.blocks_values(w.codes.cpu().numpy(), w.scale.cpu().numpy())
+        y = binding.fp8_block_linear(w, x=xt, mode="M1", out_dtype=torch.bfloat16)
+        check_values(y, xv @ wv.T, (132 * ((K + 127) // 128) + 2) * 2.0 ** -23 * (np.abs(xv) @ np.abs(wv).T), True)
+        assert w.pow2 is (factor == 1.0)
+    assert torch.equal(y, first)
+
+
+def test_scales_looked_up_late():
+    """A weight wrapped under stream capture waits for nothing; its scales are looked at by the first eager call that asks."""
+    M, K, N = 300, 528, 400
+    w0, _ = weight(2, N, K, "M1")
+    x = bf16_tensor(acts(1, M, K))
+    want = binding.fp8_block_linear(w0, x=x, mode="M1")
+    s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=s):
+        w = binding.Fp8Weight(w0.codes, w0.scale, N, K)
+        y = binding.fp8_block_linear(w, x=x, mode="M1")
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y, want) and w.pow2 is True
