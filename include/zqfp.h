@@ -346,8 +346,9 @@ int zq_w4a8_linear_noalloc_status(int* detail, void* stream);
  * where the call multiplies, may carry a promise: ZQ_SCALES_POW2 or'ed to it says that every scale the call is GIVEN, of
  * weights and of quantized activations, is a power of two (or NaN).  With many tokens and a bf16 or quantized result
  * the tensor core then applies the scales itself; the sums are the same up to the order and rounding of FP32
- * additions.  A broken promise gives wrong results.  With ZQ_SCALE_NONE and raw activations it is refused
- * (ZQ_ERR_MODE).  K (features) is a multiple of 16 throughout; codes are 16-byte aligned.
+ * additions.  Where it does so, a scale that breaks the promise makes the results it belongs to NaN (a zero stands for
+ * 2^-127).  With ZQ_SCALE_NONE and raw activations the promise is refused (ZQ_ERR_MODE).  K (features) is a multiple of 16
+ * throughout; codes are 16-byte aligned.
  */
 #define ZQ_SCALES_POW2 16
 

@@ -408,7 +408,12 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         const float* sb0 = p.sb + static_cast<int64_t>(KIND == kGated ? nt : 2 * nt) * p.kblocks;
         const float* sb1 = KIND == kGated ? sb0 + part : p.sb + static_cast<int64_t>(min(2 * nt + 1, p.nblocks - 1)) * p.kblocks;
         float a[kAhead][4], b[kAhead][2];  // (made bytes when they are used: nothing waits for a load before that)
-        auto byte4 = [](float v) { return ((__float_as_uint(v) >> 23) & 0xFFu) * 0x01010101u; };
+        // The exponent's byte, which is E8M0, four times.  A scale that is no power of two, against the caller's promise, shows as NaN
+        // (all bits set; infinities and NaN have that exponent anyway; a zero stands for 2^-127).
+        auto byte4 = [](float v) {
+          const uint32_t b = __float_as_uint(v);
+          return (b & 0x807FFFFFu) != 0u ? 0xFFFFFFFFu : __byte_perm(b << 1, 0u, 0x3333);
+        };
         const float* sa = p.sa + m0;
         auto fetch = [&](int i, int slot) {  // called for i = 0, 1, 2, ...
           if (KIND == kPlain && i == p.kblocks) {  // the second segment

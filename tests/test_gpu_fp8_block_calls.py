@@ -117,3 +117,19 @@ def test_scales_looked_up_late():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(y, want) and w.pow2 is True
+
+
+@pytest.mark.parametrize("bad", [1.5, -2.0, 2.0 ** -130, float("inf")])
+def test_broken_promise_shows(bad):
+    """A scale that is no power of two where one was promised: NaN in the results it belongs to, the others as they were."""
+    M, K, N = 300, 528, 400
+    w, _ = weight(2, N, K, "M1")
+    q = binding.quantize_fp8_block(bf16_tensor(acts(1, M, K)), "M1")
+    want = binding.fp8_block_linear(w, q=q, out_dtype=torch.bfloat16)
+    q.scale[3, 70] = bad
+    w.scale[1, 2] = bad
+    q.pow2 = w.pow2 = True
+    y = binding.fp8_block_linear(w, q=q, out_dtype=torch.bfloat16)
+    rows, cols = torch.arange(M, device=dev()) == 70, torch.arange(N, device=dev()) // 128 == 1
+    hit = rows[:, None] | cols[None, :]
+    assert torch.isnan(y[hit]).all() and torch.equal(y[~hit], want[~hit])
