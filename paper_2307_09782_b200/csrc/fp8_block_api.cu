@@ -210,7 +210,7 @@ int zq_fp8_weight_grad(const void* g_bf16, int64_t ldg, int64_t g_stride, int pa
                        size_t workspace_bytes, void* stream) {
   if (dwdt != ZQ_OUT_F32 && dwdt != ZQ_OUT_BF16) return ZQ_ERR_MODE;
   if (!rows_ok(M) || !rows_ok(N) || !k_ok(K) || ldg < N || parts < 1 || parts > 64 || g_stride < 0 ||
-      (parts > 1 && g_stride == 0))
+      (parts > 1 && g_stride == 0 && M > 0))
     return ZQ_ERR_SHAPE;
   if (N == 0) return ZQ_OK;
   if (!dw || (M > 0 && (!g_bf16 || !q || !s))) return ZQ_ERR_NULL;

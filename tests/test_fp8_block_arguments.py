@@ -162,3 +162,15 @@ def test_promise_in_inference_mode():
         w = weight(128, 128, pow2=True)
         assert binding._scales("M1", w, None) == binding.SCALE_M1 | binding.SCALES_POW2
     assert w.pow2 is True
+
+
+# ---- sizes ---------------------------------------------------------------------------------------------------------------
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are made up: only a machine without a GPU stops in time")
+def test_no_tokens_are_not_refused(L):
+    """The block's backward pass, and the weight gradient of several parts, of a batch without tokens: whatever stops them here, it
+    is not the sizes."""
+    P, K, F, N = 0x10000, 64, 32, 48
+    ws = binding.fp8_gated_ffn_workspace_bytes(0, K, F, N, True)
+    assert L.zq_fp8_gated_ffn_backward(None, N, 0, 0, K, F, N, None, None, None, None, None, 0, None, P, P, 1, P, ws, None) in (-6, -7)
+    assert L.zq_fp8_weight_grad(None, F, 0, 2, None, None, 0, F, K, P, 1, P, ws, None) in (-6, -7)
+    assert L.zq_fp8_weight_grad(P, F, 0, 2, P, P, 1, F, K, P, 1, P, ws, None) == -2  # with tokens: all parts in one place

@@ -133,3 +133,27 @@ def test_broken_promise_shows(bad):
     rows, cols = torch.arange(M, device=dev()) == 70, torch.arange(N, device=dev()) // 128 == 1
     hit = rows[:, None] | cols[None, :]
     assert torch.isnan(y[hit]).all() and torch.equal(y[~hit], want[~hit])
+
+
+@pytest.mark.parametrize("mode", ["none", "M1"])
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+def test_no_tokens(mode, out):
+    """An empty batch through every call: results without rows, weight gradients of zeros."""
+    K, F, N = 144, 272, 160
+    W = [torch.randn(s, device=dev()) for s in ((F, K), (F, K), (N, F))]
+    ffn = gated_ffn.GatedFfnFp8.from_weights(*W, mode=mode, training=True)
+    x, dy = (torch.empty((0, n), dtype=torch.bfloat16, device=dev()) for n in (K, N))
+    assert ffn.forward(x, out_dtype=out).shape == (0, N)
+    y, saved = ffn.forward_train(x, out_dtype=out)
+    torch.full((1 << 16,), 7.0, device=dev())  # what the next results' memory may hold
+    dx, dgu, dd = ffn.backward(dy, saved, out_dtype=out)
+    assert y.shape == (0, N) and dx.shape == (0, K)
+    assert dgu.shape == (2, F, K) and not dgu.any() and dd.shape == (N, F) and not dd.any()
+    q = binding.quantize_fp8_block(x, mode)
+    h, hq, gu = binding.fp8_gated_linear(ffn.gate_up, q=q, mode=mode, quantized=True, checkpoint=True)
+    assert h.shape == (0, F) and hq.codes.shape == (0, F) and gu.codes.shape == (2, 0, F)
+    d, dq = binding.fp8_gated_linear_backward(ffn.down_t, gu, dy=dy, mode=mode)
+    assert d.shape == (2, 0, F) and dq.scale.shape == (2, 3, 0)
+    dw = binding.fp8_weight_grad(d, q, out_dtype=out)
+    assert dw.shape == (2, F, K) and not dw.any()
+    assert binding.fp8_block_linear(ffn.gate_up_t, q=dq, out_dtype=out).shape == (0, K)
