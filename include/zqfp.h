@@ -424,8 +424,8 @@ int zq_fp8_gated_linear_backward(const uint8_t* q, const float* s, const void* d
 /*
  * Weight gradient from an 8-bit activation checkpoint:  dW[p][n, k] = sum_m G[p][m, n] bf16(code[m, k] s[k/128, m])
  * (the rounding to bf16 is none with power-of-two scales), summed in FP32.
- * G    : bf16, parts (1 .. 64) matrices [M, ldg], g_stride elements apart (not 0 with several of them and M > 0); ldg >= N; ldg and
- *        g_stride multiples of 8
+ * G    : bf16, parts (1 .. 64) matrices [M, ldg], g_stride elements apart (not looked at with one; not 0 with several and
+ *        M > 0); ldg >= N; ldg and g_stride multiples of 8
  * q, s : the checkpoint, [M, K] and [ceil(K/128), M]
  * dw   : out, [parts][N, K] dense, FP32 or bf16, 16-byte aligned; any N.  M == 0 gives zeros.
  */

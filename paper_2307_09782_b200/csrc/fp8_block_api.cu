@@ -209,6 +209,7 @@ int zq_fp8_weight_grad(const void* g_bf16, int64_t ldg, int64_t g_stride, int pa
                        int64_t M, int64_t N, int64_t K, void* dw, zq_out_dtype dwdt, void* workspace,
                        size_t workspace_bytes, void* stream) {
   if (dwdt != ZQ_OUT_F32 && dwdt != ZQ_OUT_BF16) return ZQ_ERR_MODE;
+  if (parts == 1) g_stride = 0;  // there is no next matrix
   if (!rows_ok(M) || !rows_ok(N) || !k_ok(K) || ldg < N || parts < 1 || parts > 64 || g_stride < 0 ||
       (parts > 1 && g_stride == 0 && M > 0))
     return ZQ_ERR_SHAPE;

@@ -174,3 +174,12 @@ def test_no_tokens_are_not_refused(L):
     assert L.zq_fp8_gated_ffn_backward(None, N, 0, 0, K, F, N, None, None, None, None, None, 0, None, P, P, 1, P, ws, None) in (-6, -7)
     assert L.zq_fp8_weight_grad(None, F, 0, 2, None, None, 0, F, K, P, 1, P, ws, None) in (-6, -7)
     assert L.zq_fp8_weight_grad(P, F, 0, 2, P, P, 1, F, K, P, 1, P, ws, None) == -2  # with tokens: all parts in one place
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are made up: only a machine without a GPU stops in time")
+def test_one_matrix_has_no_stride(L):
+    """Of one gradient matrix nothing is refused for where a second one would be."""
+    P, ws = 0x10000, binding.fp8_block_linear_workspace_bytes(0, 0, 16)
+    for stride in (0, 20, 21, -8):
+        assert L.zq_fp8_weight_grad(P, 24, stride, 1, P, P, 1, 20, 64, P, 0, P, ws, None) in (-6, -7)
+    assert L.zq_fp8_weight_grad(P, 24, 20, 2, P, P, 1, 20, 64, P, 0, P, ws, None) == -3

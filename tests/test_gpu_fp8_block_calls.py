@@ -157,3 +157,12 @@ def test_no_tokens(mode, out):
     dw = binding.fp8_weight_grad(d, q, out_dtype=out)
     assert dw.shape == (2, F, K) and not dw.any()
     assert binding.fp8_block_linear(ffn.gate_up_t, q=dq, out_dtype=out).shape == (0, K)
+
+
+def test_weight_grad_of_one_token():
+    """One token whose outputs are no multiple of eight, as a matrix and as a stack of one."""
+    g = torch.randn((1, 20), device=dev()).to(torch.bfloat16)
+    q = binding.quantize_fp8_block(torch.randn((1, 144), device=dev()).to(torch.bfloat16), "M1")
+    dw = binding.fp8_weight_grad(g, q)
+    assert torch.equal(dw, g.float().T @ q.values())  # one product each: exact
+    assert torch.equal(binding.fp8_weight_grad(g[None], q), dw[None])
