@@ -36,6 +36,7 @@
 // Persistent: one CTA per SM (MX: one pair per two) walks the tiles, blockIdx.x, + gridDim.x, ..., token tiles in groups so that
 // the CTAs running at one time share operands in L2.
 #include "fp8_block.cuh"
+#include "fp8_index.h"
 
 namespace zq {
 namespace fp8b {
@@ -625,7 +626,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
             }
             stage_put(buf, lane, j, v);
           }
-          store_rows<8, ES>(buf, yb + c * 128, p.ldy * ES, rows, min(128, (p.N - n0 - c * kCols) * ES), p.y_vec != 0, lane);
+          store_rows<8, ES>(buf, yb + c * 128, p.ldy * ES, rows, row_bytes(p.N - n0 - c * kCols, kCols, ES), p.y_vec != 0, lane);
         }
       } else if (KIND == kGated) {
         const int n0 = nt * kBlk + half * 64;
@@ -690,7 +691,7 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
             stage_put(buf, lane, j, make_uint4(pack_bf16(g[8 * j], g[8 * j + 1]), pack_bf16(g[8 * j + 2], g[8 * j + 3]),
                                                pack_bf16(g[8 * j + 4], g[8 * j + 5]), pack_bf16(g[8 * j + 6], g[8 * j + 7])));
           store_rows<8, 2>(buf, static_cast<uint8_t*>(p.y) + (static_cast<int64_t>(wm0) * p.ldy + n0) * 2, p.ldy * 2, rows,
-                           min(128, cols * 2), p.y_vec != 0, lane);
+                           row_bytes(cols, 64, 2), p.y_vec != 0, lane);
         }
       } else {  // kGatedBwd
         const int fb = 2 * nt + half;

@@ -19,5 +19,9 @@ ZQ_HOST_DEVICE int stage_token(int step0, int i, int steps, int row, int M) {
   return m < M ? m : -1;
 }
 
+// Bytes of the part of a row that starts `left` elements of `size` bytes before the row's end (none are left where it is
+// negative) and has `most` elements at the most.  Elements are compared, not bytes: 2^29 of four bytes do not fit 32 bits.
+ZQ_HOST_DEVICE int row_bytes(int left, int most, int size) { return (left < most ? left : most) * size; }
+
 }  // namespace fp8b
 }  // namespace zq

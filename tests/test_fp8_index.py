@@ -47,3 +47,19 @@ def test_chained_kernels_load_through_l2():
     text = open(os.path.join(CSRC, "fp8_block_quant.cu")).read()
     chained = text[text.index("\nquantize_block_kernel("):text.index("// One CTA per 128 x 128 block")]
     assert "__ldg(" not in chained and "__restrict__" not in chained and "pdl_wait();" in chained
+
+
+def test_row_bytes(tmp_path):
+    """Rows of up to 2^31 elements: whole pieces as long as there are enough left (their bytes, counted first, overflowed from
+    2^29 elements of four bytes on, and nothing was stored)."""
+    body = """
+  const int lefts[] = {0, 1, 31, 32, 33, 63, 64, 65, 1 << 28, 1 << 29, (1 << 29) + 1, 1 << 30, 0x7FFFFF00};
+  for (int left : lefts) {
+    if (row_bytes(left, 32, 4) != (left < 32 ? left * 4 : 128)) return 1;
+    if (row_bytes(left, 64, 2) != (left < 64 ? left * 2 : 128)) return 2;
+    if (left > 0 && left < 128 && row_bytes(-left, 64, 2) > 0) return 3;
+  }"""
+    run(tmp_path, body)
+    # and the kernel counts them this way
+    text = open(os.path.join(CSRC, "fp8_block_gemm.cu")).read()
+    assert text.count("row_bytes(") == 2 and "cols * 2" not in text

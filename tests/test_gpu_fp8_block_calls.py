@@ -166,3 +166,28 @@ def test_weight_grad_of_one_token():
     dw = binding.fp8_weight_grad(g, q)
     assert torch.equal(dw, g.float().T @ q.values())  # one product each: exact
     assert torch.equal(binding.fp8_weight_grad(g[None], q), dw[None])
+
+
+def test_outputs_beyond_32_bits_of_bytes():
+    """2^29 outputs per token in FP32: the first ones, the last ones and those around multiples of 2^29 bytes are there."""
+    M, K, N = 33, 16, (1 << 29) + 40
+    if torch.cuda.mem_get_info()[0] < 120 << 30:
+        pytest.skip("needs 85 GB")
+    probe = torch.tensor([0, 1, 127, 255, 256, 1 << 27, (1 << 28) + 3, (1 << 29) - 1, 1 << 29, N - 1], device=dev())
+    codes = torch.full((N, K), 0x38, dtype=torch.uint8, device=dev())  # ones
+    codes[probe] = torch.from_numpy(R.e4m3_round(np.random.default_rng(0).integers(-3, 4, (len(probe), K)).astype(np.float32))).to(dev())
+    w = binding.Fp8Weight(codes, torch.ones(((N + 127) // 128, 1), device=dev()), N, K, pow2=False)
+    q = binding.quantize_fp8_block(torch.randint(-3, 4, (M, K), device=dev()).to(torch.bfloat16), "M1")
+    y = torch.full((M, N), -1000.0, device=dev())
+    binding.fp8_block_linear(w, q=q, y=y)
+    torch.cuda.synchronize()
+    xv = q.values()
+    assert torch.equal(y[:, probe], xv @ codes[probe].view(torch.float8_e4m3fn).float().T)
+    step = 1 << 26
+    row_sums = xv.sum(1)
+    other = torch.ones(N, dtype=torch.bool, device=dev())
+    other[probe] = False
+    for n0 in range(0, N, step):
+        part, keep = y[:, n0:n0 + step], other[n0:n0 + step]
+        for m in (0, 7, 32):
+            assert bool((part[m] == row_sums[m])[keep].all()), (m, n0)
