@@ -572,6 +572,8 @@ def _fp8_workspace(workspace, M: int, K: int, device):
     CUDA graph gets one of its own, in the graph's memory: a graph lasts longer than a kept one, which is given back when it
     has to grow, and may be replayed on any stream."""
     if workspace is not None:
+        _expect(workspace, torch.uint8, "workspace")
+        _on_gpu(workspace)
         return workspace
     need = _fp8_workspace_need(M, K)
     if _capturing():
@@ -595,9 +597,8 @@ def fp8_block_linear(w: Fp8Weight, *, x=None, q: Optional[Fp8Block] = None, mode
         y = w.scale.new_empty((M, w.N), dtype=out_dtype)
     elif y.shape != (M, w.N) or (w.N > 1 and y.stride(1) != 1):
         raise ValueError(f"y: a [{M}, {w.N}] matrix with contiguous rows is needed")
-    if workspace is None:
-        workspace = _fp8_workspace(None, M, w.K, w.codes.device)
-    _on_gpu(y, workspace)
+    workspace = _fp8_workspace(workspace, M, w.K, w.codes.device)
+    _on_gpu(y)
     _check(lib().zq_fp8_block_linear(_ptr(codes), _ptr(scale), _ptr(x), ldx, _scales(mode, w, q), w.parts, M, w.N, w.K,
                                      _ptr(w.codes), _ptr(w.scale), _ptr(y), ydt, y.stride(0) if M > 1 else w.N,
                                      _ptr(workspace), workspace.numel(), _stream()), "zq_fp8_block_linear")
@@ -673,8 +674,7 @@ def fp8_weight_grad(g: torch.Tensor, q: Fp8Block, *, out_dtype=torch.float32,
     if Mq != M:
         raise ValueError(f"g has {M} rows, the checkpoint {Mq}")
     dw = g.new_empty((parts, N, K) if g.dim() == 3 else (N, K), dtype=out_dtype)
-    if workspace is None:
-        workspace = _fp8_workspace(None, 0, 16, g.device)
+    workspace = _fp8_workspace(workspace, 0, 16, g.device)
     _check(lib().zq_fp8_weight_grad(_ptr(g), ldg, g.stride(0) if g.dim() == 3 else 0, parts, _ptr(codes), _ptr(scale),
                                     M, N, K, _ptr(dw), dwdt, _ptr(workspace), workspace.numel(), _stream()), "zq_fp8_weight_grad")
     return dw
@@ -699,7 +699,8 @@ def fp8_gated_ffn(gate_up: Fp8Weight, down: Fp8Weight, x: torch.Tensor, *, act="
     if gate_up.parts != 2 or down.parts != 1 or gate_up.K != K or down.K != F:
         raise ValueError(f"x [{M}, {K}], gate_up {gate_up.parts} x [{F}, {gate_up.K}] and down [{N}, {down.K}] do not belong "
                          "together")
-    _on_gpu(x, gate_up.codes, gate_up.scale, down.codes, down.scale)
+    _expect(workspace, torch.uint8, "workspace")
+    _on_gpu(x, gate_up.codes, gate_up.scale, down.codes, down.scale, workspace)
     y = torch.empty((M, N), dtype=out_dtype, device=x.device)
     saved = torch.empty((fp8_gated_ffn_saved_bytes(M, K, F),), dtype=torch.uint8, device=x.device) if save else None
     _check(lib().zq_fp8_gated_ffn(x.data_ptr(), ldx, _ffn_scales(mode, gate_up, down), M, K, F, N, gate_up.codes.data_ptr(),
@@ -723,7 +724,8 @@ def fp8_gated_ffn_backward(gate_up_t: Fp8Weight, down_t: Fp8Weight, dy: torch.Te
     _expect(saved, torch.uint8, "saved")
     if saved.numel() != fp8_gated_ffn_saved_bytes(M, K, F):
         raise ValueError(f"what was saved ({saved.numel()} bytes) is not of {M} tokens")
-    _on_gpu(dy, saved, gate_up_t.codes, gate_up_t.scale, down_t.codes, down_t.scale)
+    _expect(workspace, torch.uint8, "workspace")
+    _on_gpu(dy, saved, gate_up_t.codes, gate_up_t.scale, down_t.codes, down_t.scale, workspace)
     dev = dy.device
     dx = torch.empty((M, K), dtype=out_dtype, device=dev)
     dwgu = torch.empty((2, F, K), dtype=out_dtype, device=dev)

@@ -183,3 +183,12 @@ def test_one_matrix_has_no_stride(L):
     for stride in (0, 20, 21, -8):
         assert L.zq_fp8_weight_grad(P, 24, stride, 1, P, P, 1, 20, 64, P, 0, P, ws, None) in (-6, -7)
     assert L.zq_fp8_weight_grad(P, 24, 20, 2, P, P, 1, 20, 64, P, 0, P, ws, None) == -3
+
+
+# ---- the caller's workspace ----------------------------------------------------------------------------------------------
+def test_callers_workspace(kept):
+    """Bytes in one piece, in the GPU's memory: its length is taken for granted in the library."""
+    for ws, what in ((torch.zeros(1 << 20, dtype=u8), "CUDA"), (torch.zeros(1 << 20), "workspace"),
+                     (torch.zeros(1, dtype=u8).expand(1 << 20), "workspace"), (torch.zeros(1 << 20, dtype=u8)[::2], "workspace")):
+        with pytest.raises(ValueError, match=what):
+            binding._fp8_workspace(ws, 4, 64, kept)

@@ -191,3 +191,27 @@ def test_outputs_beyond_32_bits_of_bytes():
         part, keep = y[:, n0:n0 + step], other[n0:n0 + step]
         for m in (0, 7, 32):
             assert bool((part[m] == row_sums[m])[keep].all()), (m, n0)
+
+
+def test_callers_workspace_refusals():
+    """A workspace in host memory, of another type or not in one piece, in every call that takes one."""
+    K, F, M = 144, 272, 8
+    W = [torch.randn(s, device=dev()) for s in ((F, K), (F, K), (K, F))]
+    ffn = gated_ffn.GatedFfnFp8.from_weights(*W, training=True)
+    x = torch.randn((M, K), device=dev()).to(torch.bfloat16)
+    y, saved = ffn.forward_train(x)
+    q = binding.quantize_fp8_block(x)
+    _, hq, gu = binding.fp8_gated_linear(ffn.gate_up, q=q, quantized=True, checkpoint=True)
+    calls = [lambda ws: binding.fp8_block_linear(ffn.down, q=hq, workspace=ws),
+             lambda ws: binding.fp8_gated_linear(ffn.gate_up, x=x, workspace=ws),
+             lambda ws: binding.fp8_gated_linear_backward(ffn.down_t, gu, dy=x, workspace=ws),
+             lambda ws: binding.fp8_weight_grad(x, q, workspace=ws),
+             lambda ws: binding.fp8_gated_ffn(ffn.gate_up, ffn.down, x, workspace=ws),
+             lambda ws: binding.fp8_gated_ffn_backward(ffn.gate_up_t, ffn.down_t, x, saved, workspace=ws)]
+    n = 1 << 20
+    for ws in (torch.zeros(n, dtype=torch.uint8), torch.zeros(n, device=dev()),
+               torch.zeros(1, dtype=torch.uint8, device=dev()).expand(n), torch.zeros(n, dtype=torch.uint8, device=dev())[::2]):
+        for call in calls:
+            with pytest.raises(ValueError):
+                call(ws)
+    assert torch.equal(ffn.forward(x), y)
