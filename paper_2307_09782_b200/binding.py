@@ -443,10 +443,18 @@ def _expect(t: torch.Tensor, dtype, name: str):
 
 
 def _on_gpu(*tensors: torch.Tensor):
-    """The library takes device pointers: a tensor in host memory must not get that far."""
+    """The library takes device pointers and launches on the current device: a tensor in host memory, or on another device,
+    must not get that far."""
+    here = -1
     for t in tensors:
-        if not t.is_cuda:
-            raise ValueError(f"a CUDA tensor is needed, got one of {tuple(t.shape)} on {t.device}")
+        d = t.get_device()  # -1: host memory
+        if d != here:
+            if d < 0:
+                raise ValueError(f"a CUDA tensor is needed, got one of {tuple(t.shape)} on {t.device}")
+            here = torch._C._cuda_getDevice()
+            if d != here:
+                raise ValueError(f"a tensor of {tuple(t.shape)} is on cuda:{d}, the current device is cuda:{here}: call under "
+                                 f"torch.cuda.device({d}), with all tensors there")
 
 
 def _rows(x: torch.Tensor, name: str) -> int:

@@ -17,8 +17,8 @@ class GatedFfnFp8:
 
     ``mode``: how activations are scaled, "none" (FP32 scales) or "M1" (powers of two, which the 8-bit checkpoints
     turn back into bf16 without rounding: the one to train with).  ``training`` lays the transposed weights out as well.
-    A block keeps one workspace per thread, stream and device it is used on, grown on demand; a call that is captured into a CUDA graph
-    gets one of its own, in the graph's memory.
+    A block is used on the device of its weights, which has to be the current one.  It keeps one workspace per thread and stream,
+    grown on demand; a call that is captured into a CUDA graph gets one of its own, in the graph's memory.
     """
 
     def __init__(self, gate_up: Fp8Weight, down: Fp8Weight, act: str = "silu", mode: str = "none", training: bool = False):
@@ -47,7 +47,7 @@ class GatedFfnFp8:
     def workspace(self, M: int) -> torch.Tensor:
         if binding._capturing():
             return self._new_workspace(M)
-        key = (self.down.codes.device, binding._stream())
+        key = self.down.codes.device.index, binding._stream()
         kept = self._workspaces.of
         ws, rows = kept.get(key, (None, -1))
         if rows < M:

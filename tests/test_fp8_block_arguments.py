@@ -192,3 +192,21 @@ def test_callers_workspace(kept):
                      (torch.zeros(1, dtype=u8).expand(1 << 20), "workspace"), (torch.zeros(1 << 20, dtype=u8)[::2], "workspace")):
         with pytest.raises(ValueError, match=what):
             binding._fp8_workspace(ws, 4, 64, kept)
+
+
+class On:
+    """A tensor as far as its place goes."""
+
+    def __init__(self, d):
+        self.device, self.shape, self.is_cuda, self.get_device = torch.device("cuda", d), (2, 3), True, lambda: d
+
+
+def test_other_devices_are_refused(monkeypatch):
+    """Kernels run on the current device and its stream: all tensors have to be there."""
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
+    binding._on_gpu(On(1), On(1))
+    for tensors in ((On(0), On(0)), (On(1), On(0)), (On(0), On(1)), (On(1), On(1), On(2))):
+        with pytest.raises(ValueError, match="current device is cuda:1"):
+            binding._on_gpu(*tensors)
+    with pytest.raises(ValueError, match="CUDA tensor"):
+        binding._on_gpu(On(1), torch.zeros(1))
