@@ -445,7 +445,7 @@ def _expect(t: torch.Tensor, dtype, name: str):
 def _on_gpu(*tensors: torch.Tensor):
     """The library takes device pointers and launches on the current device: a tensor in host memory, or on another device,
     must not get that far."""
-    here = -1
+    here = None
     for t in tensors:
         d = t.get_device()  # -1: host memory
         if d != here:
