@@ -7,7 +7,6 @@
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
-#include <mutex>
 
 #include "act_cast.cuh"
 #include "zq_common.cuh"
@@ -429,13 +428,9 @@ cudaError_t launch_tile(const void* x, int64_t M, int64_t K, int64_t ldx, int ve
                         const void* V, float* t, cudaStream_t st) {
   auto kernel = act_quant_tile_kernel<HAS_V, C>;
   const size_t smem = static_cast<size_t>(kRows) * (vec_per_cta + kTilePadVec) * sizeof(uint4);
-  static std::once_flag once;
-  static cudaError_t attr_err = cudaSuccess;
-  std::call_once(once, [&] {
-    attr_err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    kRows * (kTileMaxVec + kTilePadVec) * static_cast<int>(sizeof(uint4)));
-  });
-  if (attr_err != cudaSuccess) return attr_err;
+  static DeviceOnce once;
+  if (!allow_shared_memory(once, kernel, kRows * (kTileMaxVec + kTilePadVec) * static_cast<int>(sizeof(uint4))))
+    return cudaErrorInvalidValue;
   dim3 grid(C, static_cast<unsigned>((M + kRows - 1) / kRows));
   return launch_chained(kernel, grid, dim3(kTileThreads), smem, st, false, static_cast<const uint4*>(x),
                         static_cast<int>(M), static_cast<int>(K), ldx / 8, vec_per_cta, q, sx,

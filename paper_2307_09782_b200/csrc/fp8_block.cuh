@@ -6,8 +6,6 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include <mutex>
-
 #include "act_cast.cuh"
 #include "w4a8_gemm_shared.cuh"
 

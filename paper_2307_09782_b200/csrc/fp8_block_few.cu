@@ -489,13 +489,8 @@ fp8_block_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
 template <int BM, bool GATED, bool RAW>
 int launch_cfg(const CUtensorMap& tw, const CUtensorMap& tq, const PF& p, int m_tiles, cudaStream_t st) {
   using C = FewCfg<BM, GATED>;
-  static std::once_flag once;
-  static cudaError_t attr_err = cudaSuccess;
-  std::call_once(once, [] {
-    attr_err = cudaFuncSetAttribute(fp8_block_few_kernel<BM, GATED, RAW>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    C::kSmemBytes);
-  });
-  if (attr_err != cudaSuccess) return ZQ_ERR_CUDA;
+  static DeviceOnce once;
+  if (!allow_shared_memory(once, fp8_block_few_kernel<BM, GATED, RAW>, C::kSmemBytes)) return ZQ_ERR_CUDA;
   const cudaError_t e = launch_clustered(fp8_block_few_kernel<BM, GATED, RAW>,
                                          dim3(static_cast<unsigned>(p.n_tiles * p.cluster), static_cast<unsigned>(m_tiles)),
                                          dim3(C::kThreads), C::kSmemBytes, st, p.cluster, tw, tq, p);

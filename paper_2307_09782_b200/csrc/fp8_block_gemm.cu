@@ -849,12 +849,8 @@ fp8_block_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
 
 template <int KIND, int ACT, bool F32, bool MX>
 int launch_cfg(const CUtensorMap& ta, const CUtensorMap& tb, const P8& p, cudaStream_t st) {
-  static std::once_flag once;
-  static cudaError_t attr = cudaSuccess;
-  std::call_once(once, [] {
-    attr = cudaFuncSetAttribute(fp8_block_gemm_kernel<KIND, ACT, F32, MX>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-  });
-  if (attr != cudaSuccess) return ZQ_ERR_CUDA;
+  static DeviceOnce once;
+  if (!allow_shared_memory(once, fp8_block_gemm_kernel<KIND, ACT, F32, MX>, kSmemBytes)) return ZQ_ERR_CUDA;
   const int tiles = p.m_tiles * p.n_tiles, slots = MX ? sm_count() / 2 : sm_count();
   const unsigned grid = (MX ? 2u : 1u) * static_cast<unsigned>(tiles < slots ? tiles : slots);
   const cudaError_t e = launch_clustered(fp8_block_gemm_kernel<KIND, ACT, F32, MX>, dim3(grid), dim3(threads_of(MX)), kSmemBytes, st, MX ? 2 : 1,

@@ -445,12 +445,8 @@ bool make_grad_map(CUtensorMap* m, const WgradArgs& a) {
 
 template <bool F32>
 int launch_cfg(const CUtensorMap& tg, const CUtensorMap& tx, const PW& p, unsigned grid, cudaStream_t st) {
-  static std::once_flag once;
-  static cudaError_t attr = cudaSuccess;
-  std::call_once(once, [] {
-    attr = cudaFuncSetAttribute(fp8_wgrad_kernel<F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-  });
-  if (attr != cudaSuccess) return ZQ_ERR_CUDA;
+  static DeviceOnce once;
+  if (!allow_shared_memory(once, fp8_wgrad_kernel<F32>, kSmemBytes)) return ZQ_ERR_CUDA;
   const cudaError_t e = launch_clustered(fp8_wgrad_kernel<F32>, dim3(grid), dim3(kThreads), kSmemBytes, st, p.cluster, tg, tx, p);
   count_launch();
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;

@@ -589,13 +589,8 @@ int launch_cfg(const GemmArgs& a, const GemmPlan& plan, const Params& p, cudaStr
   if (!make_map(&tm_q, a.q, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.M), kBlockK, BM,
                 CU_TENSOR_MAP_SWIZZLE_128B))
     return ZQ_ERR_CUDA;
-  static std::once_flag once;
-  static cudaError_t attr_err = cudaSuccess;
-  std::call_once(once, [] {
-    attr_err = cudaFuncSetAttribute(w4a8_gemm_kernel<BM, NONE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    C::kSmemBytes);
-  });
-  if (attr_err != cudaSuccess) return ZQ_ERR_CUDA;
+  static DeviceOnce once;
+  if (!allow_shared_memory(once, w4a8_gemm_kernel<BM, NONE>, C::kSmemBytes)) return ZQ_ERR_CUDA;
   if (p.atomic_y &&
       cudaMemset2DAsync(a.y, static_cast<size_t>(a.ldy) * 4, 0, static_cast<size_t>(a.N) * 4, static_cast<size_t>(a.M),
                         st) != cudaSuccess)

@@ -1176,13 +1176,8 @@ int launch_mx_cfg(const GemmArgs& a, const GemmPlan& plan, const Params& p, cuda
   if (!make_weight_map(&tm_w, a.codes, static_cast<uint64_t>(plan.n_tiles), static_cast<uint64_t>(p.kblocks), C::kKps, W8) ||
       !make_token_map(&tm_q, a.q, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.M), BM, C::kKps))
     return ZQ_ERR_CUDA;
-  static std::once_flag once;
-  static cudaError_t attr_err = cudaSuccess;
-  std::call_once(once, [] {
-    attr_err = cudaFuncSetAttribute(w4a8_mx_gemm_kernel<BM, W8, FUSEQ, NONE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    C::kSmemBytes);
-  });
-  if (attr_err != cudaSuccess) return ZQ_ERR_CUDA;
+  static DeviceOnce once;
+  if (!allow_shared_memory(once, w4a8_mx_gemm_kernel<BM, W8, FUSEQ, NONE>, C::kSmemBytes)) return ZQ_ERR_CUDA;
   dim3 grid(static_cast<unsigned>(plan.ctas));
   const bool fused_out = a.relu || a.y_amax;  // final values must be known to one CTA: no adding into y
   const bool shared_f32 =
@@ -1250,21 +1245,22 @@ template <int BM, bool W8>
 int launch_pair_cfg(const GemmArgs& a, const GemmPlan& plan, Params p, cudaStream_t st) {
   using C = PairCfg<BM, W8>;
   auto kernel = w4a8_mx_pair_gemm_kernel<BM, W8>;
-  static std::once_flag once;
-  static cudaError_t attr_err = cudaSuccess;
-  static int max_pairs = 0;
-  std::call_once(once, [&] {
-    attr_err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
-    if (attr_err == cudaSuccess) {
-      cudaLaunchConfig_t cfg{};
-      cfg.gridDim = dim3(2 * sm_count());
-      cfg.blockDim = dim3(C::kThreads);
-      cfg.dynamicSmemBytes = C::kSmemBytes;
-      if (cudaOccupancyMaxActiveClusters(&max_pairs, kernel, &cfg) != cudaSuccess) max_pairs = 0;
-      (void)cudaGetLastError();
-    }
+  static DeviceOnce once, once_pairs;
+  static std::atomic<int> max_pairs{0};
+  int dev = 0;
+  if (!allow_shared_memory(once, kernel, C::kSmemBytes) || cudaGetDevice(&dev) != cudaSuccess) return kPairNotTaken;
+  once_pairs.run(dev, [&] {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(2 * sm_count());
+    cfg.blockDim = dim3(C::kThreads);
+    cfg.dynamicSmemBytes = C::kSmemBytes;
+    int pairs = 0;
+    if (cudaOccupancyMaxActiveClusters(&pairs, kernel, &cfg) != cudaSuccess) pairs = 0;
+    (void)cudaGetLastError();
+    max_pairs = pairs;
+    return true;
   });
-  if (attr_err != cudaSuccess || max_pairs < 1) return kPairNotTaken;
+  if (max_pairs < 1) return kPairNotTaken;
   CUtensorMap tm_w, tm_q, tm_sf;
   if (!make_weight_map(&tm_w, a.codes, static_cast<uint64_t>(plan.n_tiles), static_cast<uint64_t>(p.kblocks), 1, W8) ||
       !make_token_map(&tm_q, a.q, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.M), C::kHalf, 1) ||

@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "../../include/zqfp.h"
+#include "device_once.h"
 
 namespace zq {
 
@@ -137,6 +138,15 @@ bool exclusive_device();  // see zq_set_exclusive_device
 constexpr int kErrDetailSelfTest = 100;  // status detail written by zq_selftest_bounded_wait
 
 #ifdef __CUDACC__
+// Lets a kernel have `bytes` of dynamic shared memory on the current device; `once` belongs to that kernel.
+template <typename Kernel>
+inline bool allow_shared_memory(DeviceOnce& once, Kernel kernel, int bytes) {
+  int dev = 0;
+  return cudaGetDevice(&dev) == cudaSuccess && once.run(dev, [&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
+  });
+}
+
 // ---- programmatic dependent launch ---------------------------------------------------------------
 // The kernels of one layer (quantizer, then GEMM) and of consecutive layers are chained with programmatic
 // stream serialization: a kernel lets its successor start early (launch_dependents), and every kernel waits
