@@ -457,13 +457,15 @@ def _on_gpu(*tensors: torch.Tensor):
                                  f"torch.cuda.device({d}), with all tensors there")
 
 
-def _rows(x: torch.Tensor, name: str) -> int:
-    """The row stride of a bf16 matrix whose rows are contiguous."""
-    if x.dtype != torch.bfloat16 or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
-        raise ValueError(f"{name}: a bf16 matrix with contiguous rows is needed, got {x.dtype} {tuple(x.shape)}, "
-                         f"strides {x.stride()}")
-    M, K = x.shape
-    return x.stride(0) if M > 1 else (K + 7) // 8 * 8
+def _rows(x: torch.Tensor, name: str):
+    """(row stride, rows, columns) of a bf16 matrix whose rows are contiguous."""
+    if x.dtype is torch.bfloat16 and x.dim() == 2:
+        M, K = x.shape
+        ld, step = x.stride()
+        if step == 1 or K <= 1:
+            return ld if M > 1 else (K + 7) // 8 * 8, M, K
+    raise ValueError(f"{name}: a bf16 matrix with contiguous rows is needed, got {x.dtype} {tuple(x.shape)}, "
+                     f"strides {x.stride()}")
 
 
 def fp8_block_linear_workspace_bytes(M: int, N: int, K: int) -> int:
@@ -477,9 +479,8 @@ def _blocks(n: int) -> int:
 
 def quantize_fp8_block(x: torch.Tensor, mode="none") -> Fp8Block:
     """x: bf16 [M, K] (row stride allowed); ``mode`` "none" (FP32 scales) or "M1" (powers of two)."""
-    ldx = _rows(x, "x")
+    ldx, M, K = _rows(x, "x")
     _on_gpu(x)
-    M, K = x.shape
     q = x.new_empty((M, K), dtype=torch.uint8)
     s = x.new_empty(((K + 127) // 128, M), dtype=torch.float32)
     _check(lib().zq_quantize_fp8_block(_ptr(x), M, K, ldx, _mode(mode), _ptr(q), _ptr(s), _stream()),
@@ -518,23 +519,23 @@ def transpose_fp8_weight(w: Fp8Weight) -> Fp8Weight:
     return Fp8Weight(q, s, w.K, w.N, w.parts, w._known_pow2())
 
 
-def _activations(x, q, K: int, parts: int):
-    """(codes, scales, x, ldx, M) of an operand given raw (``x``) or quantized (``q``)."""
+def _activations(x, q, K: int, parts: int, *others: torch.Tensor):
+    """(codes, scales, x, ldx, M) of an operand given raw (``x``) or quantized (``q``); it and the ``others`` are on the GPU."""
     if (x is None) == (q is None):
         raise ValueError("give the activations either raw (x) or quantized (q)")
     if x is not None:
-        ldx = _rows(x, "x")
-        if x.shape[1] != K:
-            raise ValueError(f"x has {x.shape[1]} features, the weight {K}")
-        _on_gpu(x)
-        return None, None, x, ldx, x.shape[0]
+        ldx, M, features = _rows(x, "x")
+        if features != K:
+            raise ValueError(f"x has {features} features, the weight {K}")
+        _on_gpu(x, *others)
+        return None, None, x, ldx, M
     _expect(q.codes, torch.uint8, "q.codes")
     _expect(q.scale, torch.float32, "q.scale")
     M = q.codes.shape[-2]
     lead = (parts,) if parts > 1 else ()
     if tuple(q.codes.shape) != (*lead, M, K) or tuple(q.scale.shape) != (*lead, _blocks(K), M):
         raise ValueError(f"codes {tuple(q.codes.shape)} / scales {tuple(q.scale.shape)} do not fit {parts} x [M, {K}]")
-    _on_gpu(q.codes, q.scale)
+    _on_gpu(q.codes, q.scale, *others)
     return q.codes, q.scale, None, K, M
 
 
@@ -599,14 +600,14 @@ def fp8_block_linear(w: Fp8Weight, *, x=None, q: Optional[Fp8Block] = None, mode
     """y [M, N] = the linear layer; activations raw (bf16 ``x``, quantized with ``mode``) or quantized (``q``).  With
     ``w.parts`` = 2 the sum over two pairs of operands (``q`` then holds two as well)."""
     ydt = _out_type(out_dtype if y is None else y.dtype)
-    codes, scale, x, ldx, M = _activations(x, q, w.K, w.parts)
-    _on_gpu(w.codes, w.scale)
+    codes, scale, x, ldx, M = _activations(x, q, w.K, w.parts, w.codes, w.scale)
     if y is None:
         y = w.scale.new_empty((M, w.N), dtype=out_dtype)
-    elif y.shape != (M, w.N) or (w.N > 1 and y.stride(1) != 1):
-        raise ValueError(f"y: a [{M}, {w.N}] matrix with contiguous rows is needed")
+    else:
+        if y.shape != (M, w.N) or (w.N > 1 and y.stride(1) != 1):
+            raise ValueError(f"y: a [{M}, {w.N}] matrix with contiguous rows is needed")
+        _on_gpu(y)
     workspace = _fp8_workspace(workspace, M, w.K, w.codes.device)
-    _on_gpu(y)
     _check(lib().zq_fp8_block_linear(_ptr(codes), _ptr(scale), _ptr(x), ldx, _scales(mode, w, q), w.parts, M, w.N, w.K,
                                      _ptr(w.codes), _ptr(w.scale), _ptr(y), ydt, y.stride(0) if M > 1 else w.N,
                                      _ptr(workspace), workspace.numel(), _stream()), "zq_fp8_block_linear")
@@ -623,8 +624,7 @@ def fp8_gated_linear(w: Fp8Weight, *, x=None, q: Optional[Fp8Block] = None, act=
     h quantized | None, g and u quantized ([2, M, F]) | None) as asked for by ``bf16``, ``quantized``, ``checkpoint``."""
     if w.parts != 2:
         raise ValueError("the gated layer takes the stacked (gate, up) weights: parts = 2")
-    codes, scale, x, ldx, M = _activations(x, q, w.K, 1)
-    _on_gpu(w.codes, w.scale)
+    codes, scale, x, ldx, M = _activations(x, q, w.K, 1, w.codes, w.scale)
     F, dev, fb = w.N, w.codes.device, _blocks(w.N)
     h = torch.empty((M, F), dtype=torch.bfloat16, device=dev) if bf16 else None
     hq = gu = None
@@ -648,8 +648,7 @@ def fp8_gated_linear_backward(wt: Fp8Weight, gu: Fp8Block, *, dy=None, q: Option
     projection ``wt`` and the checkpoint ``gu``.  Returns (bf16 [2, M, F], the same quantized)."""
     if wt.parts != 1:
         raise ValueError("the backward pass takes one transposed down projection: parts = 1")
-    codes, scale, dy, lddy, M = _activations(dy, q, wt.K, 1)
-    _on_gpu(wt.codes, wt.scale, gu.codes, gu.scale)
+    codes, scale, dy, lddy, M = _activations(dy, q, wt.K, 1, wt.codes, wt.scale, gu.codes, gu.scale)
     F, dev, fb = wt.N, wt.codes.device, _blocks(wt.N)
     if tuple(gu.codes.shape) != (2, M, F) or tuple(gu.scale.shape) != (2, fb, M):
         raise ValueError(f"the checkpoint {tuple(gu.codes.shape)} does not fit [2, {M}, {F}]")
@@ -674,11 +673,9 @@ def fp8_weight_grad(g: torch.Tensor, q: Fp8Block, *, out_dtype=torch.float32,
     dwdt = _out_type(out_dtype)
     parts = g.shape[0] if g.dim() == 3 else 1
     g0 = g[0] if g.dim() == 3 else g
-    ldg = _rows(g0, "g")
-    _on_gpu(g)
-    M, N = g0.shape
+    ldg, M, N = _rows(g0, "g")
     K = q.codes.shape[-1]
-    codes, scale, _, _, Mq = _activations(None, q, K, 1)
+    codes, scale, _, _, Mq = _activations(None, q, K, 1, g)
     if Mq != M:
         raise ValueError(f"g has {M} rows, the checkpoint {Mq}")
     dw = g.new_empty((parts, N, K) if g.dim() == 3 else (N, K), dtype=out_dtype)
@@ -701,8 +698,7 @@ def fp8_gated_ffn(gate_up: Fp8Weight, down: Fp8Weight, x: torch.Tensor, *, act="
     """The gated feed-forward block in one call: y = (act(x Wg^T) * (x Wu^T)) Wd^T.  With ``save`` returns (y, the uint8
     buffer that :func:`fp8_gated_ffn_backward` reads), else y."""
     ydt = _out_type(out_dtype)
-    ldx = _rows(x, "x")
-    M, K = x.shape
+    ldx, M, K = _rows(x, "x")
     F, N = gate_up.N, down.N
     if gate_up.parts != 2 or down.parts != 1 or gate_up.K != K or down.K != F:
         raise ValueError(f"x [{M}, {K}], gate_up {gate_up.parts} x [{F}, {gate_up.K}] and down [{N}, {down.K}] do not belong "
@@ -723,8 +719,7 @@ def fp8_gated_ffn_backward(gate_up_t: Fp8Weight, down_t: Fp8Weight, dy: torch.Te
     """(dx [M, K], dW of (gate, up) [2, F, K], dW of down [N, F]) from dy bf16 [M, N], the transposed weights and what
     :func:`fp8_gated_ffn` saved."""
     dt = _out_type(out_dtype)
-    lddy = _rows(dy, "dy")
-    M, N = dy.shape
+    lddy, M, N = _rows(dy, "dy")
     F, K = down_t.N, gate_up_t.N
     if gate_up_t.parts != 2 or down_t.parts != 1 or gate_up_t.K != F or down_t.K != N:
         raise ValueError(f"dy [{M}, {N}], gate_up_t {gate_up_t.parts} x [{K}, {gate_up_t.K}] and down_t [{F}, {down_t.K}] do "
