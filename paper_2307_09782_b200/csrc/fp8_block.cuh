@@ -163,8 +163,9 @@ __device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefe
 
 // The activations.  SiLU and the tanh form of GELU are both v * sigmoid(w(v)), with w = v and
 // w = 2 sqrt(2 / pi) (v + 0.044715 v^3), since (1 + tanh z) / 2 = sigmoid(2 z).  1 / (1 + 2^(-w / ln 2)) with the special
-// function unit's power of two and reciprocal is good to about 1e-6 relative: 2^-13 of a bf16 rounding step.  A power that
-// overflows gives 0, one that underflows 1, a NaN stays one.
+// function unit's power of two and reciprocal is good to about 5e-7 relative near zero; the power's argument is rounded in
+// FP32, which adds 6e-8 |w| where w is negative (5e-6 at -80, where SiLU is 1e-33).  A bf16 result rounds by 4e-3, an E4M3
+// one by 6e-2.  A power that overflows gives 0, one that underflows 1, a NaN stays one.
 __device__ __forceinline__ float sfu_ex2(float v) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));

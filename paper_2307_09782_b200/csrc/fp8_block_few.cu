@@ -2,7 +2,7 @@
 // decoding.
 //
 // What bounds it is the weights' way from HBM.  Orientation: output channels are the lanes (the MMA's 128-row
-// operand), so that a weight tile is read once for all tokens of the call, and BM = 16, 32, 64 or 128 tokens are
+// operand), so that a weight tile is read once for all tokens of the call, and BM = 16, 32 or 64 tokens are
 // its columns.  A tile of 128 channels (kGated: 128 of the gate and the same 128 of the up projection) is worked on by
 // a cluster of 1, 2, 4 or 8 CTAs that share its K blocks; several CTAs are resident on an SM, so that the device has
 // enough copies in flight.  The cluster's partial sums meet through distributed shared memory: rank r adds up the

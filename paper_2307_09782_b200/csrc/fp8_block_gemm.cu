@@ -4,21 +4,21 @@
 //
 // The FP32 scales change every 128 elements of K, so the tensor core can add up one block only: its four MMAs fill
 // one of two accumulators, and while the next block's MMAs fill the other, the epilogue warps take the finished one
-// out of tensor memory, multiply it by the block's scale and add it to running sums in registers (in FP32: nothing
-// is rounded between the blocks).
+// out of tensor memory, multiply it by the block's scale and add it to running sums in registers (in FP32, one rounding
+// to nearest per block).
 // Orientation: token rows are the lanes (the MMA's 128-row operand), so that a thread's scale sa * sb is ONE number
 // for its 128 columns, and a promotion is one packed FMA per two columns.
 // Tile: 128 tokens x 256 columns, two accumulators of 256 columns = all of tensor memory, eight epilogue warps with 128
 // running sums per thread.  The two column halves (four warps each) give their accumulators back separately.
 //
-// What bounds it: the way of an accumulator from the MMAs to the epilogue warps and back.  Per K block the MMAs take 480
-// cycles, the promotion 460 (286 alone; tensor memory serves both), and commit, waits and hand-over 350: about 870 with two
-// accumulators, 59 % of the tensor core's cycles.  Tried and not faster: CTA pairs with four accumulators of 128
-// columns (the same time; with single CTAs MMAs of 128 columns read the token operand twice, 716 cycles), sixteen epilogue
-// warps (5 % faster without the gated epilogues, which then spill), polling instead of parked waits (slower).
-// No spills: with 227 KB of shared memory the first-level cache holds none of them; 100 bytes per thread in the gradient's
-// epilogue doubled the kernel's time.
-//
+// What bounds it: the time of the epilogue warps, block by block.  Per K block the MMAs take 480 cycles; the promotion takes 460
+// (286 alone; tensor memory serves both), and waits, fences and hand-over around it 350, one after the other: about 870 with two
+// accumulators, 55 % of the tensor core's cycles.  A free accumulator is not what is missing: CTA pairs with four
+// accumulators of 128 columns took the same time (with single CTAs MMAs of 128 columns read the token operand twice, 716
+// cycles).  Tried and not faster either: sixteen epilogue warps (5 % faster without the gated epilogues, which then
+// spill), polling instead of parked waits (slower).
+// Spills: with 227 KB of shared memory the first-level cache holds none of them; 100 bytes per thread in the gradient's
+// epilogue doubled the kernel's time.  The gated layer's epilogue has 12 - 16 bytes, the others none.
 //
 // Powers of two (MX): where all scales are (rule M1 on both sides, the caller's promise), they are E8M0 bytes that the
 // tensor core multiplies in by itself, exactly: one accumulator takes all of K, nothing is promoted, and the epilogue, with
@@ -26,7 +26,7 @@
 // has in it; four warps write the bytes straight into tensor memory (tcgen05.st), stage by stage: no second operand
 // format.  A pair of CTAs takes 256 tokens x 256 columns, so that a CTA loads half of the columns and has six stages.
 // Measured, us, promotion -> MX (2048 tokens unless said): product 4096 -> 11008 93 -> 68; 8192 tokens 7168 -> 28672 1640 -> 1220
-// (2.7 PFLOP/s); gated layer 4096 -> 11008 191 -> 145; gradient 170 -> 121, its epilogue bound.  What the steps gave, on the
+// (2.7 PFLOP/s); gated layer 4096 -> 11008 191 -> 144; gradient 170 -> 120, its epilogue bound.  What the steps gave, on the
 // product: single CTAs 86; pairs 84; scales loaded four K blocks ahead and made bytes only when used 73 (with two ahead, the
 // loads' latency set the pace); sums out of tensor memory with one wait 68.
 // What bounds MX: at 2.7 PFLOP/s and the clock that the power cap leaves (1.6 - 1.7 GHz) the MMAs run about 2/3 of the time.

@@ -46,6 +46,7 @@ constexpr int kConvWarp0 = 8, kProducerWarp = 24, kMmaWarp = 25, kThreads = 832;
 // Stages whose products go to one accumulator before it is folded into the running sums (FP32 results only).  The tensor
 // core rounds every addition to its accumulator towards zero: over 16384 tokens that adds up to 8.5e-6 of the result,
 // over 2048 to 6e-7 at most, the size of the rounding errors of an FP32 sum; a fold holds the MMAs up for about 800 cycles.
+// (bf16 results round by 4e-3 anyway: half a million tokens in one call would add a tenth of that.)
 constexpr int kFold = 32;
 
 enum { kErrProducerW = 31, kErrMmaW = 32, kErrEpilogueW = 33, kErrAlignW = 34, kErrConvertW = 35 };

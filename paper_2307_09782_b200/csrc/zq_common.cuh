@@ -151,8 +151,8 @@ inline bool allow_shared_memory(DeviceOnce& once, Kernel kernel, int bytes) {
 // The kernels of one layer (quantizer, then GEMM) and of consecutive layers are chained with programmatic
 // stream serialization: a kernel lets its successor start early (launch_dependents), and every kernel waits
 // for its predecessor's completion (pdl_wait) before it touches anything the predecessor may have written.
-// What runs before that wait is setup, and in the GEMM the first weight copies (weights are read-only data
-// of the layer).  A kernel launched without such a predecessor passes the wait at once.
+// What runs before that wait is setup, and in the W4A8 GEMM the first weight copies (weights are read-only data
+// of the layer); the FP8 GEMM for few tokens only fetches them to L2.  A kernel launched without such a predecessor passes the wait at once.
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
