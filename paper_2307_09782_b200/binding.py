@@ -382,6 +382,14 @@ class _ScalesPow2:
     def _set_pow2(self, value: Optional[bool]):
         self._pow2 = self.scale, _version(self.scale), value
 
+    def __getstate__(self):  # (a copied tensor counts its writes anew)
+        return {**self.__dict__, "_pow2": self._known_pow2()}
+
+    def __setstate__(self, state):
+        known = state.pop("_pow2")
+        self.__dict__.update(state)
+        self._set_pow2(known)
+
 
 @dataclass
 class Fp8Block(_ScalesPow2):

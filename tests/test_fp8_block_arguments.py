@@ -210,3 +210,22 @@ def test_other_devices_are_refused(monkeypatch):
             binding._on_gpu(*tensors)
     with pytest.raises(ValueError, match="CUDA tensor"):
         binding._on_gpu(On(1), torch.zeros(1))
+
+
+@pytest.mark.parametrize("writes", [0, 1, 2, 3])
+def test_promise_of_copies(writes):
+    """A copy starts with what is known of the original, and its own writes end it, however many the original had seen."""
+    for make in (lambda: weight(128, 128), lambda: binding.Fp8Block(torch.zeros((4, 128), dtype=u8), torch.ones((1, 4)))):
+        for dup in (copy.deepcopy, lambda v: pickle.loads(pickle.dumps(v)), copy.copy):
+            w = make()
+            for _ in range(writes):
+                w.scale.mul_(2.0)
+            w.pow2 = True
+            other = dup(w)
+            assert other.pow2 is True and torch.equal(other.scale, w.scale)
+            for _ in range(4):
+                other.scale.mul_(1.5)
+                assert other.pow2 is False
+            assert w.pow2 is (dup is not copy.copy)
+            w.scale.mul_(1.5)
+            assert w.pow2 is False and dup(w).pow2 is False
