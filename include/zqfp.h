@@ -459,6 +459,97 @@ int zq_fp8_gated_ffn_backward(const void* dy_bf16, int64_t lddy, int mode, int64
                               const uint8_t* down_t, const float* down_ts, zq_activation act, void* dx, void* dw_gate_up,
                               void* dw_down, zq_out_dtype dt, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Attention around an 8-bit cache ------------------------------------------------------------------------------
+ * What a decoder layer does between the projection to queries, keys and values and the output projection:
+ * norms of queries and keys with the position rotation (and its backward pass), a paged cache of keys and values in
+ * E4M3 codes with one FP32 scale for each block of tokens and head, attention over it.
+ *
+ * D (features of a head) is 64 or 128.  Rows of T tokens hold their heads side by side: head h of token t starts at
+ * t * ld + h * D elements; ld is a multiple of 8 (FP32: 4), pointers are 16-byte aligned.  Where the same rows are both
+ * input and output of a call they have to be the same in full (same pointer and ld).
+ */
+
+/* Which features the rotation pairs: i and i + rot/2, or 2i and 2i + 1. */
+typedef enum { ZQ_PAIRS_HALVES = 0, ZQ_PAIRS_NEIGHBOURS = 1 } zq_pairs;
+
+/*
+ * Norm and rotation.  For each token t and each of its Hq query heads (H key heads), x being the head's features:
+ *   n = x / sqrt(mean(x^2) + eps) ;  z = n w ;  z = x where wq = wk = NULL
+ *   y_a = z_a cos - z_b sin ;  y_b = z_b cos + z_a sin  for the rot/2 pairs (a, b) of its first `rot` features
+ * with the cosines and sines of the token's position; features from rot on pass unchanged.  FP32 inside, one rounding.
+ * q, k      : bf16 [T, ldq], [T, ldk];  q_out, k_out : out, bf16 [T, ldqo], [T, ldko]; may be the inputs themselves
+ * wq, wk    : FP32 [D], 16-byte aligned, both or neither
+ * table     : FP32 [far, rot], 16-byte aligned: a position's rot/2 cosines, then its sines.  rot % 16 == 0, 16 .. D
+ * positions : int32 [T]; a token whose position the table lacks (negative, or far and beyond) gets NaN in its rotated features
+ * Hq or H may be 0 (its pointers are not looked at then).  T == 0 is a no-op.
+ */
+int zq_qk_norm_rope(const void* q_bf16, int64_t ldq, int64_t Hq, const void* k_bf16, int64_t ldk, int64_t H, int64_t T,
+                    int64_t D, const float* wq, const float* wk, float eps, const float* table, int64_t far, int64_t rot,
+                    int pairs, const int32_t* positions, void* q_out, int64_t ldqo, void* k_out, int64_t ldko, void* stream);
+/*
+ * Its backward pass from the gradients dq, dk of the outputs and the inputs q, k (not looked at without norms):
+ *   g = rotation of dy by the opposite angles ;  dw = sum over tokens and heads of g n ;  u = g w ;
+ *   dx = (u - n mean(u n)) / sqrt(mean(x^2) + eps) ;  dx = g without norms
+ * dxq, dxk : out, bf16; may be dq, dk themselves.  dwq, dwk : out, FP32 [D], summed in FP32 in an order that does not
+ * vary (T == 0 gives zeros); not looked at without norms, nor is the workspace (256-byte aligned).
+ */
+size_t zq_qk_norm_rope_backward_workspace_bytes(int64_t D);
+int zq_qk_norm_rope_backward(const void* dq_bf16, int64_t lddq, const void* dk_bf16, int64_t lddk, const void* q_bf16,
+                             int64_t ldq, int64_t Hq, const void* k_bf16, int64_t ldk, int64_t H, int64_t T, int64_t D,
+                             const float* wq, const float* wk, float eps, const float* table, int64_t far, int64_t rot,
+                             int pairs, const int32_t* positions, void* dxq, int64_t lddxq, void* dxk, int64_t lddxk,
+                             float* dwq, float* dwk, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The cache:  codes [pages, 2, H, page, D] (E4M3; keys, then values), 16-byte aligned, and scale [pages, 2, H] (FP32).
+ * page = 16, 32, 64 or 128 tokens; pages * 2 * H < 2^31.  The sequences of a call:
+ * table : int32 [B, table_ld]: entry i of row b is the page of sequence b's tokens i * page .. i * page + page - 1
+ * lens  : int32 [B]: tokens of each sequence, the new ones of this call included
+ * cu    : int32 [B + 1], ascending: rows cu[b] .. cu[b + 1] - 1 of the tensors with T rows are the new tokens of sequence b, its
+ *         last ones; rows from cu[B] on belong to nobody and are neither read nor written.  NULL: one new token each (T == B).
+ * All three are read on the device.  What they name wrongly is not followed: offsets outside the tensors or not ascending, and
+ * more new tokens than lens has, make a sequence's new tokens nobody's (written to no page; attention takes them as described
+ * there); pages outside the cache, or beyond table_ld, hold NaN and are not written.
+ */
+
+/*
+ * New keys and values into their pages.  A block is what one page holds of one head's keys, or values.  With a the largest
+ * absolute value of the new rows in a block, it needs the scale  s = max(fl32(a / 448), 2^-64) , rounded up to a power of two
+ * with ZQ_SCALE_M1, NaN if a is not finite.  A block whose first row is written by this call gets s.  One that was begun before
+ * keeps its scale where that is at least s; else its scale becomes s and the codes in the rows before are rounded to it anew:
+ * RNE_E4M3(fl32(fl32(code old) fl32(1 / s))).  New codes are RNE_E4M3(fl32(x fl32(1 / scale))), saturating.  A block whose scale
+ * is NaN holds codes 0 and stands for NaN.  Rows behind the sequence's last token stay as they were.
+ * k, v : bf16 [T, ldk], [T, ldv].  mode : ZQ_SCALE_NONE or ZQ_SCALE_M1.  A page may be written for one sequence only in a call.
+ */
+int zq_kv_cache_write(const void* k_bf16, int64_t ldk, const void* v_bf16, int64_t ldv, int64_t T, const int32_t* cu,
+                      int64_t B, const int32_t* lens, const int32_t* table, int64_t table_ld, uint8_t* codes,
+                      float* scale, int64_t pages, int64_t H, int page, int64_t D, int mode, void* stream);
+/* The first cu[b + 1] - cu[b] tokens of each sequence's keys and values, code * scale rounded once: k, v out, [T, H, D] dense,
+ * 16-byte aligned, FP32 or bf16.  cu is required. */
+int zq_kv_cache_read(const uint8_t* codes, const float* scale, int64_t pages, int64_t H, int page, int64_t D,
+                     const int32_t* table, int64_t table_ld, const int32_t* cu, int64_t B, int64_t T, void* k, void* v,
+                     zq_out_dtype dt, void* stream);
+
+/*
+ * Attention:  o = softmax(sm_scale q K^T + mask) V  for each new token and query head, K and V being what the cache holds of
+ * head hq / (Hq / H) of the token's sequence.  New token i of n in a sequence of L stands at position p = L - n + i; it sees all
+ * L positions, with causal = 1 those up to p, with window > 0 (causal = 1 only) the last `window` of these.  A row that sees
+ * nothing (no tokens, p < 0) gets o = 0 and lse = -infinity.  A row that sees a block that stands for NaN gets NaN; blocks and
+ * codes that a row does not see have no influence on it, whatever they hold.
+ * q    : bf16 [T, ldq], ldq >= Hq * D;  out : [T, ldo], FP32 or bf16;  lse : out, FP32 [T, Hq] or NULL, ln of the sum of
+ *        exp(sm_scale q k).  Hq % H == 0, any H; sm_scale > 0, finite.
+ * workspace : zq_kv_attention_workspace_bytes bytes, 256-byte aligned, zeroed once with zq_workspace_init; one for T rows and B
+ *        sequences serves fewer.  0: refused sizes.
+ * Products take q as a sum of two E4M3 numbers times a power of two for each row and head: features below 2^-17 of the largest
+ * are lost, the others are exact.  Scores, maxima and sums are FP32, probabilities are rounded to 11 bits.  Scales of the values'
+ * blocks that a row sees lie within 2^60 of one another.  Results do not vary from run to run.
+ */
+size_t zq_kv_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D);
+int zq_kv_attention(const void* q_bf16, int64_t ldq, int64_t Hq, int64_t T, const int32_t* cu, int64_t B, const int32_t* lens,
+                    const int32_t* table, int64_t table_ld, const uint8_t* codes, const float* scale, int64_t pages,
+                    int64_t H, int page, int64_t D, float sm_scale, int causal, int64_t window, void* out,
+                    zq_out_dtype dt, int64_t ldo, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Number of kernels of this library launched by the calling process so far (all entry points). */
 int64_t zq_launch_count(void);
 

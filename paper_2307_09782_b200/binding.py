@@ -33,7 +33,11 @@ EXPORTS = [
     "zq_fp8_block_workspace_bytes", "zq_fp8_block_linear", "zq_fp8_gated_linear", "zq_fp8_gated_linear_backward",
     "zq_fp8_weight_grad", "zq_fp8_gated_ffn_saved_bytes", "zq_fp8_gated_ffn_workspace_bytes", "zq_fp8_gated_ffn",
     "zq_fp8_gated_ffn_backward",
+    "zq_qk_norm_rope", "zq_qk_norm_rope_backward_workspace_bytes", "zq_qk_norm_rope_backward", "zq_kv_cache_write",
+    "zq_kv_cache_read", "zq_kv_attention_workspace_bytes", "zq_kv_attention",
 ]
+PAIRS_HALVES, PAIRS_NEIGHBOURS = 0, 1
+PAIRS = {"halves": PAIRS_HALVES, "neighbours": PAIRS_NEIGHBOURS}
 ACT_SILU, ACT_GELU_TANH, ACT_RELU = 0, 1, 2
 ACTIVATIONS = {"silu": ACT_SILU, "gelu_tanh": ACT_GELU_TANH, "relu": ACT_RELU}
 PLAN_FIELDS = ("bm", "m_tiles", "n_tiles", "ctas", "stream", "persist", "splits", "kb_per_split", "base", "rem",
@@ -127,6 +131,24 @@ def lib() -> C.CDLL:
                                                 sz, vp]
         L.zq_fp8_weight_grad.restype = ci
         L.zq_fp8_weight_grad.argtypes = [vp, i64, i64, ci, vp, vp, i64, i64, i64, vp, ci, vp, sz, vp]
+        f32 = C.c_float
+        L.zq_qk_norm_rope.restype = ci
+        L.zq_qk_norm_rope.argtypes = [vp, i64, i64, vp, i64, i64, i64, i64, vp, vp, f32, vp, i64, i64, ci, vp, vp, i64, vp, i64,
+                                      vp]
+        L.zq_qk_norm_rope_backward_workspace_bytes.restype = sz
+        L.zq_qk_norm_rope_backward_workspace_bytes.argtypes = [i64]
+        L.zq_qk_norm_rope_backward.restype = ci
+        L.zq_qk_norm_rope_backward.argtypes = [vp, i64, vp, i64, vp, i64, i64, vp, i64, i64, i64, i64, vp, vp, f32, vp, i64, i64,
+                                               ci, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+        L.zq_kv_cache_write.restype = ci
+        L.zq_kv_cache_write.argtypes = [vp, i64, vp, i64, i64, vp, i64, vp, vp, i64, vp, vp, i64, i64, ci, i64, ci, vp]
+        L.zq_kv_cache_read.restype = ci
+        L.zq_kv_cache_read.argtypes = [vp, vp, i64, i64, ci, i64, vp, i64, vp, i64, i64, vp, vp, ci, vp]
+        L.zq_kv_attention_workspace_bytes.restype = sz
+        L.zq_kv_attention_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
+        L.zq_kv_attention.restype = ci
+        L.zq_kv_attention.argtypes = [vp, i64, i64, i64, vp, i64, vp, vp, i64, vp, vp, i64, i64, ci, i64, f32, ci, i64, vp, ci,
+                                      i64, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -749,3 +771,242 @@ def fp8_gated_ffn_backward(gate_up_t: Fp8Weight, down_t: Fp8Weight, dy: torch.Te
                                            dt, workspace.data_ptr(),
                                            workspace.numel(), _stream()), "zq_fp8_gated_ffn_backward")
     return dx, dwgu, dwd
+
+
+# ---- attention around an 8-bit cache ------------------------------------------------------------------
+
+@dataclass
+class Fp8KvCache:
+    """A paged cache of keys and values in E4M3 codes, one scale for each block of tokens and head (``zq_kv_cache_write``)."""
+    codes: torch.Tensor   # uint8 [pages, 2, H, page, D]: keys, then values
+    scale: torch.Tensor   # float32 [pages, 2, H]
+
+    def __post_init__(self):
+        if self.codes.dim() != 5 or self.codes.shape[1] != 2 or tuple(self.scale.shape) != tuple(self.codes.shape[:3]):
+            raise ValueError(f"codes [pages, 2, H, page, D] and scales [pages, 2, H] are needed, got {tuple(self.codes.shape)} and "
+                             f"{tuple(self.scale.shape)}")
+        _expect(self.codes, torch.uint8, "codes")
+        _expect(self.scale, torch.float32, "scale")
+        if self.page not in (16, 32, 64, 128) or self.D not in (64, 128):
+            raise ValueError(f"pages of 16, 32, 64 or 128 tokens and heads of 64 or 128 features are supported, got {self.page} and "
+                             f"{self.D}")
+
+    @property
+    def pages(self) -> int:
+        return self.codes.shape[0]
+
+    @property
+    def H(self) -> int:
+        return self.codes.shape[2]
+
+    @property
+    def page(self) -> int:
+        return self.codes.shape[3]
+
+    @property
+    def D(self) -> int:
+        return self.codes.shape[4]
+
+    def values(self) -> torch.Tensor:
+        """The FP32 values the codes stand for (a convenience for inspection, not a hot path)."""
+        return self.codes.view(torch.float8_e4m3fn).float() * self.scale[..., None, None]
+
+
+def make_kv_cache(pages: int, H: int, D: int, page: int = 64, device="cuda") -> Fp8KvCache:
+    """A cache of zeros."""
+    return Fp8KvCache(torch.zeros((pages, 2, H, page, D), dtype=torch.uint8, device=device),
+                      torch.zeros((pages, 2, H), dtype=torch.float32, device=device))
+
+
+def rotary_table(far: int, rot: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """Cosines and sines of positions 0 .. far - 1, float32 [far, rot]; the angles p * base^(-2i / rot) in 64 bits."""
+    angle = torch.arange(far, dtype=torch.float64)[:, None] * base ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)
+    return torch.cat([angle.cos(), angle.sin()], 1).float().to(device)
+
+
+def _heads(x: torch.Tensor, name: str):
+    """(row stride, rows, heads, features) of a bf16 tensor [T, heads, D] whose rows hold their heads side by side."""
+    if x.dtype is torch.bfloat16 and x.dim() == 3:
+        T, H, D = x.shape
+        ld, sh, sd = x.stride()
+        if (sd == 1 or D <= 1) and (sh == D or H <= 1):
+            return (ld if T > 1 else (H * D + 7) // 8 * 8), T, H, D
+    raise ValueError(f"{name}: a bf16 tensor [tokens, heads, features] with a token's heads side by side is needed, got {x.dtype} "
+                     f"{tuple(x.shape)}, strides {x.stride()}")
+
+
+def _pairs(pairs) -> int:
+    return PAIRS[pairs] if isinstance(pairs, str) else int(pairs)
+
+
+def _rope_args(q, k, table, positions, wq, wk):
+    ldq, T, Hq, D = _heads(q, "q")
+    ldk, Tk, H, Dk = _heads(k, "k")
+    if (T, D) != (Tk, Dk):
+        raise ValueError(f"q {tuple(q.shape)} and k {tuple(k.shape)} do not belong together")
+    _expect(table, torch.float32, "table")
+    _expect(positions, torch.int32, "positions")
+    if table.dim() != 2 or positions.shape != (T,):
+        raise ValueError(f"a table [far, rot] and positions [{T}] are needed, got {tuple(table.shape)} and {tuple(positions.shape)}")
+    if (wq is None) != (wk is None):
+        raise ValueError("give the weights of both norms, or of neither")
+    for w, name in ((wq, "wq"), (wk, "wk")):
+        if w is not None:
+            _expect(w, torch.float32, name)
+            if w.shape != (D,):
+                raise ValueError(f"{name}: [{D}] weights are needed, got {tuple(w.shape)}")
+    _on_gpu(q, k, table, positions, *(() if wq is None else (wq, wk)))
+    return ldq, ldk, T, Hq, H, D
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, table: torch.Tensor, positions: torch.Tensor, *, wq=None, wk=None,
+                 eps: float = 1e-6, pairs="halves", out=None):
+    """Norms of queries [T, Hq, D] and keys [T, H, D] for each head (``wq``, ``wk`` float32 [D]; none without them) and the rotation
+    by their ``positions`` (int32 [T]; ``table`` from :func:`rotary_table`).  bf16; parts of one projection's result will
+    do.  ``out``: (q, k) to write to, the inputs themselves if wanted."""
+    ldq, ldk, T, Hq, H, D = _rope_args(q, k, table, positions, wq, wk)
+    if out is None:
+        qo, ko = q.new_empty((T, Hq, D)), k.new_empty((T, H, D))
+    else:
+        qo, ko = out
+        if qo.shape != q.shape or ko.shape != k.shape:
+            raise ValueError(f"out: {tuple(q.shape)} and {tuple(k.shape)} are needed, got {tuple(qo.shape)} and {tuple(ko.shape)}")
+        _on_gpu(qo, ko)
+    ldqo, ldko = _heads(qo, "out[0]")[0], _heads(ko, "out[1]")[0]
+    _check(lib().zq_qk_norm_rope(_ptr(q), ldq, Hq, _ptr(k), ldk, H, T, D, _ptr(wq), _ptr(wk), eps, _ptr(table), table.shape[0],
+                                 table.shape[1], _pairs(pairs), _ptr(positions), _ptr(qo), ldqo, _ptr(ko), ldko, _stream()),
+           "zq_qk_norm_rope")
+    return qo, ko
+
+
+def qk_norm_rope_backward_workspace_bytes(D: int) -> int:
+    return int(lib().zq_qk_norm_rope_backward_workspace_bytes(D))
+
+
+def qk_norm_rope_backward(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k: torch.Tensor, table: torch.Tensor,
+                          positions: torch.Tensor, *, wq=None, wk=None, eps: float = 1e-6, pairs="halves",
+                          workspace: Optional[torch.Tensor] = None):
+    """Gradients of :func:`qk_norm_rope`'s inputs and weights from those of its outputs: (of q, of k, of wq, of wk); bf16, and
+    float32 or None for the weights."""
+    ldq, ldk, T, Hq, H, D = _rope_args(q, k, table, positions, wq, wk)
+    lddq, lddk = _heads(dq, "dq")[0], _heads(dk, "dk")[0]
+    if dq.shape != q.shape or dk.shape != k.shape:
+        raise ValueError(f"gradients {tuple(q.shape)} and {tuple(k.shape)} are needed, got {tuple(dq.shape)} and {tuple(dk.shape)}")
+    _on_gpu(dq, dk)
+    dxq, dxk = q.new_empty((T, Hq, D)), k.new_empty((T, H, D))
+    dwq = dwk = None
+    if wq is not None:
+        dwq, dwk = torch.empty_like(wq), torch.empty_like(wk)
+        workspace = _kept_workspace("norm_rope", workspace, lambda: qk_norm_rope_backward_workspace_bytes(D), q.device, (D,))
+    _check(lib().zq_qk_norm_rope_backward(_ptr(dq), lddq, _ptr(dk), lddk, _ptr(q), ldq, Hq, _ptr(k), ldk, H, T, D, _ptr(wq),
+                                          _ptr(wk), eps, _ptr(table), table.shape[0], table.shape[1], _pairs(pairs),
+                                          _ptr(positions), _ptr(dxq), Hq * D, _ptr(dxk), H * D, _ptr(dwq), _ptr(dwk),
+                                          _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()),
+           "zq_qk_norm_rope_backward")
+    return dxq, dxk, dwq, dwk
+
+
+_kv_workspaces = KeptWorkspaces()
+
+
+def _kept_workspace(what: str, workspace, need, device, sizes):
+    """As :func:`_fp8_workspace`: the caller's, or one kept per thread, device and stream; a captured call's is its own.  ``need``
+    is asked for the bytes when ``sizes`` are others than last time."""
+    if workspace is not None:
+        _expect(workspace, torch.uint8, "workspace")
+        _on_gpu(workspace)
+        return workspace
+    if _capturing():
+        return make_workspace(need(), device)
+    key = (what, device.index, _stream())
+    kept = _kv_workspaces.of
+    ws, of = kept.get(key, (None, None))
+    if of != sizes:
+        n = need()
+        if ws is None or ws.numel() < n:
+            ws = make_workspace(n, device)
+        kept[key] = (ws, sizes)
+    return ws
+
+
+def _sequences(table: torch.Tensor, lens, cu, T: int):
+    """B of a batch, its tensors looked over."""
+    _expect(table, torch.int32, "table")
+    if table.dim() != 2:
+        raise ValueError(f"table: [sequences, pages] is needed, got {tuple(table.shape)}")
+    B = table.shape[0]
+    if lens is not None:
+        _expect(lens, torch.int32, "lens")
+        if lens.shape != (B,):
+            raise ValueError(f"lens: [{B}] is needed, got {tuple(lens.shape)}")
+    if cu is not None:
+        _expect(cu, torch.int32, "cu")
+        if cu.shape != (B + 1,):
+            raise ValueError(f"cu: [{B + 1}] is needed, got {tuple(cu.shape)}")
+    elif T != B:
+        raise ValueError(f"{T} rows for {B} sequences: without cu each has one new token")
+    return B
+
+
+def kv_cache_write(cache: Fp8KvCache, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, *,
+                   cu: Optional[torch.Tensor] = None, mode="none") -> None:
+    """New keys and values, bf16 [T, H, D], into their sequences' pages.  ``table`` int32 [B, pages of a sequence], ``lens`` int32 [B]:
+    tokens with the new ones; ``cu`` int32 [B + 1]: the sequences' rows (without it one each); ``mode``: "none" or "M1"."""
+    ldk, T, H, D = _heads(k, "k")
+    ldv = _heads(v, "v")[0]
+    if v.shape != k.shape or (H, D) != (cache.H, cache.D):
+        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} do not fit a cache of {cache.H} heads of {cache.D}")
+    B = _sequences(table, lens, cu, T)
+    _on_gpu(cache.codes, cache.scale, k, v, table, lens, *(() if cu is None else (cu,)))
+    _check(lib().zq_kv_cache_write(k.data_ptr(), ldk, v.data_ptr(), ldv, T, _ptr(cu), B, lens.data_ptr(), table.data_ptr(),
+                                   table.shape[1], cache.codes.data_ptr(), cache.scale.data_ptr(), cache.pages, H, cache.page, D,
+                                   _mode(mode), _stream()), "zq_kv_cache_write")
+
+
+def kv_cache_read(cache: Fp8KvCache, table: torch.Tensor, cu: torch.Tensor, rows: int, *, out_dtype=torch.bfloat16):
+    """(keys, values) [rows, H, D] of each sequence's first cu[b + 1] - cu[b] tokens.  Rows from cu[B] on are not written."""
+    dt = _out_type(out_dtype)
+    if cu is None:
+        raise ValueError("cu: the sequences' rows are needed")
+    B = _sequences(table, None, cu, rows)
+    _on_gpu(cache.codes, cache.scale, table, cu)
+    k, v = [cache.scale.new_empty((rows, cache.H, cache.D), dtype=out_dtype) for _ in range(2)]
+    _check(lib().zq_kv_cache_read(cache.codes.data_ptr(), cache.scale.data_ptr(), cache.pages, cache.H, cache.page, cache.D,
+                                  table.data_ptr(), table.shape[1], cu.data_ptr(), B, rows, k.data_ptr(), v.data_ptr(), dt,
+                                  _stream()), "zq_kv_cache_read")
+    return k, v
+
+
+def kv_attention_workspace_bytes(T: int, B: int, Hq: int, H: int, D: int) -> int:
+    """Workspace for :func:`kv_attention` on T new tokens of B sequences (one for more serves fewer)."""
+    return int(lib().zq_kv_attention_workspace_bytes(T, B, Hq, H, D))
+
+
+def kv_attention(cache: Fp8KvCache, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, *, cu: Optional[torch.Tensor] = None,
+                 sm_scale: Optional[float] = None, causal: bool = True, window: int = 0, out_dtype=torch.bfloat16, out=None,
+                 lse: bool = False, workspace: Optional[torch.Tensor] = None):
+    """Attention of the new tokens' queries, bf16 [T, Hq, D], over the cache -> [T, Hq, D].  ``table``, ``lens``, ``cu`` as
+    :func:`kv_cache_write`; ``sm_scale``: 1 / sqrt(D) unless given; ``window``: how many of the last positions a token sees (0:
+    all).  With ``lse`` also the logarithms of the softmax sums, float32 [T, Hq]."""
+    ldq, T, Hq, D = _heads(q, "q")
+    if D != cache.D or Hq % cache.H or Hq == 0:
+        raise ValueError(f"q {tuple(q.shape)} does not fit a cache of {cache.H} heads of {cache.D}")
+    dt = _out_type(out_dtype if out is None else out.dtype)
+    B = _sequences(table, lens, cu, T)
+    _on_gpu(cache.codes, cache.scale, q, table, lens, *(() if cu is None else (cu,)))
+    if out is None:
+        out, ldo = q.new_empty((T, Hq, D), dtype=out_dtype), Hq * D
+    else:
+        if out.shape != q.shape or (T > 0 and out.stride()[1:] != (D, 1)):
+            raise ValueError(f"out: {tuple(q.shape)} with a token's heads side by side is needed, got {tuple(out.shape)}, strides "
+                             f"{out.stride()}")
+        _on_gpu(out)
+        ldo = out.stride(0) if T > 1 else Hq * D
+    sums = q.new_empty((T, Hq), dtype=torch.float32) if lse else None
+    workspace = _kept_workspace("attention", workspace, lambda: kv_attention_workspace_bytes(T, B, Hq, cache.H, D), q.device,
+                                (T, B, Hq, cache.H, D))
+    _check(lib().zq_kv_attention(q.data_ptr(), ldq, Hq, T, _ptr(cu), B, lens.data_ptr(), table.data_ptr(), table.shape[1],
+                                 cache.codes.data_ptr(), cache.scale.data_ptr(), cache.pages, cache.H, cache.page, D,
+                                 D ** -0.5 if sm_scale is None else sm_scale, 1 if causal else 0, window, out.data_ptr(), dt, ldo,
+                                 _ptr(sums), workspace.data_ptr(), workspace.numel(), _stream()), "zq_kv_attention")
+    return (out, sums) if lse else out
