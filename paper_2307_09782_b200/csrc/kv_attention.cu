@@ -1,5 +1,5 @@
 // Attention over the 8-bit cache: o = softmax(scale q k^T + mask) v.
-#include "kv_cache.cuh"
+#include "kv_attention.cuh"
 
 namespace zq {
 namespace kv {
@@ -21,6 +21,7 @@ __global__ void __launch_bounds__(256) attention_row_kernel(const AttnArgs a) {
   int first, n;
   rows_of(c, b, first, n);
   if (t < first || t >= first + n) return;
+  if (static_cast<int64_t>(n) * (a.Hq / c.H) <= kFewRows) return;
   const int L = max(load_chained(c.lens + b), 0);
   const int pos = L - n + static_cast<int>(t - first);
   const int hi = a.causal ? min(L, pos + 1) : L;
@@ -64,6 +65,12 @@ __global__ void __launch_bounds__(256) attention_row_kernel(const AttnArgs a) {
 }  // namespace
 
 int launch_attention(const AttnArgs& a, cudaStream_t st) {
+  const int G = a.Hq / a.c.H;
+  if (G <= kFewRows) {
+    const int64_t most = a.c.cu ? (a.c.T * G < kFewRows ? a.c.T * G : kFewRows) : G;
+    if (int e = launch_attention_few(a, static_cast<int>(most), st)) return e;
+    if (!a.c.cu) return ZQ_OK;
+  }
   const int64_t grid = (a.c.T * a.Hq + 7) / 8;
   if (grid > 0x7FFFFFFF) return ZQ_ERR_SHAPE;
   auto kernel = a.c.D == 128 ? (a.dt == ZQ_OUT_F32 ? attention_row_kernel<128, true> : attention_row_kernel<128, false>)

@@ -1,0 +1,201 @@
+// Pieces shared by the two attention kernels (few rows per sequence and head, many rows): tensor-core operands, the walk over a
+// sequence's tiles of 128 tokens, the splitting of queries, block scales.
+#pragma once
+
+#include "kv_cache.cuh"
+
+namespace zq {
+namespace kv {
+
+constexpr int kTok = 128;           // tokens of a tile
+constexpr int kFewRows = 64;        // rows (new tokens x query heads of a cache head) up to which the kernel for few rows takes a sequence
+constexpr int kMaxCtas = 148;       // CTAs whose partial results the workspace has room for
+constexpr float kLog2e = 1.4426950408889634f;
+// Probabilities are kept times 2^kShift (the row's largest at most 2^kShift), where FP16 holds 11 bits down to 2^-28 of the
+// largest and something down to 2^-38; values are kept as code / 256.  Both cancel against the sum of the probabilities.
+constexpr float kShift = 14.0f;
+constexpr float kCodeUnit = 1.0f / 256.0f;
+
+int launch_attention_few(const AttnArgs& a, int max_rows, cudaStream_t st);
+size_t few_workspace_bytes(int64_t B, int64_t H, int64_t D);
+
+#ifdef __CUDACC__
+// ---- operands ---------------------------------------------------------------------------------------------------------
+// 8-bit rows of D bytes, K-major, swizzled as the copy engine does for rows of that size (128 or 64 bytes).
+template <int D>
+__device__ __forceinline__ uint64_t desc_rows(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= uint64_t((smem_addr >> 4) & 0x3FFF);
+  d |= uint64_t(1) << 16;
+  d |= uint64_t((8 * D) >> 4) << 32;  // the next 8 rows
+  d |= uint64_t(1) << 46;
+  d |= uint64_t(D == 128 ? 2 : 4) << 61;
+  return d;
+}
+// Byte of 16-byte piece `piece` of row `row` in such rows.
+template <int D>
+__device__ __forceinline__ uint32_t row_piece(int row, int piece) {
+  return row * D + ((piece ^ (D == 128 ? row & 7 : (row >> 1) & 3)) << 4);
+}
+// FP16 values [128 tokens][64 features] (128 bytes a token, 128-byte swizzle), the features of M or N, the tokens of K; the next 64
+// features 16 KB further.
+__device__ __forceinline__ uint64_t desc_values(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= uint64_t((smem_addr >> 4) & 0x3FFF);
+  d |= uint64_t((kTok * 128) >> 4) << 16;
+  d |= uint64_t(1024 >> 4) << 32;
+  d |= uint64_t(1) << 46;
+  d |= uint64_t(2) << 61;
+  return d;
+}
+// FP16 x FP16 -> FP32, D is 128 x n
+__device__ __forceinline__ uint32_t idesc_f16(uint32_t n, bool a_mn, bool b_mn) {
+  return (1u << 4) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+__device__ __forceinline__ void umma_f16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// Codes of four E4M3 numbers -> FP16 code / 256, two and two: the exponent and mantissa bits moved into FP16's fields (which
+// have one exponent bit more, whence the factor; subnormal numbers come out right as well).  The pattern of E4M3's NaN
+// becomes 480 / 256: what nobody sees must not turn into NaN by a product with zero.
+__device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  const uint32_t a = __byte_perm(w, 0u, 0x1404), b = __byte_perm(w, 0u, 0x3424);  // each code in the upper byte of a half
+  lo = (a & 0x80008000u) | ((a >> 1) & 0x3F803F80u);
+  hi = (b & 0x80008000u) | ((b >> 1) & 0x3F803F80u);
+}
+// A converter thread's share of a tile of values: codes [128][D] (rows as they lie in memory) -> FP16 in the operand's layout.
+// Tokens from `valid` on become zeros, whatever the page holds there.
+template <int D, int THREADS>
+__device__ __forceinline__ void widen_values(const uint8_t* codes, uint8_t* out, int i, int valid) {
+  constexpr int kPieces = kTok * D / 16, kPerRow = D / 16;
+  static_assert(kPieces % THREADS == 0, "pieces per thread");
+#pragma unroll
+  for (int x = 0; x < kPieces / THREADS; ++x) {
+    const int at = x * THREADS + i, row = at / kPerRow, c = at % kPerRow;
+    const uint4 v = *reinterpret_cast<const uint4*>(codes + at * 16);
+    uint32_t o[8];
+    widen4(v.x, o[0], o[1]);
+    widen4(v.y, o[2], o[3]);
+    widen4(v.z, o[4], o[5]);
+    widen4(v.w, o[6], o[7]);
+    if (row >= valid) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = 0u;
+    }
+    uint8_t* dst = out + (c >> 2) * (kTok * 128) + row * 128;
+    const int p = (c & 3) * 2, sw = row & 7;
+    *reinterpret_cast<uint4*>(dst + ((p ^ sw) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+    *reinterpret_cast<uint4*>(dst + (((p + 1) ^ sw) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+  }
+}
+
+// ---- queries ------------------------------------------------------------------------------------------------------------
+// Eight bf16 features of a row as two E4M3 numbers each: q 2^e = a + b with the row's largest feature between 128 and 256.  A bf16
+// number has 8 bits, an E4M3 number 4: the rest after the first, rounded to nearest, fits the second, down to 2^-9.
+struct RowScale {
+  float up;    // 2^e, 0 where the row is not finite
+  float down;  // 2^-e, NaN there
+};
+__device__ __forceinline__ RowScale row_scale(uint32_t amax_bits) {  // bits of the largest |q| as FP32
+  const int e = max(static_cast<int>(amax_bits >> 23), 8);           // (rows below 2^-119: their scores are nothing)
+  RowScale r;
+  const bool finite = amax_bits < 0x7F800000u;
+  r.up = finite ? __uint_as_float(static_cast<uint32_t>(261 - e) << 23) : 0.0f;
+  r.down = finite ? __uint_as_float(static_cast<uint32_t>(e - 7) << 23) : __uint_as_float(0x7FC00000u);
+  return r;
+}
+__device__ __forceinline__ uint32_t absmax_bits8(uint4 v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t a = 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a = max(a, max((w[i] << 16) & 0x7FFF0000u, w[i] & 0x7FFF0000u));
+  return a;
+}
+__device__ __forceinline__ void split8(uint4 v, float up, uint2& first, uint2& second) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t a[4], b[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    // (a row that is not finite: zeros; its scores become NaN by the row's factor)
+    const float x = up == 0.0f ? 0.0f : bf16_lo(w[i]) * up, y = up == 0.0f ? 0.0f : bf16_hi(w[i]) * up;
+    a[i] = cvt_e4m3x2(x, y);
+    const float2 f = fp8b::decode2(static_cast<uint16_t>(a[i]));
+    b[i] = cvt_e4m3x2(x - f.x, y - f.y);
+  }
+  first = make_uint2(a[0] | (a[1] << 16), a[2] | (a[3] << 16));
+  second = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
+}
+
+// ---- block scales -------------------------------------------------------------------------------------------------------
+// What 16 tokens of a tile (part of one page) contribute: keys' scale, log2 of the values' scale, its inverse times kCodeUnit.
+// The values' scale goes into the power of two of the probability, so that nothing of it is rounded apart, and comes out of the
+// sum again by its inverse.
+__device__ __forceinline__ float4 scale_entry(const Cache& c, int b, int h, int token, int L) {
+  float4 e = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (token >= L) return e;  // nobody sees them
+  const int page = page_of(c, b, token / c.page);
+  const float ks = page < 0 ? __uint_as_float(0x7FC00000u) : load_chained(c.scale + block_at(c, page, 0, h));
+  float vs = page < 0 ? 1.0f : load_chained(c.scale + block_at(c, page, 1, h));
+  if (vs < 5.42101086242752217e-20f) vs = 5.42101086242752217e-20f;  // 2^-64: what was never written has 0
+  e.x = ks;
+  e.y = log2f(vs);
+  e.z = kCodeUnit / vs;
+  return e;
+}
+
+// Pages of consecutive tiles, a batch of 32 table entries per warp with the next batch on its way.
+struct PageWalk {
+  int b, L, base, cur, next;
+  __device__ __forceinline__ int load(const Cache& c, int i) const {
+    return static_cast<int64_t>(i) * c.page < L ? page_of(c, b, i) : -1;
+  }
+  __device__ __forceinline__ void start(const Cache& c, int seq, int len, int first_page, int lane) {
+    b = seq, L = len, base = first_page;
+    cur = load(c, base + lane);
+    next = load(c, base + 32 + lane);
+  }
+  // The page of table entry `first + lane` for lane < count; first ascends by at most 32 from call to call.
+  __device__ __forceinline__ int get(const Cache& c, int first, int lane) {
+    if (first - base >= 32) {
+      cur = next;
+      base += 32;
+      next = load(c, base + 32 + lane);
+    }
+    return __shfl_sync(0xFFFFFFFFu, cur, (first - base + lane) & 31);
+  }
+};
+
+// Largest of a warp's numbers (NaN only where all are).
+__device__ __forceinline__ float warp_max(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// A 3-D tensor of bytes [blocks][page][D], boxes of one block's page x D bytes.
+inline bool make_page_map(CUtensorMap* m, const Cache& c) {
+  gemm::EncodeTiledFn fn = gemm::encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(c.D), static_cast<cuuint64_t>(c.page), static_cast<cuuint64_t>(c.pages) * 2 * c.H};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(c.D), static_cast<cuuint64_t>(c.D) * c.page};
+  const cuuint32_t box[3] = {static_cast<cuuint32_t>(c.D), static_cast<cuuint32_t>(c.page), 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, c.codes, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            c.D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+#endif
+
+}  // namespace kv
+}  // namespace zq

@@ -1,0 +1,803 @@
+// Attention over the 8-bit cache where a sequence and cache head have few rows (new tokens x query heads of the head, up to 64):
+// decoding.  Bound by the codes, which are read once.
+//
+// The codes go from memory to the tensor core as they are on the key side, and widened to FP16 in shared memory on the value side:
+//   S^T [128 tokens, rows] = K [tokens, D] q^T      E4M3 x E4M3; q is a sum of two E4M3 numbers, side by side in the columns
+//   O^T [D, rows] += V^T [D, tokens] P^T            FP16 x FP16
+// Tokens and features are the tensor core's 128 lanes, the rows its columns, so few rows cost little: a tile's products take
+// 150 - 300 cycles, its codes come in about 1400 (32 KB at a 148th of the copy bandwidth).
+//
+// Work: the (sequence, head, tile of 128 tokens) triples of the batch are dealt out evenly, as one contiguous range per CTA; the
+// lengths are on the device, so each CTA finds its range itself.  A range is walked in segments (one per sequence and head), a
+// segment in chunks of kTiles tiles: the scores of a whole chunk stay in tensor memory, two chunks in turn, and a chunk has
+// accumulators of its own, so that a new maximum costs one multiplication per result and chunk in the epilogue's registers.
+// Where several CTAs share a sequence and head, each leaves its sums, maximum and results in the workspace;
+// attention_join_kernel adds them up in the order of the tiles.
+//
+// Warp roles: 0..7 softmax (thread = token), 8..11 epilogue (thread = feature), 12..15 converters of values, 16 keys' copies,
+// 17 values' copies, 18 MMAs, 19 queries and scales.
+#include "kv_attention.cuh"
+
+namespace zq {
+namespace kv {
+namespace {
+
+constexpr int kSoftmaxWarps = 8, kEpiWarp0 = 8, kConvWarp0 = 12, kKeyWarp = 16, kValueWarp = 17, kMmaWarp = 18, kQueryWarp = 19;
+constexpr int kThreads = 20 * 32;
+enum { kErrKeysA = 51, kErrValuesA = 52, kErrMmaA = 53, kErrScalesA = 54, kErrQueriesA = 55, kErrSoftmaxA = 56, kErrConvertA = 57, kErrEpilogueA = 58, kErrAlignA = 59 };
+
+struct P {
+  Cache c;
+  const __nv_bfloat16* q;
+  int64_t ldq;
+  int G;             // query heads of a cache head
+  float scale_log2;  // sm_scale log2(e)
+  int causal, window;
+  void* out;
+  int64_t ldo;
+  float* lse;
+  float* partial;    // [CTAs][2][R (D + 2)]
+  int2* pieces;      // [B * H]: first CTA and number of CTAs of a sequence and head
+  int* status;
+};
+
+template <int D, int R>
+struct Cfg {
+  static constexpr int kTiles = 64 / R;               // tiles of a chunk
+  static constexpr int kTileBytes = kTok * D;
+  static constexpr int kValueBytes = kTok * D * 2;    // widened
+  static constexpr int kProbBytes = kTok * R * 2;     // of a tile
+  static constexpr int kOffValues = 0;                // [2]
+  static constexpr int kOffProbs = kOffValues + 2 * kValueBytes;                // [2][kTiles]
+  static constexpr int kOffQueries = kOffProbs + 2 * kTiles * kProbBytes;       // [2][2 R rows of D]
+  static constexpr int kOffScales = kOffQueries + 2 * 2 * R * D;                // [2][kTiles][8] float4
+  static constexpr int kOffRows = kOffScales + 2 * kTiles * 8 * 16;             // [2][R] int4: factor, first and last token + 1 seen
+  static constexpr int kOffMax = kOffRows + 2 * R * 16;                         // [2][R] maximum, [2][R] factor of what came before
+  static constexpr int kOffRed = kOffMax + 4 * R * 4;                           // [R][8] warps' maxima
+  static constexpr int kOffSum = kOffRed + R * 8 * 4;                           // [R][8] warps' sums, [R] maxima
+  static constexpr int kOffBars = kOffSum + R * 9 * 4;
+  static constexpr int kFixed = (kOffBars + 64 * 8 + 36 * 8 + 1023) / 1024 * 1024;
+  static constexpr int kSlots0 = (227 * 1024 - kFixed) / kTileBytes;
+  static constexpr int kSlots = kSlots0 < 16 ? kSlots0 : 16;
+  static constexpr int kKeySlots = (kSlots + 1) / 2, kValueSlots = kSlots / 2;
+  static constexpr int kOffKeys = kFixed;
+  static constexpr int kOffCodes = kOffKeys + kKeySlots * kTileBytes;
+  static constexpr int kSmemBytes = kOffCodes + kValueSlots * kTileBytes;
+  static constexpr int kNumBars = 2 * kKeySlots + 2 * kValueSlots + 4 + 14 + 5;
+  static_assert(kSmemBytes <= 227 * 1024 && kNumBars <= 64 && kSlots >= 4, "shared memory");
+};
+
+// A sequence's part in this kernel: its rows and tiles (none where it has too many rows, or none).
+struct Seq {
+  int first, n, L;   // first row of the tensors, new tokens, tokens
+  int tile0, tiles;  // tiles that some row sees (one at least, so that rows that see nothing are written)
+};
+__device__ __forceinline__ Seq seq_of(const P& p, int b) {
+  Seq s;
+  rows_of(p.c, b, s.first, s.n);
+  s.L = max(load_chained(p.c.lens + b), 0);
+  s.tile0 = s.tiles = 0;
+  if (s.n > 0 && static_cast<int64_t>(s.n) * p.G <= kFewRows) {
+    const int64_t lo = p.window > 0 ? static_cast<int64_t>(s.L) - s.n + 1 - p.window : 0;
+    s.tile0 = lo > 0 ? static_cast<int>(lo / kTok) : 0;
+    s.tiles = max(s.L / kTok + (s.L % kTok != 0) - s.tile0, 1);
+  }
+  return s;
+}
+
+// The walk over a CTA's units.
+struct Walk {
+  Seq s;
+  int b, h, t;       // t: tile of the sequence's, from 0
+  int64_t left;      // units left
+  int nt;            // tiles of this segment
+  __device__ __forceinline__ bool start(const P& p, const int64_t* range) {
+    left = range[0];
+    b = static_cast<int>(range[1]);
+    if (left <= 0) return false;
+    s = seq_of(p, b);
+    h = static_cast<int>(range[2] / s.tiles);
+    t = static_cast<int>(range[2] % s.tiles);
+    nt = static_cast<int>(min(static_cast<int64_t>(s.tiles - t), left));
+    return true;
+  }
+  __device__ __forceinline__ bool next(const P& p) {
+    left -= nt;
+    if (left <= 0) return false;
+    t = 0;
+    if (++h == p.c.H) {
+      h = 0;
+      do {
+        if (++b >= p.c.B) return false;
+        s = seq_of(p, b);
+      } while (s.tiles == 0);
+    }
+    nt = static_cast<int>(min(static_cast<int64_t>(s.tiles), left));
+    return true;
+  }
+  __device__ __forceinline__ bool whole() const { return nt == s.tiles; }
+};
+
+// A ring position.
+struct Ring {
+  int i = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void step(int n) {
+    if (++i == n) {
+      i = 0;
+      phase ^= 1;
+    }
+  }
+};
+
+template <int D, int R, bool F32>
+__global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid_constant__ CUtensorMap tm, const P p) {
+  using C = Cfg<D, R>;
+  constexpr int kTiles = C::kTiles;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint64_t* bar = reinterpret_cast<uint64_t*>(smem + C::kOffBars);
+  uint64_t* k_full = bar;                            // [key slots] a tile's keys have landed                  (MMA)
+  uint64_t* k_empty = k_full + C::kKeySlots;         // their products are done                                (keys' copies)
+  uint64_t* v_full = k_empty + C::kKeySlots;         // [value slots] a tile's values have landed              (converters)
+  uint64_t* v_empty = v_full + C::kValueSlots;       // they are widened                                       (values' copies)
+  uint64_t* w_full = v_empty + C::kValueSlots;       // [2] widened values                                     (MMA)
+  uint64_t* w_empty = w_full + 2;                    // [2] their products are done                            (converters)
+  uint64_t* s_full = w_empty + 2;                    // [2] scores of a chunk                                  (softmax)
+  uint64_t* s_empty = s_full + 2;                    // [2] they have been used, with the scales               (MMA, scales)
+  uint64_t* e_full = s_empty + 2;                    // [2] block scales of a chunk                            (softmax)
+  uint64_t* p_full = e_full + 2;                     // [2] probabilities and row factors of a chunk           (MMA, epilogue)
+  uint64_t* o_full = p_full + 2;                     // [2] results of a chunk                                 (epilogue)
+  uint64_t* o_empty = o_full + 2;                    // [2] they are in registers                              (MMA, softmax)
+  uint64_t* q_full = o_empty + 2;                    // [2] queries of a segment                               (MMA, softmax)
+  uint64_t* q_empty = q_full + 2;                    // [2] nobody needs them any more                         (queries)
+  uint64_t* l_full = q_empty + 2;                    // sums of a segment                                      (epilogue)
+  uint64_t* l_empty = l_full + 1;                    // they have been read                                    (softmax)
+  uint64_t* meet = l_empty + 1;                      // [2] softmax warps that share rows
+  uint64_t* drain = meet + 2;
+  int64_t* s_range = reinterpret_cast<int64_t*>(smem + C::kOffBars + 64 * 8);  // units, first sequence, first unit in it
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_range + 3);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
+  int64_t* s_scan = s_range + 4;  // [32]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::kKeySlots; ++i) {
+      mbar_init(&k_full[i], 1);
+      mbar_init(&k_empty[i], 1);
+    }
+    for (int i = 0; i < C::kValueSlots; ++i) {
+      mbar_init(&v_full[i], 1);
+      mbar_init(&v_empty[i], 4);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&w_full[i], 4);
+      mbar_init(&w_empty[i], 1);
+      mbar_init(&s_full[i], 1);
+      mbar_init(&s_empty[i], kSoftmaxWarps);
+      mbar_init(&e_full[i], 1);
+      mbar_init(&p_full[i], kSoftmaxWarps);
+      mbar_init(&o_full[i], 1);
+      mbar_init(&o_empty[i], 4);
+      mbar_init(&q_full[i], 1);
+      mbar_init(&q_empty[i], 1 + kSoftmaxWarps);
+    }
+    mbar_init(l_full, kSoftmaxWarps);
+    mbar_init(l_empty, 4);
+    mbar_init(&meet[0], R == 64 ? 4 : 8);
+    mbar_init(&meet[1], 4);
+    mbar_init(drain, 1);
+    *s_abort = 0;
+    s_range[0] = 0;
+    fence_mbar_init();
+    if ((smem_u32(smem) & 1023u) != 0) fp8b::raise_error8(p.status, s_abort, kErrAlignA);
+    prefetch_tensormap(&tm);
+  }
+  if (warp == kMmaWarp) tmem_alloc(s_tmem, 512);
+  pdl_launch_dependents();
+  pdl_wait();
+  // ---- this CTA's range: units (H x tiles of a sequence) before each thread's sequences by a scan over the block
+  {
+    const int per = (p.c.B + kThreads - 1) / kThreads;
+    const int b0 = min(static_cast<int>(threadIdx.x) * per, p.c.B), b1 = min(b0 + per, p.c.B);
+    int64_t mine = 0;
+    for (int b = b0; b < b1; ++b) mine += static_cast<int64_t>(seq_of(p, b).tiles) * p.c.H;
+    int64_t incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+      if (lane >= o) incl += x;
+    }
+    if (lane == 31) s_scan[warp] = incl;
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    int64_t before = 0, total = 0;
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) before += s_scan[w];
+      total += s_scan[w];
+    }
+    const int64_t begin = before + incl - mine;
+    const int64_t ctas = min(static_cast<int64_t>(gridDim.x), total);  // each of these has a unit at least
+    const int64_t u0 = blockIdx.x < ctas ? total * blockIdx.x / ctas : 0, u1 = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : 0;
+    if (u1 > u0 && begin <= u0 && u0 < begin + mine) {
+      int64_t at = begin;
+      int b = b0;
+      for (;; ++b) {
+        const int64_t n = static_cast<int64_t>(seq_of(p, b).tiles) * p.c.H;
+        if (u0 < at + n) break;
+        at += n;
+      }
+      s_range[1] = b;
+      s_range[2] = u0 - at;
+      s_range[0] = u1 - u0;
+    }
+    if (threadIdx.x == 0) s_scan[31] = total;
+  }
+  __syncthreads();
+  const uint32_t tmem = *s_tmem;
+  const bool ok_start = *s_abort == 0;
+  Walk w;
+  const bool any = w.start(p, s_range) && ok_start;
+
+  if (warp == kKeyWarp || warp == kValueWarp) {
+    // ---- copies: a lane per page of the tile
+    const bool keys = warp == kKeyWarp;
+    const int slots = keys ? C::kKeySlots : C::kValueSlots;
+    uint64_t *full = keys ? k_full : v_full, *empty = keys ? k_empty : v_empty;
+    uint8_t* to = smem + (keys ? C::kOffKeys : C::kOffCodes);
+    const int per = kTok / p.c.page, page_bytes = p.c.page * D;
+    Ring r;
+    int issued = 0;
+    bool ok = any;
+    if (ok) do {
+        const int t0 = w.s.tile0 + w.t;
+        PageWalk pages;
+        pages.start(p.c, w.b, w.s.L, t0 * per, lane);
+        for (int j = 0; j < w.nt; ++j) {
+          const int page = pages.get(p.c, (t0 + j) * per, lane);
+          if (issued >= slots && !mbar_wait_warp(&empty[r.i], r.phase ^ 1, s_abort)) {
+            if (lane == 0) fp8b::raise_error8(p.status, s_abort, keys ? kErrKeysA : kErrValuesA);
+            ok = false;
+            break;
+          }
+          const bool has = lane < per && page >= 0;
+          const uint32_t n = __popc(__ballot_sync(0xFFFFFFFFu, has));
+          if (lane == 0) mbar_arrive_expect_tx(&full[r.i], n * page_bytes);
+          __syncwarp();
+          if (has) {
+            uint8_t* dst = to + r.i * C::kTileBytes + lane * page_bytes;
+            const int64_t block = block_at(p.c, page, keys ? 0 : 1, w.h);
+            if (keys)
+              tma_load_3d(dst, &tm, 0, 0, static_cast<int>(block), &full[r.i]);
+            else
+              bulk_load(dst, p.c.codes + block * page_bytes, page_bytes, &full[r.i]);
+          }
+          __syncwarp();
+          ++issued;
+          r.step(slots);
+        }
+      } while (ok && w.next(p));
+    // never leave with copies still in flight
+    for (int i = max(0, issued - slots); i < issued; ++i) {
+      uint32_t spin = 0;
+      while (!mbar_try_wait(&full[i % slots], (i / slots) & 1) && ++spin < kSpinLimit) {
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    const bool issuer = elect_one();
+    const uint64_t kdesc = desc_rows<D>(smem_u32(smem + C::kOffKeys)), qdesc = desc_rows<D>(smem_u32(smem + C::kOffQueries));
+    const uint64_t vdesc = desc_values(smem_u32(smem + C::kOffValues));
+    const uint64_t pdesc = umma_desc_k128(smem_u32(smem + C::kOffProbs));
+    const uint32_t sdesc_i = umma_idesc_e4m3(2 * R), odesc_i = idesc_f16(R, true, false);
+    Ring k, v;
+    bool failed = false;
+    int chunk = 0, seg = 0;
+    // results of chunk `c` of nt tiles
+    auto results = [&](int c, int nt) {
+      const int cb = c & 1;
+      if (!mbar_wait(&p_full[cb], (c >> 1) & 1, s_abort) || (c >= 2 && !mbar_wait(&o_empty[cb], ((c >> 1) - 1) & 1, s_abort))) return false;
+      for (int j = 0; j < nt; ++j) {
+        if (!mbar_wait(&w_full[v.i], v.phase, s_abort)) return false;
+        tc_fence_after_sync();
+        if (issuer) {
+          const uint64_t ad = vdesc + static_cast<uint64_t>((v.i * C::kValueBytes) >> 4);
+          const uint64_t bd = pdesc + static_cast<uint64_t>(((cb * kTiles + j) * C::kProbBytes) >> 4);
+#pragma unroll
+          for (int s = 0; s < kTok / 16; ++s)
+            umma_f16(tmem + 256 + cb * R, ad + s * (2048 >> 4), bd + (s >> 2) * ((R * 128) >> 4) + (s & 3) * 2, odesc_i, (j > 0 || s > 0) ? 1u : 0u);
+          umma_commit(&w_empty[v.i]);
+          if (j + 1 == nt) umma_commit(&o_full[cb]);
+        }
+        __syncwarp();
+        v.step(2);
+      }
+      return true;
+    };
+    int last_nt = 0;  // tiles of the chunk whose scores are issued and whose results are not
+    if (any) do {
+        if (!mbar_wait(&q_full[seg & 1], (seg >> 1) & 1, s_abort)) failed = true;
+        for (int t = 0; t < w.nt && !failed; t += kTiles, ++chunk) {
+          const int nt = min(kTiles, w.nt - t), cb = chunk & 1;
+          if (chunk >= 2 && !mbar_wait(&s_empty[cb], ((chunk >> 1) - 1) & 1, s_abort)) failed = true;
+          for (int j = 0; j < nt && !failed; ++j) {
+            if (!mbar_wait(&k_full[k.i], k.phase, s_abort)) {
+              failed = true;
+              break;
+            }
+            tc_fence_after_sync();
+            if (issuer) {
+              const uint64_t ad = kdesc + static_cast<uint64_t>((k.i * C::kTileBytes) >> 4);
+              const uint64_t bd = qdesc + static_cast<uint64_t>(((seg & 1) * 2 * R * D) >> 4);
+#pragma unroll
+              for (int s = 0; s < D / 32; ++s) umma_f8(tmem + cb * 128 + j * 2 * R, ad + s * 2, bd + s * 2, sdesc_i, s > 0 ? 1u : 0u);
+              umma_commit(&k_empty[k.i]);
+              if (j + 1 == nt) umma_commit(&s_full[cb]);
+              if (t + j + 1 == w.nt) umma_commit(&q_empty[seg & 1]);
+            }
+            __syncwarp();
+            k.step(C::kKeySlots);
+          }
+          if (!failed && chunk > 0 && !results(chunk - 1, last_nt)) failed = true;
+          last_nt = nt;
+        }
+        ++seg;
+      } while (!failed && w.next(p));
+    if (!failed && chunk > 0 && !results(chunk - 1, last_nt)) failed = true;
+    if (failed && issuer) fp8b::raise_error8(p.status, s_abort, kErrMmaA);
+    // tensor memory is released only when every MMA has completed, also where another role has given up
+    if (issuer) umma_commit(drain);
+    uint32_t spin = 0;
+    while (!mbar_try_wait(drain, 0) && ++spin < kSpinLimit) {
+    }
+    __syncwarp();
+  } else if (warp == kQueryWarp) {
+    // ---- queries of a segment (D / 8 lanes per row), then its chunks' block scales (a lane per 16 tokens)
+    constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes, kBatch = 8;
+    float4* table = reinterpret_cast<float4*>(smem + C::kOffScales);
+    int seg = 0, chunk = 0;
+    bool ok = any;
+    if (ok) do {
+        const int rows = w.s.n * p.G, qb = seg & 1;
+        if (seg >= 2 && !mbar_wait_warp(&q_empty[qb], ((seg >> 1) - 1) & 1, s_abort)) {
+          if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrQueriesA);
+          ok = false;
+          break;
+        }
+        uint8_t* to = smem + C::kOffQueries + qb * 2 * R * D;
+        int4* info = reinterpret_cast<int4*>(smem + C::kOffRows) + qb * R;
+        for (int r0 = 0; r0 < rows; r0 += kAtOnce * kBatch) {
+          uint4 x[kBatch];
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            const int r = r0 + i * kAtOnce + lane / kLanes;
+            x[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (r < rows)
+              x[i] = load_chained(reinterpret_cast<const uint4*>(p.q + (w.s.first + r / p.G) * p.ldq + (static_cast<int64_t>(w.h) * p.G + r % p.G) * D + (lane % kLanes) * 8));
+          }
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            const int r = r0 + i * kAtOnce + lane / kLanes;
+            uint32_t a = absmax_bits8(x[i]);
+#pragma unroll
+            for (int o = kLanes / 2; o; o >>= 1) a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
+            const RowScale s = row_scale(a);
+            uint2 first, second;
+            split8(x[i], s.up, first, second);
+            if (r < rows) {
+              const int piece = (lane % kLanes) >> 1, half = (lane & 1) * 8;
+              *reinterpret_cast<uint2*>(to + row_piece<D>(r, piece) + half) = first;
+              *reinterpret_cast<uint2*>(to + row_piece<D>(R + r, piece) + half) = second;
+              if (lane % kLanes == 0) {
+                const int64_t pos = static_cast<int64_t>(w.s.L) - w.s.n + r / p.G;
+                const int64_t hi = p.causal ? min(pos + 1, static_cast<int64_t>(w.s.L)) : w.s.L;
+                const int64_t lo = p.window > 0 ? pos + 1 - p.window : 0;
+                info[r] = make_int4(__float_as_int(s.down * p.scale_log2), static_cast<int>(max(lo, static_cast<int64_t>(0))),
+                                    static_cast<int>(max(hi, static_cast<int64_t>(0))), 0);
+              }
+            }
+          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&q_full[qb]);
+        ++seg;
+        for (int t = 0; t < w.nt; t += kTiles, ++chunk) {
+          const int cb = chunk & 1;
+          float4 e;
+          if (lane < kTiles * 8) {
+            const int64_t token = static_cast<int64_t>(w.s.tile0 + w.t + t) * kTok + lane * 16;
+            e = scale_entry(p.c, w.b, w.h, static_cast<int>(min(token, static_cast<int64_t>(w.s.L))), w.s.L);
+          }
+          if (chunk >= 2 && !mbar_wait_warp(&s_empty[cb], ((chunk >> 1) - 1) & 1, s_abort)) {
+            if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrScalesA);
+            ok = false;
+            break;
+          }
+          if (lane < kTiles * 8) table[cb * kTiles * 8 + lane] = e;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&e_full[cb]);
+        }
+      } while (ok && w.next(p));
+  } else if (warp >= kConvWarp0) {
+    const int i = threadIdx.x - kConvWarp0 * 32;
+    Ring v, o;
+    int n = 0;
+    bool ok = any;
+    if (ok) do {
+        for (int j = 0; j < w.nt; ++j, ++n) {
+          if (!fp8b::mbar_wait_all(&v_full[v.i], v.phase, s_abort) || (n >= 2 && !fp8b::mbar_wait_all(&w_empty[o.i], o.phase ^ 1, s_abort))) {
+            if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrConvertA);
+            ok = false;
+            break;
+          }
+          const int64_t left = w.s.L - static_cast<int64_t>(w.s.tile0 + w.t + j) * kTok;
+          widen_values<D, 128>(smem + C::kOffCodes + v.i * C::kTileBytes, smem + C::kOffValues + o.i * C::kValueBytes, i,
+                               static_cast<int>(min(left, static_cast<int64_t>(kTok))));
+          fence_proxy_async_smem();  // the tensor core reads what these stores wrote
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(&w_full[o.i]);
+            mbar_arrive(&v_empty[v.i]);
+          }
+          v.step(C::kValueSlots);
+          o.step(2);
+        }
+      } while (ok && w.next(p));
+  } else if (warp < kSoftmaxWarps) {
+    // ---- softmax: thread = token of a tile.  Two groups of four warps take tiles in turn; with 64 rows (one tile per chunk)
+    // they take half of its rows each.
+    constexpr bool kHalves = R == 64;
+    constexpr int RR = kHalves ? 32 : R;
+    const int group = warp >> 2, r0 = kHalves ? group * 32 : 0;
+    const int tok = (warp & 3) * 32 + lane;
+    const int me = kHalves ? threadIdx.x & 127 : threadIdx.x;  // among those threads
+    const int red_i = kHalves ? warp & 3 : warp;
+    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const float4* table = reinterpret_cast<const float4*>(smem + C::kOffScales);
+    float* s_max = reinterpret_cast<float*>(smem + C::kOffMax);
+    float* s_red = reinterpret_cast<float*>(smem + C::kOffRed);
+    float* s_sum = reinterpret_cast<float*>(smem + C::kOffSum);
+    bool failed = !any;
+    int chunk = 0, seg = 0;
+    uint32_t met = 0;
+    auto meet_others = [&] {  // the warps that share rows; a barrier whose wait is bounded
+      uint64_t* at = &meet[kHalves ? group : 0];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(at);
+      return fp8b::mbar_wait_all(at, met++ & 1, s_abort);
+    };
+    if (!failed) do {
+        const int rows = min(max(w.s.n * p.G - r0, 0), RR);
+        const int4* info = reinterpret_cast<const int4*>(smem + C::kOffRows) + (seg & 1) * R + r0;
+        if (!fp8b::mbar_wait_all(&q_full[seg & 1], (seg >> 1) & 1, s_abort)) {
+          failed = true;
+          break;
+        }
+        float l[RR];
+#pragma unroll
+        for (int r = 0; r < RR; ++r) l[r] = 0.0f;
+        float m_run = -INFINITY;  // of row r0 + me
+        const int64_t pos0 = static_cast<int64_t>(w.s.L) - w.s.n;
+        for (int t = 0; t < w.nt; t += kTiles, ++chunk) {
+          const int nt = min(kTiles, w.nt - t), cb = chunk & 1;
+          const uint32_t parity = (chunk >> 1) & 1;
+          if (!fp8b::mbar_wait_all(&s_full[cb], parity, s_abort) || !fp8b::mbar_wait_all(&e_full[cb], parity, s_abort)) {
+            failed = true;
+            break;
+          }
+          tc_fence_after_sync();
+          // score of rows r .. r + 7 for this thread's token of tile j, plus the values' scale: f (a + b) keys' scale + log2(values' scale)
+          auto scores = [&](int j, int r, float* x) {
+            const float4 e = table[(cb * kTiles + j) * 8 + (tok >> 4)];
+            const int64_t tile = static_cast<int64_t>(w.s.tile0 + w.t + t + j) * kTok;
+            const int64_t at = tile + tok;
+            // all of the tile is seen by all rows (the first row sees the fewest behind, the last the fewest before)
+            const bool all = tile + kTok <= (p.causal ? pos0 + 1 : w.s.L) && (p.window == 0 || tile >= w.s.L - p.window);
+            float y[8];
+            const uint32_t from = tmem + lane_base + cb * 128 + j * 2 * R + r0 + r;
+            tmem_ld8(from, x);
+            tmem_ld8(from + R, y);
+            tmem_ld_wait_regs<8>(x);
+            tmem_ld_wait_regs<8>(y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int4 ri = info[r + i];
+              x[i] = fmaf(x[i] + y[i], __int_as_float(ri.x) * e.x, e.y);
+              if (!all && !(at >= ri.y && at < ri.z)) x[i] = -INFINITY;
+            }
+          };
+          const int j0 = kHalves ? 0 : group, dj = kHalves ? 1 : 2;
+#pragma unroll
+          for (int r = 0; r < RR; r += 8)
+            if (r < rows) {
+              float mx[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) mx[i] = -INFINITY;
+              for (int j = j0; j < nt; j += dj) {
+                float x[8];
+                scores(j, r, x);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) mx[i] = fmaxf(mx[i], x[i]);
+              }
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                mx[i] = warp_max(mx[i]);
+                if (lane == 0) s_red[(r0 + r + i) * 8 + red_i] = mx[i];
+              }
+            }
+          // the chunk two before is through the epilogue: its factors, and its probabilities, make room
+          if (chunk >= 2 && !fp8b::mbar_wait_all(&o_empty[cb], ((chunk >> 1) - 1) & 1, s_abort)) failed = true;
+          if (!meet_others()) failed = true;
+          if (me < rows) {
+            const float4* v = reinterpret_cast<const float4*>(s_red + (r0 + me) * 8);
+            const float4 a = v[0];
+            float m = fmaxf(fmaxf(m_run, fmaxf(a.x, a.y)), fmaxf(a.z, a.w));
+            if (!kHalves) {
+              const float4 b = v[1];
+              m = fmaxf(m, fmaxf(fmaxf(b.x, b.y), fmaxf(b.z, b.w)));
+            }
+            const float safe = m == -INFINITY ? 0.0f : m;
+            s_max[cb * R + r0 + me] = kShift - safe;
+            s_max[2 * R + cb * R + r0 + me] = exp2f(m_run - safe);
+            m_run = m;
+          }
+          if (!meet_others()) failed = true;
+          if (failed) break;
+#pragma unroll
+          for (int r = 0; r < RR; ++r)
+            if (r < rows) l[r] *= s_max[2 * R + cb * R + r0 + r];
+          for (int j = j0; j < nt; j += dj) {
+            const float inv = table[(cb * kTiles + j) * 8 + (tok >> 4)].z;
+            // the operand's rows: 64 tokens (128 bytes) each, the next 64 tokens R rows further
+            uint8_t* to = smem + C::kOffProbs + (cb * kTiles + j) * C::kProbBytes + (tok >> 6) * (R * 128) + (tok & 7) * 2;
+            const int piece = (tok & 63) >> 3;
+#pragma unroll
+            for (int r = 0; r < RR; r += 8)
+              if (r < rows) {
+                float x[8];
+                scores(j, r, x);
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                  const float a = fp8b::sfu_ex2(x[i] + s_max[cb * R + r0 + r + i]), b = fp8b::sfu_ex2(x[i + 1] + s_max[cb * R + r0 + r + i + 1]);
+                  l[r + i] = fmaf(a, inv, l[r + i]);
+                  l[r + i + 1] = fmaf(b, inv, l[r + i + 1]);
+                  const uint32_t h = pack_f16(a, b);
+                  *reinterpret_cast<uint16_t*>(to + (r0 + r + i) * 128 + ((piece ^ i) << 4)) = static_cast<uint16_t>(h);
+                  *reinterpret_cast<uint16_t*>(to + (r0 + r + i + 1) * 128 + ((piece ^ (i + 1)) << 4)) = static_cast<uint16_t>(h >> 16);
+                }
+              }
+          }
+          fence_proxy_async_smem();
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(&s_empty[cb]);
+            mbar_arrive(&p_full[cb]);
+          }
+        }
+        if (failed) break;
+        // sums of the segment
+        if (seg > 0 && !fp8b::mbar_wait_all(l_empty, (seg - 1) & 1, s_abort)) {
+          failed = true;
+          break;
+        }
+#pragma unroll
+        for (int r = 0; r < RR; ++r)
+          if (r < rows) {
+            float v = l[r];
+#pragma unroll
+            for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+            if (lane == 0) s_sum[(r0 + r) * 8 + red_i] = v;
+          }
+        if (me < rows) s_sum[R * 8 + r0 + me] = m_run;
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(l_full);
+          mbar_arrive(&q_empty[seg & 1]);
+        }
+        ++seg;
+      } while (w.next(p));
+    if (failed && any && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrSoftmaxA);
+  } else {
+    // ---- epilogue: thread = feature
+    const int d = (warp & 3) * 32 + lane;
+    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const float* s_max = reinterpret_cast<const float*>(smem + C::kOffMax);
+    const float* s_sum = reinterpret_cast<const float*>(smem + C::kOffSum);
+    const int64_t total = s_scan[31], ctas = min(static_cast<int64_t>(gridDim.x), total);
+    bool failed = !any;
+    int chunk = 0, seg = 0;
+    int64_t unit = any ? total * blockIdx.x / ctas : 0;
+    if (!failed) do {
+        const int rows = w.s.n * p.G;
+        float o[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) o[r] = 0.0f;
+        for (int t = 0; t < w.nt; t += kTiles, ++chunk) {
+          const int cb = chunk & 1;
+          const uint32_t parity = (chunk >> 1) & 1;
+          if (!fp8b::mbar_wait_all(&p_full[cb], parity, s_abort) || !fp8b::mbar_wait_all(&o_full[cb], parity, s_abort)) {
+            failed = true;
+            break;
+          }
+          tc_fence_after_sync();
+#pragma unroll
+          for (int r = 0; r < R; r += 8)
+            if (r < rows) {
+              float x[8];
+              tmem_ld8(tmem + lane_base + 256 + cb * R + r, x);
+              tmem_ld_wait_regs<8>(x);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) o[r + i] = fmaf(o[r + i], s_max[2 * R + cb * R + r + i], x[i]);
+            }
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&o_empty[cb]);
+        }
+        if (failed || !fp8b::mbar_wait_all(l_full, seg & 1, s_abort)) {
+          failed = true;
+          break;
+        }
+        const bool whole = w.whole();
+        float* part = p.partial + (static_cast<int64_t>(blockIdx.x) * 2 + (w.t == 0 ? 1 : 0)) * (R * (D + 2));
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          if (r < rows) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int k = 0; k < (R == 64 ? 4 : 8); ++k) sum += s_sum[r * 8 + k];
+            const float m = s_sum[R * 8 + r];
+            if (!whole) {
+              if (d < D) part[r * D + d] = o[r];
+              if (d == 0) {
+                part[R * D + r] = sum;
+                part[R * D + R + r] = m;
+              }
+            } else {
+              const int64_t row = w.s.first + r / p.G;
+              const int hq = w.h * p.G + r % p.G;
+              const float v = sum == 0.0f ? 0.0f : o[r] / sum;
+              if (d < D) {
+                const int64_t at = row * p.ldo + static_cast<int64_t>(hq) * D + d;
+                if (F32)
+                  static_cast<float*>(p.out)[at] = v;
+                else
+                  static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
+              }
+              if (p.lse && d == 0) p.lse[row * (static_cast<int64_t>(p.G) * p.c.H) + hq] = sum == 0.0f ? -INFINITY : (log2f(sum) + m + 8.0f - kShift) * (1.0f / kLog2e);
+            }
+          }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(l_empty);
+        if (w.t == 0 && threadIdx.x == kEpiWarp0 * 32) {
+          // the CTAs that share this sequence and head: to the one whose range holds its last tile
+          const int64_t last = unit + w.s.tiles - 1;
+          int64_t cta = whole ? blockIdx.x : last * ctas / total;
+          while (!whole && total * (cta + 1) / ctas <= last) ++cta;
+          p.pieces[static_cast<int64_t>(w.b) * p.c.H + w.h] = make_int2(blockIdx.x, static_cast<int>(cta - blockIdx.x) + 1);
+        }
+        unit += w.nt;
+        ++seg;
+      } while (w.next(p));
+    if (failed && any && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrEpilogueA);
+  }
+
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// Results of sequences and heads that several CTAs share: a block per sequence and head, a thread per feature and every fourth row.
+template <int D, int R, bool F32>
+__global__ void __launch_bounds__(4 * D) attention_join_kernel(const P p) {
+  __shared__ float s_w[kMaxCtas];
+  __shared__ float s_l;
+  pdl_launch_dependents();
+  pdl_wait();
+  const int b = blockIdx.x / p.c.H, h = blockIdx.x % p.c.H;
+  const Seq s = seq_of(p, b);
+  if (s.tiles == 0) return;
+  const int x = load_chained(reinterpret_cast<const int*>(p.pieces + blockIdx.x));
+  const int n = load_chained(reinterpret_cast<const int*>(p.pieces + blockIdx.x) + 1);
+  if (n <= 1 || n > kMaxCtas) return;
+  const int rows = s.n * p.G;
+  constexpr int64_t kPart = R * (D + 2);
+  // piece i: the first CTA's second place, the others' first
+  auto part = [&](int i) { return p.partial + (static_cast<int64_t>(x + i) * 2 + (i == 0 ? 1 : 0)) * kPart; };
+  for (int r = blockIdx.y; r < rows; r += gridDim.y) {
+    __syncthreads();
+    if (threadIdx.x < 32) {
+      float m = -INFINITY;
+      for (int i = threadIdx.x; i < n; i += 32) m = fmaxf(m, load_chained(part(i) + R * D + R + r));
+      m = warp_max(m);
+      float l = 0.0f;
+      for (int i = threadIdx.x; i < n; i += 32) {
+        const float mi = load_chained(part(i) + R * D + R + r);
+        const float f = mi == -INFINITY ? 0.0f : exp2f(mi - m);
+        s_w[i] = f;
+        l = fmaf(f, load_chained(part(i) + R * D + r), l);
+      }
+#pragma unroll
+      for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
+      if (threadIdx.x == 0) {
+        s_l = l;
+        const int64_t row = s.first + r / p.G;
+        const int hq = h * p.G + r % p.G;
+        if (p.lse) p.lse[row * (static_cast<int64_t>(p.G) * p.c.H) + hq] = l == 0.0f ? -INFINITY : (log2f(l) + m + 8.0f - kShift) * (1.0f / kLog2e);
+      }
+    }
+    __syncthreads();
+    const int d = threadIdx.x % D, k = threadIdx.x / D;
+    __shared__ float s_o[4][D];
+    float o = 0.0f;
+#pragma unroll 4
+    for (int i = k; i < n; i += 4) o = fmaf(s_w[i], load_chained(part(i) + r * D + d), o);
+    s_o[k][d] = o;
+    __syncthreads();
+    if (k == 0) {
+      o = s_o[0][d] + s_o[1][d] + s_o[2][d] + s_o[3][d];
+      const float v = s_l == 0.0f ? 0.0f : o / s_l;
+      const int64_t at = (s.first + r / p.G) * p.ldo + (static_cast<int64_t>(h) * p.G + r % p.G) * D + d;
+      if (F32)
+        static_cast<float*>(p.out)[at] = v;
+      else
+        static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
+    }
+  }
+}
+
+template <int D, int R, bool F32>
+int launch_cfg(const CUtensorMap& tm, const P& p, int grid, int max_rows, cudaStream_t st) {
+  using C = Cfg<D, R>;
+  static DeviceOnce once;
+  if (!allow_shared_memory(once, attention_few_kernel<D, R, F32>, C::kSmemBytes)) return ZQ_ERR_CUDA;
+  cudaError_t e = launch_chained(attention_few_kernel<D, R, F32>, dim3(grid), dim3(kThreads), C::kSmemBytes, st, false, tm, p);
+  count_launch();
+  if (e != cudaSuccess) return ZQ_ERR_CUDA;
+  const int64_t blocks = static_cast<int64_t>(p.c.B) * p.c.H;
+  e = launch_chained(attention_join_kernel<D, R, F32>, dim3(static_cast<unsigned>(blocks), max_rows), dim3(4 * D), 0, st, false, p);
+  count_launch();
+  return e == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
+}
+template <int D, int R>
+int launch_type(const CUtensorMap& tm, const P& p, int grid, int max_rows, int dt, cudaStream_t st) {
+  return dt == ZQ_OUT_F32 ? launch_cfg<D, R, true>(tm, p, grid, max_rows, st) : launch_cfg<D, R, false>(tm, p, grid, max_rows, st);
+}
+template <int D>
+int launch_rows(const CUtensorMap& tm, const P& p, int grid, int max_rows, int dt, cudaStream_t st) {
+  if (max_rows <= 16) return launch_type<D, 16>(tm, p, grid, max_rows, dt, st);
+  if (max_rows <= 32) return launch_type<D, 32>(tm, p, grid, max_rows, dt, st);
+  return launch_type<D, 64>(tm, p, grid, max_rows, dt, st);
+}
+
+}  // namespace
+
+// Sums of two pieces per CTA, and which CTAs share a sequence and head.
+size_t few_workspace_bytes(int64_t B, int64_t H, int64_t D) {
+  return (sizeof(float) * kMaxCtas * 2 * kFewRows * (D + 2) + 255) / 256 * 256 + (sizeof(int2) * B * H + 255) / 256 * 256;
+}
+
+// max_rows: no sequence and head of this kernel has more rows.
+int launch_attention_few(const AttnArgs& a, int max_rows, cudaStream_t st) {
+  if (static_cast<int64_t>(a.c.B) * a.c.H > 0x7FFFFFFF) return ZQ_ERR_SHAPE;
+  P p{};
+  p.c = a.c;
+  p.q = static_cast<const __nv_bfloat16*>(a.q), p.ldq = a.ldq, p.G = a.Hq / a.c.H;
+  p.scale_log2 = a.sm_scale * kLog2e;
+  p.causal = a.causal, p.window = a.window;
+  p.out = a.out, p.ldo = a.ldo, p.lse = a.lse;
+  uint8_t* ws = static_cast<uint8_t*>(a.workspace);
+  p.status = reinterpret_cast<int*>(ws);
+  p.partial = reinterpret_cast<float*>(ws + kWsHeadBytes);
+  p.pieces = reinterpret_cast<int2*>(ws + kWsHeadBytes + (sizeof(float) * kMaxCtas * 2 * kFewRows * (a.c.D + 2) + 255) / 256 * 256);
+  CUtensorMap tm;
+  if (!make_page_map(&tm, a.c)) return ZQ_ERR_CUDA;
+  const int sms = sm_count(), grid = sms < kMaxCtas ? sms : kMaxCtas;
+  return a.c.D == 128 ? launch_rows<128>(tm, p, grid, max_rows, a.dt, st) : launch_rows<64>(tm, p, grid, max_rows, a.dt, st);
+}
+
+}  // namespace kv
+}  // namespace zq

@@ -2,7 +2,7 @@
 // over it.  Argument validation and dispatch; the operators are defined in include/zqfp.h.
 #include <cmath>
 
-#include "kv_cache.cuh"
+#include "kv_attention.cuh"
 
 using namespace zq;
 using namespace zq::kv;
@@ -145,7 +145,7 @@ int zq_kv_cache_read(const uint8_t* codes, const float* scale, int64_t pages, in
 
 size_t zq_kv_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D) {
   if (T < 0 || B < 0 || T > kMaxRows || B > kMaxRows || H < 1 || H > kMaxHeads || Hq < H || Hq > kMaxHeads || Hq % H || !dim_ok(D)) return 0;
-  return kWsHeadBytes;
+  return kWsHeadBytes + few_workspace_bytes(B, H, D);
 }
 
 int zq_kv_attention(const void* q, int64_t ldq, int64_t Hq, int64_t T, const int32_t* cu, int64_t B, const int32_t* lens,
