@@ -11,10 +11,9 @@ constexpr int kTok = 128;           // tokens of a tile
 constexpr int kFewRows = 64;        // rows (new tokens x query heads of a cache head) up to which the kernel for few rows takes a sequence
 constexpr int kMaxCtas = 148;       // CTAs whose partial results the workspace has room for
 constexpr float kLog2e = 1.4426950408889634f;
-// Probabilities are kept times 2^kShift (the row's largest at most 2^kShift), where FP16 holds 11 bits down to 2^-28 of the
-// largest and something down to 2^-38; values are kept as code / 256.  Both cancel against the sum of the probabilities.
-constexpr float kShift = 14.0f;
-constexpr float kCodeUnit = 1.0f / 256.0f;
+// Probabilities are kept times 2^kShift (the row's largest at most 2^kShift), where FP16 holds 11 bits down to 2^-22 of the
+// largest and something down to 2^-32.  The factor cancels against the sum of the probabilities.
+constexpr float kShift = 8.0f;
 
 int launch_attention_few(const AttnArgs& a, int max_rows, cudaStream_t st);
 size_t few_workspace_bytes(int64_t B, int64_t H, int64_t D);
@@ -61,37 +60,37 @@ __device__ __forceinline__ void umma_f16(uint32_t d_tmem, uint64_t a_desc, uint6
       : "memory");
 }
 
-// Codes of four E4M3 numbers -> FP16 code / 256, two and two: the exponent and mantissa bits moved into FP16's fields (which
-// have one exponent bit more, whence the factor; subnormal numbers come out right as well).  The pattern of E4M3's NaN
-// becomes 480 / 256: what nobody sees must not turn into NaN by a product with zero.
-__device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  const uint32_t a = __byte_perm(w, 0u, 0x1404), b = __byte_perm(w, 0u, 0x3424);  // each code in the upper byte of a half
-  lo = (a & 0x80008000u) | ((a >> 1) & 0x3F803F80u);
-  hi = (b & 0x80008000u) | ((b >> 1) & 0x3F803F80u);
+// A converter thread's share of a tile of values: codes [128][D] (rows as they lie in memory) -> FP16 in the operand's layout, each
+// code's own value.  Tokens from `valid` on become zeros, whatever the page holds there.  All of the share's codes are loaded
+// before the first store (the compiler cannot tell their addresses apart), kAtOnce pieces of 16 at a time.
+__device__ __forceinline__ uint32_t widen2(uint32_t codes) {  // the lower two
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(codes)));
+  return h;
 }
-// A converter thread's share of a tile of values: codes [128][D] (rows as they lie in memory) -> FP16 in the operand's layout.
-// Tokens from `valid` on become zeros, whatever the page holds there.
 template <int D, int THREADS>
 __device__ __forceinline__ void widen_values(const uint8_t* codes, uint8_t* out, int i, int valid) {
-  constexpr int kPieces = kTok * D / 16, kPerRow = D / 16;
-  static_assert(kPieces % THREADS == 0, "pieces per thread");
+  constexpr int kPieces = kTok * D / 16 / THREADS, kPerRow = D / 16, kAtOnce = kPieces < 4 ? kPieces : 4;
+  static_assert(kTok * D / 16 % THREADS == 0 && THREADS % kPerRow == 0 && kPieces % kAtOnce == 0, "pieces per thread");
+  // pieces of a thread are THREADS / kPerRow rows apart, a multiple of 8: their swizzle is the same
+  static_assert(THREADS / kPerRow % 8 == 0, "rows");
+  const int row0 = i / kPerRow, c = i % kPerRow, sw = row0 & 7, p = (c & 3) * 2;
+  uint8_t* to = out + (c >> 2) * (kTok * 128) + row0 * 128;
+  const int to0 = (p ^ sw) << 4, to1 = ((p + 1) ^ sw) << 4;
 #pragma unroll
-  for (int x = 0; x < kPieces / THREADS; ++x) {
-    const int at = x * THREADS + i, row = at / kPerRow, c = at % kPerRow;
-    const uint4 v = *reinterpret_cast<const uint4*>(codes + at * 16);
-    uint32_t o[8];
-    widen4(v.x, o[0], o[1]);
-    widen4(v.y, o[2], o[3]);
-    widen4(v.z, o[4], o[5]);
-    widen4(v.w, o[6], o[7]);
-    if (row >= valid) {
+  for (int x0 = 0; x0 < kPieces; x0 += kAtOnce) {
+    uint4 v[kAtOnce];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = 0u;
+    for (int x = 0; x < kAtOnce; ++x) {
+      v[x] = *reinterpret_cast<const uint4*>(codes + ((x0 + x) * THREADS + i) * 16);
+      if (row0 + (x0 + x) * (THREADS / kPerRow) >= valid) v[x] = make_uint4(0u, 0u, 0u, 0u);
     }
-    uint8_t* dst = out + (c >> 2) * (kTok * 128) + row * 128;
-    const int p = (c & 3) * 2, sw = row & 7;
-    *reinterpret_cast<uint4*>(dst + ((p ^ sw) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-    *reinterpret_cast<uint4*>(dst + (((p + 1) ^ sw) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+#pragma unroll
+    for (int x = 0; x < kAtOnce; ++x) {
+      uint8_t* dst = to + (x0 + x) * (THREADS / kPerRow) * 128;
+      *reinterpret_cast<uint4*>(dst + to0) = make_uint4(widen2(v[x].x), widen2(v[x].x >> 16), widen2(v[x].y), widen2(v[x].y >> 16));
+      *reinterpret_cast<uint4*>(dst + to1) = make_uint4(widen2(v[x].z), widen2(v[x].z >> 16), widen2(v[x].w), widen2(v[x].w >> 16));
+    }
   }
 }
 
@@ -133,7 +132,7 @@ __device__ __forceinline__ void split8(uint4 v, float up, uint2& first, uint2& s
 }
 
 // ---- block scales -------------------------------------------------------------------------------------------------------
-// What 16 tokens of a tile (part of one page) contribute: keys' scale, log2 of the values' scale, its inverse times kCodeUnit.
+// What 16 tokens of a tile (part of one page) contribute: keys' scale, log2 of the values' scale, its inverse.
 // The values' scale goes into the power of two of the probability, so that nothing of it is rounded apart, and comes out of the
 // sum again by its inverse.
 __device__ __forceinline__ float4 scale_entry(const Cache& c, int b, int h, int token, int L) {
@@ -145,7 +144,7 @@ __device__ __forceinline__ float4 scale_entry(const Cache& c, int b, int h, int 
   if (vs < 5.42101086242752217e-20f) vs = 5.42101086242752217e-20f;  // 2^-64: what was never written has 0
   e.x = ks;
   e.y = log2f(vs);
-  e.z = kCodeUnit / vs;
+  e.z = 1.0f / vs;
   return e;
 }
 

@@ -15,7 +15,7 @@
 // attention_join_kernel adds them up in the order of the tiles.
 //
 // Warp roles: 0..7 softmax (thread = token), 8..11 epilogue (thread = feature), 12..15 converters of values, 16 keys' copies,
-// 17 values' copies, 18 MMAs, 19 queries and scales.
+// 17 values' copies, 18 MMAs, 19 the walk, queries and scales.
 #include "kv_attention.cuh"
 
 namespace zq {
@@ -35,11 +35,25 @@ struct P {
   int causal, window;
   void* out;
   int64_t ldo;
+  int f32;
   float* lse;
   float* partial;    // [CTAs][2][R (D + 2)]
   int2* pieces;      // [B * H]: first CTA and number of CTAs of a sequence and head
   int* status;
 };
+
+// A segment, as the queries' warp announces it to the others in shared memory (kSegs of them in turn).
+struct alignas(16) Seg {
+  int nt;           // tiles; 0: no more segments
+  int tile0;        // the first of them, of the sequence's tiles of 128 tokens
+  int L, n;         // tokens and new tokens of the sequence
+  int b, h, first;  // sequence, head, the sequence's first row
+  int flags;        // 1: begins with the first tile that the sequence and head have here; 2: ends with the last
+};
+constexpr int kSegs = 4;
+
+// Registers per thread behind the set-up: softmax 120 (two warpgroups), epilogue 96 as launched, converters 64, the others 80;
+// 2 x 120 + 96 + 64 + 80 = 480, the five warpgroups' 5 x 96 at launch.
 
 template <int D, int R>
 struct Cfg {
@@ -55,7 +69,8 @@ struct Cfg {
   static constexpr int kOffMax = kOffRows + 2 * R * 16;                         // [2][R] maximum, [2][R] factor of what came before
   static constexpr int kOffRed = kOffMax + 4 * R * 4;                           // [R][8] warps' maxima
   static constexpr int kOffSum = kOffRed + R * 8 * 4;                           // [R][8] warps' sums, [R] maxima
-  static constexpr int kOffBars = kOffSum + R * 9 * 4;
+  static constexpr int kOffSegs = kOffSum + R * 9 * 4;                          // [kSegs]
+  static constexpr int kOffBars = kOffSegs + kSegs * 32;
   static constexpr int kFixed = (kOffBars + 64 * 8 + 36 * 8 + 1023) / 1024 * 1024;
   static constexpr int kSlots0 = (227 * 1024 - kFixed) / kTileBytes;
   static constexpr int kSlots = kSlots0 < 16 ? kSlots0 : 16;
@@ -63,7 +78,7 @@ struct Cfg {
   static constexpr int kOffKeys = kFixed;
   static constexpr int kOffCodes = kOffKeys + kKeySlots * kTileBytes;
   static constexpr int kSmemBytes = kOffCodes + kValueSlots * kTileBytes;
-  static constexpr int kNumBars = 2 * kKeySlots + 2 * kValueSlots + 4 + 14 + 5;
+  static constexpr int kNumBars = 2 * kKeySlots + 2 * kValueSlots + 4 + 14 + 5 + 2 * kSegs;
   static_assert(kSmemBytes <= 227 * 1024 && kNumBars <= 64 && kSlots >= 4, "shared memory");
 };
 
@@ -115,8 +130,15 @@ struct Walk {
     nt = static_cast<int>(min(static_cast<int64_t>(s.tiles), left));
     return true;
   }
-  __device__ __forceinline__ bool whole() const { return nt == s.tiles; }
 };
+
+template <int S>
+__device__ __forceinline__ void load_scores(uint32_t taddr, float* v) {
+  if (S == 4)
+    tmem_ld4(taddr, v);
+  else
+    tmem_ld8(taddr, v);
+}
 
 // A ring position.
 struct Ring {
@@ -130,7 +152,9 @@ struct Ring {
   }
 };
 
-template <int D, int R, bool F32>
+// R: columns of the tensor core for the rows (16, 32, 64); RS: rows that are worked on, at least those there are (the rest of the RS
+// are computed from whatever lies there and not looked at: a jump past them costs more, in instructions fetched anew).
+template <int D, int R, int RS>
 __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid_constant__ CUtensorMap tm, const P p) {
   using C = Cfg<D, R>;
   constexpr int kTiles = C::kTiles;
@@ -153,7 +177,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
   uint64_t* l_full = q_empty + 2;                    // sums of a segment                                      (epilogue)
   uint64_t* l_empty = l_full + 1;                    // they have been read                                    (softmax)
   uint64_t* meet = l_empty + 1;                      // [2] softmax warps that share rows
-  uint64_t* drain = meet + 2;
+  uint64_t* g_full = meet + 2;                       // [kSegs] a segment is announced                         (all)
+  uint64_t* g_empty = g_full + kSegs;                // [kSegs] everybody is through with it                   (queries)
+  uint64_t* drain = g_empty + kSegs;
+  const Seg* s_seg = reinterpret_cast<const Seg*>(smem + C::kOffSegs);
   int64_t* s_range = reinterpret_cast<int64_t*>(smem + C::kOffBars + 64 * 8);  // units, first sequence, first unit in it
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_range + 3);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
@@ -185,6 +212,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     mbar_init(l_empty, 4);
     mbar_init(&meet[0], R == 64 ? 4 : 8);
     mbar_init(&meet[1], 4);
+    for (int i = 0; i < kSegs; ++i) {
+      mbar_init(&g_full[i], 1);
+      mbar_init(&g_empty[i], kThreads / 32 - 1);
+    }
     mbar_init(drain, 1);
     *s_abort = 0;
     s_range[0] = 0;
@@ -235,48 +266,59 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
   }
   __syncthreads();
   const uint32_t tmem = *s_tmem;
-  const bool ok_start = *s_abort == 0;
-  Walk w;
-  const bool any = w.start(p, s_range) && ok_start;
+  const bool any = *s_abort == 0 && s_range[0] > 0;
+  // The next segment of a role: false behind the last one, and where something has failed.
+  auto segment = [&](int seg, int& nt) {
+    if (!fp8b::mbar_wait_all(&g_full[seg % kSegs], (seg / kSegs) & 1, s_abort)) return false;
+    nt = s_seg[seg % kSegs].nt;
+    return nt > 0;
+  };
+  auto done_with = [&](int seg) {  // a warp, converged
+    if (lane == 0) mbar_arrive(&g_empty[seg % kSegs]);
+  };
 
   if (warp == kKeyWarp || warp == kValueWarp) {
     // ---- copies: a lane per page of the tile
+    fp8b::regs_give<80>();
     const bool keys = warp == kKeyWarp;
     const int slots = keys ? C::kKeySlots : C::kValueSlots;
     uint64_t *full = keys ? k_full : v_full, *empty = keys ? k_empty : v_empty;
     uint8_t* to = smem + (keys ? C::kOffKeys : C::kOffCodes);
     const int per = kTok / p.c.page, page_bytes = p.c.page * D;
     Ring r;
-    int issued = 0;
+    int issued = 0, nt;
     bool ok = any;
-    if (ok) do {
-        const int t0 = w.s.tile0 + w.t;
-        PageWalk pages;
-        pages.start(p.c, w.b, w.s.L, t0 * per, lane);
-        for (int j = 0; j < w.nt; ++j) {
-          const int page = pages.get(p.c, (t0 + j) * per, lane);
-          if (issued >= slots && !mbar_wait_warp(&empty[r.i], r.phase ^ 1, s_abort)) {
-            if (lane == 0) fp8b::raise_error8(p.status, s_abort, keys ? kErrKeysA : kErrValuesA);
-            ok = false;
-            break;
-          }
-          const bool has = lane < per && page >= 0;
-          const uint32_t n = __popc(__ballot_sync(0xFFFFFFFFu, has));
-          if (lane == 0) mbar_arrive_expect_tx(&full[r.i], n * page_bytes);
-          __syncwarp();
-          if (has) {
-            uint8_t* dst = to + r.i * C::kTileBytes + lane * page_bytes;
-            const int64_t block = block_at(p.c, page, keys ? 0 : 1, w.h);
-            if (keys)
-              tma_load_3d(dst, &tm, 0, 0, static_cast<int>(block), &full[r.i]);
-            else
-              bulk_load(dst, p.c.codes + block * page_bytes, page_bytes, &full[r.i]);
-          }
-          __syncwarp();
-          ++issued;
-          r.step(slots);
+    for (int seg = 0; ok && segment(seg, nt); ++seg) {
+      const Seg& g = s_seg[seg % kSegs];
+      const int t0 = g.tile0, h = g.h;
+      PageWalk pages;
+      pages.start(p.c, g.b, g.L, t0 * per, lane);
+      __syncwarp();
+      done_with(seg);
+      for (int j = 0; j < nt; ++j) {
+        const int page = pages.get(p.c, (t0 + j) * per, lane);
+        if (issued >= slots && !mbar_wait_warp(&empty[r.i], r.phase ^ 1, s_abort)) {
+          if (lane == 0) fp8b::raise_error8(p.status, s_abort, keys ? kErrKeysA : kErrValuesA);
+          ok = false;
+          break;
         }
-      } while (ok && w.next(p));
+        const bool has = lane < per && page >= 0;
+        const uint32_t n = __popc(__ballot_sync(0xFFFFFFFFu, has));
+        if (lane == 0) mbar_arrive_expect_tx(&full[r.i], n * page_bytes);
+        __syncwarp();
+        if (has) {
+          uint8_t* dst = to + r.i * C::kTileBytes + lane * page_bytes;
+          const int64_t block = block_at(p.c, page, keys ? 0 : 1, h);
+          if (keys)
+            tma_load_3d(dst, &tm, 0, 0, static_cast<int>(block), &full[r.i]);
+          else
+            bulk_load(dst, p.c.codes + block * page_bytes, page_bytes, &full[r.i]);
+        }
+        __syncwarp();
+        ++issued;
+        r.step(slots);
+      }
+    }
     // never leave with copies still in flight
     for (int i = max(0, issued - slots); i < issued; ++i) {
       uint32_t spin = 0;
@@ -284,6 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
       }
     }
   } else if (warp == kMmaWarp) {
+    fp8b::regs_give<80>();
     const bool issuer = elect_one();
     const uint64_t kdesc = desc_rows<D>(smem_u32(smem + C::kOffKeys)), qdesc = desc_rows<D>(smem_u32(smem + C::kOffQueries));
     const uint64_t vdesc = desc_values(smem_u32(smem + C::kOffValues));
@@ -314,34 +357,35 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
       return true;
     };
     int last_nt = 0;  // tiles of the chunk whose scores are issued and whose results are not
-    if (any) do {
-        if (!mbar_wait(&q_full[seg & 1], (seg >> 1) & 1, s_abort)) failed = true;
-        for (int t = 0; t < w.nt && !failed; t += kTiles, ++chunk) {
-          const int nt = min(kTiles, w.nt - t), cb = chunk & 1;
-          if (chunk >= 2 && !mbar_wait(&s_empty[cb], ((chunk >> 1) - 1) & 1, s_abort)) failed = true;
-          for (int j = 0; j < nt && !failed; ++j) {
-            if (!mbar_wait(&k_full[k.i], k.phase, s_abort)) {
-              failed = true;
-              break;
-            }
-            tc_fence_after_sync();
-            if (issuer) {
-              const uint64_t ad = kdesc + static_cast<uint64_t>((k.i * C::kTileBytes) >> 4);
-              const uint64_t bd = qdesc + static_cast<uint64_t>(((seg & 1) * 2 * R * D) >> 4);
-#pragma unroll
-              for (int s = 0; s < D / 32; ++s) umma_f8(tmem + cb * 128 + j * 2 * R, ad + s * 2, bd + s * 2, sdesc_i, s > 0 ? 1u : 0u);
-              umma_commit(&k_empty[k.i]);
-              if (j + 1 == nt) umma_commit(&s_full[cb]);
-              if (t + j + 1 == w.nt) umma_commit(&q_empty[seg & 1]);
-            }
-            __syncwarp();
-            k.step(C::kKeySlots);
+    int nt_seg;
+    for (; any && !failed && segment(seg, nt_seg); ++seg) {
+      done_with(seg);
+      if (!mbar_wait(&q_full[seg & 1], (seg >> 1) & 1, s_abort)) failed = true;
+      for (int t = 0; t < nt_seg && !failed; t += kTiles, ++chunk) {
+        const int nt = min(kTiles, nt_seg - t), cb = chunk & 1;
+        if (chunk >= 2 && !mbar_wait(&s_empty[cb], ((chunk >> 1) - 1) & 1, s_abort)) failed = true;
+        for (int j = 0; j < nt && !failed; ++j) {
+          if (!mbar_wait(&k_full[k.i], k.phase, s_abort)) {
+            failed = true;
+            break;
           }
-          if (!failed && chunk > 0 && !results(chunk - 1, last_nt)) failed = true;
-          last_nt = nt;
+          tc_fence_after_sync();
+          if (issuer) {
+            const uint64_t ad = kdesc + static_cast<uint64_t>((k.i * C::kTileBytes) >> 4);
+            const uint64_t bd = qdesc + static_cast<uint64_t>(((seg & 1) * 2 * R * D) >> 4);
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s) umma_f8(tmem + cb * 128 + j * 2 * R, ad + s * 2, bd + s * 2, sdesc_i, s > 0 ? 1u : 0u);
+            umma_commit(&k_empty[k.i]);
+            if (j + 1 == nt) umma_commit(&s_full[cb]);
+            if (t + j + 1 == nt_seg) umma_commit(&q_empty[seg & 1]);
+          }
+          __syncwarp();
+          k.step(C::kKeySlots);
         }
-        ++seg;
-      } while (!failed && w.next(p));
+        if (!failed && chunk > 0 && !results(chunk - 1, last_nt)) failed = true;
+        last_nt = nt;
+      }
+    }
     if (!failed && chunk > 0 && !results(chunk - 1, last_nt)) failed = true;
     if (failed && issuer) fp8b::raise_error8(p.status, s_abort, kErrMmaA);
     // tensor memory is released only when every MMA has completed, also where another role has given up
@@ -352,12 +396,35 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     __syncwarp();
   } else if (warp == kQueryWarp) {
     // ---- queries of a segment (D / 8 lanes per row), then its chunks' block scales (a lane per 16 tokens)
+    fp8b::regs_give<80>();
     constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes, kBatch = 8;
     float4* table = reinterpret_cast<float4*>(smem + C::kOffScales);
     int seg = 0, chunk = 0;
-    bool ok = any;
+    Walk w;
+    bool ok = any && w.start(p, s_range);
+    // announces segment `seg`, or (nt = 0) that there are no more
+    auto announce = [&](int nt) {
+      if (seg >= kSegs && !mbar_wait_warp(&g_empty[seg % kSegs], (seg / kSegs - 1) & 1, s_abort)) return false;
+      if (lane == 0) {
+        Seg g{};
+        g.nt = nt;
+        if (nt > 0) {
+          g.tile0 = w.s.tile0 + w.t, g.L = w.s.L, g.n = w.s.n, g.b = w.b, g.h = w.h, g.first = w.s.first;
+          g.flags = (w.t == 0 ? 1 : 0) | (w.t + nt == w.s.tiles ? 2 : 0);
+        }
+        *const_cast<Seg*>(s_seg + seg % kSegs) = g;
+        mbar_arrive(&g_full[seg % kSegs]);
+      }
+      __syncwarp();
+      return true;
+    };
     if (ok) do {
         const int rows = w.s.n * p.G, qb = seg & 1;
+        if (!announce(w.nt)) {
+          if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrQueriesA);
+          ok = false;
+          break;
+        }
         if (seg >= 2 && !mbar_wait_warp(&q_empty[qb], ((seg >> 1) - 1) & 1, s_abort)) {
           if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrQueriesA);
           ok = false;
@@ -418,39 +485,48 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           if (lane == 0) mbar_arrive(&e_full[cb]);
         }
       } while (ok && w.next(p));
+    if (ok && !announce(0) && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrQueriesA);
   } else if (warp >= kConvWarp0) {
+    fp8b::regs_give<64>();
     const int i = threadIdx.x - kConvWarp0 * 32;
     Ring v, o;
-    int n = 0;
+    int n = 0, nt;
     bool ok = any;
-    if (ok) do {
-        for (int j = 0; j < w.nt; ++j, ++n) {
-          if (!fp8b::mbar_wait_all(&v_full[v.i], v.phase, s_abort) || (n >= 2 && !fp8b::mbar_wait_all(&w_empty[o.i], o.phase ^ 1, s_abort))) {
-            if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrConvertA);
-            ok = false;
-            break;
-          }
-          const int64_t left = w.s.L - static_cast<int64_t>(w.s.tile0 + w.t + j) * kTok;
-          widen_values<D, 128>(smem + C::kOffCodes + v.i * C::kTileBytes, smem + C::kOffValues + o.i * C::kValueBytes, i,
-                               static_cast<int>(min(left, static_cast<int64_t>(kTok))));
-          fence_proxy_async_smem();  // the tensor core reads what these stores wrote
-          __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(&w_full[o.i]);
-            mbar_arrive(&v_empty[v.i]);
-          }
-          v.step(C::kValueSlots);
-          o.step(2);
+    for (int seg = 0; ok && segment(seg, nt); ++seg) {
+      const Seg& g = s_seg[seg % kSegs];
+      const int64_t left0 = g.L - static_cast<int64_t>(g.tile0) * kTok;  // tokens from the first tile on
+      __syncwarp();
+      done_with(seg);
+      for (int j = 0; j < nt; ++j, ++n) {
+        if (!fp8b::mbar_wait_all(&v_full[v.i], v.phase, s_abort) || (n >= 2 && !fp8b::mbar_wait_all(&w_empty[o.i], o.phase ^ 1, s_abort))) {
+          if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrConvertA);
+          ok = false;
+          break;
         }
-      } while (ok && w.next(p));
+        widen_values<D, 128>(smem + C::kOffCodes + v.i * C::kTileBytes, smem + C::kOffValues + o.i * C::kValueBytes, i,
+                             static_cast<int>(min(left0 - static_cast<int64_t>(j) * kTok, static_cast<int64_t>(kTok))));
+        fence_proxy_async_smem();  // the tensor core reads what these stores wrote
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&w_full[o.i]);
+          mbar_arrive(&v_empty[v.i]);
+        }
+        v.step(C::kValueSlots);
+        o.step(2);
+      }
+    }
   } else if (warp < kSoftmaxWarps) {
     // ---- softmax: thread = token of a tile.  Two groups of four warps take tiles in turn; with 64 rows (one tile per chunk)
     // they take half of its rows each.
+    fp8b::regs_take<120>();
     constexpr bool kHalves = R == 64;
-    constexpr int RR = kHalves ? 32 : R;
+    constexpr int RR = kHalves ? 32 : RS;
     const int group = warp >> 2, r0 = kHalves ? group * 32 : 0;
     const int tok = (warp & 3) * 32 + lane;
     const int me = kHalves ? threadIdx.x & 127 : threadIdx.x;  // among those threads
+    constexpr int S = RS < 8 ? RS : 8;        // rows at a time
+    constexpr int kMine = R == 16 ? 2 : 1;    // tiles of a chunk
+    const int j0 = kHalves ? 0 : group, dj = 2;
     const int red_i = kHalves ? warp & 3 : warp;
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const float4* table = reinterpret_cast<const float4*>(smem + C::kOffScales);
@@ -466,9 +542,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
       if (lane == 0) mbar_arrive(at);
       return fp8b::mbar_wait_all(at, met++ & 1, s_abort);
     };
-    if (!failed) do {
-        const int rows = min(max(w.s.n * p.G - r0, 0), RR);
-        const int4* info = reinterpret_cast<const int4*>(smem + C::kOffRows) + (seg & 1) * R + r0;
+    int nt_seg;
+    for (; !failed && segment(seg, nt_seg); ++seg) {
+        const Seg& g = s_seg[seg % kSegs];
+        const int rows = min(max(g.n * p.G - r0, 0), RR), tile0 = g.tile0;
+        const float4* info = reinterpret_cast<const float4*>(smem + C::kOffRows) + (seg & 1) * R + r0;
         if (!fp8b::mbar_wait_all(&q_full[seg & 1], (seg >> 1) & 1, s_abort)) {
           failed = true;
           break;
@@ -477,54 +555,59 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
 #pragma unroll
         for (int r = 0; r < RR; ++r) l[r] = 0.0f;
         float m_run = -INFINITY;  // of row r0 + me
-        const int64_t pos0 = static_cast<int64_t>(w.s.L) - w.s.n;
-        for (int t = 0; t < w.nt; t += kTiles, ++chunk) {
-          const int nt = min(kTiles, w.nt - t), cb = chunk & 1;
+        const int seen_to = p.causal ? g.L - g.n : g.L - 1, seen_from = p.window > 0 ? g.L - p.window : 0;
+        __syncwarp();
+        done_with(seg);
+        for (int t = 0; t < nt_seg; t += kTiles, ++chunk) {
+          const int nt = min(kTiles, nt_seg - t), cb = chunk & 1;
           const uint32_t parity = (chunk >> 1) & 1;
+          float x[kMine][RR];
+#pragma unroll
+          for (int k = 0; k < kMine; ++k)
+#pragma unroll
+            for (int r = 0; r < RR; ++r) x[k][r] = -INFINITY;
           if (!fp8b::mbar_wait_all(&s_full[cb], parity, s_abort) || !fp8b::mbar_wait_all(&e_full[cb], parity, s_abort)) {
             failed = true;
             break;
           }
           tc_fence_after_sync();
-          // score of rows r .. r + 7 for this thread's token of tile j, plus the values' scale: f (a + b) keys' scale + log2(values' scale)
-          auto scores = [&](int j, int r, float* x) {
+          // scores of this thread's token of its tiles, x[k][r] for the k-th, plus the values' scale:
+          // (a + b) (row's factor) (keys' scale) + log2(values' scale)
+          float inv[kMine];
+#pragma unroll
+          for (int k = 0; k < kMine; ++k) {
+            const int j = j0 + k * dj;
+            if (j >= nt) break;
             const float4 e = table[(cb * kTiles + j) * 8 + (tok >> 4)];
-            const int64_t tile = static_cast<int64_t>(w.s.tile0 + w.t + t + j) * kTok;
-            const int64_t at = tile + tok;
+            inv[k] = e.z;
+            const int tile = (tile0 + t + j) * kTok;
+            const uint32_t from = tmem + lane_base + cb * 128 + j * 2 * R + r0;
+#pragma unroll
+            for (int r = 0; r < RR; r += S) {
+              float y[S];
+              load_scores<S>(from + r, x[k] + r);
+              load_scores<S>(from + R + r, y);
+              tmem_ld_wait_regs<S>(x[k] + r);
+              tmem_ld_wait_regs<S>(y);
+#pragma unroll
+              for (int i = 0; i < S; ++i) x[k][r + i] = fmaf(x[k][r + i] + y[i], info[r + i].x * e.x, e.y);
+            }
             // all of the tile is seen by all rows (the first row sees the fewest behind, the last the fewest before)
-            const bool all = tile + kTok <= (p.causal ? pos0 + 1 : w.s.L) && (p.window == 0 || tile >= w.s.L - p.window);
-            float y[8];
-            const uint32_t from = tmem + lane_base + cb * 128 + j * 2 * R + r0 + r;
-            tmem_ld8(from, x);
-            tmem_ld8(from + R, y);
-            tmem_ld_wait_regs<8>(x);
-            tmem_ld_wait_regs<8>(y);
+            if (!(tile + (kTok - 1) <= seen_to && tile >= seen_from)) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int4 ri = info[r + i];
-              x[i] = fmaf(x[i] + y[i], __int_as_float(ri.x) * e.x, e.y);
-              if (!all && !(at >= ri.y && at < ri.z)) x[i] = -INFINITY;
-            }
-          };
-          const int j0 = kHalves ? 0 : group, dj = kHalves ? 1 : 2;
-#pragma unroll
-          for (int r = 0; r < RR; r += 8)
-            if (r < rows) {
-              float mx[8];
-#pragma unroll
-              for (int i = 0; i < 8; ++i) mx[i] = -INFINITY;
-              for (int j = j0; j < nt; j += dj) {
-                float x[8];
-                scores(j, r, x);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) mx[i] = fmaxf(mx[i], x[i]);
-              }
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                mx[i] = warp_max(mx[i]);
-                if (lane == 0) s_red[(r0 + r + i) * 8 + red_i] = mx[i];
+              for (int r = 0; r < RR; ++r) {
+                const float4 ri = info[r];
+                if (tile + tok < __float_as_int(ri.y) || tile + tok >= __float_as_int(ri.z)) x[k][r] = -INFINITY;
               }
             }
+          }
+#pragma unroll
+          for (int r = 0; r < RR; ++r) {
+            float v = x[0][r];
+            if (kMine > 1) v = fmaxf(v, x[kMine - 1][r]);
+            v = warp_max(v);
+            if (lane == 0) s_red[(r0 + r) * 8 + red_i] = v;
+          }
           // the chunk two before is through the epilogue: its factors, and its probabilities, make room
           if (chunk >= 2 && !fp8b::mbar_wait_all(&o_empty[cb], ((chunk >> 1) - 1) & 1, s_abort)) failed = true;
           if (!meet_others()) failed = true;
@@ -544,28 +627,24 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           if (!meet_others()) failed = true;
           if (failed) break;
 #pragma unroll
-          for (int r = 0; r < RR; ++r)
-            if (r < rows) l[r] *= s_max[2 * R + cb * R + r0 + r];
-          for (int j = j0; j < nt; j += dj) {
-            const float inv = table[(cb * kTiles + j) * 8 + (tok >> 4)].z;
+          for (int r = 0; r < RR; ++r) l[r] *= s_max[2 * R + cb * R + r0 + r];
+#pragma unroll
+          for (int k = 0; k < kMine; ++k) {
+            const int j = j0 + k * dj;
+            if (j >= nt) break;
             // the operand's rows: 64 tokens (128 bytes) each, the next 64 tokens R rows further
             uint8_t* to = smem + C::kOffProbs + (cb * kTiles + j) * C::kProbBytes + (tok >> 6) * (R * 128) + (tok & 7) * 2;
             const int piece = (tok & 63) >> 3;
 #pragma unroll
-            for (int r = 0; r < RR; r += 8)
-              if (r < rows) {
-                float x[8];
-                scores(j, r, x);
-#pragma unroll
-                for (int i = 0; i < 8; i += 2) {
-                  const float a = fp8b::sfu_ex2(x[i] + s_max[cb * R + r0 + r + i]), b = fp8b::sfu_ex2(x[i + 1] + s_max[cb * R + r0 + r + i + 1]);
-                  l[r + i] = fmaf(a, inv, l[r + i]);
-                  l[r + i + 1] = fmaf(b, inv, l[r + i + 1]);
-                  const uint32_t h = pack_f16(a, b);
-                  *reinterpret_cast<uint16_t*>(to + (r0 + r + i) * 128 + ((piece ^ i) << 4)) = static_cast<uint16_t>(h);
-                  *reinterpret_cast<uint16_t*>(to + (r0 + r + i + 1) * 128 + ((piece ^ (i + 1)) << 4)) = static_cast<uint16_t>(h >> 16);
-                }
-              }
+            for (int r = 0; r < RR; r += 2) {
+              const float2 m = *reinterpret_cast<const float2*>(s_max + cb * R + r0 + r);
+              const float a = fp8b::sfu_ex2(x[k][r] + m.x), b = fp8b::sfu_ex2(x[k][r + 1] + m.y);
+              l[r] = fmaf(a, inv[k], l[r]);
+              l[r + 1] = fmaf(b, inv[k], l[r + 1]);
+              const uint32_t h = pack_f16(a, b);
+              *reinterpret_cast<uint16_t*>(to + (r0 + r) * 128 + ((piece ^ (r & 7)) << 4)) = static_cast<uint16_t>(h);
+              *reinterpret_cast<uint16_t*>(to + (r0 + r + 1) * 128 + ((piece ^ ((r + 1) & 7)) << 4)) = static_cast<uint16_t>(h >> 16);
+            }
           }
           fence_proxy_async_smem();
           tc_fence_before_sync();
@@ -582,21 +661,19 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           break;
         }
 #pragma unroll
-        for (int r = 0; r < RR; ++r)
-          if (r < rows) {
-            float v = l[r];
+        for (int r = 0; r < RR; ++r) {
+          float v = l[r];
 #pragma unroll
-            for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-            if (lane == 0) s_sum[(r0 + r) * 8 + red_i] = v;
-          }
+          for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+          if (lane == 0) s_sum[(r0 + r) * 8 + red_i] = v;
+        }
         if (me < rows) s_sum[R * 8 + r0 + me] = m_run;
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(l_full);
           mbar_arrive(&q_empty[seg & 1]);
         }
-        ++seg;
-      } while (w.next(p));
+    }
     if (failed && any && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrSoftmaxA);
   } else {
     // ---- epilogue: thread = feature
@@ -604,16 +681,21 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const float* s_max = reinterpret_cast<const float*>(smem + C::kOffMax);
     const float* s_sum = reinterpret_cast<const float*>(smem + C::kOffSum);
+    constexpr int S = RS < 8 ? RS : 8;
     const int64_t total = s_scan[31], ctas = min(static_cast<int64_t>(gridDim.x), total);
     bool failed = !any;
     int chunk = 0, seg = 0;
     int64_t unit = any ? total * blockIdx.x / ctas : 0;
-    if (!failed) do {
-        const int rows = w.s.n * p.G;
-        float o[R];
+    int nt_seg;
+    for (; !failed && segment(seg, nt_seg); ++seg) {
+        const Seg& g = s_seg[seg % kSegs];
+        const int rows = g.n * p.G, first = g.first, h = g.h, b = g.b, flags = g.flags;
+        __syncwarp();
+        done_with(seg);
+        float o[RS];
 #pragma unroll
-        for (int r = 0; r < R; ++r) o[r] = 0.0f;
-        for (int t = 0; t < w.nt; t += kTiles, ++chunk) {
+        for (int r = 0; r < RS; ++r) o[r] = 0.0f;
+        for (int t = 0; t < nt_seg; t += kTiles, ++chunk) {
           const int cb = chunk & 1;
           const uint32_t parity = (chunk >> 1) & 1;
           if (!fp8b::mbar_wait_all(&p_full[cb], parity, s_abort) || !fp8b::mbar_wait_all(&o_full[cb], parity, s_abort)) {
@@ -622,14 +704,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           }
           tc_fence_after_sync();
 #pragma unroll
-          for (int r = 0; r < R; r += 8)
-            if (r < rows) {
-              float x[8];
-              tmem_ld8(tmem + lane_base + 256 + cb * R + r, x);
-              tmem_ld_wait_regs<8>(x);
+          for (int r = 0; r < RS; r += S) {
+            float x[S];
+            load_scores<S>(tmem + lane_base + 256 + cb * R + r, x);
+            tmem_ld_wait_regs<S>(x);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) o[r + i] = fmaf(o[r + i], s_max[2 * R + cb * R + r + i], x[i]);
-            }
+            for (int i = 0; i < S; ++i) o[r + i] = fmaf(o[r + i], s_max[2 * R + cb * R + r + i], x[i]);
+          }
           tc_fence_before_sync();
           __syncwarp();
           if (lane == 0) mbar_arrive(&o_empty[cb]);
@@ -638,10 +719,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           failed = true;
           break;
         }
-        const bool whole = w.whole();
-        float* part = p.partial + (static_cast<int64_t>(blockIdx.x) * 2 + (w.t == 0 ? 1 : 0)) * (R * (D + 2));
+        const bool whole = flags == 3;
+        float* part = p.partial + (static_cast<int64_t>(blockIdx.x) * 2 + (flags & 1)) * (R * (D + 2));
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int r = 0; r < RS; ++r)
           if (r < rows) {
             float sum = 0.0f;
 #pragma unroll
@@ -654,31 +735,30 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
                 part[R * D + R + r] = m;
               }
             } else {
-              const int64_t row = w.s.first + r / p.G;
-              const int hq = w.h * p.G + r % p.G;
+              const int64_t row = first + r / p.G;
+              const int hq = h * p.G + r % p.G;
               const float v = sum == 0.0f ? 0.0f : o[r] / sum;
               if (d < D) {
                 const int64_t at = row * p.ldo + static_cast<int64_t>(hq) * D + d;
-                if (F32)
+                if (p.f32)
                   static_cast<float*>(p.out)[at] = v;
                 else
                   static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
               }
-              if (p.lse && d == 0) p.lse[row * (static_cast<int64_t>(p.G) * p.c.H) + hq] = sum == 0.0f ? -INFINITY : (log2f(sum) + m + 8.0f - kShift) * (1.0f / kLog2e);
+              if (p.lse && d == 0) p.lse[row * (static_cast<int64_t>(p.G) * p.c.H) + hq] = sum == 0.0f ? -INFINITY : (log2f(sum) + m - kShift) * (1.0f / kLog2e);
             }
           }
         __syncwarp();
         if (lane == 0) mbar_arrive(l_empty);
-        if (w.t == 0 && threadIdx.x == kEpiWarp0 * 32) {
+        if ((flags & 1) && threadIdx.x == kEpiWarp0 * 32) {
           // the CTAs that share this sequence and head: to the one whose range holds its last tile
-          const int64_t last = unit + w.s.tiles - 1;
+          const int64_t last = whole ? 0 : unit + seq_of(p, b).tiles - 1;
           int64_t cta = whole ? blockIdx.x : last * ctas / total;
           while (!whole && total * (cta + 1) / ctas <= last) ++cta;
-          p.pieces[static_cast<int64_t>(w.b) * p.c.H + w.h] = make_int2(blockIdx.x, static_cast<int>(cta - blockIdx.x) + 1);
+          p.pieces[static_cast<int64_t>(b) * p.c.H + h] = make_int2(blockIdx.x, static_cast<int>(cta - blockIdx.x) + 1);
         }
-        unit += w.nt;
-        ++seg;
-      } while (w.next(p));
+        unit += nt_seg;
+    }
     if (failed && any && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrEpilogueA);
   }
 
@@ -691,7 +771,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
 }
 
 // Results of sequences and heads that several CTAs share: a block per sequence and head, a thread per feature and every fourth row.
-template <int D, int R, bool F32>
+template <int D, int R>
 __global__ void __launch_bounds__(4 * D) attention_join_kernel(const P p) {
   __shared__ float s_w[kMaxCtas];
   __shared__ float s_l;
@@ -726,7 +806,7 @@ __global__ void __launch_bounds__(4 * D) attention_join_kernel(const P p) {
         s_l = l;
         const int64_t row = s.first + r / p.G;
         const int hq = h * p.G + r % p.G;
-        if (p.lse) p.lse[row * (static_cast<int64_t>(p.G) * p.c.H) + hq] = l == 0.0f ? -INFINITY : (log2f(l) + m + 8.0f - kShift) * (1.0f / kLog2e);
+        if (p.lse) p.lse[row * (static_cast<int64_t>(p.G) * p.c.H) + hq] = l == 0.0f ? -INFINITY : (log2f(l) + m - kShift) * (1.0f / kLog2e);
       }
     }
     __syncthreads();
@@ -741,7 +821,7 @@ __global__ void __launch_bounds__(4 * D) attention_join_kernel(const P p) {
       o = s_o[0][d] + s_o[1][d] + s_o[2][d] + s_o[3][d];
       const float v = s_l == 0.0f ? 0.0f : o / s_l;
       const int64_t at = (s.first + r / p.G) * p.ldo + (static_cast<int64_t>(h) * p.G + r % p.G) * D + d;
-      if (F32)
+      if (p.f32)
         static_cast<float*>(p.out)[at] = v;
       else
         static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
@@ -749,28 +829,26 @@ __global__ void __launch_bounds__(4 * D) attention_join_kernel(const P p) {
   }
 }
 
-template <int D, int R, bool F32>
+template <int D, int R, int RS>
 int launch_cfg(const CUtensorMap& tm, const P& p, int grid, int max_rows, cudaStream_t st) {
   using C = Cfg<D, R>;
   static DeviceOnce once;
-  if (!allow_shared_memory(once, attention_few_kernel<D, R, F32>, C::kSmemBytes)) return ZQ_ERR_CUDA;
-  cudaError_t e = launch_chained(attention_few_kernel<D, R, F32>, dim3(grid), dim3(kThreads), C::kSmemBytes, st, false, tm, p);
+  if (!allow_shared_memory(once, attention_few_kernel<D, R, RS>, C::kSmemBytes)) return ZQ_ERR_CUDA;
+  cudaError_t e = launch_chained(attention_few_kernel<D, R, RS>, dim3(grid), dim3(kThreads), C::kSmemBytes, st, false, tm, p);
   count_launch();
   if (e != cudaSuccess) return ZQ_ERR_CUDA;
   const int64_t blocks = static_cast<int64_t>(p.c.B) * p.c.H;
-  e = launch_chained(attention_join_kernel<D, R, F32>, dim3(static_cast<unsigned>(blocks), max_rows), dim3(4 * D), 0, st, false, p);
+  e = launch_chained(attention_join_kernel<D, R>, dim3(static_cast<unsigned>(blocks), max_rows), dim3(4 * D), 0, st, false, p);
   count_launch();
   return e == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
 }
-template <int D, int R>
-int launch_type(const CUtensorMap& tm, const P& p, int grid, int max_rows, int dt, cudaStream_t st) {
-  return dt == ZQ_OUT_F32 ? launch_cfg<D, R, true>(tm, p, grid, max_rows, st) : launch_cfg<D, R, false>(tm, p, grid, max_rows, st);
-}
 template <int D>
-int launch_rows(const CUtensorMap& tm, const P& p, int grid, int max_rows, int dt, cudaStream_t st) {
-  if (max_rows <= 16) return launch_type<D, 16>(tm, p, grid, max_rows, dt, st);
-  if (max_rows <= 32) return launch_type<D, 32>(tm, p, grid, max_rows, dt, st);
-  return launch_type<D, 64>(tm, p, grid, max_rows, dt, st);
+int launch_rows(const CUtensorMap& tm, const P& p, int grid, int max_rows, cudaStream_t st) {
+  if (max_rows <= 4) return launch_cfg<D, 16, 4>(tm, p, grid, max_rows, st);
+  if (max_rows <= 8) return launch_cfg<D, 16, 8>(tm, p, grid, max_rows, st);
+  if (max_rows <= 16) return launch_cfg<D, 16, 16>(tm, p, grid, max_rows, st);
+  if (max_rows <= 32) return launch_cfg<D, 32, 32>(tm, p, grid, max_rows, st);
+  return launch_cfg<D, 64, 64>(tm, p, grid, max_rows, st);
 }
 
 }  // namespace
@@ -788,7 +866,7 @@ int launch_attention_few(const AttnArgs& a, int max_rows, cudaStream_t st) {
   p.q = static_cast<const __nv_bfloat16*>(a.q), p.ldq = a.ldq, p.G = a.Hq / a.c.H;
   p.scale_log2 = a.sm_scale * kLog2e;
   p.causal = a.causal, p.window = a.window;
-  p.out = a.out, p.ldo = a.ldo, p.lse = a.lse;
+  p.out = a.out, p.f32 = a.dt == ZQ_OUT_F32, p.ldo = a.ldo, p.lse = a.lse;
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   p.status = reinterpret_cast<int*>(ws);
   p.partial = reinterpret_cast<float*>(ws + kWsHeadBytes);
@@ -796,7 +874,7 @@ int launch_attention_few(const AttnArgs& a, int max_rows, cudaStream_t st) {
   CUtensorMap tm;
   if (!make_page_map(&tm, a.c)) return ZQ_ERR_CUDA;
   const int sms = sm_count(), grid = sms < kMaxCtas ? sms : kMaxCtas;
-  return a.c.D == 128 ? launch_rows<128>(tm, p, grid, max_rows, a.dt, st) : launch_rows<64>(tm, p, grid, max_rows, a.dt, st);
+  return a.c.D == 128 ? launch_rows<128>(tm, p, grid, max_rows, st) : launch_rows<64>(tm, p, grid, max_rows, st);
 }
 
 }  // namespace kv
