@@ -16,6 +16,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kShift = 8.0f;
 
 int launch_attention_few(const AttnArgs& a, int max_rows, cudaStream_t st);
+int launch_attention_rows(const AttnArgs& a, cudaStream_t st);
+size_t rows_workspace_bytes(int64_t D);
 size_t few_workspace_bytes(int64_t B, int64_t H, int64_t D);
 
 #ifdef __CUDACC__
@@ -63,9 +65,11 @@ __device__ __forceinline__ void umma_f16(uint32_t d_tmem, uint64_t a_desc, uint6
 // A converter thread's share of a tile of values: codes [128][D] (rows as they lie in memory) -> FP16 in the operand's layout, each
 // code's own value.  Tokens from `valid` on become zeros, whatever the page holds there.  All of the share's codes are loaded
 // before the first store (the compiler cannot tell their addresses apart), kAtOnce pieces of 16 at a time.
+// A NaN becomes the largest FP16 number: what nobody sees (a page that was not copied, say) must not turn into NaN by a product
+// with zero.
 __device__ __forceinline__ uint32_t widen2(uint32_t codes) {  // the lower two
   uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(codes)));
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n\tmin.f16x2 %0, %0, %2;" : "=&r"(h) : "h"(static_cast<uint16_t>(codes)), "r"(0x7BFF7BFFu));
   return h;
 }
 template <int D, int THREADS>
@@ -144,7 +148,7 @@ __device__ __forceinline__ float4 scale_entry(const Cache& c, int b, int h, int 
   if (vs < 5.42101086242752217e-20f) vs = 5.42101086242752217e-20f;  // 2^-64: what was never written has 0
   e.x = ks;
   e.y = log2f(vs);
-  e.z = 1.0f / vs;
+  e.z = isnan(vs) ? 1.0f : 1.0f / vs;  // (a block that stands for NaN: the power is NaN where it is seen)
   return e;
 }
 

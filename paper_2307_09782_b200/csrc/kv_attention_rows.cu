@@ -1,0 +1,805 @@
+// Attention over the 8-bit cache where a sequence and cache head have many rows (new tokens x query heads of the head, more than
+// 64): prompts.  Bound by arithmetic: the tensor core's 4 D operations and one power of two per row and visible token.
+//
+//   S [128 rows, 128 tokens] = q K^T       E4M3 x E4M3; q is a sum of two E4M3 numbers, so two products: the keys' codes go to
+//                                          the tensor core as they are, at the price of one FP16 product
+//   O [128 rows, D] += P V                 FP16 x FP16; P from tensor memory, over the scores it was made of; the values'
+//                                          codes are widened in shared memory, once for 256 rows
+// Rows are the tensor core's lanes and a softmax thread's own: maxima and sums need no other thread.  A CTA works on two tiles of
+// 128 rows in turn, so that one's products run beside the other's softmax.  The running maximum only moves when a score exceeds
+// it by more than kSlack (in powers of two; FP16 has the room): the accumulator is then multiplied by the row's own warp.
+//
+// Items (sequence, 256 rows, head) go to the CTAs in rounds, a sequence's last rows, which see most, first.  Where there are few
+// items, each is split over several CTAs along the tokens, and attention_join_rows_kernel adds up their results in order.
+//
+// Warp roles: 0..3, 4..7 softmax and epilogue of the two tiles (thread = row), 8..11 queries and values (conversion), 12 keys'
+// copies, 13 values' copies, 14 MMAs, 15 the walk over the items and the block scales.
+#include "kv_attention.cuh"
+
+namespace zq {
+namespace kv {
+namespace {
+
+constexpr int kConvWarp0 = 8, kKeyWarp = 12, kValueWarp = 13, kMmaWarp = 14, kWalkWarp = 15;
+constexpr int kThreads = 512;
+constexpr int kRows = 256;       // of an item
+constexpr int kSegs = 4, kScaleSlots = 4;
+constexpr float kSlack = 7.0f;   // 2^(kShift + kSlack) = 32768 fits FP16
+enum { kErrKeysR = 61, kErrValuesR = 62, kErrMmaR = 63, kErrWalkR = 64, kErrSoftmaxR = 65, kErrConvertR = 66, kErrAlignR = 67 };
+// Registers per thread behind the set-up: softmax 184 (two warpgroups), converters and the others 72;
+// 2 x 184 + 2 x 72 = 512, the four warpgroups' 4 x 128 at launch.
+
+struct P {
+  Cache c;
+  const __nv_bfloat16* q;
+  int64_t ldq;
+  int G;
+  float scale_log2;
+  int causal, window;
+  void* out;
+  int64_t ldo;
+  int f32;
+  float* lse;
+  float* partial;  // [CTAs][256 (D + 2)]
+  int* status;
+};
+
+template <int D>
+struct Cfg {
+  static constexpr int kTileBytes = kTok * D;
+  static constexpr int kValueBytes = kTok * D * 2;
+  static constexpr int kKeySlots = 3, kValueSlots = 2;
+  static constexpr int kOffQueries = 0;                                     // [2 tiles][2 terms][128 rows of D]
+  static constexpr int kOffValues = kOffQueries + 4 * kTileBytes;           // [2] widened
+  static constexpr int kOffKeys = kOffValues + 2 * kValueBytes;
+  static constexpr int kOffCodes = kOffKeys + kKeySlots * kTileBytes;
+  static constexpr int kOffScales = kOffCodes + kValueSlots * kTileBytes;   // [kScaleSlots][8] float4
+  static constexpr int kOffRows = kOffScales + kScaleSlots * 8 * 16;        // [256] rows' factors
+  static constexpr int kOffSegs = kOffRows + kRows * 4;
+  static constexpr int kOffBars = kOffSegs + kSegs * 48;
+  static constexpr int kOffScan = kOffBars + 64 * 8;                        // [16 + 4] 64-bit words, then two of 32
+  static constexpr int kSmemBytes = kOffScan + 20 * 8 + 16;
+  static_assert(kSmemBytes <= 227 * 1024, "shared memory");
+};
+
+struct Seq {
+  int first, n, L;
+  int blocks;  // of 256 rows, 0 where the kernel for few rows takes the sequence
+};
+__device__ __forceinline__ Seq seq_of(const P& p, int b) {
+  Seq s;
+  rows_of(p.c, b, s.first, s.n);
+  s.L = max(load_chained(p.c.lens + b), 0);
+  const int64_t rows = static_cast<int64_t>(s.n) * p.G;
+  s.blocks = rows > kFewRows ? static_cast<int>((rows + kRows - 1) / kRows) : 0;
+  return s;
+}
+// CTAs that share an item.
+__device__ __forceinline__ int splits_of(int64_t items, int ctas) {
+  return items > 0 && 2 * items <= ctas ? static_cast<int>(ctas / items) : 1;
+}
+
+struct alignas(16) Seg {
+  int nt;            // tiles of tokens; 0: no more items; -1: none of this item are this CTA's
+  int tile0;         // the first
+  int L, n;
+  int b, h, first;
+  int row0, rows;    // first of the item's rows among the sequence's, and their number
+  int part;          // place among the partial results, or -1
+  int pad[2];
+};
+static_assert(sizeof(Seg) == 48, "Seg");
+
+struct Ring {
+  int i = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void step(int n) {
+    if (++i == n) {
+      i = 0;
+      phase ^= 1;
+    }
+  }
+};
+
+__device__ __forceinline__ void umma_f16_tmem_a(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// Results of a row: features f .. f + 15.
+__device__ __forceinline__ void store16(const P& p, int64_t at, const float* v) {
+  if (p.f32) {
+    float4* o = reinterpret_cast<float4*>(static_cast<float*>(p.out) + at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+  } else {
+    uint4* o = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + at);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      o[i] = make_uint4(fp8b::pack_bf16(v[8 * i], v[8 * i + 1]), fp8b::pack_bf16(v[8 * i + 2], v[8 * i + 3]),
+                        fp8b::pack_bf16(v[8 * i + 4], v[8 * i + 5]), fp8b::pack_bf16(v[8 * i + 6], v[8 * i + 7]));
+  }
+}
+
+// A softmax thread's tile of scores x (its row, 128 tokens) -> probabilities in tensor memory.  `lo`, `hi`: tokens of the tile that
+// the row sees (looked at with MASK).  May move the row's reference m and multiplies what is in the accumulator and l by the factor.
+template <int D, bool MASK, typename Wait>
+__device__ __forceinline__ bool softmax_tile(float* x, const float4* scales, float c, int lo, int hi, float& m, float& l, uint32_t probs,
+                                             uint32_t acc, bool first, Wait accumulated) {
+  float top = -INFINITY;
+#pragma unroll
+  for (int g = 0; g < 8; ++g) {
+    const float4 e = scales[g];
+    float v = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int at = g * 16 + i;
+      if (MASK && (at < lo || at >= hi)) x[at] = -INFINITY;
+      v = fmaxf(v, x[at]);
+    }
+    top = fmaxf(top, fmaf(v, e.x * c, e.y));  // (0 x infinity where all is masked: NaN, which fmaxf drops)
+  }
+  // a row that has seen nothing yet takes the first maximum as it is: its sums are zero
+  const bool move = top > m + kSlack || (m == -INFINITY && top > m);
+  if (__any_sync(0xFFFFFFFFu, move)) {
+    const float f = move && m > -INFINITY ? fp8b::sfu_ex2(m - top) : 1.0f;
+    if (move) m = top;
+    l *= f;
+    if (!first && __any_sync(0xFFFFFFFFu, f != 1.0f)) {
+      if (!accumulated()) return false;
+      tc_fence_after_sync();
+#pragma unroll 1
+      for (int d = 0; d < D; d += 16) {
+        float o[16];
+        tmem_ld16(acc + d, o);
+        tmem_ld_wait_regs<16>(o);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[i] *= f;
+        tmem_st16(acc + d, reinterpret_cast<const uint32_t*>(o));
+      }
+      tmem_st_wait();
+    }
+  }
+  const float base = kShift - (m == -INFINITY ? 0.0f : m);
+#pragma unroll
+  for (int g = 0; g < 8; g += 2) {
+    uint32_t h[16];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float4 e = scales[g + k];
+      const uint64_t f2 = fp8b::twice(e.x * c), a2 = fp8b::twice(e.y + base);
+      uint64_t sum = 0ull;
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const int at = (g + k) * 16 + i;
+        float a, b;
+        unpack2(fma2(pack2(x[at], x[at + 1]), f2, a2), a, b);
+        a = fp8b::sfu_ex2(a);
+        b = fp8b::sfu_ex2(b);
+        if (MASK) {
+          if (at < lo || at >= hi) a = 0.0f;
+          if (at + 1 < lo || at + 1 >= hi) b = 0.0f;
+        }
+        sum = add2(sum, pack2(a, b));
+        h[k * 8 + i / 2] = pack_f16(a, b);
+      }
+      float s0, s1;
+      unpack2(sum, s0, s1);
+      l = fmaf(s0 + s1, e.z, l);
+    }
+    tmem_st16(probs + g * 8, h);
+  }
+  tmem_st_wait();
+  return true;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __grid_constant__ CUtensorMap tm, const P p) {
+  using C = Cfg<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint64_t* bar = reinterpret_cast<uint64_t*>(smem + C::kOffBars);
+  uint64_t* k_full = bar;                          // [key slots] a tile's keys have landed                 (MMA)
+  uint64_t* k_empty = k_full + C::kKeySlots;       // their products are done                               (keys' copies)
+  uint64_t* v_full = k_empty + C::kKeySlots;       // [value slots] a tile's values have landed             (converters)
+  uint64_t* v_empty = v_full + C::kValueSlots;     // they are widened                                      (values' copies)
+  uint64_t* w_full = v_empty + C::kValueSlots;     // [2] widened values                                    (MMA)
+  uint64_t* w_empty = w_full + 2;                  // [2] their products are done                           (converters)
+  uint64_t* s_full = w_empty + 2;                  // [2 row tiles] scores                                  (softmax)
+  uint64_t* p_full = s_full + 2;                   // [2] probabilities, the accumulator up to date         (MMA)
+  uint64_t* pv_done = p_full + 2;                  // [2] they have been multiplied                         (MMA, softmax)
+  uint64_t* q_full = pv_done + 2;                  // an item's queries                                     (MMA, softmax)
+  uint64_t* q_empty = q_full + 1;                  // nobody needs them any more                            (converters)
+  uint64_t* e_full = q_empty + 1;                  // [scale slots] a tile's block scales                   (softmax)
+  uint64_t* e_empty = e_full + kScaleSlots;        // they have been used                                   (walk)
+  uint64_t* g_full = e_empty + kScaleSlots;        // [kSegs] an item is announced                          (all)
+  uint64_t* g_empty = g_full + kSegs;              // [kSegs] everybody is through with it                  (walk)
+  uint64_t* drain = g_empty + kSegs;
+  int64_t* s_scan = reinterpret_cast<int64_t*>(smem + C::kOffScan);
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_scan + 20);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
+  Seg* s_seg = reinterpret_cast<Seg*>(smem + C::kOffSegs);
+  float* s_rows = reinterpret_cast<float*>(smem + C::kOffRows);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::kKeySlots; ++i) {
+      mbar_init(&k_full[i], 1);
+      mbar_init(&k_empty[i], 1);
+    }
+    for (int i = 0; i < C::kValueSlots; ++i) {
+      mbar_init(&v_full[i], 1);
+      mbar_init(&v_empty[i], 4);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&w_full[i], 4);
+      mbar_init(&w_empty[i], 1);
+      mbar_init(&s_full[i], 1);
+      mbar_init(&p_full[i], 4);
+      mbar_init(&pv_done[i], 1);
+    }
+    mbar_init(q_full, 4);
+    mbar_init(q_empty, 1 + 8);
+    for (int i = 0; i < kScaleSlots; ++i) {
+      mbar_init(&e_full[i], 1);
+      mbar_init(&e_empty[i], 8);
+    }
+    for (int i = 0; i < kSegs; ++i) {
+      mbar_init(&g_full[i], 1);
+      mbar_init(&g_empty[i], kThreads / 32 - 1);
+    }
+    mbar_init(drain, 1);
+    *s_abort = 0;
+    fence_mbar_init();
+    if ((smem_u32(smem) & 1023u) != 0) fp8b::raise_error8(p.status, s_abort, kErrAlignR);
+    prefetch_tensormap(&tm);
+  }
+  if (warp == kMmaWarp) tmem_alloc(s_tmem, 512);
+  pdl_launch_dependents();
+  pdl_wait();
+  // ---- items before each thread's sequences, by a scan over the block; the thread that has this CTA's first one leaves it
+  {
+    const int per = (p.c.B + kThreads - 1) / kThreads;
+    const int b0 = min(static_cast<int>(threadIdx.x) * per, p.c.B), b1 = min(b0 + per, p.c.B);
+    int64_t mine = 0;
+    for (int b = b0; b < b1; ++b) mine += static_cast<int64_t>(seq_of(p, b).blocks) * p.c.H;
+    int64_t incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+      if (lane >= o) incl += x;
+    }
+    if (lane == 31) s_scan[warp] = incl;
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    int64_t before = 0, total = 0;
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) before += s_scan[w];
+      total += s_scan[w];
+    }
+    const int64_t begin = before + incl - mine;
+    const int splits = splits_of(total, gridDim.x);
+    const int64_t item = blockIdx.x / splits;
+    if (threadIdx.x == 0) {
+      s_scan[16] = total;
+      s_scan[17] = splits;
+    }
+    if (item < total && begin <= item && item < begin + mine) {
+      int64_t at = begin;
+      int b = b0;
+      for (;; ++b) {
+        const int64_t n = static_cast<int64_t>(seq_of(p, b).blocks) * p.c.H;
+        if (item < at + n) break;
+        at += n;
+      }
+      s_scan[18] = b;
+      s_scan[19] = at;
+    }
+  }
+  __syncthreads();
+  const uint32_t tmem = *s_tmem;
+  const int splits = static_cast<int>(s_scan[17]);
+  const bool any = *s_abort == 0 && blockIdx.x / splits < s_scan[16];
+  // The next item of a role: false behind the last one, and where something has failed.
+  auto segment = [&](int seg, int& nt) {
+    if (!fp8b::mbar_wait_all(&g_full[seg % kSegs], (seg / kSegs) & 1, s_abort)) return false;
+    nt = s_seg[seg % kSegs].nt;
+    return nt != 0;
+  };
+  auto done_with = [&](int seg) {  // a warp, converged
+    if (lane == 0) mbar_arrive(&g_empty[seg % kSegs]);
+  };
+
+  if (warp == kKeyWarp || warp == kValueWarp) {
+    // ---- copies: a lane per page of the tile
+    fp8b::regs_give<72>();
+    const bool keys = warp == kKeyWarp;
+    const int slots = keys ? C::kKeySlots : C::kValueSlots;
+    uint64_t *full = keys ? k_full : v_full, *empty = keys ? k_empty : v_empty;
+    uint8_t* to = smem + (keys ? C::kOffKeys : C::kOffCodes);
+    const int per = kTok / p.c.page, page_bytes = p.c.page * D;
+    Ring r;
+    int issued = 0, nt;
+    bool ok = any;
+    for (int seg = 0; ok && segment(seg, nt); ++seg) {
+      const Seg& g = s_seg[seg % kSegs];
+      const int t0 = g.tile0, h = g.h;
+      PageWalk pages;
+      pages.start(p.c, g.b, g.L, t0 * per, lane);
+      __syncwarp();
+      done_with(seg);
+      for (int j = 0; j < nt; ++j) {
+        const int page = pages.get(p.c, (t0 + j) * per, lane);
+        if (issued >= slots && !mbar_wait_warp(&empty[r.i], r.phase ^ 1, s_abort)) {
+          if (lane == 0) fp8b::raise_error8(p.status, s_abort, keys ? kErrKeysR : kErrValuesR);
+          ok = false;
+          break;
+        }
+        const bool has = lane < per && page >= 0;
+        const uint32_t n = __popc(__ballot_sync(0xFFFFFFFFu, has));
+        if (lane == 0) mbar_arrive_expect_tx(&full[r.i], n * page_bytes);
+        __syncwarp();
+        if (has) {
+          uint8_t* dst = to + r.i * C::kTileBytes + lane * page_bytes;
+          const int64_t block = block_at(p.c, page, keys ? 0 : 1, h);
+          if (keys)
+            tma_load_3d(dst, &tm, 0, 0, static_cast<int>(block), &full[r.i]);
+          else
+            bulk_load(dst, p.c.codes + block * page_bytes, page_bytes, &full[r.i]);
+        }
+        __syncwarp();
+        ++issued;
+        r.step(slots);
+      }
+    }
+    // never leave with copies still in flight
+    for (int i = max(0, issued - slots); i < issued; ++i) {
+      uint32_t spin = 0;
+      while (!mbar_try_wait(&full[i % slots], (i / slots) & 1) && ++spin < kSpinLimit) {
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    fp8b::regs_give<72>();
+    const bool issuer = elect_one();
+    const uint64_t kdesc = desc_rows<D>(smem_u32(smem + C::kOffKeys)), qdesc = desc_rows<D>(smem_u32(smem + C::kOffQueries));
+    const uint64_t vdesc = desc_values(smem_u32(smem + C::kOffValues));
+    const uint32_t sdesc_i = umma_idesc_e4m3(kTok), odesc_i = idesc_f16(D, false, true);
+    Ring k, v;
+    int done[2] = {0, 0};  // products with values begun, for each row tile
+    bool failed = false;
+    // scores of row tile q for the tile of keys in k; its columns hold the probabilities of the tile before until these are used
+    auto scores = [&](int q, bool last_q, bool last_tile) {
+      if (done[q] > 0 && !mbar_wait(&pv_done[q], (done[q] - 1) & 1, s_abort)) return false;
+      tc_fence_after_sync();
+      if (issuer) {
+        const uint64_t bd = kdesc + static_cast<uint64_t>((k.i * C::kTileBytes) >> 4);
+#pragma unroll
+        for (int term = 0; term < 2; ++term) {
+          const uint64_t ad = qdesc + static_cast<uint64_t>(((q * 2 + term) * C::kTileBytes) >> 4);
+#pragma unroll
+          for (int s = 0; s < D / 32; ++s) umma_f8(tmem + q * kTok, ad + s * 2, bd + s * 2, sdesc_i, (term > 0 || s > 0) ? 1u : 0u);
+        }
+        umma_commit(&s_full[q]);
+        if (last_q) {
+          umma_commit(&k_empty[k.i]);
+          if (last_tile) umma_commit(q_empty);
+        }
+      }
+      __syncwarp();
+      return true;
+    };
+    int nt;
+    for (int seg = 0; any && !failed && segment(seg, nt); ++seg) {
+      const int nq = s_seg[seg % kSegs].rows > kTok ? 2 : 1;
+      __syncwarp();
+      done_with(seg);
+      if (nt < 0) continue;
+      if (!mbar_wait(q_full, seg & 1, s_abort) || !mbar_wait(&k_full[k.i], k.phase, s_abort)) {
+        failed = true;
+        break;
+      }
+      for (int q = 0; q < nq && !failed; ++q) failed = !scores(q, q + 1 == nq, nt == 1);
+      k.step(C::kKeySlots);
+      for (int j = 0; j < nt && !failed; ++j) {
+        for (int q = 0; q < nq; ++q) {
+          if (!mbar_wait(&p_full[q], done[q] & 1, s_abort) || (q == 0 && !mbar_wait(&w_full[v.i], v.phase, s_abort))) {
+            failed = true;
+            break;
+          }
+          tc_fence_after_sync();
+          if (issuer) {
+            const uint64_t bd = vdesc + static_cast<uint64_t>((v.i * C::kValueBytes) >> 4);
+#pragma unroll
+            for (int s = 0; s < kTok / 16; ++s)
+              umma_f16_tmem_a(tmem + 256 + q * 128, tmem + q * kTok + s * 8, bd + s * (2048 >> 4), odesc_i, (j > 0 || s > 0) ? 1u : 0u);
+            umma_commit(&pv_done[q]);
+            if (q + 1 == nq) umma_commit(&w_empty[v.i]);
+          }
+          __syncwarp();
+          ++done[q];
+          if (j + 1 < nt) {
+            if (q == 0 && !mbar_wait(&k_full[k.i], k.phase, s_abort)) failed = true;
+            if (failed || !scores(q, q + 1 == nq, j + 2 == nt)) {
+              failed = true;
+              break;
+            }
+          }
+        }
+        v.step(2);
+        if (j + 1 < nt) k.step(C::kKeySlots);
+      }
+    }
+    if (failed && issuer) fp8b::raise_error8(p.status, s_abort, kErrMmaR);
+    // tensor memory is released only when every MMA has completed, also where another role has given up
+    if (issuer) umma_commit(drain);
+    uint32_t spin = 0;
+    while (!mbar_try_wait(drain, 0) && ++spin < kSpinLimit) {
+    }
+    __syncwarp();
+  } else if (warp == kWalkWarp) {
+    // ---- the items of this CTA, and the block scales of their tiles: a lane per 16 tokens, four tiles at a time
+    fp8b::regs_give<72>();
+    float4* table = reinterpret_cast<float4*>(smem + C::kOffScales);
+    const int64_t total = s_scan[16];
+    int64_t item = blockIdx.x / splits, at = s_scan[19];
+    const int split = blockIdx.x % splits;
+    int b = static_cast<int>(s_scan[18]), seg = 0, tiles = 0;
+    bool ok = any;
+    auto announce = [&](const Seg& g) {
+      if (seg >= kSegs && !mbar_wait_warp(&g_empty[seg % kSegs], (seg / kSegs - 1) & 1, s_abort)) return false;
+      if (lane == 0) {
+        s_seg[seg % kSegs] = g;
+        mbar_arrive(&g_full[seg % kSegs]);
+      }
+      __syncwarp();
+      ++seg;
+      return true;
+    };
+    if (any) {
+      Seq s = seq_of(p, b);
+      for (; ok && item < total; item += splits > 1 ? total : static_cast<int64_t>(gridDim.x)) {  // (an item that is split is a CTA's only one)
+        while (item >= at + static_cast<int64_t>(s.blocks) * p.c.H) {
+          at += static_cast<int64_t>(s.blocks) * p.c.H;
+          s = seq_of(p, ++b);
+        }
+        const int k = static_cast<int>(item - at);
+        Seg g{};
+        g.L = s.L, g.n = s.n, g.b = b, g.h = k % p.c.H, g.first = s.first;
+        const int block = s.blocks - 1 - k / p.c.H;
+        g.row0 = block * kRows;
+        g.rows = static_cast<int>(min(static_cast<int64_t>(s.n) * p.G - g.row0, static_cast<int64_t>(kRows)));
+        // tokens that some of the rows see
+        const int64_t p0 = static_cast<int64_t>(s.L) - s.n + g.row0 / p.G, p1 = static_cast<int64_t>(s.L) - s.n + (g.row0 + g.rows - 1) / p.G;
+        const int64_t lo = p.window > 0 ? max(p0 + 1 - p.window, static_cast<int64_t>(0)) : 0;
+        const int64_t hi = max(p.causal ? p1 + 1 : static_cast<int64_t>(s.L), static_cast<int64_t>(1));
+        const int t0 = static_cast<int>(lo / kTok), nt = max(static_cast<int>((hi + kTok - 1) / kTok) - t0, 1);
+        const int c0 = static_cast<int>(static_cast<int64_t>(nt) * split / splits), c1 = static_cast<int>(static_cast<int64_t>(nt) * (split + 1) / splits);
+        g.tile0 = t0 + c0;
+        g.nt = c1 > c0 ? c1 - c0 : -1;
+        g.part = splits > 1 ? blockIdx.x : -1;
+        if (!announce(g)) {
+          ok = false;
+          break;
+        }
+        for (int j0 = 0; j0 < g.nt && ok; j0 += 4) {
+          const int64_t token = (static_cast<int64_t>(g.tile0) + j0) * kTok + lane * 16;
+          const float4 e = scale_entry(p.c, b, g.h, static_cast<int>(min(token, static_cast<int64_t>(s.L))), s.L);
+          for (int j = 0; j < 4 && j0 + j < g.nt; ++j, ++tiles) {
+            const int slot = tiles % kScaleSlots;
+            if (tiles >= kScaleSlots && !mbar_wait_warp(&e_empty[slot], (tiles / kScaleSlots - 1) & 1, s_abort)) {
+              ok = false;
+              break;
+            }
+            if (lane >> 3 == j) table[slot * 8 + (lane & 7)] = e;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&e_full[slot]);
+          }
+        }
+      }
+      if (ok) ok = announce(Seg{});
+      if (!ok && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrWalkR);
+    }
+  } else if (warp >= kConvWarp0) {
+    fp8b::regs_give<72>();
+    const int i = threadIdx.x - kConvWarp0 * 32;
+    Ring v, o;
+    int n = 0, nt, items = 0;
+    bool ok = any;
+    for (int seg = 0; ok && segment(seg, nt); ++seg) {
+      const Seg& g = s_seg[seg % kSegs];
+      const int64_t left0 = g.L - static_cast<int64_t>(g.tile0) * kTok;  // tokens from the first tile on
+      const int first = g.first, h = g.h, row0 = g.row0, rows = g.rows;
+      __syncwarp();
+      done_with(seg);
+      if (nt < 0) continue;
+      // queries: a row per thread, of one tile and then the other
+      if (items > 0 && !fp8b::mbar_wait_all(q_empty, (items - 1) & 1, s_abort)) {
+        if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrConvertR);
+        break;
+      }
+      ++items;
+      for (int q = 0; q < 2 && q * kTok < rows; ++q) {
+        const int r = q * kTok + i;
+        const bool has = r < rows;
+        const uint4* src = reinterpret_cast<const uint4*>(p.q + (first + (row0 + r) / p.G) * p.ldq + (static_cast<int64_t>(h) * p.G + (row0 + r) % p.G) * D);
+        uint32_t a = 0u;
+#pragma unroll
+        for (int x0 = 0; x0 < D / 8; x0 += 8) {
+          uint4 x[8];
+#pragma unroll
+          for (int x1 = 0; x1 < 8; ++x1) x[x1] = has ? load_chained(src + x0 + x1) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+          for (int x1 = 0; x1 < 8; ++x1) a = max(a, absmax_bits8(x[x1]));
+        }
+        const RowScale s = row_scale(a);
+        uint8_t* to = smem + C::kOffQueries + q * 2 * C::kTileBytes;
+#pragma unroll
+        for (int x0 = 0; x0 < D / 8; x0 += 4) {
+          uint4 x[4];
+#pragma unroll
+          for (int x1 = 0; x1 < 4; ++x1) x[x1] = has ? load_chained(src + x0 + x1) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+          for (int x1 = 0; x1 < 4; x1 += 2) {
+            uint2 a0, a1, b0, b1;
+            split8(x[x1], s.up, a0, b0);
+            split8(x[x1 + 1], s.up, a1, b1);
+            const uint32_t at = row_piece<D>(i, (x0 + x1) / 2);
+            *reinterpret_cast<uint4*>(to + at) = make_uint4(a0.x, a0.y, a1.x, a1.y);
+            *reinterpret_cast<uint4*>(to + C::kTileBytes + at) = make_uint4(b0.x, b0.y, b1.x, b1.y);
+          }
+        }
+        s_rows[r] = s.down * p.scale_log2;
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_full);
+      for (int j = 0; j < nt; ++j, ++n) {
+        if (!fp8b::mbar_wait_all(&v_full[v.i], v.phase, s_abort) || (n >= 2 && !fp8b::mbar_wait_all(&w_empty[o.i], o.phase ^ 1, s_abort))) {
+          if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrConvertR);
+          ok = false;
+          break;
+        }
+        widen_values<D, 128>(smem + C::kOffCodes + v.i * C::kTileBytes, smem + C::kOffValues + o.i * C::kValueBytes, i,
+                             static_cast<int>(min(left0 - static_cast<int64_t>(j) * kTok, static_cast<int64_t>(kTok))));
+        fence_proxy_async_smem();  // the tensor core reads what these stores wrote
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&w_full[o.i]);
+          mbar_arrive(&v_empty[v.i]);
+        }
+        v.step(C::kValueSlots);
+        o.step(2);
+      }
+    }
+  } else {
+    // ---- softmax and epilogue: thread = row
+    fp8b::regs_take<184>();
+    const int q = warp >> 2, i = threadIdx.x & 127;
+    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t ts = tmem + lane_base + q * kTok, to = tmem + lane_base + 256 + q * 128;
+    const float4* table = reinterpret_cast<const float4*>(smem + C::kOffScales);
+    bool failed = !any;
+    int nt, tiles = 0, done = 0, items = 0;  // tiles: of the block scales; done: of this row tile
+    for (int seg = 0; !failed && segment(seg, nt); ++seg) {
+      const Seg& g = s_seg[seg % kSegs];
+      const int r = q * kTok + i, rows = g.rows, row = g.row0 + r, L = g.L, tile0 = g.tile0, h = g.h, part = g.part;
+      const int64_t t = g.first + row / p.G;  // row of the tensors
+      const int64_t pos = static_cast<int64_t>(L) - g.n + row / p.G;
+      __syncwarp();
+      done_with(seg);
+      const bool mine = r < rows;
+      // tokens that the row sees (a row there is none of: all, which spares the others of its warp the masked form)
+      const int hi = mine && p.causal ? static_cast<int>(max(min(pos + 1, static_cast<int64_t>(L)), static_cast<int64_t>(0))) : L;
+      const int lo = mine && p.window > 0 ? static_cast<int>(max(pos + 1 - p.window, static_cast<int64_t>(0))) : 0;
+      const int hi_all = __reduce_min_sync(0xFFFFFFFFu, hi), lo_all = __reduce_max_sync(0xFFFFFFFFu, lo);
+      float m = -INFINITY, l = 0.0f;
+      if (nt > 0) {
+        if (!fp8b::mbar_wait_all(q_full, items & 1, s_abort)) {
+          failed = true;
+          break;
+        }
+        ++items;
+        const float c = q * kTok < rows ? s_rows[r] : 0.0f;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_empty);
+        for (int j = 0; j < nt; ++j, ++tiles) {
+          const int slot = tiles % kScaleSlots;
+          if (!fp8b::mbar_wait_all(&e_full[slot], (tiles / kScaleSlots) & 1, s_abort)) {
+            failed = true;
+            break;
+          }
+          if (q * kTok < rows) {
+            if (!fp8b::mbar_wait_all(&s_full[q], done & 1, s_abort)) {
+              failed = true;
+              break;
+            }
+            tc_fence_after_sync();
+            float x[128];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) fp8b::tmem_ld32(ts + k * 32, x + k * 32);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) fp8b::tmem_ld_wait32(x + k * 32);
+            const int base = (tile0 + j) * kTok;
+            auto accumulated = [&] { return fp8b::mbar_wait_all(&pv_done[q], (done - 1) & 1, s_abort); };
+            const float4* e = table + slot * 8;
+            const bool ok = base >= lo_all && base + (kTok - 1) < hi_all
+                                ? softmax_tile<D, false>(x, e, c, 0, kTok, m, l, ts, to, j == 0, accumulated)
+                                : softmax_tile<D, true>(x, e, c, lo - base, hi - base, m, l, ts, to, j == 0, accumulated);
+            if (!ok) {
+              failed = true;
+              break;
+            }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&p_full[q]);
+            ++done;
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&e_empty[slot]);
+        }
+        if (failed) break;
+        if (q * kTok < rows) {
+          if (!fp8b::mbar_wait_all(&pv_done[q], (done - 1) & 1, s_abort)) {
+            failed = true;
+            break;
+          }
+          tc_fence_after_sync();
+        }
+      }
+      if (q * kTok >= rows) continue;
+      float* to_part = part < 0 ? nullptr : p.partial + static_cast<int64_t>(part) * (kRows * (D + 2));
+      const int hq = h * p.G + row % p.G;
+      if (part >= 0) {
+        to_part[kRows * D + r] = l;
+        to_part[kRows * D + kRows + r] = m;
+      } else if (mine && p.lse) {
+        p.lse[t * (static_cast<int64_t>(p.G) * p.c.H) + hq] = l == 0.0f ? -INFINITY : (log2f(l) + m - kShift) * (1.0f / kLog2e);
+      }
+      if (nt > 0) {
+        const float f = part >= 0 ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);
+#pragma unroll 1
+        for (int d = 0; d < D; d += 16) {
+          float o[16];
+          tmem_ld16(to + d, o);
+          tmem_ld_wait_regs<16>(o);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) o[k] *= f;
+          if (part >= 0) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) *reinterpret_cast<float4*>(to_part + r * D + d + 4 * k) = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+          } else if (mine) {
+            store16(p, t * p.ldo + static_cast<int64_t>(hq) * D + d, o);
+          }
+        }
+        tc_fence_before_sync();
+      }
+    }
+    if (failed && any && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrSoftmaxR);
+  }
+
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// Results of items that several CTAs share: a block per item and 8 rows, a warp per row, D / 32 features per lane.
+template <int D>
+__global__ void __launch_bounds__(256) attention_join_rows_kernel(const P p, int ctas) {
+  constexpr int E = D / 32;
+  __shared__ int64_t s_scan[8];
+  __shared__ int s_at[3];
+  pdl_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t item = blockIdx.x;
+  pdl_wait();
+  const int per = (p.c.B + 255) / 256;
+  const int b0 = min(static_cast<int>(threadIdx.x) * per, p.c.B), b1 = min(b0 + per, p.c.B);
+  int64_t mine = 0;
+  for (int b = b0; b < b1; ++b) mine += static_cast<int64_t>(seq_of(p, b).blocks) * p.c.H;
+  int64_t incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+    if (lane >= o) incl += x;
+  }
+  if (lane == 31) s_scan[warp] = incl;
+  __syncthreads();
+  int64_t before = 0, total = 0;
+  for (int w = 0; w < 8; ++w) {
+    if (w < warp) before += s_scan[w];
+    total += s_scan[w];
+  }
+  const int splits = splits_of(total, ctas);
+  if (splits == 1 || item >= total) return;
+  const int64_t begin = before + incl - mine;
+  if (begin <= item && item < begin + mine) {
+    int64_t at = begin;
+    int b = b0;
+    for (;; ++b) {
+      const int64_t n = static_cast<int64_t>(seq_of(p, b).blocks) * p.c.H;
+      if (item < at + n) break;
+      at += n;
+    }
+    s_at[0] = b;
+    s_at[1] = static_cast<int>(item - at);
+  }
+  __syncthreads();
+  const Seq s = seq_of(p, s_at[0]);
+  const int h = s_at[1] % p.c.H, row0 = (s.blocks - 1 - s_at[1] / p.c.H) * kRows;
+  const int r = blockIdx.y * 8 + warp;
+  if (static_cast<int64_t>(row0) + r >= static_cast<int64_t>(s.n) * p.G) return;
+  constexpr int64_t kPart = kRows * (D + 2);
+  const float* part = p.partial + item * splits * kPart;
+  float m = -INFINITY;
+  for (int i = 0; i < splits; ++i) m = fmaxf(m, load_chained(part + i * kPart + kRows * D + kRows + r));
+  float l = 0.0f, o[E] = {};
+  for (int i = 0; i < splits; ++i) {
+    const float mi = load_chained(part + i * kPart + kRows * D + kRows + r), li = load_chained(part + i * kPart + kRows * D + r);
+    if (li == 0.0f) continue;  // (a piece that saw nothing, or was empty: what lies there is nothing)
+    const float f = mi == -INFINITY ? 1.0f : exp2f(mi - m);  // (a sum that is NaN has no maximum)
+    l = fmaf(f, li, l);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(f, load_chained(part + i * kPart + r * D + e * 32 + lane), o[e]);
+  }
+  const int64_t t = s.first + (row0 + r) / p.G;
+  const int hq = h * p.G + (row0 + r) % p.G;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float v = l == 0.0f ? 0.0f : o[e] / l;
+    const int64_t at = t * p.ldo + static_cast<int64_t>(hq) * D + e * 32 + lane;
+    if (p.f32)
+      static_cast<float*>(p.out)[at] = v;
+    else
+      static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
+  }
+  if (p.lse && lane == 0) p.lse[t * (static_cast<int64_t>(p.G) * p.c.H) + hq] = l == 0.0f ? -INFINITY : (log2f(l) + m - kShift) * (1.0f / kLog2e);
+}
+
+template <int D>
+int launch_cfg(const CUtensorMap& tm, const P& p, int grid, cudaStream_t st) {
+  using C = Cfg<D>;
+  static DeviceOnce once;
+  if (!allow_shared_memory(once, attention_rows_kernel<D>, C::kSmemBytes)) return ZQ_ERR_CUDA;
+  cudaError_t e = launch_chained(attention_rows_kernel<D>, dim3(grid), dim3(kThreads), C::kSmemBytes, st, false, tm, p);
+  count_launch();
+  if (e != cudaSuccess) return ZQ_ERR_CUDA;
+  e = launch_chained(attention_join_rows_kernel<D>, dim3(grid / 2, kRows / 8), dim3(256), 0, st, false, p, grid);
+  count_launch();
+  return e == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
+}
+
+}  // namespace
+
+// (the same place as the other kernel's: the kernels of a call run one after the other)
+size_t rows_workspace_bytes(int64_t D) { return sizeof(float) * kMaxCtas * kRows * (D + 2); }
+
+int launch_attention_rows(const AttnArgs& a, cudaStream_t st) {
+  P p{};
+  p.c = a.c;
+  p.q = static_cast<const __nv_bfloat16*>(a.q), p.ldq = a.ldq, p.G = a.Hq / a.c.H;
+  p.scale_log2 = a.sm_scale * kLog2e;
+  p.causal = a.causal, p.window = a.window;
+  p.out = a.out, p.f32 = a.dt == ZQ_OUT_F32, p.ldo = a.ldo, p.lse = a.lse;
+  uint8_t* ws = static_cast<uint8_t*>(a.workspace);
+  p.status = reinterpret_cast<int*>(ws);
+  p.partial = reinterpret_cast<float*>(ws + kWsHeadBytes);
+  CUtensorMap tm;
+  if (!make_page_map(&tm, a.c)) return ZQ_ERR_CUDA;
+  const int sms = sm_count(), grid = sms < kMaxCtas ? sms : kMaxCtas;
+  return a.c.D == 128 ? launch_cfg<128>(tm, p, grid, st) : launch_cfg<64>(tm, p, grid, st);
+}
+
+}  // namespace kv
+}  // namespace zq

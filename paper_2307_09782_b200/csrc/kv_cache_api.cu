@@ -145,7 +145,8 @@ int zq_kv_cache_read(const uint8_t* codes, const float* scale, int64_t pages, in
 
 size_t zq_kv_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D) {
   if (T < 0 || B < 0 || T > kMaxRows || B > kMaxRows || H < 1 || H > kMaxHeads || Hq < H || Hq > kMaxHeads || Hq % H || !dim_ok(D)) return 0;
-  return kWsHeadBytes + few_workspace_bytes(B, H, D);
+  const size_t few = few_workspace_bytes(B, H, D), rows = rows_workspace_bytes(D);
+  return kWsHeadBytes + (few > rows ? few : rows);
 }
 
 int zq_kv_attention(const void* q, int64_t ldq, int64_t Hq, int64_t T, const int32_t* cu, int64_t B, const int32_t* lens,
@@ -155,7 +156,8 @@ int zq_kv_attention(const void* q, int64_t ldq, int64_t Hq, int64_t T, const int
   if ((dt != ZQ_OUT_F32 && dt != ZQ_OUT_BF16) || (causal != 0 && causal != 1) || (window != 0 && !causal)) return ZQ_ERR_MODE;
   AttnArgs a{};
   if (int e = check_cache(codes, scale, pages, H, page, D, table, table_ld, lens, true, cu, B, T, a.c)) return e;
-  if (Hq < H || Hq > kMaxHeads || Hq % H || window < 0 || !(sm_scale > 0.0f) || std::isinf(sm_scale)) return ZQ_ERR_SHAPE;
+  if (Hq < H || Hq > kMaxHeads || Hq % H || window < 0 || !(sm_scale > 0.0f) || std::isinf(sm_scale) || T * (Hq / H) > kMaxRows)
+    return ZQ_ERR_SHAPE;
   if (!row_ok(ldq, Hq, D) || !row_ok(ldo, Hq, D)) return ZQ_ERR_SHAPE;
   if (T == 0 || B == 0) return ZQ_OK;
   if (!q || !out) return ZQ_ERR_NULL;

@@ -83,7 +83,8 @@ def gather(codes, scale, table_row, L):
 
 
 def attention(codes, scale, q, table, lens, cu, sm_scale, causal, window):
-    """(o, lse, bound): `bound` is what errors of probabilities multiply: sum of p |v|, and the largest |q| . |k| of the row."""
+    """(o, lse, bound): `bound` is what errors multiply: sum of p |v|; the largest |q| . |k| of the row; the largest product of a
+    probability and its value's scale times the sum of |codes|."""
     T, Hq, D = q.shape
     H = codes.shape[2]
     G = Hq // H
@@ -91,12 +92,15 @@ def attention(codes, scale, q, table, lens, cu, sm_scale, causal, window):
     pv = torch.zeros_like(o)
     lse = torch.full((T, Hq), -math.inf, dtype=F64, device=q.device)
     qk = torch.zeros((T, Hq), dtype=F64, device=q.device)
+    low = torch.zeros_like(o)
     tab = table.tolist()
     for b in range(len(lens)):
         L, r0, n = lens[b], cu[b], cu[b + 1] - cu[b]
         if L <= 0 or n <= 0:
             continue
         kv = gather(codes, scale, tab[b], L)
+        ones = torch.full_like(codes[:, :, :, :, :1], 0x38)  # E4M3's 1: the blocks' scales, token by token
+        per_token = gather(ones, scale, tab[b], L)[1, :, :, 0].nan_to_num(nan=1.0)
         pos = torch.arange(L - n, L, device=q.device)[:, None]
         col = torch.arange(L, device=q.device)[None]
         seen = torch.ones((n, L), dtype=torch.bool, device=q.device)
@@ -118,10 +122,13 @@ def attention(codes, scale, q, table, lens, cu, sm_scale, causal, window):
             poison = (seen.to(F64) @ bad) > 0
             o[r0:r0 + n, hq] = torch.where(any_[:, None], torch.where(poison, math.nan, e @ clean / z), 0.0)
             pv[r0:r0 + n, hq] = torch.where(any_[:, None], e @ clean.abs() / z, 0.0)
+            sv = per_token[hq // G]
+            top = (e / torch.where(z > 0, z, 1.0) * sv).max(1, keepdim=True).values
+            low[r0:r0 + n, hq] = top * (seen.to(F64) @ (clean.abs() / torch.where(sv > 0, sv, 1.0)[:, None]))
             lse[r0:r0 + n, hq] = torch.where(any_, m + torch.log(z[:, 0]), -math.inf)
             kk = torch.nan_to_num(k, nan=0.0).abs()
             qk[r0:r0 + n, hq] = torch.where(seen, x.abs() @ kk.T, 0.0).max(1).values * sm_scale
-    return o, lse, (pv, qk)
+    return o, lse, (pv, qk, low)
 
 
 def batch(lens, new, H, D, page, seed=0, mode="none", spare=3, spread=1.0, dev="cuda"):

@@ -5,7 +5,10 @@ Tolerances.  A result of type t is off by at most finfo(t).eps / 2 of its value 
 norms: FP32 sums of D squares and a few products, 2^-20 of the larger feature of a pair.
 attention: a probability is rounded to 11 bits (2^-11); FP32 scores are off by 2^-18 of sum |q| |k| at most (two tensor-core
 sums of 128 products that round towards zero, and the parts of q below 2^-17 of its row's largest), which counts twice, in the
-numerator and in the sum; the power of two and the sums of a few thousand terms add 2^-18.
+numerator and in the sum; the power of two and the sums of a few thousand terms add 2^-18.  FP16 ends: a probability times its
+value's scale is kept with the row's largest at 2^8 or more, in steps of 2^-24 at the least, so each is off by 2^-25 / 2^8 = 2^-33
+of the largest, which multiplies its code: 2^-33 (largest p scale) (sum of |codes|).  (That shows where the tokens with the large
+probabilities have a code of zero: with sm_scale = 1 one result in 150000 is 3e-11 beside others of 1.)
 """
 import math
 
@@ -244,8 +247,8 @@ ATTN_CASES = [
 
 
 def attn_tolerance(ref, bound, out):
-    pv, qk = bound
-    return half_step(out) * ref.abs() + pv * (2.0 ** -11 + 2 * 2.0 ** -18 * qk[..., None] + 2.0 ** -17) + 1e-30
+    pv, qk, low = bound
+    return half_step(out) * ref.abs() + pv * (2.0 ** -11 + 2 * 2.0 ** -18 * qk[..., None] + 2.0 ** -17) + 2.0 ** -33 * low + 1e-30
 
 
 def check_attention(case, out, seed=0, lens_override=None, **kw):
@@ -302,13 +305,13 @@ def test_attention_zero_and_extreme_blocks(case):
 
 
 @pytest.mark.parametrize("case", [([300, 200], [1, 1], 8, 2, 128, 64, True, 0), ([300, 200], [6, 3], 8, 2, 128, 64, True, 0),
-                                  ([300, 200], [250, 200], 4, 2, 64, 32, True, 0), ([300, 200], [250, 90], 4, 2, 128, 16, True, 40)])
+                                  ([300, 200], [24, 3], 4, 2, 128, 16, True, 0), ([300, 200], [250, 200], 4, 2, 64, 32, True, 0), ([300, 200], [250, 90], 4, 2, 128, 16, True, 40)])
 def test_attention_nan_blocks(case):
     """A block that stands for NaN reaches the rows that see it and no others; so does a page the table names wrongly."""
     lens, new, Hq, H, D, page, causal, window = case
     for what in ("key", "value", "page"):
         codes, scale, table, lens, cu = R.batch(lens, new, H, D, page)
-        i = 2 if page >= 64 else 5
+        i = 2 if page >= 64 else 17 if page == 16 and new[0] == 24 else 5  # (17: some of the first sequence's rows end before it)
         p = int(table[0, i])
         if what == "page":
             table[0, i] = -3
