@@ -888,10 +888,10 @@ def qk_norm_rope_backward(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k
                           workspace: Optional[torch.Tensor] = None):
     """Gradients of :func:`qk_norm_rope`'s inputs and weights from those of its outputs: (of q, of k, of wq, of wk); bf16, and
     float32 or None for the weights."""
-    ldq, ldk, T, Hq, H, D = _rope_args(q, k, table, positions, wq, wk)
     lddq, lddk = _heads(dq, "dq")[0], _heads(dk, "dk")[0]
     if dq.shape != q.shape or dk.shape != k.shape:
         raise ValueError(f"gradients {tuple(q.shape)} and {tuple(k.shape)} are needed, got {tuple(dq.shape)} and {tuple(dk.shape)}")
+    ldq, ldk, T, Hq, H, D = _rope_args(q, k, table, positions, wq, wk)
     _on_gpu(dq, dk)
     dxq, dxk = q.new_empty((T, Hq, D)), k.new_empty((T, H, D))
     dwq = dwk = None
