@@ -12,13 +12,14 @@ constexpr int kFewRows = 64;        // rows (new tokens x query heads of a cache
 constexpr int kMaxCtas = 148;       // CTAs whose partial results the workspace has room for
 constexpr float kLog2e = 1.4426950408889634f;
 // Probabilities are kept times 2^kShift (the row's largest at most 2^kShift), where FP16 holds 11 bits down to 2^-22 of the
-// largest and something down to 2^-32.  The factor cancels against the sum of the probabilities.
+// largest and something down to 2^-32.  Values are code / 256.  Both factors cancel against the sum of the probabilities.
 constexpr float kShift = 8.0f;
+constexpr float kCodeUnit = 1.0f / 256.0f;
 
 int launch_attention_few(const AttnArgs& a, int max_rows, cudaStream_t st);
 int launch_attention_rows(const AttnArgs& a, cudaStream_t st);
 size_t rows_workspace_bytes(int64_t D);
-size_t few_workspace_bytes(int64_t B, int64_t H, int64_t D);
+size_t few_workspace_bytes(int64_t D);
 
 #ifdef __CUDACC__
 // ---- operands ---------------------------------------------------------------------------------------------------------
@@ -62,15 +63,21 @@ __device__ __forceinline__ void umma_f16(uint32_t d_tmem, uint64_t a_desc, uint6
       : "memory");
 }
 
-// A converter thread's share of a tile of values: codes [128][D] (rows as they lie in memory) -> FP16 in the operand's layout, each
-// code's own value.  Tokens from `valid` on become zeros, whatever the page holds there.  All of the share's codes are loaded
-// before the first store (the compiler cannot tell their addresses apart), kAtOnce pieces of 16 at a time.
-// A NaN becomes the largest FP16 number: what nobody sees (a page that was not copied, say) must not turn into NaN by a product
-// with zero.
-__device__ __forceinline__ uint32_t widen2(uint32_t codes) {  // the lower two
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n\tmin.f16x2 %0, %0, %2;" : "=&r"(h) : "h"(static_cast<uint16_t>(codes)), "r"(0x7BFF7BFFu));
-  return h;
+// A converter thread's share of a tile of values: codes [128][D] (rows as they lie in memory) -> FP16 code / 256 in the operand's
+// layout: E4M3's exponent and mantissa bits moved into FP16's fields, which have one exponent bit more, whence the factor
+// (subnormal numbers come out right as well).  The hardware's conversion would do it at a quarter of the rate (a tile 1300 cycles
+// instead of about 500).  Codes are taken two and two as they lie in a word, so features 1 and 2 of every four change places
+// (feature_at).  The pattern of E4M3's NaN becomes 480 / 256: what nobody sees (a page that was not copied, say) must not turn
+// into NaN by a product with zero.  Tokens from `valid` on become zeros, whatever the page holds there.  All of the share's codes
+// are loaded before the first store (the compiler cannot tell their addresses apart), kAtOnce pieces of 16 at a time.
+__device__ __forceinline__ uint2 widen4(uint32_t w) {
+  return make_uint2(((w << 8) & 0x80008000u) | ((w << 7) & 0x3F803F80u), (w & 0x80008000u) | ((w >> 1) & 0x3F803F80u));
+}
+// The feature at position d of the widened values, and the other way round.
+__host__ __device__ __forceinline__ int feature_at(int d) { return (d & ~3) | ((d & 1) << 1) | ((d >> 1) & 1); }
+__device__ __forceinline__ uint4 widen8(uint32_t a, uint32_t b) {
+  const uint2 x = widen4(a), y = widen4(b);
+  return make_uint4(x.x, x.y, y.x, y.y);
 }
 template <int D, int THREADS>
 __device__ __forceinline__ void widen_values(const uint8_t* codes, uint8_t* out, int i, int valid) {
@@ -92,8 +99,8 @@ __device__ __forceinline__ void widen_values(const uint8_t* codes, uint8_t* out,
 #pragma unroll
     for (int x = 0; x < kAtOnce; ++x) {
       uint8_t* dst = to + (x0 + x) * (THREADS / kPerRow) * 128;
-      *reinterpret_cast<uint4*>(dst + to0) = make_uint4(widen2(v[x].x), widen2(v[x].x >> 16), widen2(v[x].y), widen2(v[x].y >> 16));
-      *reinterpret_cast<uint4*>(dst + to1) = make_uint4(widen2(v[x].z), widen2(v[x].z >> 16), widen2(v[x].w), widen2(v[x].w >> 16));
+      *reinterpret_cast<uint4*>(dst + to0) = widen8(v[x].x, v[x].y);
+      *reinterpret_cast<uint4*>(dst + to1) = widen8(v[x].z, v[x].w);
     }
   }
 }
@@ -136,20 +143,26 @@ __device__ __forceinline__ void split8(uint4 v, float up, uint2& first, uint2& s
 }
 
 // ---- block scales -------------------------------------------------------------------------------------------------------
-// What 16 tokens of a tile (part of one page) contribute: keys' scale, log2 of the values' scale, its inverse.
+// What 16 tokens of a tile (part of one page) contribute: keys' scale, log2 of the values' scale, its inverse times kCodeUnit.
 // The values' scale goes into the power of two of the probability, so that nothing of it is rounded apart, and comes out of the
-// sum again by its inverse.
-__device__ __forceinline__ float4 scale_entry(const Cache& c, int b, int h, int token, int L) {
-  float4 e = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  if (token >= L) return e;  // nobody sees them
-  const int page = page_of(c, b, token / c.page);
-  const float ks = page < 0 ? __uint_as_float(0x7FC00000u) : load_chained(c.scale + block_at(c, page, 0, h));
-  float vs = page < 0 ? 1.0f : load_chained(c.scale + block_at(c, page, 1, h));
-  if (vs < 5.42101086242752217e-20f) vs = 5.42101086242752217e-20f;  // 2^-64: what was never written has 0
-  e.x = ks;
-  e.y = log2f(vs);
-  e.z = isnan(vs) ? 1.0f : 1.0f / vs;  // (a block that stands for NaN: the power is NaN where it is seen)
-  return e;
+// sum again by its inverse times kCodeUnit.
+struct RawScales {
+  float ks, vs;
+  bool seen;
+};
+__device__ __forceinline__ RawScales load_scales(const Cache& c, int b, int h, int64_t token, int L) {
+  RawScales r{0.0f, 1.0f, token < L};
+  if (!r.seen) return r;
+  const int page = page_of(c, b, static_cast<int>(token) / c.page);
+  r.ks = page < 0 ? __uint_as_float(0x7FC00000u) : load_chained(c.scale + block_at(c, page, 0, h));
+  r.vs = page < 0 ? 1.0f : load_chained(c.scale + block_at(c, page, 1, h));
+  return r;
+}
+__device__ __forceinline__ float4 scale_entry(const RawScales& r) {
+  if (!r.seen) return make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  const float vs = r.vs < 5.42101086242752217e-20f ? 5.42101086242752217e-20f : r.vs;  // 2^-64: what was never written has 0
+  // (a block that stands for NaN: the power is NaN where it is seen)
+  return make_float4(r.ks, log2f(vs), isnan(vs) ? 1.0f : kCodeUnit / vs, 0.0f);
 }
 
 // Pages of consecutive tiles, a batch of 32 table entries per warp with the next batch on its way.

@@ -14,17 +14,17 @@
 // Where several CTAs share a sequence and head, each leaves its sums, maximum and results in the workspace;
 // attention_join_kernel adds them up in the order of the tiles.
 //
-// Warp roles: 0..7 softmax (thread = token), 8..11 epilogue (thread = feature), 12..15 converters of values, 16 keys' copies,
-// 17 values' copies, 18 MMAs, 19 the walk, queries and scales.
+// Warp roles: 0..7 softmax (thread = token), 8..11 queries and epilogue (thread = feature), 12..15 converters of values, 16 keys'
+// copies, 17 values' copies, 18 MMAs, 19 the walk over the segments and the block scales.
 #include "kv_attention.cuh"
 
 namespace zq {
 namespace kv {
 namespace {
 
-constexpr int kSoftmaxWarps = 8, kEpiWarp0 = 8, kConvWarp0 = 12, kKeyWarp = 16, kValueWarp = 17, kMmaWarp = 18, kQueryWarp = 19;
+constexpr int kSoftmaxWarps = 8, kEpiWarp0 = 8, kConvWarp0 = 12, kKeyWarp = 16, kValueWarp = 17, kMmaWarp = 18, kWalkWarp = 19;
 constexpr int kThreads = 20 * 32;
-enum { kErrKeysA = 51, kErrValuesA = 52, kErrMmaA = 53, kErrScalesA = 54, kErrQueriesA = 55, kErrSoftmaxA = 56, kErrConvertA = 57, kErrEpilogueA = 58, kErrAlignA = 59 };
+enum { kErrKeysA = 51, kErrValuesA = 52, kErrMmaA = 53, kErrWalkA = 54, kErrQueriesA = 55, kErrSoftmaxA = 56, kErrConvertA = 57, kErrEpilogueA = 58, kErrAlignA = 59 };
 
 struct P {
   Cache c;
@@ -38,11 +38,11 @@ struct P {
   int f32;
   float* lse;
   float* partial;    // [CTAs][2][R (D + 2)]
-  int2* pieces;      // [B * H]: first CTA and number of CTAs of a sequence and head
+  int4* shared;      // [CTAs] what begins in the CTA and goes on in the next: sequence, head, CTAs (0: nothing does)
   int* status;
 };
 
-// A segment, as the queries' warp announces it to the others in shared memory (kSegs of them in turn).
+// A segment, as the walk announces it to the others in shared memory (kSegs of them in turn).
 struct alignas(16) Seg {
   int nt;           // tiles; 0: no more segments
   int tile0;        // the first of them, of the sequence's tiles of 128 tokens
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
   uint64_t* w_full = v_empty + C::kValueSlots;       // [2] widened values                                     (MMA)
   uint64_t* w_empty = w_full + 2;                    // [2] their products are done                            (converters)
   uint64_t* s_full = w_empty + 2;                    // [2] scores of a chunk                                  (softmax)
-  uint64_t* s_empty = s_full + 2;                    // [2] they have been used, with the scales               (MMA, scales)
+  uint64_t* s_empty = s_full + 2;                    // [2] they have been used, with the scales               (MMA, walk)
   uint64_t* e_full = s_empty + 2;                    // [2] block scales of a chunk                            (softmax)
   uint64_t* p_full = e_full + 2;                     // [2] probabilities and row factors of a chunk           (MMA, epilogue)
   uint64_t* o_full = p_full + 2;                     // [2] results of a chunk                                 (epilogue)
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
   uint64_t* l_empty = l_full + 1;                    // they have been read                                    (softmax)
   uint64_t* meet = l_empty + 1;                      // [2] softmax warps that share rows
   uint64_t* g_full = meet + 2;                       // [kSegs] a segment is announced                         (all)
-  uint64_t* g_empty = g_full + kSegs;                // [kSegs] everybody is through with it                   (queries)
+  uint64_t* g_empty = g_full + kSegs;                // [kSegs] everybody is through with it                   (walk)
   uint64_t* drain = g_empty + kSegs;
   const Seg* s_seg = reinterpret_cast<const Seg*>(smem + C::kOffSegs);
   int64_t* s_range = reinterpret_cast<int64_t*>(smem + C::kOffBars + 64 * 8);  // units, first sequence, first unit in it
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
       mbar_init(&p_full[i], kSoftmaxWarps);
       mbar_init(&o_full[i], 1);
       mbar_init(&o_empty[i], 4);
-      mbar_init(&q_full[i], 1);
+      mbar_init(&q_full[i], 4);
       mbar_init(&q_empty[i], 1 + kSoftmaxWarps);
     }
     mbar_init(l_full, kSoftmaxWarps);
@@ -394,98 +394,56 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     while (!mbar_try_wait(drain, 0) && ++spin < kSpinLimit) {
     }
     __syncwarp();
-  } else if (warp == kQueryWarp) {
-    // ---- queries of a segment (D / 8 lanes per row), then its chunks' block scales (a lane per 16 tokens)
+  } else if (warp == kWalkWarp) {
+    // ---- the walk: segments, and their chunks' block scales (a lane per 16 tokens), which are on their way one chunk ahead
     fp8b::regs_give<80>();
-    constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes, kBatch = 8;
     float4* table = reinterpret_cast<float4*>(smem + C::kOffScales);
     int seg = 0, chunk = 0;
-    Walk w;
-    bool ok = any && w.start(p, s_range);
-    // announces segment `seg`, or (nt = 0) that there are no more
-    auto announce = [&](int nt) {
+    Walk w;  // of the segment announced last
+    bool more = any && w.start(p, s_range), ok = more;
+    // Announces segment `seg`, or that there are no more.  A segment is announced when the one before it begins here: the epilogue
+    // fetches its queries ahead and must not wait for chunks that wait for the epilogue.
+    auto announce = [&] {
       if (seg >= kSegs && !mbar_wait_warp(&g_empty[seg % kSegs], (seg / kSegs - 1) & 1, s_abort)) return false;
       if (lane == 0) {
         Seg g{};
-        g.nt = nt;
-        if (nt > 0) {
-          g.tile0 = w.s.tile0 + w.t, g.L = w.s.L, g.n = w.s.n, g.b = w.b, g.h = w.h, g.first = w.s.first;
-          g.flags = (w.t == 0 ? 1 : 0) | (w.t + nt == w.s.tiles ? 2 : 0);
+        if (more) {
+          g.nt = w.nt, g.tile0 = w.s.tile0 + w.t, g.L = w.s.L, g.n = w.s.n, g.b = w.b, g.h = w.h, g.first = w.s.first;
+          g.flags = (w.t == 0 ? 1 : 0) | (w.t + w.nt == w.s.tiles ? 2 : 0);
         }
         *const_cast<Seg*>(s_seg + seg % kSegs) = g;
         mbar_arrive(&g_full[seg % kSegs]);
       }
       __syncwarp();
+      ++seg;
       return true;
     };
-    if (ok) do {
-        const int rows = w.s.n * p.G, qb = seg & 1;
-        if (!announce(w.nt)) {
-          if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrQueriesA);
-          ok = false;
-          break;
-        }
-        if (seg >= 2 && !mbar_wait_warp(&q_empty[qb], ((seg >> 1) - 1) & 1, s_abort)) {
-          if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrQueriesA);
-          ok = false;
-          break;
-        }
-        uint8_t* to = smem + C::kOffQueries + qb * 2 * R * D;
-        int4* info = reinterpret_cast<int4*>(smem + C::kOffRows) + qb * R;
-        for (int r0 = 0; r0 < rows; r0 += kAtOnce * kBatch) {
-          uint4 x[kBatch];
-#pragma unroll
-          for (int i = 0; i < kBatch; ++i) {
-            const int r = r0 + i * kAtOnce + lane / kLanes;
-            x[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (r < rows)
-              x[i] = load_chained(reinterpret_cast<const uint4*>(p.q + (w.s.first + r / p.G) * p.ldq + (static_cast<int64_t>(w.h) * p.G + r % p.G) * D + (lane % kLanes) * 8));
-          }
-#pragma unroll
-          for (int i = 0; i < kBatch; ++i) {
-            const int r = r0 + i * kAtOnce + lane / kLanes;
-            uint32_t a = absmax_bits8(x[i]);
-#pragma unroll
-            for (int o = kLanes / 2; o; o >>= 1) a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
-            const RowScale s = row_scale(a);
-            uint2 first, second;
-            split8(x[i], s.up, first, second);
-            if (r < rows) {
-              const int piece = (lane % kLanes) >> 1, half = (lane & 1) * 8;
-              *reinterpret_cast<uint2*>(to + row_piece<D>(r, piece) + half) = first;
-              *reinterpret_cast<uint2*>(to + row_piece<D>(R + r, piece) + half) = second;
-              if (lane % kLanes == 0) {
-                const int64_t pos = static_cast<int64_t>(w.s.L) - w.s.n + r / p.G;
-                const int64_t hi = p.causal ? min(pos + 1, static_cast<int64_t>(w.s.L)) : w.s.L;
-                const int64_t lo = p.window > 0 ? pos + 1 - p.window : 0;
-                info[r] = make_int4(__float_as_int(s.down * p.scale_log2), static_cast<int>(max(lo, static_cast<int64_t>(0))),
-                                    static_cast<int>(max(hi, static_cast<int64_t>(0))), 0);
-              }
-            }
-          }
-        }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&q_full[qb]);
-        ++seg;
-        for (int t = 0; t < w.nt; t += kTiles, ++chunk) {
+    auto load = [&](int b, int h, int tile, int L) {
+      return load_scales(p.c, b, h, lane < kTiles * 8 ? static_cast<int64_t>(tile) * kTok + lane * 16 : L, L);
+    };
+    if (ok) {
+      ok = announce();
+      RawScales next = load(w.b, w.h, w.s.tile0 + w.t, w.s.L);
+      while (ok && more) {
+        const int b = w.b, h = w.h, L = w.s.L, nt = w.nt, tile0 = w.s.tile0 + w.t;
+        more = w.next(p);
+        ok = announce();
+        for (int t = 0; ok && t < nt; t += kTiles, ++chunk) {
           const int cb = chunk & 1;
-          float4 e;
-          if (lane < kTiles * 8) {
-            const int64_t token = static_cast<int64_t>(w.s.tile0 + w.t + t) * kTok + lane * 16;
-            e = scale_entry(p.c, w.b, w.h, static_cast<int>(min(token, static_cast<int64_t>(w.s.L))), w.s.L);
-          }
-          if (chunk >= 2 && !mbar_wait_warp(&s_empty[cb], ((chunk >> 1) - 1) & 1, s_abort)) {
-            if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrScalesA);
-            ok = false;
-            break;
-          }
+          const float4 e = scale_entry(next);
+          if (t + kTiles < nt)
+            next = load(b, h, tile0 + t + kTiles, L);
+          else if (more)
+            next = load(w.b, w.h, w.s.tile0 + w.t, w.s.L);
+          if (chunk >= 2 && !mbar_wait_warp(&s_empty[cb], ((chunk >> 1) - 1) & 1, s_abort)) ok = false;
+          if (!ok) break;
           if (lane < kTiles * 8) table[cb * kTiles * 8 + lane] = e;
           __syncwarp();
           if (lane == 0) mbar_arrive(&e_full[cb]);
         }
-      } while (ok && w.next(p));
-    if (ok && !announce(0) && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrQueriesA);
+      }
+      if (!ok && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrWalkA);
+    }
   } else if (warp >= kConvWarp0) {
     fp8b::regs_give<64>();
     const int i = threadIdx.x - kConvWarp0 * 32;
@@ -677,7 +635,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     if (failed && any && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrSoftmaxA);
   } else {
     // ---- epilogue: thread = feature
-    const int d = (warp & 3) * 32 + lane;
+    const int d = feature_at((warp & 3) * 32 + lane);
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const float* s_max = reinterpret_cast<const float*>(smem + C::kOffMax);
     const float* s_sum = reinterpret_cast<const float*>(smem + C::kOffSum);
@@ -686,12 +644,66 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     bool failed = !any;
     int chunk = 0, seg = 0;
     int64_t unit = any ? total * blockIdx.x / ctas : 0;
-    int nt_seg;
-    for (; !failed && segment(seg, nt_seg); ++seg) {
+    if (threadIdx.x == kEpiWarp0 * 32) p.shared[blockIdx.x] = make_int4(0, 0, 0, 0);
+    // queries of segment `sg` (D / 8 lanes per row), once nobody needs those of the segment two before
+    constexpr int kLanes = D / 8, kAtOnce = 128 / kLanes, kBatch = RS < 2 * kAtOnce ? 1 : 2;
+    auto queries = [&](int sg) {
+      const Seg& g = s_seg[sg % kSegs];
+      const int rows = g.n * p.G, qb = sg & 1, i = threadIdx.x - kEpiWarp0 * 32;
+      uint8_t* to = smem + C::kOffQueries + qb * 2 * R * D;
+      int4* info = reinterpret_cast<int4*>(smem + C::kOffRows) + qb * R;
+      for (int r0 = 0; r0 < rows; r0 += kAtOnce * kBatch) {
+        uint4 x[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+          const int r = r0 + k * kAtOnce + i / kLanes;
+          x[k] = make_uint4(0u, 0u, 0u, 0u);
+          if (r < rows)
+            x[k] = load_chained(reinterpret_cast<const uint4*>(p.q + (g.first + r / p.G) * p.ldq + (static_cast<int64_t>(g.h) * p.G + r % p.G) * D + (i % kLanes) * 8));
+        }
+        if (r0 == 0 && sg >= 2 && !fp8b::mbar_wait_all(&q_empty[qb], ((sg >> 1) - 1) & 1, s_abort)) return false;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+          const int r = r0 + k * kAtOnce + i / kLanes;
+          uint32_t a = absmax_bits8(x[k]);
+#pragma unroll
+          for (int o = kLanes / 2; o; o >>= 1) a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
+          const RowScale s = row_scale(a);
+          uint2 first, second;
+          split8(x[k], s.up, first, second);
+          if (r < rows) {
+            const int piece = (i % kLanes) >> 1, half = (i & 1) * 8;
+            *reinterpret_cast<uint2*>(to + row_piece<D>(r, piece) + half) = first;
+            *reinterpret_cast<uint2*>(to + row_piece<D>(R + r, piece) + half) = second;
+            if (i % kLanes == 0) {
+              const int64_t pos = static_cast<int64_t>(g.L) - g.n + r / p.G;
+              const int64_t hi = p.causal ? min(pos + 1, static_cast<int64_t>(g.L)) : g.L;
+              const int64_t lo = p.window > 0 ? pos + 1 - p.window : 0;
+              info[r] = make_int4(__float_as_int(s.down * p.scale_log2), static_cast<int>(max(lo, static_cast<int64_t>(0))),
+                                  static_cast<int>(max(hi, static_cast<int64_t>(0))), 0);
+            }
+          }
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&q_full[qb]);
+      return true;
+    };
+    int nt_seg, nt_next = 0;
+    if (!failed && segment(0, nt_next)) failed = !queries(0);
+    for (; !failed && nt_next > 0; ++seg) {
+        nt_seg = nt_next;
         const Seg& g = s_seg[seg % kSegs];
         const int rows = g.n * p.G, first = g.first, h = g.h, b = g.b, flags = g.flags;
         __syncwarp();
         done_with(seg);
+        if (!segment(seg + 1, nt_next)) nt_next = 0;  // (an error shows in the waits below)
+        if (nt_next > 0 && !queries(seg + 1)) {
+          if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrQueriesA);
+          failed = true;
+          break;
+        }
         float o[RS];
 #pragma unroll
         for (int r = 0; r < RS; ++r) o[r] = 0.0f;
@@ -719,43 +731,63 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           failed = true;
           break;
         }
+        // each warp sums every row up for itself, a row per lane (and the 32nd after), and hands its factor round
         const bool whole = flags == 3;
         float* part = p.partial + (static_cast<int64_t>(blockIdx.x) * 2 + (flags & 1)) * (R * (D + 2));
+        float factor[(RS + 31) / 32];
 #pragma unroll
-        for (int r = 0; r < RS; ++r)
+        for (int k = 0; k < (RS + 31) / 32; ++k) {
+          const int r = k * 32 + lane;
+          factor[k] = 1.0f;
           if (r < rows) {
-            float sum = 0.0f;
-#pragma unroll
-            for (int k = 0; k < (R == 64 ? 4 : 8); ++k) sum += s_sum[r * 8 + k];
+            const float4* v = reinterpret_cast<const float4*>(s_sum + r * 8);
+            const float4 x = v[0];
+            float sum = ((x.x + x.y) + x.z) + x.w;
+            if (R != 64) {
+              const float4 y = v[1];
+              sum = (((sum + y.x) + y.y) + y.z) + y.w;
+            }
             const float m = s_sum[R * 8 + r];
-            if (!whole) {
-              if (d < D) part[r * D + d] = o[r];
-              if (d == 0) {
+            if (whole) factor[k] = sum == 0.0f ? 0.0f : 1.0f / sum;
+            if (warp == kEpiWarp0) {
+              if (!whole) {
                 part[R * D + r] = sum;
                 part[R * D + R + r] = m;
+              } else if (p.lse) {
+                p.lse[(first + r / p.G) * (static_cast<int64_t>(p.G) * p.c.H) + h * p.G + r % p.G] =
+                    sum == 0.0f ? -INFINITY : (log2f(sum) + m + 8.0f - kShift) * (1.0f / kLog2e);
               }
-            } else {
-              const int64_t row = first + r / p.G;
-              const int hq = h * p.G + r % p.G;
-              const float v = sum == 0.0f ? 0.0f : o[r] / sum;
-              if (d < D) {
-                const int64_t at = row * p.ldo + static_cast<int64_t>(hq) * D + d;
-                if (p.f32)
-                  static_cast<float*>(p.out)[at] = v;
-                else
-                  static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
-              }
-              if (p.lse && d == 0) p.lse[row * (static_cast<int64_t>(p.G) * p.c.H) + hq] = sum == 0.0f ? -INFINITY : (log2f(sum) + m - kShift) * (1.0f / kLog2e);
             }
           }
+        }
+        // row by row without divisions, which would be most of the code: G rows of a token side by side, then the next token
+        // (partial results: all rows one after the other)
+        const int esize = !whole || p.f32 ? 4 : 2, group = whole ? p.G : kFewRows;
+        const int64_t jump = whole ? (p.ldo - static_cast<int64_t>(p.G - 1) * D) * esize : 0;
+        uint8_t* to = whole ? static_cast<uint8_t*>(p.out) + (first * p.ldo + static_cast<int64_t>(h) * p.G * D + d) * esize
+                            : reinterpret_cast<uint8_t*>(part + d);
+        int left = group;
+#pragma unroll
+        for (int r = 0; r < RS; ++r) {
+          const float v = o[r] * __shfl_sync(0xFFFFFFFFu, factor[r / 32], r & 31);
+          if (r < rows && d < D) {
+            if (esize == 4)
+              *reinterpret_cast<float*>(to) = v;
+            else
+              *reinterpret_cast<__nv_bfloat16*>(to) = __float2bfloat16_rn(v);
+          }
+          const bool next = --left == 0;
+          to += next ? jump : static_cast<int64_t>(D) * esize;
+          if (next) left = group;
+        }
         __syncwarp();
         if (lane == 0) mbar_arrive(l_empty);
-        if ((flags & 1) && threadIdx.x == kEpiWarp0 * 32) {
-          // the CTAs that share this sequence and head: to the one whose range holds its last tile
-          const int64_t last = whole ? 0 : unit + seq_of(p, b).tiles - 1;
-          int64_t cta = whole ? blockIdx.x : last * ctas / total;
-          while (!whole && total * (cta + 1) / ctas <= last) ++cta;
-          p.pieces[static_cast<int64_t>(b) * p.c.H + h] = make_int2(blockIdx.x, static_cast<int>(cta - blockIdx.x) + 1);
+        if (flags == 1 && threadIdx.x == kEpiWarp0 * 32) {
+          // goes on in the next CTAs, to the one whose range holds the last tile
+          const int64_t last = unit + seq_of(p, b).tiles - 1;
+          int64_t cta = last * ctas / total;
+          while (total * (cta + 1) / ctas <= last) ++cta;
+          p.shared[blockIdx.x] = make_int4(b, h, static_cast<int>(cta - blockIdx.x) + 1, 0);
         }
         unit += nt_seg;
     }
@@ -770,19 +802,20 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
   }
 }
 
-// Results of sequences and heads that several CTAs share: a block per sequence and head, a thread per feature and every fourth row.
+// Results of sequences and heads that several CTAs share: blocks for each CTA that one begins in, a row at a time; a thread per
+// feature and every fourth CTA.
 template <int D, int R>
 __global__ void __launch_bounds__(4 * D) attention_join_kernel(const P p) {
   __shared__ float s_w[kMaxCtas];
   __shared__ float s_l;
+  __shared__ float s_o[4][D];
   pdl_launch_dependents();
   pdl_wait();
-  const int b = blockIdx.x / p.c.H, h = blockIdx.x % p.c.H;
-  const Seq s = seq_of(p, b);
-  if (s.tiles == 0) return;
-  const int x = load_chained(reinterpret_cast<const int*>(p.pieces + blockIdx.x));
-  const int n = load_chained(reinterpret_cast<const int*>(p.pieces + blockIdx.x) + 1);
+  const int x = blockIdx.x;
+  const uint4 shared = load_chained(reinterpret_cast<const uint4*>(p.shared + x));
+  const int b = static_cast<int>(shared.x), h = static_cast<int>(shared.y), n = static_cast<int>(shared.z);
   if (n <= 1 || n > kMaxCtas) return;
+  const Seq s = seq_of(p, b);
   const int rows = s.n * p.G;
   constexpr int64_t kPart = R * (D + 2);
   // piece i: the first CTA's second place, the others' first
@@ -806,12 +839,11 @@ __global__ void __launch_bounds__(4 * D) attention_join_kernel(const P p) {
         s_l = l;
         const int64_t row = s.first + r / p.G;
         const int hq = h * p.G + r % p.G;
-        if (p.lse) p.lse[row * (static_cast<int64_t>(p.G) * p.c.H) + hq] = l == 0.0f ? -INFINITY : (log2f(l) + m - kShift) * (1.0f / kLog2e);
+        if (p.lse) p.lse[row * (static_cast<int64_t>(p.G) * p.c.H) + hq] = l == 0.0f ? -INFINITY : (log2f(l) + m + 8.0f - kShift) * (1.0f / kLog2e);
       }
     }
     __syncthreads();
     const int d = threadIdx.x % D, k = threadIdx.x / D;
-    __shared__ float s_o[4][D];
     float o = 0.0f;
 #pragma unroll 4
     for (int i = k; i < n; i += 4) o = fmaf(s_w[i], load_chained(part(i) + r * D + d), o);
@@ -837,8 +869,7 @@ int launch_cfg(const CUtensorMap& tm, const P& p, int grid, int max_rows, cudaSt
   cudaError_t e = launch_chained(attention_few_kernel<D, R, RS>, dim3(grid), dim3(kThreads), C::kSmemBytes, st, false, tm, p);
   count_launch();
   if (e != cudaSuccess) return ZQ_ERR_CUDA;
-  const int64_t blocks = static_cast<int64_t>(p.c.B) * p.c.H;
-  e = launch_chained(attention_join_kernel<D, R>, dim3(static_cast<unsigned>(blocks), max_rows), dim3(4 * D), 0, st, false, p);
+  e = launch_chained(attention_join_kernel<D, R>, dim3(grid, max_rows < 16 ? max_rows : 16), dim3(4 * D), 0, st, false, p);
   count_launch();
   return e == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
 }
@@ -853,14 +884,11 @@ int launch_rows(const CUtensorMap& tm, const P& p, int grid, int max_rows, cudaS
 
 }  // namespace
 
-// Sums of two pieces per CTA, and which CTAs share a sequence and head.
-size_t few_workspace_bytes(int64_t B, int64_t H, int64_t D) {
-  return (sizeof(float) * kMaxCtas * 2 * kFewRows * (D + 2) + 255) / 256 * 256 + (sizeof(int2) * B * H + 255) / 256 * 256;
-}
+// Sums of two pieces per CTA, and what goes on in the next one.
+size_t few_workspace_bytes(int64_t D) { return sizeof(float) * kMaxCtas * 2 * kFewRows * (D + 2) + sizeof(int4) * kMaxCtas; }
 
 // max_rows: no sequence and head of this kernel has more rows.
 int launch_attention_few(const AttnArgs& a, int max_rows, cudaStream_t st) {
-  if (static_cast<int64_t>(a.c.B) * a.c.H > 0x7FFFFFFF) return ZQ_ERR_SHAPE;
   P p{};
   p.c = a.c;
   p.q = static_cast<const __nv_bfloat16*>(a.q), p.ldq = a.ldq, p.G = a.Hq / a.c.H;
@@ -869,8 +897,8 @@ int launch_attention_few(const AttnArgs& a, int max_rows, cudaStream_t st) {
   p.out = a.out, p.f32 = a.dt == ZQ_OUT_F32, p.ldo = a.ldo, p.lse = a.lse;
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   p.status = reinterpret_cast<int*>(ws);
-  p.partial = reinterpret_cast<float*>(ws + kWsHeadBytes);
-  p.pieces = reinterpret_cast<int2*>(ws + kWsHeadBytes + (sizeof(float) * kMaxCtas * 2 * kFewRows * (a.c.D + 2) + 255) / 256 * 256);
+  p.shared = reinterpret_cast<int4*>(ws + kWsHeadBytes);
+  p.partial = reinterpret_cast<float*>(p.shared + kMaxCtas);
   CUtensorMap tm;
   if (!make_page_map(&tm, a.c)) return ZQ_ERR_CUDA;
   const int sms = sm_count(), grid = sms < kMaxCtas ? sms : kMaxCtas;

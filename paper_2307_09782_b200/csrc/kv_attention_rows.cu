@@ -492,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
         }
         for (int j0 = 0; j0 < g.nt && ok; j0 += 4) {
           const int64_t token = (static_cast<int64_t>(g.tile0) + j0) * kTok + lane * 16;
-          const float4 e = scale_entry(p.c, b, g.h, static_cast<int>(min(token, static_cast<int64_t>(s.L))), s.L);
+          const float4 e = scale_entry(load_scales(p.c, b, g.h, token, s.L));
           for (int j = 0; j < 4 && j0 + j < g.nt; ++j, ++tiles) {
             const int slot = tiles % kScaleSlots;
             if (tiles >= kScaleSlots && !mbar_wait_warp(&e_empty[slot], (tiles / kScaleSlots - 1) & 1, s_abort)) {
@@ -662,7 +662,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
         to_part[kRows * D + r] = l;
         to_part[kRows * D + kRows + r] = m;
       } else if (mine && p.lse) {
-        p.lse[t * (static_cast<int64_t>(p.G) * p.c.H) + hq] = l == 0.0f ? -INFINITY : (log2f(l) + m - kShift) * (1.0f / kLog2e);
+        p.lse[t * (static_cast<int64_t>(p.G) * p.c.H) + hq] = l == 0.0f ? -INFINITY : (log2f(l) + m + 8.0f - kShift) * (1.0f / kLog2e);
       }
       if (nt > 0) {
         const float f = part >= 0 ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);
@@ -672,7 +672,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
           tmem_ld16(to + d, o);
           tmem_ld_wait_regs<16>(o);
 #pragma unroll
-          for (int k = 0; k < 16; ++k) o[k] *= f;
+          for (int k = 0; k < 16; k += 4) {  // features in their places again (see feature_at)
+            const float x = o[k + 1] * f;
+            o[k] *= f;
+            o[k + 1] = o[k + 2] * f;
+            o[k + 2] = x;
+            o[k + 3] *= f;
+          }
           if (part >= 0) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) *reinterpret_cast<float4*>(to_part + r * D + d + 4 * k) = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
@@ -764,7 +770,7 @@ __global__ void __launch_bounds__(256) attention_join_rows_kernel(const P p, int
     else
       static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
   }
-  if (p.lse && lane == 0) p.lse[t * (static_cast<int64_t>(p.G) * p.c.H) + hq] = l == 0.0f ? -INFINITY : (log2f(l) + m - kShift) * (1.0f / kLog2e);
+  if (p.lse && lane == 0) p.lse[t * (static_cast<int64_t>(p.G) * p.c.H) + hq] = l == 0.0f ? -INFINITY : (log2f(l) + m + 8.0f - kShift) * (1.0f / kLog2e);
 }
 
 template <int D>

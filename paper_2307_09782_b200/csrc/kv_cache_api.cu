@@ -145,7 +145,7 @@ int zq_kv_cache_read(const uint8_t* codes, const float* scale, int64_t pages, in
 
 size_t zq_kv_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D) {
   if (T < 0 || B < 0 || T > kMaxRows || B > kMaxRows || H < 1 || H > kMaxHeads || Hq < H || Hq > kMaxHeads || Hq % H || !dim_ok(D)) return 0;
-  const size_t few = few_workspace_bytes(B, H, D), rows = rows_workspace_bytes(D);
+  const size_t few = few_workspace_bytes(D), rows = rows_workspace_bytes(D);
   return kWsHeadBytes + (few > rows ? few : rows);
 }
 
