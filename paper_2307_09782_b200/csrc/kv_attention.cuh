@@ -39,6 +39,47 @@ template <int D>
 __device__ __forceinline__ uint32_t row_piece(int row, int piece) {
   return row * D + ((piece ^ (D == 128 ? row & 7 : (row >> 1) & 3)) << 4);
 }
+// 8-bit operand with the tokens in K: a token's ROW bytes (features, or columns) side by side, 32, 64 or 128 bytes swizzled as rows of
+// that size are, 8 tokens per atom; more than 128 bytes in parts of 128, each of all 128 tokens.  (Where M wants more features than
+// there are, 128 of 64, it gets them twice.)
+template <int ROW>
+__device__ __forceinline__ uint64_t desc_tokens(uint32_t smem_addr) {
+  constexpr int kRow = ROW < 128 ? ROW : 128;
+  uint64_t d = 0;
+  d |= uint64_t((smem_addr >> 4) & 0x3FFF);
+  d |= uint64_t(ROW > 128 ? (kTok * 128) >> 4 : 0) << 16;  // the next 128 bytes
+  d |= uint64_t((8 * kRow) >> 4) << 32;                    // the next 8 tokens
+  d |= uint64_t(1) << 46;
+  d |= uint64_t(kRow == 128 ? 2 : kRow == 64 ? 4 : 6) << 61;
+  return d;
+}
+// Byte of 16-byte piece `piece` of a token in such an operand.
+template <int ROW>
+__device__ __forceinline__ uint32_t token_piece(int token, int piece) {
+  constexpr int kRow = ROW < 128 ? ROW : 128, kPieces = kRow / 16;
+  const int sw = kRow == 128 ? token & 7 : kRow == 64 ? (token >> 1) & 3 : (token >> 2) & 1;
+  return (piece / kPieces) * (kTok * 128) + token * kRow + (((piece % kPieces) ^ sw) << 4);
+}
+// E4M3 x E4M3 -> FP32 with the tokens in K on both sides, D is 128 x n
+__device__ __forceinline__ uint32_t idesc_e4m3_mn(uint32_t n) {
+  return (1u << 4) | (1u << 15) | (1u << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+// Two FP16 numbers up to 256 -> two E4M3 numbers, three times: w = t0 + t1 / 16 + t2 / 256, each the rest of the one before.
+__device__ __forceinline__ void split3(uint32_t w, uint32_t* t) {
+  asm("{\n\t.reg .b16 a, b, c;\n\t.reg .b32 x, r;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 a, %3;\n\t"
+      "cvt.rn.f16x2.e4m3x2 x, a;\n\t"
+      "sub.f16x2 r, %3, x;\n\t"
+      "mul.f16x2 r, r, %4;\n\t"  // exact: a rest has 8 bits at the most
+      "cvt.rn.satfinite.e4m3x2.f16x2 b, r;\n\t"
+      "cvt.rn.f16x2.e4m3x2 x, b;\n\t"
+      "sub.f16x2 r, r, x;\n\t"
+      "mul.f16x2 r, r, %4;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 c, r;\n\t"
+      "cvt.u32.u16 %0, a;\n\tcvt.u32.u16 %1, b;\n\tcvt.u32.u16 %2, c;\n\t}"
+      : "=r"(t[0]), "=r"(t[1]), "=r"(t[2])
+      : "r"(w), "r"(0x4C004C00u));
+}
 // FP16 values [128 tokens][64 features] (128 bytes a token, 128-byte swizzle), the features of M or N, the tokens of K; the next 64
 // features 16 KB further.
 __device__ __forceinline__ uint64_t desc_values(uint32_t smem_addr) {

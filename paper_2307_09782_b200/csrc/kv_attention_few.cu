@@ -1,11 +1,14 @@
 // Attention over the 8-bit cache where a sequence and cache head have few rows (new tokens x query heads of the head, up to 64):
 // decoding.  Bound by the codes, which are read once.
 //
-// The codes go from memory to the tensor core as they are on the key side, and widened to FP16 in shared memory on the value side:
-//   S^T [128 tokens, rows] = K [tokens, D] q^T      E4M3 x E4M3; q is a sum of two E4M3 numbers, side by side in the columns
-//   O^T [D, rows] += V^T [D, tokens] P^T            FP16 x FP16
-// Tokens and features are the tensor core's 128 lanes, the rows its columns, so few rows cost little: a tile's products take
-// 150 - 300 cycles, its codes come in about 1400 (32 KB at a 148th of the copy bandwidth).
+// Keys' and values' codes go from memory to the tensor core as they are; what meets them is written as sums of E4M3 numbers, side
+// by side in the columns:
+//   S^T [128 tokens, 2 x rows] = K [tokens, D] q^T      q = q1 + q2, exact for bf16 features down to 2^-17 of the row's largest
+//   O^T [D, 3 x rows] += V^T [D, tokens] P^T            P = P1 + P2 / 2^4 + P3 / 2^8, each the rest of the one before, with
+//                                                       accumulators of its own: 12 bits, and something down to 2^-26 of the largest
+// Tokens and features are the tensor core's 128 lanes, the rows its columns: more columns for more terms cost little.  (With the
+// values widened to FP16 in shared memory and P in FP16 a tile of 32 KB moved 132 KB through shared memory, which takes 1050 of
+// the 1370 cycles that its bytes take from memory, a 148th of the copy bandwidth: 64 sequences of up to 8192 tokens took 143 us.)
 //
 // Work: the (sequence, head, tile of 128 tokens) triples of the batch are dealt out evenly, as one contiguous range per CTA; the
 // lengths are on the device, so each CTA finds its range itself.  A range is walked in segments (one per sequence and head), a
@@ -14,17 +17,17 @@
 // Where several CTAs share a sequence and head, each leaves its sums, maximum and results in the workspace;
 // attention_join_kernel adds them up in the order of the tiles.
 //
-// Warp roles: 0..7 softmax (thread = token), 8..11 queries and epilogue (thread = feature), 12..15 converters of values, 16 keys'
-// copies, 17 values' copies, 18 MMAs, 19 the walk over the segments and the block scales.
+// Warp roles: 0..7 softmax (thread = token), 8..11 queries and epilogue (thread = feature), 12 keys' copies, 13 values' copies,
+// 14 MMAs, 15 the walk over the segments and the block scales.
 #include "kv_attention.cuh"
 
 namespace zq {
 namespace kv {
 namespace {
 
-constexpr int kSoftmaxWarps = 8, kEpiWarp0 = 8, kConvWarp0 = 12, kKeyWarp = 16, kValueWarp = 17, kMmaWarp = 18, kWalkWarp = 19;
-constexpr int kThreads = 20 * 32;
-enum { kErrKeysA = 51, kErrValuesA = 52, kErrMmaA = 53, kErrWalkA = 54, kErrQueriesA = 55, kErrSoftmaxA = 56, kErrConvertA = 57, kErrEpilogueA = 58, kErrAlignA = 59 };
+constexpr int kSoftmaxWarps = 8, kEpiWarp0 = 8, kKeyWarp = 12, kValueWarp = 13, kMmaWarp = 14, kWalkWarp = 15;
+constexpr int kThreads = 16 * 32;
+enum { kErrKeysA = 51, kErrValuesA = 52, kErrMmaA = 53, kErrWalkA = 54, kErrQueriesA = 55, kErrSoftmaxA = 56, kErrEpilogueA = 58, kErrAlignA = 59 };
 
 struct P {
   Cache c;
@@ -37,7 +40,7 @@ struct P {
   int64_t ldo;
   int f32;
   float* lse;
-  float* partial;    // [CTAs][2][R (D + 2)]
+  float* partial;    // [CTAs][2][RS (D + 2)]
   int4* shared;      // [CTAs] what begins in the CTA and goes on in the next: sequence, head, CTAs (0: nothing does)
   int* status;
 };
@@ -52,34 +55,38 @@ struct alignas(16) Seg {
 };
 constexpr int kSegs = 4;
 
-// Registers per thread behind the set-up: softmax 120 (two warpgroups), epilogue 96 as launched, converters 64, the others 80;
-// 2 x 120 + 96 + 64 + 80 = 480, the five warpgroups' 5 x 96 at launch.
-
-template <int D, int R>
+// RS: rows that are worked on, at least those there are (the rest are computed from whatever lies there and not looked at: a jump
+// past them costs more, in instructions fetched anew).
+template <int D, int RS>
 struct Cfg {
-  static constexpr int kTiles = 64 / R;               // tiles of a chunk
+  static constexpr int kScoreCols = RS < 8 ? 16 : 2 * RS;                       // two terms of q (16 columns at the least)
+  static constexpr int kProbCols = RS == 4 ? 16 : RS == 8 ? 32 : 3 * RS;        // three terms of P (multiples of 16)
+  static constexpr int kProbRow = RS <= 8 ? 32 : RS == 16 ? 64 : RS == 32 ? 128 : 256;  // bytes of a token's probabilities
+  static constexpr int kTiles = 128 / kScoreCols;                               // tiles of a chunk
+  static constexpr int kOutBufs = RS == 64 ? 1 : 2;                             // accumulators: 512 columns, 256 of them scores
   static constexpr int kTileBytes = kTok * D;
-  static constexpr int kValueBytes = kTok * D * 2;    // widened
-  static constexpr int kProbBytes = kTok * R * 2;     // of a tile
-  static constexpr int kOffValues = 0;                // [2]
-  static constexpr int kOffProbs = kOffValues + 2 * kValueBytes;                // [2][kTiles]
-  static constexpr int kOffQueries = kOffProbs + 2 * kTiles * kProbBytes;       // [2][2 R rows of D]
-  static constexpr int kOffScales = kOffQueries + 2 * 2 * R * D;                // [2][kTiles][8] float4
-  static constexpr int kOffRows = kOffScales + 2 * kTiles * 8 * 16;             // [2][R] int4: factor, first and last token + 1 seen
-  static constexpr int kOffMax = kOffRows + 2 * R * 16;                         // [2][R] maximum, [2][R] factor of what came before
-  static constexpr int kOffRed = kOffMax + 4 * R * 4;                           // [R][8] warps' maxima
-  static constexpr int kOffSum = kOffRed + R * 8 * 4;                           // [R][8] warps' sums, [R] maxima
-  static constexpr int kOffSegs = kOffSum + R * 9 * 4;                          // [kSegs]
-  static constexpr int kOffBars = kOffSegs + kSegs * 32;
-  static constexpr int kFixed = (kOffBars + 64 * 8 + 36 * 8 + 1023) / 1024 * 1024;
+  static constexpr int kProbBytes = kTok * kProbRow;                            // of a tile
+  static constexpr int kOffProbs = 0;                                           // [2][kTiles]
+  static constexpr int kOffQueries = kOffProbs + 2 * kTiles * kProbBytes;       // [2][kScoreCols rows of D]
+  static constexpr int kOffScales = kOffQueries + 2 * kScoreCols * D;           // [2][kTiles][8] float4
+  static constexpr int kOffRows = kOffScales + 2 * kTiles * 8 * 16;             // [2][RS] int4: factor, first and last token + 1 seen
+  static constexpr int kOffMax = kOffRows + 2 * RS * 16;                        // [2][RS] maximum, [2][RS] factor of what came before
+  static constexpr int kOffRed = kOffMax + 4 * RS * 4;                          // [RS][8] warps' maxima
+  static constexpr int kOffSum = kOffRed + RS * 8 * 4;                          // [RS][8] warps' sums, [RS] maxima
+  static constexpr int kOffSegs = kOffSum + RS * 9 * 4;                         // [kSegs]
+  static constexpr int kOffMiss = kOffSegs + kSegs * 32;                        // [value slots] pages that were not copied
+  static constexpr int kOffBars = kOffMiss + 64;
+  static constexpr int kMaxBars = 72;
+  static constexpr int kFixed = (kOffBars + kMaxBars * 8 + 36 * 8 + 1023) / 1024 * 1024;
   static constexpr int kSlots0 = (227 * 1024 - kFixed) / kTileBytes;
-  static constexpr int kSlots = kSlots0 < 16 ? kSlots0 : 16;
+  static constexpr int kSlots = kSlots0 < 18 ? kSlots0 : 18;
   static constexpr int kKeySlots = (kSlots + 1) / 2, kValueSlots = kSlots / 2;
   static constexpr int kOffKeys = kFixed;
   static constexpr int kOffCodes = kOffKeys + kKeySlots * kTileBytes;
   static constexpr int kSmemBytes = kOffCodes + kValueSlots * kTileBytes;
-  static constexpr int kNumBars = 2 * kKeySlots + 2 * kValueSlots + 4 + 14 + 5 + 2 * kSegs;
-  static_assert(kSmemBytes <= 227 * 1024 && kNumBars <= 64 && kSlots >= 4, "shared memory");
+  static constexpr int kNumBars = 2 * kKeySlots + 2 * kValueSlots + 14 + 5 + 2 * kSegs;
+  static_assert(kSmemBytes <= 227 * 1024 && kNumBars <= kMaxBars && kSlots >= 4 && kValueSlots <= 16, "shared memory");
+  static_assert(256 + kOutBufs * kProbCols <= 512, "tensor memory");
 };
 
 // A sequence's part in this kernel: its rows and tiles (none where it has too many rows, or none).
@@ -152,21 +159,17 @@ struct Ring {
   }
 };
 
-// R: columns of the tensor core for the rows (16, 32, 64); RS: rows that are worked on, at least those there are (the rest of the RS
-// are computed from whatever lies there and not looked at: a jump past them costs more, in instructions fetched anew).
-template <int D, int R, int RS>
+template <int D, int RS>
 __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid_constant__ CUtensorMap tm, const P p) {
-  using C = Cfg<D, R>;
+  using C = Cfg<D, RS>;
   constexpr int kTiles = C::kTiles;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bar = reinterpret_cast<uint64_t*>(smem + C::kOffBars);
   uint64_t* k_full = bar;                            // [key slots] a tile's keys have landed                  (MMA)
   uint64_t* k_empty = k_full + C::kKeySlots;         // their products are done                                (keys' copies)
-  uint64_t* v_full = k_empty + C::kKeySlots;         // [value slots] a tile's values have landed              (converters)
-  uint64_t* v_empty = v_full + C::kValueSlots;       // they are widened                                       (values' copies)
-  uint64_t* w_full = v_empty + C::kValueSlots;       // [2] widened values                                     (MMA)
-  uint64_t* w_empty = w_full + 2;                    // [2] their products are done                            (converters)
-  uint64_t* s_full = w_empty + 2;                    // [2] scores of a chunk                                  (softmax)
+  uint64_t* v_full = k_empty + C::kKeySlots;         // [value slots] a tile's values have landed              (MMA)
+  uint64_t* v_empty = v_full + C::kValueSlots;       // their products are done                                (values' copies)
+  uint64_t* s_full = v_empty + C::kValueSlots;                  // [2] scores of a chunk                                  (softmax)
   uint64_t* s_empty = s_full + 2;                    // [2] they have been used, with the scales               (MMA, walk)
   uint64_t* e_full = s_empty + 2;                    // [2] block scales of a chunk                            (softmax)
   uint64_t* p_full = e_full + 2;                     // [2] probabilities and row factors of a chunk           (MMA, epilogue)
@@ -181,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
   uint64_t* g_empty = g_full + kSegs;                // [kSegs] everybody is through with it                   (walk)
   uint64_t* drain = g_empty + kSegs;
   const Seg* s_seg = reinterpret_cast<const Seg*>(smem + C::kOffSegs);
-  int64_t* s_range = reinterpret_cast<int64_t*>(smem + C::kOffBars + 64 * 8);  // units, first sequence, first unit in it
+  int64_t* s_range = reinterpret_cast<int64_t*>(smem + C::kOffBars + C::kMaxBars * 8);  // units, first sequence, first unit in it
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_range + 3);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
   int64_t* s_scan = s_range + 4;  // [32]
@@ -194,11 +197,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     }
     for (int i = 0; i < C::kValueSlots; ++i) {
       mbar_init(&v_full[i], 1);
-      mbar_init(&v_empty[i], 4);
+      mbar_init(&v_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&w_full[i], 4);
-      mbar_init(&w_empty[i], 1);
       mbar_init(&s_full[i], 1);
       mbar_init(&s_empty[i], kSoftmaxWarps);
       mbar_init(&e_full[i], 1);
@@ -210,7 +211,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     }
     mbar_init(l_full, kSoftmaxWarps);
     mbar_init(l_empty, 4);
-    mbar_init(&meet[0], R == 64 ? 4 : 8);
+    mbar_init(&meet[0], RS == 64 ? 4 : 8);
     mbar_init(&meet[1], 4);
     for (int i = 0; i < kSegs; ++i) {
       mbar_init(&g_full[i], 1);
@@ -279,12 +280,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
 
   if (warp == kKeyWarp || warp == kValueWarp) {
     // ---- copies: a lane per page of the tile
-    fp8b::regs_give<80>();
     const bool keys = warp == kKeyWarp;
     const int slots = keys ? C::kKeySlots : C::kValueSlots;
     uint64_t *full = keys ? k_full : v_full, *empty = keys ? k_empty : v_empty;
     uint8_t* to = smem + (keys ? C::kOffKeys : C::kOffCodes);
     const int per = kTok / p.c.page, page_bytes = p.c.page * D;
+    uint32_t* miss = reinterpret_cast<uint32_t*>(smem + C::kOffMiss);
     Ring r;
     int issued = 0, nt;
     bool ok = any;
@@ -303,16 +304,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           break;
         }
         const bool has = lane < per && page >= 0;
-        const uint32_t n = __popc(__ballot_sync(0xFFFFFFFFu, has));
-        if (lane == 0) mbar_arrive_expect_tx(&full[r.i], n * page_bytes);
+        const uint32_t n = __ballot_sync(0xFFFFFFFFu, has);
+        if (lane == 0) {
+          if (!keys) miss[r.i] = ~n & ((1u << per) - 1u);
+          mbar_arrive_expect_tx(&full[r.i], __popc(n) * page_bytes);
+        }
         __syncwarp();
         if (has) {
           uint8_t* dst = to + r.i * C::kTileBytes + lane * page_bytes;
           const int64_t block = block_at(p.c, page, keys ? 0 : 1, h);
-          if (keys)
-            tma_load_3d(dst, &tm, 0, 0, static_cast<int>(block), &full[r.i]);
-          else
-            bulk_load(dst, p.c.codes + block * page_bytes, page_bytes, &full[r.i]);
+          tma_load_3d(dst, &tm, 0, 0, static_cast<int>(block), &full[r.i]);
         }
         __syncwarp();
         ++issued;
@@ -326,39 +327,53 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
       }
     }
   } else if (warp == kMmaWarp) {
-    fp8b::regs_give<80>();
     const bool issuer = elect_one();
     const uint64_t kdesc = desc_rows<D>(smem_u32(smem + C::kOffKeys)), qdesc = desc_rows<D>(smem_u32(smem + C::kOffQueries));
-    const uint64_t vdesc = desc_values(smem_u32(smem + C::kOffValues));
-    const uint64_t pdesc = umma_desc_k128(smem_u32(smem + C::kOffProbs));
-    const uint32_t sdesc_i = umma_idesc_e4m3(2 * R), odesc_i = idesc_f16(R, true, false);
+    const uint64_t vdesc = desc_tokens<D>(smem_u32(smem + C::kOffCodes)), pdesc = desc_tokens<C::kProbRow>(smem_u32(smem + C::kOffProbs));
+    const uint32_t sdesc_i = umma_idesc_e4m3(C::kScoreCols), odesc_i = idesc_e4m3_mn(C::kProbCols);
+    const uint32_t* miss = reinterpret_cast<const uint32_t*>(smem + C::kOffMiss);
     Ring k, v;
     bool failed = false;
     int chunk = 0, seg = 0;
-    // results of chunk `c` of nt tiles
-    auto results = [&](int c, int nt) {
-      const int cb = c & 1;
-      if (!mbar_wait(&p_full[cb], (c >> 1) & 1, s_abort) || (c >= 2 && !mbar_wait(&o_empty[cb], ((c >> 1) - 1) & 1, s_abort))) return false;
-      for (int j = 0; j < nt; ++j) {
-        if (!mbar_wait(&w_full[v.i], v.phase, s_abort)) return false;
+    // results of chunk `c` of nt tiles, with `left` tokens from the first on
+    auto results = [&](int c, int nt, int64_t left) {
+      const int cb = c & 1, ob = C::kOutBufs == 2 ? cb : 0, before = c - C::kOutBufs;  // the chunk that had these columns before
+      if (!mbar_wait(&p_full[cb], (c >> 1) & 1, s_abort) || (before >= 0 && !mbar_wait(&o_empty[before & 1], (before >> 1) & 1, s_abort))) return false;
+      for (int j = 0; j < nt; ++j, left -= kTok) {
+        if (!mbar_wait(&v_full[v.i], v.phase, s_abort)) return false;
+        const uint32_t gone = miss[v.i];
+        if (gone != 0u || left < kTok) {
+          // what lies behind the last token, or in pages that were not copied, must not turn into NaN by a product with zero
+          uint8_t* at = smem + C::kOffCodes + v.i * C::kTileBytes;
+          for (int i = lane; i < kTok * D / 16; i += 32) {
+            const int row = i / (D / 16);
+            if (row >= left || (gone >> (row / p.c.page) & 1u)) *reinterpret_cast<uint4*>(at + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
         tc_fence_after_sync();
         if (issuer) {
-          const uint64_t ad = vdesc + static_cast<uint64_t>((v.i * C::kValueBytes) >> 4);
+          const uint64_t ad = vdesc + static_cast<uint64_t>((v.i * C::kTileBytes) >> 4);
           const uint64_t bd = pdesc + static_cast<uint64_t>(((cb * kTiles + j) * C::kProbBytes) >> 4);
+          constexpr int kRow = C::kProbRow < 128 ? C::kProbRow : 128;  // (256: two halves of 128 bytes)
 #pragma unroll
-          for (int s = 0; s < kTok / 16; ++s)
-            umma_f16(tmem + 256 + cb * R, ad + s * (2048 >> 4), bd + (s >> 2) * ((R * 128) >> 4) + (s & 3) * 2, odesc_i, (j > 0 || s > 0) ? 1u : 0u);
-          umma_commit(&w_empty[v.i]);
+          for (int s = 0; s < kTok / 32; ++s)  // 32 tokens further
+            umma_f8(tmem + 256 + ob * C::kProbCols, ad + s * ((32 * D) >> 4), bd + s * ((32 * kRow) >> 4), odesc_i, (j > 0 || s > 0) ? 1u : 0u);
+          umma_commit(&v_empty[v.i]);
           if (j + 1 == nt) umma_commit(&o_full[cb]);
         }
         __syncwarp();
-        v.step(2);
+        v.step(C::kValueSlots);
       }
       return true;
     };
+    int64_t last_left = 0;
     int last_nt = 0;  // tiles of the chunk whose scores are issued and whose results are not
     int nt_seg;
     for (; any && !failed && segment(seg, nt_seg); ++seg) {
+      const int64_t left = s_seg[seg % kSegs].L - static_cast<int64_t>(s_seg[seg % kSegs].tile0) * kTok;
+      __syncwarp();
       done_with(seg);
       if (!mbar_wait(&q_full[seg & 1], (seg >> 1) & 1, s_abort)) failed = true;
       for (int t = 0; t < nt_seg && !failed; t += kTiles, ++chunk) {
@@ -372,9 +387,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           tc_fence_after_sync();
           if (issuer) {
             const uint64_t ad = kdesc + static_cast<uint64_t>((k.i * C::kTileBytes) >> 4);
-            const uint64_t bd = qdesc + static_cast<uint64_t>(((seg & 1) * 2 * R * D) >> 4);
+            const uint64_t bd = qdesc + static_cast<uint64_t>(((seg & 1) * C::kScoreCols * D) >> 4);
 #pragma unroll
-            for (int s = 0; s < D / 32; ++s) umma_f8(tmem + cb * 128 + j * 2 * R, ad + s * 2, bd + s * 2, sdesc_i, s > 0 ? 1u : 0u);
+            for (int s = 0; s < D / 32; ++s) umma_f8(tmem + cb * 128 + j * C::kScoreCols, ad + s * 2, bd + s * 2, sdesc_i, s > 0 ? 1u : 0u);
             umma_commit(&k_empty[k.i]);
             if (j + 1 == nt) umma_commit(&s_full[cb]);
             if (t + j + 1 == nt_seg) umma_commit(&q_empty[seg & 1]);
@@ -382,11 +397,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           __syncwarp();
           k.step(C::kKeySlots);
         }
-        if (!failed && chunk > 0 && !results(chunk - 1, last_nt)) failed = true;
+        if (!failed && chunk > 0 && !results(chunk - 1, last_nt, last_left)) failed = true;
         last_nt = nt;
+        last_left = left - static_cast<int64_t>(t) * kTok;
       }
     }
-    if (!failed && chunk > 0 && !results(chunk - 1, last_nt)) failed = true;
+    if (!failed && chunk > 0 && !results(chunk - 1, last_nt, last_left)) failed = true;
     if (failed && issuer) fp8b::raise_error8(p.status, s_abort, kErrMmaA);
     // tensor memory is released only when every MMA has completed, also where another role has given up
     if (issuer) umma_commit(drain);
@@ -396,7 +412,6 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     __syncwarp();
   } else if (warp == kWalkWarp) {
     // ---- the walk: segments, and their chunks' block scales (a lane per 16 tokens), which are on their way one chunk ahead
-    fp8b::regs_give<80>();
     float4* table = reinterpret_cast<float4*>(smem + C::kOffScales);
     int seg = 0, chunk = 0;
     Walk w;  // of the segment announced last
@@ -418,72 +433,50 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
       ++seg;
       return true;
     };
+    constexpr int kMany = (kTiles * 8 + 31) / 32;
+    RawScales next[kMany];
     auto load = [&](int b, int h, int tile, int L) {
-      return load_scales(p.c, b, h, lane < kTiles * 8 ? static_cast<int64_t>(tile) * kTok + lane * 16 : L, L);
+#pragma unroll
+      for (int i = 0; i < kMany; ++i)
+        next[i] = load_scales(p.c, b, h, lane < kTiles * 8 ? static_cast<int64_t>(tile) * kTok + (i * 32 + lane) * 16 : L, L);
     };
     if (ok) {
       ok = announce();
-      RawScales next = load(w.b, w.h, w.s.tile0 + w.t, w.s.L);
+      load(w.b, w.h, w.s.tile0 + w.t, w.s.L);
       while (ok && more) {
         const int b = w.b, h = w.h, L = w.s.L, nt = w.nt, tile0 = w.s.tile0 + w.t;
         more = w.next(p);
         ok = announce();
         for (int t = 0; ok && t < nt; t += kTiles, ++chunk) {
           const int cb = chunk & 1;
-          const float4 e = scale_entry(next);
+          float4 e[kMany];
+#pragma unroll
+          for (int i = 0; i < kMany; ++i) e[i] = scale_entry(next[i]);
           if (t + kTiles < nt)
-            next = load(b, h, tile0 + t + kTiles, L);
+            load(b, h, tile0 + t + kTiles, L);
           else if (more)
-            next = load(w.b, w.h, w.s.tile0 + w.t, w.s.L);
+            load(w.b, w.h, w.s.tile0 + w.t, w.s.L);
           if (chunk >= 2 && !mbar_wait_warp(&s_empty[cb], ((chunk >> 1) - 1) & 1, s_abort)) ok = false;
           if (!ok) break;
-          if (lane < kTiles * 8) table[cb * kTiles * 8 + lane] = e;
+#pragma unroll
+          for (int i = 0; i < kMany; ++i)
+            if (lane < kTiles * 8) table[cb * kTiles * 8 + i * 32 + lane] = e[i];
           __syncwarp();
           if (lane == 0) mbar_arrive(&e_full[cb]);
         }
       }
       if (!ok && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrWalkA);
     }
-  } else if (warp >= kConvWarp0) {
-    fp8b::regs_give<64>();
-    const int i = threadIdx.x - kConvWarp0 * 32;
-    Ring v, o;
-    int n = 0, nt;
-    bool ok = any;
-    for (int seg = 0; ok && segment(seg, nt); ++seg) {
-      const Seg& g = s_seg[seg % kSegs];
-      const int64_t left0 = g.L - static_cast<int64_t>(g.tile0) * kTok;  // tokens from the first tile on
-      __syncwarp();
-      done_with(seg);
-      for (int j = 0; j < nt; ++j, ++n) {
-        if (!fp8b::mbar_wait_all(&v_full[v.i], v.phase, s_abort) || (n >= 2 && !fp8b::mbar_wait_all(&w_empty[o.i], o.phase ^ 1, s_abort))) {
-          if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrConvertA);
-          ok = false;
-          break;
-        }
-        widen_values<D, 128>(smem + C::kOffCodes + v.i * C::kTileBytes, smem + C::kOffValues + o.i * C::kValueBytes, i,
-                             static_cast<int>(min(left0 - static_cast<int64_t>(j) * kTok, static_cast<int64_t>(kTok))));
-        fence_proxy_async_smem();  // the tensor core reads what these stores wrote
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(&w_full[o.i]);
-          mbar_arrive(&v_empty[v.i]);
-        }
-        v.step(C::kValueSlots);
-        o.step(2);
-      }
-    }
   } else if (warp < kSoftmaxWarps) {
     // ---- softmax: thread = token of a tile.  Two groups of four warps take tiles in turn; with 64 rows (one tile per chunk)
     // they take half of its rows each.
-    fp8b::regs_take<120>();
-    constexpr bool kHalves = R == 64;
+    constexpr bool kHalves = RS == 64;
     constexpr int RR = kHalves ? 32 : RS;
     const int group = warp >> 2, r0 = kHalves ? group * 32 : 0;
     const int tok = (warp & 3) * 32 + lane;
     const int me = kHalves ? threadIdx.x & 127 : threadIdx.x;  // among those threads
     constexpr int S = RS < 8 ? RS : 8;        // rows at a time
-    constexpr int kMine = R == 16 ? 2 : 1;    // tiles of a chunk
+    constexpr int kMine = kTiles > 1 ? kTiles / 2 : 1;  // tiles of a chunk
     const int j0 = kHalves ? 0 : group, dj = 2;
     const int red_i = kHalves ? warp & 3 : warp;
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -504,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     for (; !failed && segment(seg, nt_seg); ++seg) {
         const Seg& g = s_seg[seg % kSegs];
         const int rows = min(max(g.n * p.G - r0, 0), RR), tile0 = g.tile0;
-        const float4* info = reinterpret_cast<const float4*>(smem + C::kOffRows) + (seg & 1) * R + r0;
+        const float4* info = reinterpret_cast<const float4*>(smem + C::kOffRows) + (seg & 1) * RS + r0;
         if (!fp8b::mbar_wait_all(&q_full[seg & 1], (seg >> 1) & 1, s_abort)) {
           failed = true;
           break;
@@ -539,12 +532,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
             const float4 e = table[(cb * kTiles + j) * 8 + (tok >> 4)];
             inv[k] = e.z;
             const int tile = (tile0 + t + j) * kTok;
-            const uint32_t from = tmem + lane_base + cb * 128 + j * 2 * R + r0;
+            const uint32_t from = tmem + lane_base + cb * 128 + j * C::kScoreCols + r0;
 #pragma unroll
             for (int r = 0; r < RR; r += S) {
               float y[S];
               load_scores<S>(from + r, x[k] + r);
-              load_scores<S>(from + R + r, y);
+              load_scores<S>(from + RS + r, y);
               tmem_ld_wait_regs<S>(x[k] + r);
               tmem_ld_wait_regs<S>(y);
 #pragma unroll
@@ -562,7 +555,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
 #pragma unroll
           for (int r = 0; r < RR; ++r) {
             float v = x[0][r];
-            if (kMine > 1) v = fmaxf(v, x[kMine - 1][r]);
+#pragma unroll
+            for (int k = 1; k < kMine; ++k) v = fmaxf(v, x[k][r]);
             v = warp_max(v);
             if (lane == 0) s_red[(r0 + r) * 8 + red_i] = v;
           }
@@ -578,30 +572,48 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
               m = fmaxf(m, fmaxf(fmaxf(b.x, b.y), fmaxf(b.z, b.w)));
             }
             const float safe = m == -INFINITY ? 0.0f : m;
-            s_max[cb * R + r0 + me] = kShift - safe;
-            s_max[2 * R + cb * R + r0 + me] = exp2f(m_run - safe);
+            s_max[cb * RS + r0 + me] = kShift - safe;
+            s_max[2 * RS + cb * RS + r0 + me] = exp2f(m_run - safe);
             m_run = m;
           }
           if (!meet_others()) failed = true;
           if (failed) break;
 #pragma unroll
-          for (int r = 0; r < RR; ++r) l[r] *= s_max[2 * R + cb * R + r0 + r];
+          for (int r = 0; r < RR; ++r) l[r] *= s_max[2 * RS + cb * RS + r0 + r];
 #pragma unroll
           for (int k = 0; k < kMine; ++k) {
             const int j = j0 + k * dj;
             if (j >= nt) break;
-            // the operand's rows: 64 tokens (128 bytes) each, the next 64 tokens R rows further
-            uint8_t* to = smem + C::kOffProbs + (cb * kTiles + j) * C::kProbBytes + (tok >> 6) * (R * 128) + (tok & 7) * 2;
-            const int piece = (tok & 63) >> 3;
+            // the token's row of the operand: the first terms of all rows, the second, the third (RS bytes each)
+            uint32_t term[3][RR / 4];
 #pragma unroll
-            for (int r = 0; r < RR; r += 2) {
-              const float2 m = *reinterpret_cast<const float2*>(s_max + cb * R + r0 + r);
-              const float a = fp8b::sfu_ex2(x[k][r] + m.x), b = fp8b::sfu_ex2(x[k][r + 1] + m.y);
-              l[r] = fmaf(a, inv[k], l[r]);
-              l[r + 1] = fmaf(b, inv[k], l[r + 1]);
-              const uint32_t h = pack_f16(a, b);
-              *reinterpret_cast<uint16_t*>(to + (r0 + r) * 128 + ((piece ^ (r & 7)) << 4)) = static_cast<uint16_t>(h);
-              *reinterpret_cast<uint16_t*>(to + (r0 + r + 1) * 128 + ((piece ^ ((r + 1) & 7)) << 4)) = static_cast<uint16_t>(h >> 16);
+            for (int r = 0; r < RR; r += 4) {
+              const float4 m = *reinterpret_cast<const float4*>(s_max + cb * RS + r0 + r);
+              const float w0 = fp8b::sfu_ex2(x[k][r] + m.x), w1 = fp8b::sfu_ex2(x[k][r + 1] + m.y);
+              const float w2 = fp8b::sfu_ex2(x[k][r + 2] + m.z), w3 = fp8b::sfu_ex2(x[k][r + 3] + m.w);
+              l[r] = fmaf(w0, inv[k], l[r]);
+              l[r + 1] = fmaf(w1, inv[k], l[r + 1]);
+              l[r + 2] = fmaf(w2, inv[k], l[r + 2]);
+              l[r + 3] = fmaf(w3, inv[k], l[r + 3]);
+              uint32_t a[3], b[3];
+              split3(pack_f16(w0, w1), a);
+              split3(pack_f16(w2, w3), b);
+#pragma unroll
+              for (int i = 0; i < 3; ++i) term[i][r / 4] = a[i] | (b[i] << 16);
+            }
+            uint8_t* to = smem + C::kOffProbs + (cb * kTiles + j) * C::kProbBytes;
+            if (RS == 4) {
+              *reinterpret_cast<uint4*>(to + token_piece<C::kProbRow>(tok, 0)) = make_uint4(term[0][0], term[1][0], term[2][0], 0u);
+            } else if (RS == 8) {
+              *reinterpret_cast<uint4*>(to + token_piece<C::kProbRow>(tok, 0)) = make_uint4(term[0][0], term[0][RR / 4 - 1], term[1][0], term[1][RR / 4 - 1]);
+              *reinterpret_cast<uint2*>(to + token_piece<C::kProbRow>(tok, 1)) = make_uint2(term[2][0], term[2][RR / 4 - 1]);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 3; ++i)
+#pragma unroll
+                for (int c = 0; c < RR / 16; ++c)
+                  *reinterpret_cast<uint4*>(to + token_piece<C::kProbRow>(tok, (i * RS + r0) / 16 + c)) =
+                      make_uint4(term[i][c * 4], term[i][c * 4 + 1], term[i][c * 4 + 2], term[i][c * 4 + 3]);
             }
           }
           fence_proxy_async_smem();
@@ -625,7 +637,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
           if (lane == 0) s_sum[(r0 + r) * 8 + red_i] = v;
         }
-        if (me < rows) s_sum[R * 8 + r0 + me] = m_run;
+        if (me < rows) s_sum[RS * 8 + r0 + me] = m_run;
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(l_full);
@@ -635,7 +647,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     if (failed && any && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrSoftmaxA);
   } else {
     // ---- epilogue: thread = feature
-    const int d = feature_at((warp & 3) * 32 + lane);
+    const int d = (warp & 3) * 32 + lane;
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const float* s_max = reinterpret_cast<const float*>(smem + C::kOffMax);
     const float* s_sum = reinterpret_cast<const float*>(smem + C::kOffSum);
@@ -650,8 +662,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     auto queries = [&](int sg) {
       const Seg& g = s_seg[sg % kSegs];
       const int rows = g.n * p.G, qb = sg & 1, i = threadIdx.x - kEpiWarp0 * 32;
-      uint8_t* to = smem + C::kOffQueries + qb * 2 * R * D;
-      int4* info = reinterpret_cast<int4*>(smem + C::kOffRows) + qb * R;
+      uint8_t* to = smem + C::kOffQueries + qb * C::kScoreCols * D;
+      int4* info = reinterpret_cast<int4*>(smem + C::kOffRows) + qb * RS;
       for (int r0 = 0; r0 < rows; r0 += kAtOnce * kBatch) {
         uint4 x[kBatch];
 #pragma unroll
@@ -674,7 +686,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           if (r < rows) {
             const int piece = (i % kLanes) >> 1, half = (i & 1) * 8;
             *reinterpret_cast<uint2*>(to + row_piece<D>(r, piece) + half) = first;
-            *reinterpret_cast<uint2*>(to + row_piece<D>(R + r, piece) + half) = second;
+            *reinterpret_cast<uint2*>(to + row_piece<D>(RS + r, piece) + half) = second;
             if (i % kLanes == 0) {
               const int64_t pos = static_cast<int64_t>(g.L) - g.n + r / p.G;
               const int64_t hi = p.causal ? min(pos + 1, static_cast<int64_t>(g.L)) : g.L;
@@ -717,11 +729,14 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           tc_fence_after_sync();
 #pragma unroll
           for (int r = 0; r < RS; r += S) {
-            float x[S];
-            load_scores<S>(tmem + lane_base + 256 + cb * R + r, x);
-            tmem_ld_wait_regs<S>(x);
+            float x[3][S];
 #pragma unroll
-            for (int i = 0; i < S; ++i) o[r + i] = fmaf(o[r + i], s_max[2 * R + cb * R + r + i], x[i]);
+            for (int i = 0; i < 3; ++i) load_scores<S>(tmem + lane_base + 256 + (C::kOutBufs == 2 ? cb : 0) * C::kProbCols + i * RS + r, x[i]);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) tmem_ld_wait_regs<S>(x[i]);
+#pragma unroll
+            for (int i = 0; i < S; ++i)
+              o[r + i] = fmaf(o[r + i], s_max[2 * RS + cb * RS + r + i], fmaf(x[2][i], 1.0f / 256.0f, fmaf(x[1][i], 1.0f / 16.0f, x[0][i])));
           }
           tc_fence_before_sync();
           __syncwarp();
@@ -733,7 +748,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
         }
         // each warp sums every row up for itself, a row per lane (and the 32nd after), and hands its factor round
         const bool whole = flags == 3;
-        float* part = p.partial + (static_cast<int64_t>(blockIdx.x) * 2 + (flags & 1)) * (R * (D + 2));
+        float* part = p.partial + (static_cast<int64_t>(blockIdx.x) * 2 + (flags & 1)) * (RS * (D + 2));
         float factor[(RS + 31) / 32];
 #pragma unroll
         for (int k = 0; k < (RS + 31) / 32; ++k) {
@@ -743,16 +758,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
             const float4* v = reinterpret_cast<const float4*>(s_sum + r * 8);
             const float4 x = v[0];
             float sum = ((x.x + x.y) + x.z) + x.w;
-            if (R != 64) {
+            if (RS != 64) {
               const float4 y = v[1];
               sum = (((sum + y.x) + y.y) + y.z) + y.w;
             }
-            const float m = s_sum[R * 8 + r];
-            if (whole) factor[k] = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const float m = s_sum[RS * 8 + r];
+            if (whole) factor[k] = sum == 0.0f ? 0.0f : kCodeUnit / sum;
             if (warp == kEpiWarp0) {
               if (!whole) {
-                part[R * D + r] = sum;
-                part[R * D + R + r] = m;
+                part[RS * D + r] = sum;
+                part[RS * D + RS + r] = m;
               } else if (p.lse) {
                 p.lse[(first + r / p.G) * (static_cast<int64_t>(p.G) * p.c.H) + h * p.G + r % p.G] =
                     sum == 0.0f ? -INFINITY : (log2f(sum) + m + 8.0f - kShift) * (1.0f / kLog2e);
@@ -804,7 +819,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
 
 // Results of sequences and heads that several CTAs share: blocks for each CTA that one begins in, a row at a time; a thread per
 // feature and every fourth CTA.
-template <int D, int R>
+template <int D, int RS>
 __global__ void __launch_bounds__(4 * D) attention_join_kernel(const P p) {
   __shared__ float s_w[kMaxCtas];
   __shared__ float s_l;
@@ -817,21 +832,21 @@ __global__ void __launch_bounds__(4 * D) attention_join_kernel(const P p) {
   if (n <= 1 || n > kMaxCtas) return;
   const Seq s = seq_of(p, b);
   const int rows = s.n * p.G;
-  constexpr int64_t kPart = R * (D + 2);
+  constexpr int64_t kPart = RS * (D + 2);
   // piece i: the first CTA's second place, the others' first
   auto part = [&](int i) { return p.partial + (static_cast<int64_t>(x + i) * 2 + (i == 0 ? 1 : 0)) * kPart; };
   for (int r = blockIdx.y; r < rows; r += gridDim.y) {
     __syncthreads();
     if (threadIdx.x < 32) {
       float m = -INFINITY;
-      for (int i = threadIdx.x; i < n; i += 32) m = fmaxf(m, load_chained(part(i) + R * D + R + r));
+      for (int i = threadIdx.x; i < n; i += 32) m = fmaxf(m, load_chained(part(i) + RS * D + RS + r));
       m = warp_max(m);
       float l = 0.0f;
       for (int i = threadIdx.x; i < n; i += 32) {
-        const float mi = load_chained(part(i) + R * D + R + r);
+        const float mi = load_chained(part(i) + RS * D + RS + r);
         const float f = mi == -INFINITY ? 0.0f : exp2f(mi - m);
         s_w[i] = f;
-        l = fmaf(f, load_chained(part(i) + R * D + r), l);
+        l = fmaf(f, load_chained(part(i) + RS * D + r), l);
       }
 #pragma unroll
       for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
@@ -851,7 +866,7 @@ __global__ void __launch_bounds__(4 * D) attention_join_kernel(const P p) {
     __syncthreads();
     if (k == 0) {
       o = s_o[0][d] + s_o[1][d] + s_o[2][d] + s_o[3][d];
-      const float v = s_l == 0.0f ? 0.0f : o / s_l;
+      const float v = s_l == 0.0f ? 0.0f : o * kCodeUnit / s_l;
       const int64_t at = (s.first + r / p.G) * p.ldo + (static_cast<int64_t>(h) * p.G + r % p.G) * D + d;
       if (p.f32)
         static_cast<float*>(p.out)[at] = v;
@@ -861,25 +876,25 @@ __global__ void __launch_bounds__(4 * D) attention_join_kernel(const P p) {
   }
 }
 
-template <int D, int R, int RS>
+template <int D, int RS>
 int launch_cfg(const CUtensorMap& tm, const P& p, int grid, int max_rows, cudaStream_t st) {
-  using C = Cfg<D, R>;
+  using C = Cfg<D, RS>;
   static DeviceOnce once;
-  if (!allow_shared_memory(once, attention_few_kernel<D, R, RS>, C::kSmemBytes)) return ZQ_ERR_CUDA;
-  cudaError_t e = launch_chained(attention_few_kernel<D, R, RS>, dim3(grid), dim3(kThreads), C::kSmemBytes, st, false, tm, p);
+  if (!allow_shared_memory(once, attention_few_kernel<D, RS>, C::kSmemBytes)) return ZQ_ERR_CUDA;
+  cudaError_t e = launch_chained(attention_few_kernel<D, RS>, dim3(grid), dim3(kThreads), C::kSmemBytes, st, false, tm, p);
   count_launch();
   if (e != cudaSuccess) return ZQ_ERR_CUDA;
-  e = launch_chained(attention_join_kernel<D, R>, dim3(grid, max_rows < 16 ? max_rows : 16), dim3(4 * D), 0, st, false, p);
+  e = launch_chained(attention_join_kernel<D, RS>, dim3(grid, max_rows < 16 ? max_rows : 16), dim3(4 * D), 0, st, false, p);
   count_launch();
   return e == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
 }
 template <int D>
 int launch_rows(const CUtensorMap& tm, const P& p, int grid, int max_rows, cudaStream_t st) {
-  if (max_rows <= 4) return launch_cfg<D, 16, 4>(tm, p, grid, max_rows, st);
-  if (max_rows <= 8) return launch_cfg<D, 16, 8>(tm, p, grid, max_rows, st);
-  if (max_rows <= 16) return launch_cfg<D, 16, 16>(tm, p, grid, max_rows, st);
-  if (max_rows <= 32) return launch_cfg<D, 32, 32>(tm, p, grid, max_rows, st);
-  return launch_cfg<D, 64, 64>(tm, p, grid, max_rows, st);
+  if (max_rows <= 4) return launch_cfg<D, 4>(tm, p, grid, max_rows, st);
+  if (max_rows <= 8) return launch_cfg<D, 8>(tm, p, grid, max_rows, st);
+  if (max_rows <= 16) return launch_cfg<D, 16>(tm, p, grid, max_rows, st);
+  if (max_rows <= 32) return launch_cfg<D, 32>(tm, p, grid, max_rows, st);
+  return launch_cfg<D, 64>(tm, p, grid, max_rows, st);
 }
 
 }  // namespace

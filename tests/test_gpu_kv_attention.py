@@ -5,9 +5,10 @@ Tolerances.  A result of type t is off by at most finfo(t).eps / 2 of its value 
 norms: FP32 sums of D squares and a few products, 2^-20 of the larger feature of a pair.
 attention: a probability is rounded to 11 bits (2^-11); FP32 scores are off by 2^-18 of sum |q| |k| at most (two tensor-core
 sums of 128 products that round towards zero, and the parts of q below 2^-17 of its row's largest), which counts twice, in the
-numerator and in the sum; the power of two and the sums of a few thousand terms add 2^-18.  FP16 ends: a probability times its
-value's scale is kept with the row's largest at 2^8 or more, in steps of 2^-24 at the least, so each is off by 2^-25 / 2^8 = 2^-33
-of the largest, which multiplies its code: 2^-33 (largest p scale) (sum of |codes|).  (That shows where the tokens with the large
+numerator and in the sum; the power of two and the sums of a few thousand terms add 2^-18.  Small ones end: a
+probability times its value's scale, with the row's largest at 2^8 or more, is held in steps of 2^-24 (FP16) where there are many
+rows, and as three E4M3 numbers, the third in steps of 2^-9 / 2^8, where there are few: it is off by 2^-18 / 2^8 = 2^-26 of the largest at
+most, which multiplies its code: 2^-26 (largest p scale) (sum of |codes|).  (That shows where the tokens with the large
 probabilities have a code of zero: with sm_scale = 1 one result in 150000 is 3e-11 beside others of 1.)
 """
 import math
@@ -248,7 +249,7 @@ ATTN_CASES = [
 
 def attn_tolerance(ref, bound, out):
     pv, qk, low = bound
-    return half_step(out) * ref.abs() + pv * (2.0 ** -11 + 2 * 2.0 ** -18 * qk[..., None] + 2.0 ** -17) + 2.0 ** -33 * low + 1e-30
+    return half_step(out) * ref.abs() + pv * (2.0 ** -11 + 2 * 2.0 ** -18 * qk[..., None] + 2.0 ** -17) + 2.0 ** -26 * low + 1e-30
 
 
 def check_attention(case, out, seed=0, lens_override=None, **kw):
