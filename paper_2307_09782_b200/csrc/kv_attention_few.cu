@@ -67,13 +67,13 @@ struct Cfg {
   static constexpr int kTileBytes = kTok * D;
   static constexpr int kProbBytes = kTok * kProbRow;                            // of a tile
   static constexpr int kOffProbs = 0;                                           // [2][kTiles]
-  static constexpr int kOffQueries = kOffProbs + 2 * kTiles * kProbBytes;       // [2][kScoreCols rows of D]
-  static constexpr int kOffScales = kOffQueries + 2 * kScoreCols * D;           // [2][kTiles][8] float4
-  static constexpr int kOffRows = kOffScales + 2 * kTiles * 8 * 16;             // [2][RS] int4: factor, first and last token + 1 seen
-  static constexpr int kOffMax = kOffRows + 2 * RS * 16;                        // [2][RS] maximum, [2][RS] factor of what came before
+  static constexpr int kOffQueries = kOffProbs + 2 * kTiles * kProbBytes;       // [3][kScoreCols rows of D]
+  static constexpr int kOffScales = kOffQueries + 3 * kScoreCols * D;           // [2][kTiles][8] float4
+  static constexpr int kOffRows = kOffScales + 2 * kTiles * 8 * 16;             // [3][RS] int4: factor, first and last token + 1 seen
+  static constexpr int kOffMax = kOffRows + 3 * RS * 16;                        // [2][RS] maximum, [2][RS] factor of what came before
   static constexpr int kOffRed = kOffMax + 4 * RS * 4;                          // [RS][8] warps' maxima
-  static constexpr int kOffSum = kOffRed + RS * 8 * 4;                          // [RS][8] warps' sums, [RS] maxima
-  static constexpr int kOffSegs = kOffSum + RS * 9 * 4;                         // [kSegs]
+  static constexpr int kOffSum = kOffRed + RS * 8 * 4;                          // [2] x ([RS][8] warps' sums, [RS] maxima)
+  static constexpr int kOffSegs = kOffSum + 2 * RS * 9 * 4;                     // [kSegs]
   static constexpr int kOffMiss = kOffSegs + kSegs * 32;                        // [value slots] pages that were not copied
   static constexpr int kOffBars = kOffMiss + 64;
   static constexpr int kMaxBars = 72;
@@ -84,7 +84,7 @@ struct Cfg {
   static constexpr int kOffKeys = kFixed;
   static constexpr int kOffCodes = kOffKeys + kKeySlots * kTileBytes;
   static constexpr int kSmemBytes = kOffCodes + kValueSlots * kTileBytes;
-  static constexpr int kNumBars = 2 * kKeySlots + 2 * kValueSlots + 14 + 5 + 2 * kSegs;
+  static constexpr int kNumBars = 2 * kKeySlots + 2 * kValueSlots + 10 + 6 + 4 + 3 + 2 * kSegs;
   static_assert(kSmemBytes <= 227 * 1024 && kNumBars <= kMaxBars && kSlots >= 4 && kValueSlots <= 16, "shared memory");
   static_assert(256 + kOutBufs * kProbCols <= 512, "tensor memory");
 };
@@ -175,11 +175,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
   uint64_t* p_full = e_full + 2;                     // [2] probabilities and row factors of a chunk           (MMA, epilogue)
   uint64_t* o_full = p_full + 2;                     // [2] results of a chunk                                 (epilogue)
   uint64_t* o_empty = o_full + 2;                    // [2] they are in registers                              (MMA, softmax)
-  uint64_t* q_full = o_empty + 2;                    // [2] queries of a segment                               (MMA, softmax)
-  uint64_t* q_empty = q_full + 2;                    // [2] nobody needs them any more                         (queries)
-  uint64_t* l_full = q_empty + 2;                    // sums of a segment                                      (epilogue)
-  uint64_t* l_empty = l_full + 1;                    // they have been read                                    (softmax)
-  uint64_t* meet = l_empty + 1;                      // [2] softmax warps that share rows
+  uint64_t* q_full = o_empty + 2;                    // [3] queries of a segment                               (MMA, softmax)
+  uint64_t* q_empty = q_full + 3;                    // [3] nobody needs them any more                         (queries)
+  uint64_t* l_full = q_empty + 3;                    // [2] sums of a segment                                  (epilogue)
+  uint64_t* l_empty = l_full + 2;                    // [2] they have been read                                (softmax)
+  uint64_t* meet = l_empty + 2;                      // [2] softmax warps that share rows
   uint64_t* g_full = meet + 2;                       // [kSegs] a segment is announced                         (all)
   uint64_t* g_empty = g_full + kSegs;                // [kSegs] everybody is through with it                   (walk)
   uint64_t* drain = g_empty + kSegs;
@@ -206,11 +206,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
       mbar_init(&p_full[i], kSoftmaxWarps);
       mbar_init(&o_full[i], 1);
       mbar_init(&o_empty[i], 4);
+      mbar_init(&l_full[i], kSoftmaxWarps);
+      mbar_init(&l_empty[i], 4);
+    }
+    for (int i = 0; i < 3; ++i) {
       mbar_init(&q_full[i], 4);
       mbar_init(&q_empty[i], 1 + kSoftmaxWarps);
     }
-    mbar_init(l_full, kSoftmaxWarps);
-    mbar_init(l_empty, 4);
     mbar_init(&meet[0], RS == 64 ? 4 : 8);
     mbar_init(&meet[1], 4);
     for (int i = 0; i < kSegs; ++i) {
@@ -335,74 +337,82 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     Ring k, v;
     bool failed = false;
     int chunk = 0, seg = 0;
-    // results of chunk `c` of nt tiles, with `left` tokens from the first on
-    auto results = [&](int c, int nt, int64_t left) {
+    // Results of tile j of a chunk: `left` tokens from the tile on.
+    auto results = [&](int c, int j, bool last, int64_t left) {
       const int cb = c & 1, ob = C::kOutBufs == 2 ? cb : 0, before = c - C::kOutBufs;  // the chunk that had these columns before
-      if (!mbar_wait(&p_full[cb], (c >> 1) & 1, s_abort) || (before >= 0 && !mbar_wait(&o_empty[before & 1], (before >> 1) & 1, s_abort))) return false;
-      for (int j = 0; j < nt; ++j, left -= kTok) {
-        if (!mbar_wait(&v_full[v.i], v.phase, s_abort)) return false;
-        const uint32_t gone = miss[v.i];
-        if (gone != 0u || left < kTok) {
-          // what lies behind the last token, or in pages that were not copied, must not turn into NaN by a product with zero
-          uint8_t* at = smem + C::kOffCodes + v.i * C::kTileBytes;
-          for (int i = lane; i < kTok * D / 16; i += 32) {
-            const int row = i / (D / 16);
-            if (row >= left || (gone >> (row / p.c.page) & 1u)) *reinterpret_cast<uint4*>(at + i * 16) = make_uint4(0u, 0u, 0u, 0u);
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
+      if (j == 0 && (!mbar_wait(&p_full[cb], (c >> 1) & 1, s_abort) || (before >= 0 && !mbar_wait(&o_empty[before & 1], (before >> 1) & 1, s_abort))))
+        return false;
+      if (!mbar_wait(&v_full[v.i], v.phase, s_abort)) return false;
+      const uint32_t gone = miss[v.i];
+      if (gone != 0u || left < kTok) {
+        // what lies behind the last token, or in pages that were not copied, must not turn into NaN by a product with zero
+        uint8_t* at = smem + C::kOffCodes + v.i * C::kTileBytes;
+        const int from = static_cast<int>(max(left, static_cast<int64_t>(0)));
+        for (int i = from * (D / 16) + lane; i < kTok * D / 16; i += 32) *reinterpret_cast<uint4*>(at + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+        for (uint32_t rest = gone; rest != 0u; rest &= rest - 1u) {
+          uint8_t* page = at + (__ffs(rest) - 1) * p.c.page * D;
+          for (int i = lane; i < p.c.page * D / 16; i += 32) *reinterpret_cast<uint4*>(page + i * 16) = make_uint4(0u, 0u, 0u, 0u);
         }
-        tc_fence_after_sync();
-        if (issuer) {
-          const uint64_t ad = vdesc + static_cast<uint64_t>((v.i * C::kTileBytes) >> 4);
-          const uint64_t bd = pdesc + static_cast<uint64_t>(((cb * kTiles + j) * C::kProbBytes) >> 4);
-          constexpr int kRow = C::kProbRow < 128 ? C::kProbRow : 128;  // (256: two halves of 128 bytes)
-#pragma unroll
-          for (int s = 0; s < kTok / 32; ++s)  // 32 tokens further
-            umma_f8(tmem + 256 + ob * C::kProbCols, ad + s * ((32 * D) >> 4), bd + s * ((32 * kRow) >> 4), odesc_i, (j > 0 || s > 0) ? 1u : 0u);
-          umma_commit(&v_empty[v.i]);
-          if (j + 1 == nt) umma_commit(&o_full[cb]);
-        }
+        fence_proxy_async_smem();
         __syncwarp();
-        v.step(C::kValueSlots);
       }
+      tc_fence_after_sync();
+      if (issuer) {
+        const uint64_t ad = vdesc + static_cast<uint64_t>((v.i * C::kTileBytes) >> 4);
+        const uint64_t bd = pdesc + static_cast<uint64_t>(((cb * kTiles + j) * C::kProbBytes) >> 4);
+        constexpr int kRow = C::kProbRow < 128 ? C::kProbRow : 128;  // (256: two halves of 128 bytes)
+#pragma unroll
+        for (int s = 0; s < kTok / 32; ++s)  // 32 tokens further
+          umma_f8(tmem + 256 + ob * C::kProbCols, ad + s * ((32 * D) >> 4), bd + s * ((32 * kRow) >> 4), odesc_i, (j > 0 || s > 0) ? 1u : 0u);
+        umma_commit(&v_empty[v.i]);
+        if (last) umma_commit(&o_full[cb]);
+      }
+      __syncwarp();
+      v.step(C::kValueSlots);
       return true;
     };
-    int64_t last_left = 0;
-    int last_nt = 0;  // tiles of the chunk whose scores are issued and whose results are not
+    // Scores of a chunk go tile by tile in turn with the results of the chunk two before: keys and values are used up evenly, while
+    // the softmax works on the chunk in between.
+    int had[2] = {0, 0};          // tiles of the last chunk and the one before it
+    int64_t had_left[2] = {0, 0};
     int nt_seg;
     for (; any && !failed && segment(seg, nt_seg); ++seg) {
       const int64_t left = s_seg[seg % kSegs].L - static_cast<int64_t>(s_seg[seg % kSegs].tile0) * kTok;
       __syncwarp();
       done_with(seg);
-      if (!mbar_wait(&q_full[seg & 1], (seg >> 1) & 1, s_abort)) failed = true;
+      if (!mbar_wait(&q_full[seg % 3], (seg / 3) & 1, s_abort)) failed = true;
       for (int t = 0; t < nt_seg && !failed; t += kTiles, ++chunk) {
         const int nt = min(kTiles, nt_seg - t), cb = chunk & 1;
         if (chunk >= 2 && !mbar_wait(&s_empty[cb], ((chunk >> 1) - 1) & 1, s_abort)) failed = true;
-        for (int j = 0; j < nt && !failed; ++j) {
-          if (!mbar_wait(&k_full[k.i], k.phase, s_abort)) {
-            failed = true;
-            break;
-          }
-          tc_fence_after_sync();
-          if (issuer) {
-            const uint64_t ad = kdesc + static_cast<uint64_t>((k.i * C::kTileBytes) >> 4);
-            const uint64_t bd = qdesc + static_cast<uint64_t>(((seg & 1) * C::kScoreCols * D) >> 4);
+        for (int j = 0; j < max(nt, had[1]) && !failed; ++j) {
+          if (j < nt) {
+            if (!mbar_wait(&k_full[k.i], k.phase, s_abort)) {
+              failed = true;
+              break;
+            }
+            tc_fence_after_sync();
+            if (issuer) {
+              const uint64_t ad = kdesc + static_cast<uint64_t>((k.i * C::kTileBytes) >> 4);
+              const uint64_t bd = qdesc + static_cast<uint64_t>(((seg % 3) * C::kScoreCols * D) >> 4);
 #pragma unroll
-            for (int s = 0; s < D / 32; ++s) umma_f8(tmem + cb * 128 + j * C::kScoreCols, ad + s * 2, bd + s * 2, sdesc_i, s > 0 ? 1u : 0u);
-            umma_commit(&k_empty[k.i]);
-            if (j + 1 == nt) umma_commit(&s_full[cb]);
-            if (t + j + 1 == nt_seg) umma_commit(&q_empty[seg & 1]);
+              for (int s = 0; s < D / 32; ++s) umma_f8(tmem + cb * 128 + j * C::kScoreCols, ad + s * 2, bd + s * 2, sdesc_i, s > 0 ? 1u : 0u);
+              umma_commit(&k_empty[k.i]);
+              if (j + 1 == nt) umma_commit(&s_full[cb]);
+              if (t + j + 1 == nt_seg) umma_commit(&q_empty[seg % 3]);
+            }
+            __syncwarp();
+            k.step(C::kKeySlots);
           }
-          __syncwarp();
-          k.step(C::kKeySlots);
+          if (j < had[1] && !results(chunk - 2, j, j + 1 == had[1], had_left[1] - static_cast<int64_t>(j) * kTok)) failed = true;
         }
-        if (!failed && chunk > 0 && !results(chunk - 1, last_nt, last_left)) failed = true;
-        last_nt = nt;
-        last_left = left - static_cast<int64_t>(t) * kTok;
+        had[1] = had[0];
+        had_left[1] = had_left[0];
+        had[0] = nt;
+        had_left[0] = left - static_cast<int64_t>(t) * kTok;
       }
     }
-    if (!failed && chunk > 0 && !results(chunk - 1, last_nt, last_left)) failed = true;
+    for (int c = 1; c >= 0; --c)  // the last two chunks
+      for (int j = 0; j < had[c] && !failed; ++j) failed = !results(chunk - 1 - c, j, j + 1 == had[c], had_left[c] - static_cast<int64_t>(j) * kTok);
     if (failed && issuer) fp8b::raise_error8(p.status, s_abort, kErrMmaA);
     // tensor memory is released only when every MMA has completed, also where another role has given up
     if (issuer) umma_commit(drain);
@@ -416,8 +426,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     int seg = 0, chunk = 0;
     Walk w;  // of the segment announced last
     bool more = any && w.start(p, s_range), ok = more;
-    // Announces segment `seg`, or that there are no more.  A segment is announced when the one before it begins here: the epilogue
-    // fetches its queries ahead and must not wait for chunks that wait for the epilogue.
+    // Announces segment `seg`, or that there are no more.  Segments are announced two ahead: the epilogue fetches queries ahead and
+    // must not wait for chunks that wait for the epilogue.
     auto announce = [&] {
       if (seg >= kSegs && !mbar_wait_warp(&g_empty[seg % kSegs], (seg / kSegs - 1) & 1, s_abort)) return false;
       if (lane == 0) {
@@ -433,6 +443,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
       ++seg;
       return true;
     };
+    // what the scales need of a segment: the one at hand and the two announced
+    struct Place {
+      int b, h, L, nt, tile0;
+    };
+    auto place = [&] { return more ? Place{w.b, w.h, w.s.L, w.nt, w.s.tile0 + w.t} : Place{0, 0, 0, 0, 0}; };
+    auto advance = [&] {
+      if (!more) return true;  // the end has been announced
+      more = w.next(p);
+      return announce();
+    };
     constexpr int kMany = (kTiles * 8 + 31) / 32;
     RawScales next[kMany];
     auto load = [&](int b, int h, int tile, int L) {
@@ -442,20 +462,22 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     };
     if (ok) {
       ok = announce();
-      load(w.b, w.h, w.s.tile0 + w.t, w.s.L);
-      while (ok && more) {
-        const int b = w.b, h = w.h, L = w.s.L, nt = w.nt, tile0 = w.s.tile0 + w.t;
-        more = w.next(p);
-        ok = announce();
-        for (int t = 0; ok && t < nt; t += kTiles, ++chunk) {
+      Place here = place();
+      if (ok) ok = advance();
+      Place after = place();
+      load(here.b, here.h, here.tile0, here.L);
+      while (ok && here.nt > 0) {
+        ok = advance();
+        const Place last = place();
+        for (int t = 0; ok && t < here.nt; t += kTiles, ++chunk) {
           const int cb = chunk & 1;
           float4 e[kMany];
 #pragma unroll
           for (int i = 0; i < kMany; ++i) e[i] = scale_entry(next[i]);
-          if (t + kTiles < nt)
-            load(b, h, tile0 + t + kTiles, L);
-          else if (more)
-            load(w.b, w.h, w.s.tile0 + w.t, w.s.L);
+          if (t + kTiles < here.nt)
+            load(here.b, here.h, here.tile0 + t + kTiles, here.L);
+          else if (after.nt > 0)
+            load(after.b, after.h, after.tile0, after.L);
           if (chunk >= 2 && !mbar_wait_warp(&s_empty[cb], ((chunk >> 1) - 1) & 1, s_abort)) ok = false;
           if (!ok) break;
 #pragma unroll
@@ -464,6 +486,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           __syncwarp();
           if (lane == 0) mbar_arrive(&e_full[cb]);
         }
+        here = after;
+        after = last;
       }
       if (!ok && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrWalkA);
     }
@@ -497,8 +521,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     for (; !failed && segment(seg, nt_seg); ++seg) {
         const Seg& g = s_seg[seg % kSegs];
         const int rows = min(max(g.n * p.G - r0, 0), RR), tile0 = g.tile0;
-        const float4* info = reinterpret_cast<const float4*>(smem + C::kOffRows) + (seg & 1) * RS + r0;
-        if (!fp8b::mbar_wait_all(&q_full[seg & 1], (seg >> 1) & 1, s_abort)) {
+        const float4* info = reinterpret_cast<const float4*>(smem + C::kOffRows) + (seg % 3) * RS + r0;
+        if (!fp8b::mbar_wait_all(&q_full[seg % 3], (seg / 3) & 1, s_abort)) {
           failed = true;
           break;
         }
@@ -626,22 +650,23 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
         }
         if (failed) break;
         // sums of the segment
-        if (seg > 0 && !fp8b::mbar_wait_all(l_empty, (seg - 1) & 1, s_abort)) {
+        if (seg >= 2 && !fp8b::mbar_wait_all(&l_empty[seg & 1], ((seg >> 1) - 1) & 1, s_abort)) {
           failed = true;
           break;
         }
+        float* sums = s_sum + (seg & 1) * RS * 9;
 #pragma unroll
         for (int r = 0; r < RR; ++r) {
           float v = l[r];
 #pragma unroll
           for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-          if (lane == 0) s_sum[(r0 + r) * 8 + red_i] = v;
+          if (lane == 0) sums[(r0 + r) * 8 + red_i] = v;
         }
-        if (me < rows) s_sum[RS * 8 + r0 + me] = m_run;
+        if (me < rows) sums[RS * 8 + r0 + me] = m_run;
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(l_full);
-          mbar_arrive(&q_empty[seg & 1]);
+          mbar_arrive(&l_full[seg & 1]);
+          mbar_arrive(&q_empty[seg % 3]);
         }
     }
     if (failed && any && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrSoftmaxA);
@@ -657,11 +682,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
     int chunk = 0, seg = 0;
     int64_t unit = any ? total * blockIdx.x / ctas : 0;
     if (threadIdx.x == kEpiWarp0 * 32) p.shared[blockIdx.x] = make_int4(0, 0, 0, 0);
-    // queries of segment `sg` (D / 8 lanes per row), once nobody needs those of the segment two before
+    // queries of segment `sg` (D / 8 lanes per row), once nobody needs those of the segment three before
     constexpr int kLanes = D / 8, kAtOnce = 128 / kLanes, kBatch = RS < 2 * kAtOnce ? 1 : 2;
     auto queries = [&](int sg) {
       const Seg& g = s_seg[sg % kSegs];
-      const int rows = g.n * p.G, qb = sg & 1, i = threadIdx.x - kEpiWarp0 * 32;
+      const int rows = g.n * p.G, qb = sg % 3, i = threadIdx.x - kEpiWarp0 * 32;
       uint8_t* to = smem + C::kOffQueries + qb * C::kScoreCols * D;
       int4* info = reinterpret_cast<int4*>(smem + C::kOffRows) + qb * RS;
       for (int r0 = 0; r0 < rows; r0 += kAtOnce * kBatch) {
@@ -673,7 +698,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           if (r < rows)
             x[k] = load_chained(reinterpret_cast<const uint4*>(p.q + (g.first + r / p.G) * p.ldq + (static_cast<int64_t>(g.h) * p.G + r % p.G) * D + (i % kLanes) * 8));
         }
-        if (r0 == 0 && sg >= 2 && !fp8b::mbar_wait_all(&q_empty[qb], ((sg >> 1) - 1) & 1, s_abort)) return false;
+        if (r0 == 0 && sg >= 3 && !fp8b::mbar_wait_all(&q_empty[qb], (sg / 3 - 1) & 1, s_abort)) return false;
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
           const int r = r0 + k * kAtOnce + i / kLanes;
@@ -702,16 +727,19 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
       if (lane == 0) mbar_arrive(&q_full[qb]);
       return true;
     };
-    int nt_seg, nt_next = 0;
-    if (!failed && segment(0, nt_next)) failed = !queries(0);
-    for (; !failed && nt_next > 0; ++seg) {
-        nt_seg = nt_next;
+    // segments `seg`, seg + 1, seg + 2 are announced, the queries of the first two on their way (or there are no more)
+    int nt_seg = 0, nt_next = 0, nt_last = 0;
+    if (!failed && segment(0, nt_seg)) {
+      failed = !queries(0);
+      if (!failed && segment(1, nt_next)) failed = !queries(1);
+    }
+    for (; !failed && nt_seg > 0; ++seg, nt_seg = nt_next, nt_next = nt_last) {
         const Seg& g = s_seg[seg % kSegs];
         const int rows = g.n * p.G, first = g.first, h = g.h, b = g.b, flags = g.flags;
         __syncwarp();
         done_with(seg);
-        if (!segment(seg + 1, nt_next)) nt_next = 0;  // (an error shows in the waits below)
-        if (nt_next > 0 && !queries(seg + 1)) {
+        nt_last = 0;
+        if (nt_next > 0 && segment(seg + 2, nt_last) && !queries(seg + 2)) {
           if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrQueriesA);
           failed = true;
           break;
@@ -742,27 +770,28 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           __syncwarp();
           if (lane == 0) mbar_arrive(&o_empty[cb]);
         }
-        if (failed || !fp8b::mbar_wait_all(l_full, seg & 1, s_abort)) {
+        if (failed || !fp8b::mbar_wait_all(&l_full[seg & 1], (seg >> 1) & 1, s_abort)) {
           failed = true;
           break;
         }
         // each warp sums every row up for itself, a row per lane (and the 32nd after), and hands its factor round
         const bool whole = flags == 3;
         float* part = p.partial + (static_cast<int64_t>(blockIdx.x) * 2 + (flags & 1)) * (RS * (D + 2));
+        const float* sums = s_sum + (seg & 1) * RS * 9;
         float factor[(RS + 31) / 32];
 #pragma unroll
         for (int k = 0; k < (RS + 31) / 32; ++k) {
           const int r = k * 32 + lane;
           factor[k] = 1.0f;
           if (r < rows) {
-            const float4* v = reinterpret_cast<const float4*>(s_sum + r * 8);
+            const float4* v = reinterpret_cast<const float4*>(sums + r * 8);
             const float4 x = v[0];
             float sum = ((x.x + x.y) + x.z) + x.w;
             if (RS != 64) {
               const float4 y = v[1];
               sum = (((sum + y.x) + y.y) + y.z) + y.w;
             }
-            const float m = s_sum[RS * 8 + r];
+            const float m = sums[RS * 8 + r];
             if (whole) factor[k] = sum == 0.0f ? 0.0f : kCodeUnit / sum;
             if (warp == kEpiWarp0) {
               if (!whole) {
@@ -796,7 +825,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           if (next) left = group;
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(l_empty);
+        if (lane == 0) mbar_arrive(&l_empty[seg & 1]);
         if (flags == 1 && threadIdx.x == kEpiWarp0 * 32) {
           // goes on in the next CTAs, to the one whose range holds the last tile
           const int64_t last = unit + seq_of(p, b).tiles - 1;
