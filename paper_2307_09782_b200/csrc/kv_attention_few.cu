@@ -380,11 +380,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
       const int64_t left = s_seg[seg % kSegs].L - static_cast<int64_t>(s_seg[seg % kSegs].tile0) * kTok;
       __syncwarp();
       done_with(seg);
-      if (!mbar_wait(&q_full[seg % 3], (seg / 3) & 1, s_abort)) failed = true;
       for (int t = 0; t < nt_seg && !failed; t += kTiles, ++chunk) {
         const int nt = min(kTiles, nt_seg - t), cb = chunk & 1;
-        if (chunk >= 2 && !mbar_wait(&s_empty[cb], ((chunk >> 1) - 1) & 1, s_abort)) failed = true;
-        for (int j = 0; j < max(nt, had[1]) && !failed; ++j) {
+        int done = 0;  // of the results that are due
+        if (t == 0 && !__all_sync(0xFFFFFFFFu, mbar_try_wait(&q_full[seg % 3], (seg / 3) & 1))) {
+          // a new segment's queries are late: what is due does not wait for them
+          for (; done < had[1] && !failed; ++done) failed = !results(chunk - 2, done, done + 1 == had[1], had_left[1] - static_cast<int64_t>(done) * kTok);
+          if (!failed && !mbar_wait(&q_full[seg % 3], (seg / 3) & 1, s_abort)) failed = true;
+        }
+        if (!failed && chunk >= 2 && !mbar_wait(&s_empty[cb], ((chunk >> 1) - 1) & 1, s_abort)) failed = true;
+        for (int j = 0; j < max(nt, had[1] - done) && !failed; ++j) {
           if (j < nt) {
             if (!mbar_wait(&k_full[k.i], k.phase, s_abort)) {
               failed = true;
@@ -403,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
             __syncwarp();
             k.step(C::kKeySlots);
           }
-          if (j < had[1] && !results(chunk - 2, j, j + 1 == had[1], had_left[1] - static_cast<int64_t>(j) * kTok)) failed = true;
+          if (done == 0 && j < had[1] && !results(chunk - 2, j, j + 1 == had[1], had_left[1] - static_cast<int64_t>(j) * kTok)) failed = true;
         }
         had[1] = had[0];
         had_left[1] = had_left[0];
