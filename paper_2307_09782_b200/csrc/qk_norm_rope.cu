@@ -2,10 +2,13 @@
 //   n = x / sqrt(mean(x^2) + eps);  z = n w;  y = R(p) z      (R rotates pairs of features by the position's angles)
 //   backward:  g = R(-p) dy;  dw = sum g n;  dx = (g w - n mean(g w n)) / sqrt(mean(x^2) + eps)
 //
-// Bound by memory: 4 bytes per element forward (6 backward).  A lane holds 16 bytes (8 features) of a head, so a warp takes 2
-// heads of 128 features (4 of 64) at a time and kSteps of them in flight; cosines, sines and weights of the lane's features
-// stay in its registers for all of them.  The sum of squares takes shuffles over the head's lanes; the partner of a feature is
-// in the lane itself (neighbours) or in one other lane (halves).  All arithmetic in FP32, one rounding to bf16 at the end.
+// Bound by memory: 4 bytes per element forward, 6 backward.  A lane holds 16 bytes (8 features) of a head, so a warp takes 2 heads
+// of 128 features (4 of 64) at a time, kSteps of them per unit.  Warps walk over contiguous ranges of units, the next unit's rows
+// on their way while one is worked on; a token's angles and weights become two factors per feature that all of its heads share:
+//   y = (x c w + x' s' w') / sqrt(..)     (x', w': the feature it is paired with; s' carries the sign)
+// The partner's x comes as bf16 pairs from one other lane (halves) or from the lane itself (neighbours).  All arithmetic in FP32, one
+// rounding to bf16 at the end.  16384 tokens of 40 heads of 128: without the walk and the shared factors 84 us (32 warps per SM,
+// each waiting for its position, then for its angles; half of the issue slots used).
 #include "kv_cache.cuh"
 
 namespace zq {
@@ -14,6 +17,9 @@ namespace {
 
 constexpr int kWarps = 8;
 constexpr int kSteps = 4;
+constexpr int kBackSteps = 2;       // in flight at a time, backward
+constexpr int kForwardBlocks = 3;   // per SM: 24 warps with the registers that a unit ahead needs
+constexpr int kBackwardBlocks = 3;
 
 struct P {
   const __nv_bfloat16 *x[2], *dy[2];
@@ -51,199 +57,247 @@ __device__ __forceinline__ float head_sum(float v) {
   return v;
 }
 
-// The angles of a lane's 8 features at a token's position.
-struct Angles {
-  float c[8], s[8];  // halves: of the 8 features; neighbours: of the 4 pairs
-  int partner;       // halves: the lane with the other features of the pairs (itself where nothing is rotated)
-  bool rotated;
+// Unit u -> token, queries (0) or keys (1), first head.
+struct Unit {
+  int64_t t;
+  int which, h0;
 };
 template <int LANES>
-__device__ __forceinline__ void load_angles(const P& p, int64_t t, int l, int lane, Angles& a) {
-  const int pos = load_chained(p.positions + t);
-  const bool known = pos >= 0 && pos < p.far;
-  const int half = p.rot >> 1;
-  a.rotated = l * 8 < p.rot;
-  a.partner = lane;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) a.c[i] = a.s[i] = __uint_as_float(0x7FC00000u);  // a position the table lacks: no angle
-  if (!a.rotated) return;
-  const float* row = p.table + static_cast<int64_t>(known ? pos : 0) * p.rot;
-  if (p.neighbours) {
-    if (known) {
-      const float4 c = load_chained(reinterpret_cast<const float4*>(row + l * 4));
-      const float4 s = load_chained(reinterpret_cast<const float4*>(row + half + l * 4));
-      a.c[0] = c.x, a.c[1] = c.y, a.c[2] = c.z, a.c[3] = c.w;
-      a.s[0] = s.x, a.s[1] = s.y, a.s[2] = s.z, a.s[3] = s.w;
-    }
-    return;
-  }
-  const int hl = half >> 3;  // lanes of half a pair
-  const bool second = l >= hl;
-  a.partner = second ? lane - hl : lane + hl;
-  if (known) {
-    load8(row + (second ? l - hl : l) * 8, a.c);
-    load8(row + half + (second ? l - hl : l) * 8, a.s);
-  }
-  if (!second) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) a.s[i] = -a.s[i];  // y_a = z_a cos - z_b sin, y_b = z_b cos + z_a sin
-  }
+__device__ __forceinline__ Unit unit_of(const P& p, int64_t u) {
+  const int per = p.chunks[0] + p.chunks[1];
+  Unit r;
+  r.t = u / per;
+  int c = static_cast<int>(u - r.t * per);
+  r.which = c >= p.chunks[0];
+  if (r.which) c -= p.chunks[0];
+  r.h0 = c * kSteps * (32 / LANES);
+  return r;
 }
-// Rotation by the angles, or back.  All lanes of the warp take part.
-template <bool BACK>
-__device__ __forceinline__ void rotate(const P& p, const Angles& a, float* z) {
-  if (p.neighbours) {
-    if (!a.rotated) return;
+// A warp's units: contiguous, as even as can be.
+__device__ __forceinline__ void range_of(const P& p, int64_t& u0, int64_t& u1) {
+  const int64_t warps = static_cast<int64_t>(gridDim.x) * kWarps, w = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const int64_t each = p.units / warps, rest = p.units % warps;
+  u0 = w * each + (w < rest ? w : rest);
+  u1 = u0 + each + (w < rest ? 1 : 0);
+}
+template <int D>
+__device__ __forceinline__ void load_rows(const __nv_bfloat16* x, int64_t ld, const Unit& n, int heads, int lane, uint4* v) {
+  constexpr int L = D / 8;
+  const __nv_bfloat16* from = x + n.t * ld + (lane % L) * 8;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float u = z[2 * i], v = z[2 * i + 1], s = BACK ? -a.s[i] : a.s[i];
-      z[2 * i] = u * a.c[i] - v * s;
-      z[2 * i + 1] = v * a.c[i] + u * s;
-    }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float o = __shfl_sync(0xFFFFFFFFu, z[i], a.partner);
-    if (a.rotated) z[i] = z[i] * a.c[i] + o * (BACK ? -a.s[i] : a.s[i]);
+  for (int i = 0; i < kSteps; ++i) {
+    const int h = n.h0 + i * (32 / L) + lane / L;
+    v[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (h < heads) v[i] = load_chained(reinterpret_cast<const uint4*>(from + static_cast<int64_t>(h) * D));
   }
 }
 
-// Unit u -> token, queries (0) or keys (1), first head.
+// Cosines and sines for a lane's 8 features at position `pos` (NaN where the table lacks it), the sine's sign as the forward pass has
+// it; 1 and 0 where nothing is rotated.  `partner`: the lane of the paired features (halves).
 template <int LANES>
-__device__ __forceinline__ void unit_of(const P& p, int64_t u, int64_t& t, int& which, int& h0) {
-  const int per = p.chunks[0] + p.chunks[1];
-  t = u / per;
-  int c = static_cast<int>(u - t * per);
-  which = c >= p.chunks[0];
-  if (which) c -= p.chunks[0];
-  h0 = c * kSteps * (32 / LANES);
+__device__ __forceinline__ void load_angles(const P& p, int pos, int l, int lane, float* c, float* s, int& partner) {
+  const bool known = pos >= 0 && pos < p.far;
+  const int half = p.rot >> 1;
+  const float* row = p.table + static_cast<int64_t>(known ? pos : 0) * p.rot;
+  partner = lane;
+  if (l * 8 >= p.rot) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = 1.0f, s[i] = 0.0f;
+    return;
+  }
+  if (p.neighbours) {
+    const float4 a = load_chained(reinterpret_cast<const float4*>(row + l * 4)), b = load_chained(reinterpret_cast<const float4*>(row + half + l * 4));
+    c[0] = c[1] = a.x, c[2] = c[3] = a.y, c[4] = c[5] = a.z, c[6] = c[7] = a.w;
+    s[0] = -b.x, s[1] = b.x, s[2] = -b.y, s[3] = b.y, s[4] = -b.z, s[5] = b.z, s[6] = -b.w, s[7] = b.w;
+  } else {
+    const int hl = half >> 3;  // lanes of one half
+    const bool second = l >= hl;
+    partner = second ? lane - hl : lane + hl;
+    load8(row + (second ? l - hl : l) * 8, c);
+    load8(row + half + (second ? l - hl : l) * 8, s);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = second ? s[i] : -s[i];
+  }
+  if (!known) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = s[i] = __uint_as_float(0x7FC00000u);
+  }
+}
+// The paired features of 8, as bf16 pairs.  All lanes of the warp take part.
+__device__ __forceinline__ uint4 paired(const P& p, uint4 v, int partner, bool rotated) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    w[i] = p.neighbours ? __byte_perm(w[i], 0u, 0x1032) : __shfl_sync(0xFFFFFFFFu, w[i], partner);
+    if (!rotated) w[i] = 0u;  // (times a sine of zero: an infinity must not become NaN)
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// The weights of the paired features.
+__device__ __forceinline__ void paired_weights(const P& p, const float* w, int partner, float* wp) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) wp[i] = p.neighbours ? w[i ^ 1] : __shfl_sync(0xFFFFFFFFu, w[i], partner);
 }
 
 template <int D>
-__global__ void __launch_bounds__(kWarps * 32) norm_rope_kernel(const P p) {
+__global__ void __launch_bounds__(kWarps * 32, kForwardBlocks) norm_rope_kernel(const P p) {
   constexpr int L = D / 8;
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, l = lane % L;
-  const int64_t u = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const bool rotated = l * 8 < p.rot, norm = p.w[0] != nullptr;
+  int64_t u, end;
+  range_of(p, u, end);
   pdl_wait();
-  if (u >= p.units) return;
-  int64_t t;
-  int which, h0;
-  unit_of<L>(p, u, t, which, h0);
-  const int heads = p.heads[which];
-  const __nv_bfloat16* x = p.x[which] + t * p.ldx[which] + l * 8;
+  if (u >= end) return;
+  Unit n = unit_of<L>(p, u);
+  int pos = load_chained(p.positions + n.t), partner = lane;
   uint4 v[kSteps];
+  load_rows<D>(p.x[n.which], p.ldx[n.which], n, p.heads[n.which], lane, v);
+  int64_t at = -1;     // token and kind the factors belong to
+  float wc[8], ws[8];  // of the feature and of the one paired with it
+  for (; u < end; ++u) {
+    const int64_t key = n.t * 2 + n.which;
+    if (key != at) {
+      at = key;
+      load_angles<L>(p, pos, l, lane, wc, ws, partner);
+      if (norm) {
+        float w[8], wp[8];
+        load8(p.w[n.which] + l * 8, w);
+        paired_weights(p, w, partner, wp);
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const int h = h0 + i * (32 / L) + lane / L;
-    v[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (h < heads) v[i] = load_chained(reinterpret_cast<const uint4*>(x + static_cast<int64_t>(h) * D));
-  }
-  Angles a;
-  load_angles<L>(p, t, l, lane, a);
-  float w[8];
-  const bool norm = p.w[which] != nullptr;
-  if (norm) load8(p.w[which] + l * 8, w);
-  __nv_bfloat16* out = p.out[which] + t * p.ldo[which] + l * 8;
-#pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const int h = h0 + i * (32 / L) + lane / L;
-    float z[8];
-    unpack8(v[i], z);
-    if (norm) {
-      float ss = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(z[e], z[e], ss);
-      const float r = rsqrtf(head_sum<L>(ss) * (1.0f / D) + p.eps);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = z[e] * r * w[e];
+        for (int e = 0; e < 8; ++e) wc[e] *= w[e], ws[e] *= wp[e];
+      }
     }
-    rotate<false>(p, a, z);
-    if (h < heads) *reinterpret_cast<uint4*>(out + static_cast<int64_t>(h) * D) = pack8(z);
+    Unit next = n;
+    uint4 ahead[kSteps];
+    if (u + 1 < end) {
+      next = unit_of<L>(p, u + 1);
+      if (next.t != n.t) pos = load_chained(p.positions + next.t);
+      load_rows<D>(p.x[next.which], p.ldx[next.which], next, p.heads[next.which], lane, ahead);
+    }
+    __nv_bfloat16* out = p.out[n.which] + n.t * p.ldo[n.which] + l * 8;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int h = n.h0 + i * (32 / L) + lane / L;
+      float z[8], y[8];
+      unpack8(paired(p, v[i], partner, rotated), y);
+      unpack8(v[i], z);
+      float r = 1.0f;
+      if (norm) {
+        float ss = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = fmaf(z[e], z[e], ss);
+        r = rsqrtf(head_sum<L>(ss) * (1.0f / D) + p.eps);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = r * fmaf(z[e], wc[e], y[e] * ws[e]);
+      if (h < p.heads[n.which]) *reinterpret_cast<uint4*>(out + static_cast<int64_t>(h) * D) = pack8(y);
+    }
+    n = next;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) v[i] = ahead[i];
   }
 }
 
-// Warps take units one after the other and sum the weights' gradients of their lanes' features over them, always the same
-// units in the same order; a block's sums go to its own place among the partial sums, which norm_grad_sum_kernel adds up.
+// Warps sum the weights' gradients of their lanes' features over their units, always the same ones in the same order; a block's sums
+// go to its own place among the partial sums, which norm_grad_sum_kernel adds up.
 template <int D>
-__global__ void __launch_bounds__(kWarps * 32) norm_rope_backward_kernel(const P p) {
+__global__ void __launch_bounds__(kWarps * 32, kBackwardBlocks) norm_rope_backward_kernel(const P p) {
   constexpr int L = D / 8;
   __shared__ float s_dw[kWarps][2][D];
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, l = lane % L, warp = threadIdx.x >> 5;
-  float dw[2][8] = {};
-  pdl_wait();
-  for (int64_t u = static_cast<int64_t>(blockIdx.x) * kWarps + warp; u < p.units; u += static_cast<int64_t>(gridDim.x) * kWarps) {
-    int64_t t;
-    int which, h0;
-    unit_of<L>(p, u, t, which, h0);
-    const int heads = p.heads[which];
-    const bool norm = p.w[which] != nullptr;
-    const __nv_bfloat16* x = p.x[which] + t * p.ldx[which] + l * 8;
-    const __nv_bfloat16* dy = p.dy[which] + t * p.lddy[which] + l * 8;
-    uint4 v[kSteps], d[kSteps];
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const int h = h0 + i * (32 / L) + lane / L;
-      v[i] = d[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (h < heads) {
-        d[i] = load_chained(reinterpret_cast<const uint4*>(dy + static_cast<int64_t>(h) * D));
-        if (norm) v[i] = load_chained(reinterpret_cast<const uint4*>(x + static_cast<int64_t>(h) * D));
-      }
-    }
-    Angles a;
-    load_angles<L>(p, t, l, lane, a);
-    float w[8];
-    if (norm) load8(p.w[which] + l * 8, w);
-    __nv_bfloat16* out = p.out[which] + t * p.ldo[which] + l * 8;
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const int h = h0 + i * (32 / L) + lane / L;
-      float g[8];
-      unpack8(d[i], g);
-      rotate<true>(p, a, g);
-      if (norm) {
-        float z[8], ss = 0.0f, dot = 0.0f;
-        unpack8(v[i], z);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ss = fmaf(z[e], z[e], ss);
-        const float r = rsqrtf(head_sum<L>(ss) * (1.0f / D) + p.eps);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          z[e] *= r;
-          if (h < heads) {
-            if (which == 0)
-              dw[0][e] = fmaf(g[e], z[e], dw[0][e]);
-            else
-              dw[1][e] = fmaf(g[e], z[e], dw[1][e]);
-          }
-          g[e] *= w[e];
-          dot = fmaf(g[e], z[e], dot);
-        }
-        const float mean = head_sum<L>(dot) * (1.0f / D);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] = r * (g[e] - z[e] * mean);
-      }
-      if (h < heads) *reinterpret_cast<uint4*>(out + static_cast<int64_t>(h) * D) = pack8(g);
-    }
-  }
-  if (!p.partial) return;
-#pragma unroll
-  for (int k = 0; k < 2; ++k)
+  const bool rotated = l * 8 < p.rot, norm = p.w[0] != nullptr;
+  float dw[8] = {};  // of the kind at hand; on a change of kind it goes to shared memory
+  int64_t u, end;
+  range_of(p, u, end);
+  if (norm)
+    for (int i = lane; i < 2 * D; i += 32) s_dw[warp][i / D][i % D] = 0.0f;
+  __syncwarp();
+  auto settle = [&](int which) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      float s = dw[k][e];
+      float v = dw[e];
 #pragma unroll
-      for (int o = L; o < 32; o <<= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-      if (lane < L) s_dw[warp][k][l * 8 + e] = s;
+      for (int o = L; o < 32; o <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+      if (lane < L) s_dw[warp][which][l * 8 + e] += v;
+      dw[e] = 0.0f;
     }
+  };
+  pdl_wait();
+  if (u < end) {
+    Unit n = unit_of<L>(p, u);
+    int pos = load_chained(p.positions + n.t), partner = lane;
+    uint4 d[kBackSteps], v[kBackSteps];
+    int64_t at = -1;
+    float c[8], s[8], w[8];
+    for (; u < end; ++u) {
+      const int heads = p.heads[n.which];
+      const int64_t key = n.t * 2 + n.which;
+      if (key != at) {
+        if (norm && at >= 0 && n.which != static_cast<int>(at & 1)) settle(static_cast<int>(at & 1));
+        at = key;
+        load_angles<L>(p, pos, l, lane, c, s, partner);
+        if (norm) load8(p.w[n.which] + l * 8, w);
+      }
+      Unit next = n;
+      if (u + 1 < end) {
+        next = unit_of<L>(p, u + 1);
+        if (next.t != n.t) pos = load_chained(p.positions + next.t);
+      }
+      const __nv_bfloat16* x = p.x[n.which] + n.t * p.ldx[n.which] + l * 8;
+      const __nv_bfloat16* dy = p.dy[n.which] + n.t * p.lddy[n.which] + l * 8;
+      __nv_bfloat16* out = p.out[n.which] + n.t * p.ldo[n.which] + l * 8;
+#pragma unroll
+      for (int i0 = 0; i0 < kSteps; i0 += kBackSteps) {
+#pragma unroll
+        for (int i = 0; i < kBackSteps; ++i) {
+          const int h = n.h0 + (i0 + i) * (32 / L) + lane / L;
+          v[i] = d[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (h < heads) {
+            d[i] = load_chained(reinterpret_cast<const uint4*>(dy + static_cast<int64_t>(h) * D));
+            if (norm) v[i] = load_chained(reinterpret_cast<const uint4*>(x + static_cast<int64_t>(h) * D));
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kBackSteps; ++i) {
+          const int h = n.h0 + (i0 + i) * (32 / L) + lane / L;
+          float g[8], y[8];
+          unpack8(paired(p, d[i], partner, rotated), y);
+          unpack8(d[i], g);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) g[e] = fmaf(g[e], c[e], -y[e] * s[e]);  // by the opposite angle
+          if (norm) {
+            float z[8], ss = 0.0f, dot = 0.0f;
+            unpack8(v[i], z);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ss = fmaf(z[e], z[e], ss);
+            const float r = rsqrtf(head_sum<L>(ss) * (1.0f / D) + p.eps);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              z[e] *= r;
+              dw[e] = fmaf(g[e], z[e], dw[e]);  // (zeros where there is no head)
+              g[e] *= w[e];
+              dot = fmaf(g[e], z[e], dot);
+            }
+            const float mean = head_sum<L>(dot) * (1.0f / D);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[e] = r * fmaf(-z[e], mean, g[e]);
+          }
+          if (h < heads) *reinterpret_cast<uint4*>(out + static_cast<int64_t>(h) * D) = pack8(g);
+        }
+      }
+      n = next;
+    }
+    if (norm) settle(static_cast<int>(at & 1));
+  }
+  if (!norm) return;
   __syncthreads();
   for (int i = threadIdx.x; i < 2 * D; i += kWarps * 32) {
-    float s = 0.0f;
+    float v = 0.0f;
 #pragma unroll
-    for (int k = 0; k < kWarps; ++k) s += s_dw[k][i / D][i % D];
-    p.partial[static_cast<int64_t>(blockIdx.x) * 2 * D + i] = s;
+    for (int k = 0; k < kWarps; ++k) v += s_dw[k][i / D][i % D];
+    p.partial[static_cast<int64_t>(blockIdx.x) * 2 * D + i] = v;
   }
 }
 
@@ -280,10 +334,9 @@ P params(const NormRopeArgs& a) {
 
 int launch_norm_rope(const NormRopeArgs& a, cudaStream_t st) {
   const P p = params(a);
-  const int64_t grid = (p.units + kWarps - 1) / kWarps;
-  if (grid > 0x7FFFFFFF) return ZQ_ERR_SHAPE;
-  const cudaError_t e = launch_chained(a.D == 128 ? norm_rope_kernel<128> : norm_rope_kernel<64>, dim3(static_cast<unsigned>(grid)),
-                                       dim3(kWarps * 32), 0, st, false, p);
+  const int64_t want = (p.units + kWarps - 1) / kWarps, room = static_cast<int64_t>(kForwardBlocks) * sm_count();
+  const cudaError_t e = launch_chained(a.D == 128 ? norm_rope_kernel<128> : norm_rope_kernel<64>,
+                                       dim3(static_cast<unsigned>(want < room ? want : room)), dim3(kWarps * 32), 0, st, false, p);
   count_launch();
   return e == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
 }
@@ -291,14 +344,16 @@ int launch_norm_rope(const NormRopeArgs& a, cudaStream_t st) {
 int launch_norm_rope_backward(const NormRopeArgs& a, cudaStream_t st) {
   P p = params(a);
   if (a.wq) p.partial = a.partial;
-  const int64_t want = (p.units + kWarps - 1) / kWarps;
-  const int grid = static_cast<int>(want < kNormGradBlocks ? want : kNormGradBlocks);
-  cudaError_t e = launch_chained(a.D == 128 ? norm_rope_backward_kernel<128> : norm_rope_backward_kernel<64>, dim3(grid),
+  int64_t grid = (p.units + kWarps - 1) / kWarps;
+  const int64_t room = static_cast<int64_t>(kBackwardBlocks) * sm_count();
+  if (grid > room) grid = room;
+  if (grid > kNormGradBlocks) grid = kNormGradBlocks;
+  cudaError_t e = launch_chained(a.D == 128 ? norm_rope_backward_kernel<128> : norm_rope_backward_kernel<64>, dim3(static_cast<unsigned>(grid)),
                                  dim3(kWarps * 32), 0, st, false, p);
   count_launch();
   if (e != cudaSuccess) return ZQ_ERR_CUDA;
   if (a.wq) {
-    e = launch_chained(norm_grad_sum_kernel, dim3(2 * a.D / 8), dim3(256), 0, st, false, a.partial, grid, a.D, a.dwq, a.dwk);
+    e = launch_chained(norm_grad_sum_kernel, dim3(2 * a.D / 8), dim3(256), 0, st, false, a.partial, static_cast<int>(grid), a.D, a.dwq, a.dwk);
     count_launch();
   }
   return e == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
