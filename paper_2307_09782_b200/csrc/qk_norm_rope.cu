@@ -57,21 +57,33 @@ __device__ __forceinline__ float head_sum(float v) {
   return v;
 }
 
-// Unit u -> token, queries (0) or keys (1), first head.
+// A unit: token, chunk of it; queries (0) or keys (1), first head.  Divisions only for a warp's first one.
 struct Unit {
   int64_t t;
-  int which, h0;
+  int c, which, h0;
 };
 template <int LANES>
-__device__ __forceinline__ Unit unit_of(const P& p, int64_t u) {
+__device__ __forceinline__ void place(const P& p, Unit& n) {
+  n.which = n.c >= p.chunks[0];
+  n.h0 = (n.which ? n.c - p.chunks[0] : n.c) * kSteps * (32 / LANES);
+}
+template <int LANES>
+__device__ __forceinline__ Unit first_unit(const P& p, int64_t u) {
   const int per = p.chunks[0] + p.chunks[1];
-  Unit r;
-  r.t = u / per;
-  int c = static_cast<int>(u - r.t * per);
-  r.which = c >= p.chunks[0];
-  if (r.which) c -= p.chunks[0];
-  r.h0 = c * kSteps * (32 / LANES);
-  return r;
+  Unit n;
+  n.t = u / per;
+  n.c = static_cast<int>(u - n.t * per);
+  place<LANES>(p, n);
+  return n;
+}
+template <int LANES>
+__device__ __forceinline__ Unit next_unit(const P& p, Unit n) {
+  if (++n.c == p.chunks[0] + p.chunks[1]) {
+    n.c = 0;
+    ++n.t;
+  }
+  place<LANES>(p, n);
+  return n;
 }
 // A warp's units: contiguous, as even as can be.
 __device__ __forceinline__ void range_of(const P& p, int64_t& u0, int64_t& u1) {
@@ -149,16 +161,14 @@ __global__ void __launch_bounds__(kWarps * 32, kForwardBlocks) norm_rope_kernel(
   range_of(p, u, end);
   pdl_wait();
   if (u >= end) return;
-  Unit n = unit_of<L>(p, u);
+  Unit n = first_unit<L>(p, u);
   int pos = load_chained(p.positions + n.t), partner = lane;
   uint4 v[kSteps];
   load_rows<D>(p.x[n.which], p.ldx[n.which], n, p.heads[n.which], lane, v);
-  int64_t at = -1;     // token and kind the factors belong to
+  bool fresh = true;   // another token or kind: other factors
   float wc[8], ws[8];  // of the feature and of the one paired with it
   for (; u < end; ++u) {
-    const int64_t key = n.t * 2 + n.which;
-    if (key != at) {
-      at = key;
+    if (fresh) {
       load_angles<L>(p, pos, l, lane, wc, ws, partner);
       if (norm) {
         float w[8], wp[8];
@@ -171,7 +181,7 @@ __global__ void __launch_bounds__(kWarps * 32, kForwardBlocks) norm_rope_kernel(
     Unit next = n;
     uint4 ahead[kSteps];
     if (u + 1 < end) {
-      next = unit_of<L>(p, u + 1);
+      next = next_unit<L>(p, n);
       if (next.t != n.t) pos = load_chained(p.positions + next.t);
       load_rows<D>(p.x[next.which], p.ldx[next.which], next, p.heads[next.which], lane, ahead);
     }
@@ -193,6 +203,7 @@ __global__ void __launch_bounds__(kWarps * 32, kForwardBlocks) norm_rope_kernel(
       for (int e = 0; e < 8; ++e) y[e] = r * fmaf(z[e], wc[e], y[e] * ws[e]);
       if (h < p.heads[n.which]) *reinterpret_cast<uint4*>(out + static_cast<int64_t>(h) * D) = pack8(y);
     }
+    fresh = next.t != n.t || next.which != n.which;
     n = next;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) v[i] = ahead[i];
@@ -226,23 +237,20 @@ __global__ void __launch_bounds__(kWarps * 32, kBackwardBlocks) norm_rope_backwa
   };
   pdl_wait();
   if (u < end) {
-    Unit n = unit_of<L>(p, u);
+    Unit n = first_unit<L>(p, u);
     int pos = load_chained(p.positions + n.t), partner = lane;
     uint4 d[kBackSteps], v[kBackSteps];
-    int64_t at = -1;
+    bool fresh = true;
     float c[8], s[8], w[8];
     for (; u < end; ++u) {
       const int heads = p.heads[n.which];
-      const int64_t key = n.t * 2 + n.which;
-      if (key != at) {
-        if (norm && at >= 0 && n.which != static_cast<int>(at & 1)) settle(static_cast<int>(at & 1));
-        at = key;
+      if (fresh) {
         load_angles<L>(p, pos, l, lane, c, s, partner);
         if (norm) load8(p.w[n.which] + l * 8, w);
       }
       Unit next = n;
       if (u + 1 < end) {
-        next = unit_of<L>(p, u + 1);
+        next = next_unit<L>(p, n);
         if (next.t != n.t) pos = load_chained(p.positions + next.t);
       }
       const __nv_bfloat16* x = p.x[n.which] + n.t * p.ldx[n.which] + l * 8;
@@ -287,9 +295,10 @@ __global__ void __launch_bounds__(kWarps * 32, kBackwardBlocks) norm_rope_backwa
           if (h < heads) *reinterpret_cast<uint4*>(out + static_cast<int64_t>(h) * D) = pack8(g);
         }
       }
+      fresh = next.t != n.t || next.which != n.which;
+      if (norm && (next.which != n.which || u + 1 == end)) settle(n.which);
       n = next;
     }
-    if (norm) settle(static_cast<int>(at & 1));
   }
   if (!norm) return;
   __syncthreads();
