@@ -6,8 +6,10 @@
 //   O [128 rows, D] += P V                 FP16 x FP16; P from tensor memory, over the scores it was made of; the values'
 //                                          codes are widened in shared memory, once for 256 rows
 // Rows are the tensor core's lanes and a softmax thread's own: maxima and sums need no other thread.  A CTA works on two tiles of
-// 128 rows in turn, so that one's products run beside the other's softmax.  The running maximum only moves when a score exceeds
-// it by more than kSlack (in powers of two; FP16 has the room): the accumulator is then multiplied by the row's own warp.
+// 128 rows in turn, each in steps of 64 tokens whose scores alternate between two places in tensor memory: the next step's are there
+// when a softmax is done (with steps of 128 and one place it waited 2400 of 5800 cycles).  The running maximum only moves when a
+// score exceeds it by more than kSlack (in powers of two; FP16 has the room): the accumulator is then multiplied by the row's own
+// warp.
 //
 // Items (sequence, 256 rows, head) go to the CTAs in rounds, a sequence's last rows, which see most, first.  Where there are few
 // items, each is split over several CTAs along the tokens, and attention_join_rows_kernel adds up their results in order.
@@ -24,6 +26,7 @@ constexpr int kConvWarp0 = 8, kKeyWarp = 12, kValueWarp = 13, kMmaWarp = 14, kWa
 constexpr int kThreads = 512;
 constexpr int kRows = 256;       // of an item
 constexpr int kSegs = 4, kScaleSlots = 4;
+constexpr int kStep = 64;        // tokens of a step
 constexpr float kSlack = 7.0f;   // 2^(kShift + kSlack) = 32768 fits FP16
 enum { kErrKeysR = 61, kErrValuesR = 62, kErrMmaR = 63, kErrWalkR = 64, kErrSoftmaxR = 65, kErrConvertR = 66, kErrAlignR = 67 };
 // Registers per thread behind the set-up: softmax 184 (two warpgroups), converters and the others 72;
@@ -81,12 +84,13 @@ __device__ __forceinline__ int splits_of(int64_t items, int ctas) {
 
 struct alignas(16) Seg {
   int nt;            // tiles of tokens; 0: no more items; -1: none of this item are this CTA's
+  int steps;         // steps of 64 tokens in them: 2 per tile, the last has one where nobody sees its second half
   int tile0;         // the first
   int L, n;
   int b, h, first;
   int row0, rows;    // first of the item's rows among the sequence's, and their number
   int part;          // place among the partial results, or -1
-  int pad[2];
+  int pad;
 };
 static_assert(sizeof(Seg) == 48, "Seg");
 
@@ -130,14 +134,15 @@ __device__ __forceinline__ void store16(const P& p, int64_t at, const float* v) 
   }
 }
 
-// A softmax thread's tile of scores x (its row, 128 tokens) -> probabilities in tensor memory.  `lo`, `hi`: tokens of the tile that
-// the row sees (looked at with MASK).  May move the row's reference m and multiplies what is in the accumulator and l by the factor.
+// A softmax thread's step of scores x (its row, 64 tokens) -> probabilities in tensor memory.  `scales`: of its 4 groups of 16 tokens;
+// `lo`, `hi`: tokens of the step that the row sees (looked at with MASK).  May move the row's reference m and multiplies what is in
+// the accumulator and l by the factor.
 template <int D, bool MASK, typename Wait>
-__device__ __forceinline__ bool softmax_tile(float* x, const float4* scales, float c, int lo, int hi, float& m, float& l, uint32_t probs,
+__device__ __forceinline__ bool softmax_step(float* x, const float4* scales, float c, int lo, int hi, float& m, float& l, uint32_t probs,
                                              uint32_t acc, bool first, Wait accumulated) {
   float top = -INFINITY;
 #pragma unroll
-  for (int g = 0; g < 8; ++g) {
+  for (int g = 0; g < kStep / 16; ++g) {
     const float4 e = scales[g];
     float v = -INFINITY;
 #pragma unroll
@@ -171,7 +176,7 @@ __device__ __forceinline__ bool softmax_tile(float* x, const float4* scales, flo
   }
   const float base = kShift - (m == -INFINITY ? 0.0f : m);
 #pragma unroll
-  for (int g = 0; g < 8; g += 2) {
+  for (int g = 0; g < kStep / 16; g += 2) {
     uint32_t h[16];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -213,10 +218,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
   uint64_t* v_empty = v_full + C::kValueSlots;     // they are widened                                      (values' copies)
   uint64_t* w_full = v_empty + C::kValueSlots;     // [2] widened values                                    (MMA)
   uint64_t* w_empty = w_full + 2;                  // [2] their products are done                           (converters)
-  uint64_t* s_full = w_empty + 2;                  // [2 row tiles] scores                                  (softmax)
-  uint64_t* p_full = s_full + 2;                   // [2] probabilities, the accumulator up to date         (MMA)
-  uint64_t* pv_done = p_full + 2;                  // [2] they have been multiplied                         (MMA, softmax)
-  uint64_t* q_full = pv_done + 2;                  // an item's queries                                     (MMA, softmax)
+  uint64_t* s_full = w_empty + 2;                  // [2 row tiles][2] scores                               (softmax)
+  // (a barrier for each place: a warp can be a step ahead of another, or of the products)
+  uint64_t* p_full = s_full + 4;                   // [2][2] probabilities, the accumulator up to date      (MMA)
+  uint64_t* pv_done = p_full + 4;                  // [2][2] they have been multiplied                      (MMA, softmax)
+  uint64_t* q_full = pv_done + 4;                  // an item's queries                                     (MMA, softmax)
   uint64_t* q_empty = q_full + 1;                  // nobody needs them any more                            (converters)
   uint64_t* e_full = q_empty + 1;                  // [scale slots] a tile's block scales                   (softmax)
   uint64_t* e_empty = e_full + kScaleSlots;        // they have been used                                   (walk)
@@ -242,9 +248,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
     for (int i = 0; i < 2; ++i) {
       mbar_init(&w_full[i], 4);
       mbar_init(&w_empty[i], 1);
-      mbar_init(&s_full[i], 1);
-      mbar_init(&p_full[i], 4);
-      mbar_init(&pv_done[i], 1);
+      mbar_init(&s_full[2 * i], 1);
+      mbar_init(&s_full[2 * i + 1], 1);
+      mbar_init(&p_full[2 * i], 4);
+      mbar_init(&p_full[2 * i + 1], 4);
+      mbar_init(&pv_done[2 * i], 1);
+      mbar_init(&pv_done[2 * i + 1], 1);
     }
     mbar_init(q_full, 4);
     mbar_init(q_empty, 1 + 8);
@@ -372,71 +381,89 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
     const bool issuer = elect_one();
     const uint64_t kdesc = desc_rows<D>(smem_u32(smem + C::kOffKeys)), qdesc = desc_rows<D>(smem_u32(smem + C::kOffQueries));
     const uint64_t vdesc = desc_values(smem_u32(smem + C::kOffValues));
-    const uint32_t sdesc_i = umma_idesc_e4m3(kTok), odesc_i = idesc_f16(D, false, true);
+    const uint32_t sdesc_i = umma_idesc_e4m3(kStep), odesc_i = idesc_f16(D, false, true);
     Ring k, v;
-    int done[2] = {0, 0};  // products with values begun, for each row tile
+    int seg_queries = 0;
+    int done[2] = {0, 0};    // products with values begun, for each row tile
+    int scored[2] = {0, 0};  // steps of scores begun
     bool failed = false;
-    // scores of row tile q for the tile of keys in k; its columns hold the probabilities of the tile before until these are used
-    auto scores = [&](int q, bool last_q, bool last_tile) {
-      if (done[q] > 0 && !mbar_wait(&pv_done[q], (done[q] - 1) & 1, s_abort)) return false;
+    // Scores of row tile q for half `half` of the tile of keys in slot `slot`.  They go to the place of the probabilities two steps
+    // before, once these are used.
+    auto scores = [&](int q, int slot, int half, bool frees, bool last) {
+      const int buf = scored[q] & 1;
+      if (scored[q] >= 2 && !mbar_wait(&pv_done[q * 2 + buf], ((scored[q] >> 1) - 1) & 1, s_abort)) return false;
       tc_fence_after_sync();
       if (issuer) {
-        const uint64_t bd = kdesc + static_cast<uint64_t>((k.i * C::kTileBytes) >> 4);
+        const uint64_t bd = kdesc + static_cast<uint64_t>((slot * C::kTileBytes + half * kStep * D) >> 4);
 #pragma unroll
         for (int term = 0; term < 2; ++term) {
           const uint64_t ad = qdesc + static_cast<uint64_t>(((q * 2 + term) * C::kTileBytes) >> 4);
 #pragma unroll
-          for (int s = 0; s < D / 32; ++s) umma_f8(tmem + q * kTok, ad + s * 2, bd + s * 2, sdesc_i, (term > 0 || s > 0) ? 1u : 0u);
+          for (int s = 0; s < D / 32; ++s) umma_f8(tmem + q * kTok + buf * kStep, ad + s * 2, bd + s * 2, sdesc_i, (term > 0 || s > 0) ? 1u : 0u);
         }
-        umma_commit(&s_full[q]);
-        if (last_q) {
-          umma_commit(&k_empty[k.i]);
-          if (last_tile) umma_commit(q_empty);
-        }
+        umma_commit(&s_full[q * 2 + buf]);
+        if (frees) umma_commit(&k_empty[slot]);
+        if (last) umma_commit(q_empty);
       }
       __syncwarp();
+      ++scored[q];
       return true;
     };
     int nt;
     for (int seg = 0; any && !failed && segment(seg, nt); ++seg) {
-      const int nq = s_seg[seg % kSegs].rows > kTok ? 2 : 1;
+      const int nq = s_seg[seg % kSegs].rows > kTok ? 2 : 1, steps = s_seg[seg % kSegs].steps;
       __syncwarp();
       done_with(seg);
       if (nt < 0) continue;
-      if (!mbar_wait(q_full, seg & 1, s_abort) || !mbar_wait(&k_full[k.i], k.phase, s_abort)) {
+      if (!mbar_wait(q_full, seg_queries++ & 1, s_abort)) {
         failed = true;
         break;
       }
-      for (int q = 0; q < nq && !failed; ++q) failed = !scores(q, q + 1 == nq, nt == 1);
-      k.step(C::kKeySlots);
-      for (int j = 0; j < nt && !failed; ++j) {
-        for (int q = 0; q < nq; ++q) {
-          if (!mbar_wait(&p_full[q], done[q] & 1, s_abort) || (q == 0 && !mbar_wait(&w_full[v.i], v.phase, s_abort))) {
+      // step of keys: the tile's slot; a tile is waited for at its first step (by row tile 0, which is ahead), and released by the last
+      // row tile's scores for its last step
+      int k_step[2] = {0, 0};       // steps of scores begun in this item
+      Ring k_at[2] = {k, k};
+      auto next_scores = [&](int q) {
+        const int st = k_step[q];
+        if (st >= steps) return true;
+        if ((st & 1) == 0 && !mbar_wait(&k_full[k_at[q].i], k_at[q].phase, s_abort)) return false;
+        const bool ends = (st & 1) != 0 || st + 1 == steps;  // of the tile
+        if (!scores(q, k_at[q].i, st & 1, q + 1 == nq && ends, q + 1 == nq && st + 1 == steps)) return false;
+        if (ends) k_at[q].step(C::kKeySlots);
+        ++k_step[q];
+        return true;
+      };
+      failed = !next_scores(0) || (nq == 2 && !next_scores(1)) || !next_scores(0);
+      for (int st = 0; st < steps && !failed; ++st) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          if (q >= nq) break;
+          if (!mbar_wait(&p_full[q * 2 + (done[q] & 1)], (done[q] >> 1) & 1, s_abort) || (q == 0 && (st & 1) == 0 && !mbar_wait(&w_full[v.i], v.phase, s_abort))) {
             failed = true;
             break;
           }
           tc_fence_after_sync();
           if (issuer) {
-            const uint64_t bd = vdesc + static_cast<uint64_t>((v.i * C::kValueBytes) >> 4);
+            const uint64_t bd = vdesc + static_cast<uint64_t>((v.i * C::kValueBytes + (st & 1) * kStep * 128) >> 4);
+            const uint32_t probs = tmem + q * kTok + (done[q] & 1) * kStep;
 #pragma unroll
-            for (int s = 0; s < kTok / 16; ++s)
-              umma_f16_tmem_a(tmem + 256 + q * 128, tmem + q * kTok + s * 8, bd + s * (2048 >> 4), odesc_i, (j > 0 || s > 0) ? 1u : 0u);
-            umma_commit(&pv_done[q]);
-            if (q + 1 == nq) umma_commit(&w_empty[v.i]);
+            for (int s = 0; s < kStep / 16; ++s)
+              umma_f16_tmem_a(tmem + 256 + q * 128, probs + s * 8, bd + s * (2048 >> 4), odesc_i, (st > 0 || s > 0) ? 1u : 0u);
+            umma_commit(&pv_done[q * 2 + (done[q] & 1)]);
+            if (q + 1 == nq && ((st & 1) != 0 || st + 1 == steps)) umma_commit(&w_empty[v.i]);
           }
           __syncwarp();
           ++done[q];
-          if (j + 1 < nt) {
-            if (q == 0 && !mbar_wait(&k_full[k.i], k.phase, s_abort)) failed = true;
-            if (failed || !scores(q, q + 1 == nq, j + 2 == nt)) {
-              failed = true;
-              break;
-            }
+          // the other row tile's next scores: theirs waits for products that are long done
+          const bool ok = q == 0 && nq == 2 ? next_scores(1) : next_scores(0);
+          if (!ok) {
+            failed = true;
+            break;
           }
         }
-        v.step(2);
-        if (j + 1 < nt) k.step(C::kKeySlots);
+        if ((st & 1) != 0 || st + 1 == steps) v.step(2);
       }
+      k = k_at[0];
     }
     if (failed && issuer) fp8b::raise_error8(p.status, s_abort, kErrMmaR);
     // tensor memory is released only when every MMA has completed, also where another role has given up
@@ -482,9 +509,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
         const int64_t lo = p.window > 0 ? max(p0 + 1 - p.window, static_cast<int64_t>(0)) : 0;
         const int64_t hi = max(p.causal ? p1 + 1 : static_cast<int64_t>(s.L), static_cast<int64_t>(1));
         const int t0 = static_cast<int>(lo / kTok), nt = max(static_cast<int>((hi + kTok - 1) / kTok) - t0, 1);
+        const int half = hi - static_cast<int64_t>(t0 + nt - 1) * kTok <= kStep ? 1 : 0;  // nobody sees the last tile's second half
         const int c0 = static_cast<int>(static_cast<int64_t>(nt) * split / splits), c1 = static_cast<int>(static_cast<int64_t>(nt) * (split + 1) / splits);
         g.tile0 = t0 + c0;
         g.nt = c1 > c0 ? c1 - c0 : -1;
+        g.steps = 2 * (c1 - c0) - (c1 == nt ? half : 0);
         g.part = splits > 1 ? blockIdx.x : -1;
         if (!announce(g)) {
           ok = false;
@@ -591,7 +620,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
     int nt, tiles = 0, done = 0, items = 0;  // tiles: of the block scales; done: of this row tile
     for (int seg = 0; !failed && segment(seg, nt); ++seg) {
       const Seg& g = s_seg[seg % kSegs];
-      const int r = q * kTok + i, rows = g.rows, row = g.row0 + r, L = g.L, tile0 = g.tile0, h = g.h, part = g.part;
+      const int r = q * kTok + i, rows = g.rows, row = g.row0 + r, L = g.L, tile0 = g.tile0, h = g.h, part = g.part, steps = g.steps;
       const int64_t t = g.first + row / p.G;  // row of the tensors
       const int64_t pos = static_cast<int64_t>(L) - g.n + row / p.G;
       __syncwarp();
@@ -611,44 +640,51 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
         const float c = q * kTok < rows ? s_rows[r] : 0.0f;
         __syncwarp();
         if (lane == 0) mbar_arrive(q_empty);
-        for (int j = 0; j < nt; ++j, ++tiles) {
+        for (int st = 0; st < steps; ++st) {
           const int slot = tiles % kScaleSlots;
-          if (!fp8b::mbar_wait_all(&e_full[slot], (tiles / kScaleSlots) & 1, s_abort)) {
+          if ((st & 1) == 0 && !fp8b::mbar_wait_all(&e_full[slot], (tiles / kScaleSlots) & 1, s_abort)) {
             failed = true;
             break;
           }
           if (q * kTok < rows) {
-            if (!fp8b::mbar_wait_all(&s_full[q], done & 1, s_abort)) {
+            const int buf = done & 1;
+            if (!fp8b::mbar_wait_all(&s_full[q * 2 + buf], (done >> 1) & 1, s_abort)) {
               failed = true;
               break;
             }
             tc_fence_after_sync();
-            float x[128];
+            float x[kStep];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) fp8b::tmem_ld32(ts + k * 32, x + k * 32);
+            for (int k = 0; k < kStep / 32; ++k) fp8b::tmem_ld32(ts + buf * kStep + k * 32, x + k * 32);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) fp8b::tmem_ld_wait32(x + k * 32);
-            const int base = (tile0 + j) * kTok;
-            auto accumulated = [&] { return fp8b::mbar_wait_all(&pv_done[q], (done - 1) & 1, s_abort); };
-            const float4* e = table + slot * 8;
-            const bool ok = base >= lo_all && base + (kTok - 1) < hi_all
-                                ? softmax_tile<D, false>(x, e, c, 0, kTok, m, l, ts, to, j == 0, accumulated)
-                                : softmax_tile<D, true>(x, e, c, lo - base, hi - base, m, l, ts, to, j == 0, accumulated);
+            for (int k = 0; k < kStep / 32; ++k) fp8b::tmem_ld_wait32(x + k * 32);
+            const int base = tile0 * kTok + st * kStep;
+            auto accumulated = [&] { return fp8b::mbar_wait_all(&pv_done[q * 2 + (buf ^ 1)], ((done - 1) >> 1) & 1, s_abort); };
+            const float4* e = table + slot * 8 + (st & 1) * (kStep / 16);
+            const uint32_t probs = ts + buf * kStep;
+            const bool ok = base >= lo_all && base + (kStep - 1) < hi_all
+                                ? softmax_step<D, false>(x, e, c, 0, kStep, m, l, probs, to, st == 0, accumulated)
+                                : softmax_step<D, true>(x, e, c, lo - base, hi - base, m, l, probs, to, st == 0, accumulated);
             if (!ok) {
               failed = true;
               break;
             }
             tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&p_full[q]);
+            if (lane == 0) mbar_arrive(&p_full[q * 2 + buf]);
             ++done;
           }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&e_empty[slot]);
+          if ((st & 1) != 0 || st + 1 == steps) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&e_empty[slot]);
+            ++tiles;
+          }
         }
         if (failed) break;
         if (q * kTok < rows) {
-          if (!fp8b::mbar_wait_all(&pv_done[q], (done - 1) & 1, s_abort)) {
+          // the products of the last two steps
+          if ((steps > 1 && !fp8b::mbar_wait_all(&pv_done[q * 2 + (done & 1)], ((done - 2) >> 1) & 1, s_abort)) ||
+              !fp8b::mbar_wait_all(&pv_done[q * 2 + ((done - 1) & 1)], ((done - 1) >> 1) & 1, s_abort)) {
             failed = true;
             break;
           }
