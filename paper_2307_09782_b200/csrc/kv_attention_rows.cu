@@ -14,21 +14,22 @@
 // Items (sequence, 256 rows, head) go to the CTAs in rounds, a sequence's last rows, which see most, first.  Where there are few
 // items, each is split over several CTAs along the tokens, and attention_join_rows_kernel adds up their results in order.
 //
-// Warp roles: 0..3, 4..7 softmax and epilogue of the two tiles (thread = row), 8..11 queries and values (conversion), 12 keys'
-// copies, 13 values' copies, 14 MMAs, 15 the walk over the items and the block scales.
+// Warp roles: 0..3, 4..7 softmax and epilogue of the two tiles (thread = row), 8..11 queries and values (conversion), 12 copies, 13,
+// 14 MMAs of the two tiles (one warp for both spent 1400 cycles a step on issuing, and waited for either tile in turn), 15 the
+// walk over the items and the block scales.
 #include "kv_attention.cuh"
 
 namespace zq {
 namespace kv {
 namespace {
 
-constexpr int kConvWarp0 = 8, kKeyWarp = 12, kValueWarp = 13, kMmaWarp = 14, kWalkWarp = 15;
+constexpr int kConvWarp0 = 8, kCopyWarp = 12, kMmaWarp = 13, kWalkWarp = 15;  // kMmaWarp + 1: of the second row tile
 constexpr int kThreads = 512;
 constexpr int kRows = 256;       // of an item
 constexpr int kSegs = 4, kScaleSlots = 4;
 constexpr int kStep = 64;        // tokens of a step
 constexpr float kSlack = 7.0f;   // 2^(kShift + kSlack) = 32768 fits FP16
-enum { kErrKeysR = 61, kErrValuesR = 62, kErrMmaR = 63, kErrWalkR = 64, kErrSoftmaxR = 65, kErrConvertR = 66, kErrAlignR = 67 };
+enum { kErrCopyR = 61, kErrMmaR = 63, kErrWalkR = 64, kErrSoftmaxR = 65, kErrConvertR = 66, kErrAlignR = 67 };
 // Registers per thread behind the set-up: softmax 184 (two warpgroups), converters and the others 72;
 // 2 x 184 + 2 x 72 = 512, the four warpgroups' 4 x 128 at launch.
 
@@ -144,13 +145,14 @@ __device__ __forceinline__ bool softmax_step(float* x, const float4* scales, flo
 #pragma unroll
   for (int g = 0; g < kStep / 16; ++g) {
     const float4 e = scales[g];
-    float v = -INFINITY;
+    float w[4];  // (four at a time: one after the other a maximum takes 4 cycles each)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int at = g * 16 + i;
       if (MASK && (at < lo || at >= hi)) x[at] = -INFINITY;
-      v = fmaxf(v, x[at]);
+      w[i & 3] = i < 4 ? x[at] : fmaxf(w[i & 3], x[at]);
     }
+    const float v = fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
     top = fmaxf(top, fmaf(v, e.x * c, e.y));  // (0 x infinity where all is masked: NaN, which fmaxf drops)
   }
   // a row that has seen nothing yet takes the first maximum as it is: its sums are zero
@@ -213,9 +215,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bar = reinterpret_cast<uint64_t*>(smem + C::kOffBars);
   uint64_t* k_full = bar;                          // [key slots] a tile's keys have landed                 (MMA)
-  uint64_t* k_empty = k_full + C::kKeySlots;       // their products are done                               (keys' copies)
+  uint64_t* k_empty = k_full + C::kKeySlots;       // their products are done                               (copies)
   uint64_t* v_full = k_empty + C::kKeySlots;       // [value slots] a tile's values have landed             (converters)
-  uint64_t* v_empty = v_full + C::kValueSlots;     // they are widened                                      (values' copies)
+  uint64_t* v_empty = v_full + C::kValueSlots;     // they are widened                                      (copies)
   uint64_t* w_full = v_empty + C::kValueSlots;     // [2] widened values                                    (MMA)
   uint64_t* w_empty = w_full + 2;                  // [2] their products are done                           (converters)
   uint64_t* s_full = w_empty + 2;                  // [2 row tiles][2] scores                               (softmax)
@@ -228,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
   uint64_t* e_empty = e_full + kScaleSlots;        // they have been used                                   (walk)
   uint64_t* g_full = e_empty + kScaleSlots;        // [kSegs] an item is announced                          (all)
   uint64_t* g_empty = g_full + kSegs;              // [kSegs] everybody is through with it                  (walk)
-  uint64_t* drain = g_empty + kSegs;
+  uint64_t* drain = g_empty + kSegs;               // [2]
   int64_t* s_scan = reinterpret_cast<int64_t*>(smem + C::kOffScan);
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_scan + 20);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
@@ -239,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kKeySlots; ++i) {
       mbar_init(&k_full[i], 1);
-      mbar_init(&k_empty[i], 1);
+      mbar_init(&k_empty[i], 2);
     }
     for (int i = 0; i < C::kValueSlots; ++i) {
       mbar_init(&v_full[i], 1);
@@ -247,7 +249,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&w_full[i], 4);
-      mbar_init(&w_empty[i], 1);
+      mbar_init(&w_empty[i], 2);
       mbar_init(&s_full[2 * i], 1);
       mbar_init(&s_full[2 * i + 1], 1);
       mbar_init(&p_full[2 * i], 4);
@@ -256,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       mbar_init(&pv_done[2 * i + 1], 1);
     }
     mbar_init(q_full, 4);
-    mbar_init(q_empty, 1 + 8);
+    mbar_init(q_empty, 2 + 8);
     for (int i = 0; i < kScaleSlots; ++i) {
       mbar_init(&e_full[i], 1);
       mbar_init(&e_empty[i], 8);
@@ -265,7 +267,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       mbar_init(&g_full[i], 1);
       mbar_init(&g_empty[i], kThreads / 32 - 1);
     }
-    mbar_init(drain, 1);
+    mbar_init(&drain[0], 1);
+    mbar_init(&drain[1], 1);
     *s_abort = 0;
     fence_mbar_init();
     if ((smem_u32(smem) & 1023u) != 0) fp8b::raise_error8(p.status, s_abort, kErrAlignR);
@@ -328,16 +331,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
     if (lane == 0) mbar_arrive(&g_empty[seg % kSegs]);
   };
 
-  if (warp == kKeyWarp || warp == kValueWarp) {
-    // ---- copies: a lane per page of the tile
+  if (warp == kCopyWarp) {
+    // ---- copies: a lane per page of the tile, keys, then values
     fp8b::regs_give<72>();
-    const bool keys = warp == kKeyWarp;
-    const int slots = keys ? C::kKeySlots : C::kValueSlots;
-    uint64_t *full = keys ? k_full : v_full, *empty = keys ? k_empty : v_empty;
-    uint8_t* to = smem + (keys ? C::kOffKeys : C::kOffCodes);
     const int per = kTok / p.c.page, page_bytes = p.c.page * D;
-    Ring r;
-    int issued = 0, nt;
+    Ring rk, rv;
+    int keys = 0, values = 0, nt;
     bool ok = any;
     for (int seg = 0; ok && segment(seg, nt); ++seg) {
       const Seg& g = s_seg[seg % kSegs];
@@ -348,128 +347,130 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       done_with(seg);
       for (int j = 0; j < nt; ++j) {
         const int page = pages.get(p.c, (t0 + j) * per, lane);
-        if (issued >= slots && !mbar_wait_warp(&empty[r.i], r.phase ^ 1, s_abort)) {
-          if (lane == 0) fp8b::raise_error8(p.status, s_abort, keys ? kErrKeysR : kErrValuesR);
-          ok = false;
-          break;
-        }
         const bool has = lane < per && page >= 0;
-        const uint32_t n = __popc(__ballot_sync(0xFFFFFFFFu, has));
-        if (lane == 0) mbar_arrive_expect_tx(&full[r.i], n * page_bytes);
+        const uint32_t bytes = __popc(__ballot_sync(0xFFFFFFFFu, has)) * page_bytes;
+        const int64_t block = block_at(p.c, has ? page : 0, 0, h);
+        if (keys >= C::kKeySlots && !mbar_wait_warp(&k_empty[rk.i], rk.phase ^ 1, s_abort)) ok = false;
+        if (!ok) break;
+        if (lane == 0) mbar_arrive_expect_tx(&k_full[rk.i], bytes);
         __syncwarp();
-        if (has) {
-          uint8_t* dst = to + r.i * C::kTileBytes + lane * page_bytes;
-          const int64_t block = block_at(p.c, page, keys ? 0 : 1, h);
-          if (keys)
-            tma_load_3d(dst, &tm, 0, 0, static_cast<int>(block), &full[r.i]);
-          else
-            bulk_load(dst, p.c.codes + block * page_bytes, page_bytes, &full[r.i]);
-        }
+        if (has) tma_load_3d(smem + C::kOffKeys + rk.i * C::kTileBytes + lane * page_bytes, &tm, 0, 0, static_cast<int>(block), &k_full[rk.i]);
         __syncwarp();
-        ++issued;
-        r.step(slots);
+        ++keys;
+        if (values >= C::kValueSlots && !mbar_wait_warp(&v_empty[rv.i], rv.phase ^ 1, s_abort)) ok = false;
+        if (!ok) break;
+        if (lane == 0) mbar_arrive_expect_tx(&v_full[rv.i], bytes);
+        __syncwarp();
+        if (has) bulk_load(smem + C::kOffCodes + rv.i * C::kTileBytes + lane * page_bytes, p.c.codes + (block + p.c.H) * page_bytes, page_bytes, &v_full[rv.i]);
+        __syncwarp();
+        ++values;
+        rk.step(C::kKeySlots);
+        rv.step(C::kValueSlots);
       }
     }
-    // never leave with copies still in flight
-    for (int i = max(0, issued - slots); i < issued; ++i) {
+    if (!ok && any && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrCopyR);
+    // never leave with copies still in flight (only those that were asked for are waited for)
+    for (int i = max(0, keys - C::kKeySlots); i < keys; ++i) {
       uint32_t spin = 0;
-      while (!mbar_try_wait(&full[i % slots], (i / slots) & 1) && ++spin < kSpinLimit) {
+      while (!mbar_try_wait(&k_full[i % C::kKeySlots], (i / C::kKeySlots) & 1) && ++spin < kSpinLimit) {
       }
     }
-  } else if (warp == kMmaWarp) {
+    for (int i = max(0, values - C::kValueSlots); i < values; ++i) {
+      uint32_t spin = 0;
+      while (!mbar_try_wait(&v_full[i % C::kValueSlots], (i / C::kValueSlots) & 1) && ++spin < kSpinLimit) {
+      }
+    }
+  } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
+    // ---- products of row tile q
     fp8b::regs_give<72>();
+    const int q = warp - kMmaWarp;
     const bool issuer = elect_one();
-    const uint64_t kdesc = desc_rows<D>(smem_u32(smem + C::kOffKeys)), qdesc = desc_rows<D>(smem_u32(smem + C::kOffQueries));
+    const uint64_t kdesc = desc_rows<D>(smem_u32(smem + C::kOffKeys)), qdesc = desc_rows<D>(smem_u32(smem + C::kOffQueries + q * 2 * C::kTileBytes));
     const uint64_t vdesc = desc_values(smem_u32(smem + C::kOffValues));
     const uint32_t sdesc_i = umma_idesc_e4m3(kStep), odesc_i = idesc_f16(D, false, true);
+    const uint32_t to_s = tmem + q * kTok, to_o = tmem + 256 + q * 128;
     Ring k, v;
-    int seg_queries = 0;
-    int done[2] = {0, 0};    // products with values begun, for each row tile
-    int scored[2] = {0, 0};  // steps of scores begun
+    int done = 0, scored = 0, items = 0;  // steps of products with values, and of scores, begun
     bool failed = false;
-    // Scores of row tile q for half `half` of the tile of keys in slot `slot`.  They go to the place of the probabilities two steps
-    // before, once these are used.
-    auto scores = [&](int q, int slot, int half, bool frees, bool last) {
-      const int buf = scored[q] & 1;
-      if (scored[q] >= 2 && !mbar_wait(&pv_done[q * 2 + buf], ((scored[q] >> 1) - 1) & 1, s_abort)) return false;
-      tc_fence_after_sync();
-      if (issuer) {
-        const uint64_t bd = kdesc + static_cast<uint64_t>((slot * C::kTileBytes + half * kStep * D) >> 4);
-#pragma unroll
-        for (int term = 0; term < 2; ++term) {
-          const uint64_t ad = qdesc + static_cast<uint64_t>(((q * 2 + term) * C::kTileBytes) >> 4);
-#pragma unroll
-          for (int s = 0; s < D / 32; ++s) umma_f8(tmem + q * kTok + buf * kStep, ad + s * 2, bd + s * 2, sdesc_i, (term > 0 || s > 0) ? 1u : 0u);
-        }
-        umma_commit(&s_full[q * 2 + buf]);
-        if (frees) umma_commit(&k_empty[slot]);
-        if (last) umma_commit(q_empty);
-      }
-      __syncwarp();
-      ++scored[q];
-      return true;
-    };
     int nt;
     for (int seg = 0; any && !failed && segment(seg, nt); ++seg) {
-      const int nq = s_seg[seg % kSegs].rows > kTok ? 2 : 1, steps = s_seg[seg % kSegs].steps;
+      const bool active = q == 0 || s_seg[seg % kSegs].rows > kTok;
+      const int steps = s_seg[seg % kSegs].steps;
       __syncwarp();
       done_with(seg);
       if (nt < 0) continue;
-      if (!mbar_wait(q_full, seg_queries++ & 1, s_abort)) {
+      if (!mbar_wait(q_full, items++ & 1, s_abort)) {
         failed = true;
         break;
       }
-      // step of keys: the tile's slot; a tile is waited for at its first step (by row tile 0, which is ahead), and released by the last
-      // row tile's scores for its last step
-      int k_step[2] = {0, 0};       // steps of scores begun in this item
-      Ring k_at[2] = {k, k};
-      auto next_scores = [&](int q) {
-        const int st = k_step[q];
-        if (st >= steps) return true;
-        if ((st & 1) == 0 && !mbar_wait(&k_full[k_at[q].i], k_at[q].phase, s_abort)) return false;
-        const bool ends = (st & 1) != 0 || st + 1 == steps;  // of the tile
-        if (!scores(q, k_at[q].i, st & 1, q + 1 == nq && ends, q + 1 == nq && st + 1 == steps)) return false;
-        if (ends) k_at[q].step(C::kKeySlots);
-        ++k_step[q];
+      if (!active) {  // no rows: the other tile's operands pass by
+        if (lane == 0) mbar_arrive(q_empty);
+        for (int j = 0; j < nt; ++j) {
+          if (!mbar_wait_warp(&k_full[k.i], k.phase, s_abort)) failed = true;
+          if (!failed && lane == 0) mbar_arrive(&k_empty[k.i]);
+          if (!failed && !mbar_wait_warp(&w_full[v.i], v.phase, s_abort)) failed = true;
+          if (failed) break;
+          if (lane == 0) mbar_arrive(&w_empty[v.i]);
+          __syncwarp();
+          k.step(C::kKeySlots);
+          v.step(2);
+        }
+        continue;
+      }
+      // Scores of the item's next step.  They go to the place of the probabilities two steps before, once these are used.
+      int at = 0;
+      auto scores = [&] {
+        if (at >= steps) return true;
+        const int buf = scored & 1, half = at & 1;
+        const bool ends = half != 0 || at + 1 == steps;  // of the tile of keys
+        if (half == 0 && !mbar_wait(&k_full[k.i], k.phase, s_abort)) return false;
+        if (scored >= 2 && !mbar_wait(&pv_done[q * 2 + buf], ((scored >> 1) - 1) & 1, s_abort)) return false;
+        tc_fence_after_sync();
+        if (issuer) {
+          const uint64_t bd = kdesc + static_cast<uint64_t>((k.i * C::kTileBytes + half * kStep * D) >> 4);
+#pragma unroll
+          for (int term = 0; term < 2; ++term)
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s)
+              umma_f8(to_s + buf * kStep, qdesc + static_cast<uint64_t>((term * C::kTileBytes) >> 4) + s * 2, bd + s * 2, sdesc_i, (term > 0 || s > 0) ? 1u : 0u);
+          umma_commit(&s_full[q * 2 + buf]);
+          if (ends) umma_commit(&k_empty[k.i]);
+          if (at + 1 == steps) umma_commit(q_empty);
+        }
+        __syncwarp();
+        if (ends) k.step(C::kKeySlots);
+        ++scored;
+        ++at;
         return true;
       };
-      failed = !next_scores(0) || (nq == 2 && !next_scores(1)) || !next_scores(0);
+      failed = !scores() || !scores();
       for (int st = 0; st < steps && !failed; ++st) {
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          if (q >= nq) break;
-          if (!mbar_wait(&p_full[q * 2 + (done[q] & 1)], (done[q] >> 1) & 1, s_abort) || (q == 0 && (st & 1) == 0 && !mbar_wait(&w_full[v.i], v.phase, s_abort))) {
-            failed = true;
-            break;
-          }
-          tc_fence_after_sync();
-          if (issuer) {
-            const uint64_t bd = vdesc + static_cast<uint64_t>((v.i * C::kValueBytes + (st & 1) * kStep * 128) >> 4);
-            const uint32_t probs = tmem + q * kTok + (done[q] & 1) * kStep;
-#pragma unroll
-            for (int s = 0; s < kStep / 16; ++s)
-              umma_f16_tmem_a(tmem + 256 + q * 128, probs + s * 8, bd + s * (2048 >> 4), odesc_i, (st > 0 || s > 0) ? 1u : 0u);
-            umma_commit(&pv_done[q * 2 + (done[q] & 1)]);
-            if (q + 1 == nq && ((st & 1) != 0 || st + 1 == steps)) umma_commit(&w_empty[v.i]);
-          }
-          __syncwarp();
-          ++done[q];
-          // the other row tile's next scores: theirs waits for products that are long done
-          const bool ok = q == 0 && nq == 2 ? next_scores(1) : next_scores(0);
-          if (!ok) {
-            failed = true;
-            break;
-          }
+        const int buf = done & 1;
+        const bool ends = (st & 1) != 0 || st + 1 == steps;
+        if (((st & 1) == 0 && !mbar_wait(&w_full[v.i], v.phase, s_abort)) || !mbar_wait(&p_full[q * 2 + buf], (done >> 1) & 1, s_abort)) {
+          failed = true;
+          break;
         }
-        if ((st & 1) != 0 || st + 1 == steps) v.step(2);
+        tc_fence_after_sync();
+        if (issuer) {
+          const uint64_t bd = vdesc + static_cast<uint64_t>((v.i * C::kValueBytes + (st & 1) * kStep * 128) >> 4);
+#pragma unroll
+          for (int s = 0; s < kStep / 16; ++s)
+            umma_f16_tmem_a(to_o, to_s + buf * kStep + s * 8, bd + s * (2048 >> 4), odesc_i, (st > 0 || s > 0) ? 1u : 0u);
+          umma_commit(&pv_done[q * 2 + buf]);
+          if (ends) umma_commit(&w_empty[v.i]);
+        }
+        __syncwarp();
+        ++done;
+        if (ends) v.step(2);
+        failed = !scores();
       }
-      k = k_at[0];
     }
     if (failed && issuer) fp8b::raise_error8(p.status, s_abort, kErrMmaR);
     // tensor memory is released only when every MMA has completed, also where another role has given up
-    if (issuer) umma_commit(drain);
+    if (issuer) umma_commit(&drain[q]);
     uint32_t spin = 0;
-    while (!mbar_try_wait(drain, 0) && ++spin < kSpinLimit) {
+    while (!mbar_try_wait(&drain[q], 0) && ++spin < kSpinLimit) {
     }
     __syncwarp();
   } else if (warp == kWalkWarp) {
