@@ -161,23 +161,37 @@ __device__ __forceinline__ RowScale row_scale(uint32_t amax_bits) {  // bits of 
   r.down = finite ? __uint_as_float(static_cast<uint32_t>(e - 7) << 23) : __uint_as_float(0x7FC00000u);
   return r;
 }
-__device__ __forceinline__ uint32_t absmax_bits8(uint4 v) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  uint32_t a = 0u;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) a = max(a, max((w[i] << 16) & 0x7FFF0000u, w[i] & 0x7FFF0000u));
-  return a;
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
 }
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t absmax_bits8(uint4 v) {
+  const uint32_t m = max_u16x2(max_u16x2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), max_u16x2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+  return max(m << 16, m & 0xFFFF0000u);
+}
+// Eight numbers times `up` as two E4M3 numbers each.  In between they are FP16, which holds them: 8 bits, the largest below 2^8
+// (what is below FP16's 2^-24 is zero in E4M3 too).  A row that is not finite has up = 0, NaN for what is not finite in it, and a
+// factor that makes all of its scores NaN.
 __device__ __forceinline__ void split8(uint4 v, float up, uint2& first, uint2& second) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
   uint32_t a[4], b[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    // (a row that is not finite: zeros; its scores become NaN by the row's factor)
-    const float x = up == 0.0f ? 0.0f : bf16_lo(w[i]) * up, y = up == 0.0f ? 0.0f : bf16_hi(w[i]) * up;
-    a[i] = cvt_e4m3x2(x, y);
-    const float2 f = fp8b::decode2(static_cast<uint16_t>(a[i]));
-    b[i] = cvt_e4m3x2(x - f.x, y - f.y);
+    const uint32_t x = pack_f16(bf16_lo(w[i]) * up, bf16_hi(w[i]) * up);
+    uint16_t c, d;
+    uint32_t y;
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(c) : "r"(x));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y) : "h"(c));
+    asm("sub.f16x2 %0, %1, %2;" : "=r"(y) : "r"(x), "r"(y));
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(d) : "r"(y));
+    a[i] = c;
+    b[i] = d;
   }
   first = make_uint2(a[0] | (a[1] << 16), a[2] | (a[3] << 16));
   second = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
@@ -232,11 +246,6 @@ struct PageWalk {
 __device__ __forceinline__ float warp_max(float v) {
   float r;
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-  return r;
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
 

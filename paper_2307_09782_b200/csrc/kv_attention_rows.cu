@@ -11,8 +11,10 @@
 // score exceeds it by more than kSlack (in powers of two; FP16 has the room): the accumulator is then multiplied by the row's own
 // warp.
 //
-// Items (sequence, 256 rows, head) go to the CTAs in rounds, a sequence's last rows, which see most, first.  Where there are few
-// items, each is split over several CTAs along the tokens, and attention_join_rows_kernel adds up their results in order.
+// All items (sequence, 256 rows, head) stand in a row, each as long as its tokens and what it costs to begin and end one, and every CTA
+// gets an equal part of the row (whole items in rounds: a prompt of 8191 tokens 732 us instead of 655).  An item that reaches over a
+// boundary is worked on by the CTAs on both sides (by many, where there are few items), and attention_join_rows_kernel adds up their
+// results in order.
 //
 // Warp roles: 0..3, 4..7 softmax and epilogue of the two tiles (thread = row), 8..11 queries and values (conversion), 12 copies, 13,
 // 14 MMAs of the two tiles (one warp for both spent 1400 cycles a step on issuing, and waited for either tile in turn), 15 the
@@ -28,6 +30,10 @@ constexpr int kThreads = 512;
 constexpr int kRows = 256;       // of an item
 constexpr int kSegs = 4, kScaleSlots = 4;
 constexpr int kStep = 64;        // tokens of a step
+// What beginning and ending an item costs, in tokens: 13000 cycles, and the masked steps at its ends (a prompt of 8191 tokens took
+// 824, 681, 658, 670 us with 256, 512, 768, 1024).
+constexpr int kItemTokens = 768;
+constexpr int kLeastTiles = 4;   // no item is split for less (chunks of 777 tokens behind others: 2 262 us, 4 255, 8 270)
 constexpr float kSlack = 7.0f;   // 2^(kShift + kSlack) = 32768 fits FP16
 enum { kErrCopyR = 61, kErrMmaR = 63, kErrWalkR = 64, kErrSoftmaxR = 65, kErrConvertR = 66, kErrAlignR = 67 };
 // Registers per thread behind the set-up: softmax 184 (two warpgroups), converters and the others 72;
@@ -37,14 +43,16 @@ struct P {
   Cache c;
   const __nv_bfloat16* q;
   int64_t ldq;
-  int G;
+  int G, boxes;
   float scale_log2;
   int causal, window;
   void* out;
   int64_t ldo;
   int f32;
   float* lse;
-  float* partial;  // [CTAs][256 (D + 2)]
+  int4* shared;    // [CTAs] the item that begins in the CTA and goes on in the next: sequence, number, 1 (0: none does); and of the
+                   // item that came from the CTA before: 1 it goes on, 2 it ends here (0: none came)
+  float* partial;  // [CTAs][2: what came from the CTA before, what goes on][256 (D + 2)]
   int* status;
 };
 
@@ -78,13 +86,90 @@ __device__ __forceinline__ Seq seq_of(const P& p, int b) {
   s.blocks = rows > kFewRows ? static_cast<int>((rows + kRows - 1) / kRows) : 0;
   return s;
 }
-// CTAs that share an item.
-__device__ __forceinline__ int splits_of(int64_t items, int ctas) {
-  return items > 0 && 2 * items <= ctas ? static_cast<int>(ctas / items) : 1;
+// An item's tokens, in tiles: those that some of its rows see (at least one).
+struct Item {
+  int t0, nt;
+  int half;  // 1: nobody sees the last tile's second half
+};
+__device__ __forceinline__ Item item_of(const P& p, const Seq& s, int64_t row0, int rows) {
+  const int64_t p0 = static_cast<int64_t>(s.L) - s.n + row0 / p.G, p1 = static_cast<int64_t>(s.L) - s.n + (row0 + rows - 1) / p.G;
+  const int64_t lo = p.window > 0 ? max(p0 + 1 - p.window, static_cast<int64_t>(0)) : 0;
+  const int64_t hi = max(p.causal ? p1 + 1 : static_cast<int64_t>(s.L), static_cast<int64_t>(1));
+  Item i;
+  i.t0 = static_cast<int>(lo / kTok);
+  i.nt = max(static_cast<int>((hi + kTok - 1) / kTok) - i.t0, 1);
+  i.half = hi - static_cast<int64_t>(i.t0 + i.nt - 1) * kTok <= kStep ? 1 : 0;
+  return i;
+}
+// Rows of a sequence's block k, counted from the last, which sees most.
+__device__ __forceinline__ int64_t block_row0(const Seq& s, int k) { return static_cast<int64_t>(s.blocks - 1 - k) * kRows; }
+__device__ __forceinline__ int block_rows(const P& p, const Seq& s, int64_t row0) {
+  return static_cast<int>(min(static_cast<int64_t>(s.n) * p.G - row0, static_cast<int64_t>(kRows)));
+}
+
+// Lengths of a sequence's items in the row of all, in 1 / G tokens (a block's rows are 256 / G tokens), and sums of them in closed
+// form: the blocks' tokens fall by 256 from one to the next, except where a window cuts them off.
+struct Lengths {
+  int64_t top, cap, item;
+  __device__ __forceinline__ Lengths(const P& p, const Seq& s) {
+    const int64_t all = static_cast<int64_t>(s.L) * p.G;
+    item = kItemTokens * static_cast<int64_t>(p.G);
+    cap = p.window > 0 ? min(static_cast<int64_t>(p.window) * p.G + kRows, all) : all;
+    top = p.causal ? max(static_cast<int64_t>(s.L) - s.n, static_cast<int64_t>(0)) * p.G + static_cast<int64_t>(s.blocks) * kRows : kNone;
+  }
+  static constexpr int64_t kNone = int64_t{1} << 62;
+  __device__ __forceinline__ int64_t of(int k) const { return (k == 0 ? cap : min(top - static_cast<int64_t>(k) * kRows, cap)) + item; }
+  __device__ __forceinline__ int64_t before(int k) const {  // of the blocks 0 .. k - 1
+    if (k == 0) return 0;
+    // of 1 .. k - 1 the first `cut` are cut off
+    int64_t cut = k - 1;
+    if (top != kNone) cut = max(min((top - cap + kRows - 1) / kRows - 1, cut), static_cast<int64_t>(0));
+    const int64_t rest = k - 1 - cut;
+    int64_t sum = (1 + cut) * cap + k * item;
+    if (rest > 0) sum += rest * top - rest * (k + cut) * (kRows / 2);
+    return sum;
+  }
+};
+__device__ __forceinline__ int64_t length_of(const P& p, const Seq& s) { return s.blocks > 0 ? Lengths(p, s).before(s.blocks) * p.c.H : 0; }
+// Begin of a CTA's part of a row of that length.
+__device__ __forceinline__ int64_t part_begin(int64_t total, int cta, int ctas) { return total / ctas * cta + total % ctas * cta / ctas; }
+
+// A place in the row: a sequence, its item (block x heads + head; all of them: its end), and a tile of that.
+struct Place {
+  int b, k, tile;
+};
+__device__ __forceinline__ Place place_of(const P& p, const Seq& s, int b, int64_t at, int64_t share) {
+  const Lengths w(p, s);
+  int k = 0;
+  for (int n = s.blocks; n > 1;) {  // the last block that begins at or before `at` is among the n from k on
+    const int m = n / 2;
+    if (w.before(k + m) * p.c.H <= at) {
+      k += m;
+      n -= m;
+    } else {
+      n = m;
+    }
+  }
+  const int64_t length = w.of(k), in = at - w.before(k) * p.c.H;
+  const int h = static_cast<int>(min(in / length, static_cast<int64_t>(p.c.H - 1)));
+  const int64_t off = in - h * length;
+  // too short a piece is left with its neighbour
+  const int64_t least = min(share / 8, static_cast<int64_t>(kLeastTiles * kTok) * p.G);
+  const int64_t row0 = block_row0(s, k);
+  const int nt = item_of(p, s, row0, block_rows(p, s, row0)).nt;
+  int tile = static_cast<int>(min(off * nt / length, static_cast<int64_t>(nt - 1)));
+  int item = k * p.c.H + h;
+  if (off < least) {
+    tile = 0;
+  } else if (length - off < least) {
+    tile = 0;
+    ++item;
+  }
+  return {b, item, tile};
 }
 
 struct alignas(16) Seg {
-  int nt;            // tiles of tokens; 0: no more items; -1: none of this item are this CTA's
+  int nt;            // tiles of tokens; 0: no more items
   int steps;         // steps of 64 tokens in them: 2 per tile, the last has one where nobody sees its second half
   int tile0;         // the first
   int L, n;
@@ -210,7 +295,7 @@ __device__ __forceinline__ bool softmax_step(float* x, const float4* scales, flo
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __grid_constant__ CUtensorMap tm, const P p) {
+__global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ CUtensorMap tm_q, const P p) {
   using C = Cfg<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bar = reinterpret_cast<uint64_t*>(smem + C::kOffBars);
@@ -226,7 +311,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
   uint64_t* pv_done = p_full + 4;                  // [2][2] they have been multiplied                      (MMA, softmax)
   uint64_t* q_full = pv_done + 4;                  // an item's queries                                     (MMA, softmax)
   uint64_t* q_empty = q_full + 1;                  // nobody needs them any more                            (converters)
-  uint64_t* e_full = q_empty + 1;                  // [scale slots] a tile's block scales                   (softmax)
+  uint64_t* r_full = q_empty + 1;                  // an item's queries have landed                         (converters)
+  uint64_t* e_full = r_full + 1;                   // [scale slots] a tile's block scales                   (softmax)
   uint64_t* e_empty = e_full + kScaleSlots;        // they have been used                                   (walk)
   uint64_t* g_full = e_empty + kScaleSlots;        // [kSegs] an item is announced                          (all)
   uint64_t* g_empty = g_full + kSegs;              // [kSegs] everybody is through with it                  (walk)
@@ -259,6 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
     }
     mbar_init(q_full, 4);
     mbar_init(q_empty, 2 + 8);
+    mbar_init(r_full, 1);
     for (int i = 0; i < kScaleSlots; ++i) {
       mbar_init(&e_full[i], 1);
       mbar_init(&e_empty[i], 8);
@@ -273,16 +360,18 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
     fence_mbar_init();
     if ((smem_u32(smem) & 1023u) != 0) fp8b::raise_error8(p.status, s_abort, kErrAlignR);
     prefetch_tensormap(&tm);
+    if (p.boxes) prefetch_tensormap(&tm_q);
   }
   if (warp == kMmaWarp) tmem_alloc(s_tmem, 512);
   pdl_launch_dependents();
   pdl_wait();
-  // ---- items before each thread's sequences, by a scan over the block; the thread that has this CTA's first one leaves it
+  // ---- lengths of the items before each thread's sequences, by a scan over the block; the threads that have them leave the ends of
+  // this CTA's part
   {
     const int per = (p.c.B + kThreads - 1) / kThreads;
     const int b0 = min(static_cast<int>(threadIdx.x) * per, p.c.B), b1 = min(b0 + per, p.c.B);
     int64_t mine = 0;
-    for (int b = b0; b < b1; ++b) mine += static_cast<int64_t>(seq_of(p, b).blocks) * p.c.H;
+    for (int b = b0; b < b1; ++b) mine += length_of(p, seq_of(p, b));
     int64_t incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -299,28 +388,31 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       total += s_scan[w];
     }
     const int64_t begin = before + incl - mine;
-    const int splits = splits_of(total, gridDim.x);
-    const int64_t item = blockIdx.x / splits;
+    Place* ends = reinterpret_cast<Place*>(s_scan + 17);
     if (threadIdx.x == 0) {
       s_scan[16] = total;
-      s_scan[17] = splits;
+      ends[1] = {p.c.B, 0, 0};
     }
-    if (item < total && begin <= item && item < begin + mine) {
-      int64_t at = begin;
-      int b = b0;
-      for (;; ++b) {
-        const int64_t n = static_cast<int64_t>(seq_of(p, b).blocks) * p.c.H;
-        if (item < at + n) break;
-        at += n;
+    __syncthreads();
+    for (int e = 0; e < 2; ++e) {
+      const int64_t place = part_begin(total, blockIdx.x + e, gridDim.x);
+      if (place < total && begin <= place && place < begin + mine) {
+        int64_t at = begin;
+        int b = b0;
+        Seq s;
+        for (;; ++b) {
+          s = seq_of(p, b);
+          const int64_t n = length_of(p, s);
+          if (place < at + n) break;
+          at += n;
+        }
+        ends[e] = place_of(p, s, b, place - at, total / gridDim.x);
       }
-      s_scan[18] = b;
-      s_scan[19] = at;
     }
   }
   __syncthreads();
   const uint32_t tmem = *s_tmem;
-  const int splits = static_cast<int>(s_scan[17]);
-  const bool any = *s_abort == 0 && blockIdx.x / splits < s_scan[16];
+  const bool any = *s_abort == 0 && s_scan[16] > 0;
   // The next item of a role: false behind the last one, and where something has failed.
   auto segment = [&](int seg, int& nt) {
     if (!fp8b::mbar_wait_all(&g_full[seg % kSegs], (seg / kSegs) & 1, s_abort)) return false;
@@ -398,7 +490,6 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       const int steps = s_seg[seg % kSegs].steps;
       __syncwarp();
       done_with(seg);
-      if (nt < 0) continue;
       if (!mbar_wait(q_full, items++ & 1, s_abort)) {
         failed = true;
         break;
@@ -477,10 +568,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
     // ---- the items of this CTA, and the block scales of their tiles: a lane per 16 tokens, four tiles at a time
     fp8b::regs_give<72>();
     float4* table = reinterpret_cast<float4*>(smem + C::kOffScales);
-    const int64_t total = s_scan[16];
-    int64_t item = blockIdx.x / splits, at = s_scan[19];
-    const int split = blockIdx.x % splits;
-    int b = static_cast<int>(s_scan[18]), seg = 0, tiles = 0;
+    const Place begin = reinterpret_cast<const Place*>(s_scan + 17)[0], end = reinterpret_cast<const Place*>(s_scan + 17)[1];
+    int seg = 0, tiles = 0;
     bool ok = any;
     auto announce = [&](const Seg& g) {
       if (seg >= kSegs && !mbar_wait_warp(&g_empty[seg % kSegs], (seg / kSegs - 1) & 1, s_abort)) return false;
@@ -492,30 +581,33 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       ++seg;
       return true;
     };
+    const bool same = begin.b == end.b && begin.k == end.k;
+    if (lane == 0) {
+      const bool goes_on = any && end.tile > 0 && (!same || begin.tile == 0);
+      const int came = any && begin.tile > 0 && !(same && end.tile == begin.tile) ? (same ? 1 : 2) : 0;
+      p.shared[blockIdx.x] = make_int4(goes_on ? end.b : 0, goes_on ? end.k : 0, goes_on ? 1 : 0, came);
+    }
     if (any) {
+      int b = begin.b, k = begin.k, tile = begin.tile;
       Seq s = seq_of(p, b);
-      for (; ok && item < total; item += splits > 1 ? total : static_cast<int64_t>(gridDim.x)) {  // (an item that is split is a CTA's only one)
-        while (item >= at + static_cast<int64_t>(s.blocks) * p.c.H) {
-          at += static_cast<int64_t>(s.blocks) * p.c.H;
-          s = seq_of(p, ++b);
+      for (; ok; ++k, tile = 0) {
+        while (b < end.b && k >= s.blocks * p.c.H) {
+          k = 0;
+          if (++b < p.c.B) s = seq_of(p, b);
         }
-        const int k = static_cast<int>(item - at);
+        const bool ends = b == end.b && k == end.k;  // the part ends in this item
+        if (b == p.c.B || (b == end.b && k > end.k) || (ends && tile >= end.tile)) break;
         Seg g{};
         g.L = s.L, g.n = s.n, g.b = b, g.h = k % p.c.H, g.first = s.first;
-        const int block = s.blocks - 1 - k / p.c.H;
-        g.row0 = block * kRows;
-        g.rows = static_cast<int>(min(static_cast<int64_t>(s.n) * p.G - g.row0, static_cast<int64_t>(kRows)));
-        // tokens that some of the rows see
-        const int64_t p0 = static_cast<int64_t>(s.L) - s.n + g.row0 / p.G, p1 = static_cast<int64_t>(s.L) - s.n + (g.row0 + g.rows - 1) / p.G;
-        const int64_t lo = p.window > 0 ? max(p0 + 1 - p.window, static_cast<int64_t>(0)) : 0;
-        const int64_t hi = max(p.causal ? p1 + 1 : static_cast<int64_t>(s.L), static_cast<int64_t>(1));
-        const int t0 = static_cast<int>(lo / kTok), nt = max(static_cast<int>((hi + kTok - 1) / kTok) - t0, 1);
-        const int half = hi - static_cast<int64_t>(t0 + nt - 1) * kTok <= kStep ? 1 : 0;  // nobody sees the last tile's second half
-        const int c0 = static_cast<int>(static_cast<int64_t>(nt) * split / splits), c1 = static_cast<int>(static_cast<int64_t>(nt) * (split + 1) / splits);
-        g.tile0 = t0 + c0;
-        g.nt = c1 > c0 ? c1 - c0 : -1;
-        g.steps = 2 * (c1 - c0) - (c1 == nt ? half : 0);
-        g.part = splits > 1 ? blockIdx.x : -1;
+        const int64_t row0 = block_row0(s, k / p.c.H);
+        g.row0 = static_cast<int>(row0);
+        g.rows = block_rows(p, s, row0);
+        const Item item = item_of(p, s, row0, g.rows);
+        const int c1 = ends ? end.tile : item.nt;
+        g.tile0 = item.t0 + tile;
+        g.nt = c1 - tile;
+        g.steps = 2 * g.nt - (ends ? 0 : item.half);
+        g.part = tile > 0 ? 2 * blockIdx.x : ends ? 2 * blockIdx.x + 1 : -1;
         if (!announce(g)) {
           ok = false;
           break;
@@ -540,6 +632,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
     }
   } else if (warp >= kConvWarp0) {
     fp8b::regs_give<72>();
+    constexpr int kLanes = D / 8, kRowsPer = 32 / kLanes, kRowsStep = 4 * kRowsPer, kBatch = 4;
     const int i = threadIdx.x - kConvWarp0 * 32;
     Ring v, o;
     int n = 0, nt, items = 0;
@@ -550,44 +643,66 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       const int first = g.first, h = g.h, row0 = g.row0, rows = g.rows;
       __syncwarp();
       done_with(seg);
-      if (nt < 0) continue;
-      // queries: a row per thread, of one tile and then the other
+      // Queries, once those there are done with (two steps before the item's end): all rows are copied to where they are going to
+      // be, half of a row in the place of each of its terms, then converted there.  (Loads to registers, of which there were
+      // 16 per warp on their way, cost 28000 cycles between two items, and copies of rows 10000 just to ask for, where two boxes
+      // per tile cannot have them.)
       if (items > 0 && !fp8b::mbar_wait_all(q_empty, (items - 1) & 1, s_abort)) {
         if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrConvertR);
         break;
       }
+      if (p.boxes) {
+        if (i == 0) {
+          mbar_arrive_expect_tx(r_full, (rows > kTok ? kRows : kTok) * 2 * D);
+          for (int r = 0; r < rows; r += kTok)
+            for (int half = 0; half < 2; ++half)
+              tma_load_4d(smem + C::kOffQueries + (r / kTok * 2 + half) * C::kTileBytes, &tm_q, 0, half, h * p.G, first + (row0 + r) / p.G, r_full);
+        }
+      } else {
+        if (i == 0) mbar_arrive_expect_tx(r_full, rows * 2 * D);
+        for (int r = i; r < rows; r += kTok) {
+          const __nv_bfloat16* src = p.q + (first + (row0 + r) / p.G) * p.ldq + (static_cast<int64_t>(h) * p.G + (row0 + r) % p.G) * D;
+          uint8_t* to = smem + C::kOffQueries + (r / kTok) * 2 * C::kTileBytes + i * D;
+          bulk_load(to, src, D, r_full);
+          bulk_load(to + C::kTileBytes, src + D / 2, D, r_full);
+        }
+      }
+      __syncwarp();
+      if (!fp8b::mbar_wait_all(r_full, items & 1, s_abort)) {
+        uint32_t spin = 0;  // never leave with copies still in flight
+        while (!mbar_try_wait(r_full, items & 1) && ++spin < kSpinLimit) {
+        }
+        if (lane == 0) fp8b::raise_error8(p.status, s_abort, kErrConvertR);
+        break;
+      }
       ++items;
-      for (int q = 0; q < 2 && q * kTok < rows; ++q) {
-        const int r = q * kTok + i;
-        const bool has = r < rows;
-        const uint4* src = reinterpret_cast<const uint4*>(p.q + (first + (row0 + r) / p.G) * p.ldq + (static_cast<int64_t>(h) * p.G + (row0 + r) % p.G) * D);
-        uint32_t a = 0u;
+      // D / 8 lanes per row, kBatch independent rows at a time: a warp per scheduler is bound by its instructions' latencies here
+#pragma unroll 1
+      for (int r0 = (warp - kConvWarp0) * kRowsPer + lane / kLanes; r0 < (rows > kTok ? kRows : kTok); r0 += kBatch * kRowsStep) {
+        const int l = lane % kLanes;
+        uint8_t* row = smem + C::kOffQueries + (r0 / kTok * 2 * kTok + r0 % kTok) * D;
+        const uint8_t* from = row + l / (kLanes / 2) * C::kTileBytes + l % (kLanes / 2) * 16;
+        uint8_t* to = row - r0 % kTok * D + row_piece<D>(r0 % kTok, l / 2) + (l & 1) * 8;
+        uint4 x[kBatch];
+        uint32_t a[kBatch];
 #pragma unroll
-        for (int x0 = 0; x0 < D / 8; x0 += 8) {
-          uint4 x[8];
+        for (int u = 0; u < kBatch; ++u) x[u] = r0 + u * kRowsStep < rows ? *reinterpret_cast<const uint4*>(from + u * (kRowsStep * D)) : make_uint4(0u, 0u, 0u, 0u);
+        __syncwarp();
 #pragma unroll
-          for (int x1 = 0; x1 < 8; ++x1) x[x1] = has ? load_chained(src + x0 + x1) : make_uint4(0u, 0u, 0u, 0u);
+        for (int u = 0; u < kBatch; ++u) a[u] = absmax_bits8(x[u]);
 #pragma unroll
-          for (int x1 = 0; x1 < 8; ++x1) a = max(a, absmax_bits8(x[x1]));
+        for (int o = 1; o < kLanes; o <<= 1)
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) a[u] = max(a[u], __shfl_xor_sync(0xFFFFFFFFu, a[u], o));
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const RowScale s = row_scale(a[u]);
+          uint2 a0, b0;
+          split8(x[u], s.up, a0, b0);
+          *reinterpret_cast<uint2*>(to + u * (kRowsStep * D)) = a0;  // (a step of 8 rows or 16, which the swizzle does not see)
+          *reinterpret_cast<uint2*>(to + C::kTileBytes + u * (kRowsStep * D)) = b0;
+          if (l == 0) s_rows[r0 + u * kRowsStep] = s.down * p.scale_log2;
         }
-        const RowScale s = row_scale(a);
-        uint8_t* to = smem + C::kOffQueries + q * 2 * C::kTileBytes;
-#pragma unroll
-        for (int x0 = 0; x0 < D / 8; x0 += 4) {
-          uint4 x[4];
-#pragma unroll
-          for (int x1 = 0; x1 < 4; ++x1) x[x1] = has ? load_chained(src + x0 + x1) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-          for (int x1 = 0; x1 < 4; x1 += 2) {
-            uint2 a0, a1, b0, b1;
-            split8(x[x1], s.up, a0, b0);
-            split8(x[x1 + 1], s.up, a1, b1);
-            const uint32_t at = row_piece<D>(i, (x0 + x1) / 2);
-            *reinterpret_cast<uint4*>(to + at) = make_uint4(a0.x, a0.y, a1.x, a1.y);
-            *reinterpret_cast<uint4*>(to + C::kTileBytes + at) = make_uint4(b0.x, b0.y, b1.x, b1.y);
-          }
-        }
-        s_rows[r] = s.down * p.scale_log2;
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -632,67 +747,63 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       const int lo = mine && p.window > 0 ? static_cast<int>(max(pos + 1 - p.window, static_cast<int64_t>(0))) : 0;
       const int hi_all = __reduce_min_sync(0xFFFFFFFFu, hi), lo_all = __reduce_max_sync(0xFFFFFFFFu, lo);
       float m = -INFINITY, l = 0.0f;
-      if (nt > 0) {
-        if (!fp8b::mbar_wait_all(q_full, items & 1, s_abort)) {
+      if (!fp8b::mbar_wait_all(q_full, items & 1, s_abort)) {
+        failed = true;
+        break;
+      }
+      ++items;
+      const float c = q * kTok < rows ? s_rows[r] : 0.0f;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_empty);
+      for (int st = 0; st < steps; ++st) {
+        const int slot = tiles % kScaleSlots;
+        if ((st & 1) == 0 && !fp8b::mbar_wait_all(&e_full[slot], (tiles / kScaleSlots) & 1, s_abort)) {
           failed = true;
           break;
         }
-        ++items;
-        const float c = q * kTok < rows ? s_rows[r] : 0.0f;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(q_empty);
-        for (int st = 0; st < steps; ++st) {
-          const int slot = tiles % kScaleSlots;
-          if ((st & 1) == 0 && !fp8b::mbar_wait_all(&e_full[slot], (tiles / kScaleSlots) & 1, s_abort)) {
-            failed = true;
-            break;
-          }
-          if (q * kTok < rows) {
-            const int buf = done & 1;
-            if (!fp8b::mbar_wait_all(&s_full[q * 2 + buf], (done >> 1) & 1, s_abort)) {
-              failed = true;
-              break;
-            }
-            tc_fence_after_sync();
-            float x[kStep];
-#pragma unroll
-            for (int k = 0; k < kStep / 32; ++k) fp8b::tmem_ld32(ts + buf * kStep + k * 32, x + k * 32);
-#pragma unroll
-            for (int k = 0; k < kStep / 32; ++k) fp8b::tmem_ld_wait32(x + k * 32);
-            const int base = tile0 * kTok + st * kStep;
-            auto accumulated = [&] { return fp8b::mbar_wait_all(&pv_done[q * 2 + (buf ^ 1)], ((done - 1) >> 1) & 1, s_abort); };
-            const float4* e = table + slot * 8 + (st & 1) * (kStep / 16);
-            const uint32_t probs = ts + buf * kStep;
-            const bool ok = base >= lo_all && base + (kStep - 1) < hi_all
-                                ? softmax_step<D, false>(x, e, c, 0, kStep, m, l, probs, to, st == 0, accumulated)
-                                : softmax_step<D, true>(x, e, c, lo - base, hi - base, m, l, probs, to, st == 0, accumulated);
-            if (!ok) {
-              failed = true;
-              break;
-            }
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&p_full[q * 2 + buf]);
-            ++done;
-          }
-          if ((st & 1) != 0 || st + 1 == steps) {
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&e_empty[slot]);
-            ++tiles;
-          }
-        }
-        if (failed) break;
         if (q * kTok < rows) {
-          // the products of the last two steps
-          if ((steps > 1 && !fp8b::mbar_wait_all(&pv_done[q * 2 + (done & 1)], ((done - 2) >> 1) & 1, s_abort)) ||
-              !fp8b::mbar_wait_all(&pv_done[q * 2 + ((done - 1) & 1)], ((done - 1) >> 1) & 1, s_abort)) {
+          const int buf = done & 1;
+          if (!fp8b::mbar_wait_all(&s_full[q * 2 + buf], (done >> 1) & 1, s_abort)) {
             failed = true;
             break;
           }
           tc_fence_after_sync();
+          float x[kStep];
+#pragma unroll
+          for (int k = 0; k < kStep / 32; ++k) fp8b::tmem_ld32(ts + buf * kStep + k * 32, x + k * 32);
+#pragma unroll
+          for (int k = 0; k < kStep / 32; ++k) fp8b::tmem_ld_wait32(x + k * 32);
+          const int base = tile0 * kTok + st * kStep;
+          auto accumulated = [&] { return fp8b::mbar_wait_all(&pv_done[q * 2 + (buf ^ 1)], ((done - 1) >> 1) & 1, s_abort); };
+          const float4* e = table + slot * 8 + (st & 1) * (kStep / 16);
+          const uint32_t probs = ts + buf * kStep;
+          const bool ok = base >= lo_all && base + (kStep - 1) < hi_all
+                              ? softmax_step<D, false>(x, e, c, 0, kStep, m, l, probs, to, st == 0, accumulated)
+                              : softmax_step<D, true>(x, e, c, lo - base, hi - base, m, l, probs, to, st == 0, accumulated);
+          if (!ok) {
+            failed = true;
+            break;
+          }
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&p_full[q * 2 + buf]);
+          ++done;
+        }
+        if ((st & 1) != 0 || st + 1 == steps) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&e_empty[slot]);
+          ++tiles;
         }
       }
+      if (failed) break;
       if (q * kTok >= rows) continue;
+      // the products of the last two steps
+      if ((steps > 1 && !fp8b::mbar_wait_all(&pv_done[q * 2 + (done & 1)], ((done - 2) >> 1) & 1, s_abort)) ||
+          !fp8b::mbar_wait_all(&pv_done[q * 2 + ((done - 1) & 1)], ((done - 1) >> 1) & 1, s_abort)) {
+        failed = true;
+        break;
+      }
+      tc_fence_after_sync();
       float* to_part = part < 0 ? nullptr : p.partial + static_cast<int64_t>(part) * (kRows * (D + 2));
       const int hq = h * p.G + row % p.G;
       if (part >= 0) {
@@ -701,30 +812,29 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       } else if (mine && p.lse) {
         p.lse[t * (static_cast<int64_t>(p.G) * p.c.H) + hq] = l == 0.0f ? -INFINITY : (log2f(l) + m + 8.0f - kShift) * (1.0f / kLog2e);
       }
-      if (nt > 0) {
-        const float f = part >= 0 ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);
+      const float f = part >= 0 ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);
 #pragma unroll 1
-        for (int d = 0; d < D; d += 16) {
-          float o[16];
-          tmem_ld16(to + d, o);
-          tmem_ld_wait_regs<16>(o);
+      for (int d = 0; d < D; d += 32) {
+        float o[32];
+        fp8b::tmem_ld32(to + d, o);
+        fp8b::tmem_ld_wait32(o);
 #pragma unroll
-          for (int k = 0; k < 16; k += 4) {  // features in their places again (see feature_at)
-            const float x = o[k + 1] * f;
-            o[k] *= f;
-            o[k + 1] = o[k + 2] * f;
-            o[k + 2] = x;
-            o[k + 3] *= f;
-          }
-          if (part >= 0) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) *reinterpret_cast<float4*>(to_part + r * D + d + 4 * k) = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
-          } else if (mine) {
-            store16(p, t * p.ldo + static_cast<int64_t>(hq) * D + d, o);
-          }
+        for (int k = 0; k < 32; k += 4) {  // features in their places again (see feature_at)
+          const float x = o[k + 1] * f;
+          o[k] *= f;
+          o[k + 1] = o[k + 2] * f;
+          o[k + 2] = x;
+          o[k + 3] *= f;
         }
-        tc_fence_before_sync();
+        if (part >= 0) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) *reinterpret_cast<float4*>(to_part + r * D + d + 4 * k) = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+        } else if (mine) {
+          store16(p, t * p.ldo + static_cast<int64_t>(hq) * D + d, o);
+          store16(p, t * p.ldo + static_cast<int64_t>(hq) * D + d + 16, o + 16);
+        }
       }
+      tc_fence_before_sync();
     }
     if (failed && any && lane == 0) fp8b::raise_error8(p.status, s_abort, kErrSoftmaxR);
   }
@@ -737,67 +847,59 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
   }
 }
 
-// Results of items that several CTAs share: a block per item and 8 rows, a warp per row, D / 32 features per lane.
+// Results of items that several CTAs share: a block per CTA where one begins and 8 rows, a warp per row, D / 32 features per lane.
 template <int D>
 __global__ void __launch_bounds__(256) attention_join_rows_kernel(const P p, int ctas) {
   constexpr int E = D / 32;
-  __shared__ int64_t s_scan[8];
-  __shared__ int s_at[3];
+  __shared__ int s_came[kMaxCtas];
+  __shared__ float s_w[8][kMaxCtas + 1];
   pdl_launch_dependents();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t item = blockIdx.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, x = blockIdx.x;
   pdl_wait();
-  const int per = (p.c.B + 255) / 256;
-  const int b0 = min(static_cast<int>(threadIdx.x) * per, p.c.B), b1 = min(b0 + per, p.c.B);
-  int64_t mine = 0;
-  for (int b = b0; b < b1; ++b) mine += static_cast<int64_t>(seq_of(p, b).blocks) * p.c.H;
-  int64_t incl = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-    if (lane >= o) incl += x;
-  }
-  if (lane == 31) s_scan[warp] = incl;
-  __syncthreads();
-  int64_t before = 0, total = 0;
-  for (int w = 0; w < 8; ++w) {
-    if (w < warp) before += s_scan[w];
-    total += s_scan[w];
-  }
-  const int splits = splits_of(total, ctas);
-  if (splits == 1 || item >= total) return;
-  const int64_t begin = before + incl - mine;
-  if (begin <= item && item < begin + mine) {
-    int64_t at = begin;
-    int b = b0;
-    for (;; ++b) {
-      const int64_t n = static_cast<int64_t>(seq_of(p, b).blocks) * p.c.H;
-      if (item < at + n) break;
-      at += n;
-    }
-    s_at[0] = b;
-    s_at[1] = static_cast<int>(item - at);
-  }
-  __syncthreads();
-  const Seq s = seq_of(p, s_at[0]);
-  const int h = s_at[1] % p.c.H, row0 = (s.blocks - 1 - s_at[1] / p.c.H) * kRows;
+  const uint4 shared = load_chained(reinterpret_cast<const uint4*>(p.shared + x));
+  if (shared.z == 0) return;
+  for (int i = threadIdx.x; i < ctas; i += 256) s_came[i] = static_cast<int>(load_chained(reinterpret_cast<const uint4*>(p.shared + i)).w);
+  const Seq s = seq_of(p, static_cast<int>(shared.x));
+  const int k = static_cast<int>(shared.y), h = k % p.c.H;
+  const int64_t row0 = block_row0(s, k / p.c.H);
   const int r = blockIdx.y * 8 + warp;
-  if (static_cast<int64_t>(row0) + r >= static_cast<int64_t>(s.n) * p.G) return;
+  __syncthreads();
+  if (row0 + r >= static_cast<int64_t>(s.n) * p.G) return;
+  // the CTAs behind x that it reaches (one between them may have nothing of it)
+  int end = x + 1;
+  while (end < ctas && s_came[end] != 2) ++end;
+  end = min(end + 1, ctas);
   constexpr int64_t kPart = kRows * (D + 2);
-  const float* part = p.partial + item * splits * kPart;
+  auto piece = [&](int i) { return p.partial + (2 * i + (i == x ? 1 : 0)) * kPart; };
+  auto has = [&](int i) { return i == x || s_came[i] != 0; };
   float m = -INFINITY;
-  for (int i = 0; i < splits; ++i) m = fmaxf(m, load_chained(part + i * kPart + kRows * D + kRows + r));
-  float l = 0.0f, o[E] = {};
-  for (int i = 0; i < splits; ++i) {
-    const float mi = load_chained(part + i * kPart + kRows * D + kRows + r), li = load_chained(part + i * kPart + kRows * D + r);
-    if (li == 0.0f) continue;  // (a piece that saw nothing, or was empty: what lies there is nothing)
-    const float f = mi == -INFINITY ? 1.0f : exp2f(mi - m);  // (a sum that is NaN has no maximum)
-    l = fmaf(f, li, l);
+  for (int i = x + lane; i < end; i += 32)
+    if (has(i)) m = fmaxf(m, load_chained(piece(i) + kRows * D + kRows + r));
+  m = warp_max(m);
+  float l = 0.0f;
+  for (int i = x + lane; i < end; i += 32) {
+    float f = 0.0f;
+    if (has(i)) {
+      const float mi = load_chained(piece(i) + kRows * D + kRows + r), li = load_chained(piece(i) + kRows * D + r);
+      // (a piece that saw nothing counts for nothing; a sum that is NaN has no maximum)
+      if (li != 0.0f) f = mi == -INFINITY ? 1.0f : exp2f(mi - m);
+      if (li != 0.0f) l = fmaf(f, li, l);
+    }
+    s_w[warp][i - x] = f;
+  }
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(f, load_chained(part + i * kPart + r * D + e * 32 + lane), o[e]);
+  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
+  __syncwarp();
+  float o[E] = {};
+#pragma unroll 4
+  for (int i = x; i < end; ++i) {
+    const float f = s_w[warp][i - x];
+    if (f == 0.0f) continue;  // (what lies there is nothing)
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(f, load_chained(piece(i) + r * D + e * 32 + lane), o[e]);
   }
   const int64_t t = s.first + (row0 + r) / p.G;
-  const int hq = h * p.G + (row0 + r) % p.G;
+  const int hq = h * p.G + static_cast<int>((row0 + r) % p.G);
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const float v = l == 0.0f ? 0.0f : o[e] / l;
@@ -811,22 +913,35 @@ __global__ void __launch_bounds__(256) attention_join_rows_kernel(const P p, int
 }
 
 template <int D>
-int launch_cfg(const CUtensorMap& tm, const P& p, int grid, cudaStream_t st) {
+int launch_cfg(const CUtensorMap& tm, const CUtensorMap& tm_q, const P& p, int grid, cudaStream_t st) {
   using C = Cfg<D>;
   static DeviceOnce once;
   if (!allow_shared_memory(once, attention_rows_kernel<D>, C::kSmemBytes)) return ZQ_ERR_CUDA;
-  cudaError_t e = launch_chained(attention_rows_kernel<D>, dim3(grid), dim3(kThreads), C::kSmemBytes, st, false, tm, p);
+  cudaError_t e = launch_chained(attention_rows_kernel<D>, dim3(grid), dim3(kThreads), C::kSmemBytes, st, false, tm, tm_q, p);
   count_launch();
   if (e != cudaSuccess) return ZQ_ERR_CUDA;
-  e = launch_chained(attention_join_rows_kernel<D>, dim3(grid / 2, kRows / 8), dim3(256), 0, st, false, p, grid);
+  e = launch_chained(attention_join_rows_kernel<D>, dim3(grid, kRows / 8), dim3(256), 0, st, false, p, grid);
   count_launch();
   return e == cudaSuccess ? ZQ_OK : ZQ_ERR_CUDA;
+}
+
+// Queries [T][Hq][2 halves][D / 2], boxes of one half of a tile's rows: 128 / G tokens' G heads.
+bool make_query_map(CUtensorMap* m, const AttnArgs& a, int G) {
+  gemm::EncodeTiledFn fn = gemm::encode_fn();
+  if (!fn) return false;
+  const cuuint64_t half = static_cast<cuuint64_t>(a.c.D);  // bytes
+  const cuuint64_t dims[4] = {half / 2, 2, static_cast<cuuint64_t>(a.Hq), static_cast<cuuint64_t>(a.c.T)};
+  const cuuint64_t strides[3] = {half, 2 * half, static_cast<cuuint64_t>(a.ldq) * 2};
+  const cuuint32_t box[4] = {static_cast<cuuint32_t>(half / 2), 1, static_cast<cuuint32_t>(G), static_cast<cuuint32_t>(kTok / G)};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(a.q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace
 
 // (the same place as the other kernel's: the kernels of a call run one after the other)
-size_t rows_workspace_bytes(int64_t D) { return sizeof(float) * kMaxCtas * kRows * (D + 2); }
+size_t rows_workspace_bytes(int64_t D) { return sizeof(float) * kMaxCtas * 2 * kRows * (D + 2) + sizeof(int4) * kMaxCtas; }
 
 int launch_attention_rows(const AttnArgs& a, cudaStream_t st) {
   P p{};
@@ -837,11 +952,14 @@ int launch_attention_rows(const AttnArgs& a, cudaStream_t st) {
   p.out = a.out, p.f32 = a.dt == ZQ_OUT_F32, p.ldo = a.ldo, p.lse = a.lse;
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   p.status = reinterpret_cast<int*>(ws);
-  p.partial = reinterpret_cast<float*>(ws + kWsHeadBytes);
-  CUtensorMap tm;
-  if (!make_page_map(&tm, a.c)) return ZQ_ERR_CUDA;
+  p.shared = reinterpret_cast<int4*>(ws + kWsHeadBytes);
+  p.partial = reinterpret_cast<float*>(p.shared + kMaxCtas);
+  CUtensorMap tm, tm_q{};
+  // a tile's queries as two boxes where whole tokens fill it and a token's stride is one of whole heads
+  p.boxes = kTok % p.G == 0 && a.ldq % a.c.D == 0 ? 1 : 0;
+  if (!make_page_map(&tm, a.c) || (p.boxes && !make_query_map(&tm_q, a, p.G))) return ZQ_ERR_CUDA;
   const int sms = sm_count(), grid = sms < kMaxCtas ? sms : kMaxCtas;
-  return a.c.D == 128 ? launch_cfg<128>(tm, p, grid, st) : launch_cfg<64>(tm, p, grid, st);
+  return a.c.D == 128 ? launch_cfg<128>(tm, tm_q, p, grid, st) : launch_cfg<64>(tm, tm_q, p, grid, st);
 }
 
 }  // namespace kv

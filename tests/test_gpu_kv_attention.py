@@ -281,6 +281,35 @@ def test_attention(case, out):
     check_attention(case, out)
 
 
+@pytest.mark.parametrize("case", [
+    ([2500, 2500, 40, 1900], [700, 1, 40, 650], 12, 12, 64, 32, True, 0),  # fewer row blocks than CTAs: several for each
+    ([900] * 9, [200] * 9, 32, 8, 128, 64, True, 0),                       # more of them: CTAs that end inside one
+    ([1500] * 3, [150] * 3, 40, 8, 128, 64, True, 200),                    # tokens' heads that do not fill a tile
+    ([70] * 90, [70] * 90, 2, 1, 64, 16, True, 0),
+    ([6000], [100], 4, 1, 128, 128, False, 0),                             # two blocks for all CTAs
+    ([40, 0, 900] * 40, [40, 0, 33] * 40, 4, 2, 64, 64, True, 0),          # most sequences have none
+])
+def test_attention_blocks_over_ctas(case):
+    check_attention(case, torch.float32)
+
+
+@pytest.mark.parametrize("pad", [8, 64, 128])
+def test_attention_rows_of_other_strides(pad):
+    """Queries and results inside wider rows, whole heads wide or not."""
+    for lens, new, Hq, H, D, page, causal, window in (ATTN_CASES[10], ATTN_CASES[11], ATTN_CASES[12]):
+        codes, scale, table, lens, cu = R.batch(lens, new, H, D, page)
+        q = R.heads(cu[-1], Hq, D, 7)
+        args = (binding.Fp8KvCache(codes, scale), q, table, R.ints(lens))
+        want = binding.kv_attention(*args, cu=R.ints(cu), causal=causal, window=window)
+        wide = torch.full((cu[-1], Hq * D + pad), float("nan"), device="cuda", dtype=torch.bfloat16)
+        rows = wide[:, :Hq * D].view(cu[-1], Hq, D)
+        rows.copy_(q)
+        out = torch.zeros((cu[-1], Hq * D + pad), device="cuda", dtype=torch.bfloat16)
+        binding.kv_attention(args[0], rows, *args[2:], cu=R.ints(cu), causal=causal, window=window, out=out[:, :Hq * D].view(cu[-1], Hq, D))
+        assert torch.equal(out[:, :Hq * D].reshape(want.shape), want)
+        assert not out[:, Hq * D:].any()
+
+
 @pytest.mark.parametrize("sm_scale", [1.0, 0.01])
 def test_attention_scale(sm_scale):
     check_attention(ATTN_CASES[2], torch.float32, 3, sm_scale=sm_scale)
