@@ -542,7 +542,8 @@ int zq_kv_cache_read(const uint8_t* codes, const float* scale, int64_t pages, in
  *        sequences serves fewer.  0: refused sizes.
  * Products take q as a sum of two E4M3 numbers times a power of two for each row and head: features below 2^-17 of the largest
  * are lost, the others are exact.  Scores, maxima and sums are FP32; probabilities times their blocks' scales are rounded to 11
- * bits, and what is below 2^-26 of the row's largest is lost.  Scales of the values' blocks that a row sees lie within 2^60 of one
+ * bits for bf16 results and to 22 for FP32 ones, and what is below 2^-26 of the row's largest is lost.  FP32 results of sequences
+ * with few rows take two to four times as long as bf16 ones.  Scales of the values' blocks that a row sees lie within 2^60 of one
  * another.  The codes of a sequence's tokens are numbers (0x7F and 0xFF are none).  Results do not vary from run to run.
  */
 size_t zq_kv_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D);

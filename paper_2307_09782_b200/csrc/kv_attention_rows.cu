@@ -3,7 +3,8 @@
 //
 //   S [128 rows, 128 tokens] = q K^T       E4M3 x E4M3; q is a sum of two E4M3 numbers, so two products: the keys' codes go to
 //                                          the tensor core as they are, at the price of one FP16 product
-//   O [128 rows, D] += P V                 FP16 x FP16; P from tensor memory, over the scores it was made of; the values'
+//   O [128 rows, D] += P V                 FP16 x FP16 (FP32 results: P is the sum of two FP16 numbers, 11 bits are not enough for
+//                                          them, and the sequences with few rows are here too); P from tensor memory, over the scores it was made of; the values'
 //                                          codes are widened in shared memory, once for 256 rows
 // Rows are the tensor core's lanes and a softmax thread's own: maxima and sums need no other thread.  A CTA works on two tiles of
 // 128 rows in turn, each in steps of 64 tokens whose scores alternate between two places in tensor memory: the next step's are there
@@ -83,7 +84,7 @@ __device__ __forceinline__ Seq seq_of(const P& p, int b) {
   rows_of(p.c, b, s.first, s.n);
   s.L = max(load_chained(p.c.lens + b), 0);
   const int64_t rows = static_cast<int64_t>(s.n) * p.G;
-  s.blocks = rows > kFewRows ? static_cast<int>((rows + kRows - 1) / kRows) : 0;
+  s.blocks = rows > (p.f32 ? 0 : kFewRows) ? static_cast<int>((rows + kRows - 1) / kRows) : 0;
   return s;
 }
 // An item's tokens, in tiles: those that some of its rows see (at least one).
@@ -223,7 +224,7 @@ __device__ __forceinline__ void store16(const P& p, int64_t at, const float* v) 
 // A softmax thread's step of scores x (its row, 64 tokens) -> probabilities in tensor memory.  `scales`: of its 4 groups of 16 tokens;
 // `lo`, `hi`: tokens of the step that the row sees (looked at with MASK).  May move the row's reference m and multiplies what is in
 // the accumulator and l by the factor.
-template <int D, bool MASK, typename Wait>
+template <int D, bool EXACT, bool MASK, typename Wait>
 __device__ __forceinline__ bool softmax_step(float* x, const float4* scales, float c, int lo, int hi, float& m, float& l, uint32_t probs,
                                              uint32_t acc, bool first, Wait accumulated) {
   float top = -INFINITY;
@@ -264,7 +265,7 @@ __device__ __forceinline__ bool softmax_step(float* x, const float4* scales, flo
   const float base = kShift - (m == -INFINITY ? 0.0f : m);
 #pragma unroll
   for (int g = 0; g < kStep / 16; g += 2) {
-    uint32_t h[16];
+    uint32_t h[16], r[EXACT ? 16 : 1];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const float4 e = scales[g + k];
@@ -283,18 +284,23 @@ __device__ __forceinline__ bool softmax_step(float* x, const float4* scales, flo
         }
         sum = add2(sum, pack2(a, b));
         h[k * 8 + i / 2] = pack_f16(a, b);
+        if (EXACT) {
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[k * 8 + i / 2]));
+          r[k * 8 + i / 2] = pack_f16(a - f.x, b - f.y);
+        }
       }
       float s0, s1;
       unpack2(sum, s0, s1);
       l = fmaf(s0 + s1, e.z, l);
     }
     tmem_st16(probs + g * 8, h);
+    if (EXACT) tmem_st16(probs + kStep / 2 + g * 8, r);
   }
   tmem_st_wait();
   return true;
 }
 
-template <int D>
+template <int D, bool EXACT>
 __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ CUtensorMap tm_q, const P p) {
   using C = Cfg<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -548,6 +554,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
 #pragma unroll
           for (int s = 0; s < kStep / 16; ++s)
             umma_f16_tmem_a(to_o, to_s + buf * kStep + s * 8, bd + s * (2048 >> 4), odesc_i, (st > 0 || s > 0) ? 1u : 0u);
+          if (EXACT)
+#pragma unroll
+            for (int s = 0; s < kStep / 16; ++s)
+              umma_f16_tmem_a(to_o, to_s + buf * kStep + kStep / 2 + s * 8, bd + s * (2048 >> 4), odesc_i, 1u);
           umma_commit(&pv_done[q * 2 + buf]);
           if (ends) umma_commit(&w_empty[v.i]);
         }
@@ -778,8 +788,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
           const float4* e = table + slot * 8 + (st & 1) * (kStep / 16);
           const uint32_t probs = ts + buf * kStep;
           const bool ok = base >= lo_all && base + (kStep - 1) < hi_all
-                              ? softmax_step<D, false>(x, e, c, 0, kStep, m, l, probs, to, st == 0, accumulated)
-                              : softmax_step<D, true>(x, e, c, lo - base, hi - base, m, l, probs, to, st == 0, accumulated);
+                              ? softmax_step<D, EXACT, false>(x, e, c, 0, kStep, m, l, probs, to, st == 0, accumulated)
+                              : softmax_step<D, EXACT, true>(x, e, c, lo - base, hi - base, m, l, probs, to, st == 0, accumulated);
           if (!ok) {
             failed = true;
             break;
@@ -912,12 +922,12 @@ __global__ void __launch_bounds__(256) attention_join_rows_kernel(const P p, int
   if (p.lse && lane == 0) p.lse[t * (static_cast<int64_t>(p.G) * p.c.H) + hq] = l == 0.0f ? -INFINITY : (log2f(l) + m + 8.0f - kShift) * (1.0f / kLog2e);
 }
 
-template <int D>
+template <int D, bool EXACT>
 int launch_cfg(const CUtensorMap& tm, const CUtensorMap& tm_q, const P& p, int grid, cudaStream_t st) {
   using C = Cfg<D>;
   static DeviceOnce once;
-  if (!allow_shared_memory(once, attention_rows_kernel<D>, C::kSmemBytes)) return ZQ_ERR_CUDA;
-  cudaError_t e = launch_chained(attention_rows_kernel<D>, dim3(grid), dim3(kThreads), C::kSmemBytes, st, false, tm, tm_q, p);
+  if (!allow_shared_memory(once, attention_rows_kernel<D, EXACT>, C::kSmemBytes)) return ZQ_ERR_CUDA;
+  cudaError_t e = launch_chained(attention_rows_kernel<D, EXACT>, dim3(grid), dim3(kThreads), C::kSmemBytes, st, false, tm, tm_q, p);
   count_launch();
   if (e != cudaSuccess) return ZQ_ERR_CUDA;
   e = launch_chained(attention_join_rows_kernel<D>, dim3(grid, kRows / 8), dim3(256), 0, st, false, p, grid);
@@ -959,7 +969,8 @@ int launch_attention_rows(const AttnArgs& a, cudaStream_t st) {
   p.boxes = kTok % p.G == 0 && a.ldq % a.c.D == 0 ? 1 : 0;
   if (!make_page_map(&tm, a.c) || (p.boxes && !make_query_map(&tm_q, a, p.G))) return ZQ_ERR_CUDA;
   const int sms = sm_count(), grid = sms < kMaxCtas ? sms : kMaxCtas;
-  return a.c.D == 128 ? launch_cfg<128>(tm, tm_q, p, grid, st) : launch_cfg<64>(tm, tm_q, p, grid, st);
+  if (p.f32) return a.c.D == 128 ? launch_cfg<128, true>(tm, tm_q, p, grid, st) : launch_cfg<64, true>(tm, tm_q, p, grid, st);
+  return a.c.D == 128 ? launch_cfg<128, false>(tm, tm_q, p, grid, st) : launch_cfg<64, false>(tm, tm_q, p, grid, st);
 }
 
 }  // namespace kv

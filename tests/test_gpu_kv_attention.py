@@ -293,6 +293,19 @@ def test_attention_blocks_over_ctas(case):
     check_attention(case, torch.float32)
 
 
+@pytest.mark.parametrize("case", [([6001], [200], 4, 4, 128, 32, True, 0), ([9000] * 5, [1] * 5, 16, 8, 128, 64, True, 0),
+                                  ([700, 30], [5, 30], 8, 2, 64, 64, True, 0)])
+def test_attention_fp32_results_keep_more_than_probabilities_of_12_bits(case):
+    """In the 2-norm.  The queries' two terms leave at most 2^-18 of a row's largest feature (about 4 sigma) per feature; over D independent
+    ones times D^-1/2 a score is off by 4 / sqrt(3) 2^-18 < 2^-16.  Powers, FP32 sums and products (1e-8 each) are below that."""
+    lens, new, Hq, H, D, page, causal, window = case
+    codes, scale, table, lens, cu = R.batch(lens, new, H, D, page)
+    q = R.heads(cu[-1], Hq, D, 7)
+    got = binding.kv_attention(binding.Fp8KvCache(codes, scale), q, table, R.ints(lens), cu=R.ints(cu), out_dtype=torch.float32)
+    ref, _, _ = R.attention(codes, scale, q, table, lens, cu, D ** -0.5, causal, window)
+    assert (got.to(R.F64) - ref).norm() <= 2.0 ** -16 * ref.norm()
+
+
 @pytest.mark.parametrize("pad", [8, 64, 128])
 def test_attention_rows_of_other_strides(pad):
     """Queries and results inside wider rows, whole heads wide or not."""
