@@ -1,5 +1,5 @@
 // Attention over the 8-bit cache where a sequence and cache head have few rows (new tokens x query heads of the head, up to 64):
-// decoding.  Bound by the codes, which are read once.
+// decoding, bf16 results.  Bound by the codes, which are read once.
 //
 // Keys' and values' codes go from memory to the tensor core as they are; what meets them is written as sums of E4M3 numbers, side
 // by side in the columns:
@@ -38,7 +38,6 @@ struct P {
   int causal, window;
   void* out;
   int64_t ldo;
-  int f32;
   float* lse;
   float* partial;    // [CTAs][2][RS (D + 2)]
   int4* shared;      // [CTAs] what begins in the CTA and goes on in the next: sequence, head, CTAs (0: nothing does)
@@ -811,7 +810,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
         }
         // row by row without divisions, which would be most of the code: G rows of a token side by side, then the next token
         // (partial results: all rows one after the other)
-        const int esize = !whole || p.f32 ? 4 : 2, group = whole ? p.G : kFewRows;
+        const int esize = whole ? 2 : 4, group = whole ? p.G : kFewRows;
         const int64_t jump = whole ? (p.ldo - static_cast<int64_t>(p.G - 1) * D) * esize : 0;
         uint8_t* to = whole ? static_cast<uint8_t*>(p.out) + (first * p.ldo + static_cast<int64_t>(h) * p.G * D + d) * esize
                             : reinterpret_cast<uint8_t*>(part + d);
@@ -902,10 +901,7 @@ __global__ void __launch_bounds__(4 * D) attention_join_kernel(const P p) {
       o = s_o[0][d] + s_o[1][d] + s_o[2][d] + s_o[3][d];
       const float v = s_l == 0.0f ? 0.0f : o * kCodeUnit / s_l;
       const int64_t at = (s.first + r / p.G) * p.ldo + (static_cast<int64_t>(h) * p.G + r % p.G) * D + d;
-      if (p.f32)
-        static_cast<float*>(p.out)[at] = v;
-      else
-        static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
+      static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
     }
   }
 }
@@ -943,7 +939,7 @@ int launch_attention_few(const AttnArgs& a, int max_rows, cudaStream_t st) {
   p.q = static_cast<const __nv_bfloat16*>(a.q), p.ldq = a.ldq, p.G = a.Hq / a.c.H;
   p.scale_log2 = a.sm_scale * kLog2e;
   p.causal = a.causal, p.window = a.window;
-  p.out = a.out, p.f32 = a.dt == ZQ_OUT_F32, p.ldo = a.ldo, p.lse = a.lse;
+  p.out = a.out, p.ldo = a.ldo, p.lse = a.lse;
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   p.status = reinterpret_cast<int*>(ws);
   p.shared = reinterpret_cast<int4*>(ws + kWsHeadBytes);
