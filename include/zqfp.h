@@ -479,6 +479,7 @@ typedef enum { ZQ_PAIRS_HALVES = 0, ZQ_PAIRS_NEIGHBOURS = 1 } zq_pairs;
  * with the cosines and sines of the token's position; features from rot on pass unchanged.  FP32 inside, one rounding.
  * q, k      : bf16 [T, ldq], [T, ldk];  q_out, k_out : out, bf16 [T, ldqo], [T, ldko]; may be the inputs themselves
  * wq, wk    : FP32 [D], 16-byte aligned, both or neither
+ * eps       : finite, >= 0 (with 0 a head of zeros gives NaN, and NaN gradients)
  * table     : FP32 [far, rot], 16-byte aligned: a position's rot/2 cosines, then its sines.  rot % 16 == 0, 16 .. D
  * positions : int32 [T]; a token whose position the table lacks (negative, or far and beyond) gets NaN in its rotated features
  * Hq or H may be 0 (its pointers are not looked at then).  T == 0 is a no-op.

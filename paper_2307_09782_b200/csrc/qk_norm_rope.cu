@@ -280,7 +280,8 @@ __global__ void __launch_bounds__(kWarps * 32, kBackwardBlocks) norm_rope_backwa
             unpack8(v[i], z);
 #pragma unroll
             for (int e = 0; e < 8; ++e) ss = fmaf(z[e], z[e], ss);
-            const float r = rsqrtf(head_sum<L>(ss) * (1.0f / D) + p.eps);
+            const float square = head_sum<L>(ss) * (1.0f / D) + p.eps;
+            const float r = h < heads ? rsqrtf(square) : 0.0f;  // (where there is no head it need not be a number: eps may be 0)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               z[e] *= r;

@@ -1,0 +1,48 @@
+"""Norms with the position rotation where a warp works on several units, where heads do not fill a unit, and on numbers that have to come
+out as they went in.  Tolerances as in test_gpu_kv_attention.py."""
+import pytest
+import torch
+
+import kv_ref as R
+from paper_2307_09782_b200 import binding
+from test_gpu_kv_attention import half_step, norm_inputs
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-6
+
+
+def check_forward(case, eps=EPS):
+    q, k, wq, wk, table, positions = norm_inputs(case)
+    yq, yk = binding.qk_norm_rope(q, k, table, positions, wq=wq, wk=wk, eps=eps, pairs=case[5])
+    for x, w, y in ((q, wq, yq), (k, wk, yk)):
+        ref = R.norm_rope(x.to(R.F64), None if w is None else w.to(R.F64), table, positions, eps, case[5])
+        big = ref.abs().amax(-1, keepdim=True)
+        assert ((y.to(R.F64) - ref).abs() <= half_step(torch.bfloat16) * ref.abs() + 2.0 ** -20 * big).all()
+
+
+def check_backward(case, eps=EPS):
+    q, k, wq, wk, table, positions = norm_inputs(case)
+    T, Hq, H, D = case[:4]
+    dq, dk = R.heads(T, Hq, D, 11, 2), R.heads(T, H, D, 12)
+    got = binding.qk_norm_rope_backward(dq, dk, q, k, table, positions, wq=wq, wk=wk, eps=eps, pairs=case[5])
+    for x, w, dy, dx, dw in ((q, wq, dq, got[0], got[2]), (k, wk, dk, got[1], got[3])):
+        x64 = x.to(R.F64).requires_grad_()
+        w64 = None if w is None else w.to(R.F64).requires_grad_()
+        R.norm_rope(x64, w64, table, positions, eps, case[5]).backward(dy.to(R.F64))
+        rms = (x.to(R.F64).square().mean(-1, keepdim=True) + eps).sqrt()
+        length = dy.to(R.F64).norm(dim=-1, keepdim=True)
+        size = dy.to(R.F64).abs().amax(-1, keepdim=True) if w is None else length * 2 * w.abs().max() / rms
+        assert ((dx.to(R.F64) - x64.grad).abs() <= half_step(torch.bfloat16) * x64.grad.abs() + 2.0 ** -19 * size).all()
+        if w is None:
+            assert dw is None
+        else:
+            terms = (length * (x.to(R.F64) / rms).abs()).sum((0, 1))
+            assert ((dw.to(R.F64) - w64.grad).abs() <= 2.0 ** -20 * terms).all()
+
+
+@pytest.mark.parametrize("Hq,H,D", [(1, 1, 128), (2, 1, 64), (12, 12, 64), (9, 3, 128), (16, 8, 128)])
+def test_no_epsilon(Hq, H, D):
+    """eps = 0, which only a head of zeros cannot take; heads that fill a unit and heads that do not."""
+    case = (37, Hq, H, D, D, "halves", True, 1)
+    check_forward(case, 0.0)
+    check_backward(case, 0.0)
