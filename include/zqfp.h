@@ -476,7 +476,8 @@ typedef enum { ZQ_PAIRS_HALVES = 0, ZQ_PAIRS_NEIGHBOURS = 1 } zq_pairs;
  * Norm and rotation.  For each token t and each of its Hq query heads (H key heads), x being the head's features:
  *   n = x / sqrt(mean(x^2) + eps) ;  z = n w ;  z = x where wq = wk = NULL
  *   y_a = z_a cos - z_b sin ;  y_b = z_b cos + z_a sin  for the rot/2 pairs (a, b) of its first `rot` features
- * with the cosines and sines of the token's position; features from rot on pass unchanged.  FP32 inside, one rounding.
+ * with the cosines and sines of the token's position; features from rot on are z (without norms x as it is, -0 too; NaN as some
+ * NaN).  FP32 inside, one rounding.
  * q, k      : bf16 [T, ldq], [T, ldk];  q_out, k_out : out, bf16 [T, ldqo], [T, ldko]; may be the inputs themselves
  * wq, wk    : FP32 [D], 16-byte aligned, both or neither
  * eps       : finite, >= 0 (with 0 a head of zeros gives NaN, and NaN gradients)

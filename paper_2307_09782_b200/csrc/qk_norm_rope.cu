@@ -177,6 +177,10 @@ __global__ void __launch_bounds__(kWarps * 32, kForwardBlocks) norm_rope_kernel(
 #pragma unroll
         for (int e = 0; e < 8; ++e) wc[e] *= w[e], ws[e] *= wp[e];
       }
+      if (!rotated) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ws[e] = -0.0f;  // -0 is added to what passes: adding +0 would turn a -0 into +0
+      }
     }
     Unit next = n;
     uint4 ahead[kSteps];

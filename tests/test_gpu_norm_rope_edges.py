@@ -46,3 +46,19 @@ def test_no_epsilon(Hq, H, D):
     case = (37, Hq, H, D, D, "halves", True, 1)
     check_forward(case, 0.0)
     check_backward(case, 0.0)
+
+
+def test_features_that_are_not_rotated_pass_unchanged():
+    """Every bf16 number there is, zeros of both signs among them, in both directions and both pairings; NaN as some NaN."""
+    T, D, rot = 1366, 64, 16
+    x = torch.zeros((T, 1, D), dtype=torch.bfloat16, device="cuda")
+    bits = torch.arange(T * (D - rot), device="cuda").to(torch.int16).view(T, 1, D - rot)
+    x.view(torch.int16)[..., rot:] = bits
+    nan = x[..., rot:].isnan()
+    table = binding.rotary_table(100, rot)
+    positions = torch.arange(T, device="cuda", dtype=torch.int32) % 100
+    for pairs in ("halves", "neighbours"):
+        for y in (*binding.qk_norm_rope(x, x, table, positions, pairs=pairs),
+                  *binding.qk_norm_rope_backward(x, x, x, x, table, positions, pairs=pairs)[:2]):
+            assert torch.equal(y.view(torch.int16)[..., rot:][~nan], bits[~nan]) and y[..., rot:][nan].isnan().all()
+            assert not y[..., :rot].any()
