@@ -62,3 +62,31 @@ def test_features_that_are_not_rotated_pass_unchanged():
                   *binding.qk_norm_rope_backward(x, x, x, x, table, positions, pairs=pairs)[:2]):
             assert torch.equal(y.view(torch.int16)[..., rot:][~nan], bits[~nan]) and y[..., rot:][nan].isnan().all()
             assert not y[..., :rot].any()
+
+
+
+WALKS = [
+    # more units than the device has warps, several units per token and kind
+    (2500, 20, 3, 128, 128, "halves", True, 2),
+    (2500, 20, 3, 128, 32, "neighbours", True, 0),
+    (2501, 20, 3, 64, 48, "halves", True, 1),
+    (3001, 17, 33, 64, 64, "neighbours", False, 0),
+]
+
+
+@pytest.mark.parametrize("case", WALKS)
+def test_several_units_per_warp(case):
+    check_forward(case)
+    check_backward(case)
+
+
+@pytest.mark.parametrize("case", [WALKS[0], WALKS[3]])
+def test_several_units_per_warp_in_place_and_on_parts(case):
+    """In place as out of place; and what is computed for a part of the tokens does not depend on the others."""
+    q, k, wq, wk, table, positions = norm_inputs(case)
+    kw = dict(wq=wq, wk=wk, pairs=case[5])
+    whole = binding.qk_norm_rope(q, k, table, positions, **kw)
+    part = binding.qk_norm_rope(q[77:131], k[77:131], table, positions[77:131].contiguous(), **kw)
+    assert all(torch.equal(w[77:131], p) for w, p in zip(whole, part))
+    binding.qk_norm_rope(q, k, table, positions, **kw, out=(q, k))
+    assert torch.equal(q, whole[0]) and torch.equal(k, whole[1])
