@@ -512,6 +512,8 @@ int zq_qk_norm_rope_backward(const void* dq_bf16, int64_t lddq, const void* dk_b
  * All three are read on the device.  What they name wrongly is not followed: offsets outside the tensors or not ascending, and
  * more new tokens than lens has, make a sequence's new tokens nobody's (written to no page; attention takes them as described
  * there); pages outside the cache, or beyond table_ld, hold NaN and are not written.
+ * Where offsets fall from one sequence to a later one, so that both name the same rows, the first one's new tokens are written in
+ * full, the later one's perhaps only in part, the same ones every time; a result's row that several name is made of theirs.
  */
 
 /*

@@ -1,23 +1,23 @@
 // The 8-bit cache of keys and values: new tokens are quantized as they are written into their pages, and read back.
 //
 // Both are bound by memory: 3 bytes per element (2 read, 1 written; reading back 1 + 2 or 1 + 4).
+#include <climits>
+
 #include "kv_cache.cuh"
 
 namespace zq {
 namespace kv {
 namespace {
 
-// The sequence that owns unit u (see unit_base), found by all threads of the block at once; -1 where none does.
+// The first sequence that owns unit u, found by all threads of the block at once; -1 where none does.
 template <int THREADS>
 __device__ __forceinline__ int block_sequence(const Cache& c, int64_t u, int extra, int* shared) {
-  if (threadIdx.x == 0) *shared = -1;
+  if (threadIdx.x == 0) *shared = INT_MAX;
   __syncthreads();
-  for (int b = threadIdx.x; b < c.B; b += THREADS) {
-    const int64_t lo = load_chained(c.cu + b), hi = load_chained(c.cu + b + 1);
-    if (unit_base(lo, b, c.page, extra) <= u && u < unit_base(hi, b + 1, c.page, extra)) *shared = b;
-  }
+  const int b = unit_sequence(u, c.B, c.page, extra, [&](int i) { return load_chained(c.cu + i); }, c.T, threadIdx.x, THREADS);
+  if (b >= 0) atomicMin(shared, b);
   __syncthreads();
-  return *shared;
+  return *shared == INT_MAX ? -1 : *shared;
 }
 
 // ---- writing ------------------------------------------------------------------------------------------------------
