@@ -60,6 +60,8 @@ __device__ __forceinline__ uint32_t token_piece(int token, int piece) {
   const int sw = kRow == 128 ? token & 7 : kRow == 64 ? (token >> 1) & 3 : (token >> 2) & 1;
   return (piece / kPieces) * (kTok * 128) + token * kRow + (((piece % kPieces) ^ sw) << 4);
 }
+// The first operand is E5M2 instead of E4M3 (or'ed to an instruction descriptor).
+constexpr uint32_t kFirstE5m2 = 1u << 7;
 // E4M3 x E4M3 -> FP32 with the tokens in K on both sides, D is 128 x n
 __device__ __forceinline__ uint32_t idesc_e4m3_mn(uint32_t n) {
   return (1u << 4) | (1u << 15) | (1u << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
@@ -147,8 +149,12 @@ __device__ __forceinline__ void widen_values(const uint8_t* codes, uint8_t* out,
 }
 
 // ---- queries ------------------------------------------------------------------------------------------------------------
-// Eight bf16 features of a row as two E4M3 numbers each: q 2^e = a + b with the row's largest feature between 128 and 256.  A bf16
-// number has 8 bits, an E4M3 number 4: the rest after the first, rounded to nearest, fits the second, down to 2^-9.
+// Eight bf16 features of a row as two 8-bit numbers each: q 2^e = a + b with the row's largest feature between 128 and 256.  A bf16
+// number has 8 bits, a (E4M3) 4; the rest is at most half of a's step, so 3 bits hold it, where b's smallest step does.  That
+// is why b is no E4M3 number as it is (their smallest step is 2^-9: features below 2^-2 lost bits, those below 2^-10 all of them):
+//   few rows    b = E4M3 / 2^5, its products in columns of their own: exact from 2^-7 on (2^-14 of the row's largest and less),
+//               off by 2^-15 at most below (2^-22 of the largest)
+//   many rows   b = E5M2, its products added to a's by the tensor core: exact from 2^-6 on (2^-13), off by 2^-14 at most below (2^-21)
 struct RowScale {
   float up;    // 2^e, 0 where the row is not finite
   float down;  // 2^-e, NaN there
@@ -175,9 +181,11 @@ __device__ __forceinline__ uint32_t absmax_bits8(uint4 v) {
   const uint32_t m = max_u16x2(max_u16x2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), max_u16x2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
   return max(m << 16, m & 0xFFFF0000u);
 }
-// Eight numbers times `up` as two E4M3 numbers each.  In between they are FP16, which holds them: 8 bits, the largest below 2^8
-// (what is below FP16's 2^-24 is zero in E4M3 too).  A row that is not finite has up = 0, NaN for what is not finite in it, and a
-// factor that makes all of its scores NaN.
+// Eight numbers times `up` as two 8-bit numbers each, the second an E4M3 number times 2^-kRestBits (FEW) or an E5M2 one.  In between
+// they are FP16, which holds them: 8 bits, the largest below 2^8, the steps 2^-24.  A row that is not finite has up = 0, NaN for
+// what is not finite in it, and a factor that makes all of its scores NaN.
+constexpr int kRestBits = 5;
+template <bool FEW>
 __device__ __forceinline__ void split8(uint4 v, float up, uint2& first, uint2& second) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
   uint32_t a[4], b[4];
@@ -189,7 +197,12 @@ __device__ __forceinline__ void split8(uint4 v, float up, uint2& first, uint2& s
     asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(c) : "r"(x));
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y) : "h"(c));
     asm("sub.f16x2 %0, %1, %2;" : "=r"(y) : "r"(x), "r"(y));
-    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(d) : "r"(y));
+    if (FEW) {
+      asm("mul.f16x2 %0, %1, %2;" : "=r"(y) : "r"(y), "r"(((15u + kRestBits) << 10) * 0x10001u));  // 2^kRestBits; at most 2^8
+      asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(d) : "r"(y));
+    } else {
+      asm("cvt.rn.satfinite.e5m2x2.f16x2 %0, %1;" : "=h"(d) : "r"(y));
+    }
     a[i] = c;
     b[i] = d;
   }

@@ -3,7 +3,7 @@
 //
 // Keys' and values' codes go from memory to the tensor core as they are; what meets them is written as sums of E4M3 numbers, side
 // by side in the columns:
-//   S^T [128 tokens, 2 x rows] = K [tokens, D] q^T      q = q1 + q2, exact for bf16 features down to 2^-17 of the row's largest
+//   S^T [128 tokens, 2 x rows] = K [tokens, D] q^T      q = q1 + q2 / 2^5, exact for bf16 features from 2^-14 of the row's largest on
 //   O^T [D, 3 x rows] += V^T [D, tokens] P^T            P = P1 + P2 / 2^4 + P3 / 2^8, each the rest of the one before, with
 //                                                       accumulators of its own: 12 bits, and something down to 2^-26 of the largest
 // Tokens and features are the tensor core's 128 lanes, the rows its columns: more columns for more terms cost little.  (With the
@@ -551,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           }
           tc_fence_after_sync();
           // scores of this thread's token of its tiles, x[k][r] for the k-th, plus the values' scale:
-          // (a + b) (row's factor) (keys' scale) + log2(values' scale)
+          // (a + b / 2^5) (row's factor) (keys' scale) + log2(values' scale)
           float inv[kMine];
 #pragma unroll
           for (int k = 0; k < kMine; ++k) {
@@ -569,7 +569,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
               tmem_ld_wait_regs<S>(x[k] + r);
               tmem_ld_wait_regs<S>(y);
 #pragma unroll
-              for (int i = 0; i < S; ++i) x[k][r + i] = fmaf(x[k][r + i] + y[i], info[r + i].x * e.x, e.y);
+              for (int i = 0; i < S; ++i) x[k][r + i] = fmaf(fmaf(y[i], 1.0f / (1 << kRestBits), x[k][r + i]), info[r + i].x * e.x, e.y);
             }
             // all of the tile is seen by all rows (the first row sees the fewest behind, the last the fewest before)
             if (!(tile + (kTok - 1) <= seen_to && tile >= seen_from)) {
@@ -711,7 +711,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
           for (int o = kLanes / 2; o; o >>= 1) a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
           const RowScale s = row_scale(a);
           uint2 first, second;
-          split8(x[k], s.up, first, second);
+          split8<true>(x[k], s.up, first, second);
           if (r < rows) {
             const int piece = (i % kLanes) >> 1, half = (i & 1) * 8;
             *reinterpret_cast<uint2*>(to + row_piece<D>(r, piece) + half) = first;

@@ -1,7 +1,7 @@
 // Attention over the 8-bit cache where a sequence and cache head have many rows (new tokens x query heads of the head, more than
 // 64): prompts.  Bound by arithmetic: the tensor core's 4 D operations and one power of two per row and visible token.
 //
-//   S [128 rows, 128 tokens] = q K^T       E4M3 x E4M3; q is a sum of two E4M3 numbers, so two products: the keys' codes go to
+//   S [128 rows, 128 tokens] = q K^T       q is the sum of an E4M3 and an E5M2 number, so two products: the keys' codes go to
 //                                          the tensor core as they are, at the price of one FP16 product
 //   O [128 rows, D] += P V                 FP16 x FP16 (FP32 results: P is the sum of two FP16 numbers, 11 bits are not enough for
 //                                          them, and the sequences with few rows are here too); P from tensor memory, over the scores it was made of; the values'
@@ -529,7 +529,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
           for (int term = 0; term < 2; ++term)
 #pragma unroll
             for (int s = 0; s < D / 32; ++s)
-              umma_f8(to_s + buf * kStep, qdesc + static_cast<uint64_t>((term * C::kTileBytes) >> 4) + s * 2, bd + s * 2, sdesc_i, (term > 0 || s > 0) ? 1u : 0u);
+              umma_f8(to_s + buf * kStep, qdesc + static_cast<uint64_t>((term * C::kTileBytes) >> 4) + s * 2, bd + s * 2,
+                      term > 0 ? sdesc_i | kFirstE5m2 : sdesc_i, (term > 0 || s > 0) ? 1u : 0u);
           umma_commit(&s_full[q * 2 + buf]);
           if (ends) umma_commit(&k_empty[k.i]);
           if (at + 1 == steps) umma_commit(q_empty);
@@ -708,7 +709,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
         for (int u = 0; u < kBatch; ++u) {
           const RowScale s = row_scale(a[u]);
           uint2 a0, b0;
-          split8(x[u], s.up, a0, b0);
+          split8<false>(x[u], s.up, a0, b0);
           *reinterpret_cast<uint2*>(to + u * (kRowsStep * D)) = a0;  // (a step of 8 rows or 16, which the swizzle does not see)
           *reinterpret_cast<uint2*>(to + C::kTileBytes + u * (kRowsStep * D)) = b0;
           if (l == 0) s_rows[r0 + u * kRowsStep] = s.down * p.scale_log2;

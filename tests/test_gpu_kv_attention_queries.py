@@ -1,0 +1,33 @@
+"""What the tensor core's terms leave of the queries: attention over the 8-bit cache where a query's features differ much in size.
+
+A row is scaled so that its largest feature lies in [128, 256).  The two terms of a feature are exact from 2^-13 of the
+largest on."""
+import pytest
+import torch
+
+import kv_ref as R
+from paper_2307_09782_b200 import binding
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.mark.parametrize("lens,new,Hq,H,D,page", [([700, 40], [1, 1], 4, 2, 128, 64), ([700, 40], [7, 3], 8, 2, 64, 16),
+                                                  ([500, 300], [400, 120], 4, 2, 128, 32)])
+@pytest.mark.parametrize("out,exponent", [(BF16, -3), (BF16, -6), (F32, -3), (F32, -6)])
+def test_small_features_beside_a_large_one(lens, new, Hq, H, D, page, out, exponent):
+    """One feature of 200 that all keys answer with zero, the others 2^exponent 183 / 128, a number of 8 bits, against
+    positive keys: whatever is lost of one is lost of all, and shows in the logarithm of the sum.  That is FP32 for both
+    types: off by 2^-18 of sum |q| |k| and 2^-17 at most, as in test_gpu_kv_attention.py."""
+    codes, scale, table, lens, cu = R.batch(lens, new, H, D, page)
+    codes[:, 0] &= 0x7F
+    codes[:, 0, :, :, 5] = 0
+    q = torch.full((cu[-1], Hq, D), 2.0 ** exponent * 183 / 128, device="cuda").to(BF16)
+    q[..., 5] = 200.0
+    sm = 2.0 ** -exponent / D  # scores of a few units
+    _, lse = binding.kv_attention(binding.Fp8KvCache(codes, scale), q, table, R.ints(lens), cu=R.ints(cu), sm_scale=sm, out_dtype=out,
+                                  lse=True)
+    _, ref, (_, qk, _) = R.attention(codes, scale, q, table, lens, cu, sm, True, 0)
+    err, tol = (lse.to(R.F64) - ref).abs(), 2.0 ** -17 + 2.0 ** -18 * qk + 2.0 ** -22 * ref.abs()
+    assert (err <= tol).all(), float((err / tol).max())
+
