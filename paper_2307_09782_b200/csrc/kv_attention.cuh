@@ -155,6 +155,7 @@ __device__ __forceinline__ void widen_values(const uint8_t* codes, uint8_t* out,
 //   few rows    b = E4M3 / 2^5, its products in columns of their own: exact from 2^-7 on (2^-14 of the row's largest and less),
 //               off by 2^-15 at most below (2^-22 of the largest)
 //   many rows   b = E5M2, its products added to a's by the tensor core: exact from 2^-6 on (2^-13), off by 2^-14 at most below (2^-21)
+//   and for FP32 results what b leaves as E5M2 once more: exact from 2^-9 on (2^-16), off by 2^-17 at most below (2^-24)
 struct RowScale {
   float up;    // 2^e, 0 where the row is not finite
   float down;  // 2^-e, NaN there
@@ -181,33 +182,39 @@ __device__ __forceinline__ uint32_t absmax_bits8(uint4 v) {
   const uint32_t m = max_u16x2(max_u16x2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), max_u16x2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
   return max(m << 16, m & 0xFFFF0000u);
 }
-// Eight numbers times `up` as two 8-bit numbers each, the second an E4M3 number times 2^-kRestBits (FEW) or an E5M2 one.  In between
-// they are FP16, which holds them: 8 bits, the largest below 2^8, the steps 2^-24.  A row that is not finite has up = 0, NaN for
-// what is not finite in it, and a factor that makes all of its scores NaN.
+// Eight numbers times `up` as TERMS 8-bit numbers each: an E4M3 number, then an E4M3 number times 2^-kRestBits (FEW) or E5M2 ones.  In
+// between they are FP16, which holds them: 8 bits, the largest below 2^8, the steps 2^-24.  A row that is not finite has up = 0,
+// NaN for what is not finite in it, and a factor that makes all of its scores NaN.
 constexpr int kRestBits = 5;
-template <bool FEW>
-__device__ __forceinline__ void split8(uint4 v, float up, uint2& first, uint2& second) {
+template <bool FEW, int TERMS>
+__device__ __forceinline__ void split8(uint4 v, float up, uint2* term) {
+  static_assert(TERMS == 2 || (TERMS == 3 && !FEW), "terms");
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  uint32_t a[4], b[4];
+  uint32_t t[TERMS][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t x = pack_f16(bf16_lo(w[i]) * up, bf16_hi(w[i]) * up);
-    uint16_t c, d;
-    uint32_t y;
+    uint32_t x = pack_f16(bf16_lo(w[i]) * up, bf16_hi(w[i]) * up), y;
+    uint16_t c;
     asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(c) : "r"(x));
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y) : "h"(c));
-    asm("sub.f16x2 %0, %1, %2;" : "=r"(y) : "r"(x), "r"(y));
+    asm("sub.f16x2 %0, %1, %2;" : "=r"(x) : "r"(x), "r"(y));
+    t[0][i] = c;
     if (FEW) {
-      asm("mul.f16x2 %0, %1, %2;" : "=r"(y) : "r"(y), "r"(((15u + kRestBits) << 10) * 0x10001u));  // 2^kRestBits; at most 2^8
-      asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(d) : "r"(y));
+      asm("mul.f16x2 %0, %1, %2;" : "=r"(x) : "r"(x), "r"(((15u + kRestBits) << 10) * 0x10001u));  // 2^kRestBits; at most 2^8
+      asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(c) : "r"(x));
     } else {
-      asm("cvt.rn.satfinite.e5m2x2.f16x2 %0, %1;" : "=h"(d) : "r"(y));
+      asm("cvt.rn.satfinite.e5m2x2.f16x2 %0, %1;" : "=h"(c) : "r"(x));
     }
-    a[i] = c;
-    b[i] = d;
+    t[1][i] = c;
+    if (TERMS == 3) {
+      asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(y) : "h"(c));
+      asm("sub.f16x2 %0, %1, %2;" : "=r"(x) : "r"(x), "r"(y));
+      asm("cvt.rn.satfinite.e5m2x2.f16x2 %0, %1;" : "=h"(c) : "r"(x));
+      t[TERMS - 1][i] = c;
+    }
   }
-  first = make_uint2(a[0] | (a[1] << 16), a[2] | (a[3] << 16));
-  second = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
+#pragma unroll
+  for (int k = 0; k < TERMS; ++k) term[k] = make_uint2(t[k][0] | (t[k][1] << 16), t[k][2] | (t[k][3] << 16));
 }
 
 // ---- block scales -------------------------------------------------------------------------------------------------------

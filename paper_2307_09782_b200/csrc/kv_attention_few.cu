@@ -710,12 +710,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
 #pragma unroll
           for (int o = kLanes / 2; o; o >>= 1) a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
           const RowScale s = row_scale(a);
-          uint2 first, second;
-          split8<true>(x[k], s.up, first, second);
+          uint2 term[2];
+          split8<true, 2>(x[k], s.up, term);
           if (r < rows) {
             const int piece = (i % kLanes) >> 1, half = (i & 1) * 8;
-            *reinterpret_cast<uint2*>(to + row_piece<D>(r, piece) + half) = first;
-            *reinterpret_cast<uint2*>(to + row_piece<D>(RS + r, piece) + half) = second;
+            *reinterpret_cast<uint2*>(to + row_piece<D>(r, piece) + half) = term[0];
+            *reinterpret_cast<uint2*>(to + row_piece<D>(RS + r, piece) + half) = term[1];
             if (i % kLanes == 0) {
               const int64_t pos = static_cast<int64_t>(g.L) - g.n + r / p.G;
               const int64_t hi = p.causal ? min(pos + 1, static_cast<int64_t>(g.L)) : g.L;

@@ -1,8 +1,8 @@
 // Attention over the 8-bit cache where a sequence and cache head have many rows (new tokens x query heads of the head, more than
 // 64): prompts.  Bound by arithmetic: the tensor core's 4 D operations and one power of two per row and visible token.
 //
-//   S [128 rows, 128 tokens] = q K^T       q is the sum of an E4M3 and an E5M2 number, so two products: the keys' codes go to
-//                                          the tensor core as they are, at the price of one FP16 product
+//   S [128 rows, 128 tokens] = q K^T       q is the sum of an E4M3 and an E5M2 number (FP32 results: and of another), so two
+//                                          products: the keys' codes go to the tensor core as they are, at the price of one FP16 product
 //   O [128 rows, D] += P V                 FP16 x FP16 (FP32 results: P is the sum of two FP16 numbers, 11 bits are not enough for
 //                                          them, and the sequences with few rows are here too); P from tensor memory, over the scores it was made of; the values'
 //                                          codes are widened in shared memory, once for 256 rows
@@ -57,13 +57,14 @@ struct P {
   int* status;
 };
 
-template <int D>
+template <int D, bool EXACT>
 struct Cfg {
+  static constexpr int kTerms = EXACT ? 3 : 2;                              // of the queries
   static constexpr int kTileBytes = kTok * D;
   static constexpr int kValueBytes = kTok * D * 2;
-  static constexpr int kKeySlots = 3, kValueSlots = 2;
-  static constexpr int kOffQueries = 0;                                     // [2 tiles][2 terms][128 rows of D]
-  static constexpr int kOffValues = kOffQueries + 4 * kTileBytes;           // [2] widened
+  static constexpr int kKeySlots = EXACT && D == 128 ? 2 : 3, kValueSlots = 2;  // (what there is room for)
+  static constexpr int kOffQueries = 0;                                     // [2 tiles][kTerms][128 rows of D]
+  static constexpr int kOffValues = kOffQueries + 2 * kTerms * kTileBytes;  // [2] widened
   static constexpr int kOffKeys = kOffValues + 2 * kValueBytes;
   static constexpr int kOffCodes = kOffKeys + kKeySlots * kTileBytes;
   static constexpr int kOffScales = kOffCodes + kValueSlots * kTileBytes;   // [kScaleSlots][8] float4
@@ -302,7 +303,7 @@ __device__ __forceinline__ bool softmax_step(float* x, const float4* scales, flo
 
 template <int D, bool EXACT>
 __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ CUtensorMap tm_q, const P p) {
-  using C = Cfg<D>;
+  using C = Cfg<D, EXACT>;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bar = reinterpret_cast<uint64_t*>(smem + C::kOffBars);
   uint64_t* k_full = bar;                          // [key slots] a tile's keys have landed                 (MMA)
@@ -483,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
     fp8b::regs_give<72>();
     const int q = warp - kMmaWarp;
     const bool issuer = elect_one();
-    const uint64_t kdesc = desc_rows<D>(smem_u32(smem + C::kOffKeys)), qdesc = desc_rows<D>(smem_u32(smem + C::kOffQueries + q * 2 * C::kTileBytes));
+    const uint64_t kdesc = desc_rows<D>(smem_u32(smem + C::kOffKeys)), qdesc = desc_rows<D>(smem_u32(smem + C::kOffQueries + q * C::kTerms * C::kTileBytes));
     const uint64_t vdesc = desc_values(smem_u32(smem + C::kOffValues));
     const uint32_t sdesc_i = umma_idesc_e4m3(kStep), odesc_i = idesc_f16(D, false, true);
     const uint32_t to_s = tmem + q * kTok, to_o = tmem + 256 + q * 128;
@@ -526,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
         if (issuer) {
           const uint64_t bd = kdesc + static_cast<uint64_t>((k.i * C::kTileBytes + half * kStep * D) >> 4);
 #pragma unroll
-          for (int term = 0; term < 2; ++term)
+          for (int term = 0; term < C::kTerms; ++term)
 #pragma unroll
             for (int s = 0; s < D / 32; ++s)
               umma_f8(to_s + buf * kStep, qdesc + static_cast<uint64_t>((term * C::kTileBytes) >> 4) + s * 2, bd + s * 2,
@@ -655,7 +656,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       __syncwarp();
       done_with(seg);
       // Queries, once those there are done with (two steps before the item's end): all rows are copied to where they are going to
-      // be, half of a row in the place of each of its terms, then converted there.  (Loads to registers, of which there were
+      // be, half of a row in the place of each of its first two terms, then converted there.  (Loads to registers, of which there were
       // 16 per warp on their way, cost 28000 cycles between two items, and copies of rows 10000 just to ask for, where two boxes
       // per tile cannot have them.)
       if (items > 0 && !fp8b::mbar_wait_all(q_empty, (items - 1) & 1, s_abort)) {
@@ -667,13 +668,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
           mbar_arrive_expect_tx(r_full, (rows > kTok ? kRows : kTok) * 2 * D);
           for (int r = 0; r < rows; r += kTok)
             for (int half = 0; half < 2; ++half)
-              tma_load_4d(smem + C::kOffQueries + (r / kTok * 2 + half) * C::kTileBytes, &tm_q, 0, half, h * p.G, first + (row0 + r) / p.G, r_full);
+              tma_load_4d(smem + C::kOffQueries + (r / kTok * C::kTerms + half) * C::kTileBytes, &tm_q, 0, half, h * p.G, first + (row0 + r) / p.G, r_full);
         }
       } else {
         if (i == 0) mbar_arrive_expect_tx(r_full, rows * 2 * D);
         for (int r = i; r < rows; r += kTok) {
           const __nv_bfloat16* src = p.q + (first + (row0 + r) / p.G) * p.ldq + (static_cast<int64_t>(h) * p.G + (row0 + r) % p.G) * D;
-          uint8_t* to = smem + C::kOffQueries + (r / kTok) * 2 * C::kTileBytes + i * D;
+          uint8_t* to = smem + C::kOffQueries + (r / kTok) * C::kTerms * C::kTileBytes + i * D;
           bulk_load(to, src, D, r_full);
           bulk_load(to + C::kTileBytes, src + D / 2, D, r_full);
         }
@@ -691,7 +692,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
 #pragma unroll 1
       for (int r0 = (warp - kConvWarp0) * kRowsPer + lane / kLanes; r0 < (rows > kTok ? kRows : kTok); r0 += kBatch * kRowsStep) {
         const int l = lane % kLanes;
-        uint8_t* row = smem + C::kOffQueries + (r0 / kTok * 2 * kTok + r0 % kTok) * D;
+        uint8_t* row = smem + C::kOffQueries + (r0 / kTok * C::kTerms * kTok + r0 % kTok) * D;
         const uint8_t* from = row + l / (kLanes / 2) * C::kTileBytes + l % (kLanes / 2) * 16;
         uint8_t* to = row - r0 % kTok * D + row_piece<D>(r0 % kTok, l / 2) + (l & 1) * 8;
         uint4 x[kBatch];
@@ -708,10 +709,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
           const RowScale s = row_scale(a[u]);
-          uint2 a0, b0;
-          split8<false>(x[u], s.up, a0, b0);
-          *reinterpret_cast<uint2*>(to + u * (kRowsStep * D)) = a0;  // (a step of 8 rows or 16, which the swizzle does not see)
-          *reinterpret_cast<uint2*>(to + C::kTileBytes + u * (kRowsStep * D)) = b0;
+          uint2 term[C::kTerms];
+          split8<false, C::kTerms>(x[u], s.up, term);
+#pragma unroll
+          for (int k = 0; k < C::kTerms; ++k)  // (a step of 8 rows or 16, which the swizzle does not see)
+            *reinterpret_cast<uint2*>(to + k * C::kTileBytes + u * (kRowsStep * D)) = term[k];
           if (l == 0) s_rows[r0 + u * kRowsStep] = s.down * p.scale_log2;
         }
       }
@@ -925,7 +927,7 @@ __global__ void __launch_bounds__(256) attention_join_rows_kernel(const P p, int
 
 template <int D, bool EXACT>
 int launch_cfg(const CUtensorMap& tm, const CUtensorMap& tm_q, const P& p, int grid, cudaStream_t st) {
-  using C = Cfg<D>;
+  using C = Cfg<D, EXACT>;
   static DeviceOnce once;
   if (!allow_shared_memory(once, attention_rows_kernel<D, EXACT>, C::kSmemBytes)) return ZQ_ERR_CUDA;
   cudaError_t e = launch_chained(attention_rows_kernel<D, EXACT>, dim3(grid), dim3(kThreads), C::kSmemBytes, st, false, tm, tm_q, p);

@@ -1,7 +1,7 @@
 """What the tensor core's terms leave of the queries: attention over the 8-bit cache where a query's features differ much in size.
 
-A row is scaled so that its largest feature lies in [128, 256).  The two terms of a feature are exact from 2^-13 of the
-largest on."""
+A row is scaled so that its largest feature lies in [128, 256).  bf16 results: two terms, exact for the features from 2^-13 of the
+largest on.  FP32 results: three terms, exact from 2^-16 of the largest on; smaller features are off by 2^-24 of the largest at most."""
 import pytest
 import torch
 
@@ -14,7 +14,7 @@ BF16, F32 = torch.bfloat16, torch.float32
 
 @pytest.mark.parametrize("lens,new,Hq,H,D,page", [([700, 40], [1, 1], 4, 2, 128, 64), ([700, 40], [7, 3], 8, 2, 64, 16),
                                                   ([500, 300], [400, 120], 4, 2, 128, 32)])
-@pytest.mark.parametrize("out,exponent", [(BF16, -3), (BF16, -6), (F32, -3), (F32, -6)])
+@pytest.mark.parametrize("out,exponent", [(BF16, -3), (BF16, -6), (F32, -3), (F32, -6), (F32, -9)])
 def test_small_features_beside_a_large_one(lens, new, Hq, H, D, page, out, exponent):
     """One feature of 200 that all keys answer with zero, the others 2^exponent 183 / 128, a number of 8 bits, against
     positive keys: whatever is lost of one is lost of all, and shows in the logarithm of the sum.  That is FP32 for both
@@ -31,3 +31,22 @@ def test_small_features_beside_a_large_one(lens, new, Hq, H, D, page, out, expon
     err, tol = (lse.to(R.F64) - ref).abs(), 2.0 ** -17 + 2.0 ** -18 * qk + 2.0 ** -22 * ref.abs()
     assert (err <= tol).all(), float((err / tol).max())
 
+
+@pytest.mark.parametrize("case", [([4096], [130], 4, 4, 128, 32, True, 0), ([4000] * 3, [1] * 3, 16, 8, 128, 64, True, 0),
+                                  ([2000, 90], [9, 60], 8, 2, 64, 64, True, 0)])
+@pytest.mark.parametrize("factor", [20.0, 100.0])
+def test_fp32_results_beside_a_large_feature(case, factor):
+    """In the 2-norm, one feature of each query `factor` times as large as the others.  What the three terms leave is nothing beside the
+    rest; a score of the size s = factor D^-1/2 is summed up in 3 D / 32 <= 12 steps, each off by 2^-23 of a partial sum at most
+    and half of it on average: 6 2^-23 s < 2^-17.2 for factor 100 (s = 8.9; D = 64: 3 2^-23 12.5), which counts in the numerator and in the
+    sum, and two roundings of scores and factors (2^-24 s each): < 2^-15.9."""
+    lens, new, Hq, H, D, page, causal, window = case
+    codes, scale, table, lens, cu = R.batch(lens, new, H, D, page, spread=0.0)
+    q = torch.randn((cu[-1], Hq, D), generator=torch.Generator(device="cuda").manual_seed(5), device="cuda")
+    q[..., 17] *= factor
+    q = q.to(BF16)
+    got = binding.kv_attention(binding.Fp8KvCache(codes, scale), q, table, R.ints(lens), cu=R.ints(cu), out_dtype=F32)
+    ref, _, _ = R.attention(codes, scale, q, table, lens, cu, D ** -0.5, causal, window)
+    err = float((got.to(R.F64) - ref).norm() / ref.norm())
+    print(f"factor {factor}: {err:.2e}")
+    assert err <= 2.0 ** -15.5
