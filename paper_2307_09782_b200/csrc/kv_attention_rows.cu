@@ -4,13 +4,20 @@
 //   S [128 rows, 128 tokens] = q K^T       q is the sum of an E4M3 and an E5M2 number (FP32 results: and of another), so two
 //                                          products: the keys' codes go to the tensor core as they are, at the price of one FP16 product
 //   O [128 rows, D] += P V                 FP16 x FP16 (FP32 results: P is the sum of two FP16 numbers, 11 bits are not enough for
-//                                          them, and the sequences with few rows are here too); P from tensor memory, over the scores it was made of; the values'
-//                                          codes are widened in shared memory, once for 256 rows
+//                                          them, and the sequences with few rows are here too); P from tensor memory, over the
+//                                          scores it was made of; the values' codes are widened in shared memory, once for 256 rows
 // Rows are the tensor core's lanes and a softmax thread's own: maxima and sums need no other thread.  A CTA works on two tiles of
 // 128 rows in turn, each in steps of 64 tokens whose scores alternate between two places in tensor memory: the next step's are there
 // when a softmax is done (with steps of 128 and one place it waited 2400 of 5800 cycles).  The running maximum only moves when a
 // score exceeds it by more than kSlack (in powers of two; FP16 has the room): the accumulator is then multiplied by the row's own
 // warp.
+//
+// The tensor core adds to an accumulator by cutting off (2^-23 of it at most for each product of 16 tokens; a tenth to a third of
+// that, measured), so a long sum shrinks: with two terms of P by 1e-5 to 4e-5 over 8192 tokens.  For FP32 results the row's warp
+// therefore adds it after kSumSteps steps, rounding to nearest, to a sum in the workspace (the place of the CTA's partial results that
+// the item has, or nobody yet), and the next product begins anew: 1e-6 to 3e-6 whatever the number of tokens, chunks of 777 tokens behind
+// others 331 -> 349 us (16 steps: twice that, 338 us).  bf16 results, with one term, are left as they are: N tokens take
+// N 2^-27 at most, below their rounding of 2^-9 up to 2^18 tokens (and the loop is not the same: prompt of 8191 tokens 696 -> 745 us).
 //
 // All items (sequence, 256 rows, head) stand in a row, each as long as its tokens and what it costs to begin and end one, and every CTA
 // gets an equal part of the row (whole items in rounds: a prompt of 8191 tokens 732 us instead of 655).  An item that reaches over a
@@ -53,12 +60,13 @@ struct P {
   float* lse;
   int4* shared;    // [CTAs] the item that begins in the CTA and goes on in the next: sequence, number, 1 (0: none does); and of the
                    // item that came from the CTA before: 1 it goes on, 2 it ends here (0: none came)
-  float* partial;  // [CTAs][2: what came from the CTA before, what goes on][256 (D + 2)]
+  float* partial;  // [CTAs][2: what came from the CTA before, what goes on][256 (D + 2)]: results (sum_at), then sums, then maxima
   int* status;
 };
 
 template <int D, bool EXACT>
 struct Cfg {
+  static constexpr int kSumSteps = 8;                                       // that an accumulator takes (EXACT)
   static constexpr int kTerms = EXACT ? 3 : 2;                              // of the queries
   static constexpr int kTileBytes = kTok * D;
   static constexpr int kValueBytes = kTok * D * 2;
@@ -182,6 +190,9 @@ struct alignas(16) Seg {
 };
 static_assert(sizeof(Seg) == 48, "Seg");
 
+// Features d .. d + 3 of row r among the results of a place: rows side by side, as the threads are that have them.
+__device__ __forceinline__ int64_t sum_at(int r, int d) { return (static_cast<int64_t>(d >> 2) * kRows + r) * 4; }
+
 struct Ring {
   int i = 0;
   uint32_t phase = 0;
@@ -223,8 +234,8 @@ __device__ __forceinline__ void store16(const P& p, int64_t at, const float* v) 
 }
 
 // A softmax thread's step of scores x (its row, 64 tokens) -> probabilities in tensor memory.  `scales`: of its 4 groups of 16 tokens;
-// `lo`, `hi`: tokens of the step that the row sees (looked at with MASK).  May move the row's reference m and multiplies what is in
-// the accumulator and l by the factor.
+// `lo`, `hi`: tokens of the step that the row sees (looked at with MASK).  May move the row's reference m and multiplies l and,
+// unless it begins anew (`first`), what is in the accumulator by the factor.
 template <int D, bool EXACT, bool MASK, typename Wait>
 __device__ __forceinline__ bool softmax_step(float* x, const float4* scales, float c, int lo, int hi, float& m, float& l, uint32_t probs,
                                              uint32_t acc, bool first, Wait accumulated) {
@@ -299,6 +310,36 @@ __device__ __forceinline__ bool softmax_step(float* x, const float4* scales, flo
   }
   tmem_st_wait();
   return true;
+}
+
+// Results o of a row, features d .. d + 31, and the sum in the workspace times f.
+__device__ __forceinline__ void add_sum32(float* o, const float* sum, int r, int d, float f) {
+  float4 s[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) s[k] = *reinterpret_cast<const float4*>(sum + sum_at(r, d + 4 * k));
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    o[4 * k] = fmaf(s[k].x, f, o[4 * k]);
+    o[4 * k + 1] = fmaf(s[k].y, f, o[4 * k + 1]);
+    o[4 * k + 2] = fmaf(s[k].z, f, o[4 * k + 2]);
+    o[4 * k + 3] = fmaf(s[k].w, f, o[4 * k + 3]);
+  }
+}
+// What a sum with the reference m_sum is multiplied by where the reference is m.
+__device__ __forceinline__ float carried(float m_sum, float m) { return m_sum == m ? 1.0f : fp8b::sfu_ex2(m_sum - m); }
+// The accumulator of a row into its sum in the workspace (into nothing where there is none yet).  The features stand where the
+// accumulator has them, until the item ends.
+template <int D>
+__device__ __forceinline__ void add_to_sum(uint32_t acc, float* sum, int r, bool has, float f) {
+#pragma unroll 1
+  for (int d = 0; d < D; d += 32) {
+    float o[32];
+    fp8b::tmem_ld32(acc + d, o);
+    fp8b::tmem_ld_wait32(o);
+    if (has) add_sum32(o, sum, r, d, f);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) *reinterpret_cast<float4*>(sum + sum_at(r, d + 4 * k)) = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+  }
 }
 
 template <int D, bool EXACT>
@@ -555,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
           const uint64_t bd = vdesc + static_cast<uint64_t>((v.i * C::kValueBytes + (st & 1) * kStep * 128) >> 4);
 #pragma unroll
           for (int s = 0; s < kStep / 16; ++s)
-            umma_f16_tmem_a(to_o, to_s + buf * kStep + s * 8, bd + s * (2048 >> 4), odesc_i, (st > 0 || s > 0) ? 1u : 0u);
+            umma_f16_tmem_a(to_o, to_s + buf * kStep + s * 8, bd + s * (2048 >> 4), odesc_i, ((EXACT ? st % C::kSumSteps : st) != 0 || s > 0) ? 1u : 0u);
           if (EXACT)
 #pragma unroll
             for (int s = 0; s < kStep / 16; ++s)
@@ -759,7 +800,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       const int hi = mine && p.causal ? static_cast<int>(max(min(pos + 1, static_cast<int64_t>(L)), static_cast<int64_t>(0))) : L;
       const int lo = mine && p.window > 0 ? static_cast<int>(max(pos + 1 - p.window, static_cast<int64_t>(0))) : 0;
       const int hi_all = __reduce_min_sync(0xFFFFFFFFu, hi), lo_all = __reduce_max_sync(0xFFFFFFFFu, lo);
-      float m = -INFINITY, l = 0.0f;
+      float m = -INFINITY, l = 0.0f, m_sum = -INFINITY;  // m_sum: the reference of the sum in the workspace
+      auto place = [&] { return p.partial + static_cast<int64_t>(part >= 0 ? part : 2 * blockIdx.x + 1) * (kRows * (D + 2)); };
       if (!fp8b::mbar_wait_all(q_full, items & 1, s_abort)) {
         failed = true;
         break;
@@ -768,18 +810,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       const float c = q * kTok < rows ? s_rows[r] : 0.0f;
       __syncwarp();
       if (lane == 0) mbar_arrive(q_empty);
-      for (int st = 0; st < steps; ++st) {
+      auto step = [&](int st, bool first) {
         const int slot = tiles % kScaleSlots;
-        if ((st & 1) == 0 && !fp8b::mbar_wait_all(&e_full[slot], (tiles / kScaleSlots) & 1, s_abort)) {
-          failed = true;
-          break;
-        }
+        if ((st & 1) == 0 && !fp8b::mbar_wait_all(&e_full[slot], (tiles / kScaleSlots) & 1, s_abort)) return false;
         if (q * kTok < rows) {
           const int buf = done & 1;
-          if (!fp8b::mbar_wait_all(&s_full[q * 2 + buf], (done >> 1) & 1, s_abort)) {
-            failed = true;
-            break;
-          }
+          if (!fp8b::mbar_wait_all(&s_full[q * 2 + buf], (done >> 1) & 1, s_abort)) return false;
           tc_fence_after_sync();
           float x[kStep];
 #pragma unroll
@@ -791,12 +827,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
           const float4* e = table + slot * 8 + (st & 1) * (kStep / 16);
           const uint32_t probs = ts + buf * kStep;
           const bool ok = base >= lo_all && base + (kStep - 1) < hi_all
-                              ? softmax_step<D, EXACT, false>(x, e, c, 0, kStep, m, l, probs, to, st == 0, accumulated)
-                              : softmax_step<D, EXACT, true>(x, e, c, lo - base, hi - base, m, l, probs, to, st == 0, accumulated);
-          if (!ok) {
-            failed = true;
-            break;
-          }
+                              ? softmax_step<D, EXACT, false>(x, e, c, 0, kStep, m, l, probs, to, first, accumulated)
+                              : softmax_step<D, EXACT, true>(x, e, c, lo - base, hi - base, m, l, probs, to, first, accumulated);
+          if (!ok) return false;
           tc_fence_before_sync();
           __syncwarp();
           if (lane == 0) mbar_arrive(&p_full[q * 2 + buf]);
@@ -807,6 +840,23 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
           if (lane == 0) mbar_arrive(&e_empty[slot]);
           ++tiles;
         }
+        return true;
+      };
+      if (EXACT) {
+        for (int begin = 0; begin < steps && !failed; begin += C::kSumSteps) {
+          if (begin > 0 && q * kTok < rows) {
+            if (!fp8b::mbar_wait_all(&pv_done[q * 2 + ((done - 1) & 1)], ((done - 1) >> 1) & 1, s_abort)) {
+              failed = true;
+              break;
+            }
+            tc_fence_after_sync();
+            add_to_sum<D>(to, place(), r, begin > C::kSumSteps, carried(m_sum, m));
+            m_sum = m;
+          }
+          for (int st = begin; st < min(steps, begin + C::kSumSteps) && !failed; ++st) failed = !step(st, st == begin);
+        }
+      } else {
+        for (int st = 0; st < steps && !failed; ++st) failed = !step(st, st == 0);
       }
       if (failed) break;
       if (q * kTok >= rows) continue;
@@ -817,11 +867,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
         break;
       }
       tc_fence_after_sync();
-      float* to_part = part < 0 ? nullptr : p.partial + static_cast<int64_t>(part) * (kRows * (D + 2));
+      float* sum = place();
       const int hq = h * p.G + row % p.G;
       if (part >= 0) {
-        to_part[kRows * D + r] = l;
-        to_part[kRows * D + kRows + r] = m;
+        sum[kRows * D + r] = l;
+        sum[kRows * D + kRows + r] = m;
       } else if (mine && p.lse) {
         p.lse[t * (static_cast<int64_t>(p.G) * p.c.H) + hq] = l == 0.0f ? -INFINITY : (log2f(l) + m + 8.0f - kShift) * (1.0f / kLog2e);
       }
@@ -831,6 +881,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
         float o[32];
         fp8b::tmem_ld32(to + d, o);
         fp8b::tmem_ld_wait32(o);
+        if (EXACT && steps > C::kSumSteps) add_sum32(o, sum, r, d, carried(m_sum, m));
 #pragma unroll
         for (int k = 0; k < 32; k += 4) {  // features in their places again (see feature_at)
           const float x = o[k + 1] * f;
@@ -841,7 +892,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
         }
         if (part >= 0) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) *reinterpret_cast<float4*>(to_part + r * D + d + 4 * k) = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+          for (int k = 0; k < 8; ++k) *reinterpret_cast<float4*>(sum + sum_at(r, d + 4 * k)) = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
         } else if (mine) {
           store16(p, t * p.ldo + static_cast<int64_t>(hq) * D + d, o);
           store16(p, t * p.ldo + static_cast<int64_t>(hq) * D + d + 16, o + 16);
@@ -909,7 +960,7 @@ __global__ void __launch_bounds__(256) attention_join_rows_kernel(const P p, int
     const float f = s_w[warp][i - x];
     if (f == 0.0f) continue;  // (what lies there is nothing)
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(f, load_chained(piece(i) + r * D + e * 32 + lane), o[e]);
+    for (int e = 0; e < E; ++e) o[e] = fmaf(f, load_chained(piece(i) + sum_at(r, e * 32 + lane) + (lane & 3)), o[e]);
   }
   const int64_t t = s.first + (row0 + r) / p.G;
   const int hq = h * p.G + static_cast<int>((row0 + r) % p.G);

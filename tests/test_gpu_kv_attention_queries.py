@@ -50,3 +50,35 @@ def test_fp32_results_beside_a_large_feature(case, factor):
     err = float((got.to(R.F64) - ref).norm() / ref.norm())
     print(f"factor {factor}: {err:.2e}")
     assert err <= 2.0 ** -15.5
+
+
+@pytest.mark.parametrize("out", [F32, BF16])
+@pytest.mark.parametrize("L,n,Hq,H,D,window", [(8192, 513, 64, 64, 128, 0), (8192, 257, 128, 128, 64, 0), (5000, 4100, 32, 8, 128, 0),
+                                               (4500, 700, 64, 32, 64, 3000), (40000, 256, 160, 160, 64, 0)])
+def test_long_sums(L, n, Hq, H, D, window, out):
+    """Values around 1 and scores near zero: what the sums over many tokens lose shows as a part of every result.  The tensor core cuts off
+    2^-23 of a sum at most with each product of 16 tokens.  FP32 results: sums of 8 steps of 64 tokens with two terms each, 64 2^-23 = 2^-17
+    at most, and less than that for all else.  bf16 results: L / 16 2^-23 = L 2^-27 at most; they are rounded by 2^-9 of themselves at
+    most, all in one direction if they are nearly equal, as here."""
+    page = 128
+    per = -(-L // page)
+    cache = binding.make_kv_cache(per, H, D, page)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    table = torch.arange(per, dtype=torch.int32, device="cuda").view(1, per)
+    for i in range(0, L, 4096):  # in parts: the inputs in 32 bits are large
+        m = min(4096, L - i)
+        k = torch.randn((m, H, D), generator=g, device="cuda").to(BF16)
+        v = (1 + 0.1 * torch.randn((m, H, D), generator=g, device="cuda")).to(BF16)
+        binding.kv_cache_write(cache, k, v, table, R.ints([i + m]), cu=R.ints([0, m]))
+    q = (0.2 * torch.randn((n, Hq, D), generator=g, device="cuda")).to(BF16)
+    got = binding.kv_attention(cache, q, table, R.ints([L]), cu=R.ints([0, n]), window=window, out_dtype=out)
+    heads = 2
+    codes, scale = cache.codes[:, :, :heads].contiguous(), cache.scale[:, :, :heads].contiguous()
+    G = Hq // H
+    ref, _, _ = R.attention(codes, scale, q[:, :heads * G].contiguous(), table, [L], [0, n], D ** -0.5, True, window)
+    got = got[:, :heads * G].to(R.F64)
+    shrunk = float(1 - got.sum() / ref.sum())
+    print(f"{out} {L}: {shrunk:.2e}, 2-norm {float((got - ref).norm() / ref.norm()):.2e}")
+    assert abs(shrunk) <= (2.0 ** -16 if out == F32 else L * 2.0 ** -27 + 2.0 ** -9)
+    if out == F32:
+        assert (got - ref).norm() <= 2.0 ** -16 * ref.norm()
