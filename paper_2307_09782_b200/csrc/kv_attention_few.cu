@@ -83,7 +83,8 @@ struct Cfg {
   static constexpr int kOffKeys = kFixed;
   static constexpr int kOffCodes = kOffKeys + kKeySlots * kTileBytes;
   static constexpr int kSmemBytes = kOffCodes + kValueSlots * kTileBytes;
-  static constexpr int kNumBars = 2 * kKeySlots + 2 * kValueSlots + 10 + 6 + 4 + 3 + 2 * kSegs;
+  // slots; six pairs from s_full to o_empty; q, l, meet and drain; g
+  static constexpr int kNumBars = 2 * kKeySlots + 2 * kValueSlots + 6 * 2 + 2 * 3 + 2 * 2 + 2 + 1 + 2 * kSegs;
   static_assert(kSmemBytes <= 227 * 1024 && kNumBars <= kMaxBars && kSlots >= 4 && kValueSlots <= 16, "shared memory");
   static_assert(256 + kOutBufs * kProbCols <= 512, "tensor memory");
 };

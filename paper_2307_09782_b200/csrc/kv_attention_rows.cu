@@ -79,9 +79,12 @@ struct Cfg {
   static constexpr int kOffRows = kOffScales + kScaleSlots * 8 * 16;        // [256] rows' factors
   static constexpr int kOffSegs = kOffRows + kRows * 4;
   static constexpr int kOffBars = kOffSegs + kSegs * 48;
-  static constexpr int kOffScan = kOffBars + 64 * 8;                        // [16 + 4] 64-bit words, then two of 32
+  static constexpr int kMaxBars = 64;
+  // slots; w; s, p and pv; q and r; e; g; drain
+  static constexpr int kNumBars = 2 * kKeySlots + 2 * kValueSlots + 2 * 2 + 3 * 4 + 3 + 2 * kScaleSlots + 2 * kSegs + 2;
+  static constexpr int kOffScan = kOffBars + kMaxBars * 8;                  // [16 + 4] 64-bit words, then two of 32
   static constexpr int kSmemBytes = kOffScan + 20 * 8 + 16;
-  static_assert(kSmemBytes <= 227 * 1024, "shared memory");
+  static_assert(kSmemBytes <= 227 * 1024 && kNumBars <= kMaxBars, "shared memory");
 };
 
 struct Seq {
