@@ -110,14 +110,12 @@ __device__ __forceinline__ void umma_f16(uint32_t d_tmem, uint64_t a_desc, uint6
 // layout: E4M3's exponent and mantissa bits moved into FP16's fields, which have one exponent bit more, whence the factor
 // (subnormal numbers come out right as well).  The hardware's conversion would do it at a quarter of the rate (a tile 1300 cycles
 // instead of about 500).  Codes are taken two and two as they lie in a word, so features 1 and 2 of every four change places
-// (feature_at).  The pattern of E4M3's NaN becomes 480 / 256: what nobody sees (a page that was not copied, say) must not turn
+// until the results are stored.  The pattern of E4M3's NaN becomes 480 / 256: what nobody sees (a page that was not copied, say) must not turn
 // into NaN by a product with zero.  Tokens from `valid` on become zeros, whatever the page holds there.  All of the share's codes
 // are loaded before the first store (the compiler cannot tell their addresses apart), kAtOnce pieces of 16 at a time.
 __device__ __forceinline__ uint2 widen4(uint32_t w) {
   return make_uint2(((w << 8) & 0x80008000u) | ((w << 7) & 0x3F803F80u), (w & 0x80008000u) | ((w >> 1) & 0x3F803F80u));
 }
-// The feature at position d of the widened values, and the other way round.
-__host__ __device__ __forceinline__ int feature_at(int d) { return (d & ~3) | ((d & 1) << 1) | ((d >> 1) & 1); }
 __device__ __forceinline__ uint4 widen8(uint32_t a, uint32_t b) {
   const uint2 x = widen4(a), y = widen4(b);
   return make_uint4(x.x, x.y, y.x, y.y);

@@ -886,7 +886,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
         fp8b::tmem_ld_wait32(o);
         if (EXACT && steps > C::kSumSteps) add_sum32(o, sum, r, d, carried(m_sum, m));
 #pragma unroll
-        for (int k = 0; k < 32; k += 4) {  // features in their places again (see feature_at)
+        for (int k = 0; k < 32; k += 4) {  // features 1 and 2 of every four change places again (see widen4)
           const float x = o[k + 1] * f;
           o[k] *= f;
           o[k + 1] = o[k + 2] * f;
