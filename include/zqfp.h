@@ -547,10 +547,12 @@ int zq_kv_cache_read(const uint8_t* codes, const float* scale, int64_t pages, in
  * Products take q as a sum of two 8-bit numbers (FP32 results: three) times a power of two for each row and head: features from
  * 2^-13 (2^-16) of the largest on are exact, smaller ones off by 2^-21 (2^-24) of the largest at most.  Scores, maxima and sums are
  * FP32; probabilities times their blocks' scales are rounded to 11 bits for bf16 results and to 22 for FP32 ones, and what is
- * below 2^-26 of the row's largest is lost.  FP32 results are off by 1e-6 to 3e-6 in all; in bf16 ones the sum over N tokens, which the
- * tensor core cuts off instead of rounding, is N 2^-27 of itself too small at most.  FP32 results of sequences
- * with few rows take two to four times as long as bf16 ones.  Scales of the values' blocks that a row sees lie within 2^60 of one
- * another.  The codes of a sequence's tokens are numbers (0x7F and 0xFF are none).  Results do not vary from run to run.
+ * below 2^-26 of the row's largest such product is lost.  FP32 results are off as FP32 arithmetic is (measured 1e-6 to 3e-6, 2-norm); in
+ * bf16 ones the sum over N tokens, which the tensor core cuts off instead of rounding, is N 2^-27 of itself too small at most.
+ * FP32 results of sequences with few rows take two to four times as long as bf16 ones.  The softmax sum lacks a token whose product
+ * is below 2^-134 of the row's largest: less than 2^-24 of the sum each as long as the values' scales that a row sees lie within 2^110
+ * of one another (those of zeros, 2^-64, and of values up to 2^54 do).  The codes of a sequence's tokens are numbers (0x7F and 0xFF
+ * are none).  Results do not vary from run to run.
  */
 size_t zq_kv_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D);
 int zq_kv_attention(const void* q_bf16, int64_t ldq, int64_t Hq, int64_t T, const int32_t* cu, int64_t B, const int32_t* lens,

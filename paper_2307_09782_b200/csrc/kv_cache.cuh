@@ -113,8 +113,8 @@ __device__ __forceinline__ int64_t block_at(const Cache& c, int page, int which,
 }
 
 // The scale a block needs whose largest absolute value has these bits (see fp8b::block_scale on bits and not finite values).
-// It is at least 2^-64, also where all is zero: scales of one sequence then differ by less than FP32's range, and a block that
-// is begun with zeros takes its scale from the first values that follow.
+// It is at least 2^-64, also where all is zero: it has an inverse, and a block that is begun with zeros takes its scale from the
+// first values that follow.  (The largest bf16 numbers need 2^119; how far apart the attention lets scales be says include/zqfp.h.)
 __device__ __forceinline__ float cache_scale(uint32_t amax_bits, bool pow2) {
   if (amax_bits >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
   float s = fmaxf(__fdiv_rn(__uint_as_float(amax_bits), 448.0f), 5.42101086242752217e-20f);

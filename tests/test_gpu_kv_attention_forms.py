@@ -90,7 +90,7 @@ def test_zero_and_extreme_blocks(case, out):
 
 
 @pytest.mark.parametrize("L,n,Hq,H,D,page", [(700, 1, 8, 2, 128, 64), (700, 5, 4, 2, 64, 16), (500, 300, 4, 2, 128, 32)])
-@pytest.mark.parametrize("size", [1.0, 2.0 ** 30])
+@pytest.mark.parametrize("size", [1.0, 2.0 ** 30, 2.0 ** 48])
 @TYPES
 def test_written_zeros_beside_values(L, n, Hq, H, D, page, size, out):
     """Padding: tokens whose values are zeros fill blocks (their scale is the smallest, 2^-64), the others' values are as large as `size`."""
