@@ -14,9 +14,8 @@
 //
 // The tensor core adds to an accumulator by cutting off (2^-23 of it at most for each product of 16 tokens; a tenth to a third of
 // that, measured), so a long sum shrinks: with two terms of P by 1e-5 to 4e-5 over 8192 tokens.  For FP32 results the row's warp
-// therefore adds it after kSumSteps steps, rounding to nearest, to a sum in the workspace (the place of the CTA's partial results that
-// the item has, or nobody yet), and the next product begins anew: 1e-6 to 3e-6 whatever the number of tokens, chunks of 777 tokens behind
-// others 331 -> 349 us (16 steps: twice that, 338 us).  bf16 results, with one term, are left as they are: N tokens take
+// therefore adds it after kSumSteps steps, rounding to nearest, to a sum in the workspace (the CTA's own, which the L2 keeps), and
+// the next product begins anew: 1e-6 to 3e-6 whatever the number of tokens, chunks of 777 tokens behind others 331 -> 349 us (16 steps: twice that, 338 us).  bf16 results, with one term, are left as they are: N tokens take
 // N 2^-27 at most, below their rounding of 2^-9 up to 2^18 tokens (and the loop is not the same: prompt of 8191 tokens 696 -> 745 us).
 //
 // All items (sequence, 256 rows, head) stand in a row, each as long as its tokens and what it costs to begin and end one, and every CTA
@@ -60,7 +59,8 @@ struct P {
   float* lse;
   int4* shared;    // [CTAs] the item that begins in the CTA and goes on in the next: sequence, number, 1 (0: none does); and of the
                    // item that came from the CTA before: 1 it goes on, 2 it ends here (0: none came)
-  float* partial;  // [CTAs][2: what came from the CTA before, what goes on][256 (D + 2)]: results (sum_at), then sums, then maxima
+  float* partial;  // [CTAs][2: what came from the CTA before, what goes on][256 (D + 2)]
+  float* sums;     // [CTAs][256 D] of the item at hand (sum_at)
   int* status;
 };
 
@@ -193,7 +193,7 @@ struct alignas(16) Seg {
 };
 static_assert(sizeof(Seg) == 48, "Seg");
 
-// Features d .. d + 3 of row r among the results of a place: rows side by side, as the threads are that have them.
+// Features d .. d + 3 of row r in a sum: rows side by side, as the threads are that have them.
 __device__ __forceinline__ int64_t sum_at(int r, int d) { return (static_cast<int64_t>(d >> 2) * kRows + r) * 4; }
 
 struct Ring {
@@ -804,7 +804,6 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       const int lo = mine && p.window > 0 ? static_cast<int>(max(pos + 1 - p.window, static_cast<int64_t>(0))) : 0;
       const int hi_all = __reduce_min_sync(0xFFFFFFFFu, hi), lo_all = __reduce_max_sync(0xFFFFFFFFu, lo);
       float m = -INFINITY, l = 0.0f, m_sum = -INFINITY;  // m_sum: the reference of the sum in the workspace
-      auto place = [&] { return p.partial + static_cast<int64_t>(part >= 0 ? part : 2 * blockIdx.x + 1) * (kRows * (D + 2)); };
       if (!fp8b::mbar_wait_all(q_full, items & 1, s_abort)) {
         failed = true;
         break;
@@ -853,7 +852,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
               break;
             }
             tc_fence_after_sync();
-            add_to_sum<D>(to, place(), r, begin > C::kSumSteps, carried(m_sum, m));
+            add_to_sum<D>(to, p.sums + static_cast<int64_t>(blockIdx.x) * (kRows * D), r, begin > C::kSumSteps, carried(m_sum, m));
             m_sum = m;
           }
           for (int st = begin; st < min(steps, begin + C::kSumSteps) && !failed; ++st) failed = !step(st, st == begin);
@@ -870,11 +869,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
         break;
       }
       tc_fence_after_sync();
-      float* sum = place();
+      float* to_part = part < 0 ? nullptr : p.partial + static_cast<int64_t>(part) * (kRows * (D + 2));
       const int hq = h * p.G + row % p.G;
       if (part >= 0) {
-        sum[kRows * D + r] = l;
-        sum[kRows * D + kRows + r] = m;
+        to_part[kRows * D + r] = l;
+        to_part[kRows * D + kRows + r] = m;
       } else if (mine && p.lse) {
         p.lse[t * (static_cast<int64_t>(p.G) * p.c.H) + hq] = l == 0.0f ? -INFINITY : (log2f(l) + m + 8.0f - kShift) * (1.0f / kLog2e);
       }
@@ -884,7 +883,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
         float o[32];
         fp8b::tmem_ld32(to + d, o);
         fp8b::tmem_ld_wait32(o);
-        if (EXACT && steps > C::kSumSteps) add_sum32(o, sum, r, d, carried(m_sum, m));
+        if (EXACT && steps > C::kSumSteps) add_sum32(o, p.sums + static_cast<int64_t>(blockIdx.x) * (kRows * D), r, d, carried(m_sum, m));
 #pragma unroll
         for (int k = 0; k < 32; k += 4) {  // features 1 and 2 of every four change places again (see widen4)
           const float x = o[k + 1] * f;
@@ -895,7 +894,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
         }
         if (part >= 0) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) *reinterpret_cast<float4*>(sum + sum_at(r, d + 4 * k)) = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+          for (int k = 0; k < 8; ++k) *reinterpret_cast<float4*>(to_part + r * D + d + 4 * k) = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
         } else if (mine) {
           store16(p, t * p.ldo + static_cast<int64_t>(hq) * D + d, o);
           store16(p, t * p.ldo + static_cast<int64_t>(hq) * D + d + 16, o + 16);
@@ -963,7 +962,7 @@ __global__ void __launch_bounds__(256) attention_join_rows_kernel(const P p, int
     const float f = s_w[warp][i - x];
     if (f == 0.0f) continue;  // (what lies there is nothing)
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(f, load_chained(piece(i) + sum_at(r, e * 32 + lane) + (lane & 3)), o[e]);
+    for (int e = 0; e < E; ++e) o[e] = fmaf(f, load_chained(piece(i) + r * D + e * 32 + lane), o[e]);
   }
   const int64_t t = s.first + (row0 + r) / p.G;
   const int hq = h * p.G + static_cast<int>((row0 + r) % p.G);
@@ -1008,7 +1007,7 @@ bool make_query_map(CUtensorMap* m, const AttnArgs& a, int G) {
 }  // namespace
 
 // (the same place as the other kernel's: the kernels of a call run one after the other)
-size_t rows_workspace_bytes(int64_t D) { return sizeof(float) * kMaxCtas * 2 * kRows * (D + 2) + sizeof(int4) * kMaxCtas; }
+size_t rows_workspace_bytes(int64_t D) { return sizeof(float) * kMaxCtas * kRows * (2 * (D + 2) + D) + sizeof(int4) * kMaxCtas; }
 
 int launch_attention_rows(const AttnArgs& a, cudaStream_t st) {
   P p{};
@@ -1021,6 +1020,7 @@ int launch_attention_rows(const AttnArgs& a, cudaStream_t st) {
   p.status = reinterpret_cast<int*>(ws);
   p.shared = reinterpret_cast<int4*>(ws + kWsHeadBytes);
   p.partial = reinterpret_cast<float*>(p.shared + kMaxCtas);
+  p.sums = p.partial + static_cast<int64_t>(kMaxCtas) * 2 * kRows * (a.c.D + 2);
   CUtensorMap tm, tm_q{};
   // a tile's queries as two boxes where whole tokens fill it and a token's stride is one of whole heads
   p.boxes = kTok % p.G == 0 && a.ldq % a.c.D == 0 ? 1 : 0;
