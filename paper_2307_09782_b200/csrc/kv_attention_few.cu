@@ -570,7 +570,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_few_kernel(const __grid
               tmem_ld_wait_regs<S>(x[k] + r);
               tmem_ld_wait_regs<S>(y);
 #pragma unroll
-              for (int i = 0; i < S; ++i) x[k][r + i] = fmaf(fmaf(y[i], 1.0f / (1 << kRestBits), x[k][r + i]), info[r + i].x * e.x, e.y);
+              for (int i = 0; i < S; i += 2) {
+                float a, b;
+                unpack2(fma2(pack2(y[i], y[i + 1]), fp8b::twice(1.0f / (1 << kRestBits)), pack2(x[k][r + i], x[k][r + i + 1])), a, b);
+                x[k][r + i] = fmaf(a, info[r + i].x * e.x, e.y);
+                x[k][r + i + 1] = fmaf(b, info[r + i + 1].x * e.x, e.y);
+              }
             }
             // all of the tile is seen by all rows (the first row sees the fewest behind, the last the fewest before)
             if (!(tile + (kTok - 1) <= seen_to && tile >= seen_from)) {
