@@ -549,7 +549,9 @@ int zq_kv_cache_read(const uint8_t* codes, const float* scale, int64_t pages, in
  * FP32; probabilities times their blocks' scales are rounded to 11 bits for bf16 results and to 22 for FP32 ones, and what is
  * below 2^-26 of the row's largest such product is lost.  FP32 results are off as FP32 arithmetic is (measured 1e-6 to 3e-6, 2-norm); in
  * bf16 ones the sum over N tokens, which the tensor core cuts off instead of rounding, is N 2^-27 of itself too small at most.
- * FP32 results of sequences with few rows take two to four times as long as bf16 ones.  The softmax sum lacks a token whose product
+ * FP32 results of sequences with few rows (new tokens x Hq / H, up to 64) take up to five times as long as bf16 ones.  With cu the
+ * host knows the rows of a sequence only as T * Hq / H at most and chooses by that: 64 sequences of one token each, Hq / H = 4, take
+ * four times as long with cu = 0 .. 64 as with NULL, which says the same.  The softmax sum lacks a token whose product
  * is below 2^-134 of the row's largest: less than 2^-24 of the sum each as long as the values' scales that a row sees lie within 2^110
  * of one another (those of zeros, 2^-64, and of values up to 2^54 do).  The codes of a sequence's tokens are numbers (0x7F and 0xFF
  * are none).  Results do not vary from run to run.

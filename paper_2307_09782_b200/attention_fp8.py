@@ -43,7 +43,8 @@ class AttentionFp8:
     def forward(self, x: torch.Tensor, cache: Fp8KvCache, pages: torch.Tensor, lens: torch.Tensor, positions: torch.Tensor, *,
                 cu: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16) -> torch.Tensor:
         """x bf16 [T, K], the new tokens of B sequences -> [T, K_out].  ``pages`` int32 [B, pages of a sequence], ``lens`` int32 [B]: tokens
-        with the new ones, ``cu`` int32 [B + 1]: the sequences' rows (without it one new token each), ``positions`` int32 [T]."""
+        with the new ones, ``cu`` int32 [B + 1]: the sequences' rows (without it one new token each, which is faster), ``positions``
+        int32 [T].  Rows from cu[B] on are padding: only the projections work on them, and what comes out for them means nothing."""
         T, Hq, H = x.shape[0], self.Hq, self.H
         qkv = binding.fp8_block_linear(self.qkv, x=x, mode=self.mode, out_dtype=torch.bfloat16).view(T, Hq + 2 * H, self.D)
         q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + H], qkv[:, Hq + H:]

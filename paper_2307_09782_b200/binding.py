@@ -986,7 +986,7 @@ def kv_attention(cache: Fp8KvCache, q: torch.Tensor, table: torch.Tensor, lens: 
                  sm_scale: Optional[float] = None, causal: bool = True, window: int = 0, out_dtype=torch.bfloat16, out=None,
                  lse: bool = False, workspace: Optional[torch.Tensor] = None):
     """Attention of the new tokens' queries, bf16 [T, Hq, D], over the cache -> [T, Hq, D].  ``table``, ``lens``, ``cu`` as
-    :func:`kv_cache_write`; ``sm_scale``: 1 / sqrt(D) unless given; ``window``: how many of the last positions a token sees (0:
+    :func:`kv_cache_write` (one new token each: without ``cu`` is faster); rows from cu[B] on are not written; ``sm_scale``: 1 / sqrt(D) unless given; ``window``: how many of the last positions a token sees (0:
     all).  With ``lse`` also the logarithms of the softmax sums, float32 [T, Hq]."""
     ldq, T, Hq, D = _heads(q, "q")
     if D != cache.D or Hq % cache.H or Hq == 0:

@@ -15,8 +15,9 @@
 // The tensor core adds to an accumulator by cutting off (2^-23 of it at most for each product of 16 tokens; a tenth to a third of
 // that, measured), so a long sum shrinks: with two terms of P by 1e-5 to 4e-5 over 8192 tokens.  For FP32 results the row's warp
 // therefore adds it after kSumSteps steps, rounding to nearest, to a sum in the workspace (the CTA's own, which the L2 keeps), and
-// the next product begins anew: 1e-6 to 3e-6 whatever the number of tokens, chunks of 777 tokens behind others 331 -> 349 us (16 steps: twice that, 338 us).  bf16 results, with one term, are left as they are: N tokens take
-// N 2^-27 at most, below their rounding of 2^-9 up to 2^18 tokens (and the loop is not the same: prompt of 8191 tokens 696 -> 745 us).
+// the next product begins anew: 1e-6 to 3e-6 whatever the number of tokens, chunks of 777 tokens behind others 331 -> 343 us (16 steps:
+// twice the error).  bf16 results, with one term, are left as they are: N tokens take N 2^-27 at most, below their rounding of 2^-9
+// up to 2^18 tokens (and the loop would not be the same: prompt of 8191 tokens 696 -> 745 us).
 //
 // All items (sequence, 256 rows, head) stand in a row, each as long as its tokens and what it costs to begin and end one, and every CTA
 // gets an equal part of the row (whole items in rounds: a prompt of 8191 tokens 732 us instead of 655).  An item that reaches over a

@@ -205,3 +205,23 @@ def test_several_rounds_of_blocks_per_cta(B, H, D, page, mode):
         assert torch.equal(simple[0], expect[0]) and same_scales(simple[1], expect[1])
     binding.kv_cache_write(binding.Fp8KvCache(codes, scale), k, v, table, R.ints(lens), cu=R.ints(cu), mode=mode)
     assert torch.equal(codes, expect[0]) and same_scales(scale, expect[1])
+
+
+# ---- the layer ----------------------------------------------------------------------------------------------------------
+def test_padding_of_a_batch_reaches_nobody():
+    """Rows behind the last sequence, whatever they hold: the others' results and the cache are the same."""
+    from test_gpu_kv_attention_calls import block, inputs
+
+    b, new = block(), [40, 1, 70]
+    pages = torch.arange(30, dtype=torch.int32, device="cuda").view(3, 10)
+    results = []
+    for fill in (0.0, math.nan, 1e30):
+        cache = b.new_cache(30, 16)
+        x = inputs(128)
+        x[111:] = fill
+        positions = torch.cat([torch.arange(n) for n in new] + [torch.full((17,), -1 if fill else 0)]).to(torch.int32).cuda()
+        y = b.forward(x, cache, pages, R.ints(new), positions, cu=R.ints([0, 40, 41, 111]))
+        results.append((y[:111].clone(), cache.codes, cache.scale))
+    for other in results[1:]:
+        assert all(torch.equal(a, o) for a, o in zip(results[0], other))
+    assert not results[0][0].isnan().any()
