@@ -139,6 +139,26 @@ def test_nan_blocks(case, what, out):
     assert ((got.to(R.F64) - ref).abs() <= tolerance(ref, bound, out))[~hit].all()
 
 
+@pytest.mark.parametrize("case", [([300, 200], [5, 1], 8, 2, 128, 64, True, 0), ([300, 200], [90, 70], 8, 2, 128, 64, True, 0),
+                                  ([3000, 200], [40, 33], 10, 2, 64, 32, True, 0), ([1500, 300], [1200, 300], 4, 4, 64, 16, True, 0)])
+@TYPES
+def test_not_finite_queries(case, out):
+    """A query that is not finite gives NaN in its own row and head only."""
+    lens, new, Hq, H, D, page, causal, window = case
+    codes, scale, table, lens, cu = R.batch(lens, new, H, D, page)
+    q = R.heads(cu[-1], Hq, D, 7)
+    args = (binding.Fp8KvCache(codes, scale), q, table, R.ints(lens))
+    good, sums = binding.kv_attention(*args, cu=R.ints(cu), out_dtype=out, lse=True)
+    bad = [(2, 3, 9, math.nan), (cu[-1] - 1, 0, 0, math.inf), (0, 1, D - 1, -math.inf)]
+    hit = torch.zeros((cu[-1], Hq), dtype=torch.bool, device="cuda")
+    for t, h, d, value in bad:
+        q[t, h, d] = value
+        hit[t, h] = True
+    got, lse = binding.kv_attention(*args, cu=R.ints(cu), out_dtype=out, lse=True)
+    assert got[hit].isnan().all() and lse[hit].isnan().all()
+    assert torch.equal(got[~hit], good[~hit]) and torch.equal(lse[~hit], sums[~hit])
+
+
 @pytest.mark.parametrize("case", [ATTN_CASES[0], ATTN_CASES[2], ATTN_CASES[8], ATTN_CASES[11], ATTN_CASES[12],
                                   ([5000], [1], 8, 2, 128, 64, True, 0), ([3000], [40], 8, 2, 128, 64, True, 0)])
 def test_results_in_the_place_of_queries(case):
